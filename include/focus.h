@@ -66,6 +66,26 @@ typedef struct {
     int64_t stride_n;
 } focus_tensor;
 
+/* The rotation of query and key heads by their positions (focus_qk_norm_rope). */
+typedef struct {
+    int32_t rotary;       /* leading dimensions of a head that are rotated: even, 0 (none) to D */
+    int32_t interleaved;  /* 0: dimension i is paired with i + rotary/2; 1: 2i with 2i + 1 */
+    float amplitude;      /* factor on every cosine and sine (some long-context scalings have one); 0 selects 1 */
+    float eps;            /* >= 0, added to the mean square of a head vector before the root */
+} focus_rope;
+
+/* A cache of keys and values in 4 bits, in pages (focus_kv4_append and the entry points after it). */
+typedef struct {
+    void* pages;           /* device, num_pages * focus_kv4_page_bytes(shape, page_tokens) bytes, 16-byte aligned */
+    const int32_t* table;  /* device int32 [batch, max_pages]: the page of tokens p*page_tokens .. of a sequence */
+    const int32_t* lens;   /* device int32 [batch]: tokens of each sequence */
+    int32_t num_pages;
+    int32_t page_tokens;   /* tokens per page: 16, 32, 64, 128 or 256 */
+    int32_t max_pages;     /* row length of the table */
+    float k_scale;         /* powers of two from 2^-16 to 2^16 that keys and values are divided by before they are coded */
+    float v_scale;
+} focus_kv4;
+
 /* Tile sizes of the summaries written by focus_build_tiles (fixed by the ABI). */
 #define FOCUS_TILE_M 128
 #define FOCUS_TILE_N 128
@@ -271,6 +291,110 @@ FOCUS_API size_t focus_decode_workspace_bytes(const focus_shape* shape);
 FOCUS_API int focus_decode_step(const focus_shape* shape, focus_tensor q, focus_tensor k, focus_tensor v,
                                 const uint32_t* mq_new, const uint32_t* mk, focus_tensor o, float* lse, void* ws,
                                 size_t ws_bytes, void* stream);
+
+/*
+ * focus_qk_norm_rope -- what comes between the projections of a layer and focus_assign / focus_attn_fwd in most models (the
+ * paper takes finished queries and keys): every query and key head is normalised on its own (root mean square, times a weight per
+ * dimension) and its leading `rotary` dimensions are rotated by its token's position, in one pass.
+ *     y = x (mean x^2 + eps)^(-1/2) w;   pair (a, b) of frequency i -> amplitude (a cos t - b sin t, a sin t + b cos t),
+ *     t = position * freq[i]
+ *   shape       batch, Hq, Hkv, n, D are read
+ *   q, k        device bf16 [batch, Hq, n, D], [batch, Hkv, n, D]; 16-byte aligned, strides multiples of 8 (token-major views of a
+ *               projection's output are as good as head-major ones)
+ *   wq, wk      device fp32 [D], 4-byte aligned; NULL: the heads are rotated without a norm
+ *   freq        device fp64 [rotary/2], angle per position (focus_rope_frequencies); may be NULL when rotary is 0
+ *   positions   device int32 [batch, n]; NULL: 0, 1, ..., n-1 in every sequence
+ *   q_out, k_out  as q, k; may be q, k themselves, and must not overlap them otherwise
+ * fp32 arithmetic on the bf16 inputs, angles reduced in fp64, one rounding to bf16 at the end.
+ *
+ * focus_qk_norm_rope_bwd -- its derivative: from the gradients of q_out and k_out those of q, k and of the weights.
+ *   q, k, wq, wk, freq, positions   as in the forward call (the vectors before the norm)
+ *   dq_out, dk_out  gradients of the results, like q, k          dq, dk   device bf16, written; may be dq_out, dk_out themselves
+ *   dwq, dwk    device fp32 [D], overwritten; NULL exactly where wq, wk are.  Sums over all rows in fp32, in an order that depends on
+ *               the shape alone (the same bits in every call)
+ *   ws          device scratch of focus_qk_norm_rope_bwd_workspace_bytes(shape) bytes, 16-byte aligned
+ *
+ * focus_rope_frequencies -- host only: freq_out (host, rotary/2 doubles): base^(-2i/rotary), for contexts beyond `trained` tokens
+ *   FOCUS_ROPE_LINEAR   divided by factor
+ *   FOCUS_ROPE_BASE     with base * factor^(rotary/(rotary-2)) in the place of base
+ *   FOCUS_ROPE_PARTS    divided by factor where a pair turns fewer than `low` times over `trained` tokens, kept where it turns more than
+ *                       `high` times, in between in proportion (arXiv 2309.00071, Sec. 3.2); amplitude_out = 0.1 ln(factor) + 1 (its Sec. 3.4)
+ *   amplitude_out (nullable) is 1 in the other cases.
+ */
+#define FOCUS_ROPE_PLAIN 0
+#define FOCUS_ROPE_LINEAR 1
+#define FOCUS_ROPE_BASE 2
+#define FOCUS_ROPE_PARTS 3
+FOCUS_API int focus_rope_frequencies(int32_t rotary, double base, int32_t scaling, double factor, double low, double high, double trained,
+                                     double* freq_out, float* amplitude_out);
+FOCUS_API int focus_qk_norm_rope(const focus_shape* shape, const focus_rope* rope, focus_tensor q, focus_tensor k, const float* wq,
+                                 const float* wk, const double* freq, const int32_t* positions, focus_tensor q_out, focus_tensor k_out,
+                                 void* stream);
+FOCUS_API size_t focus_qk_norm_rope_bwd_workspace_bytes(const focus_shape* shape);
+FOCUS_API int focus_qk_norm_rope_bwd(const focus_shape* shape, const focus_rope* rope, focus_tensor q, focus_tensor k, const float* wq,
+                                     const float* wk, const double* freq, const int32_t* positions, focus_tensor dq_out,
+                                     focus_tensor dk_out, focus_tensor dq, focus_tensor dk, float* dwq, float* dwk, void* ws,
+                                     size_t ws_bytes, void* stream);
+
+/*
+ * The 4-bit cache: keys, values and key masks of a layer in pages, for sequences of their own lengths.
+ *
+ * A page holds page_tokens tokens of all KV heads: [Hkv][page_tokens] rows of D bytes (codes of the key, then of the value, two
+ * dimensions a byte, the even one in the low bits), [Hkv][page_tokens] rows of D/8 bytes (scales of blocks of 16 dimensions, key then
+ * value), [Hkv][page_tokens] uint32 masks.  A code is a sign (8) and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (0..7); a scale is an 8-bit
+ * float with four exponent and three fraction bits; the number is code * scale * k_scale (v_scale).  Coding: with x' = x / k_scale, the
+ * scale is min(amax' / 6, 448) of its block and the code x' / scale, both to nearest, ties to even, codes beyond 6 to 6 (exact: the
+ * scales on top are powers of two).  A token whose key or value of a head holds an infinity or a NaN is stored as NaN throughout for
+ * that head.
+ *
+ * `lens` counts the tokens of a sequence with the new ones of a call among them, as focus_decode_step's n does: the caller sets it (and
+ * the pages in `table`) before it appends.  Entries of `table` behind a sequence's last page are not read.  Sequences may share pages
+ * that none of them writes to.
+ *   dev_status  device int32[4], nullable, zeroed by the caller: [0] stays 0 on success.  1: an entry of `table` that is no page ([1]
+ *               sequence, [2] place in its row, [3] the entry); 2: a length that cannot be ([1] sequence, [2] its entry of lens, [3] the
+ *               count, the first token or the bound it does not agree with); 3: a pair of pages that are not both in the pool ([1] pair,
+ *               [2] source, [3] destination).  What is wrong is left out: its tokens are not written, read or attended, a sequence of an
+ *               impossible length counts as empty.
+ *
+ * focus_kv4_page_bytes -- host only: Hkv * page_tokens * (D + D/8 + 4); 0 on bad arguments.
+ *
+ * focus_kv4_append -- the last tokens of every sequence go into its pages: token t < counts[b] of sequence b becomes token
+ * lens[b] - counts[b] + t.
+ *   shape       n = new tokens per sequence at most; batch, Hkv, D are read
+ *   k, v        device bf16 [batch, Hkv, n, D], 16-byte aligned, strides multiples of 8       mk   device uint32 [batch*Hkv, n]
+ *   counts      device int32 [batch], 0 to n; NULL: n for every sequence
+ *
+ * focus_kv4_read -- the way back: tokens first[b] .. first[b] + n - 1 of every sequence as bf16 (exact), for a pass of focus_attn_fwd over
+ * a cached prefix.  Rows behind the last token of a sequence are left as they were.
+ *   shape       n = tokens per sequence; batch, Hkv, D are read
+ *   first       device int32 [batch]; NULL: 0     k, v  device bf16 [batch, Hkv, n, D], written     mk  device uint32 [batch*Hkv, n] or NULL
+ *
+ * focus_kv4_copy_pages -- page src[i] to page dst[i], all heads: a sequence forked, a pool compacted.  Device lists of `count` pages; no
+ * page may be destination twice, nor source and destination of different pairs (the result is then undefined, but within the pool).
+ *   shape       Hkv and D are read            cache   pages, num_pages and page_tokens are read (table and lens may be NULL)
+ */
+FOCUS_API size_t focus_kv4_page_bytes(const focus_shape* shape, int32_t page_tokens);
+FOCUS_API int focus_kv4_append(const focus_shape* shape, const focus_kv4* cache, focus_tensor k, focus_tensor v, const uint32_t* mk,
+                               const int32_t* counts, int32_t* dev_status, void* stream);
+FOCUS_API int focus_kv4_read(const focus_shape* shape, const focus_kv4* cache, const int32_t* first, focus_tensor k, focus_tensor v,
+                             uint32_t* mk, int32_t* dev_status, void* stream);
+FOCUS_API int focus_kv4_copy_pages(const focus_shape* shape, const focus_kv4* cache, const int32_t* src, const int32_t* dst, int32_t count,
+                                   int32_t* dev_status, void* stream);
+
+/*
+ * focus_kv4_decode_step -- focus_decode_step over the 4-bit cache: one new token per sequence (position lens[b]-1, appended before) as
+ * the only query, sequences of their own lengths.  Key j is attended iff lens[b]-1-j <= window or mq_new[b*Hq+h] & mask(j) != 0; exact
+ * softmax over the attended keys, on the numbers that the codes stand for.  Products of fp16 operands (Q with a power of two per head;
+ * probabilities with 11 significant bits), fp32 accumulation.  An empty sequence has o = 0 and lse = -inf.
+ *   shape       n = the longest length that `lens` may hold, at most max_pages * page_tokens; Hq / Hkv <= 8, batch <= 1024
+ *   q, o        device bf16 [batch, Hq, D] (stride_n ignored; q 4-byte aligned with even strides)
+ *   mq_new      device uint32 [batch*Hq]           lse   device fp32 [batch*Hq], natural log
+ *   ws          device scratch of focus_kv4_decode_workspace_bytes(shape) bytes (the same for every n), 16-byte aligned; contents need
+ *               not be preserved between calls, calls that may overlap need one each
+ */
+FOCUS_API size_t focus_kv4_decode_workspace_bytes(const focus_shape* shape);
+FOCUS_API int focus_kv4_decode_step(const focus_shape* shape, const focus_kv4* cache, focus_tensor q, const uint32_t* mq_new, focus_tensor o,
+                                    float* lse, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
 
 /*
  * focus_count_kept -- exact number of attended pairs per query head (the denominator-free

@@ -5,6 +5,7 @@ fallback: loading fails loudly when the library has not been built (``python -m 
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import warnings
 
@@ -21,6 +22,10 @@ FOCUS_LAYOUT_AUTO = 2
 FOCUS_LAYOUT_SORTED_LOCAL = 3
 FOCUS_LAYOUT_GROUP_MAJOR = 4
 FOCUS_MAX_CLASSES = 64
+FOCUS_ROPE_PLAIN = 0
+FOCUS_ROPE_LINEAR = 1
+FOCUS_ROPE_BASE = 2
+FOCUS_ROPE_PARTS = 3
 
 
 class focus_shape(C.Structure):
@@ -46,6 +51,15 @@ class focus_tiles_layout(C.Structure):
                 ("qrange", C.c_size_t), ("order", C.c_size_t), ("gbits_s", C.c_size_t), ("qs", C.c_size_t), ("ks", C.c_size_t),
                 ("vs", C.c_size_t), ("scratch", C.c_size_t), ("o_sorted", C.c_size_t), ("o_local", C.c_size_t),
                 ("lse_local", C.c_size_t)]
+
+
+class focus_rope(C.Structure):
+    _fields_ = [("rotary", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_float), ("eps", C.c_float)]
+
+
+class focus_kv4(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("table", C.c_void_p), ("lens", C.c_void_p), ("num_pages", C.c_int32), ("page_tokens", C.c_int32),
+                ("max_pages", C.c_int32), ("k_scale", C.c_float), ("v_scale", C.c_float)]
 
 
 class FocusError(RuntimeError):
@@ -102,6 +116,28 @@ def lib():
         L.focus_sinkhorn_bwd.argtypes = [SP, vp, f32, i32, vp, sz, vp, vp, vp]
         L.focus_gate_attn_fwd.restype = C.c_int
         L.focus_gate_attn_fwd.argtypes = [SP, focus_tensor, focus_tensor, focus_tensor, vp, f32, focus_tensor, vp, vp, vp]
+        RP, KP, ft = C.POINTER(focus_rope), C.POINTER(focus_kv4), focus_tensor
+        f64 = C.c_double
+        L.focus_rope_frequencies.restype = C.c_int
+        L.focus_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp, C.POINTER(f32)]
+        L.focus_qk_norm_rope.restype = C.c_int
+        L.focus_qk_norm_rope.argtypes = [SP, RP, ft, ft, vp, vp, vp, vp, ft, ft, vp]
+        L.focus_qk_norm_rope_bwd_workspace_bytes.restype = sz
+        L.focus_qk_norm_rope_bwd_workspace_bytes.argtypes = [SP]
+        L.focus_qk_norm_rope_bwd.restype = C.c_int
+        L.focus_qk_norm_rope_bwd.argtypes = [SP, RP, ft, ft, vp, vp, vp, vp, ft, ft, ft, ft, vp, vp, vp, sz, vp]
+        L.focus_kv4_page_bytes.restype = sz
+        L.focus_kv4_page_bytes.argtypes = [SP, i32]
+        L.focus_kv4_append.restype = C.c_int
+        L.focus_kv4_append.argtypes = [SP, KP, ft, ft, vp, vp, vp, vp]
+        L.focus_kv4_read.restype = C.c_int
+        L.focus_kv4_read.argtypes = [SP, KP, vp, ft, ft, vp, vp, vp]
+        L.focus_kv4_copy_pages.restype = C.c_int
+        L.focus_kv4_copy_pages.argtypes = [SP, KP, vp, vp, i32, vp, vp]
+        L.focus_kv4_decode_workspace_bytes.restype = sz
+        L.focus_kv4_decode_workspace_bytes.argtypes = [SP]
+        L.focus_kv4_decode_step.restype = C.c_int
+        L.focus_kv4_decode_step.argtypes = [SP, KP, ft, vp, ft, vp, vp, sz, vp, vp]
         L.focus_count_kept.restype = C.c_int
         L.focus_count_kept.argtypes = [SP, vp, vp, vp, vp]
         L.focus_count_kept_noalloc.restype = C.c_int
@@ -255,6 +291,127 @@ def focus_decode_step(shape, q, k, v, mq_new, mk, o, lse, ws, stream=None):
         rc = lib().focus_decode_step(C.byref(shape), vec_arg(q), tensor_arg(k), tensor_arg(v), _p(mq_new), _p(mk), vec_arg(o),
                                      _p(lse), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
     _check(rc)
+
+
+def _dev(t, dtype, *shape):
+    """the tensor, checked: on the GPU, of this type, contiguous, of this many elements"""
+    assert t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.numel() == math.prod(shape), (t.dtype, tuple(t.shape), t.stride(), shape)
+    return t.data_ptr()
+
+
+def _opt(t, dtype, *shape):
+    return None if t is None else _dev(t, dtype, *shape)
+
+
+def _heads(t, shape, H, n=None):
+    """tensor_arg of a [batch, H, n, D] tensor (or [H, n, D] for one sequence), with its sizes checked"""
+    n = shape.n if n is None else n
+    assert tuple(t.shape) == (shape.batch, H, n, shape.D) or (shape.batch == 1 and tuple(t.shape) == (H, n, shape.D)), (tuple(t.shape), (shape.batch, H, n, shape.D))
+    st = t.stride()
+    assert t.is_cuda and t.dtype is torch.bfloat16 and st[-1] == 1
+    # (the stride of a dimension of one element is any number: not used)
+    sb, sh, sn = (st[0] if len(st) == 4 and shape.batch > 1 else 0), (st[-3] if H > 1 else shape.D), (st[-2] if n > 1 else shape.D)
+    return focus_tensor(t.data_ptr(), sb, sh, sn)
+
+
+def _vecs(t, shape, H):
+    """the argument for [batch, H, D] query or output vectors (or [H, D] for one sequence)"""
+    assert tuple(t.shape) == (shape.batch, H, shape.D) or (shape.batch == 1 and tuple(t.shape) == (H, shape.D)), (tuple(t.shape), (shape.batch, H, shape.D))
+    st = t.stride()
+    assert t.is_cuda and t.dtype is torch.bfloat16 and st[-1] == 1
+    return focus_tensor(t.data_ptr(), st[0] if len(st) == 3 and shape.batch > 1 else 0, st[-2] if H > 1 else shape.D, shape.D)
+
+
+def make_rope(rotary, interleaved=False, amplitude=1.0, eps=1e-6) -> focus_rope:
+    return focus_rope(rotary, int(interleaved), amplitude, eps)
+
+
+def focus_rope_frequencies(rotary, base=10000.0, scaling=FOCUS_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, trained=1.0, device="cuda"):
+    """(float64 tensor [rotary/2] on `device`, amplitude)"""
+    out, amplitude = (C.c_double * (max(0, rotary) // 2 + 1))(), C.c_float()
+    _check(lib().focus_rope_frequencies(rotary, base, scaling, factor, low, high, trained, C.cast(out, C.c_void_p), C.byref(amplitude)))
+    return torch.tensor(out[:rotary // 2], dtype=torch.float64, device=device), amplitude.value
+
+
+def focus_qk_norm_rope(shape, rope, q, k, wq, wk, freq, positions, q_out, k_out, stream=None):
+    """q, q_out bf16 [batch, Hq, n, D], k, k_out [batch, Hkv, n, D] (any strides with D contiguous; the outputs may be the inputs);
+    wq, wk fp32 [D] or None; freq fp64 [rotary/2]; positions int32 [batch, n] or None"""
+    D, B, n = shape.D, shape.batch, shape.n
+    _check(lib().focus_qk_norm_rope(C.byref(shape), C.byref(rope), _heads(q, shape, shape.Hq), _heads(k, shape, shape.Hkv), _opt(wq, torch.float32, D),
+                                    _opt(wk, torch.float32, D), _opt(freq, torch.float64, rope.rotary // 2), _opt(positions, torch.int32, B, n),
+                                    _heads(q_out, shape, shape.Hq), _heads(k_out, shape, shape.Hkv), _stream(stream)))
+
+
+def focus_qk_norm_rope_bwd_workspace_bytes(shape) -> int:
+    return int(lib().focus_qk_norm_rope_bwd_workspace_bytes(C.byref(shape)))
+
+
+def focus_qk_norm_rope_bwd(shape, rope, q, k, wq, wk, freq, positions, dq_out, dk_out, dq, dk, dwq, dwk, ws, stream=None):
+    """gradients dq, dk (bf16, like q and k; may be dq_out, dk_out) and dwq, dwk (fp32 [D]; None where the weight is) from those of the
+    results; ws uint8 scratch"""
+    D, B, n = shape.D, shape.batch, shape.n
+    _check(lib().focus_qk_norm_rope_bwd(C.byref(shape), C.byref(rope), _heads(q, shape, shape.Hq), _heads(k, shape, shape.Hkv),
+                                        _opt(wq, torch.float32, D), _opt(wk, torch.float32, D), _opt(freq, torch.float64, rope.rotary // 2),
+                                        _opt(positions, torch.int32, B, n), _heads(dq_out, shape, shape.Hq), _heads(dk_out, shape, shape.Hkv),
+                                        _heads(dq, shape, shape.Hq), _heads(dk, shape, shape.Hkv), _opt(dwq, torch.float32, D),
+                                        _opt(dwk, torch.float32, D), _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def focus_kv4_page_bytes(shape, page_tokens) -> int:
+    return int(lib().focus_kv4_page_bytes(C.byref(shape), page_tokens))
+
+
+def make_kv4(pages, page_tokens, table=None, lens=None, k_scale=1.0, v_scale=1.0) -> focus_kv4:
+    """pages uint8 [num_pages, focus_kv4_page_bytes]; table int32 [batch, max_pages]; lens int32 [batch].  The struct holds the tensors."""
+    assert pages.is_cuda and pages.dtype is torch.uint8 and pages.dim() == 2 and pages.is_contiguous()
+    assert (table is None) == (lens is None)
+    if table is not None:
+        assert table.is_cuda and table.dtype is torch.int32 and table.dim() == 2 and table.is_contiguous()
+        assert lens.is_cuda and lens.dtype is torch.int32 and lens.dim() == 1 and lens.is_contiguous() and lens.shape[0] == table.shape[0]
+    c = focus_kv4(pages.data_ptr(), _p(table), _p(lens), pages.shape[0], page_tokens, table.shape[1] if table is not None else 0, k_scale, v_scale)
+    c.tensors = (pages, table, lens)
+    return c
+
+
+def _cache(cache, shape, paged=True):
+    """the cache's tensors against the shape of a call"""
+    pages, table, lens = cache.tensors
+    want = focus_kv4_page_bytes(shape, cache.page_tokens)
+    assert want in (0, pages.shape[1]), f"pages of {pages.shape[1]} bytes, {want} for this shape"      # (0: the library says what is wrong)
+    assert not paged or (lens is not None and lens.shape[0] == shape.batch), "table and lens of another batch"
+    return C.byref(cache)
+
+
+def focus_kv4_append(shape, cache, k, v, mk, counts=None, dev_status=None, stream=None):
+    """k, v bf16 [batch, Hkv, n, D] (or [Hkv, n, D]); mk int32 [batch*Hkv, n]; counts int32 [batch] or None"""
+    _check(lib().focus_kv4_append(C.byref(shape), _cache(cache, shape), _heads(k, shape, shape.Hkv), _heads(v, shape, shape.Hkv),
+                                  _dev(mk, torch.int32, shape.batch, shape.Hkv, shape.n), _opt(counts, torch.int32, shape.batch),
+                                  _opt(dev_status, torch.int32, 4), _stream(stream)))
+
+
+def focus_kv4_read(shape, cache, first, k, v, mk=None, dev_status=None, stream=None):
+    """tokens first[b] .. first[b] + n - 1 (first int32 [batch] or None: from the start) into k, v bf16 [batch, Hkv, n, D] and mk int32 [batch*Hkv, n]"""
+    _check(lib().focus_kv4_read(C.byref(shape), _cache(cache, shape), _opt(first, torch.int32, shape.batch), _heads(k, shape, shape.Hkv),
+                                _heads(v, shape, shape.Hkv), _opt(mk, torch.int32, shape.batch, shape.Hkv, shape.n), _opt(dev_status, torch.int32, 4),
+                                _stream(stream)))
+
+
+def focus_kv4_copy_pages(shape, cache, src, dst, dev_status=None, stream=None):
+    """pages src[i] -> dst[i]; int32 lists on the GPU"""
+    count = src.numel()
+    _check(lib().focus_kv4_copy_pages(C.byref(shape), _cache(cache, shape, False), _dev(src, torch.int32, count), _dev(dst, torch.int32, count), count,
+                                      _opt(dev_status, torch.int32, 4), _stream(stream)))
+
+
+def focus_kv4_decode_workspace_bytes(shape) -> int:
+    return int(lib().focus_kv4_decode_workspace_bytes(C.byref(shape)))
+
+
+def focus_kv4_decode_step(shape, cache, q, mq_new, o, lse, ws, dev_status=None, stream=None):
+    """q, o bf16 [batch, Hq, D] (or [Hq, D]); mq_new int32 [batch*Hq]; lse fp32 [batch*Hq]; shape.n bounds the lengths"""
+    _check(lib().focus_kv4_decode_step(C.byref(shape), _cache(cache, shape), _vecs(q, shape, shape.Hq), _dev(mq_new, torch.int32, shape.batch, shape.Hq),
+                                       _vecs(o, shape, shape.Hq), _dev(lse, torch.float32, shape.batch, shape.Hq), _p(ws),
+                                       ws.numel() * ws.element_size(), _opt(dev_status, torch.int32, 4), _stream(stream)))
 
 
 def focus_soft_ld(K) -> int:

@@ -1,6 +1,8 @@
 // C-ABI entry points: argument validation, workspace layout, dispatch.  No kernels here.
 #include "common.cuh"
+#include "kv4_common.cuh"
 
+#include <math.h>
 #include <stdlib.h>
 #include <string.h>
 
@@ -342,6 +344,173 @@ int focus_decode_step(const focus_shape* shape, focus_tensor q, focus_tensor k, 
     if ((rc = require_sm100())) return rc;
     const float scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)shape->D);
     return launch_decode(shape, q, k, v, mq_new, mk, o, lse, (float*)ws, scale, (cudaStream_t)stream);
+}
+
+int focus_rope_frequencies(int32_t rotary, double base, int32_t scaling, double factor, double low, double high, double trained,
+                           double* freq_out, float* amplitude_out) {
+    if (rotary < 0 || rotary % 2 || rotary > 256) return fail(FOCUS_ERR_INVALID_ARG, "rotary (%d) must be even and in [0, 256]", rotary);
+    if (!freq_out && rotary > 0) return fail(FOCUS_ERR_INVALID_ARG, "freq_out is NULL");
+    if (!(base > 0.0) || !isfinite(base)) return fail(FOCUS_ERR_INVALID_ARG, "base must be positive and finite");
+    if (scaling < FOCUS_ROPE_PLAIN || scaling > FOCUS_ROPE_PARTS) return fail(FOCUS_ERR_INVALID_ARG, "unknown scaling (%d)", scaling);
+    if (scaling != FOCUS_ROPE_PLAIN && (!(factor > 0.0) || !isfinite(factor))) return fail(FOCUS_ERR_INVALID_ARG, "factor must be positive and finite");
+    if (scaling == FOCUS_ROPE_PARTS && (!(high > low) || !isfinite(high) || !isfinite(low) || !(trained > 0.0) || !isfinite(trained)))
+        return fail(FOCUS_ERR_INVALID_ARG, "low must be below high and trained positive");
+    return rope_frequencies(rotary, base, scaling, factor, low, high, trained, freq_out, amplitude_out);
+}
+
+static int validate_rope(const focus_shape* shape, const focus_rope* rope, const float* wq, const float* wk, const double* freq,
+                         const int32_t* positions) {
+    if (!rope) return fail(FOCUS_ERR_INVALID_ARG, "rope is NULL");
+    if (rope->rotary < 0 || rope->rotary % 2 || rope->rotary > shape->D)
+        return fail(FOCUS_ERR_INVALID_ARG, "rotary (%d) must be even and in [0, D]", rope->rotary);
+    if (rope->interleaved != 0 && rope->interleaved != 1) return fail(FOCUS_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+    if (!(rope->eps >= 0.f) || !isfinite(rope->amplitude)) return fail(FOCUS_ERR_INVALID_ARG, "eps must be >= 0 and amplitude finite");
+    if (rope->rotary > 0 && !freq) return fail(FOCUS_ERR_INVALID_ARG, "freq is NULL");
+    if ((uintptr_t)freq % 8 || (uintptr_t)wq % 4 || (uintptr_t)wk % 4 || (uintptr_t)positions % 4)
+        return fail(FOCUS_ERR_INVALID_ARG, "freq must be 8-byte aligned, weights and positions 4-byte aligned");
+    return FOCUS_OK;
+}
+
+int focus_qk_norm_rope(const focus_shape* shape, const focus_rope* rope, focus_tensor q, focus_tensor k, const float* wq, const float* wk,
+                       const double* freq, const int32_t* positions, focus_tensor q_out, focus_tensor k_out, void* stream) {
+    int rc = validate_shape(shape);
+    if (rc) return rc;
+    const int nb = shape->batch;
+    if ((rc = validate_rope(shape, rope, wq, wk, freq, positions))) return rc;
+    if ((rc = validate_tensor("q", q, true, nb)) || (rc = validate_tensor("k", k, true, nb)) || (rc = validate_tensor("q_out", q_out, true, nb)) ||
+        (rc = validate_tensor("k_out", k_out, true, nb)))
+        return rc;
+    if ((rc = require_sm100())) return rc;
+    return launch_qk_norm_rope(shape, rope, {q, k}, {wq, wk}, freq, positions, nullptr, {q_out, k_out}, nullptr, nullptr, nullptr,
+                               (cudaStream_t)stream);
+}
+
+size_t focus_qk_norm_rope_bwd_workspace_bytes(const focus_shape* shape) {
+    if (validate_shape(shape)) return 0;
+    return qk_norm_rope_bwd_workspace_bytes(shape);
+}
+
+int focus_qk_norm_rope_bwd(const focus_shape* shape, const focus_rope* rope, focus_tensor q, focus_tensor k, const float* wq, const float* wk,
+                           const double* freq, const int32_t* positions, focus_tensor dq_out, focus_tensor dk_out, focus_tensor dq,
+                           focus_tensor dk, float* dwq, float* dwk, void* ws, size_t ws_bytes, void* stream) {
+    int rc = validate_shape(shape);
+    if (rc) return rc;
+    const int nb = shape->batch;
+    if ((rc = validate_rope(shape, rope, wq, wk, freq, positions))) return rc;
+    if ((rc = validate_tensor("q", q, true, nb)) || (rc = validate_tensor("k", k, true, nb)) || (rc = validate_tensor("dq_out", dq_out, true, nb)) ||
+        (rc = validate_tensor("dk_out", dk_out, true, nb)) || (rc = validate_tensor("dq", dq, true, nb)) || (rc = validate_tensor("dk", dk, true, nb)))
+        return rc;
+    if (!wq != !dwq || !wk != !dwk) return fail(FOCUS_ERR_INVALID_ARG, "dwq and dwk are NULL exactly where wq and wk are");
+    if ((uintptr_t)dwq % 4 || (uintptr_t)dwk % 4) return fail(FOCUS_ERR_INVALID_ARG, "dwq and dwk must be 4-byte aligned");
+    if (dwq && dwq == dwk) return fail(FOCUS_ERR_INVALID_ARG, "dwq and dwk are the same buffer");
+    if (!ws || (uintptr_t)ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is NULL or not 16-byte aligned");
+    if (ws_bytes < qk_norm_rope_bwd_workspace_bytes(shape))
+        return fail(FOCUS_ERR_CAPACITY, "workspace has %zu bytes, %zu needed", ws_bytes, qk_norm_rope_bwd_workspace_bytes(shape));
+    if ((rc = require_sm100())) return rc;
+    const focus_tensor grads[2] = {dq_out, dk_out};
+    return launch_qk_norm_rope(shape, rope, {q, k}, {wq, wk}, freq, positions, grads, {dq, dk}, dwq, dwk, (float*)ws, (cudaStream_t)stream);
+}
+
+// the parts of a 4-bit cache that every entry point uses, checked; `paged`: table and lens too
+static int kv4_view(const focus_shape* shape, const focus_kv4* c, bool paged, Kv4View* out) {
+    if (!c) return fail(FOCUS_ERR_INVALID_ARG, "cache is NULL");
+    const int P = c->page_tokens;
+    if (P < 16 || P > 256 || (P & (P - 1))) return fail(FOCUS_ERR_INVALID_ARG, "page_tokens (%d) must be 16, 32, 64, 128 or 256", P);
+    if (!c->pages || (uintptr_t)c->pages % 16) return fail(FOCUS_ERR_INVALID_ARG, "pages is NULL or not 16-byte aligned");
+    if (c->num_pages < 1 || (long long)c->num_pages * P >= (1ll << 31))
+        return fail(FOCUS_ERR_INVALID_ARG, "num_pages (%d) must be positive and hold fewer than 2^31 tokens", c->num_pages);
+    int e = 0, f = 0;
+    if (!(frexpf(c->k_scale, &e) == 0.5f) || !(frexpf(c->v_scale, &f) == 0.5f) || e < -15 || e > 17 || f < -15 || f > 17)
+        return fail(FOCUS_ERR_INVALID_ARG, "k_scale and v_scale must be powers of two from 2^-16 to 2^16");
+    const size_t bytes = kv4_page_bytes(shape->Hkv, shape->D, P);
+    if (bytes >= (1ull << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "a page of %zu bytes is too large", bytes);
+    if (paged) {
+        if (!c->table || !c->lens || (uintptr_t)c->table % 4 || (uintptr_t)c->lens % 4)
+            return fail(FOCUS_ERR_INVALID_ARG, "table or lens is NULL or misaligned");
+        if (c->max_pages < 1) return fail(FOCUS_ERR_INVALID_ARG, "max_pages must be >= 1");
+    }
+    out->pages = (unsigned char*)c->pages;
+    out->table = c->table;
+    out->lens = c->lens;
+    out->page_bytes = bytes;
+    out->scale_off = (uint32_t)((size_t)shape->Hkv * P * shape->D);
+    out->mask_off = (uint32_t)((size_t)shape->Hkv * P * (shape->D + shape->D / 8));
+    out->num_pages = c->num_pages;
+    out->max_pages = c->max_pages;
+    out->lgP = 0;
+    while ((1 << out->lgP) < P) ++out->lgP;
+    out->Hkv = shape->Hkv;
+    out->k_scale = c->k_scale;
+    out->v_scale = c->v_scale;
+    return FOCUS_OK;
+}
+
+size_t focus_kv4_page_bytes(const focus_shape* shape, int32_t page_tokens) {
+    if (validate_shape(shape)) return 0;
+    if (page_tokens < 16 || page_tokens > 256 || (page_tokens & (page_tokens - 1))) {
+        set_error("page_tokens (%d) must be 16, 32, 64, 128 or 256", page_tokens);
+        return 0;
+    }
+    return kv4_page_bytes(shape->Hkv, shape->D, page_tokens);
+}
+
+int focus_kv4_append(const focus_shape* shape, const focus_kv4* cache, focus_tensor k, focus_tensor v, const uint32_t* mk, const int32_t* counts,
+                     int32_t* dev_status, void* stream) {
+    Kv4View c;
+    int rc = validate_shape(shape);
+    if (rc || (rc = kv4_view(shape, cache, true, &c))) return rc;
+    if ((rc = validate_tensor("k", k, true, shape->batch)) || (rc = validate_tensor("v", v, true, shape->batch))) return rc;
+    if (!mk) return fail(FOCUS_ERR_INVALID_ARG, "mk is NULL");
+    if ((rc = require_sm100())) return rc;
+    return launch_kv4_append(shape, c, k, v, mk, counts, dev_status, (cudaStream_t)stream);
+}
+
+int focus_kv4_read(const focus_shape* shape, const focus_kv4* cache, const int32_t* first, focus_tensor k, focus_tensor v, uint32_t* mk,
+                   int32_t* dev_status, void* stream) {
+    Kv4View c;
+    int rc = validate_shape(shape);
+    if (rc || (rc = kv4_view(shape, cache, true, &c))) return rc;
+    if ((rc = validate_tensor("k", k, true, shape->batch)) || (rc = validate_tensor("v", v, true, shape->batch))) return rc;
+    if ((rc = require_sm100())) return rc;
+    return launch_kv4_read(shape, c, first, k, v, mk, dev_status, (cudaStream_t)stream);
+}
+
+int focus_kv4_copy_pages(const focus_shape* shape, const focus_kv4* cache, const int32_t* src, const int32_t* dst, int32_t count, int32_t* dev_status,
+                         void* stream) {
+    Kv4View c;
+    int rc = validate_shape(shape);
+    if (rc || (rc = kv4_view(shape, cache, false, &c))) return rc;
+    if (count < 0) return fail(FOCUS_ERR_INVALID_ARG, "count must be >= 0");
+    if (count == 0) return FOCUS_OK;
+    if (!src || !dst) return fail(FOCUS_ERR_INVALID_ARG, "src or dst is NULL");
+    if ((rc = require_sm100())) return rc;
+    return launch_kv4_copy(c, src, dst, count, dev_status, (cudaStream_t)stream);
+}
+
+size_t focus_kv4_decode_workspace_bytes(const focus_shape* shape) {
+    if (validate_shape(shape)) return 0;
+    return kv4_decode_workspace_bytes(shape);
+}
+
+int focus_kv4_decode_step(const focus_shape* shape, const focus_kv4* cache, focus_tensor q, const uint32_t* mq_new, focus_tensor o, float* lse,
+                          void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) {
+    Kv4View c;
+    int rc = validate_shape(shape);
+    if (rc || (rc = kv4_view(shape, cache, true, &c))) return rc;
+    if (!q.ptr || !o.ptr || !mq_new || !lse || !ws) return fail(FOCUS_ERR_INVALID_ARG, "a pointer argument is NULL");
+    if (shape->n > (long long)cache->max_pages * cache->page_tokens)
+        return fail(FOCUS_ERR_INVALID_ARG, "n (%d) is more than max_pages * page_tokens", shape->n);
+    // the query vectors are read two elements at a time
+    if ((uintptr_t)q.ptr % 4 || q.stride_h % 2 || q.stride_b % 2 || q.stride_h < 1 || o.stride_h < 1 || q.stride_b < 0 || o.stride_b < 0)
+        return fail(FOCUS_ERR_INVALID_ARG, "q must be 4-byte aligned with even, positive head strides (o: positive strides)");
+    if (shape->batch > 1 && (q.stride_b < 1 || o.stride_b < 1))
+        return fail(FOCUS_ERR_INVALID_ARG, "q.stride_b and o.stride_b must be positive when batch > 1");
+    if ((uintptr_t)ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is not 16-byte aligned");
+    if (ws_bytes < kv4_decode_workspace_bytes(shape))
+        return fail(FOCUS_ERR_CAPACITY, "decode workspace has %zu bytes, %zu needed", ws_bytes, kv4_decode_workspace_bytes(shape));
+    if ((rc = require_sm100())) return rc;
+    const float scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)shape->D);
+    return launch_kv4_decode(shape, c, q, mq_new, o, lse, ws, scale, dev_status, (cudaStream_t)stream);
 }
 
 int focus_count_kept(const focus_shape* shape, const uint32_t* mq, const void* tiles_ws,

@@ -126,6 +126,12 @@ size_t decode_workspace_bytes(const focus_shape* s);
 int launch_decode(const focus_shape* s, const focus_tensor& q, const focus_tensor& k, const focus_tensor& v,
                   const uint32_t* mq_new, const uint32_t* mk, const focus_tensor& o, float* lse, float* part, float scale,
                   cudaStream_t st);
+size_t qk_norm_rope_bwd_workspace_bytes(const focus_shape* s);
+// grads == nullptr: forward
+int launch_qk_norm_rope(const focus_shape* s, const focus_rope* rope, const focus_tensor (&x)[2], const float* const (&w)[2], const double* freq,
+                        const int32_t* positions, const focus_tensor* grads, const focus_tensor (&out)[2], float* dwq, float* dwk, float* partial,
+                        cudaStream_t st);
+int rope_frequencies(int rotary, double base, int scaling, double factor, double low, double high, double trained, double* out, float* amplitude);
 int launch_build_tiles(const focus_shape* s, const uint32_t* mq, const uint32_t* mk, int layout,
                        const focus_tiles_layout& L, char* ws, cudaStream_t st);
 // class-sorted layout: copy the rows of Q, K and V into the sorted order of the workspace

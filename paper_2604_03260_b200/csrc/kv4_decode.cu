@@ -2,16 +2,20 @@
 // token at position len-1 attends key j when len-1-j <= w or its groups meet the key's groups), sequences of their own lengths.
 //
 // HBM-bound by its bytes (D + D / 8 per attended key of a KV head, a quarter of bf16's 4 D), but only just: at the card's copy rate an SM
-// takes in 24 bytes a cycle, 43 codes, and each costs an SM about 1.5 thread instructions to become an operand of the matrix unit, where
-// it has 128 a cycle.  So the kernel is laid out for few instructions per code:
-//   - The rows are loaded straight into the registers of the matrix instruction that needs them.  The order in which a contraction
-//     meets its dimensions is free, so lane q of a quad takes the contiguous quarter q of a key row (16 bytes at D = 128, two whole
-//     blocks of scales), and lane row r of the warp the contiguous eighth r of a value row.
+// takes in 24 bytes a cycle, 16 keys of D = 128 in 96 cycles, in which its four integer pipes, which turn codes into fp16 (2 cycles a
+// pair, measured) and move them about, have time for 192 warp instructions.  So the kernel is laid out for few instructions per code:
+//   - The order in which a contraction meets its dimensions is free, so a lane's operands are the codes of one 16-byte piece of a key row,
+//     and of one piece of a value row, in the order in which they lie there.
 //   - Keys are the row operand, the query heads of the group (at most 8) the column operand: no row of a tile is padding.
 //   - A code times its scale has six significant bits at most: exact in fp16, so the products with Q are the products of the values that
 //     the codes stand for.  Q goes to fp16 with a power of two per head (exact but for elements 2^27 smaller than the head's largest),
 //     probabilities carry a factor 2^10 into fp16, so that they lose bits only below 2^-24 of the largest.
+//   - The operand of P V holds two keys per register.  Their codes are put side by side four at a time, before they are converted (2
+//     instructions for 8 numbers; after it, 8).
+//   - The maximum that probabilities are relative to follows the scores only when one of them is 2^5 beyond it: a vote per tile instead
+//     of six exchanges.
 //   - Only attended keys become rows of a tile: a warp walks the masks, lists the attended keys, and takes 16 off the list at a time.
+// Rows come through a ring in shared memory, private to a warp, by asynchronous copies: one address per 16 bytes, none for the operands.
 // Every warp keeps its own maximum, sum and O; a CTA joins its warps, a second kernel the CTAs.
 #include "kv4_common.cuh"
 
@@ -22,14 +26,24 @@ constexpr int KD_WARPS = 4;
 constexpr int KD_UNIT = 64;              // keys: the grain of the split over CTAs, 16 per warp
 constexpr int KD_SMS = 148;
 constexpr int KD_MAX_BATCH = 1024;
-constexpr int KD_LIST = 16 + 128;        // attended keys a warp has listed: what is left of a tile, and 128 more
+constexpr int KD_LIST = 256;             // ring of listed keys: at most 15 left over, 128 new, and those of the stages
+constexpr int KD_STAGES = 3;             // tiles of 16 keys in a warp's ring
 constexpr float KD_LOG2E = 1.4426950408889634f;
 constexpr float KD_LN2 = 0.6931471805599453f;
 constexpr float KD_PSHIFT = 10.f;
+constexpr float KD_SLACK = 5.f;          // 2^15 < 65504, the largest fp16 number
 
 template <int D> struct KdCfg {
-    static constexpr int PER_SM = D == 256 ? 3 : 4;           // CTAs that fit an SM by their registers
+    static constexpr int PER_SM = D == 256 ? 3 : 4;           // CTAs that fit an SM
     static constexpr int CTAS = KD_SMS * PER_SM;
+    // a stage: 16 rows of key codes, of value codes, of scales.  A lane reads 16 bytes of a key row (8 at D = 64), eight lanes two whole rows
+    // (half rows at D = 256, where the halves of odd rows are swapped): no bank is asked twice.  Of a value row a lane reads an eighth, 4 rows
+    // two apart at once: the rows are 16 bytes longer.
+    static constexpr int KROW = D / 2, VROW = D / 2 + 16, SROW = D / 8;
+    static constexpr int V_AT = 16 * KROW, S_AT = V_AT + 16 * VROW, STAGE = S_AT + 16 * SROW;
+    static constexpr int RING = KD_WARPS * KD_STAGES * STAGE;
+    static constexpr int JOIN = KD_WARPS * KD_GMAX * (D + 2) * (int)sizeof(float);         // over the rings, when they are through
+    static constexpr size_t SMEM = RING > JOIN ? RING : JOIN;
 };
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -60,20 +74,25 @@ __device__ __forceinline__ uint32_t kd_no_nan(uint32_t s) {
     return r;
 }
 
-// words per lane: of a key row, of a value row
+__device__ __forceinline__ void kd_copy16(uint32_t dst, const unsigned char* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void kd_copy8(uint32_t dst, const unsigned char* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint32_t kd_low_high(uint32_t x, uint32_t y) { return (x & 0x0f0f0f0fu) | (y & 0xf0f0f0f0u); }
+
+// `WORDS` words of shared memory; a key row's second half at D = 256 is 64 bytes away, in the direction that the row's place says
 template <int WORDS>
-__device__ __forceinline__ void kd_load(uint32_t (&r)[WORDS], const unsigned char* p) {
+__device__ __forceinline__ void kd_read(uint32_t (&r)[WORDS], const unsigned char* p) {
     if constexpr (WORDS == 1) {
         r[0] = *reinterpret_cast<const uint32_t*>(p);
     } else if constexpr (WORDS == 2) {
         const uint2 x = *reinterpret_cast<const uint2*>(p);
         r[0] = x.x; r[1] = x.y;
     } else {
-#pragma unroll
-        for (int i = 0; i < WORDS / 4; ++i) {
-            const uint4 x = reinterpret_cast<const uint4*>(p)[i];
-            r[4 * i] = x.x; r[4 * i + 1] = x.y; r[4 * i + 2] = x.z; r[4 * i + 3] = x.w;
-        }
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        r[0] = x.x; r[1] = x.y; r[2] = x.z; r[3] = x.w;
     }
 }
 
@@ -97,23 +116,32 @@ __device__ __forceinline__ int kd_length(const Kv4View& c, int b, int n, int32_t
     return len;
 }
 
+// units of a head in the list
+__device__ __forceinline__ long long kd_padded(int len, const KdPlan& p) {
+    const long long u = kd_cdiv(len, KD_UNIT);
+    return p.aligned ? (u + p.per - 1) / p.per * p.per : u;
+}
+
 template <int D>
 __global__ void __launch_bounds__(KD_WARPS * 32, KdCfg<D>::PER_SM)
 kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t q_sh, const uint32_t* mq_new, int batch, int Hq, int G, int n, int w,
                   float scale, float softcap, float* part, int2* ranges, __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, float* lse, int32_t* status) {
-    constexpr int KW = D / 32, VW = D / 64;                    // words per lane of a key row, of a value row
+    using C = KdCfg<D>;
+    constexpr int KW = D == 64 ? 2 : 4, KH = D == 256 ? 2 : 1;     // words a lane reads of a key row at once, and how often
+    constexpr int VW = D / 64;                                 // words of a value row
     constexpr int MT = D / 16;                                 // 16-row tiles of O
-    constexpr int KSB = D / 64;                                // blocks of scales in a lane's part of a key row
-    __shared__ long long start_s[KD_MAX_BATCH + 1];            // first unit of each sequence
-    __shared__ int len_s[KD_MAX_BATCH];
+    constexpr int CPT = D / 16;                                // 16-byte pieces of a token's codes
+    constexpr int COPIES = 16 * CPT / 32, ROWSTEP = 32 / CPT;  // copies per lane and tile; tokens apart
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ long long chunk_s[KD_MAX_BATCH / 32 + 1];       // first unit of every 32 sequences
     __shared__ long long red_s[KD_WARPS][4];
-    __shared__ uint32_t key_s[KD_WARPS][KD_LIST];              // listed keys: page * P + slot
-    __shared__ uint8_t bit_s[KD_WARPS][KD_LIST];               // and which heads attend them
-    __shared__ float xw[KD_WARPS][KD_GMAX][D + 2];
+    __shared__ uint2 key_s[KD_WARPS][KD_LIST];                 // listed keys: where their codes are (in 16 bytes) and scales (in 8)
+    __shared__ uint8_t bit_s[KD_WARPS][KD_LIST];               // which heads attend them
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, qd = lane & 3;
     const int Hkv = c.Hkv, lgP = c.lgP;
     const uint32_t pmask = (1u << lgP) - 1u;
+    unsigned char* ring = smem + warp * KD_STAGES * C::STAGE;
     dep_wait();
     dep_trigger();
 
@@ -122,12 +150,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     long long total;
     {
         const int ctas = gridDim.x;
-        long long sum = 0;
-        for (int b = threadIdx.x; b < batch; b += KD_WARPS * 32) {
-            const int len = kd_length(c, b, n, blockIdx.x == 0 ? status : nullptr);
-            len_s[b] = len;
-            sum += kd_cdiv(len, KD_UNIT);
-        }
+        // (the first 128 lengths stay in a register)
+        const int len0 = (int)threadIdx.x < batch ? kd_length(c, threadIdx.x, n, blockIdx.x == 0 ? status : nullptr) : 0;
+        long long sum = kd_cdiv(len0, KD_UNIT);
+        for (int b = threadIdx.x + KD_WARPS * 32; b < batch; b += KD_WARPS * 32)
+            sum += kd_cdiv(kd_length(c, b, n, blockIdx.x == 0 ? status : nullptr), KD_UNIT);
 #pragma unroll
         for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
         if (lane == 0) red_s[warp][0] = sum;
@@ -141,7 +168,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         const long long cand[3] = {per0, per0 + (per0 + 7) / 8, per0 + (per0 + 3) / 4};
         long long cnt[3] = {0, 0, 0};
         for (int b = threadIdx.x; b < batch; b += KD_WARPS * 32) {
-            const int u = kd_cdiv(len_s[b], KD_UNIT);
+            const int u = kd_cdiv(b < KD_WARPS * 32 ? len0 : kd_length(c, b, n, nullptr), KD_UNIT);
 #pragma unroll
             for (int i = 0; i < 3; ++i) cnt[i] += (u + (uint32_t)cand[i] - 1u) / (uint32_t)cand[i];
         }
@@ -161,48 +188,49 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             for (int j = 0; j < KD_WARPS; ++j) ranges_needed += red_s[j][1 + i];
             if (ranges_needed * Hkv <= ctas) { plan.per = cand[i]; plan.aligned = 1; }
         }
-        // first unit of each sequence: a scan of the padded heads, by the first warp
+        // first unit of every 32 sequences, by the first warp
         if (warp == 0) {
             long long base = 0;
             for (int b0 = 0; b0 < batch; b0 += 32) {
-                const int b = b0 + lane;
-                long long u = 0;
-                if (b < batch) {
-                    u = kd_cdiv(len_s[b], KD_UNIT);
-                    if (plan.aligned) u = (u + plan.per - 1) / plan.per * plan.per;
-                    u *= Hkv;
-                }
-                long long incl = u;
+                long long u = b0 + lane < batch ? kd_padded(b0 == 0 ? len0 : kd_length(c, b0 + lane, n, nullptr), plan) * Hkv : 0;
 #pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const long long t = __shfl_up_sync(0xffffffffu, incl, off);
-                    if (lane >= off) incl += t;
-                }
-                if (b < batch) start_s[b] = base + incl - u;
-                base += __shfl_sync(0xffffffffu, incl, 31);
+                for (int off = 16; off >= 1; off >>= 1) u += __shfl_xor_sync(0xffffffffu, u, off);
+                if (lane == 0) chunk_s[b0 / 32] = base;
+                base += u;
             }
-            if (lane == 0) start_s[batch] = base;
+            if (lane == 0) chunk_s[kd_cdiv(batch, 32)] = base;
         }
         __syncthreads();
-        total = start_s[batch];
+        total = chunk_s[kd_cdiv(batch, 32)];
     }
 
     const long long f_end = min((long long)(blockIdx.x + 1) * plan.per, total);
     for (long long f = (long long)blockIdx.x * plan.per; f < f_end;) {
-        // ---- the sequence and head of unit f
-        int b;
+        // ---- the sequence and head of unit f (every warp for itself)
+        int b, len;
+        long long start;
         {
-            int lo = 0, hi = batch;                            // start_s[lo] <= f < start_s[hi]
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (start_s[mid] <= f) lo = mid; else hi = mid;
+            int ch = 0;
+            while (chunk_s[ch + 1] <= f) ++ch;
+            const int mine = ch * 32 + lane;
+            const int l = mine < batch ? kd_length(c, mine, n, nullptr) : 0;
+            const long long u = kd_padded(l, plan) * Hkv;
+            long long incl = u;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const long long t = __shfl_up_sync(0xffffffffu, incl, off);
+                if (lane >= off) incl += t;
             }
-            b = lo;
+            incl += chunk_s[ch];
+            const int at = __ffs(__ballot_sync(0xffffffffu, incl > f)) - 1;
+            b = ch * 32 + at;
+            len = __shfl_sync(0xffffffffu, l, at);
+            start = __shfl_sync(0xffffffffu, incl - u, at);
         }
-        const int len = len_s[b], units = kd_cdiv(len, KD_UNIT);
-        const long long stride = plan.aligned ? (units + plan.per - 1) / plan.per * plan.per : units;
-        const int hk = (int)((f - start_s[b]) / stride);
-        const long long f0 = start_s[b] + hk * stride;         // the head's first unit
+        const int units = kd_cdiv(len, KD_UNIT);
+        const long long stride = kd_padded(len, plan);
+        const int hk = (int)((f - start) / stride);
+        const long long f0 = start + hk * stride;              // the head's first unit
         const int bh = b * Hkv + hk;
         const int u0 = (int)(f - f0);
         const int u1 = (int)min((long long)units, u0 + (f_end - f));
@@ -212,60 +240,26 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         if (u0 >= u1) continue;                                // (the padding of a head)
         const int t0 = u0 * KD_UNIT, t1 = min(u1 * KD_UNIT, len), last = len - 1;
 
-        // ---- Q as the column operand: this lane has quarter qd of head g
-        uint32_t qb[MT][2];
-        float qf;                                              // what a score of this lane's head is multiplied by
-        {
-            const __nv_bfloat16* qrow = q + (size_t)b * q_sb + (size_t)(hk * G + (g < G ? g : 0)) * q_sh + qd * (D / 4);
-            uint32_t raw[D / 8];
-            float top = 0.f;
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-                raw[i] = g < G ? *reinterpret_cast<const uint32_t*>(qrow + 2 * i) : 0u;
-                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[i] << 16)), fabsf(__uint_as_float(raw[i] & 0xffff0000u))));
-            }
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            // 2^13 <= top * up < 2^14 (a head of zeros or of denormal numbers: as if its largest were 2^-100)
-            const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
-            const float up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
-            qf = __uint_as_float((uint32_t)(e - 13 + 127) << 23);
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-                qb[i >> 1][i & 1] = kd_pack(__uint_as_float(raw[i] << 16) * up, __uint_as_float(raw[i] & 0xffff0000u) * up);
-        }
-        // scores come out as (key, head) with heads 2 qd and 2 qd + 1 in this lane; in log2 units they are S * mul, or tanh(S * cap_in) * sl2
-        float mul[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float x = __shfl_sync(0xffffffffu, qf, (2 * qd + e) * 4) * c.k_scale * scale;
-            mul[e] = softcap > 0.f ? x / softcap : x * KD_LOG2E;
-        }
-        const float cap2 = softcap * KD_LOG2E;
         uint32_t mq_all[KD_GMAX];
 #pragma unroll
         for (int gg = 0; gg < KD_GMAX; ++gg) mq_all[gg] = gg < G ? dep_load(mq_new + (size_t)b * Hq + hk * G + gg) : 0u;
 
-        const unsigned char* codes = c.pages + ((size_t)hk << lgP) * D;
-        const unsigned char* scales = c.pages + c.scale_off + ((size_t)hk << lgP) * (D / 8);
-        const unsigned char* masks = c.pages + c.mask_off + ((size_t)hk << lgP) * 4;
-        const int32_t* table = c.table + (size_t)b * c.max_pages;
-
         // ---- this warp's keys: blocks of 16, every fourth one; x-th key -> position
+        const int32_t* table = c.table + (size_t)b * c.max_pages;
+        const unsigned char* masks = c.pages + c.mask_off + ((size_t)hk << lgP) * 4;
+        const uint32_t page16 = (uint32_t)(c.page_bytes / 16);
         const int blocks = kd_cdiv(t1 - t0, 16);
         const int mine = (blocks - warp + KD_WARPS - 1) / KD_WARPS * 16;           // (may pass the end: checked per key)
         auto position = [&](int x) { return t0 + (((x >> 4) * KD_WARPS + warp) << 4) + (x & 15); };
-        int scanned = 0, head = 0, tail = 0;
+        int scanned = 0, tail = 0, issued = 0;                 // keys walked, keys listed, tiles whose copies are under way or done
         int pg[4];                                             // pages of the next 128 keys
         uint32_t mk[4];                                        // and their masks
-        auto fetch_pages = [&](int x0) {
+        auto fetch = [&](int x0) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int x = x0 + 32 * k + lane, j = position(x);
                 pg[k] = x < mine && j < t1 ? dep_load(table + (j >> lgP)) : -1;
             }
-        };
-        auto fetch_masks = [&](int x0) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int x = x0 + 32 * k + lane, j = position(x);
@@ -278,129 +272,169 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 }
             }
         };
-        // list attended keys until a tile is full or the keys are through
+        // list attended keys until there is a tile more or the keys are through; the last tile is filled up with its last key, attended by no head
         auto refill = [&] {
-            while (tail - head < 16 && scanned < mine) {
-                const int left = tail - head;
-                if (head > 0) {
-                    uint32_t kk = 0;
-                    uint8_t bb = 0;
-                    if (lane < left) { kk = key_s[warp][head + lane]; bb = bit_s[warp][head + lane]; }
-                    __syncwarp();
-                    if (lane < left) { key_s[warp][lane] = kk; bit_s[warp][lane] = bb; }
-                    head = 0;
-                    tail = left;
-                }
+            while (tail < (issued + 1) * 16 && scanned < mine) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int x = scanned + 32 * k + lane, j = position(x);
                     uint32_t bits = 0;
                     if (x < mine && j < t1 && pg[k] >= 0 && pg[k] < c.num_pages) {
-                        const bool local = last - j <= w;
+                        if (last - j <= w) {
+                            bits = (1u << G) - 1u;
+                        } else {
 #pragma unroll
-                        for (int gg = 0; gg < KD_GMAX; ++gg)
-                            if (gg < G && (local || (mq_all[gg] & mk[k]))) bits |= 1u << gg;
+                            for (int gg = 0; gg < KD_GMAX; ++gg)
+                                if (gg < G && (mq_all[gg] & mk[k])) bits |= 1u << gg;
+                        }
                     }
                     const uint32_t any = __ballot_sync(0xffffffffu, bits != 0u);
                     if (bits) {
-                        const int at = tail + __popc(any & ((1u << lane) - 1u));
-                        key_s[warp][at] = ((uint32_t)pg[k] << lgP) | (j & pmask);
+                        const int at = (tail + __popc(any & ((1u << lane) - 1u))) & (KD_LIST - 1);
+                        const uint32_t slot = j & pmask;
+                        key_s[warp][at] = make_uint2((uint32_t)pg[k] * page16 + slot * (D / 16), (uint32_t)pg[k] * (2 * page16) + slot * (D / 64));
                         bit_s[warp][at] = (uint8_t)bits;
                     }
                     tail += __popc(any);
                 }
                 scanned += 128;
-                if (scanned < mine) { fetch_pages(scanned); fetch_masks(scanned); }
+                if (scanned < mine) fetch(scanned);
+                __syncwarp();
+            }
+            if (scanned >= mine && (tail & 15) && tail < (issued + 1) * 16) {
+                const uint2 pad = key_s[warp][(tail - 1) & (KD_LIST - 1)];
+                if (lane < 16 - (tail & 15)) {
+                    key_s[warp][(tail + lane) & (KD_LIST - 1)] = pad;
+                    bit_s[warp][(tail + lane) & (KD_LIST - 1)] = 0;
+                }
+                tail = (tail + 15) & ~15;
                 __syncwarp();
             }
         };
-        // the tile's rows: keys g and g + 8 of K, keys 2 qd, 2 qd + 1, 2 qd + 8, 2 qd + 9 of V (past the list's end: its last key, attended by no head)
-        uint32_t kr[2][KW], vr[4][VW], ks[2], vs[4], bits[2];
-        auto load_k = [&](int cnt) {
+        // copies of a tile: piece `lane % CPT` of token `lane / CPT`, and on by ROWSTEP tokens; then the scales
+        const int ctok = lane / CPT, piece = lane % CPT;
+        const bool cv = piece >= CPT / 2;
+        const unsigned char* csrc = c.pages + ((size_t)hk << lgP) * D + piece * 16;
+        // (at D = 256 ROWSTEP is 2: the row's parity, which says how its halves lie, is the lane's)
+        const int cdst = cv ? C::V_AT + ctok * C::VROW + (piece - CPT / 2) * 16 : ctok * C::KROW + (D == 256 ? (piece ^ ((ctok & 1) << 2)) * 16 : piece * 16);
+        const int cstep = ROWSTEP * (cv ? C::VROW : C::KROW);
+        constexpr int SP = D == 256 ? 2 : 1;                   // pieces of a row of scales
+        const unsigned char* ssrc = c.pages + c.scale_off + ((size_t)hk << lgP) * (D / 8) + (lane % SP) * 16;
+        const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
+        auto issue = [&] {
+            refill();
+            if (tail >= (issued + 1) * 16) {
+                const uint32_t st = ring_u32 + (issued % KD_STAGES) * C::STAGE;
+                const uint2* keys = &key_s[warp][(issued * 16) & (KD_LIST - 1)];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int x = g + 8 * i, y = head + min(x, cnt - 1);
-                const uint32_t key = key_s[warp][y];
-                bits[i] = x < cnt ? bit_s[warp][y] : 0u;
-                const size_t page = (size_t)(key >> lgP) * c.page_bytes;
-                const uint32_t slot = key & pmask;
-                kd_load<KW>(kr[i], codes + page + slot * D + qd * (D / 8));
-                const unsigned char* sp = scales + page + slot * (D / 8) + qd * KSB;
-                if constexpr (KSB == 1) ks[i] = *sp;
-                else if constexpr (KSB == 2) ks[i] = *reinterpret_cast<const uint16_t*>(sp);
-                else ks[i] = *reinterpret_cast<const uint32_t*>(sp);
+                for (int i = 0; i < COPIES; ++i) kd_copy16(st + cdst + i * cstep, csrc + (size_t)keys[ctok + i * ROWSTEP].x * 16);
+                if (lane < 16 * SP) {
+                    const unsigned char* src = ssrc + (size_t)keys[lane / SP].y * 8;
+                    if constexpr (D == 64) kd_copy8(st + C::S_AT + lane * 8, src);
+                    else kd_copy16(st + C::S_AT + lane * 16, src);
+                }
+                ++issued;
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        auto load_v = [&](int cnt) {
+        if (mine > 0) fetch(0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int x = 2 * qd + (i & 1) + 8 * (i >> 1), y = head + min(x, cnt - 1);
-                const uint32_t key = key_s[warp][y];
-                const size_t page = (size_t)(key >> lgP) * c.page_bytes;
-                const uint32_t slot = key & pmask;
-                kd_load<VW>(vr[i], codes + page + slot * D + D / 2 + g * (D / 16));
-                const unsigned char* sp = scales + page + slot * (D / 8) + D / 16;
-                if constexpr (D == 64) vs[i] = sp[g >> 1];
-                else if constexpr (D == 128) vs[i] = sp[g];
-                else vs[i] = *reinterpret_cast<const uint16_t*>(sp + 2 * g);
-            }
-        };
+        for (int i = 0; i < KD_STAGES - 1; ++i) issue();
 
-        float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};    // of heads 2 qd, 2 qd + 1; l: this lane's keys alone
+        // ---- Q as the column operand: this lane has, of head g, the dimensions of its pieces of a key row
+        uint32_t qb[MT][2];
+        float qf;                                              // what a score of this lane's head is multiplied by
+        {
+            const __nv_bfloat16* qrow = q + (size_t)b * q_sb + (size_t)(hk * G + (g < G ? g : 0)) * q_sh;
+            uint32_t raw[D / 8];
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+                const int d = (i / (4 * KW)) * (D / 2) + qd * (8 * KW) + 2 * (i % (4 * KW));
+                raw[i] = g < G ? *reinterpret_cast<const uint32_t*>(qrow + d) : 0u;
+                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[i] << 16)), fabsf(__uint_as_float(raw[i] & 0xffff0000u))));
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // 2^13 <= top * up < 2^14 (a head of zeros or of denormal numbers: as if its largest were 2^-100)
+            const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
+            const float up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
+            qf = __uint_as_float((uint32_t)(e - 13 + 127) << 23);
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+                qb[i >> 1][i & 1] = kd_pack(__uint_as_float(raw[i] << 16) * up, __uint_as_float(raw[i] & 0xffff0000u) * up);
+        }
+        // scores come out as (key, head) with heads 2 qd and 2 qd + 1 in this lane; in log2 units they are S * mul, or tanh(S * mul) * cap2
+        float mul[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float x = __shfl_sync(0xffffffffu, qf, (2 * qd + e) * 4) * c.k_scale * scale;
+            mul[e] = softcap > 0.f ? x / softcap : x * KD_LOG2E;
+        }
+        const float cap2 = softcap * KD_LOG2E;
+
+        float m_ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};    // of heads 2 qd, 2 qd + 1; l: this lane's keys alone
         float acc[MT][4];                                      // O: dimensions (D / 8) g + 2 i (elements 0, 1) and + 1 (2, 3), heads 2 qd, 2 qd + 1
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 
-        if (mine > 0) { fetch_pages(0); fetch_masks(0); }
-        refill();
-        int cnt = min(16, tail - head);
-        if (cnt > 0) { load_k(cnt); load_v(cnt); }
-        while (cnt > 0) {
-            // ---- S = K Q^T for 16 keys
+        for (int tile = 0;; ++tile) {
+            issue();                                           // into the stage that the tile before has left
+            if (tile >= issued) break;
+            asm volatile("cp.async.wait_group %0;" ::"n"(KD_STAGES - 1) : "memory");
+            __syncwarp();
+            const unsigned char* st = ring + (tile % KD_STAGES) * C::STAGE;
+            const uint8_t* flags = &bit_s[warp][(tile * 16) & (KD_LIST - 1)];
+            const uint32_t bt[2] = {(uint32_t)flags[g] >> (2 * qd), (uint32_t)flags[g + 8] >> (2 * qd)};
+            // ---- S = K Q^T: keys g and g + 8 of the tile, two sums in turn
             float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int wd = 0; wd < KW; ++wd) {
-                uint32_t a[2][4];
+            for (int h = 0; h < KH; ++h) {
+                uint32_t kr[2][KW], sc[2][2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    kv4_unpack8(kr[i][wd], a[i]);
-                    const uint32_t two = kv4_scales(ks[i] >> (16 * (wd >> 2)));
-                    const uint32_t sb = __byte_perm(two, two, (wd >> 1) & 1 ? 0x3232 : 0x1010);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) a[i][e] = kv4_mul2(a[i][e], sb);
+                    kd_read<KW>(kr[i], st + (g + 8 * i) * C::KROW + (KH == 2 ? (h ^ (g & 1)) * 64 : 0) + qd * (4 * KW));
+                    const unsigned char* sp = st + C::S_AT + (g + 8 * i) * C::SROW;
+                    const uint32_t two = kv4_scales(D == 64 ? (uint32_t)sp[qd] : (uint32_t) * reinterpret_cast<const uint16_t*>(sp + 8 * h + 2 * qd));
+                    sc[i][0] = __byte_perm(two, two, 0x1010);
+                    sc[i][1] = __byte_perm(two, two, 0x3232);
                 }
-                mma_f16_16816(s0, a[0][0], a[1][0], a[0][1], a[1][1], qb[2 * wd][0], qb[2 * wd][1]);
-                mma_f16_16816(s1, a[0][2], a[1][2], a[0][3], a[1][3], qb[2 * wd + 1][0], qb[2 * wd + 1][1]);
+#pragma unroll
+                for (int wd = 0; wd < KW; ++wd) {
+                    uint32_t a[2][4];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        kv4_unpack8(kr[i][wd], a[i]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) a[i][e] = kv4_mul2(a[i][e], sc[i][wd >> 1]);
+                    }
+                    const uint32_t(*qx)[2] = &qb[2 * (h * KW + wd)];
+                    mma_f16_16816(s0, a[0][0], a[1][0], a[0][1], a[1][1], qx[0][0], qx[0][1]);
+                    mma_f16_16816(s1, a[0][2], a[1][2], a[0][3], a[1][3], qx[1][0], qx[1][1]);
+                }
             }
-            const uint32_t bt[2] = {bits[0] >> (2 * qd), bits[1] >> (2 * qd)};
-            // the next tile's keys on their way
-            head += cnt;
-            __syncwarp();
-            refill();
-            const int nxt = min(16, tail - head);
-            if (nxt > 0) load_k(nxt);
             // ---- scores of keys g (elements 0, 1) and g + 8 (2, 3) for heads 2 qd, 2 qd + 1, in log2 units
-            float x[4];
-            float top[2] = {-INFINITY, -INFINITY};
+            float x[4], top[2];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float t = (s0[e] + s1[e]) * mul[e & 1];
                 if (softcap > 0.f) t = tanhf(t) * cap2;
                 x[e] = (bt[e >> 1] >> (e & 1)) & 1u ? t : -INFINITY;
-                top[e & 1] = fmaxf(top[e & 1], x[e]);
             }
+            top[0] = fmaxf(x[0], x[2]);
+            top[1] = fmaxf(x[1], x[3]);
+            if (__any_sync(0xffffffffu, top[0] > m_ref[0] + KD_SLACK || top[1] > m_ref[1] + KD_SLACK)) {
 #pragma unroll
-            for (int off = 4; off <= 16; off <<= 1) {
-                top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], off));
-                top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], off));
-            }
-            if (__any_sync(0xffffffffu, top[0] > m_run[0] || top[1] > m_run[1])) {
+                for (int off = 4; off <= 16; off <<= 1) {
+                    top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], off));
+                    top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], off));
+                }
                 float fac[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float m_new = fmaxf(m_run[e], top[e]);
-                    fac[e] = m_new == -INFINITY ? 1.f : kd_exp2(m_run[e] - m_new);
-                    m_run[e] = m_new;
+                    const float m_new = fmaxf(m_ref[e], top[e]);
+                    fac[e] = m_new == -INFINITY ? 1.f : kd_exp2(m_ref[e] - m_new);
+                    m_ref[e] = m_new;
                     l_run[e] *= fac[e];
                 }
 #pragma unroll
@@ -409,13 +443,21 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             float p[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                // (a NaN score goes through; a maximum of minus infinity means that no key of the head has come yet)
-                p[e] = x[e] == -INFINITY ? 0.f : kd_exp2(x[e] - m_run[e & 1] + KD_PSHIFT);
+                // (a NaN score goes through; a reference of minus infinity means that no key of the head has come yet)
+                p[e] = x[e] == -INFINITY ? 0.f : kd_exp2(x[e] - m_ref[e & 1] + KD_PSHIFT);
                 l_run[e & 1] += p[e];
             }
             // probabilities as the column operand (key, head): two transposed 8 x 8 blocks
             const uint32_t pb0 = kd_transpose(kd_pack(p[0], p[1])), pb1 = kd_transpose(kd_pack(p[2], p[3]));
-            // ---- O += V^T P
+            // ---- O += V^T P: keys 2 qd, 2 qd + 1 (A, B) and 2 qd + 8, 2 qd + 9 (C, D) of the tile
+            uint32_t vr[4][VW], vs[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 2 * qd + (i & 1) + 8 * (i >> 1);
+                kd_read<VW>(vr[i], st + C::V_AT + row * C::VROW + g * (D / 16));
+                const unsigned char* sp = st + C::S_AT + row * C::SROW + D / 16;
+                vs[i] = D == 64 ? sp[g >> 1] : D == 128 ? sp[g] : *reinterpret_cast<const uint16_t*>(sp + 2 * g);
+            }
             uint32_t sab[D == 256 ? 2 : 1], scd[D == 256 ? 2 : 1];
 #pragma unroll
             for (int i = 0; i < (D == 256 ? 2 : 1); ++i) {
@@ -424,18 +466,20 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             }
 #pragma unroll
             for (int wd = 0; wd < VW; ++wd) {
-                uint32_t a[4][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) kv4_unpack8(vr[i][wd], a[i]);
+                // codes of the same dimension of two keys in a byte: even dimensions, odd ones
+                uint32_t ab[2][4], cd[2][4];
+                kv4_unpack8(kd_low_high(vr[0][wd], vr[1][wd] << 4), ab[0]);
+                kv4_unpack8(kd_low_high(vr[0][wd] >> 4, vr[1][wd]), ab[1]);
+                kv4_unpack8(kd_low_high(vr[2][wd], vr[3][wd] << 4), cd[0]);
+                kv4_unpack8(kd_low_high(vr[2][wd] >> 4, vr[3][wd]), cd[1]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    mma_f16_16816(acc[4 * wd + e], kv4_mul2(__byte_perm(a[0][e], a[1][e], 0x5410), sab[wd >> 1]),
-                                  kv4_mul2(__byte_perm(a[0][e], a[1][e], 0x7632), sab[wd >> 1]), kv4_mul2(__byte_perm(a[2][e], a[3][e], 0x5410), scd[wd >> 1]),
-                                  kv4_mul2(__byte_perm(a[2][e], a[3][e], 0x7632), scd[wd >> 1]), pb0, pb1);
+                    mma_f16_16816(acc[4 * wd + e], kv4_mul2(ab[0][e], sab[wd >> 1]), kv4_mul2(ab[1][e], sab[wd >> 1]), kv4_mul2(cd[0][e], scd[wd >> 1]),
+                                  kv4_mul2(cd[1][e], scd[wd >> 1]), pb0, pb1);
             }
-            if (nxt > 0) load_v(nxt);
-            cnt = nxt;
+            __syncwarp();                                      // the stage and its place in the list are free
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
 
         // ---- join the warps
 #pragma unroll
@@ -443,9 +487,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], off);
             l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], off);
         }
+        __syncthreads();                                       // the rings are through
+        auto xw = reinterpret_cast<float(*)[KD_GMAX][D + 2]>(smem);
         if (g == 0) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { xw[warp][2 * qd + e][0] = m_run[e]; xw[warp][2 * qd + e][1] = l_run[e]; }
+            for (int e = 0; e < 2; ++e) { xw[warp][2 * qd + e][0] = m_ref[e]; xw[warp][2 * qd + e][1] = l_run[e]; }
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -476,7 +522,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 dst[2 + d] = a;
             }
         }
-        __syncthreads();                                       // the next head's results
+        __syncthreads();                                       // the next head's rows and results
     }
 }
 
@@ -576,7 +622,9 @@ static int decode_d(const focus_shape* s, const Kv4View& c, const focus_tensor& 
     const int G = s->Hq / s->Hkv;
     int2* ranges = reinterpret_cast<int2*>(ws);
     float* part = reinterpret_cast<float*>((char*)ws + align_up((size_t)s->batch * s->Hkv * sizeof(int2), 16));
-    int rc = check_cuda(launch_dependent(kv4_decode_kernel<D>, dim3(grid), dim3(KD_WARPS * 32), 0, st, c, reinterpret_cast<const __nv_bfloat16*>(q.ptr),
+    int rc = check_cuda(allow_smem<kv4_decode_kernel<D>>(KdCfg<D>::SMEM, true), "cudaFuncSetAttribute(kv4 decode)");
+    if (rc) return rc;
+    rc = check_cuda(launch_dependent(kv4_decode_kernel<D>, dim3(grid), dim3(KD_WARPS * 32), KdCfg<D>::SMEM, st, c, reinterpret_cast<const __nv_bfloat16*>(q.ptr),
                                          q.stride_b, q.stride_h, mq_new, s->batch, s->Hq, G, s->n, s->window, scale, s->softcap, part, ranges,
                                          reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse, status), "kv4 decode kernel launch");
     if (rc) return rc;
@@ -588,6 +636,7 @@ int launch_kv4_decode(const focus_shape* s, const Kv4View& c, const focus_tensor
                       float scale, int32_t* status, cudaStream_t st) {
     if (s->Hq / s->Hkv > KD_GMAX) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d query heads per KV head", KD_GMAX);
     if ((long long)s->batch * s->Hkv * cdiv(s->n, KD_UNIT) >= (1ll << 38)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: batch * Hkv * n is too large");
+    if ((size_t)c.num_pages * c.page_bytes >= (1ull << 35)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: a pool of 32 GiB or more");
     if (s->batch > KD_MAX_BATCH) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d sequences in one call", KD_MAX_BATCH);
     switch (s->D) {
         case 64: return decode_d<64>(s, c, q, mq_new, o, lse, ws, scale, status, st);

@@ -19,6 +19,8 @@
 // Every warp keeps its own maximum, sum and O; a CTA joins its warps, a second kernel the CTAs.
 #include "kv4_common.cuh"
 
+#include <float.h>
+
 namespace focus {
 
 constexpr int KD_GMAX = 8;
@@ -55,6 +57,10 @@ __device__ __forceinline__ uint32_t kd_transpose(uint32_t x) {           // an 8
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
+}
+// (lo, lo) and (hi, hi) of a pair (lo, hi): half selections that a multiplication takes along
+__device__ __forceinline__ void kd_halves(uint32_t two, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tmov.b32 %0, {l, l};\n\tmov.b32 %1, {h, h};\n\t}" : "=r"(lo), "=r"(hi) : "r"(two));
 }
 __device__ __forceinline__ uint32_t kd_pack(float lo, float hi) {
     uint32_t r;
@@ -103,8 +109,7 @@ __host__ __device__ __forceinline__ int kd_cdiv(int a, int b) { return (a + b - 
 // the heads are padded to whole ranges where that still leaves no more ranges than CTAs.  The lengths are on the device, and so every
 // CTA works this out for itself (a microsecond; the sums are over the sequences of the batch).
 struct KdPlan {
-    long long per;
-    int aligned;
+    int per, aligned;
 };
 
 __device__ __forceinline__ int kd_length(const Kv4View& c, int b, int n, int32_t* status) {
@@ -117,12 +122,13 @@ __device__ __forceinline__ int kd_length(const Kv4View& c, int b, int n, int32_t
 }
 
 // units of a head in the list
-__device__ __forceinline__ long long kd_padded(int len, const KdPlan& p) {
-    const long long u = kd_cdiv(len, KD_UNIT);
-    return p.aligned ? (u + p.per - 1) / p.per * p.per : u;
+__device__ __forceinline__ int kd_padded(int len, const KdPlan& p) {
+    const int u = kd_cdiv(len, KD_UNIT);
+    return p.aligned ? kd_cdiv(u, p.per) * p.per : u;
 }
 
-template <int D>
+// GP: query heads per KV head, G, rounded up to a power of two
+template <int D, int GP>
 __global__ void __launch_bounds__(KD_WARPS * 32, KdCfg<D>::PER_SM)
 kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t q_sh, const uint32_t* mq_new, int batch, int Hq, int G, int n, int w,
                   float scale, float softcap, float* part, int2* ranges, __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, float* lse, int32_t* status) {
@@ -133,49 +139,48 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     constexpr int CPT = D / 16;                                // 16-byte pieces of a token's codes
     constexpr int COPIES = 16 * CPT / 32, ROWSTEP = 32 / CPT;  // copies per lane and tile; tokens apart
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ long long chunk_s[KD_MAX_BATCH / 32 + 1];       // first unit of every 32 sequences
-    __shared__ long long red_s[KD_WARPS][4];
+    __shared__ int chunk_s[KD_MAX_BATCH / 32 + 1];       // first unit of every 32 sequences
+    __shared__ int red_s[KD_WARPS][4];
     __shared__ uint2 key_s[KD_WARPS][KD_LIST];                 // listed keys: where their codes are (in 16 bytes) and scales (in 8)
     __shared__ uint8_t bit_s[KD_WARPS][KD_LIST];               // which heads attend them
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, qd = lane & 3;
     const int Hkv = c.Hkv, lgP = c.lgP;
-    const uint32_t pmask = (1u << lgP) - 1u;
+    const uint32_t pmask = (1u << lgP) - 1u, lower = (1u << lane) - 1u;
     unsigned char* ring = smem + warp * KD_STAGES * C::STAGE;
     dep_wait();
     dep_trigger();
 
-    // ---- the plan
+    // ---- the plan (the host has seen to it that the list has fewer than 2^30 units)
     KdPlan plan;
-    long long total;
+    int total;
+    const int chunks = kd_cdiv(batch, 32);
     {
         const int ctas = gridDim.x;
         // (the first 128 lengths stay in a register)
         const int len0 = (int)threadIdx.x < batch ? kd_length(c, threadIdx.x, n, blockIdx.x == 0 ? status : nullptr) : 0;
-        long long sum = kd_cdiv(len0, KD_UNIT);
+        int sum = kd_cdiv(len0, KD_UNIT);
         for (int b = threadIdx.x + KD_WARPS * 32; b < batch; b += KD_WARPS * 32)
             sum += kd_cdiv(kd_length(c, b, n, blockIdx.x == 0 ? status : nullptr), KD_UNIT);
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        sum = __reduce_add_sync(0xffffffffu, sum);
         if (lane == 0) red_s[warp][0] = sum;
         __syncthreads();
         total = 0;
 #pragma unroll
         for (int i = 0; i < KD_WARPS; ++i) total += red_s[i][0];
         total *= Hkv;
-        const long long per0 = total > ctas ? (total + ctas - 1) / ctas : 1;
+        const int per0 = total > ctas ? kd_cdiv(total, ctas) : 1;
         // three lengths of a range to try with whole ranges per head: the shortest, an eighth and a quarter longer
-        const long long cand[3] = {per0, per0 + (per0 + 7) / 8, per0 + (per0 + 3) / 4};
-        long long cnt[3] = {0, 0, 0};
+        const int cand[3] = {per0, per0 + kd_cdiv(per0, 8), per0 + kd_cdiv(per0, 4)};
+        int cnt[3] = {0, 0, 0};
         for (int b = threadIdx.x; b < batch; b += KD_WARPS * 32) {
             const int u = kd_cdiv(b < KD_WARPS * 32 ? len0 : kd_length(c, b, n, nullptr), KD_UNIT);
 #pragma unroll
-            for (int i = 0; i < 3; ++i) cnt[i] += (u + (uint32_t)cand[i] - 1u) / (uint32_t)cand[i];
+            for (int i = 0; i < 3; ++i) cnt[i] += kd_cdiv(u, cand[i]);
         }
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
-#pragma unroll
-            for (int off = 16; off >= 1; off >>= 1) cnt[i] += __shfl_xor_sync(0xffffffffu, cnt[i], off);
+            cnt[i] = __reduce_add_sync(0xffffffffu, cnt[i]);
             if (lane == 0) red_s[warp][1 + i] = cnt[i];
         }
         __syncthreads();
@@ -183,42 +188,39 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         plan.aligned = 0;
 #pragma unroll
         for (int i = 2; i >= 0; --i) {
-            long long ranges_needed = 0;
+            int wanted = 0;
 #pragma unroll
-            for (int j = 0; j < KD_WARPS; ++j) ranges_needed += red_s[j][1 + i];
-            if (ranges_needed * Hkv <= ctas) { plan.per = cand[i]; plan.aligned = 1; }
+            for (int j = 0; j < KD_WARPS; ++j) wanted += red_s[j][1 + i];
+            if (wanted * Hkv <= ctas) { plan.per = cand[i]; plan.aligned = 1; }
         }
         // first unit of every 32 sequences, by the first warp
         if (warp == 0) {
-            long long base = 0;
+            int base = 0;
             for (int b0 = 0; b0 < batch; b0 += 32) {
-                long long u = b0 + lane < batch ? kd_padded(b0 == 0 ? len0 : kd_length(c, b0 + lane, n, nullptr), plan) * Hkv : 0;
-#pragma unroll
-                for (int off = 16; off >= 1; off >>= 1) u += __shfl_xor_sync(0xffffffffu, u, off);
+                const int u = b0 + lane < batch ? kd_padded(b0 == 0 ? len0 : kd_length(c, b0 + lane, n, nullptr), plan) * Hkv : 0;
                 if (lane == 0) chunk_s[b0 / 32] = base;
-                base += u;
+                base += __reduce_add_sync(0xffffffffu, u);
             }
-            if (lane == 0) chunk_s[kd_cdiv(batch, 32)] = base;
+            if (lane == 0) chunk_s[chunks] = base;
         }
         __syncthreads();
-        total = chunk_s[kd_cdiv(batch, 32)];
+        total = chunk_s[chunks];
     }
 
-    const long long f_end = min((long long)(blockIdx.x + 1) * plan.per, total);
-    for (long long f = (long long)blockIdx.x * plan.per; f < f_end;) {
+    const int f_end = min(((int)blockIdx.x + 1) * plan.per, total);
+    for (int f = (int)blockIdx.x * plan.per; f < f_end;) {
         // ---- the sequence and head of unit f (every warp for itself)
-        int b, len;
-        long long start;
+        int b, len, start;
         {
             int ch = 0;
             while (chunk_s[ch + 1] <= f) ++ch;
             const int mine = ch * 32 + lane;
             const int l = mine < batch ? kd_length(c, mine, n, nullptr) : 0;
-            const long long u = kd_padded(l, plan) * Hkv;
-            long long incl = u;
+            const int u = kd_padded(l, plan) * Hkv;
+            int incl = u;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
-                const long long t = __shfl_up_sync(0xffffffffu, incl, off);
+                const int t = __shfl_up_sync(0xffffffffu, incl, off);
                 if (lane >= off) incl += t;
             }
             incl += chunk_s[ch];
@@ -227,81 +229,71 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             len = __shfl_sync(0xffffffffu, l, at);
             start = __shfl_sync(0xffffffffu, incl - u, at);
         }
-        const int units = kd_cdiv(len, KD_UNIT);
-        const long long stride = kd_padded(len, plan);
-        const int hk = (int)((f - start) / stride);
-        const long long f0 = start + hk * stride;              // the head's first unit
+        const int units = kd_cdiv(len, KD_UNIT), stride = kd_padded(len, plan);
+        const int hk = (f - start) / stride;
+        const int f0 = start + hk * stride;                    // the head's first unit
         const int bh = b * Hkv + hk;
-        const int u0 = (int)(f - f0);
-        const int u1 = (int)min((long long)units, u0 + (f_end - f));
+        const int u0 = f - f0, u1 = min(units, u0 + (f_end - f));
         f = min(f_end, f0 + stride);
-        if (u0 == 0 && threadIdx.x == 0)
-            ranges[bh] = make_int2((int)(f0 / plan.per), (int)((f0 + units - 1) / plan.per));
+        if (u0 == 0 && threadIdx.x == 0) ranges[bh] = make_int2(f0 / plan.per, (f0 + units - 1) / plan.per);
         if (u0 >= u1) continue;                                // (the padding of a head)
-        const int t0 = u0 * KD_UNIT, t1 = min(u1 * KD_UNIT, len), last = len - 1;
+        const int t0 = u0 * KD_UNIT, t1 = min(u1 * KD_UNIT, len), near = len - 1 - w;      // keys from `near` on are local
 
-        uint32_t mq_all[KD_GMAX];
+        uint32_t mq_all[GP];
 #pragma unroll
-        for (int gg = 0; gg < KD_GMAX; ++gg) mq_all[gg] = gg < G ? dep_load(mq_new + (size_t)b * Hq + hk * G + gg) : 0u;
+        for (int gg = 0; gg < GP; ++gg) mq_all[gg] = gg < G ? dep_load(mq_new + (size_t)b * Hq + hk * G + gg) : 0u;
 
-        // ---- this warp's keys: blocks of 16, every fourth one; x-th key -> position
+        // ---- this warp's keys: a quarter of the range, in whole tiles
         const int32_t* table = c.table + (size_t)b * c.max_pages;
         const unsigned char* masks = c.pages + c.mask_off + ((size_t)hk << lgP) * 4;
         const uint32_t page16 = (uint32_t)(c.page_bytes / 16);
-        const int blocks = kd_cdiv(t1 - t0, 16);
-        const int mine = (blocks - warp + KD_WARPS - 1) / KD_WARPS * 16;           // (may pass the end: checked per key)
-        auto position = [&](int x) { return t0 + (((x >> 4) * KD_WARPS + warp) << 4) + (x & 15); };
-        int scanned = 0, tail = 0, issued = 0;                 // keys walked, keys listed, tiles whose copies are under way or done
-        int pg[4];                                             // pages of the next 128 keys
-        uint32_t mk[4];                                        // and their masks
-        auto fetch = [&](int x0) {
+        const int quarter = kd_cdiv(t1 - t0, 16 * KD_WARPS) * 16;
+        const int k_end = min(t0 + (warp + 1) * quarter, t1);
+        int next = t0 + warp * quarter;                        // keys walked so far
+        int tail = 0, issued = 0;                              // keys listed; 16 times the tiles whose copies are under way or done
+        uint32_t pg[4], mk[4];                                 // pages of the next 128 keys (beyond any where there is no key), and their masks
+        auto fetch = [&] {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int x = x0 + 32 * k + lane, j = position(x);
-                pg[k] = x < mine && j < t1 ? dep_load(table + (j >> lgP)) : -1;
+                const int j = next + 32 * k + lane;
+                pg[k] = j < k_end ? (uint32_t)dep_load(table + (j >> lgP)) : 0xffffffffu;
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int x = x0 + 32 * k + lane, j = position(x);
+                const int j = next + 32 * k + lane;
                 mk[k] = 0u;
-                if (x < mine && j < t1) {
-                    if (pg[k] >= 0 && pg[k] < c.num_pages)
-                        mk[k] = dep_load(reinterpret_cast<const uint32_t*>(masks + (size_t)pg[k] * c.page_bytes) + (j & pmask));
-                    else
-                        kv4_report(status, KV4_BAD_PAGE, b, j >> lgP, pg[k]);      // its keys are passed over
-                }
+                if (pg[k] < (uint32_t)c.num_pages)
+                    mk[k] = dep_load(reinterpret_cast<const uint32_t*>(masks + (size_t)pg[k] * c.page_bytes) + (j & pmask));
+                else if (j < k_end)
+                    kv4_report(status, KV4_BAD_PAGE, b, j >> lgP, (int)pg[k]);     // its keys are passed over
             }
         };
         // list attended keys until there is a tile more or the keys are through; the last tile is filled up with its last key, attended by no head
         auto refill = [&] {
-            while (tail < (issued + 1) * 16 && scanned < mine) {
+            while (tail < issued + 16 && next < k_end) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int x = scanned + 32 * k + lane, j = position(x);
+                    const int j = next + 32 * k + lane;
                     uint32_t bits = 0;
-                    if (x < mine && j < t1 && pg[k] >= 0 && pg[k] < c.num_pages) {
-                        if (last - j <= w) {
-                            bits = (1u << G) - 1u;
-                        } else {
 #pragma unroll
-                            for (int gg = 0; gg < KD_GMAX; ++gg)
-                                if (gg < G && (mq_all[gg] & mk[k])) bits |= 1u << gg;
-                        }
-                    }
+                    for (int gg = 0; gg < GP; ++gg)
+                        if (mq_all[gg] & mk[k]) bits |= 1u << gg;
+                    if (j >= near) bits = (1u << G) - 1u;
+                    if (pg[k] >= (uint32_t)c.num_pages) bits = 0;
                     const uint32_t any = __ballot_sync(0xffffffffu, bits != 0u);
                     if (bits) {
-                        const int at = (tail + __popc(any & ((1u << lane) - 1u))) & (KD_LIST - 1);
+                        const int at = (tail + __popc(any & lower)) & (KD_LIST - 1);
                         const uint32_t slot = j & pmask;
-                        key_s[warp][at] = make_uint2((uint32_t)pg[k] * page16 + slot * (D / 16), (uint32_t)pg[k] * (2 * page16) + slot * (D / 64));
+                        key_s[warp][at] = make_uint2(pg[k] * page16 + slot * (D / 16), pg[k] * (2 * page16) + slot * (D / 64));
                         bit_s[warp][at] = (uint8_t)bits;
                     }
                     tail += __popc(any);
                 }
-                scanned += 128;
-                if (scanned < mine) fetch(scanned);
+                next += 128;
+                if (next < k_end) fetch();
                 __syncwarp();
             }
-            if (scanned >= mine && (tail & 15) && tail < (issued + 1) * 16) {
+            if ((tail & 15) && tail < issued + 16) {           // (the keys are through)
                 const uint2 pad = key_s[warp][(tail - 1) & (KD_LIST - 1)];
                 if (lane < 16 - (tail & 15)) {
                     key_s[warp][(tail + lane) & (KD_LIST - 1)] = pad;
@@ -321,23 +313,24 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         constexpr int SP = D == 256 ? 2 : 1;                   // pieces of a row of scales
         const unsigned char* ssrc = c.pages + c.scale_off + ((size_t)hk << lgP) * (D / 8) + (lane % SP) * 16;
         const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
+        uint32_t into = ring_u32;                              // the stage of the next tile's copies
         auto issue = [&] {
             refill();
-            if (tail >= (issued + 1) * 16) {
-                const uint32_t st = ring_u32 + (issued % KD_STAGES) * C::STAGE;
-                const uint2* keys = &key_s[warp][(issued * 16) & (KD_LIST - 1)];
+            if (tail > issued) {
+                const uint2* keys = &key_s[warp][issued & (KD_LIST - 1)];
 #pragma unroll
-                for (int i = 0; i < COPIES; ++i) kd_copy16(st + cdst + i * cstep, csrc + (size_t)keys[ctok + i * ROWSTEP].x * 16);
+                for (int i = 0; i < COPIES; ++i) kd_copy16(into + cdst + i * cstep, csrc + (size_t)keys[ctok + i * ROWSTEP].x * 16);
                 if (lane < 16 * SP) {
                     const unsigned char* src = ssrc + (size_t)keys[lane / SP].y * 8;
-                    if constexpr (D == 64) kd_copy8(st + C::S_AT + lane * 8, src);
-                    else kd_copy16(st + C::S_AT + lane * 16, src);
+                    if constexpr (D == 64) kd_copy8(into + C::S_AT + lane * 8, src);
+                    else kd_copy16(into + C::S_AT + lane * 16, src);
                 }
-                ++issued;
+                issued += 16;
+                into = into == ring_u32 + (KD_STAGES - 1) * C::STAGE ? ring_u32 : into + C::STAGE;
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        if (mine > 0) fetch(0);
+        if (next < k_end) fetch();
 #pragma unroll
         for (int i = 0; i < KD_STAGES - 1; ++i) issue();
 
@@ -373,19 +366,20 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         }
         const float cap2 = softcap * KD_LOG2E;
 
-        float m_ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};    // of heads 2 qd, 2 qd + 1; l: this lane's keys alone
+        // of heads 2 qd, 2 qd + 1; l: this lane's keys alone.  No score is as low as the first reference but minus infinity
+        float m_ref[2] = {-FLT_MAX, -FLT_MAX}, l_run[2] = {0.f, 0.f};
         float acc[MT][4];                                      // O: dimensions (D / 8) g + 2 i (elements 0, 1) and + 1 (2, 3), heads 2 qd, 2 qd + 1
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 
-        for (int tile = 0;; ++tile) {
+        const unsigned char* st = ring;
+        for (int tile = 0;; tile += 16) {
             issue();                                           // into the stage that the tile before has left
             if (tile >= issued) break;
             asm volatile("cp.async.wait_group %0;" ::"n"(KD_STAGES - 1) : "memory");
             __syncwarp();
-            const unsigned char* st = ring + (tile % KD_STAGES) * C::STAGE;
-            const uint8_t* flags = &bit_s[warp][(tile * 16) & (KD_LIST - 1)];
-            const uint32_t bt[2] = {(uint32_t)flags[g] >> (2 * qd), (uint32_t)flags[g + 8] >> (2 * qd)};
+            const uint8_t* flags = &bit_s[warp][(tile & (KD_LIST - 1)) + g];
+            const uint32_t bt[2] = {(uint32_t)flags[0] >> (2 * qd), (uint32_t)flags[8] >> (2 * qd)};
             // ---- S = K Q^T: keys g and g + 8 of the tile, two sums in turn
             float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -396,8 +390,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                     kd_read<KW>(kr[i], st + (g + 8 * i) * C::KROW + (KH == 2 ? (h ^ (g & 1)) * 64 : 0) + qd * (4 * KW));
                     const unsigned char* sp = st + C::S_AT + (g + 8 * i) * C::SROW;
                     const uint32_t two = kv4_scales(D == 64 ? (uint32_t)sp[qd] : (uint32_t) * reinterpret_cast<const uint16_t*>(sp + 8 * h + 2 * qd));
-                    sc[i][0] = __byte_perm(two, two, 0x1010);
-                    sc[i][1] = __byte_perm(two, two, 0x3232);
+                    kd_halves(two, sc[i][0], sc[i][1]);
                 }
 #pragma unroll
                 for (int wd = 0; wd < KW; ++wd) {
@@ -416,11 +409,14 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             // ---- scores of keys g (elements 0, 1) and g + 8 (2, 3) for heads 2 qd, 2 qd + 1, in log2 units
             float x[4], top[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float t = (s0[e] + s1[e]) * mul[e & 1];
-                if (softcap > 0.f) t = tanhf(t) * cap2;
-                x[e] = (bt[e >> 1] >> (e & 1)) & 1u ? t : -INFINITY;
+            for (int e = 0; e < 4; ++e) x[e] = (s0[e] + s1[e]) * mul[e & 1];
+            if (softcap > 0.f) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = tanhf(x[e]) * cap2;
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!((bt[e >> 1] >> (e & 1)) & 1u)) x[e] = -INFINITY;
             top[0] = fmaxf(x[0], x[2]);
             top[1] = fmaxf(x[1], x[3]);
             if (__any_sync(0xffffffffu, top[0] > m_ref[0] + KD_SLACK || top[1] > m_ref[1] + KD_SLACK)) {
@@ -433,7 +429,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float m_new = fmaxf(m_ref[e], top[e]);
-                    fac[e] = m_new == -INFINITY ? 1.f : kd_exp2(m_ref[e] - m_new);
+                    fac[e] = kd_exp2(m_ref[e] - m_new);
                     m_ref[e] = m_new;
                     l_run[e] *= fac[e];
                 }
@@ -443,8 +439,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             float p[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                // (a NaN score goes through; a reference of minus infinity means that no key of the head has come yet)
-                p[e] = x[e] == -INFINITY ? 0.f : kd_exp2(x[e] - m_ref[e & 1] + KD_PSHIFT);
+                p[e] = kd_exp2(x[e] - (m_ref[e & 1] - KD_PSHIFT));
                 l_run[e & 1] += p[e];
             }
             // probabilities as the column operand (key, head): two transposed 8 x 8 blocks
@@ -477,6 +472,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                     mma_f16_16816(acc[4 * wd + e], kv4_mul2(ab[0][e], sab[wd >> 1]), kv4_mul2(ab[1][e], sab[wd >> 1]), kv4_mul2(cd[0][e], scd[wd >> 1]),
                                   kv4_mul2(cd[1][e], scd[wd >> 1]), pb0, pb1);
             }
+            st = st == ring + (KD_STAGES - 1) * C::STAGE ? ring : st + C::STAGE;
             __syncwarp();                                      // the stage and its place in the list are free
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -503,13 +499,13 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         const bool whole = u0 == 0 && u1 == units;             // the head's only range: its result, no partial one
         for (int idx = threadIdx.x; idx < G * D; idx += KD_WARPS * 32) {
             const int gg = idx / D, d = idx % D;
-            float M = -INFINITY;
+            float M = -FLT_MAX;
 #pragma unroll
             for (int ww = 0; ww < KD_WARPS; ++ww) M = fmaxf(M, xw[ww][gg][0]);
             float L = 0.f, a = 0.f;
 #pragma unroll
             for (int ww = 0; ww < KD_WARPS; ++ww) {
-                const float wgt = xw[ww][gg][0] == -INFINITY ? 0.f : exp2f(xw[ww][gg][0] - M);
+                const float wgt = exp2f(xw[ww][gg][0] - M);
                 L = fmaf(xw[ww][gg][1], wgt, L);
                 a = fmaf(xw[ww][gg][2 + d], wgt, a);
             }
@@ -557,7 +553,7 @@ kv4_merge_kernel(const Kv4View c, const float* part, const int2* ranges, int Hq,
         const int s = row + j * ROWS;
         v[j] = s < cnt ? *reinterpret_cast<const float2*>(p + s * step + 2 + 2 * col) : make_float2(0.f, 0.f);
     }
-    float m = -INFINITY;
+    float m = -FLT_MAX;
     for (int s = t; s < cnt; s += 256) m = fmaxf(m, p[s * step]);
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
@@ -569,7 +565,7 @@ kv4_merge_kernel(const Kv4View c, const float* part, const int2* ranges, int Hq,
     float l = 0.f;
     for (int s = t; s < cnt; s += 256) {
         const float ms = p[s * step];
-        const float wg = ms == -INFINITY ? 0.f : exp2f(ms - M);
+        const float wg = exp2f(ms - M);
         wgt_s[s] = wg;
         l = fmaf(p[s * step + 1], wg, l);
     }
@@ -614,17 +610,17 @@ size_t kv4_decode_workspace_bytes(const focus_shape* s) {
     return align_up(heads * sizeof(int2), 16) + (heads + ctas) * (s->Hq / s->Hkv) * (s->D + 2) * sizeof(float);
 }
 
-template <int D>
-static int decode_d(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
+template <int D, int GP>
+static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
                     float scale, int32_t* status, cudaStream_t st) {
     const long long most = (long long)s->batch * s->Hkv * cdiv(s->n, KD_UNIT);
     const int grid = (int)(most < KdCfg<D>::CTAS ? most : KdCfg<D>::CTAS);
     const int G = s->Hq / s->Hkv;
     int2* ranges = reinterpret_cast<int2*>(ws);
     float* part = reinterpret_cast<float*>((char*)ws + align_up((size_t)s->batch * s->Hkv * sizeof(int2), 16));
-    int rc = check_cuda(allow_smem<kv4_decode_kernel<D>>(KdCfg<D>::SMEM, true), "cudaFuncSetAttribute(kv4 decode)");
+    int rc = check_cuda(allow_smem<kv4_decode_kernel<D, GP>>(KdCfg<D>::SMEM, true), "cudaFuncSetAttribute(kv4 decode)");
     if (rc) return rc;
-    rc = check_cuda(launch_dependent(kv4_decode_kernel<D>, dim3(grid), dim3(KD_WARPS * 32), KdCfg<D>::SMEM, st, c, reinterpret_cast<const __nv_bfloat16*>(q.ptr),
+    rc = check_cuda(launch_dependent(kv4_decode_kernel<D, GP>, dim3(grid), dim3(KD_WARPS * 32), KdCfg<D>::SMEM, st, c, reinterpret_cast<const __nv_bfloat16*>(q.ptr),
                                          q.stride_b, q.stride_h, mq_new, s->batch, s->Hq, G, s->n, s->window, scale, s->softcap, part, ranges,
                                          reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse, status), "kv4 decode kernel launch");
     if (rc) return rc;
@@ -632,10 +628,20 @@ static int decode_d(const focus_shape* s, const Kv4View& c, const focus_tensor& 
                                        reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse), "kv4 merge kernel launch");
 }
 
+template <int D>
+static int decode_d(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
+                    float scale, int32_t* status, cudaStream_t st) {
+    const int G = s->Hq / s->Hkv;
+    if (G == 1) return decode_dg<D, 1>(s, c, q, mq_new, o, lse, ws, scale, status, st);
+    if (G == 2) return decode_dg<D, 2>(s, c, q, mq_new, o, lse, ws, scale, status, st);
+    if (G <= 4) return decode_dg<D, 4>(s, c, q, mq_new, o, lse, ws, scale, status, st);
+    return decode_dg<D, 8>(s, c, q, mq_new, o, lse, ws, scale, status, st);
+}
+
 int launch_kv4_decode(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
                       float scale, int32_t* status, cudaStream_t st) {
     if (s->Hq / s->Hkv > KD_GMAX) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d query heads per KV head", KD_GMAX);
-    if ((long long)s->batch * s->Hkv * cdiv(s->n, KD_UNIT) >= (1ll << 38)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: batch * Hkv * n is too large");
+    if ((long long)s->batch * s->Hkv * cdiv(s->n, KD_UNIT) >= (1ll << 29)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: batch * Hkv * n is too large");
     if ((size_t)c.num_pages * c.page_bytes >= (1ull << 35)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: a pool of 32 GiB or more");
     if (s->batch > KD_MAX_BATCH) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d sequences in one call", KD_MAX_BATCH);
     switch (s->D) {

@@ -12,7 +12,8 @@
 namespace focus {
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_GRID = 148 * 4;
+constexpr int ROPE_SMS = 148;
+constexpr int ROPE_GRID = ROPE_SMS * 4;           // CTAs that sum weight gradients, at most
 constexpr int ROPE_TOKENS = 16;                   // per tile at most
 
 struct RopeArgs {
@@ -22,291 +23,523 @@ struct RopeArgs {
     const float* w[2];
     const double* freq;
     const int32_t* positions;
-    float* partial;                               // backward with a norm: [blocks][2][D] sums of g xhat
-    int heads[2], n, rot, interleaved;
+    float* partial;                               // backward with a norm: [CTAs of a side][D] sums of g xhat, queries' CTAs first
+    int heads[2], batch, n, rot, interleaved;
     float eps, amplitude;
-    int T, lgT, hsplit;                           // tokens per tile (a power of two), parts that the heads of a tile are cut into
-    long long tiles;                              // batch * ceil(n / T) * hsplit
+    int lgT[2], parts[2];                         // of a side: tokens per tile (log), parts that the heads of a tile are cut into
+    int ctas[2];                                  // backward: CTAs of a side
 };
 
-// A row is cut into units of 2 * V dimensions: V pairs that are turned together.  Rotating halves, unit u < rot / (2 V) holds dimensions
-// V u .. and rot / 2 + V u ..; interleaved, and behind the rotated part, 2 V consecutive ones.  V = 8 (16-byte pieces) unless halves are
-// not whole pieces (rot % 16 != 0), where V = 1.
-template <int D, int V> struct RopeCfg {
-    static constexpr int UNITS = D / (2 * V);
-    static constexpr int LPR = UNITS < 32 ? UNITS : 32;       // lanes per row
-    static constexpr int UPL = UNITS / LPR;                   // units per lane
+// two fp32 operations at once
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 f2_get(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 f2_neg(F2 a) {
+    F2 r;
+    r.v = a.v ^ 0x8000000080000000ull;
+    return r;
+}
+
+// cos and sin (times the amplitude) of position * freq: the angle is reduced in 64 bits, since positions reach a million and fp32 would
+// leave an error of 0.06 there
+__device__ __forceinline__ float2 rope_cos_sin(const RopeArgs& a, int pos, int f) {
+    double turns = (double)pos * (dep_load(a.freq + f) * 0.15915494309189533577);
+    turns -= rint(turns);
+    float sn, cn;
+    sincospif((float)(2.0 * turns), &sn, &cn);
+    return make_float2(cn * a.amplitude, sn * a.amplitude);
+}
+
+// A row is cut into units of 16 dimensions, one per lane: two 16-byte pieces, whose eight pairs are turned.  Rotating halves, unit
+// u < rot / 16 has the pieces at 8 u and rot / 2 + 8 u; interleaved, and behind the rotated part, the two from 16 u on.  In registers a unit
+// is the pairs' first numbers and their second ones, which only the unpacking tells apart: in halves the first piece and the second,
+// interleaved the low and the high numbers of the words.
+template <int D> struct RopeCfg {
+    static constexpr int LPR = D / 16;                        // lanes per row
     static constexpr int RPP = ROPE_THREADS / LPR;            // rows per pass of a CTA
 };
 
-template <int V>
-__device__ __forceinline__ void rope_load(float (&f)[V], const __nv_bfloat16* p) {
-    if constexpr (V == 8) {
-        const uint4 r = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = __bfloat162float(p[i]);
-    }
-}
-template <int V>
-__device__ __forceinline__ void rope_store(__nv_bfloat16* p, const float (&f)[V]) {
-    if constexpr (V == 8) {
-        uint32_t w[4];
+struct RopeUnit {
+    F2 p[4], r[4];                                            // firsts and seconds of pairs (0, 1), (2, 3), (4, 5), (6, 7)
+};
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ RopeUnit rope_unpack(const uint4 (&raw)[2], bool inter) {
+    const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+    RopeUnit u;
+    if (inter) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&t);
+            u.p[i] = f2(bf_lo(w[2 * i]), bf_lo(w[2 * i + 1]));
+            u.r[i] = f2(bf_hi(w[2 * i]), bf_hi(w[2 * i + 1]));
         }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) p[i] = __float2bfloat16(f[i]);
+        for (int i = 0; i < 4; ++i) {
+            u.p[i] = f2(bf_lo(w[i]), bf_hi(w[i]));
+            u.r[i] = f2(bf_lo(w[4 + i]), bf_hi(w[4 + i]));
+        }
+    }
+    return u;
+}
+__device__ __forceinline__ uint32_t bf_pack(float lo, float hi) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ void rope_pack(const RopeUnit& u, bool inter, uint4 (&raw)[2]) {
+    uint32_t w[8];
+    if (inter) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = f2_get(u.p[i]), r = f2_get(u.r[i]);
+            w[2 * i] = bf_pack(p.x, r.x);
+            w[2 * i + 1] = bf_pack(p.y, r.y);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = f2_get(u.p[i]), r = f2_get(u.r[i]);
+            w[i] = bf_pack(p.x, p.y);
+            w[4 + i] = bf_pack(r.x, r.y);
+        }
+    }
+    raw[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    raw[1] = make_uint4(w[4], w[5], w[6], w[7]);
+}
+// pairs (p, r) -> (p c - r s, p s + r c); `s` with the sign of the direction
+__device__ __forceinline__ void rope_turn(RopeUnit& u, const F2 (&c)[4], const F2 (&s)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const F2 p = u.p[i], r = u.r[i];
+        u.p[i] = f2_fma(p, c[i], f2_neg(f2_mul(r, s[i])));
+        u.r[i] = f2_fma(p, s[i], f2_mul(r, c[i]));
+    }
+}
+__device__ __forceinline__ float rope_dot(const RopeUnit& a, const RopeUnit& b) {
+    F2 t = f2_mul(a.p[0], b.p[0]), v = f2_mul(a.r[0], b.r[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) { t = f2_fma(a.p[i], b.p[i], t); v = f2_fma(a.r[i], b.r[i], v); }
+    const float2 x = f2_get(t), y = f2_get(v);
+    return (x.x + x.y) + (y.x + y.y);
+}
+template <int LPR>
+__device__ __forceinline__ float rope_row_sum(float x) {
+#pragma unroll
+    for (int off = LPR / 2; off >= 1; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+    return x;
+}
+
+// where a lane's unit lies in a row, and whether it is turned
+struct RopePlace {
+    int d0, d1;
+    bool turned, inter;
+};
+__device__ __forceinline__ RopePlace rope_place(const RopeArgs& a, int u) {
+    RopePlace x;
+    x.turned = 16 * u < a.rot;
+    x.inter = a.interleaved || !x.turned;
+    x.d0 = x.inter ? 16 * u : 8 * u;
+    x.d1 = x.inter ? 16 * u + 8 : a.rot / 2 + 8 * u;
+    return x;
+}
+// the unit's numbers out of a row of fp32 (weights, in shared memory), and out of the table of cosines and sines; no rotation behind `rot`,
+// nor for a token that is not there (`live`), whose row of the table is not written
+__device__ __forceinline__ RopeUnit rope_weights(const float* w, const RopePlace& x) {
+    RopeUnit u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (x.inter) {
+            const float4 t = *reinterpret_cast<const float4*>(w + x.d0 + 4 * i);
+            u.p[i] = f2(t.x, t.z);
+            u.r[i] = f2(t.y, t.w);
+        } else {
+            const float2 p = *reinterpret_cast<const float2*>(w + x.d0 + 2 * i), r = *reinterpret_cast<const float2*>(w + x.d1 + 2 * i);
+            u.p[i] = f2(p.x, p.y);
+            u.r[i] = f2(r.x, r.y);
+        }
+    }
+    return u;
+}
+__device__ __forceinline__ void rope_angles(const float2* row, int unit, const RopePlace& x, int half, bool live, float sign, F2 (&c)[4], F2 (&s)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float2 t[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int f = 8 * unit + 2 * i + e;
+            t[e] = live && x.turned && f < half ? row[f] : make_float2(1.f, 0.f);
+        }
+        c[i] = f2(t[0].x, t[1].x);
+        s[i] = f2(sign * t[0].y, sign * t[1].y);
     }
 }
 
-__device__ __forceinline__ void rope_turn(float& p, float& r, float cs, float sn) {
-    const float p0 = p;
-    p = p0 * cs - r * sn;
-    r = p0 * sn + r * cs;
-}
-
-// A CTA takes T tokens and (a part of) all their heads.  The thread's token and its place in the row are the same in every pass, so the
-// sines and cosines of its pairs, which cost a reduction of the angle in 64 bits (positions reach a million, and fp32 would leave an
-// error of 0.06 there), are worked out once per token and stay in registers; the weights do too.
-template <int D, int V, bool BWD>
+// Forward: a CTA takes 2^lgT tokens of one side (queries or keys) and as many of its heads as four passes cover, so that all it reads is
+// under way at once; the cosines and sines of its tokens are worked out meanwhile.  A thread's token and place in the row are the same in
+// every pass.  Grid: tiles of tokens x parts of heads, queries first.
+constexpr int ROPE_PASSES = 4;
+template <int D>
 __global__ void __launch_bounds__(ROPE_THREADS)
 qk_norm_rope_kernel(const RopeArgs a) {
-    using C = RopeCfg<D, V>;
+    using C = RopeCfg<D>;
     __shared__ float2 cs_s[ROPE_TOKENS][D / 2 + 1];           // [token][pair]
-    __shared__ float red_s[BWD ? C::RPP : 1][BWD ? D : 1];
-    const int lane_r = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
-    const int tok = rs & (a.T - 1), hofs = rs >> a.lgT, hstep = C::RPP >> a.lgT;
-    const int half = a.rot >> 1;
-    const int turned = a.interleaved ? (a.rot + 2 * V - 1) / (2 * V) : a.rot / (2 * V);    // units with a rotation
-    // a unit's two pieces
-    int d0[C::UPL], d1[C::UPL];
-#pragma unroll
-    for (int i = 0; i < C::UPL; ++i) {
-        const int u = lane_r + i * C::LPR;
-        const bool halves = !a.interleaved && u < turned;
-        d0[i] = halves ? V * u : 2 * V * u;
-        d1[i] = halves ? half + V * u : 2 * V * u + V;
-    }
+    __shared__ float w_s[D];
+    const int unit = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
+    const int tiles_q = a.batch * ((a.n + (1 << a.lgT[0]) - 1) >> a.lgT[0]);
+    const int side = blockIdx.x >= tiles_q * a.parts[0];
+    const int lgT = a.lgT[side], T = 1 << lgT, per_seq = (a.n + T - 1) >> lgT;
+    const int id = blockIdx.x - (side ? tiles_q * a.parts[0] : 0);
+    const int part = id % a.parts[side], tile = id / a.parts[side], b = tile / per_seq, t0 = (tile - b * per_seq) << lgT;
+    const int tok = rs & (T - 1), hstep = C::RPP >> lgT, h0 = part * ROPE_PASSES * hstep + (rs >> lgT), half = a.rot >> 1;
+    const RopePlace at = rope_place(a, unit);
+    const bool live = t0 + tok < a.n, norm = a.w[side] != nullptr;
     dep_wait();
     dep_trigger();
-    float dw[2][C::UPL][2 * V];
-    if constexpr (BWD) {
+    const __nv_bfloat16* src = a.x[side] + (size_t)b * a.x_b[side] + (size_t)(t0 + tok) * a.x_n[side];
+    uint4 raw[ROPE_PASSES][2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int i = 0; i < C::UPL; ++i)
-#pragma unroll
-                for (int e = 0; e < 2 * V; ++e) dw[s][i][e] = 0.f;
+    for (int i = 0; i < ROPE_PASSES; ++i) {
+        const int h = h0 + i * hstep;
+        raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
+        if (live && h < a.heads[side]) {
+            const __nv_bfloat16* p = src + (size_t)h * a.x_h[side];
+            raw[i][0] = *reinterpret_cast<const uint4*>(p + at.d0);
+            raw[i][1] = *reinterpret_cast<const uint4*>(p + at.d1);
+        }
     }
-    const int per_seq = (a.n + a.T - 1) >> a.lgT;
-    const int all = a.heads[0] + a.heads[1];
-    for (long long tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const int part = (int)(tile % a.hsplit);
-        const long long tt = tile / a.hsplit;
-        const int b = (int)(tt / per_seq), t0 = (int)(tt - (long long)b * per_seq) << a.lgT;
-        // sines and cosines of the tile
-        if (half > 0) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < half << a.lgT; i += ROPE_THREADS) {
-                const int t = i / half, f = i - t * half;
-                if (t0 + t < a.n) {
-                    const int pos = a.positions ? dep_load(a.positions + (size_t)b * a.n + t0 + t) : t0 + t;
-                    double turns = (double)pos * (dep_load(a.freq + f) * 0.15915494309189533577);
-                    turns -= rint(turns);
-                    float sn, cn;
-                    sincospif((float)(2.0 * turns), &sn, &cn);
-                    cs_s[t][f] = make_float2(cn * a.amplitude, sn * a.amplitude);
-                }
+    for (int i = threadIdx.x; i < half << lgT; i += ROPE_THREADS) {
+        const int t = i / half, f = i - t * half;
+        if (t0 + t < a.n) cs_s[t][f] = rope_cos_sin(a, a.positions ? dep_load(a.positions + (size_t)b * a.n + t0 + t) : t0 + t, f);
+    }
+    for (int d = threadIdx.x; d < D; d += ROPE_THREADS) w_s[d] = norm ? dep_load(a.w[side] + d) : 1.f;
+    __syncthreads();
+    F2 c[4], sn[4];
+    rope_angles(cs_s[tok], unit, at, half, live, 1.f, c, sn);
+    __nv_bfloat16* dst = a.out[side] + (size_t)b * a.o_b[side] + (size_t)(t0 + tok) * a.o_n[side];
+#pragma unroll
+    for (int i = 0; i < ROPE_PASSES; ++i) {
+        const int h = h0 + i * hstep;
+        if (part * ROPE_PASSES * hstep + i * hstep >= a.heads[side]) break;      // (the same for all threads)
+        RopeUnit x = rope_unpack(raw[i], at.inter);
+        if (norm) {
+            const float r = 1.f / sqrtf(rope_row_sum<C::LPR>(rope_dot(x, x)) * (1.f / D) + a.eps);
+            const F2 r2 = f2(r, r);
+            const RopeUnit w = rope_weights(w_s, at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x.p[e] = f2_mul(f2_mul(x.p[e], r2), w.p[e]);
+                x.r[e] = f2_mul(f2_mul(x.r[e], r2), w.r[e]);
             }
-            __syncthreads();
         }
+        rope_turn(x, c, sn);
+        if (live && h < a.heads[side]) {
+            uint4 out[2];
+            rope_pack(x, at.inter, out);
+            __nv_bfloat16* p = dst + (size_t)h * a.o_h[side];
+            *reinterpret_cast<uint4*>(p + at.d0) = out[0];
+            *reinterpret_cast<uint4*>(p + at.d1) = out[1];
+        }
+    }
+}
+
+// Backward: the CTAs of a side walk its tiles of tokens, all heads of a tile, two rows a thread under way; the sums over rows of g xhat
+// stay in registers to the end, then go to `partial`.
+template <int D>
+__global__ void __launch_bounds__(ROPE_THREADS, 2)
+qk_norm_rope_bwd_kernel(const RopeArgs a) {
+    using C = RopeCfg<D>;
+    constexpr int AHEAD = 2;
+    constexpr size_t TABLES = sizeof(float2) * 2 * ROPE_TOKENS * (D / 2 + 1), SUMS = sizeof(float) * C::RPP * (D + 4);
+    __shared__ __align__(16) unsigned char space_s[TABLES > SUMS ? TABLES : SUMS];
+    auto cs_s = reinterpret_cast<float2(*)[ROPE_TOKENS][D / 2 + 1]>(space_s);
+    auto red_s = reinterpret_cast<float(*)[D + 4]>(space_s);  // when the tables are through
+    __shared__ float w_s[D];
+    const int unit = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
+    const int side = (int)blockIdx.x >= a.ctas[0];
+    const int id = blockIdx.x - (side ? a.ctas[0] : 0);
+    const int lgT = a.lgT[side], T = 1 << lgT, per_seq = (a.n + T - 1) >> lgT, tiles = a.batch * per_seq;
+    const int tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT, half = a.rot >> 1, H = a.heads[side];
+    const RopePlace at = rope_place(a, unit);
+    const bool norm = a.w[side] != nullptr;
+    dep_wait();
+    dep_trigger();
+    for (int d = threadIdx.x; d < D; d += ROPE_THREADS) w_s[d] = norm ? dep_load(a.w[side] + d) : 1.f;
+    RopeUnit dw;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dw.p[e] = dw.r[e] = f2(0.f, 0.f);
+    int buf = 0;
+    for (int tile = id; tile < tiles; tile += a.ctas[side], buf ^= 1) {
+        const int b = tile / per_seq, t0 = (tile - b * per_seq) << lgT;
+        for (int i = threadIdx.x; i < half << lgT; i += ROPE_THREADS) {
+            const int t = i / half, f = i - t * half;
+            if (t0 + t < a.n) cs_s[buf][t][f] = rope_cos_sin(a, a.positions ? dep_load(a.positions + (size_t)b * a.n + t0 + t) : t0 + t, f);
+        }
+        __syncthreads();                                       // (the other table is free: its readers have passed this barrier)
         const bool live = t0 + tok < a.n;
-        float cn[C::UPL][V], sn[C::UPL][V];
+        F2 c[4], sn[4];
+        rope_angles(cs_s[buf][tok], unit, at, half, live, -1.f, c, sn);
+        const __nv_bfloat16* xs = a.x[side] + (size_t)b * a.x_b[side] + (size_t)(t0 + tok) * a.x_n[side];
+        const __nv_bfloat16* gs = a.g[side] + (size_t)b * a.g_b[side] + (size_t)(t0 + tok) * a.g_n[side];
+        __nv_bfloat16* os = a.out[side] + (size_t)b * a.o_b[side] + (size_t)(t0 + tok) * a.o_n[side];
+        for (int hb = 0; hb < H; hb += AHEAD * hstep) {
+            uint4 xr[AHEAD][2], gr[AHEAD][2];
 #pragma unroll
-        for (int i = 0; i < C::UPL; ++i) {
-            const int u = lane_r + i * C::LPR;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                cn[i][e] = 1.f;
-                sn[i][e] = 0.f;
-                if (live && u < turned && V * u + e < half) {
-                    const float2 x = cs_s[tok][V * u + e];
-                    cn[i][e] = x.x;
-                    sn[i][e] = x.y;
+            for (int i = 0; i < AHEAD; ++i) {
+                const int h = hb + i * hstep + hofs;
+                xr[i][0] = xr[i][1] = gr[i][0] = gr[i][1] = make_uint4(0, 0, 0, 0);
+                if (live && h < H) {
+                    const __nv_bfloat16* p = gs + (size_t)h * a.g_h[side];
+                    gr[i][0] = *reinterpret_cast<const uint4*>(p + at.d0);
+                    gr[i][1] = *reinterpret_cast<const uint4*>(p + at.d1);
+                    if (norm) {
+                        const __nv_bfloat16* q = xs + (size_t)h * a.x_h[side];
+                        xr[i][0] = *reinterpret_cast<const uint4*>(q + at.d0);
+                        xr[i][1] = *reinterpret_cast<const uint4*>(q + at.d1);
+                    }
                 }
             }
-        }
-        const int h0 = (int)((long long)all * part / a.hsplit), h1 = (int)((long long)all * (part + 1) / a.hsplit);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int lo = s ? max(h0 - a.heads[0], 0) : h0, hi = s ? h1 - a.heads[0] : min(h1, a.heads[0]);
-            const bool norm = a.w[s] != nullptr;
-            float w[C::UPL][2 * V];
-#pragma unroll
-            for (int i = 0; i < C::UPL; ++i)
-#pragma unroll
-                for (int e = 0; e < 2 * V; ++e) w[i][e] = norm ? dep_load(a.w[s] + (e < V ? d0[i] + e : d1[i] + e - V)) : 1.f;
-            const size_t xo = (size_t)b * a.x_b[s] + (size_t)(t0 + tok) * a.x_n[s];
-            const size_t go = BWD ? (size_t)b * a.g_b[s] + (size_t)(t0 + tok) * a.g_n[s] : 0;
-            const size_t oo = (size_t)b * a.o_b[s] + (size_t)(t0 + tok) * a.o_n[s];
-            // (all lanes of a row take part in its sums; the bound is the same for the whole warp)
-#pragma unroll 2
-            for (int hb = lo; hb < hi; hb += hstep) {
-                const int h = hb + hofs;
-                const bool on = live && h < hi;
-                float x[C::UPL][2 * V], y[C::UPL][2 * V];
-                float ss = 0.f, dot = 0.f;
-#pragma unroll
-                for (int i = 0; i < C::UPL; ++i) {
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) x[i][e] = y[i][e] = 0.f;
-                    if (on && (!BWD || norm)) {
-                        const __nv_bfloat16* p = a.x[s] + xo + (size_t)h * a.x_h[s];
-                        rope_load<V>(*reinterpret_cast<float(*)[V]>(&x[i][0]), p + d0[i]);
-                        rope_load<V>(*reinterpret_cast<float(*)[V]>(&x[i][V]), p + d1[i]);
-                    }
-                    if (BWD && on) {
-                        const __nv_bfloat16* p = a.g[s] + go + (size_t)h * a.g_h[s];
-                        rope_load<V>(*reinterpret_cast<float(*)[V]>(&y[i][0]), p + d0[i]);
-                        rope_load<V>(*reinterpret_cast<float(*)[V]>(&y[i][V]), p + d1[i]);
-                    }
-                }
-                // element (first, second) of pair e of a unit: (e, V + e) where halves turn, (2 e, 2 e + 1) where pairs are interleaved
-                auto turn = [&](float (&f)[2 * V], int i, float sign) {
-                    if (a.interleaved) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e) rope_turn(f[2 * e], f[2 * e + 1], cn[i][e], sign * sn[i][e]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < V; ++e) rope_turn(f[e], f[V + e], cn[i][e], sign * sn[i][e]);
-                    }
-                };
-                if constexpr (BWD) {
-#pragma unroll
-                    for (int i = 0; i < C::UPL; ++i) turn(y[i], i, -1.f);
-                }
+            for (int i = 0; i < AHEAD; ++i) {
+                const int h = hb + i * hstep + hofs;
+                if (hb + i * hstep >= H) break;                // (the same for all threads)
+                RopeUnit g = rope_unpack(gr[i], at.inter);
+                rope_turn(g, c, sn);
                 if (norm) {
+                    RopeUnit x = rope_unpack(xr[i], at.inter);
+                    const RopeUnit w = rope_weights(w_s, at);
+                    RopeUnit u;
 #pragma unroll
-                    for (int i = 0; i < C::UPL; ++i)
-#pragma unroll
-                        for (int e = 0; e < 2 * V; ++e) {
-                            ss = fmaf(x[i][e], x[i][e], ss);
-                            if (BWD) dot = fmaf(x[i][e], y[i][e] * w[i][e], dot);
-                        }
+                    for (int e = 0; e < 4; ++e) { u.p[e] = f2_mul(g.p[e], w.p[e]); u.r[e] = f2_mul(g.r[e], w.r[e]); }
+                    float ss = rope_dot(x, x), dot = rope_dot(x, u);
 #pragma unroll
                     for (int off = C::LPR / 2; off >= 1; off >>= 1) {
                         ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                        if (BWD) dot += __shfl_xor_sync(0xffffffffu, dot, off);
+                        dot += __shfl_xor_sync(0xffffffffu, dot, off);
                     }
                     const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-                    if constexpr (!BWD) {
+                    const float m = dot * r * (1.f / D);       // mean(u xhat)
+                    const bool on = live && h < H;             // (a row that is not there: x = 0, g = 0, and r may be infinite)
+                    const float rx = on ? r : 0.f;
+                    const F2 r2 = f2(r, r), rx2 = f2(rx, rx), mr2 = f2(-m * r, -m * r);
 #pragma unroll
-                        for (int i = 0; i < C::UPL; ++i)
+                    for (int e = 0; e < 4; ++e) {
+                        const F2 xp = f2_mul(x.p[e], rx2), xq = f2_mul(x.r[e], rx2);
+                        dw.p[e] = f2_fma(g.p[e], xp, dw.p[e]);
+                        dw.r[e] = f2_fma(g.r[e], xq, dw.r[e]);
+                        g.p[e] = f2_fma(xp, mr2, f2_mul(u.p[e], r2));
+                        g.r[e] = f2_fma(xq, mr2, f2_mul(u.r[e], r2));
+                    }
+                }
+                if (live && h < H) {
+                    uint4 out[2];
+                    rope_pack(g, at.inter, out);
+                    __nv_bfloat16* p = os + (size_t)h * a.o_h[side];
+                    *reinterpret_cast<uint4*>(p + at.d0) = out[0];
+                    *reinterpret_cast<uint4*>(p + at.d1) = out[1];
+                }
+            }
+        }
+    }
+    if (!a.partial) return;
+    // the CTA's sums: rows of threads in a fixed order
+    __syncthreads();
 #pragma unroll
-                            for (int e = 0; e < 2 * V; ++e) x[i][e] *= r * w[i][e];
+    for (int e = 0; e < 4; ++e) {
+        const float2 p = f2_get(dw.p[e]), r = f2_get(dw.r[e]);
+        float* row = red_s[rs];
+        if (at.inter) {
+            row[at.d0 + 4 * e] = p.x; row[at.d0 + 4 * e + 1] = r.x; row[at.d0 + 4 * e + 2] = p.y; row[at.d0 + 4 * e + 3] = r.y;
+        } else {
+            row[at.d0 + 2 * e] = p.x; row[at.d0 + 2 * e + 1] = p.y; row[at.d1 + 2 * e] = r.x; row[at.d1 + 2 * e + 1] = r.y;
+        }
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < D; d += ROPE_THREADS) {
+        float t = 0.f;
+#pragma unroll 8
+        for (int r = 0; r < C::RPP; ++r) t += red_s[r][d];
+        a.partial[(size_t)blockIdx.x * D + d] = t;
+    }
+}
+
+// Rotating halves that are not whole 16-byte pieces (rot % 16 != 0): a warp per row, lane l has the pairs l, l + 32, ... of it, number by
+// number.  Rows of a side over the warps of its CTAs, which in the backward pass sum their g xhat as above.
+template <int D, bool BWD>
+__global__ void __launch_bounds__(ROPE_THREADS)
+qk_norm_rope_odd_kernel(const RopeArgs a) {
+    constexpr int UPL = D / 64, WARPS = ROPE_THREADS / 32;     // pairs per lane
+    __shared__ float red_s[BWD ? WARPS : 1][BWD ? D : 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int side = (int)blockIdx.x >= a.ctas[0];
+    const int id = blockIdx.x - (side ? a.ctas[0] : 0);
+    const int half = a.rot >> 1, H = a.heads[side];
+    const bool norm = a.w[side] != nullptr;
+    dep_wait();
+    dep_trigger();
+    int d0[UPL], d1[UPL];
+    float w0[UPL], w1[UPL], dw0[UPL], dw1[UPL];
+#pragma unroll
+    for (int i = 0; i < UPL; ++i) {
+        const int u = lane + 32 * i;
+        d0[i] = u < half ? u : 2 * u;
+        d1[i] = u < half ? half + u : 2 * u + 1;
+        w0[i] = norm ? dep_load(a.w[side] + d0[i]) : 1.f;
+        w1[i] = norm ? dep_load(a.w[side] + d1[i]) : 1.f;
+        dw0[i] = dw1[i] = 0.f;
+    }
+    const int tokens = a.batch * a.n;
+    for (int t = id * WARPS + warp; t < tokens; t += a.ctas[side] * WARPS) {
+        const int b = t / a.n, i0 = t - b * a.n;
+        const int pos = a.positions ? dep_load(a.positions + t) : i0;
+        float cn[UPL], sn[UPL];
+#pragma unroll
+        for (int i = 0; i < UPL; ++i) {
+            const float2 x = lane + 32 * i < half ? rope_cos_sin(a, pos, lane + 32 * i) : make_float2(1.f, 0.f);
+            cn[i] = x.x;
+            sn[i] = BWD ? -x.y : x.y;
+        }
+        for (int h = 0; h < H; ++h) {
+            const __nv_bfloat16* xp = a.x[side] + (size_t)b * a.x_b[side] + (size_t)h * a.x_h[side] + (size_t)i0 * a.x_n[side];
+            const __nv_bfloat16* gp = a.g[side] + (BWD ? (size_t)b * a.g_b[side] + (size_t)h * a.g_h[side] + (size_t)i0 * a.g_n[side] : 0);
+            __nv_bfloat16* op = a.out[side] + (size_t)b * a.o_b[side] + (size_t)h * a.o_h[side] + (size_t)i0 * a.o_n[side];
+            float x0[UPL], x1[UPL], g0[UPL], g1[UPL];
+            float ss = 0.f, dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < UPL; ++i) {
+                x0[i] = x1[i] = g0[i] = g1[i] = 0.f;
+                if (!BWD || norm) { x0[i] = __bfloat162float(xp[d0[i]]); x1[i] = __bfloat162float(xp[d1[i]]); }
+                if (BWD) {
+                    const float p = __bfloat162float(gp[d0[i]]), r = __bfloat162float(gp[d1[i]]);
+                    g0[i] = p * cn[i] - r * sn[i];
+                    g1[i] = p * sn[i] + r * cn[i];
+                }
+                ss = fmaf(x0[i], x0[i], fmaf(x1[i], x1[i], ss));
+                dot = fmaf(x0[i], g0[i] * w0[i], fmaf(x1[i], g1[i] * w1[i], dot));
+            }
+            if (norm) {
+                ss = rope_row_sum<32>(ss);
+                if (BWD) dot = rope_row_sum<32>(dot);
+                const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps), m = dot * r * (1.f / D);
+#pragma unroll
+                for (int i = 0; i < UPL; ++i) {
+                    x0[i] *= r;
+                    x1[i] *= r;
+                    if (BWD) {
+                        dw0[i] = fmaf(g0[i], x0[i], dw0[i]);
+                        dw1[i] = fmaf(g1[i], x1[i], dw1[i]);
+                        g0[i] = r * (g0[i] * w0[i] - x0[i] * m);
+                        g1[i] = r * (g1[i] * w1[i] - x1[i] * m);
                     } else {
-                        const float m = dot * r * (1.f / D);                   // mean(u xhat)
-#pragma unroll
-                        for (int i = 0; i < C::UPL; ++i)
-#pragma unroll
-                            for (int e = 0; e < 2 * V; ++e) {
-                                const float xhat = x[i][e] * r;
-                                dw[s][i][e] = fmaf(y[i][e], on ? xhat : 0.f, dw[s][i][e]);
-                                y[i][e] = r * (y[i][e] * w[i][e] - xhat * m);
-                            }
+                        x0[i] *= w0[i];
+                        x1[i] *= w1[i];
                     }
                 }
-                if (on) {
-                    __nv_bfloat16* p = a.out[s] + oo + (size_t)h * a.o_h[s];
+            }
+            __syncwarp();                                      // (the result may lie over the input: all of the row has been read)
 #pragma unroll
-                    for (int i = 0; i < C::UPL; ++i) {
-                        if constexpr (!BWD) turn(x[i], i, 1.f);
-                        float(&f)[2 * V] = BWD ? y[i] : x[i];
-                        rope_store<V>(p + d0[i], *reinterpret_cast<float(*)[V]>(&f[0]));
-                        rope_store<V>(p + d1[i], *reinterpret_cast<float(*)[V]>(&f[V]));
-                    }
-                }
+            for (int i = 0; i < UPL; ++i) {
+                op[d0[i]] = __float2bfloat16(BWD ? g0[i] : x0[i] * cn[i] - x1[i] * sn[i]);
+                op[d1[i]] = __float2bfloat16(BWD ? g1[i] : x0[i] * sn[i] + x1[i] * cn[i]);
             }
         }
     }
     if constexpr (BWD) {
         if (!a.partial) return;
-        // the CTA's sums: rows of threads in a fixed order
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            __syncthreads();
+        for (int i = 0; i < UPL; ++i) { red_s[warp][d0[i]] = dw0[i]; red_s[warp][d1[i]] = dw1[i]; }
+        __syncthreads();
+        for (int d = threadIdx.x; d < D; d += ROPE_THREADS) {
+            float t = 0.f;
 #pragma unroll
-            for (int i = 0; i < C::UPL; ++i)
-#pragma unroll
-                for (int e = 0; e < 2 * V; ++e) red_s[rs][e < V ? d0[i] + e : d1[i] + e - V] = dw[s][i][e];
-            __syncthreads();
-            for (int d = threadIdx.x; d < D; d += ROPE_THREADS) {
-                float t = 0.f;
-                for (int r = 0; r < C::RPP; ++r) t += red_s[r][d];
-                a.partial[((size_t)blockIdx.x * 2 + s) * D + d] = t;
-            }
+            for (int r = 0; r < WARPS; ++r) t += red_s[r][d];
+            a.partial[(size_t)blockIdx.x * D + d] = t;
         }
     }
 }
 
-// dw[s][d] = sum over the CTAs of partial[cta][s][d]; a block per 32 dimensions, 32 rows of threads in a fixed order
+// dw[d] of a side = sum over its CTAs of partial[cta][d]; a block per 32 dimensions, 32 rows of threads in a fixed order
 __global__ void __launch_bounds__(1024)
-norm_weight_grad_kernel(const float* partial, int ctas, int D, float* dwq, float* dwk) {
+norm_weight_grad_kernel(const float* partial, int ctas_q, int ctas_k, int D, float* dwq, float* dwk) {
     __shared__ float red[32][33];
-    const int col = blockIdx.x * 32 + threadIdx.x;            // 0 .. 2 D - 1
+    const int side = blockIdx.x * 32 >= D, col = blockIdx.x * 32 - (side ? D : 0) + threadIdx.x;
+    const int first = side ? ctas_q : 0, last = first + (side ? ctas_k : ctas_q);
     dep_wait();
     dep_trigger();
     float t = 0.f;
 #pragma unroll 4
-    for (int r = threadIdx.y; r < ctas; r += 32) t += dep_load(partial + (size_t)r * 2 * D + col);
+    for (int r = first + threadIdx.y; r < last; r += 32) t += dep_load(partial + (size_t)r * D + col);
     red[threadIdx.y][threadIdx.x] = t;
     __syncthreads();
     if (threadIdx.y == 0) {
         t = 0.f;
 #pragma unroll
         for (int r = 0; r < 32; ++r) t += red[r][threadIdx.x];
-        float* dst = col < D ? dwq : dwk;
-        if (dst) dst[col < D ? col : col - D] = t;
+        float* dst = side ? dwk : dwq;
+        if (dst) dst[col] = t;
     }
 }
 
-size_t qk_norm_rope_bwd_workspace_bytes(const focus_shape* s) { return (size_t)ROPE_GRID * 2 * s->D * sizeof(float); }
+size_t qk_norm_rope_bwd_workspace_bytes(const focus_shape* s) { return (size_t)ROPE_GRID * s->D * sizeof(float); }
 
-template <int D, int V, bool BWD>
-static int launch_rope_dv(const focus_shape* s, RopeArgs& a, float* dwq, float* dwk, cudaStream_t st) {
-    using C = RopeCfg<D, V>;
-    const int all = s->Hq + s->Hkv;
-    // tokens per tile: as many as leave every multiprocessor two tiles, 16 at most (16 head-major rows of a token block are 4 KB in one piece)
-    const int most = C::RPP < ROPE_TOKENS ? C::RPP : ROPE_TOKENS;
-    a.T = 1;
-    a.lgT = 0;
-    while (a.T < most && (long long)s->batch * cdiv(s->n, 2 * a.T) >= 2 * 148) { a.T *= 2; ++a.lgT; }
-    const long long tok_tiles = (long long)s->batch * cdiv(s->n, a.T);
-    // few tiles: the heads of a tile over several CTAs, a pass each at the least
-    const int passes = cdiv(all * a.T, C::RPP);
-    long long split = tok_tiles >= ROPE_GRID ? 1 : ROPE_GRID / tok_tiles;
-    if (split > passes) split = passes;
-    if (split > all) split = all;
-    a.hsplit = (int)split;
-    a.tiles = tok_tiles * split;
-    const int grid = (int)(a.tiles < ROPE_GRID ? a.tiles : ROPE_GRID);
-    int rc = check_cuda(launch_dependent(qk_norm_rope_kernel<D, V, BWD>, dim3(grid), dim3(ROPE_THREADS), 0, st, a), "norm and rotation kernel launch");
-    if (rc || !BWD || !a.partial) return rc;
-    return check_cuda(launch_dependent(norm_weight_grad_kernel, dim3(2 * D / 32), dim3(32, 32), 0, st, a.partial, grid, D, dwq, dwk),
-                      "norm weight gradient kernel launch");
+// tokens per tile of a side: as many as leave room for all its heads in a CTA's passes (16 rows of a token block are 4 KB in one piece when the
+// layout is head by head), fewer where that leaves multiprocessors without a tile
+static int rope_tile(int rows, int heads, int batch, int n) {
+    int lg = 0;
+    while ((2 << lg) <= ROPE_TOKENS && (long long)(2 << lg) * heads <= rows && (long long)batch * cdiv(n, 2 << lg) >= ROPE_SMS) ++lg;
+    return lg;
 }
 
-template <int D, bool BWD>
-static int launch_rope_d(const focus_shape* s, RopeArgs& a, float* dwq, float* dwk, cudaStream_t st) {
-    return a.interleaved || a.rot % 16 == 0 ? launch_rope_dv<D, 8, BWD>(s, a, dwq, dwk, st) : launch_rope_dv<D, 1, BWD>(s, a, dwq, dwk, st);
+template <int D>
+static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq, float* dwk, cudaStream_t st) {
+    using C = RopeCfg<D>;
+    const bool odd = !a.interleaved && a.rot % 16 != 0;
+    const long long tokens = (long long)s->batch * s->n;
+    if (tokens >= (1ll << 30)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: batch * n (%lld) is too large for one call", tokens);
+    long long tiles[2], grid = 0;
+    for (int i = 0; i < 2; ++i) {
+        a.lgT[i] = rope_tile(ROPE_PASSES * C::RPP, a.heads[i], s->batch, s->n);
+        a.parts[i] = cdiv(a.heads[i], ROPE_PASSES * (C::RPP >> a.lgT[i]));
+        tiles[i] = (long long)s->batch * cdiv(s->n, 1 << a.lgT[i]);
+        grid += tiles[i] * a.parts[i];
+    }
+    if (!bwd && !odd) {
+        if (grid >= (1ll << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: too many heads and tokens for one call");
+        return check_cuda(launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)grid), dim3(ROPE_THREADS), 0, st, a), "norm and rotation kernel launch");
+    }
+    // CTAs of the two sides: in proportion to their heads, no more than they have tiles (or rows for the warps)
+    const int places = bwd && !odd ? 2 * ROPE_SMS : ROPE_GRID;
+    if (odd) tiles[0] = tiles[1] = (tokens + 7) / 8;
+    int kc = (int)((long long)places * a.heads[1] / (a.heads[0] + a.heads[1]));
+    if (kc < 1) kc = 1;
+    a.ctas[0] = (int)(tiles[0] < places - kc ? tiles[0] : places - kc);
+    a.ctas[1] = (int)(tiles[1] < kc ? tiles[1] : kc);
+    const dim3 g(a.ctas[0] + a.ctas[1]), t(ROPE_THREADS);
+    int rc = odd ? check_cuda(bwd ? launch_dependent(qk_norm_rope_odd_kernel<D, true>, g, t, 0, st, a) : launch_dependent(qk_norm_rope_odd_kernel<D, false>, g, t, 0, st, a),
+                              "norm and rotation kernel launch")
+                 : check_cuda(launch_dependent(qk_norm_rope_bwd_kernel<D>, g, t, 0, st, a), "norm and rotation backward kernel launch");
+    if (rc || !bwd || !a.partial) return rc;
+    return check_cuda(launch_dependent(norm_weight_grad_kernel, dim3(2 * D / 32), dim3(32, 32), 0, st, a.partial, a.ctas[0], a.ctas[1], D, dwq, dwk),
+                      "norm weight gradient kernel launch");
 }
 
 static void put(RopeArgs& a, int s, const focus_tensor& x, const focus_tensor& out) {
@@ -330,6 +563,7 @@ int launch_qk_norm_rope(const focus_shape* s, const focus_rope* rope, const focu
     }
     a.heads[0] = s->Hq;
     a.heads[1] = s->Hkv;
+    a.batch = s->batch;
     a.n = s->n;
     a.rot = rope->rotary;
     a.interleaved = rope->interleaved;
@@ -338,17 +572,10 @@ int launch_qk_norm_rope(const focus_shape* s, const focus_rope* rope, const focu
     a.freq = freq;
     a.positions = positions;
     a.partial = w[0] || w[1] ? partial : nullptr;
-    if (grads) {
-        switch (s->D) {
-            case 64: return launch_rope_d<64, true>(s, a, dwq, dwk, st);
-            case 128: return launch_rope_d<128, true>(s, a, dwq, dwk, st);
-            default: return launch_rope_d<256, true>(s, a, dwq, dwk, st);
-        }
-    }
     switch (s->D) {
-        case 64: return launch_rope_d<64, false>(s, a, nullptr, nullptr, st);
-        case 128: return launch_rope_d<128, false>(s, a, nullptr, nullptr, st);
-        default: return launch_rope_d<256, false>(s, a, nullptr, nullptr, st);
+        case 64: return launch_rope_d<64>(s, a, grads != nullptr, dwq, dwk, st);
+        case 128: return launch_rope_d<128>(s, a, grads != nullptr, dwq, dwk, st);
+        default: return launch_rope_d<256>(s, a, grads != nullptr, dwq, dwk, st);
     }
 }
 

@@ -26,7 +26,7 @@ struct RopeArgs {
     float* partial;                               // backward with a norm: [CTAs of a side][D] sums of g xhat, queries' CTAs first
     int heads[2], batch, n, rot, interleaved;
     float eps, amplitude;
-    int lgT[2], parts[2];                         // of a side: tokens per tile (log), parts that the heads of a tile are cut into
+    int lgT[2], parts;                            // tokens per tile (log; forward: [0]), parts that the heads of a tile are cut into (forward)
     int ctas[2];                                  // backward: CTAs of a side
 };
 
@@ -52,11 +52,6 @@ __device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
 __device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
     F2 r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-__device__ __forceinline__ F2 f2_neg(F2 a) {
-    F2 r;
-    r.v = a.v ^ 0x8000000080000000ull;
     return r;
 }
 
@@ -126,13 +121,16 @@ __device__ __forceinline__ void rope_pack(const RopeUnit& u, bool inter, uint4 (
     raw[0] = make_uint4(w[0], w[1], w[2], w[3]);
     raw[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
-// pairs (p, r) -> (p c - r s, p s + r c); `s` with the sign of the direction
-__device__ __forceinline__ void rope_turn(RopeUnit& u, const F2 (&c)[4], const F2 (&s)[4]) {
+// cosines, sines and negative sines of a unit's pairs; (p, r) -> (p c - r s, p s + r c)
+struct RopeAngles {
+    F2 c[4], s[4], ns[4];
+};
+__device__ __forceinline__ void rope_turn(RopeUnit& u, const RopeAngles& a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const F2 p = u.p[i], r = u.r[i];
-        u.p[i] = f2_fma(p, c[i], f2_neg(f2_mul(r, s[i])));
-        u.r[i] = f2_fma(p, s[i], f2_mul(r, c[i]));
+        u.p[i] = f2_fma(p, a.c[i], f2_mul(r, a.ns[i]));
+        u.r[i] = f2_fma(p, a.s[i], f2_mul(r, a.c[i]));
     }
 }
 __device__ __forceinline__ float rope_dot(const RopeUnit& a, const RopeUnit& b) {
@@ -149,214 +147,214 @@ __device__ __forceinline__ float rope_row_sum(float x) {
     return x;
 }
 
-// where a lane's unit lies in a row, and whether it is turned
+// where a lane's unit lies in a row
 struct RopePlace {
     int d0, d1;
-    bool turned, inter;
+    bool inter;
 };
 __device__ __forceinline__ RopePlace rope_place(const RopeArgs& a, int u) {
     RopePlace x;
-    x.turned = 16 * u < a.rot;
-    x.inter = a.interleaved || !x.turned;
+    x.inter = a.interleaved || 16 * u >= a.rot;
     x.d0 = x.inter ? 16 * u : 8 * u;
     x.d1 = x.inter ? 16 * u + 8 : a.rot / 2 + 8 * u;
     return x;
 }
-// the unit's numbers out of a row of fp32 (weights, in shared memory), and out of the table of cosines and sines; no rotation behind `rot`,
-// nor for a token that is not there (`live`), whose row of the table is not written
-__device__ __forceinline__ RopeUnit rope_weights(const float* w, const RopePlace& x) {
+// Weights and angles wait in shared memory as the units want them, 16 numbers each (firsts then seconds; cosines then sines), 4 numbers
+// apart: eight lanes read eight units' 16 bytes without asking a bank twice.
+constexpr int ROPE_UROW = 20;
+template <int D>
+__device__ __forceinline__ void rope_put_weights(float (*w)[ROPE_UROW], const RopeArgs& a, int side) {
+    for (int i = threadIdx.x; i < D; i += ROPE_THREADS) {
+        const int u = i / 16, e = i % 16;
+        const RopePlace x = rope_place(a, u);
+        // e-th number of the unit: pair e % 8, its first (e < 8) or second
+        const int pr = e % 8, d = x.inter ? x.d0 + 2 * pr + e / 8 : (e < 8 ? x.d0 : x.d1) + pr;
+        w[u][e] = a.w[side] ? dep_load(a.w[side] + d) : 1.f;
+    }
+}
+template <int D>
+__device__ __forceinline__ void rope_put_angles(float (*t)[D / 16][ROPE_UROW], const RopeArgs& a, int b, int t0, int T, float sign) {
+    for (int i = threadIdx.x; i < T * (D / 2); i += ROPE_THREADS) {
+        const int k = i / (D / 2), f = i % (D / 2);
+        float2 x = make_float2(1.f, 0.f);                     // (behind the rotated part, and where there is no token)
+        if (2 * f < a.rot && t0 + k < a.n) x = rope_cos_sin(a, a.positions ? dep_load(a.positions + (size_t)b * a.n + t0 + k) : t0 + k, f);
+        t[k][f / 8][f % 8] = x.x;
+        t[k][f / 8][8 + f % 8] = sign * x.y;
+    }
+}
+__device__ __forceinline__ RopeUnit rope_get(const float* row) {
     RopeUnit u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (x.inter) {
-            const float4 t = *reinterpret_cast<const float4*>(w + x.d0 + 4 * i);
-            u.p[i] = f2(t.x, t.z);
-            u.r[i] = f2(t.y, t.w);
-        } else {
-            const float2 p = *reinterpret_cast<const float2*>(w + x.d0 + 2 * i), r = *reinterpret_cast<const float2*>(w + x.d1 + 2 * i);
-            u.p[i] = f2(p.x, p.y);
-            u.r[i] = f2(r.x, r.y);
-        }
+        const float4 t = *reinterpret_cast<const float4*>(row + 4 * i);
+        F2(&to)[4] = i < 2 ? u.p : u.r;
+        to[2 * (i & 1)] = f2(t.x, t.y);
+        to[2 * (i & 1) + 1] = f2(t.z, t.w);
     }
     return u;
 }
-__device__ __forceinline__ void rope_angles(const float2* row, int unit, const RopePlace& x, int half, bool live, float sign, F2 (&c)[4], F2 (&s)[4]) {
+__device__ __forceinline__ RopeAngles rope_get_angles(const float* row) {
+    const RopeUnit u = rope_get(row);
+    RopeAngles x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float2 t[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int f = 8 * unit + 2 * i + e;
-            t[e] = live && x.turned && f < half ? row[f] : make_float2(1.f, 0.f);
-        }
-        c[i] = f2(t[0].x, t[1].x);
-        s[i] = f2(sign * t[0].y, sign * t[1].y);
+        x.c[i] = u.p[i];
+        x.s[i] = u.r[i];
+        const float2 t = f2_get(u.r[i]);
+        x.ns[i] = f2(-t.x, -t.y);
     }
+    return x;
 }
 
-// Forward: a CTA takes 2^lgT tokens of one side (queries or keys) and as many of its heads as four passes cover, so that all it reads is
-// under way at once; the cosines and sines of its tokens are worked out meanwhile.  A thread's token and place in the row are the same in
-// every pass.  Grid: tiles of tokens x parts of heads, queries first.
-constexpr int ROPE_PASSES = 4;
+// Forward: a CTA takes 2^lgT tokens and all their heads, queries then keys (a part of them where there are few tokens).  A thread's token
+// and place in the row are the same in every pass, and so the angles, worked out once per token, stay in registers.  A pass's rows
+// are on their way while the pass before is worked on.
 template <int D>
-__global__ void __launch_bounds__(ROPE_THREADS)
+__global__ void __launch_bounds__(ROPE_THREADS, 3)
 qk_norm_rope_kernel(const RopeArgs a) {
     using C = RopeCfg<D>;
-    __shared__ float2 cs_s[ROPE_TOKENS][D / 2 + 1];           // [token][pair]
-    __shared__ float w_s[D];
+    __shared__ __align__(16) float cs_s[ROPE_TOKENS][D / 16][ROPE_UROW];
+    __shared__ __align__(16) float w_s[2][D / 16][ROPE_UROW];
     const int unit = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
-    const int tiles_q = a.batch * ((a.n + (1 << a.lgT[0]) - 1) >> a.lgT[0]);
-    const int side = blockIdx.x >= tiles_q * a.parts[0];
-    const int lgT = a.lgT[side], T = 1 << lgT, per_seq = (a.n + T - 1) >> lgT;
-    const int id = blockIdx.x - (side ? tiles_q * a.parts[0] : 0);
-    const int part = id % a.parts[side], tile = id / a.parts[side], b = tile / per_seq, t0 = (tile - b * per_seq) << lgT;
-    const int tok = rs & (T - 1), hstep = C::RPP >> lgT, h0 = part * ROPE_PASSES * hstep + (rs >> lgT), half = a.rot >> 1;
+    const int lgT = a.lgT[0], T = 1 << lgT, per_seq = (a.n + T - 1) >> lgT;
+    const int part = blockIdx.x % a.parts, tile = blockIdx.x / a.parts, b = tile / per_seq, t0 = (tile - b * per_seq) << lgT;
+    const int tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT;
+    const int Hq = a.heads[0], all = Hq + a.heads[1], passes = (all + hstep - 1) / hstep;
+    const int h_begin = passes * part / a.parts * hstep, h_end = min(passes * (part + 1) / a.parts * hstep, all);
     const RopePlace at = rope_place(a, unit);
-    const bool live = t0 + tok < a.n, norm = a.w[side] != nullptr;
+    const bool live = t0 + tok < a.n;
     dep_wait();
     dep_trigger();
-    const __nv_bfloat16* src = a.x[side] + (size_t)b * a.x_b[side] + (size_t)(t0 + tok) * a.x_n[side];
-    uint4 raw[ROPE_PASSES][2];
-#pragma unroll
-    for (int i = 0; i < ROPE_PASSES; ++i) {
-        const int h = h0 + i * hstep;
-        raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
-        if (live && h < a.heads[side]) {
-            const __nv_bfloat16* p = src + (size_t)h * a.x_h[side];
-            raw[i][0] = *reinterpret_cast<const uint4*>(p + at.d0);
-            raw[i][1] = *reinterpret_cast<const uint4*>(p + at.d1);
+    const __nv_bfloat16 *xq = a.x[0] + (size_t)b * a.x_b[0] + (size_t)(t0 + tok) * a.x_n[0], *xk = a.x[1] + (size_t)b * a.x_b[1] + (size_t)(t0 + tok) * a.x_n[1];
+    __nv_bfloat16 *oq = a.out[0] + (size_t)b * a.o_b[0] + (size_t)(t0 + tok) * a.o_n[0], *ok = a.out[1] + (size_t)b * a.o_b[1] + (size_t)(t0 + tok) * a.o_n[1];
+    uint4 raw[2];
+    auto load = [&](int h) {
+        raw[0] = raw[1] = make_uint4(0, 0, 0, 0);
+        if (live && h < h_end) {
+            const __nv_bfloat16* p = h < Hq ? xq + (size_t)h * a.x_h[0] : xk + (size_t)(h - Hq) * a.x_h[1];
+            raw[0] = *reinterpret_cast<const uint4*>(p + at.d0);
+            raw[1] = *reinterpret_cast<const uint4*>(p + at.d1);
         }
-    }
-    for (int i = threadIdx.x; i < half << lgT; i += ROPE_THREADS) {
-        const int t = i / half, f = i - t * half;
-        if (t0 + t < a.n) cs_s[t][f] = rope_cos_sin(a, a.positions ? dep_load(a.positions + (size_t)b * a.n + t0 + t) : t0 + t, f);
-    }
-    for (int d = threadIdx.x; d < D; d += ROPE_THREADS) w_s[d] = norm ? dep_load(a.w[side] + d) : 1.f;
+    };
+    load(h_begin + hofs);
+    rope_put_weights<D>(w_s[0], a, 0);
+    rope_put_weights<D>(w_s[1], a, 1);
+    rope_put_angles<D>(cs_s, a, b, t0, T, 1.f);
     __syncthreads();
-    F2 c[4], sn[4];
-    rope_angles(cs_s[tok], unit, at, half, live, 1.f, c, sn);
-    __nv_bfloat16* dst = a.out[side] + (size_t)b * a.o_b[side] + (size_t)(t0 + tok) * a.o_n[side];
-#pragma unroll
-    for (int i = 0; i < ROPE_PASSES; ++i) {
-        const int h = h0 + i * hstep;
-        if (part * ROPE_PASSES * hstep + i * hstep >= a.heads[side]) break;      // (the same for all threads)
-        RopeUnit x = rope_unpack(raw[i], at.inter);
-        if (norm) {
-            const float r = 1.f / sqrtf(rope_row_sum<C::LPR>(rope_dot(x, x)) * (1.f / D) + a.eps);
+    const RopeAngles ang = rope_get_angles(cs_s[tok][unit]);
+    for (int hb = h_begin; hb < h_end; hb += hstep) {
+        const int h = hb + hofs, side = h >= Hq;
+        RopeUnit x = rope_unpack(raw, at.inter);
+        load(h + hstep);
+        if (a.w[0] || a.w[1]) {                                // (one of them alone: the others' weights are 1 and their scale too)
+            const float scale = rsqrtf(rope_row_sum<C::LPR>(rope_dot(x, x)) * (1.f / D) + a.eps);
+            const float r = a.w[side] ? scale : 1.f;
             const F2 r2 = f2(r, r);
-            const RopeUnit w = rope_weights(w_s, at);
+            const RopeUnit w = rope_get(w_s[side][unit]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 x.p[e] = f2_mul(f2_mul(x.p[e], r2), w.p[e]);
                 x.r[e] = f2_mul(f2_mul(x.r[e], r2), w.r[e]);
             }
         }
-        rope_turn(x, c, sn);
-        if (live && h < a.heads[side]) {
+        rope_turn(x, ang);
+        if (live && h < h_end) {
             uint4 out[2];
             rope_pack(x, at.inter, out);
-            __nv_bfloat16* p = dst + (size_t)h * a.o_h[side];
+            __nv_bfloat16* p = side ? ok + (size_t)(h - Hq) * a.o_h[1] : oq + (size_t)h * a.o_h[0];
             *reinterpret_cast<uint4*>(p + at.d0) = out[0];
             *reinterpret_cast<uint4*>(p + at.d1) = out[1];
         }
     }
 }
 
-// Backward: the CTAs of a side walk its tiles of tokens, all heads of a tile, two rows a thread under way; the sums over rows of g xhat
-// stay in registers to the end, then go to `partial`.
+// Backward: the CTAs of a side walk its tiles of tokens, all heads of a tile, a row's loads under way while the row before is worked on; the
+// sums over rows of g xhat stay in registers to the end, then go to `partial`.
 template <int D>
 __global__ void __launch_bounds__(ROPE_THREADS, 2)
 qk_norm_rope_bwd_kernel(const RopeArgs a) {
     using C = RopeCfg<D>;
-    constexpr int AHEAD = 2;
-    constexpr size_t TABLES = sizeof(float2) * 2 * ROPE_TOKENS * (D / 2 + 1), SUMS = sizeof(float) * C::RPP * (D + 4);
+    constexpr size_t TABLES = sizeof(float) * 2 * ROPE_TOKENS * (D / 16) * ROPE_UROW, SUMS = sizeof(float) * C::RPP * (D + 4);
     __shared__ __align__(16) unsigned char space_s[TABLES > SUMS ? TABLES : SUMS];
-    auto cs_s = reinterpret_cast<float2(*)[ROPE_TOKENS][D / 2 + 1]>(space_s);
+    auto cs_s = reinterpret_cast<float(*)[ROPE_TOKENS][D / 16][ROPE_UROW]>(space_s);       // two tables in turn
     auto red_s = reinterpret_cast<float(*)[D + 4]>(space_s);  // when the tables are through
-    __shared__ float w_s[D];
+    __shared__ __align__(16) float w_s[D / 16][ROPE_UROW];
     const int unit = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
     const int side = (int)blockIdx.x >= a.ctas[0];
     const int id = blockIdx.x - (side ? a.ctas[0] : 0);
     const int lgT = a.lgT[side], T = 1 << lgT, per_seq = (a.n + T - 1) >> lgT, tiles = a.batch * per_seq;
-    const int tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT, half = a.rot >> 1, H = a.heads[side];
+    const int tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT, H = a.heads[side];
     const RopePlace at = rope_place(a, unit);
     const bool norm = a.w[side] != nullptr;
+    const int64_t x_h = a.x_h[side], g_h = a.g_h[side], o_h = a.o_h[side];
     dep_wait();
     dep_trigger();
-    for (int d = threadIdx.x; d < D; d += ROPE_THREADS) w_s[d] = norm ? dep_load(a.w[side] + d) : 1.f;
+    rope_put_weights<D>(w_s, a, side);
     RopeUnit dw;
 #pragma unroll
     for (int e = 0; e < 4; ++e) dw.p[e] = dw.r[e] = f2(0.f, 0.f);
     int buf = 0;
     for (int tile = id; tile < tiles; tile += a.ctas[side], buf ^= 1) {
         const int b = tile / per_seq, t0 = (tile - b * per_seq) << lgT;
-        for (int i = threadIdx.x; i < half << lgT; i += ROPE_THREADS) {
-            const int t = i / half, f = i - t * half;
-            if (t0 + t < a.n) cs_s[buf][t][f] = rope_cos_sin(a, a.positions ? dep_load(a.positions + (size_t)b * a.n + t0 + t) : t0 + t, f);
-        }
-        __syncthreads();                                       // (the other table is free: its readers have passed this barrier)
         const bool live = t0 + tok < a.n;
-        F2 c[4], sn[4];
-        rope_angles(cs_s[buf][tok], unit, at, half, live, -1.f, c, sn);
         const __nv_bfloat16* xs = a.x[side] + (size_t)b * a.x_b[side] + (size_t)(t0 + tok) * a.x_n[side];
         const __nv_bfloat16* gs = a.g[side] + (size_t)b * a.g_b[side] + (size_t)(t0 + tok) * a.g_n[side];
         __nv_bfloat16* os = a.out[side] + (size_t)b * a.o_b[side] + (size_t)(t0 + tok) * a.o_n[side];
-        for (int hb = 0; hb < H; hb += AHEAD * hstep) {
-            uint4 xr[AHEAD][2], gr[AHEAD][2];
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const int h = hb + i * hstep + hofs;
-                xr[i][0] = xr[i][1] = gr[i][0] = gr[i][1] = make_uint4(0, 0, 0, 0);
-                if (live && h < H) {
-                    const __nv_bfloat16* p = gs + (size_t)h * a.g_h[side];
-                    gr[i][0] = *reinterpret_cast<const uint4*>(p + at.d0);
-                    gr[i][1] = *reinterpret_cast<const uint4*>(p + at.d1);
-                    if (norm) {
-                        const __nv_bfloat16* q = xs + (size_t)h * a.x_h[side];
-                        xr[i][0] = *reinterpret_cast<const uint4*>(q + at.d0);
-                        xr[i][1] = *reinterpret_cast<const uint4*>(q + at.d1);
-                    }
+        uint4 xr[2], gr[2];
+        auto load = [&](int h) {
+            xr[0] = xr[1] = gr[0] = gr[1] = make_uint4(0, 0, 0, 0);
+            if (live && h < H) {
+                const __nv_bfloat16* p = gs + h * g_h;
+                gr[0] = *reinterpret_cast<const uint4*>(p + at.d0);
+                gr[1] = *reinterpret_cast<const uint4*>(p + at.d1);
+                if (norm) {
+                    const __nv_bfloat16* q = xs + h * x_h;
+                    xr[0] = *reinterpret_cast<const uint4*>(q + at.d0);
+                    xr[1] = *reinterpret_cast<const uint4*>(q + at.d1);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const int h = hb + i * hstep + hofs;
-                if (hb + i * hstep >= H) break;                // (the same for all threads)
-                RopeUnit g = rope_unpack(gr[i], at.inter);
-                rope_turn(g, c, sn);
-                if (norm) {
-                    RopeUnit x = rope_unpack(xr[i], at.inter);
-                    const RopeUnit w = rope_weights(w_s, at);
-                    RopeUnit u;
+        };
+        load(hofs);
+        rope_put_angles<D>(cs_s[buf], a, b, t0, T, -1.f);
+        __syncthreads();                                       // (the other table is free: its readers have passed this barrier)
+        const RopeAngles ang = rope_get_angles(cs_s[buf][tok][unit]);
+        for (int hb = 0; hb < H; hb += hstep) {
+            const int h = hb + hofs;
+            const bool on = live && h < H;
+            RopeUnit g = rope_unpack(gr, at.inter), x = rope_unpack(xr, at.inter);
+            load(h + hstep);
+            rope_turn(g, ang);
+            if (norm) {
+                RopeUnit u;
+                {
+                    const RopeUnit w = rope_get(w_s[unit]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) { u.p[e] = f2_mul(g.p[e], w.p[e]); u.r[e] = f2_mul(g.r[e], w.r[e]); }
-                    float ss = rope_dot(x, x), dot = rope_dot(x, u);
-#pragma unroll
-                    for (int off = C::LPR / 2; off >= 1; off >>= 1) {
-                        ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                        dot += __shfl_xor_sync(0xffffffffu, dot, off);
-                    }
-                    const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-                    const float m = dot * r * (1.f / D);       // mean(u xhat)
-                    const bool on = live && h < H;             // (a row that is not there: x = 0, g = 0, and r may be infinite)
-                    const float rx = on ? r : 0.f;
-                    const F2 r2 = f2(r, r), rx2 = f2(rx, rx), mr2 = f2(-m * r, -m * r);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const F2 xp = f2_mul(x.p[e], rx2), xq = f2_mul(x.r[e], rx2);
-                        dw.p[e] = f2_fma(g.p[e], xp, dw.p[e]);
-                        dw.r[e] = f2_fma(g.r[e], xq, dw.r[e]);
-                        g.p[e] = f2_fma(xp, mr2, f2_mul(u.p[e], r2));
-                        g.r[e] = f2_fma(xq, mr2, f2_mul(u.r[e], r2));
-                    }
                 }
-                if (live && h < H) {
-                    uint4 out[2];
-                    rope_pack(g, at.inter, out);
-                    __nv_bfloat16* p = os + (size_t)h * a.o_h[side];
-                    *reinterpret_cast<uint4*>(p + at.d0) = out[0];
-                    *reinterpret_cast<uint4*>(p + at.d1) = out[1];
+                float ss = rope_dot(x, x), dot = rope_dot(x, u);
+#pragma unroll
+                for (int off = C::LPR / 2; off >= 1; off >>= 1) {
+                    ss += __shfl_xor_sync(0xffffffffu, ss, off);
+                    dot += __shfl_xor_sync(0xffffffffu, dot, off);
                 }
+                // (a row that is not there has x = 0 and g = 0, and without eps an infinite r)
+                const float r = on ? rsqrtf(ss * (1.f / D) + a.eps) : 0.f, m = dot * r * (1.f / D);        // m = mean(u xhat)
+                const F2 r2 = f2(r, r), mr2 = f2(-m * r, -m * r);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const F2 xp = f2_mul(x.p[e], r2), xq = f2_mul(x.r[e], r2);
+                    dw.p[e] = f2_fma(g.p[e], xp, dw.p[e]);
+                    dw.r[e] = f2_fma(g.r[e], xq, dw.r[e]);
+                    g.p[e] = f2_fma(xp, mr2, f2_mul(u.p[e], r2));
+                    g.r[e] = f2_fma(xq, mr2, f2_mul(u.r[e], r2));
+                }
+            }
+            if (on) {
+                uint4 out[2];
+                rope_pack(g, at.inter, out);
+                __nv_bfloat16* p = os + h * o_h;
+                *reinterpret_cast<uint4*>(p + at.d0) = out[0];
+                *reinterpret_cast<uint4*>(p + at.d1) = out[1];
             }
         }
     }
@@ -439,7 +437,7 @@ qk_norm_rope_odd_kernel(const RopeArgs a) {
             if (norm) {
                 ss = rope_row_sum<32>(ss);
                 if (BWD) dot = rope_row_sum<32>(dot);
-                const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps), m = dot * r * (1.f / D);
+                const float r = rsqrtf(ss * (1.f / D) + a.eps), m = dot * r * (1.f / D);
 #pragma unroll
                 for (int i = 0; i < UPL; ++i) {
                     x0[i] *= r;
@@ -501,13 +499,15 @@ norm_weight_grad_kernel(const float* partial, int ctas_q, int ctas_k, int D, flo
 
 size_t qk_norm_rope_bwd_workspace_bytes(const focus_shape* s) { return (size_t)ROPE_GRID * s->D * sizeof(float); }
 
-// tokens per tile of a side: as many as leave room for all its heads in a CTA's passes (16 rows of a token block are 4 KB in one piece when the
-// layout is head by head), fewer where that leaves multiprocessors without a tile
+// Tokens per tile: as many as `rows` rows of a CTA have room for all their heads (16 rows of a token block are 4 KB in one piece when the
+// layout is head by head), fewer where that leaves multiprocessors without a tile.
 static int rope_tile(int rows, int heads, int batch, int n) {
     int lg = 0;
-    while ((2 << lg) <= ROPE_TOKENS && (long long)(2 << lg) * heads <= rows && (long long)batch * cdiv(n, 2 << lg) >= ROPE_SMS) ++lg;
+    while ((2 << lg) <= ROPE_TOKENS && (long long)(2 << lg) * heads <= rows && (long long)batch * cdiv(n, 2 << lg) >= 2 * ROPE_SMS) ++lg;
     return lg;
 }
+
+constexpr int ROPE_PASSES = 8;                    // of a CTA over a tile's heads
 
 template <int D>
 static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq, float* dwk, cudaStream_t st) {
@@ -515,16 +515,21 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
     const bool odd = !a.interleaved && a.rot % 16 != 0;
     const long long tokens = (long long)s->batch * s->n;
     if (tokens >= (1ll << 30)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: batch * n (%lld) is too large for one call", tokens);
-    long long tiles[2], grid = 0;
+    if (!bwd && !odd) {
+        const int all = s->Hq + s->Hkv;
+        a.lgT[0] = rope_tile(ROPE_PASSES * C::RPP, all, s->batch, s->n);
+        const long long tiles = (long long)s->batch * cdiv(s->n, 1 << a.lgT[0]);
+        const int passes = cdiv(all, C::RPP >> a.lgT[0]);
+        // few tiles: a tile's passes over several CTAs
+        long long parts = tiles >= ROPE_SMS ? 1 : ROPE_SMS / tiles;
+        a.parts = (int)(parts > passes ? passes : parts);
+        return check_cuda(launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)(tiles * a.parts)), dim3(ROPE_THREADS), 0, st, a),
+                          "norm and rotation kernel launch");
+    }
+    long long tiles[2];
     for (int i = 0; i < 2; ++i) {
         a.lgT[i] = rope_tile(ROPE_PASSES * C::RPP, a.heads[i], s->batch, s->n);
-        a.parts[i] = cdiv(a.heads[i], ROPE_PASSES * (C::RPP >> a.lgT[i]));
         tiles[i] = (long long)s->batch * cdiv(s->n, 1 << a.lgT[i]);
-        grid += tiles[i] * a.parts[i];
-    }
-    if (!bwd && !odd) {
-        if (grid >= (1ll << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: too many heads and tokens for one call");
-        return check_cuda(launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)grid), dim3(ROPE_THREADS), 0, st, a), "norm and rotation kernel launch");
     }
     // CTAs of the two sides: in proportion to their heads, no more than they have tiles (or rows for the warps)
     const int places = bwd && !odd ? 2 * ROPE_SMS : ROPE_GRID;

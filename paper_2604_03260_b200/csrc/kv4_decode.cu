@@ -14,7 +14,8 @@
 //     instructions for 8 numbers; after it, 8).
 //   - The maximum that probabilities are relative to follows the scores only when one of them is 2^5 beyond it: a vote per tile instead
 //     of six exchanges.
-//   - Only attended keys become rows of a tile: a warp walks the masks, lists the attended keys, and takes 16 off the list at a time.
+//   - A warp walks the masks.  16 keys in a row of which most are attended are a tile as they lie (one address); of the others the attended
+//     ones are listed, and 16 off the list are a tile.
 // Rows come through a ring in shared memory, private to a warp, by asynchronous copies: one address per 16 bytes, none for the operands.
 // Every warp keeps its own maximum, sum and O; a CTA joins its warps, a second kernel the CTAs.
 #include "kv4_common.cuh"
@@ -29,6 +30,8 @@ constexpr int KD_UNIT = 64;              // keys: the grain of the split over CT
 constexpr int KD_SMS = 148;
 constexpr int KD_MAX_BATCH = 1024;
 constexpr int KD_LIST = 256;             // ring of listed keys: at most 15 left over, 128 new, and those of the stages
+constexpr int KD_BATCH = 128;            // keys whose masks a warp looks at together
+constexpr int KD_WHOLE = 12;             // of the 16 keys of an aligned tile: from here on all are loaded, attended or not
 constexpr int KD_STAGES = 3;             // tiles of 16 keys in a warp's ring
 constexpr float KD_LOG2E = 1.4426950408889634f;
 constexpr float KD_LN2 = 0.6931471805599453f;
@@ -142,7 +145,10 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     __shared__ int chunk_s[KD_MAX_BATCH / 32 + 1];       // first unit of every 32 sequences
     __shared__ int red_s[KD_WARPS][4];
     __shared__ uint2 key_s[KD_WARPS][KD_LIST];                 // listed keys: where their codes are (in 16 bytes) and scales (in 8)
-    __shared__ uint8_t bit_s[KD_WARPS][KD_LIST];               // which heads attend them
+    __shared__ uint2 tile_s[KD_WARPS][KD_BATCH / 16];          // where the tiles that are taken as they lie start
+    // which heads attend a key: of the listed keys, and of the last four batches that had whole tiles (the tiles under way, at most two, are
+    // of two of them, and a third is being written)
+    __shared__ uint8_t bit_s[KD_WARPS][KD_LIST + 4 * KD_BATCH];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, qd = lane & 3;
     const int Hkv = c.Hkv, lgP = c.lgP;
@@ -250,7 +256,9 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         const int quarter = kd_cdiv(t1 - t0, 16 * KD_WARPS) * 16;
         const int k_end = min(t0 + (warp + 1) * quarter, t1);
         int next = t0 + warp * quarter;                        // keys walked so far
-        int tail = 0, issued = 0;                              // keys listed; 16 times the tiles whose copies are under way or done
+        int tail = 0, taken = 0;                               // keys listed, and taken off the list
+        uint32_t whole = 0, batches = 0;                       // whole tiles of the batch still to come; batches that had some
+        uint32_t under_way = 0, depth = 0;                     // where the tiles under way have their flags, 10 bits each; how many they are
         uint32_t pg[4], mk[4];                                 // pages of the next 128 keys (beyond any where there is no key), and their masks
         auto fetch = [&] {
 #pragma unroll
@@ -268,40 +276,51 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                     kv4_report(status, KV4_BAD_PAGE, b, j >> lgP, (int)pg[k]);     // its keys are passed over
             }
         };
-        // list attended keys until there is a tile more or the keys are through; the last tile is filled up with its last key, attended by no head
-        auto refill = [&] {
-            while (tail < issued + 16 && next < k_end) {
+        // look at the next batch: its whole tiles, and its other attended keys for the list
+        auto look = [&] {
+            uint32_t bits[4], any[4];
+            whole = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int j = next + 32 * k + lane;
+                bits[k] = 0;
+#pragma unroll
+                for (int gg = 0; gg < GP; ++gg)
+                    if (mq_all[gg] & mk[k]) bits[k] |= 1u << gg;
+                if (j >= near) bits[k] = (1u << G) - 1u;
+                if (pg[k] >= (uint32_t)c.num_pages) bits[k] = 0;
+                any[k] = __ballot_sync(0xffffffffu, bits[k] != 0u);
+                if (__popc(any[k] & 0xffffu) >= KD_WHOLE) { whole |= 1u << (2 * k); any[k] &= 0xffff0000u; }
+                if (__popc(any[k] >> 16) >= KD_WHOLE) { whole |= 2u << (2 * k); any[k] &= 0xffffu; }
+            }
+            const uint32_t slot = (next + lane) & pmask;
+            if (whole) {
+                uint8_t* flags = &bit_s[warp][KD_LIST + (batches & 3u) * KD_BATCH + lane];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int j = next + 32 * k + lane;
-                    uint32_t bits = 0;
-#pragma unroll
-                    for (int gg = 0; gg < GP; ++gg)
-                        if (mq_all[gg] & mk[k]) bits |= 1u << gg;
-                    if (j >= near) bits = (1u << G) - 1u;
-                    if (pg[k] >= (uint32_t)c.num_pages) bits = 0;
-                    const uint32_t any = __ballot_sync(0xffffffffu, bits != 0u);
-                    if (bits) {
-                        const int at = (tail + __popc(any & lower)) & (KD_LIST - 1);
-                        const uint32_t slot = j & pmask;
-                        key_s[warp][at] = make_uint2(pg[k] * page16 + slot * (D / 16), pg[k] * (2 * page16) + slot * (D / 64));
-                        bit_s[warp][at] = (uint8_t)bits;
+                    flags[32 * k] = (uint8_t)bits[k];
+                    if ((lane & 15) == 0) {
+                        const uint32_t sl = (slot + 32 * k) & pmask;
+                        tile_s[warp][2 * k + (lane >> 4)] = make_uint2(pg[k] * page16 + sl * (D / 16), pg[k] * (2 * page16) + sl * (D / 64));
                     }
-                    tail += __popc(any);
                 }
-                next += 128;
-                if (next < k_end) fetch();
-                __syncwarp();
+                ++batches;
             }
-            if ((tail & 15) && tail < issued + 16) {           // (the keys are through)
-                const uint2 pad = key_s[warp][(tail - 1) & (KD_LIST - 1)];
-                if (lane < 16 - (tail & 15)) {
-                    key_s[warp][(tail + lane) & (KD_LIST - 1)] = pad;
-                    bit_s[warp][(tail + lane) & (KD_LIST - 1)] = 0;
+            if (any[0] | any[1] | any[2] | any[3]) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if ((any[k] >> lane) & 1u) {
+                        const int at = (tail + __popc(any[k] & lower)) & (KD_LIST - 1);
+                        const uint32_t sl = (slot + 32 * k) & pmask;
+                        key_s[warp][at] = make_uint2(pg[k] * page16 + sl * (D / 16), pg[k] * (2 * page16) + sl * (D / 64));
+                        bit_s[warp][at] = (uint8_t)bits[k];
+                    }
+                    tail += __popc(any[k]);
                 }
-                tail = (tail + 15) & ~15;
-                __syncwarp();
             }
+            next += KD_BATCH;
+            if (next < k_end) fetch();
+            __syncwarp();
         };
         // copies of a tile: piece `lane % CPT` of token `lane / CPT`, and on by ROWSTEP tokens; then the scales
         const int ctok = lane / CPT, piece = lane % CPT;
@@ -311,23 +330,51 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         const int cdst = cv ? C::V_AT + ctok * C::VROW + (piece - CPT / 2) * 16 : ctok * C::KROW + (D == 256 ? (piece ^ ((ctok & 1) << 2)) * 16 : piece * 16);
         const int cstep = ROWSTEP * (cv ? C::VROW : C::KROW);
         constexpr int SP = D == 256 ? 2 : 1;                   // pieces of a row of scales
-        const unsigned char* ssrc = c.pages + c.scale_off + ((size_t)hk << lgP) * (D / 8) + (lane % SP) * 16;
+        const unsigned char* scales = c.pages + c.scale_off + ((size_t)hk << lgP) * (D / 8);
         const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
         uint32_t into = ring_u32;                              // the stage of the next tile's copies
+        // the next tile's copies, if there is one: a whole tile, or 16 keys off the list
         auto issue = [&] {
-            refill();
-            if (tail > issued) {
-                const uint2* keys = &key_s[warp][issued & (KD_LIST - 1)];
+            while (whole == 0 && tail - taken < 16 && next < k_end) look();
+            if (whole) {
+                const int t = __ffs(whole) - 1;
+                whole &= whole - 1;
+                const uint2 at = tile_s[warp][t];
+                const unsigned char* src = csrc + ctok * D + (size_t)at.x * 16;
+#pragma unroll
+                for (int i = 0; i < COPIES; ++i) kd_copy16(into + cdst + i * cstep, src + i * ROWSTEP * D);
+                if (lane < 16 * SP) {
+                    const unsigned char* sc = scales + lane * (D == 64 ? 8 : 16) + (size_t)at.y * 8;
+                    if constexpr (D == 64) kd_copy8(into + C::S_AT + lane * 8, sc);
+                    else kd_copy16(into + C::S_AT + lane * 16, sc);
+                }
+                under_way |= (KD_LIST + ((batches - 1) & 3u) * KD_BATCH + 16 * t) << (10 * depth);
+            } else if (tail > taken) {
+                if (tail - taken < 16) {                       // the last ones: filled up with the last key, attended by no head
+                    const uint2 pad = key_s[warp][(tail - 1) & (KD_LIST - 1)];
+                    if (lane < taken + 16 - tail) {
+                        key_s[warp][(tail + lane) & (KD_LIST - 1)] = pad;
+                        bit_s[warp][(tail + lane) & (KD_LIST - 1)] = 0;
+                    }
+                    tail = taken + 16;
+                    __syncwarp();
+                }
+                const uint2* keys = &key_s[warp][taken & (KD_LIST - 1)];
 #pragma unroll
                 for (int i = 0; i < COPIES; ++i) kd_copy16(into + cdst + i * cstep, csrc + (size_t)keys[ctok + i * ROWSTEP].x * 16);
                 if (lane < 16 * SP) {
-                    const unsigned char* src = ssrc + (size_t)keys[lane / SP].y * 8;
-                    if constexpr (D == 64) kd_copy8(into + C::S_AT + lane * 8, src);
-                    else kd_copy16(into + C::S_AT + lane * 16, src);
+                    const unsigned char* sc = scales + (lane % SP) * 16 + (size_t)keys[lane / SP].y * 8;
+                    if constexpr (D == 64) kd_copy8(into + C::S_AT + lane * 8, sc);
+                    else kd_copy16(into + C::S_AT + lane * 16, sc);
                 }
-                issued += 16;
-                into = into == ring_u32 + (KD_STAGES - 1) * C::STAGE ? ring_u32 : into + C::STAGE;
+                under_way |= (taken & (KD_LIST - 1)) << (10 * depth);
+                taken += 16;
+            } else {
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                return;
             }
+            ++depth;
+            into = into == ring_u32 + (KD_STAGES - 1) * C::STAGE ? ring_u32 : into + C::STAGE;
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         if (next < k_end) fetch();
@@ -373,12 +420,14 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 
         const unsigned char* st = ring;
-        for (int tile = 0;; tile += 16) {
+        while (true) {
             issue();                                           // into the stage that the tile before has left
-            if (tile >= issued) break;
+            if (depth == 0) break;
             asm volatile("cp.async.wait_group %0;" ::"n"(KD_STAGES - 1) : "memory");
             __syncwarp();
-            const uint8_t* flags = &bit_s[warp][(tile & (KD_LIST - 1)) + g];
+            const uint8_t* flags = &bit_s[warp][(under_way & 1023u) + g];
+            under_way >>= 10;
+            --depth;
             const uint32_t bt[2] = {(uint32_t)flags[0] >> (2 * qd), (uint32_t)flags[8] >> (2 * qd)};
             // ---- S = K Q^T: keys g and g + 8 of the tile, two sums in turn
             float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
@@ -496,7 +545,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 *reinterpret_cast<float2*>(&xw[warp][2 * qd + e][2 + (D / 8) * g + 2 * i]) = make_float2(acc[i][e], acc[i][2 + e]);
         }
         __syncthreads();
-        const bool whole = u0 == 0 && u1 == units;             // the head's only range: its result, no partial one
+        const bool alone = u0 == 0 && u1 == units;             // the head's only range: its result, no partial one
         for (int idx = threadIdx.x; idx < G * D; idx += KD_WARPS * 32) {
             const int gg = idx / D, d = idx % D;
             float M = -FLT_MAX;
@@ -509,7 +558,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 L = fmaf(xw[ww][gg][1], wgt, L);
                 a = fmaf(xw[ww][gg][2 + d], wgt, a);
             }
-            if (whole) {
+            if (alone) {
                 o[(size_t)b * o_sb + (size_t)(hk * G + gg) * o_sh + d] = __float2bfloat16(L == 0.f ? 0.f : a / L * c.v_scale);
                 if (d == 0) lse[(size_t)b * Hq + hk * G + gg] = L == 0.f ? -INFINITY : (M + log2f(L) - KD_PSHIFT) * KD_LN2;
             } else {

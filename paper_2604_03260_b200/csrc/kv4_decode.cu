@@ -29,10 +29,8 @@ constexpr int KD_WARPS = 4;
 constexpr int KD_UNIT = 64;              // keys: the grain of the split over CTAs, 16 per warp
 constexpr int KD_SMS = 148;
 constexpr int KD_MAX_BATCH = 1024;
-constexpr int KD_LIST = 256;             // ring of listed keys: at most 15 left over, 128 new, and those of the stages
+constexpr int KD_LIST = 256;             // ring of listed keys: at most 31 left over, 128 new, and those of the tiles under way
 constexpr int KD_BATCH = 128;            // keys whose masks a warp looks at together
-constexpr int KD_WHOLE = 12;             // of the 16 keys of an aligned tile: from here on all are loaded, attended or not
-constexpr int KD_STAGES = 3;             // tiles of 16 keys in a warp's ring
 constexpr float KD_LOG2E = 1.4426950408889634f;
 constexpr float KD_LN2 = 0.6931471805599453f;
 constexpr float KD_PSHIFT = 10.f;
@@ -41,12 +39,16 @@ constexpr float KD_SLACK = 5.f;          // 2^15 < 65504, the largest fp16 numbe
 template <int D> struct KdCfg {
     static constexpr int PER_SM = D == 256 ? 3 : 4;           // CTAs that fit an SM
     static constexpr int CTAS = KD_SMS * PER_SM;
-    // a stage: 16 rows of key codes, of value codes, of scales.  A lane reads 16 bytes of a key row (8 at D = 64), eight lanes two whole rows
+    static constexpr int SUB = D == 256 ? 1 : 2;              // a tile of the walk: 16 or 32 keys, whose copies, flags and vote are one
+    static constexpr int KEYS = 16 * SUB;
+    static constexpr int WHOLE = KEYS * 3 / 4;                // attended keys of an aligned tile from which on all are loaded
+    static constexpr int STAGES = D == 128 ? 2 : 3;           // tiles in a warp's ring
+    // a stage: rows of key codes, of value codes, of scales.  A lane reads 16 bytes of a key row (8 at D = 64), eight lanes two whole rows
     // (half rows at D = 256, where the halves of odd rows are swapped): no bank is asked twice.  Of a value row a lane reads an eighth, 4 rows
     // two apart at once: the rows are 16 bytes longer.
     static constexpr int KROW = D / 2, VROW = D / 2 + 16, SROW = D / 8;
-    static constexpr int V_AT = 16 * KROW, S_AT = V_AT + 16 * VROW, STAGE = S_AT + 16 * SROW;
-    static constexpr int RING = KD_WARPS * KD_STAGES * STAGE;
+    static constexpr int V_AT = KEYS * KROW, S_AT = V_AT + KEYS * VROW, STAGE = S_AT + KEYS * SROW;
+    static constexpr int RING = KD_WARPS * STAGES * STAGE;
     static constexpr int JOIN = KD_WARPS * KD_GMAX * (D + 2) * (int)sizeof(float);         // over the rings, when they are through
     static constexpr size_t SMEM = RING > JOIN ? RING : JOIN;
 };
@@ -55,6 +57,11 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t kd_transpose(uint32_t x) {           // an 8 x 8 matrix of fp16
     uint32_t r;
@@ -136,16 +143,17 @@ __global__ void __launch_bounds__(KD_WARPS * 32, KdCfg<D>::PER_SM)
 kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t q_sh, const uint32_t* mq_new, int batch, int Hq, int G, int n, int w,
                   float scale, float softcap, float* part, int2* ranges, __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, float* lse, int32_t* status) {
     using C = KdCfg<D>;
+    constexpr int SUB = C::SUB, KEYS = C::KEYS, STAGES = C::STAGES;
     constexpr int KW = D == 64 ? 2 : 4, KH = D == 256 ? 2 : 1;     // words a lane reads of a key row at once, and how often
     constexpr int VW = D / 64;                                 // words of a value row
     constexpr int MT = D / 16;                                 // 16-row tiles of O
     constexpr int CPT = D / 16;                                // 16-byte pieces of a token's codes
-    constexpr int COPIES = 16 * CPT / 32, ROWSTEP = 32 / CPT;  // copies per lane and tile; tokens apart
+    constexpr int COPIES = 16 * CPT / 32, ROWSTEP = 32 / CPT;  // copies per lane and 16 keys; tokens apart
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int chunk_s[KD_MAX_BATCH / 32 + 1];       // first unit of every 32 sequences
+    __shared__ int chunk_s[KD_MAX_BATCH / 32 + 1];             // first unit of every 32 sequences (more than 32 of them)
     __shared__ int red_s[KD_WARPS][4];
     __shared__ uint2 key_s[KD_WARPS][KD_LIST];                 // listed keys: where their codes are (in 16 bytes) and scales (in 8)
-    __shared__ uint2 tile_s[KD_WARPS][KD_BATCH / 16];          // where the tiles that are taken as they lie start
+    __shared__ uint2 tile_s[KD_WARPS][KD_BATCH / 16];          // where the 16 keys start of tiles that are taken as they lie
     // which heads attend a key: of the listed keys, and of the last four batches that had whole tiles (the tiles under way, at most two, are
     // of two of them, and a third is being written)
     __shared__ uint8_t bit_s[KD_WARPS][KD_LIST + 4 * KD_BATCH];
@@ -153,64 +161,73 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     const int g = lane >> 2, qd = lane & 3;
     const int Hkv = c.Hkv, lgP = c.lgP;
     const uint32_t pmask = (1u << lgP) - 1u, lower = (1u << lane) - 1u;
-    unsigned char* ring = smem + warp * KD_STAGES * C::STAGE;
+    unsigned char* ring = smem + warp * STAGES * C::STAGE;
     dep_wait();
     dep_trigger();
 
-    // ---- the plan (the host has seen to it that the list has fewer than 2^30 units)
+    // ---- the plan (the host has seen to it that the list has fewer than 2^29 units)
     KdPlan plan;
     int total;
-    const int chunks = kd_cdiv(batch, 32);
+    const int len0 = lane < batch ? kd_length(c, lane, n, blockIdx.x == 0 && warp == 0 ? status : nullptr) : 0;   // of the first 32 sequences
     {
         const int ctas = gridDim.x;
-        // (the first 128 lengths stay in a register)
-        const int len0 = (int)threadIdx.x < batch ? kd_length(c, threadIdx.x, n, blockIdx.x == 0 ? status : nullptr) : 0;
         int sum = kd_cdiv(len0, KD_UNIT);
-        for (int b = threadIdx.x + KD_WARPS * 32; b < batch; b += KD_WARPS * 32)
-            sum += kd_cdiv(kd_length(c, b, n, blockIdx.x == 0 ? status : nullptr), KD_UNIT);
-        sum = __reduce_add_sync(0xffffffffu, sum);
-        if (lane == 0) red_s[warp][0] = sum;
-        __syncthreads();
-        total = 0;
-#pragma unroll
-        for (int i = 0; i < KD_WARPS; ++i) total += red_s[i][0];
-        total *= Hkv;
+        // a wider batch: the warps share the rest out (every warp has the first 32)
+        if (batch > 32) {
+            int more = 0;
+            for (int b = 32 + threadIdx.x; b < batch; b += KD_WARPS * 32)
+                more += kd_cdiv(kd_length(c, b, n, blockIdx.x == 0 ? status : nullptr), KD_UNIT);
+            more = __reduce_add_sync(0xffffffffu, more);
+            if (lane == 0) red_s[warp][0] = more;
+            __syncthreads();
+            if (lane < KD_WARPS) sum += red_s[lane][0];
+        }
+        total = (int)__reduce_add_sync(0xffffffffu, sum) * Hkv;
         const int per0 = total > ctas ? kd_cdiv(total, ctas) : 1;
         // three lengths of a range to try with whole ranges per head: the shortest, an eighth and a quarter longer
         const int cand[3] = {per0, per0 + kd_cdiv(per0, 8), per0 + kd_cdiv(per0, 4)};
-        int cnt[3] = {0, 0, 0};
-        for (int b = threadIdx.x; b < batch; b += KD_WARPS * 32) {
-            const int u = kd_cdiv(b < KD_WARPS * 32 ? len0 : kd_length(c, b, n, nullptr), KD_UNIT);
+        int cnt[3];
 #pragma unroll
-            for (int i = 0; i < 3; ++i) cnt[i] += kd_cdiv(u, cand[i]);
-        }
+        for (int i = 0; i < 3; ++i) cnt[i] = kd_cdiv(kd_cdiv(len0, KD_UNIT), cand[i]);
+        if (batch > 32) {
+            int more[3] = {0, 0, 0};
+            for (int b = 32 + threadIdx.x; b < batch; b += KD_WARPS * 32) {
+                const int u = kd_cdiv(kd_length(c, b, n, nullptr), KD_UNIT);
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            cnt[i] = __reduce_add_sync(0xffffffffu, cnt[i]);
-            if (lane == 0) red_s[warp][1 + i] = cnt[i];
+                for (int i = 0; i < 3; ++i) more[i] += kd_cdiv(u, cand[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                more[i] = __reduce_add_sync(0xffffffffu, more[i]);
+                if (lane == 0) red_s[warp][1 + i] = more[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (lane < KD_WARPS) cnt[i] += red_s[lane][1 + i];
         }
-        __syncthreads();
         plan.per = per0;
         plan.aligned = 0;
 #pragma unroll
-        for (int i = 2; i >= 0; --i) {
-            int wanted = 0;
-#pragma unroll
-            for (int j = 0; j < KD_WARPS; ++j) wanted += red_s[j][1 + i];
-            if (wanted * Hkv <= ctas) { plan.per = cand[i]; plan.aligned = 1; }
-        }
-        // first unit of every 32 sequences, by the first warp
-        if (warp == 0) {
-            int base = 0;
-            for (int b0 = 0; b0 < batch; b0 += 32) {
-                const int u = b0 + lane < batch ? kd_padded(b0 == 0 ? len0 : kd_length(c, b0 + lane, n, nullptr), plan) * Hkv : 0;
-                if (lane == 0) chunk_s[b0 / 32] = base;
-                base += __reduce_add_sync(0xffffffffu, u);
+        for (int i = 2; i >= 0; --i)
+            if ((int)__reduce_add_sync(0xffffffffu, cnt[i]) * Hkv <= ctas) { plan.per = cand[i]; plan.aligned = 1; }
+        int u = kd_padded(len0, plan) * Hkv;
+        if (batch > 32) {
+            // first unit of every 32 sequences, by the first warp
+            if (warp == 0) {
+                int base = 0;
+                for (int b0 = 0; b0 < batch; b0 += 32) {
+                    if (b0 > 0) u = b0 + lane < batch ? kd_padded(kd_length(c, b0 + lane, n, nullptr), plan) * Hkv : 0;
+                    if (lane == 0) chunk_s[b0 / 32] = base;
+                    base += __reduce_add_sync(0xffffffffu, u);
+                }
+                if (lane == 0) chunk_s[kd_cdiv(batch, 32)] = base;
             }
-            if (lane == 0) chunk_s[chunks] = base;
+            __syncthreads();
+            total = chunk_s[kd_cdiv(batch, 32)];
+        } else {
+            total = __reduce_add_sync(0xffffffffu, u);
         }
-        __syncthreads();
-        total = chunk_s[chunks];
     }
 
     const int f_end = min(((int)blockIdx.x + 1) * plan.per, total);
@@ -218,10 +235,12 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         // ---- the sequence and head of unit f (every warp for itself)
         int b, len, start;
         {
-            int ch = 0;
-            while (chunk_s[ch + 1] <= f) ++ch;
-            const int mine = ch * 32 + lane;
-            const int l = mine < batch ? kd_length(c, mine, n, nullptr) : 0;
+            int ch = 0, base = 0, l = len0;
+            if (batch > 32) {
+                while (chunk_s[ch + 1] <= f) ++ch;
+                base = chunk_s[ch];
+                if (ch > 0) l = ch * 32 + lane < batch ? kd_length(c, ch * 32 + lane, n, nullptr) : 0;
+            }
             const int u = kd_padded(l, plan) * Hkv;
             int incl = u;
 #pragma unroll
@@ -229,7 +248,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 const int t = __shfl_up_sync(0xffffffffu, incl, off);
                 if (lane >= off) incl += t;
             }
-            incl += chunk_s[ch];
+            incl += base;
             const int at = __ffs(__ballot_sync(0xffffffffu, incl > f)) - 1;
             b = ch * 32 + at;
             len = __shfl_sync(0xffffffffu, l, at);
@@ -245,30 +264,26 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         if (u0 >= u1) continue;                                // (the padding of a head)
         const int t0 = u0 * KD_UNIT, t1 = min(u1 * KD_UNIT, len), near = len - 1 - w;      // keys from `near` on are local
 
-        uint32_t mq_all[GP];
-#pragma unroll
-        for (int gg = 0; gg < GP; ++gg) mq_all[gg] = gg < G ? dep_load(mq_new + (size_t)b * Hq + hk * G + gg) : 0u;
-
-        // ---- this warp's keys: a quarter of the range, in whole tiles
+        // ---- this warp's keys: a quarter of the range, in whole tiles.  Pages are on their way two batches ahead, masks one
         const int32_t* table = c.table + (size_t)b * c.max_pages;
         const unsigned char* masks = c.pages + c.mask_off + ((size_t)hk << lgP) * 4;
         const uint32_t page16 = (uint32_t)(c.page_bytes / 16);
-        const int quarter = kd_cdiv(t1 - t0, 16 * KD_WARPS) * 16;
+        const int quarter = kd_cdiv(t1 - t0, KEYS * KD_WARPS) * KEYS;
         const int k_end = min(t0 + (warp + 1) * quarter, t1);
-        int next = t0 + warp * quarter;                        // keys walked so far
-        int tail = 0, taken = 0;                               // keys listed, and taken off the list
-        uint32_t whole = 0, batches = 0;                       // whole tiles of the batch still to come; batches that had some
-        uint32_t under_way = 0, depth = 0;                     // where the tiles under way have their flags, 10 bits each; how many they are
-        uint32_t pg[4], mk[4];                                 // pages of the next 128 keys (beyond any where there is no key), and their masks
-        auto fetch = [&] {
+        int next = t0 + warp * quarter;                        // keys looked at so far
+        uint32_t pg[4], pg_next[4], mk[4];                     // pages of the next 128 keys (beyond any where there is no key) and of the 128 after, masks
+        auto fetch_pages = [&](int from) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int j = next + 32 * k + lane;
-                pg[k] = j < k_end ? (uint32_t)dep_load(table + (j >> lgP)) : 0xffffffffu;
+                const int j = from + 32 * k + lane;
+                pg_next[k] = j < k_end ? (uint32_t)dep_load(table + (j >> lgP)) : 0xffffffffu;
             }
+        };
+        auto fetch_masks = [&](int from) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int j = next + 32 * k + lane;
+                const int j = from + 32 * k + lane;
+                pg[k] = pg_next[k];
                 mk[k] = 0u;
                 if (pg[k] < (uint32_t)c.num_pages)
                     mk[k] = dep_load(reinterpret_cast<const uint32_t*>(masks + (size_t)pg[k] * c.page_bytes) + (j & pmask));
@@ -276,6 +291,15 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                     kv4_report(status, KV4_BAD_PAGE, b, j >> lgP, (int)pg[k]);     // its keys are passed over
             }
         };
+        fetch_pages(next);
+        uint32_t mq_all[GP];
+#pragma unroll
+        for (int gg = 0; gg < GP; ++gg) mq_all[gg] = gg < G ? dep_load(mq_new + (size_t)b * Hq + hk * G + gg) : 0u;
+        fetch_masks(next);
+        fetch_pages(next + KD_BATCH);
+        int tail = 0, taken = 0;                               // keys listed, and taken off the list
+        uint32_t whole = 0, batches = 0;                       // whole tiles of the batch still to come; batches that had some
+        uint32_t under_way = 0, depth = 0;                     // where the tiles under way have their flags, 10 bits each; how many they are
         // look at the next batch: its whole tiles, and its other attended keys for the list
         auto look = [&] {
             uint32_t bits[4], any[4];
@@ -290,18 +314,23 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 if (j >= near) bits[k] = (1u << G) - 1u;
                 if (pg[k] >= (uint32_t)c.num_pages) bits[k] = 0;
                 any[k] = __ballot_sync(0xffffffffu, bits[k] != 0u);
-                if (__popc(any[k] & 0xffffu) >= KD_WHOLE) { whole |= 1u << (2 * k); any[k] &= 0xffff0000u; }
-                if (__popc(any[k] >> 16) >= KD_WHOLE) { whole |= 2u << (2 * k); any[k] &= 0xffffu; }
+                if constexpr (SUB == 2) {
+                    if (__popc(any[k]) >= C::WHOLE) { whole |= 1u << k; any[k] = 0; }
+                } else {
+                    if (__popc(any[k] & 0xffffu) >= C::WHOLE) { whole |= 1u << (2 * k); any[k] &= 0xffff0000u; }
+                    if (__popc(any[k] >> 16) >= C::WHOLE) { whole |= 2u << (2 * k); any[k] &= 0xffffu; }
+                }
             }
-            const uint32_t slot = (next + lane) & pmask;
+            const uint32_t slot = next + lane;
             if (whole) {
                 uint8_t* flags = &bit_s[warp][KD_LIST + (batches & 3u) * KD_BATCH + lane];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     flags[32 * k] = (uint8_t)bits[k];
                     if ((lane & 15) == 0) {
-                        const uint32_t sl = (slot + 32 * k) & pmask;
-                        tile_s[warp][2 * k + (lane >> 4)] = make_uint2(pg[k] * page16 + sl * (D / 16), pg[k] * (2 * page16) + sl * (D / 64));
+                        // (a page beyond the pool, or none, in a whole tile of 32: its 16 keys are attended by no head, and any rows do for them)
+                        const uint32_t p = pg[k] < (uint32_t)c.num_pages ? pg[k] : 0u, sl = (slot + 32 * k) & pmask;
+                        tile_s[warp][2 * k + (lane >> 4)] = make_uint2(p * page16 + sl * (D / 16), p * (2 * page16) + sl * (D / 64));
                     }
                 }
                 ++batches;
@@ -319,10 +348,13 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 }
             }
             next += KD_BATCH;
-            if (next < k_end) fetch();
+            if (next < k_end) {
+                fetch_masks(next);
+                fetch_pages(next + KD_BATCH);
+            }
             __syncwarp();
         };
-        // copies of a tile: piece `lane % CPT` of token `lane / CPT`, and on by ROWSTEP tokens; then the scales
+        // copies of 16 keys: piece `lane % CPT` of token `lane / CPT`, and on by ROWSTEP tokens; then the scales
         const int ctok = lane / CPT, piece = lane % CPT;
         const bool cv = piece >= CPT / 2;
         const unsigned char* csrc = c.pages + ((size_t)hk << lgP) * D + piece * 16;
@@ -333,88 +365,100 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         const unsigned char* scales = c.pages + c.scale_off + ((size_t)hk << lgP) * (D / 8);
         const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
         uint32_t into = ring_u32;                              // the stage of the next tile's copies
-        // the next tile's copies, if there is one: a whole tile, or 16 keys off the list
+        // the next tile's copies, if there is one: a whole tile, or KEYS keys off the list
         auto issue = [&] {
-            while (whole == 0 && tail - taken < 16 && next < k_end) look();
+            while (whole == 0 && tail - taken < KEYS && next < k_end) look();
+            uint32_t flags;
             if (whole) {
                 const int t = __ffs(whole) - 1;
                 whole &= whole - 1;
-                const uint2 at = tile_s[warp][t];
-                const unsigned char* src = csrc + ctok * D + (size_t)at.x * 16;
 #pragma unroll
-                for (int i = 0; i < COPIES; ++i) kd_copy16(into + cdst + i * cstep, src + i * ROWSTEP * D);
-                if (lane < 16 * SP) {
-                    const unsigned char* sc = scales + lane * (D == 64 ? 8 : 16) + (size_t)at.y * 8;
-                    if constexpr (D == 64) kd_copy8(into + C::S_AT + lane * 8, sc);
-                    else kd_copy16(into + C::S_AT + lane * 16, sc);
+                for (int u = 0; u < SUB; ++u) {
+                    const uint2 at = tile_s[warp][t * SUB + u];
+                    const unsigned char* src = csrc + ctok * D + (size_t)at.x * 16;
+#pragma unroll
+                    for (int i = 0; i < COPIES; ++i) kd_copy16(into + cdst + (u * COPIES + i) * cstep, src + i * ROWSTEP * D);
+                    if (lane < 16 * SP) {
+                        const unsigned char* sc = scales + lane * (D == 64 ? 8 : 16) + (size_t)at.y * 8;
+                        const uint32_t to = into + C::S_AT + (u * 16 * SP + lane) * (D == 64 ? 8 : 16);
+                        if constexpr (D == 64) kd_copy8(to, sc);
+                        else kd_copy16(to, sc);
+                    }
                 }
-                under_way |= (KD_LIST + ((batches - 1) & 3u) * KD_BATCH + 16 * t) << (10 * depth);
+                flags = KD_LIST + ((batches - 1) & 3u) * KD_BATCH + KEYS * t;
             } else if (tail > taken) {
-                if (tail - taken < 16) {                       // the last ones: filled up with the last key, attended by no head
+                if (tail - taken < KEYS) {                     // the last ones: filled up with the last key, attended by no head
                     const uint2 pad = key_s[warp][(tail - 1) & (KD_LIST - 1)];
-                    if (lane < taken + 16 - tail) {
+                    if (lane < taken + KEYS - tail) {
                         key_s[warp][(tail + lane) & (KD_LIST - 1)] = pad;
                         bit_s[warp][(tail + lane) & (KD_LIST - 1)] = 0;
                     }
-                    tail = taken + 16;
+                    tail = taken + KEYS;
                     __syncwarp();
                 }
-                const uint2* keys = &key_s[warp][taken & (KD_LIST - 1)];
+                flags = taken & (KD_LIST - 1);
+                const uint2* keys = &key_s[warp][flags];
 #pragma unroll
-                for (int i = 0; i < COPIES; ++i) kd_copy16(into + cdst + i * cstep, csrc + (size_t)keys[ctok + i * ROWSTEP].x * 16);
-                if (lane < 16 * SP) {
-                    const unsigned char* sc = scales + (lane % SP) * 16 + (size_t)keys[lane / SP].y * 8;
-                    if constexpr (D == 64) kd_copy8(into + C::S_AT + lane * 8, sc);
-                    else kd_copy16(into + C::S_AT + lane * 16, sc);
+                for (int i = 0; i < COPIES * SUB; ++i) kd_copy16(into + cdst + i * cstep, csrc + (size_t)keys[ctok + i * ROWSTEP].x * 16);
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    if (lane < 16 * SP) {
+                        const unsigned char* sc = scales + (lane % SP) * 16 + (size_t)keys[u * 16 + lane / SP].y * 8;
+                        const uint32_t to = into + C::S_AT + (u * 16 * SP + lane) * (D == 64 ? 8 : 16);
+                        if constexpr (D == 64) kd_copy8(to, sc);
+                        else kd_copy16(to, sc);
+                    }
                 }
-                under_way |= (taken & (KD_LIST - 1)) << (10 * depth);
-                taken += 16;
+                taken += KEYS;
             } else {
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 return;
             }
+            under_way |= flags << (10 * depth);
             ++depth;
-            into = into == ring_u32 + (KD_STAGES - 1) * C::STAGE ? ring_u32 : into + C::STAGE;
+            into = into == ring_u32 + (STAGES - 1) * C::STAGE ? ring_u32 : into + C::STAGE;
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        if (next < k_end) fetch();
-#pragma unroll
-        for (int i = 0; i < KD_STAGES - 1; ++i) issue();
-
         // ---- Q as the column operand: this lane has, of head g, the dimensions of its pieces of a key row
-        uint32_t qb[MT][2];
-        float qf;                                              // what a score of this lane's head is multiplied by
+        uint32_t raw[D / 8];
         {
             const __nv_bfloat16* qrow = q + (size_t)b * q_sb + (size_t)(hk * G + (g < G ? g : 0)) * q_sh;
-            uint32_t raw[D / 8];
-            float top = 0.f;
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
                 const int d = (i / (4 * KW)) * (D / 2) + qd * (8 * KW) + 2 * (i % (4 * KW));
                 raw[i] = g < G ? *reinterpret_cast<const uint32_t*>(qrow + d) : 0u;
-                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[i] << 16)), fabsf(__uint_as_float(raw[i] & 0xffff0000u))));
             }
+        }
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) issue();
+        uint32_t qb[MT][2];
+        // a score is y = S (or, with a cap, tanh(S * cap_in)) times `mul`, in log2 units; per head of this lane's two
+        float mul[2], cap_in[2];
+        {
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[i] << 16)), fabsf(__uint_as_float(raw[i] & 0xffff0000u))));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             // 2^13 <= top * up < 2^14 (a head of zeros or of denormal numbers: as if its largest were 2^-100)
             const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
-            const float up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
-            qf = __uint_as_float((uint32_t)(e - 13 + 127) << 23);
+            const float up = __uint_as_float((uint32_t)(13 - e + 127) << 23), down = __uint_as_float((uint32_t)(e - 13 + 127) << 23);
 #pragma unroll
             for (int i = 0; i < D / 8; ++i)
                 qb[i >> 1][i & 1] = kd_pack(__uint_as_float(raw[i] << 16) * up, __uint_as_float(raw[i] & 0xffff0000u) * up);
-        }
-        // scores come out as (key, head) with heads 2 qd and 2 qd + 1 in this lane; in log2 units they are S * mul, or tanh(S * mul) * cap2
-        float mul[2];
+            // scores come out as (key, head) with heads 2 qd and 2 qd + 1 in this lane
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float x = __shfl_sync(0xffffffffu, qf, (2 * qd + e) * 4) * c.k_scale * scale;
-            mul[e] = softcap > 0.f ? x / softcap : x * KD_LOG2E;
+            for (int i = 0; i < 2; ++i) {
+                const float x = __shfl_sync(0xffffffffu, down, (2 * qd + i) * 4) * c.k_scale * scale;
+                mul[i] = softcap > 0.f ? softcap * KD_LOG2E : x * KD_LOG2E;
+                cap_in[i] = softcap > 0.f ? x / softcap : 0.f;
+            }
         }
-        const float cap2 = softcap * KD_LOG2E;
 
-        // of heads 2 qd, 2 qd + 1; l: this lane's keys alone.  No score is as low as the first reference but minus infinity
-        float m_ref[2] = {-FLT_MAX, -FLT_MAX}, l_run[2] = {0.f, 0.f};
+        // of heads 2 qd, 2 qd + 1; l: this lane's keys alone.  A reference that no key has moved yet is FLT_MAX below everything, and its limit
+        // for y is such that any score but minus infinity is beyond it
+        float m_ref[2] = {-FLT_MAX, -FLT_MAX}, limit[2] = {-FLT_MAX, -FLT_MAX}, l_run[2] = {0.f, 0.f};
         float acc[MT][4];                                      // O: dimensions (D / 8) g + 2 i (elements 0, 1) and + 1 (2, 3), heads 2 qd, 2 qd + 1
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
@@ -423,105 +467,122 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         while (true) {
             issue();                                           // into the stage that the tile before has left
             if (depth == 0) break;
-            asm volatile("cp.async.wait_group %0;" ::"n"(KD_STAGES - 1) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
             __syncwarp();
             const uint8_t* flags = &bit_s[warp][(under_way & 1023u) + g];
             under_way >>= 10;
             --depth;
-            const uint32_t bt[2] = {(uint32_t)flags[0] >> (2 * qd), (uint32_t)flags[8] >> (2 * qd)};
-            // ---- S = K Q^T: keys g and g + 8 of the tile, two sums in turn
-            float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+            // ---- S = K Q^T: keys g (elements 0, 1) and g + 8 (2, 3) of 16 for heads 2 qd, 2 qd + 1; two sums in turn
+            float y[SUB][4];
 #pragma unroll
-            for (int h = 0; h < KH; ++h) {
-                uint32_t kr[2][KW], sc[2][2];
+            for (int u = 0; u < SUB; ++u) {
+                float s0[4], s1[4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    kd_read<KW>(kr[i], st + (g + 8 * i) * C::KROW + (KH == 2 ? (h ^ (g & 1)) * 64 : 0) + qd * (4 * KW));
-                    const unsigned char* sp = st + C::S_AT + (g + 8 * i) * C::SROW;
-                    const uint32_t two = kv4_scales(D == 64 ? (uint32_t)sp[qd] : (uint32_t) * reinterpret_cast<const uint16_t*>(sp + 8 * h + 2 * qd));
-                    kd_halves(two, sc[i][0], sc[i][1]);
-                }
-#pragma unroll
-                for (int wd = 0; wd < KW; ++wd) {
-                    uint32_t a[2][4];
+                for (int h = 0; h < KH; ++h) {
+                    uint32_t kr[2][KW], sc[2][2];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        kv4_unpack8(kr[i][wd], a[i]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) a[i][e] = kv4_mul2(a[i][e], sc[i][wd >> 1]);
+                        const int row = u * 16 + g + 8 * i;
+                        kd_read<KW>(kr[i], st + row * C::KROW + (KH == 2 ? (h ^ (g & 1)) * 64 : 0) + qd * (4 * KW));
+                        const unsigned char* sp = st + C::S_AT + row * C::SROW;
+                        const uint32_t two = kv4_scales(D == 64 ? (uint32_t)sp[qd] : (uint32_t) * reinterpret_cast<const uint16_t*>(sp + 8 * h + 2 * qd));
+                        kd_halves(two, sc[i][0], sc[i][1]);
                     }
-                    const uint32_t(*qx)[2] = &qb[2 * (h * KW + wd)];
-                    mma_f16_16816(s0, a[0][0], a[1][0], a[0][1], a[1][1], qx[0][0], qx[0][1]);
-                    mma_f16_16816(s1, a[0][2], a[1][2], a[0][3], a[1][3], qx[1][0], qx[1][1]);
-                }
-            }
-            // ---- scores of keys g (elements 0, 1) and g + 8 (2, 3) for heads 2 qd, 2 qd + 1, in log2 units
-            float x[4], top[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = (s0[e] + s1[e]) * mul[e & 1];
+                    for (int wd = 0; wd < KW; ++wd) {
+                        uint32_t a[2][4];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            kv4_unpack8(kr[i][wd], a[i]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) a[i][e] = kv4_mul2(a[i][e], sc[i][wd >> 1]);
+                        }
+                        const uint32_t(*qx)[2] = &qb[2 * (h * KW + wd)];
+                        if (h == 0 && wd == 0) {
+                            mma_f16_16816_first(s0, a[0][0], a[1][0], a[0][1], a[1][1], qx[0][0], qx[0][1]);
+                            mma_f16_16816_first(s1, a[0][2], a[1][2], a[0][3], a[1][3], qx[1][0], qx[1][1]);
+                        } else {
+                            mma_f16_16816(s0, a[0][0], a[1][0], a[0][1], a[1][1], qx[0][0], qx[0][1]);
+                            mma_f16_16816(s1, a[0][2], a[1][2], a[0][3], a[1][3], qx[1][0], qx[1][1]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[u][e] = s0[e] + s1[e];
+            }
             if (softcap > 0.f) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = tanhf(x[e]) * cap2;
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[u][e] = tanhf(y[u][e] * cap_in[e & 1]);
             }
+            bool beyond = false;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (!((bt[e >> 1] >> (e & 1)) & 1u)) x[e] = -INFINITY;
-            top[0] = fmaxf(x[0], x[2]);
-            top[1] = fmaxf(x[1], x[3]);
-            if (__any_sync(0xffffffffu, top[0] > m_ref[0] + KD_SLACK || top[1] > m_ref[1] + KD_SLACK)) {
+            for (int u = 0; u < SUB; ++u) {
+                const uint32_t bt[2] = {(uint32_t)flags[u * 16] >> (2 * qd), (uint32_t)flags[u * 16 + 8] >> (2 * qd)};
 #pragma unroll
-                for (int off = 4; off <= 16; off <<= 1) {
-                    top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], off));
-                    top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], off));
+                for (int e = 0; e < 4; ++e) {
+                    if (!((bt[e >> 1] >> (e & 1)) & 1u)) y[u][e] = -INFINITY;
+                    beyond |= y[u][e] > limit[e & 1];
                 }
+            }
+            if (__any_sync(0xffffffffu, beyond)) {
                 float fac[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float m_new = fmaxf(m_ref[e], top[e]);
+                    float top = fmaxf(y[0][e], y[0][e + 2]);
+                    if (SUB == 2) top = fmaxf(top, fmaxf(y[SUB - 1][e], y[SUB - 1][e + 2]));
+#pragma unroll
+                    for (int off = 4; off <= 16; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                    const float m_new = fmaxf(m_ref[e], top * mul[e]);
                     fac[e] = kd_exp2(m_ref[e] - m_new);
                     m_ref[e] = m_new;
+                    limit[e] = m_new == -FLT_MAX ? -FLT_MAX : (m_new + KD_SLACK) / mul[e];
                     l_run[e] *= fac[e];
                 }
 #pragma unroll
                 for (int i = 0; i < MT; ++i) { acc[i][0] *= fac[0]; acc[i][1] *= fac[1]; acc[i][2] *= fac[0]; acc[i][3] *= fac[1]; }
             }
-            float p[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                p[e] = kd_exp2(x[e] - (m_ref[e & 1] - KD_PSHIFT));
-                l_run[e & 1] += p[e];
+            for (int u = 0; u < SUB; ++u) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = kd_exp2(fmaf(y[u][e], mul[e & 1], KD_PSHIFT - m_ref[e & 1]));
+                    l_run[e & 1] += p[e];
+                }
+                // probabilities as the column operand (key, head): two transposed 8 x 8 blocks
+                const uint32_t pb0 = kd_transpose(kd_pack(p[0], p[1])), pb1 = kd_transpose(kd_pack(p[2], p[3]));
+                // ---- O += V^T P: keys 2 qd, 2 qd + 1 (A, B) and 2 qd + 8, 2 qd + 9 (C, D) of 16
+                uint32_t vr[4][VW], vs[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = u * 16 + 2 * qd + (i & 1) + 8 * (i >> 1);
+                    kd_read<VW>(vr[i], st + C::V_AT + row * C::VROW + g * (D / 16));
+                    const unsigned char* sp = st + C::S_AT + row * C::SROW + D / 16;
+                    vs[i] = D == 64 ? sp[g >> 1] : D == 128 ? sp[g] : *reinterpret_cast<const uint16_t*>(sp + 2 * g);
+                }
+                uint32_t sab[D == 256 ? 2 : 1], scd[D == 256 ? 2 : 1];
+#pragma unroll
+                for (int i = 0; i < (D == 256 ? 2 : 1); ++i) {
+                    sab[i] = kd_no_nan(kv4_scales(__byte_perm(vs[0], vs[1], 0x0040 + 0x11 * i)));
+                    scd[i] = kd_no_nan(kv4_scales(__byte_perm(vs[2], vs[3], 0x0040 + 0x11 * i)));
+                }
+#pragma unroll
+                for (int wd = 0; wd < VW; ++wd) {
+                    // codes of the same dimension of two keys in a byte: even dimensions, odd ones
+                    uint32_t ab[2][4], cd[2][4];
+                    kv4_unpack8(kd_low_high(vr[0][wd], vr[1][wd] << 4), ab[0]);
+                    kv4_unpack8(kd_low_high(vr[0][wd] >> 4, vr[1][wd]), ab[1]);
+                    kv4_unpack8(kd_low_high(vr[2][wd], vr[3][wd] << 4), cd[0]);
+                    kv4_unpack8(kd_low_high(vr[2][wd] >> 4, vr[3][wd]), cd[1]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        mma_f16_16816(acc[4 * wd + e], kv4_mul2(ab[0][e], sab[wd >> 1]), kv4_mul2(ab[1][e], sab[wd >> 1]), kv4_mul2(cd[0][e], scd[wd >> 1]),
+                                      kv4_mul2(cd[1][e], scd[wd >> 1]), pb0, pb1);
+                }
             }
-            // probabilities as the column operand (key, head): two transposed 8 x 8 blocks
-            const uint32_t pb0 = kd_transpose(kd_pack(p[0], p[1])), pb1 = kd_transpose(kd_pack(p[2], p[3]));
-            // ---- O += V^T P: keys 2 qd, 2 qd + 1 (A, B) and 2 qd + 8, 2 qd + 9 (C, D) of the tile
-            uint32_t vr[4][VW], vs[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 2 * qd + (i & 1) + 8 * (i >> 1);
-                kd_read<VW>(vr[i], st + C::V_AT + row * C::VROW + g * (D / 16));
-                const unsigned char* sp = st + C::S_AT + row * C::SROW + D / 16;
-                vs[i] = D == 64 ? sp[g >> 1] : D == 128 ? sp[g] : *reinterpret_cast<const uint16_t*>(sp + 2 * g);
-            }
-            uint32_t sab[D == 256 ? 2 : 1], scd[D == 256 ? 2 : 1];
-#pragma unroll
-            for (int i = 0; i < (D == 256 ? 2 : 1); ++i) {
-                sab[i] = kd_no_nan(kv4_scales(__byte_perm(vs[0], vs[1], 0x0040 + 0x11 * i)));
-                scd[i] = kd_no_nan(kv4_scales(__byte_perm(vs[2], vs[3], 0x0040 + 0x11 * i)));
-            }
-#pragma unroll
-            for (int wd = 0; wd < VW; ++wd) {
-                // codes of the same dimension of two keys in a byte: even dimensions, odd ones
-                uint32_t ab[2][4], cd[2][4];
-                kv4_unpack8(kd_low_high(vr[0][wd], vr[1][wd] << 4), ab[0]);
-                kv4_unpack8(kd_low_high(vr[0][wd] >> 4, vr[1][wd]), ab[1]);
-                kv4_unpack8(kd_low_high(vr[2][wd], vr[3][wd] << 4), cd[0]);
-                kv4_unpack8(kd_low_high(vr[2][wd] >> 4, vr[3][wd]), cd[1]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    mma_f16_16816(acc[4 * wd + e], kv4_mul2(ab[0][e], sab[wd >> 1]), kv4_mul2(ab[1][e], sab[wd >> 1]), kv4_mul2(cd[0][e], scd[wd >> 1]),
-                                  kv4_mul2(cd[1][e], scd[wd >> 1]), pb0, pb1);
-            }
-            st = st == ring + (KD_STAGES - 1) * C::STAGE ? ring : st + C::STAGE;
+            st = st == ring + (STAGES - 1) * C::STAGE ? ring : st + C::STAGE;
             __syncwarp();                                      // the stage and its place in the list are free
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");

@@ -162,6 +162,7 @@ class _Ctypes:
     def assign(*args):
         return None
     assign_hidden = build_tiles = attn_fwd = decode_step = assign
+    qk_norm_rope = qk_norm_rope_bwd = kv4_append = kv4_read = kv4_copy_pages = kv4_decode_step = assign
 
 
 def _load_marshal(L):
@@ -173,8 +174,10 @@ def _load_marshal(L):
     except ImportError as e:
         warnings.warn(f"{e}: short calls take some 10 us longer through ctypes; `python -m paper_2604_03260_b200.build` builds the module", RuntimeWarning)
         return _Ctypes
-    m.init(focus_shape, *(C.cast(f, C.c_void_p).value for f in (L.focus_assign, L.focus_assign_hidden, L.focus_build_tiles, L.focus_attn_fwd,
-                                                                L.focus_decode_step)))
+    at = lambda *entries: (C.cast(f, C.c_void_p).value for f in entries)
+    m.init(focus_shape, *at(L.focus_assign, L.focus_assign_hidden, L.focus_build_tiles, L.focus_attn_fwd, L.focus_decode_step))
+    m.init_kv4(focus_rope, focus_kv4, *at(L.focus_qk_norm_rope, L.focus_qk_norm_rope_bwd, L.focus_kv4_append, L.focus_kv4_read, L.focus_kv4_copy_pages,
+                                          L.focus_kv4_decode_step))
     return m
 
 
@@ -336,10 +339,13 @@ def focus_rope_frequencies(rotary, base=10000.0, scaling=FOCUS_ROPE_PLAIN, facto
 def focus_qk_norm_rope(shape, rope, q, k, wq, wk, freq, positions, q_out, k_out, stream=None):
     """q, q_out bf16 [batch, Hq, n, D], k, k_out [batch, Hkv, n, D] (any strides with D contiguous; the outputs may be the inputs);
     wq, wk fp32 [D] or None; freq fp64 [rotary/2]; positions int32 [batch, n] or None"""
-    D, B, n = shape.D, shape.batch, shape.n
-    _check(lib().focus_qk_norm_rope(C.byref(shape), C.byref(rope), _heads(q, shape, shape.Hq), _heads(k, shape, shape.Hkv), _opt(wq, torch.float32, D),
-                                    _opt(wk, torch.float32, D), _opt(freq, torch.float64, rope.rotary // 2), _opt(positions, torch.int32, B, n),
-                                    _heads(q_out, shape, shape.Hq), _heads(k_out, shape, shape.Hkv), _stream(stream)))
+    rc = _short().qk_norm_rope(shape, rope, q, k, wq, wk, freq, positions, q_out, k_out, stream)
+    if rc is None:
+        D, B, n = shape.D, shape.batch, shape.n
+        rc = lib().focus_qk_norm_rope(C.byref(shape), C.byref(rope), _heads(q, shape, shape.Hq), _heads(k, shape, shape.Hkv), _opt(wq, torch.float32, D),
+                                      _opt(wk, torch.float32, D), _opt(freq, torch.float64, rope.rotary // 2), _opt(positions, torch.int32, B, n),
+                                      _heads(q_out, shape, shape.Hq), _heads(k_out, shape, shape.Hkv), _stream(stream))
+    _check(rc)
 
 
 def focus_qk_norm_rope_bwd_workspace_bytes(shape) -> int:
@@ -349,12 +355,15 @@ def focus_qk_norm_rope_bwd_workspace_bytes(shape) -> int:
 def focus_qk_norm_rope_bwd(shape, rope, q, k, wq, wk, freq, positions, dq_out, dk_out, dq, dk, dwq, dwk, ws, stream=None):
     """gradients dq, dk (bf16, like q and k; may be dq_out, dk_out) and dwq, dwk (fp32 [D]; None where the weight is) from those of the
     results; ws uint8 scratch"""
-    D, B, n = shape.D, shape.batch, shape.n
-    _check(lib().focus_qk_norm_rope_bwd(C.byref(shape), C.byref(rope), _heads(q, shape, shape.Hq), _heads(k, shape, shape.Hkv),
-                                        _opt(wq, torch.float32, D), _opt(wk, torch.float32, D), _opt(freq, torch.float64, rope.rotary // 2),
-                                        _opt(positions, torch.int32, B, n), _heads(dq_out, shape, shape.Hq), _heads(dk_out, shape, shape.Hkv),
-                                        _heads(dq, shape, shape.Hq), _heads(dk, shape, shape.Hkv), _opt(dwq, torch.float32, D),
-                                        _opt(dwk, torch.float32, D), _p(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    rc = _short().qk_norm_rope_bwd(shape, rope, q, k, wq, wk, freq, positions, dq_out, dk_out, dq, dk, dwq, dwk, ws, stream)
+    if rc is None:
+        D, B, n = shape.D, shape.batch, shape.n
+        rc = lib().focus_qk_norm_rope_bwd(C.byref(shape), C.byref(rope), _heads(q, shape, shape.Hq), _heads(k, shape, shape.Hkv),
+                                          _opt(wq, torch.float32, D), _opt(wk, torch.float32, D), _opt(freq, torch.float64, rope.rotary // 2),
+                                          _opt(positions, torch.int32, B, n), _heads(dq_out, shape, shape.Hq), _heads(dk_out, shape, shape.Hkv),
+                                          _heads(dq, shape, shape.Hq), _heads(dk, shape, shape.Hkv), _opt(dwq, torch.float32, D),
+                                          _opt(dwk, torch.float32, D), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+    _check(rc)
 
 
 def focus_kv4_page_bytes(shape, page_tokens) -> int:
@@ -373,34 +382,46 @@ def make_kv4(pages, page_tokens, table=None, lens=None, k_scale=1.0, v_scale=1.0
     return c
 
 
-def _cache(cache, shape, paged=True):
+def _fits(cache, shape, paged=True):
     """the cache's tensors against the shape of a call"""
     pages, table, lens = cache.tensors
-    want = focus_kv4_page_bytes(shape, cache.page_tokens)
-    assert want in (0, pages.shape[1]), f"pages of {pages.shape[1]} bytes, {want} for this shape"      # (0: the library says what is wrong)
+    want, D = cache.page_tokens, shape.D
+    want *= shape.Hkv * (D + D // 8 + 4)
+    assert want == pages.shape[1], f"pages of {pages.shape[1]} bytes, {want} for this shape"
     assert not paged or (lens is not None and lens.shape[0] == shape.batch), "table and lens of another batch"
-    return C.byref(cache)
 
 
 def focus_kv4_append(shape, cache, k, v, mk, counts=None, dev_status=None, stream=None):
     """k, v bf16 [batch, Hkv, n, D] (or [Hkv, n, D]); mk int32 [batch*Hkv, n]; counts int32 [batch] or None"""
-    _check(lib().focus_kv4_append(C.byref(shape), _cache(cache, shape), _heads(k, shape, shape.Hkv), _heads(v, shape, shape.Hkv),
-                                  _dev(mk, torch.int32, shape.batch, shape.Hkv, shape.n), _opt(counts, torch.int32, shape.batch),
-                                  _opt(dev_status, torch.int32, 4), _stream(stream)))
+    _fits(cache, shape)
+    rc = _short().kv4_append(shape, cache, k, v, mk, counts, dev_status, stream)
+    if rc is None:
+        rc = lib().focus_kv4_append(C.byref(shape), C.byref(cache), _heads(k, shape, shape.Hkv), _heads(v, shape, shape.Hkv),
+                                    _dev(mk, torch.int32, shape.batch, shape.Hkv, shape.n), _opt(counts, torch.int32, shape.batch),
+                                    _opt(dev_status, torch.int32, 4), _stream(stream))
+    _check(rc)
 
 
 def focus_kv4_read(shape, cache, first, k, v, mk=None, dev_status=None, stream=None):
     """tokens first[b] .. first[b] + n - 1 (first int32 [batch] or None: from the start) into k, v bf16 [batch, Hkv, n, D] and mk int32 [batch*Hkv, n]"""
-    _check(lib().focus_kv4_read(C.byref(shape), _cache(cache, shape), _opt(first, torch.int32, shape.batch), _heads(k, shape, shape.Hkv),
-                                _heads(v, shape, shape.Hkv), _opt(mk, torch.int32, shape.batch, shape.Hkv, shape.n), _opt(dev_status, torch.int32, 4),
-                                _stream(stream)))
+    _fits(cache, shape)
+    rc = _short().kv4_read(shape, cache, first, k, v, mk, dev_status, stream)
+    if rc is None:
+        rc = lib().focus_kv4_read(C.byref(shape), C.byref(cache), _opt(first, torch.int32, shape.batch), _heads(k, shape, shape.Hkv),
+                                  _heads(v, shape, shape.Hkv), _opt(mk, torch.int32, shape.batch, shape.Hkv, shape.n),
+                                  _opt(dev_status, torch.int32, 4), _stream(stream))
+    _check(rc)
 
 
 def focus_kv4_copy_pages(shape, cache, src, dst, dev_status=None, stream=None):
     """pages src[i] -> dst[i]; int32 lists on the GPU"""
-    count = src.numel()
-    _check(lib().focus_kv4_copy_pages(C.byref(shape), _cache(cache, shape, False), _dev(src, torch.int32, count), _dev(dst, torch.int32, count), count,
-                                      _opt(dev_status, torch.int32, 4), _stream(stream)))
+    _fits(cache, shape, False)
+    rc = _short().kv4_copy_pages(shape, cache, src, dst, dev_status, stream)
+    if rc is None:
+        count = src.numel()
+        rc = lib().focus_kv4_copy_pages(C.byref(shape), C.byref(cache), _dev(src, torch.int32, count), _dev(dst, torch.int32, count), count,
+                                        _opt(dev_status, torch.int32, 4), _stream(stream))
+    _check(rc)
 
 
 def focus_kv4_decode_workspace_bytes(shape) -> int:
@@ -409,9 +430,13 @@ def focus_kv4_decode_workspace_bytes(shape) -> int:
 
 def focus_kv4_decode_step(shape, cache, q, mq_new, o, lse, ws, dev_status=None, stream=None):
     """q, o bf16 [batch, Hq, D] (or [Hq, D]); mq_new int32 [batch*Hq]; lse fp32 [batch*Hq]; shape.n bounds the lengths"""
-    _check(lib().focus_kv4_decode_step(C.byref(shape), _cache(cache, shape), _vecs(q, shape, shape.Hq), _dev(mq_new, torch.int32, shape.batch, shape.Hq),
-                                       _vecs(o, shape, shape.Hq), _dev(lse, torch.float32, shape.batch, shape.Hq), _p(ws),
-                                       ws.numel() * ws.element_size(), _opt(dev_status, torch.int32, 4), _stream(stream)))
+    _fits(cache, shape)
+    rc = _short().kv4_decode_step(shape, cache, q, mq_new, o, lse, ws, dev_status, stream)
+    if rc is None:
+        rc = lib().focus_kv4_decode_step(C.byref(shape), C.byref(cache), _vecs(q, shape, shape.Hq), _dev(mq_new, torch.int32, shape.batch, shape.Hq),
+                                         _vecs(o, shape, shape.Hq), _dev(lse, torch.float32, shape.batch, shape.Hq), _p(ws),
+                                         ws.numel() * ws.element_size(), _opt(dev_status, torch.int32, 4), _stream(stream))
+    _check(rc)
 
 
 def focus_soft_ld(K) -> int:

@@ -29,6 +29,23 @@ int require_sm100();
 inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// x / d for 0 <= x < 2^31 and a divisor d >= 1 that a whole launch shares: with s = ceil(log2 d), m = floor(2^(31+s) / d) + 1 the product
+// x m is off x 2^(31+s) / d by at most x 2^s / 2^(31+s), less than 1 / d (Granlund and Montgomery, PLDI 1994)
+struct FixedDiv {
+    uint32_t m;
+    int s;
+#ifdef __CUDACC__
+    __host__ __device__ uint32_t operator()(uint32_t x) const { return (uint32_t)(((unsigned long long)x * m) >> (31 + s)); }
+#endif
+};
+inline FixedDiv fixed_div(uint32_t d) {
+    FixedDiv f;
+    f.s = 0;
+    while ((1ull << f.s) < d) ++f.s;
+    f.m = (uint32_t)((1ull << (31 + f.s)) / d + 1);
+    return f;
+}
+
 // layout-1 padded sorted length: room for every class segment to be rounded up to 256 slots
 inline int sorted_capacity(int n) { return (int)align_up((size_t)n + (size_t)FOCUS_MAX_CLASSES * 255, 256); }
 // group-major keys: every key once per group it belongs to (topk of them), every list padded to 128 slots

@@ -52,10 +52,12 @@ __device__ __forceinline__ uint32_t kv4_mul2(uint32_t a, uint32_t b) {
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-// two numbers as codes: `lo` in the low bits; to nearest, a tie to the even code, beyond 6 to 6
-__device__ __forceinline__ uint32_t kv4_code2(float lo, float hi) {
-    uint16_t r;
-    asm("{\n\t.reg .b8 b;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %1, %2;\n\tcvt.u16.u8 %0, b;\n\t}" : "=h"(r) : "f"(hi), "f"(lo));
+// eight numbers as codes of a word, the first in the low bits; to nearest, a tie to the even code, beyond 6 to 6
+__device__ __forceinline__ uint32_t kv4_code8(const float2 (&y)[4]) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tcvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\tmov.b32 %0, {b0, b1, b2, b3};\n\t}"
+        : "=r"(r) : "f"(y[0].x), "f"(y[0].y), "f"(y[1].x), "f"(y[1].y), "f"(y[2].x), "f"(y[2].y), "f"(y[3].x), "f"(y[3].y));
     return r;
 }
 __device__ __forceinline__ uint32_t kv4_scale_code(float s) {

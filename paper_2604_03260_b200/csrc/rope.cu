@@ -26,7 +26,10 @@ struct RopeArgs {
     float* partial;                               // backward with a norm: [CTAs of a side][D] sums of g xhat, queries' CTAs first
     int heads[2], batch, n, rot, interleaved;
     float eps, amplitude;
-    int lgT[2], parts;                            // tokens per tile (log; forward: [0]), parts that the heads of a tile are cut into (forward)
+    int lgT[2], per_seq[2];                       // tokens per tile (log), tiles per sequence (forward: [0] for both sides)
+    FixedDiv by_seq[2];                           // division by per_seq
+    uint32_t parts;                               // forward: parts that a tile's heads are cut into
+    FixedDiv by_parts;
     int ctas[2];                                  // backward: CTAs of a side
 };
 
@@ -206,125 +209,196 @@ __device__ __forceinline__ RopeAngles rope_get_angles(const float* row) {
     return x;
 }
 
+// A thread's pieces wait in places of its own in shared memory, `STAGES` rows of them: copied there asynchronously, so that rows under way cost no
+// registers, and read by nobody else, so that no barrier is needed.  Place of piece i of a stage: 16 bytes per thread, thread by thread.
+__device__ __forceinline__ uint32_t rope_place_of(int stage, int pieces, int i) { return (uint32_t)(((stage * pieces + i) * ROPE_THREADS + threadIdx.x) * 16); }
+__device__ __forceinline__ void rope_copy(uint32_t dst, const __nv_bfloat16* src, bool on) {          // zeros where it is not `on`
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void rope_store(__nv_bfloat16* p, int apart, const RopeUnit& u, bool inter) {
+    uint4 out[2];
+    rope_pack(u, inter, out);
+    *reinterpret_cast<uint4*>(p) = out[0];
+    *reinterpret_cast<uint4*>(p + apart) = out[1];
+}
+
 // Forward: a CTA takes 2^lgT tokens and all their heads, queries then keys (a part of them where there are few tokens).  A thread's token
-// and place in the row are the same in every pass, and so the angles, worked out once per token, stay in registers.  A pass's rows
-// are on their way while the pass before is worked on.
+// and place in the row are the same in every pass, and so what a pair is multiplied by, cosine and sine (worked out once per token) times
+// the side's weights, stays in registers; the row's own scale comes last.
+constexpr int ROPE_FWD_STAGES = 4;
 template <int D>
 __global__ void __launch_bounds__(ROPE_THREADS, 3)
 qk_norm_rope_kernel(const RopeArgs a) {
     using C = RopeCfg<D>;
+    constexpr int STAGES = ROPE_FWD_STAGES;
+    extern __shared__ __align__(16) unsigned char smem[];     // the stages
     __shared__ __align__(16) float cs_s[ROPE_TOKENS][D / 16][ROPE_UROW];
     __shared__ __align__(16) float w_s[2][D / 16][ROPE_UROW];
     const int unit = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
-    const int lgT = a.lgT[0], T = 1 << lgT, per_seq = (a.n + T - 1) >> lgT;
-    const int part = blockIdx.x % a.parts, tile = blockIdx.x / a.parts, b = tile / per_seq, t0 = (tile - b * per_seq) << lgT;
-    const int tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT;
-    const int Hq = a.heads[0], all = Hq + a.heads[1], passes = (all + hstep - 1) / hstep;
-    const int h_begin = passes * part / a.parts * hstep, h_end = min(passes * (part + 1) / a.parts * hstep, all);
+    const int lgT = a.lgT[0], T = 1 << lgT, tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT;
     const RopePlace at = rope_place(a, unit);
+    const int apart = at.d1 - at.d0;
+    const uint32_t tile = a.by_parts(blockIdx.x), part = blockIdx.x - tile * a.parts;
+    const int b = a.by_seq[0](tile), t0 = (int)(tile - b * a.per_seq[0]) << lgT, t = min(t0 + tok, a.n - 1);
     const bool live = t0 + tok < a.n;
+    // heads of the part, of either side, in whole passes; passes are counted over both
+    int h_lo[2], h_hi[2], passes[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int whole = (a.heads[s] + hstep - 1) / hstep, lo = (int)a.by_parts(whole * part), hi = (int)a.by_parts(whole * (part + 1));
+        h_lo[s] = lo * hstep + hofs;
+        h_hi[s] = min(hi * hstep, a.heads[s]);
+        passes[s] = hi - lo;
+    }
     dep_wait();
     dep_trigger();
-    const __nv_bfloat16 *xq = a.x[0] + (size_t)b * a.x_b[0] + (size_t)(t0 + tok) * a.x_n[0], *xk = a.x[1] + (size_t)b * a.x_b[1] + (size_t)(t0 + tok) * a.x_n[1];
-    __nv_bfloat16 *oq = a.out[0] + (size_t)b * a.o_b[0] + (size_t)(t0 + tok) * a.o_n[0], *ok = a.out[1] + (size_t)b * a.o_b[1] + (size_t)(t0 + tok) * a.o_n[1];
-    uint4 raw[2];
-    auto load = [&](int h) {
-        raw[0] = raw[1] = make_uint4(0, 0, 0, 0);
-        if (live && h < h_end) {
-            const __nv_bfloat16* p = h < Hq ? xq + (size_t)h * a.x_h[0] : xk + (size_t)(h - Hq) * a.x_h[1];
-            raw[0] = *reinterpret_cast<const uint4*>(p + at.d0);
-            raw[1] = *reinterpret_cast<const uint4*>(p + at.d1);
+    const uint32_t stages = (uint32_t)__cvta_generic_to_shared(smem);
+    const int all = passes[0] + passes[1];
+    auto issue = [&](int i) {
+        if (i < all) {
+            const int s = i >= passes[0], h = h_lo[s] + (i - (s ? passes[0] : 0)) * hstep;
+            const bool on = h < h_hi[s];
+            const __nv_bfloat16* p = a.x[s] + b * a.x_b[s] + t * a.x_n[s] + (on ? h : 0) * a.x_h[s] + at.d0;
+            rope_copy(stages + rope_place_of(i % STAGES, 2, 0), p, on);
+            rope_copy(stages + rope_place_of(i % STAGES, 2, 1), p + apart, on);
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    load(h_begin + hofs);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) issue(i);
     rope_put_weights<D>(w_s[0], a, 0);
     rope_put_weights<D>(w_s[1], a, 1);
     rope_put_angles<D>(cs_s, a, b, t0, T, 1.f);
     __syncthreads();
-    const RopeAngles ang = rope_get_angles(cs_s[tok][unit]);
-    for (int hb = h_begin; hb < h_end; hb += hstep) {
-        const int h = hb + hofs, side = h >= Hq;
-        RopeUnit x = rope_unpack(raw, at.inter);
-        load(h + hstep);
-        if (a.w[0] || a.w[1]) {                                // (one of them alone: the others' weights are 1 and their scale too)
-            const float scale = rsqrtf(rope_row_sum<C::LPR>(rope_dot(x, x)) * (1.f / D) + a.eps);
-            const float r = a.w[side] ? scale : 1.f;
-            const F2 r2 = f2(r, r);
-            const RopeUnit w = rope_get(w_s[side][unit]);
+    int i = 0;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const bool norm = a.w[s] != nullptr;
+        // (p, r) -> (p A + r B, p E + r F)
+        F2 A[4], B[4], E[4], F[4];
+        {
+            const RopeUnit w = rope_get(w_s[s][unit]), cs = rope_get(cs_s[tok][unit]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x.p[e] = f2_mul(f2_mul(x.p[e], r2), w.p[e]);
-                x.r[e] = f2_mul(f2_mul(x.r[e], r2), w.r[e]);
+                const float2 sn = f2_get(cs.r[e]);
+                A[e] = f2_mul(cs.p[e], w.p[e]);
+                B[e] = f2_mul(f2(-sn.x, -sn.y), w.r[e]);
+                E[e] = f2_mul(cs.r[e], w.p[e]);
+                F[e] = f2_mul(cs.p[e], w.r[e]);
             }
         }
-        rope_turn(x, ang);
-        if (live && h < h_end) {
-            uint4 out[2];
-            rope_pack(x, at.inter, out);
-            __nv_bfloat16* p = side ? ok + (size_t)(h - Hq) * a.o_h[1] : oq + (size_t)h * a.o_h[0];
-            *reinterpret_cast<uint4*>(p + at.d0) = out[0];
-            *reinterpret_cast<uint4*>(p + at.d1) = out[1];
+        const int64_t o_step = hstep * a.o_h[s];
+        __nv_bfloat16* z = a.out[s] + b * a.o_b[s] + t * a.o_n[s] + h_lo[s] * a.o_h[s] + at.d0;
+        for (int k = 0; k < passes[s]; ++k, ++i) {
+            issue(i + STAGES - 1);                             // into the stage that the pass before has left
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+            uint4 raw[2];
+            raw[0] = *reinterpret_cast<const uint4*>(smem + rope_place_of(i % STAGES, 2, 0));
+            raw[1] = *reinterpret_cast<const uint4*>(smem + rope_place_of(i % STAGES, 2, 1));
+            RopeUnit x = rope_unpack(raw, at.inter);
+            const float r = norm ? rsqrtf(rope_row_sum<C::LPR>(rope_dot(x, x)) * (1.f / D) + a.eps) : 1.f;
+            const F2 r2 = f2(r, r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const F2 p = x.p[e], q = x.r[e];
+                x.p[e] = f2_mul(f2_fma(q, B[e], f2_mul(p, A[e])), r2);
+                x.r[e] = f2_mul(f2_fma(q, F[e], f2_mul(p, E[e])), r2);
+            }
+            if (live && h_lo[s] + k * hstep < h_hi[s]) rope_store(z, apart, x, at.inter);
+            z += o_step;
         }
     }
 }
 
-// Backward: the CTAs of a side walk its tiles of tokens, all heads of a tile, a row's loads under way while the row before is worked on; the
-// sums over rows of g xhat stay in registers to the end, then go to `partial`.
+// Backward: the CTAs of a side walk its tiles of tokens, all heads of a tile, the copies two rows ahead; the sums over rows of g xhat stay in
+// registers to the end, then go to `partial`.
+constexpr int ROPE_BWD_STAGES = 3;
+template <int D>
+struct RopeBwd {
+    static constexpr size_t TABLES = sizeof(float) * 2 * ROPE_TOKENS * (D / 16) * ROPE_UROW, SUMS = sizeof(float) * RopeCfg<D>::RPP * (D + 4);
+    static constexpr size_t COPIES = (size_t)ROPE_BWD_STAGES * 4 * ROPE_THREADS * 16;
+    static constexpr size_t SMEM = COPIES + (TABLES > SUMS ? TABLES : SUMS);
+};
 template <int D>
 __global__ void __launch_bounds__(ROPE_THREADS, 2)
 qk_norm_rope_bwd_kernel(const RopeArgs a) {
     using C = RopeCfg<D>;
-    constexpr size_t TABLES = sizeof(float) * 2 * ROPE_TOKENS * (D / 16) * ROPE_UROW, SUMS = sizeof(float) * C::RPP * (D + 4);
-    __shared__ __align__(16) unsigned char space_s[TABLES > SUMS ? TABLES : SUMS];
-    auto cs_s = reinterpret_cast<float(*)[ROPE_TOKENS][D / 16][ROPE_UROW]>(space_s);       // two tables in turn
-    auto red_s = reinterpret_cast<float(*)[D + 4]>(space_s);  // when the tables are through
+    constexpr int STAGES = ROPE_BWD_STAGES;
+    extern __shared__ __align__(16) unsigned char smem[];
+    auto cs_s = reinterpret_cast<float(*)[ROPE_TOKENS][D / 16][ROPE_UROW]>(smem + RopeBwd<D>::COPIES);     // two tables in turn
+    auto red_s = reinterpret_cast<float(*)[D + 4]>(smem + RopeBwd<D>::COPIES);             // when the tables are through
     __shared__ __align__(16) float w_s[D / 16][ROPE_UROW];
     const int unit = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
     const int side = (int)blockIdx.x >= a.ctas[0];
     const int id = blockIdx.x - (side ? a.ctas[0] : 0);
-    const int lgT = a.lgT[side], T = 1 << lgT, per_seq = (a.n + T - 1) >> lgT, tiles = a.batch * per_seq;
+    const int lgT = a.lgT[side], T = 1 << lgT, tiles = a.batch * a.per_seq[side];
     const int tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT, H = a.heads[side];
     const RopePlace at = rope_place(a, unit);
+    const int apart = at.d1 - at.d0;
     const bool norm = a.w[side] != nullptr;
-    const int64_t x_h = a.x_h[side], g_h = a.g_h[side], o_h = a.o_h[side];
+    const int64_t x_step = hstep * a.x_h[side], g_step = hstep * a.g_h[side], o_step = hstep * a.o_h[side];
     dep_wait();
     dep_trigger();
     rope_put_weights<D>(w_s, a, side);
     RopeUnit dw;
 #pragma unroll
     for (int e = 0; e < 4; ++e) dw.p[e] = dw.r[e] = f2(0.f, 0.f);
-    int buf = 0;
-    for (int tile = id; tile < tiles; tile += a.ctas[side], buf ^= 1) {
-        const int b = tile / per_seq, t0 = (tile - b * per_seq) << lgT;
-        const bool live = t0 + tok < a.n;
-        const __nv_bfloat16* xs = a.x[side] + (size_t)b * a.x_b[side] + (size_t)(t0 + tok) * a.x_n[side];
-        const __nv_bfloat16* gs = a.g[side] + (size_t)b * a.g_b[side] + (size_t)(t0 + tok) * a.g_n[side];
-        __nv_bfloat16* os = a.out[side] + (size_t)b * a.o_b[side] + (size_t)(t0 + tok) * a.o_n[side];
-        uint4 xr[2], gr[2];
-        auto load = [&](int h) {
-            xr[0] = xr[1] = gr[0] = gr[1] = make_uint4(0, 0, 0, 0);
-            if (live && h < H) {
-                const __nv_bfloat16* p = gs + h * g_h;
-                gr[0] = *reinterpret_cast<const uint4*>(p + at.d0);
-                gr[1] = *reinterpret_cast<const uint4*>(p + at.d1);
-                if (norm) {
-                    const __nv_bfloat16* q = xs + h * x_h;
-                    xr[0] = *reinterpret_cast<const uint4*>(q + at.d0);
-                    xr[1] = *reinterpret_cast<const uint4*>(q + at.d1);
-                }
+    // the copies' own walk over the rows, ahead of the work's
+    const uint32_t stages = (uint32_t)__cvta_generic_to_shared(smem);
+    int c_tile = id, c_h = 0, into = 0;
+    const __nv_bfloat16 *xp = nullptr, *gp = nullptr;
+    bool c_live = false;
+    auto aim = [&] {                                           // at the rows of the tile c_tile
+        const int b = a.by_seq[side](c_tile), t0 = (int)(c_tile - b * a.per_seq[side]) << lgT, t = min(t0 + tok, a.n - 1);
+        c_live = t0 + tok < a.n;
+        xp = a.x[side] + b * a.x_b[side] + t * a.x_n[side] + at.d0;
+        gp = a.g[side] + b * a.g_b[side] + t * a.g_n[side] + at.d0;
+        c_h = hofs;
+    };
+    auto issue = [&] {
+        if (c_tile < tiles) {
+            const bool on = c_live && c_h < H;
+            const __nv_bfloat16* p = gp + (on ? c_h : 0) * a.g_h[side];
+            rope_copy(stages + rope_place_of(into, 4, 0), p, on);
+            rope_copy(stages + rope_place_of(into, 4, 1), p + apart, on);
+            if (norm) {
+                const __nv_bfloat16* q = xp + (on ? c_h : 0) * a.x_h[side];
+                rope_copy(stages + rope_place_of(into, 4, 2), q, on);
+                rope_copy(stages + rope_place_of(into, 4, 3), q + apart, on);
             }
-        };
-        load(hofs);
-        rope_put_angles<D>(cs_s[buf], a, b, t0, T, -1.f);
+            c_h += hstep;
+            if (c_h - hofs >= H) {
+                c_tile += a.ctas[side];
+                if (c_tile < tiles) aim();
+            }
+        }
+        into = into == STAGES - 1 ? 0 : into + 1;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (c_tile < tiles) aim();
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) issue();
+    int buf = 0, from = 0;
+    for (int tile = id; tile < tiles; tile += a.ctas[side], buf ^= 1) {
+        const int b = a.by_seq[side](tile), t0 = (int)(tile - b * a.per_seq[side]) << lgT, t = min(t0 + tok, a.n - 1);
+        const bool live = t0 + tok < a.n;
+        __nv_bfloat16* z = a.out[side] + b * a.o_b[side] + t * a.o_n[side] + hofs * a.o_h[side] + at.d0;
+        rope_put_angles<D>(cs_s[buf], a, b, t0, T, -1.f);      // (worked out a tile ahead instead: 47.6 -> 49.0 us)
         __syncthreads();                                       // (the other table is free: its readers have passed this barrier)
         const RopeAngles ang = rope_get_angles(cs_s[buf][tok][unit]);
-        for (int hb = 0; hb < H; hb += hstep) {
-            const int h = hb + hofs;
+        for (int h = hofs; h - hofs < H; h += hstep) {
             const bool on = live && h < H;
-            RopeUnit g = rope_unpack(gr, at.inter), x = rope_unpack(xr, at.inter);
-            load(h + hstep);
+            issue();                                           // into the stage that the row before has left
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+            uint4 raw[2];
+            raw[0] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 4, 0));
+            raw[1] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 4, 1));
+            RopeUnit g = rope_unpack(raw, at.inter);
             rope_turn(g, ang);
             if (norm) {
+                raw[0] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 4, 2));
+                raw[1] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 4, 3));
+                const RopeUnit x = rope_unpack(raw, at.inter);
                 RopeUnit u;
                 {
                     const RopeUnit w = rope_get(w_s[unit]);
@@ -342,20 +416,16 @@ qk_norm_rope_bwd_kernel(const RopeArgs a) {
                 const F2 r2 = f2(r, r), mr2 = f2(-m * r, -m * r);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const F2 xp = f2_mul(x.p[e], r2), xq = f2_mul(x.r[e], r2);
-                    dw.p[e] = f2_fma(g.p[e], xp, dw.p[e]);
-                    dw.r[e] = f2_fma(g.r[e], xq, dw.r[e]);
-                    g.p[e] = f2_fma(xp, mr2, f2_mul(u.p[e], r2));
-                    g.r[e] = f2_fma(xq, mr2, f2_mul(u.r[e], r2));
+                    const F2 xp2 = f2_mul(x.p[e], r2), xq2 = f2_mul(x.r[e], r2);
+                    dw.p[e] = f2_fma(g.p[e], xp2, dw.p[e]);
+                    dw.r[e] = f2_fma(g.r[e], xq2, dw.r[e]);
+                    g.p[e] = f2_fma(xp2, mr2, f2_mul(u.p[e], r2));
+                    g.r[e] = f2_fma(xq2, mr2, f2_mul(u.r[e], r2));
                 }
             }
-            if (on) {
-                uint4 out[2];
-                rope_pack(g, at.inter, out);
-                __nv_bfloat16* p = os + h * o_h;
-                *reinterpret_cast<uint4*>(p + at.d0) = out[0];
-                *reinterpret_cast<uint4*>(p + at.d1) = out[1];
-            }
+            if (on) rope_store(z, apart, g, at.inter);
+            z += o_step;
+            from = from == STAGES - 1 ? 0 : from + 1;
         }
     }
     if (!a.partial) return;
@@ -518,18 +588,27 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
     if (!bwd && !odd) {
         const int all = s->Hq + s->Hkv;
         a.lgT[0] = rope_tile(ROPE_PASSES * C::RPP, all, s->batch, s->n);
-        const long long tiles = (long long)s->batch * cdiv(s->n, 1 << a.lgT[0]);
-        const int passes = cdiv(all, C::RPP >> a.lgT[0]);
+        a.per_seq[0] = cdiv(s->n, 1 << a.lgT[0]);
+        a.by_seq[0] = fixed_div(a.per_seq[0]);
+        const long long tiles = (long long)s->batch * a.per_seq[0];
+        const int passes = cdiv(s->Hq, C::RPP >> a.lgT[0]) + cdiv(s->Hkv, C::RPP >> a.lgT[0]);
         // few tiles: a tile's passes over several CTAs
         long long parts = tiles >= ROPE_SMS ? 1 : ROPE_SMS / tiles;
-        a.parts = (int)(parts > passes ? passes : parts);
-        return check_cuda(launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)(tiles * a.parts)), dim3(ROPE_THREADS), 0, st, a),
+        if (parts > passes) parts = passes;
+        a.parts = (uint32_t)parts;
+        a.by_parts = fixed_div(a.parts);
+        constexpr size_t smem = (size_t)ROPE_FWD_STAGES * 2 * ROPE_THREADS * 16;
+        const int rc = check_cuda(allow_smem<qk_norm_rope_kernel<D>>(smem), "cudaFuncSetAttribute(norm and rotation)");
+        if (rc) return rc;
+        return check_cuda(launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)(tiles * parts)), dim3(ROPE_THREADS), smem, st, a),
                           "norm and rotation kernel launch");
     }
     long long tiles[2];
     for (int i = 0; i < 2; ++i) {
         a.lgT[i] = rope_tile(ROPE_PASSES * C::RPP, a.heads[i], s->batch, s->n);
-        tiles[i] = (long long)s->batch * cdiv(s->n, 1 << a.lgT[i]);
+        a.per_seq[i] = cdiv(s->n, 1 << a.lgT[i]);
+        a.by_seq[i] = fixed_div(a.per_seq[i]);
+        tiles[i] = (long long)s->batch * a.per_seq[i];
     }
     // CTAs of the two sides: in proportion to their heads, no more than they have tiles (or rows for the warps)
     const int places = bwd && !odd ? 2 * ROPE_SMS : ROPE_GRID;
@@ -539,9 +618,11 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
     a.ctas[0] = (int)(tiles[0] < places - kc ? tiles[0] : places - kc);
     a.ctas[1] = (int)(tiles[1] < kc ? tiles[1] : kc);
     const dim3 g(a.ctas[0] + a.ctas[1]), t(ROPE_THREADS);
-    int rc = odd ? check_cuda(bwd ? launch_dependent(qk_norm_rope_odd_kernel<D, true>, g, t, 0, st, a) : launch_dependent(qk_norm_rope_odd_kernel<D, false>, g, t, 0, st, a),
+    int rc = odd ? FOCUS_OK : check_cuda(allow_smem<qk_norm_rope_bwd_kernel<D>>(RopeBwd<D>::SMEM), "cudaFuncSetAttribute(norm and rotation backward)");
+    if (rc) return rc;
+    rc = odd ? check_cuda(bwd ? launch_dependent(qk_norm_rope_odd_kernel<D, true>, g, t, 0, st, a) : launch_dependent(qk_norm_rope_odd_kernel<D, false>, g, t, 0, st, a),
                               "norm and rotation kernel launch")
-                 : check_cuda(launch_dependent(qk_norm_rope_bwd_kernel<D>, g, t, 0, st, a), "norm and rotation backward kernel launch");
+                 : check_cuda(launch_dependent(qk_norm_rope_bwd_kernel<D>, g, t, RopeBwd<D>::SMEM, st, a), "norm and rotation backward kernel launch");
     if (rc || !bwd || !a.partial) return rc;
     return check_cuda(launch_dependent(norm_weight_grad_kernel, dim3(2 * D / 32), dim3(32, 32), 0, st, a.partial, a.ctas[0], a.ctas[1], D, dwq, dwk),
                       "norm weight gradient kernel launch");

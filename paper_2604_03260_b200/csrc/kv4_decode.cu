@@ -152,6 +152,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ int chunk_s[KD_MAX_BATCH / 32 + 1];             // first unit of every 32 sequences (more than 32 of them)
     __shared__ int red_s[KD_WARPS][4];
+    __shared__ float wgt_s[KD_GMAX][KD_WARPS], sum_s[KD_GMAX][2];
     __shared__ uint2 key_s[KD_WARPS][KD_LIST];                 // listed keys: where their codes are (in 16 bytes) and scales (in 8)
     __shared__ uint2 tile_s[KD_WARPS][KD_BATCH / 16];          // where the 16 keys start of tiles that are taken as they lie
     // which heads attend a key: of the listed keys, and of the last four batches that had whole tiles (the tiles under way, at most two, are
@@ -516,25 +517,22 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[u][e] = tanhf(y[u][e] * cap_in[e & 1]);
             }
-            bool beyond = false;
+            float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
                 const uint32_t bt[2] = {(uint32_t)flags[u * 16] >> (2 * qd), (uint32_t)flags[u * 16 + 8] >> (2 * qd)};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (!((bt[e >> 1] >> (e & 1)) & 1u)) y[u][e] = -INFINITY;
-                    beyond |= y[u][e] > limit[e & 1];
-                }
+                for (int e = 0; e < 4; ++e) y[u][e] = bt[e >> 1] & (1u << (e & 1)) ? y[u][e] : -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) top[e] = fmaxf(top[e], fmaxf(y[u][e], y[u][e + 2]));
             }
-            if (__any_sync(0xffffffffu, beyond)) {
+            if (__any_sync(0xffffffffu, top[0] > limit[0] || top[1] > limit[1])) {
                 float fac[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float top = fmaxf(y[0][e], y[0][e + 2]);
-                    if (SUB == 2) top = fmaxf(top, fmaxf(y[SUB - 1][e], y[SUB - 1][e + 2]));
 #pragma unroll
-                    for (int off = 4; off <= 16; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                    const float m_new = fmaxf(m_ref[e], top * mul[e]);
+                    for (int off = 4; off <= 16; off <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], off));
+                    const float m_new = fmaxf(m_ref[e], top[e] * mul[e]);
                     fac[e] = kd_exp2(m_ref[e] - m_new);
                     m_ref[e] = m_new;
                     limit[e] = m_new == -FLT_MAX ? -FLT_MAX : (m_new + KD_SLACK) / mul[e];
@@ -606,65 +604,88 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 *reinterpret_cast<float2*>(&xw[warp][2 * qd + e][2 + (D / 8) * g + 2 * i]) = make_float2(acc[i][e], acc[i][2 + e]);
         }
         __syncthreads();
+        // what each warp's sums count for, by the first warp: lane (head, warp)
+        if (warp == 0) {
+            const int gg = lane >> 2, ww = lane & 3;
+            const float m = xw[ww][gg][0];
+            float M = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 2));
+            const float wgt = exp2f(m - M);
+            float L = xw[ww][gg][1] * wgt;
+            L += __shfl_xor_sync(0xffffffffu, L, 1);
+            L += __shfl_xor_sync(0xffffffffu, L, 2);
+            wgt_s[gg][ww] = wgt;
+            if (ww == 0) { sum_s[gg][0] = M; sum_s[gg][1] = L; }
+        }
+        __syncthreads();
         const bool alone = u0 == 0 && u1 == units;             // the head's only range: its result, no partial one
-        for (int idx = threadIdx.x; idx < G * D; idx += KD_WARPS * 32) {
-            const int gg = idx / D, d = idx % D;
-            float M = -FLT_MAX;
-#pragma unroll
-            for (int ww = 0; ww < KD_WARPS; ++ww) M = fmaxf(M, xw[ww][gg][0]);
-            float L = 0.f, a = 0.f;
+        for (int idx = threadIdx.x; idx < G * (D / 2); idx += KD_WARPS * 32) {
+            const int gg = idx / (D / 2), d = idx % (D / 2) * 2;
+            float2 a = make_float2(0.f, 0.f);
 #pragma unroll
             for (int ww = 0; ww < KD_WARPS; ++ww) {
-                const float wgt = exp2f(xw[ww][gg][0] - M);
-                L = fmaf(xw[ww][gg][1], wgt, L);
-                a = fmaf(xw[ww][gg][2 + d], wgt, a);
+                const float2 x = *reinterpret_cast<const float2*>(&xw[ww][gg][2 + d]);
+                const float wgt = wgt_s[gg][ww];
+                a.x = fmaf(x.x, wgt, a.x);
+                a.y = fmaf(x.y, wgt, a.y);
             }
+            const float M = sum_s[gg][0], L = sum_s[gg][1];
             if (alone) {
-                o[(size_t)b * o_sb + (size_t)(hk * G + gg) * o_sh + d] = __float2bfloat16(L == 0.f ? 0.f : a / L * c.v_scale);
+                const float f = L == 0.f ? 0.f : c.v_scale / L;
+                __nv_bfloat16* dst = o + (size_t)b * o_sb + (size_t)(hk * G + gg) * o_sh + d;
+                dst[0] = __float2bfloat16(L == 0.f ? 0.f : a.x * f);
+                dst[1] = __float2bfloat16(L == 0.f ? 0.f : a.y * f);
                 if (d == 0) lse[(size_t)b * Hq + hk * G + gg] = L == 0.f ? -INFINITY : (M + log2f(L) - KD_PSHIFT) * KD_LN2;
             } else {
                 float* dst = part + ((size_t)(bh + (int)blockIdx.x) * G + gg) * (D + 2);
-                if (d == 0) { dst[0] = M; dst[1] = L; }
-                dst[2 + d] = a;
+                if (d == 0) *reinterpret_cast<float2*>(dst) = make_float2(M, L);
+                *reinterpret_cast<float2*>(dst + 2 + d) = a;
             }
         }
         __syncthreads();                                       // the next head's rows and results
     }
 }
 
-// One block per query head whose keys went to several CTAs: their partial results, joined by their maxima.  Partial result s of KV head bh
-// is in place bh + s of the list: each step along the list of ranges moves to another head or to another CTA.
-template <int D>
+// Joins the partial results of a query head whose keys went to several CTAs by their maxima; a block per 2 LANES dimensions: 32 where that
+// leaves room for all blocks at once (ragged, 24 sequences of 32 heads: 63 us with it, 58 without), else all.  Partial result s of KV
+// head bh is in place bh + s of the list: each step along the list of ranges moves to another head or to another CTA.  Latency is all of it:
+// the threads form 256 / LANES rows, row r taking every so many partials, eight of a thread's loads are under way while the weights are worked out
+// (a block per head with 4 rows, 74 partials: 7.4 us behind the partial pass; so MERGE_FIGURE).
+template <int D, int LANES>
 __global__ void __launch_bounds__(256)
 kv4_merge_kernel(const Kv4View c, const float* part, const int2* ranges, int Hq, int G, int n, __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, float* lse) {
-    constexpr int LANES = D / 2, ROWS = 256 / LANES, AHEAD = 8;
+    constexpr int ROWS = 256 / LANES, AHEAD = 8, SLICES = D / (2 * LANES);
     __shared__ float wgt_s[KD_SMS * 4 + 1];
     __shared__ float red_s[2][8];
-    __shared__ float2 acc_s[ROWS][LANES];
-    const int b = blockIdx.x / Hq, hq = blockIdx.x - b * Hq, t = threadIdx.x, row = t / LANES, col = t % LANES;
+    __shared__ float2 acc_s[ROWS][LANES + 1];
+    const int head = blockIdx.x / SLICES, slice = blockIdx.x % SLICES;
+    const int b = head / Hq, hq = head - b * Hq, t = threadIdx.x, row = t / LANES, col = t % LANES;
     const int hk = hq / G, bh = b * c.Hkv + hk;
     dep_wait();
     dep_trigger();
-    __nv_bfloat16* dst = o + (size_t)b * o_sb + (size_t)hq * o_sh + 2 * col;
+    __nv_bfloat16* dst = o + (size_t)b * o_sb + (size_t)hq * o_sh + slice * (2 * LANES) + 2 * col;
     const int len = dep_load(c.lens + b);
+    const int2 rg = ranges[bh];                                // (of an empty sequence: not written, not used)
     if (len <= 0 || len > n) {                                 // nothing to attend
         if (row == 0) dst[0] = dst[1] = __float2bfloat16(0.f);
-        if (t == 0) lse[blockIdx.x] = -INFINITY;
+        if (t == 0 && slice == 0) lse[head] = -INFINITY;
         return;
     }
-    const int2 rg = ranges[bh];
     const int cnt = rg.y - rg.x + 1;
     if (cnt == 1) return;                                      // written by its CTA
     const float* p = part + ((size_t)(bh + rg.x) * G + (hq - hk * G)) * (D + 2);
+    const float* pv = p + 2 + slice * (2 * LANES) + 2 * col;
     const size_t step = (size_t)G * (D + 2);
     float2 v[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
         const int s = row + j * ROWS;
-        v[j] = s < cnt ? *reinterpret_cast<const float2*>(p + s * step + 2 + 2 * col) : make_float2(0.f, 0.f);
+        v[j] = s < cnt ? *reinterpret_cast<const float2*>(pv + s * step) : make_float2(0.f, 0.f);
     }
-    float m = -FLT_MAX;
-    for (int s = t; s < cnt; s += 256) m = fmaxf(m, p[s * step]);
+    float2 ml[3];                                              // maxima and sums: at most 592 partials
+#pragma unroll
+    for (int j = 0; j < 3; ++j) ml[j] = t + 256 * j < cnt ? *reinterpret_cast<const float2*>(p + (size_t)(t + 256 * j) * step) : make_float2(-FLT_MAX, 0.f);
+    float m = fmaxf(ml[0].x, fmaxf(ml[1].x, ml[2].x));
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
     if ((t & 31) == 0) red_s[0][t >> 5] = m;
@@ -673,11 +694,11 @@ kv4_merge_kernel(const Kv4View c, const float* part, const int2* ranges, int Hq,
 #pragma unroll
     for (int i = 1; i < 8; ++i) M = fmaxf(M, red_s[0][i]);
     float l = 0.f;
-    for (int s = t; s < cnt; s += 256) {
-        const float ms = p[s * step];
-        const float wg = exp2f(ms - M);
-        wgt_s[s] = wg;
-        l = fmaf(p[s * step + 1], wg, l);
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+        const float wg = exp2f(ml[j].x - M);
+        if (t + 256 * j < cnt) wgt_s[t + 256 * j] = wg;
+        l = fmaf(ml[j].y, wg, l);
     }
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
@@ -691,26 +712,25 @@ kv4_merge_kernel(const Kv4View c, const float* part, const int2* ranges, int Hq,
         acc.x = fmaf(v[j].x, wg, acc.x);
         acc.y = fmaf(v[j].y, wg, acc.y);
     }
-#pragma unroll 4
+#pragma unroll 8
     for (int s = row + AHEAD * ROWS; s < cnt; s += ROWS) {
-        const float2 x = *reinterpret_cast<const float2*>(p + s * step + 2 + 2 * col);
+        const float2 x = *reinterpret_cast<const float2*>(pv + s * step);
         const float wg = wgt_s[s];
         acc.x = fmaf(x.x, wg, acc.x);
         acc.y = fmaf(x.y, wg, acc.y);
     }
     acc_s[row][col] = acc;
     __syncthreads();
+    if (t >= LANES) return;
     float L = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) L += red_s[1][i];
-    if (row == 0) {
 #pragma unroll
-        for (int r = 1; r < ROWS; ++r) { acc.x += acc_s[r][col].x; acc.y += acc_s[r][col].y; }
-        const float f = L == 0.f ? 0.f : c.v_scale / L;
-        dst[0] = __float2bfloat16(L == 0.f ? 0.f : acc.x * f);
-        dst[1] = __float2bfloat16(L == 0.f ? 0.f : acc.y * f);
-    }
-    if (t == 0) lse[blockIdx.x] = L == 0.f ? -INFINITY : (M + log2f(L) - KD_PSHIFT) * KD_LN2;
+    for (int r = 1; r < ROWS; ++r) { acc.x += acc_s[r][col].x; acc.y += acc_s[r][col].y; }
+    const float f = L == 0.f ? 0.f : c.v_scale / L;
+    dst[0] = __float2bfloat16(L == 0.f ? 0.f : acc.x * f);
+    dst[1] = __float2bfloat16(L == 0.f ? 0.f : acc.y * f);
+    if (t == 0 && slice == 0) lse[head] = L == 0.f ? -INFINITY : (M + log2f(L) - KD_PSHIFT) * KD_LN2;
 }
 
 // the partial results, one more than ranges per head, and the ranges of the heads; a function of the shape without its length
@@ -734,7 +754,8 @@ static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor&
                                          q.stride_b, q.stride_h, mq_new, s->batch, s->Hq, G, s->n, s->window, scale, s->softcap, part, ranges,
                                          reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse, status), "kv4 decode kernel launch");
     if (rc) return rc;
-    return check_cuda(launch_dependent(kv4_merge_kernel<D>, dim3(s->batch * s->Hq), dim3(256), 0, st, c, part, ranges, s->Hq, G, s->n,
+    const bool narrow = (long long)s->batch * s->Hq * (D / 32) <= KD_SMS * 8;
+    return check_cuda(launch_dependent(narrow ? kv4_merge_kernel<D, 16> : kv4_merge_kernel<D, D / 2>, dim3(s->batch * s->Hq * (narrow ? D / 32 : 1)), dim3(256), 0, st, c, part, ranges, s->Hq, G, s->n,
                                        reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse), "kv4 merge kernel launch");
 }
 

@@ -115,12 +115,14 @@ __device__ __forceinline__ void kd_read(uint32_t (&r)[WORDS], const unsigned cha
 __host__ __device__ __forceinline__ int kd_cdiv(int a, int b) { return (a + b - 1) / b; }
 
 // How the work is cut.  Every KV head of a sequence has ceil(len / 64) units of 64 keys; the units of all heads form one list, dealt out
-// in equal contiguous ranges of `per` units.  A CTA whose range enters another head writes one more partial result and starts over, so
-// the heads are padded to whole ranges where that still leaves no more ranges than CTAs.  The lengths are on the device, and so every
-// CTA works this out for itself (a microsecond; the sums are over the sequences of the batch).
+// in equal contiguous ranges of `per` units.  A CTA whose range enters another head writes one more partial result and starts over, which
+// takes as long as KD_TURN units: every head ends with that many empty ones, so that such a CTA gets the fewer keys.  Where whole ranges per
+// head make no longer ranges, the heads are padded to them instead (`aligned`).  The lengths are on the device, and so every CTA works
+// this out for itself (a microsecond; the sums are over the sequences of the batch).
 struct KdPlan {
     int per, aligned;
 };
+constexpr int KD_TURN = 5;
 
 __device__ __forceinline__ int kd_length(const Kv4View& c, int b, int n, int32_t* status) {
     const int len = dep_load(c.lens + b);
@@ -134,7 +136,7 @@ __device__ __forceinline__ int kd_length(const Kv4View& c, int b, int n, int32_t
 // units of a head in the list
 __device__ __forceinline__ int kd_padded(int len, const KdPlan& p) {
     const int u = kd_cdiv(len, KD_UNIT);
-    return p.aligned ? kd_cdiv(u, p.per) * p.per : u;
+    return u == 0 ? 0 : p.aligned ? kd_cdiv(u, p.per) * p.per : u + KD_TURN;
 }
 
 // GP: query heads per KV head, G, rounded up to a power of two
@@ -151,7 +153,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     constexpr int COPIES = 16 * CPT / 32, ROWSTEP = 32 / CPT;  // copies per lane and 16 keys; tokens apart
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ int chunk_s[KD_MAX_BATCH / 32 + 1];             // first unit of every 32 sequences (more than 32 of them)
-    __shared__ int red_s[KD_WARPS][4];
+    __shared__ int red_s[KD_WARPS][5];
     __shared__ float wgt_s[KD_GMAX][KD_WARPS], sum_s[KD_GMAX][2];
     __shared__ uint2 key_s[KD_WARPS][KD_LIST];                 // listed keys: where their codes are (in 16 bytes) and scales (in 8)
     __shared__ uint2 tile_s[KD_WARPS][KD_BATCH / 16];          // where the 16 keys start of tiles that are taken as they lie
@@ -172,18 +174,23 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     const int len0 = lane < batch ? kd_length(c, lane, n, blockIdx.x == 0 && warp == 0 ? status : nullptr) : 0;   // of the first 32 sequences
     {
         const int ctas = gridDim.x;
-        int sum = kd_cdiv(len0, KD_UNIT);
+        int sum = kd_cdiv(len0, KD_UNIT), turns = len0 > 0 ? KD_TURN : 0;
         // a wider batch: the warps share the rest out (every warp has the first 32)
         if (batch > 32) {
-            int more = 0;
-            for (int b = 32 + threadIdx.x; b < batch; b += KD_WARPS * 32)
-                more += kd_cdiv(kd_length(c, b, n, blockIdx.x == 0 ? status : nullptr), KD_UNIT);
+            int more = 0, more_turns = 0;
+            for (int b = 32 + threadIdx.x; b < batch; b += KD_WARPS * 32) {
+                const int len = kd_length(c, b, n, blockIdx.x == 0 ? status : nullptr);
+                more += kd_cdiv(len, KD_UNIT);
+                more_turns += len > 0 ? KD_TURN : 0;
+            }
             more = __reduce_add_sync(0xffffffffu, more);
-            if (lane == 0) red_s[warp][0] = more;
+            more_turns = __reduce_add_sync(0xffffffffu, more_turns);
+            if (lane == 0) { red_s[warp][0] = more; red_s[warp][4] = more_turns; }
             __syncthreads();
-            if (lane < KD_WARPS) sum += red_s[lane][0];
+            if (lane < KD_WARPS) { sum += red_s[lane][0]; turns += red_s[lane][4]; }
         }
         total = (int)__reduce_add_sync(0xffffffffu, sum) * Hkv;
+        const int with_turns = total + (int)__reduce_add_sync(0xffffffffu, turns) * Hkv;
         const int per0 = total > ctas ? kd_cdiv(total, ctas) : 1;
         // three lengths of a range to try with whole ranges per head: the shortest, an eighth and a quarter longer
         const int cand[3] = {per0, per0 + kd_cdiv(per0, 8), per0 + kd_cdiv(per0, 4)};
@@ -207,11 +214,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             for (int i = 0; i < 3; ++i)
                 if (lane < KD_WARPS) cnt[i] += red_s[lane][1 + i];
         }
-        plan.per = per0;
+        plan.per = kd_cdiv(with_turns, ctas);
         plan.aligned = 0;
 #pragma unroll
         for (int i = 2; i >= 0; --i)
-            if ((int)__reduce_add_sync(0xffffffffu, cnt[i]) * Hkv <= ctas) { plan.per = cand[i]; plan.aligned = 1; }
+            if ((int)__reduce_add_sync(0xffffffffu, cnt[i]) * Hkv <= ctas && cand[i] <= plan.per) { plan.per = cand[i]; plan.aligned = 1; }
         int u = kd_padded(len0, plan) * Hkv;
         if (batch > 32) {
             // first unit of every 32 sequences, by the first warp

@@ -386,7 +386,8 @@ FOCUS_API int focus_kv4_copy_pages(const focus_shape* shape, const focus_kv4* ca
  * the only query, sequences of their own lengths.  Key j is attended iff lens[b]-1-j <= window or mq_new[b*Hq+h] & mask(j) != 0; exact
  * softmax over the attended keys, on the numbers that the codes stand for.  Products of fp16 operands (Q with a power of two per head;
  * probabilities with 11 significant bits), fp32 accumulation.  An empty sequence has o = 0 and lse = -inf.
- *   shape       n = the longest length that `lens` may hold, at most max_pages * page_tokens; Hq / Hkv <= 8, batch <= 1024
+ *   shape       n = the longest length that `lens` may hold, at most max_pages * page_tokens; Hq / Hkv <= 8, batch <= 1024, the pool
+ *               smaller than 32 GiB (FOCUS_ERR_UNSUPPORTED otherwise)
  *   q, o        device bf16 [batch, Hq, D] (stride_n ignored; q 4-byte aligned with even strides)
  *   mq_new      device uint32 [batch*Hq]           lse   device fp32 [batch*Hq], natural log
  *   ws          device scratch of focus_kv4_decode_workspace_bytes(shape) bytes (the same for every n), 16-byte aligned; contents need

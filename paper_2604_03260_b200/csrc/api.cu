@@ -506,6 +506,7 @@ int focus_kv4_decode_step(const focus_shape* shape, const focus_kv4* cache, focu
     if (shape->batch > 1 && (q.stride_b < 1 || o.stride_b < 1))
         return fail(FOCUS_ERR_INVALID_ARG, "q.stride_b and o.stride_b must be positive when batch > 1");
     if ((uintptr_t)ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is not 16-byte aligned");
+    if ((rc = kv4_decode_check(shape, c))) return rc;
     if (ws_bytes < kv4_decode_workspace_bytes(shape))
         return fail(FOCUS_ERR_CAPACITY, "decode workspace has %zu bytes, %zu needed", ws_bytes, kv4_decode_workspace_bytes(shape));
     if ((rc = require_sm100())) return rc;

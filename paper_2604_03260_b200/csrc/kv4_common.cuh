@@ -74,6 +74,7 @@ int launch_kv4_read(const focus_shape* s, const Kv4View& c, const int32_t* first
                     uint32_t* mk, int32_t* status, cudaStream_t st);
 int launch_kv4_copy(const Kv4View& c, const int32_t* src, const int32_t* dst, int count, int32_t* status, cudaStream_t st);
 size_t kv4_decode_workspace_bytes(const focus_shape* s);
+int kv4_decode_check(const focus_shape* s, const Kv4View& c);           // what the kernels take, beyond the checks of a shape and a cache
 int launch_kv4_decode(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o,
                       float* lse, void* ws, float scale, int32_t* status, cudaStream_t st);
 

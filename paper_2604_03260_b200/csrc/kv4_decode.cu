@@ -335,10 +335,10 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     flags[32 * k] = (uint8_t)bits[k];
+                    // (used where the tile is whole: then either 16 of its keys hold an attended one, and with it their first has a page)
                     if ((lane & 15) == 0) {
-                        // (a page beyond the pool, or none, in a whole tile of 32: its 16 keys are attended by no head, and any rows do for them)
-                        const uint32_t p = pg[k] < (uint32_t)c.num_pages ? pg[k] : 0u, sl = (slot + 32 * k) & pmask;
-                        tile_s[warp][2 * k + (lane >> 4)] = make_uint2(p * page16 + sl * (D / 16), p * (2 * page16) + sl * (D / 64));
+                        const uint32_t sl = (slot + 32 * k) & pmask;
+                        tile_s[warp][2 * k + (lane >> 4)] = make_uint2(pg[k] * page16 + sl * (D / 16), pg[k] * (2 * page16) + sl * (D / 64));
                     }
                 }
                 ++batches;
@@ -776,12 +776,17 @@ static int decode_d(const focus_shape* s, const Kv4View& c, const focus_tensor& 
     return decode_dg<D, 8>(s, c, q, mq_new, o, lse, ws, scale, status, st);
 }
 
+int kv4_decode_check(const focus_shape* s, const Kv4View& c) {
+    if (s->Hq / s->Hkv > KD_GMAX) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d query heads per KV head", KD_GMAX);
+    if (s->batch > KD_MAX_BATCH) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d sequences in one call", KD_MAX_BATCH);
+    if ((long long)s->batch * s->Hkv * cdiv(s->n, KD_UNIT) >= (1ll << 29)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: batch * Hkv * n is too large");
+    // listed keys say where their codes are in 16 bytes and their scales in 8
+    if ((size_t)c.num_pages * c.page_bytes >= (1ull << 35)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: a pool of 32 GiB or more");
+    return FOCUS_OK;
+}
+
 int launch_kv4_decode(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
                       float scale, int32_t* status, cudaStream_t st) {
-    if (s->Hq / s->Hkv > KD_GMAX) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d query heads per KV head", KD_GMAX);
-    if ((long long)s->batch * s->Hkv * cdiv(s->n, KD_UNIT) >= (1ll << 29)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: batch * Hkv * n is too large");
-    if ((size_t)c.num_pages * c.page_bytes >= (1ull << 35)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: a pool of 32 GiB or more");
-    if (s->batch > KD_MAX_BATCH) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d sequences in one call", KD_MAX_BATCH);
     switch (s->D) {
         case 64: return decode_d<64>(s, c, q, mq_new, o, lse, ws, scale, status, st);
         case 128: return decode_d<128>(s, c, q, mq_new, o, lse, ws, scale, status, st);

@@ -197,7 +197,8 @@ RAGGED = [0, 1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 129, 300, 1000, 0, 513]
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("Hq,Hkv,lens,P,K,topk,w", [
     (4, 2, [1], 16, 4, 2, 0), (2, 2, RAGGED, 16, 4, 1, 5), (8, 1, RAGGED, 64, 8, 1, 0), (12, 4, RAGGED, 32, 4, 2, 40), (5, 1, [777], 128, 32, 1, 3),
-    (14, 2, [2049, 2048], 256, 4, 2, 3000), (1, 1, [4097], 64, 1, 1, 0), (16, 8, [8200], 64, 8, 2, 100)])
+    (14, 2, [2049, 2048], 256, 4, 2, 3000), (1, 1, [4097], 64, 1, 1, 0), (16, 8, [8200], 64, 8, 2, 100), (2, 2, [9001, 500], 16, 4, 2, 7),
+    (3, 3, [5000, 77], 32, 8, 4, 1)])
 def test_decode(D, Hq, Hkv, lens, P, K, topk, w):
     cache, q, mq, mk, k, v = filled(lens, P, Hq, Hkv, D, K, topk, D + Hq)
     n = max(lens)
@@ -236,6 +237,35 @@ def test_decode_ranges_across_heads(batch, Hq, Hkv, most, D):
     compare(sub(o), sub(lse), [lens[b] for b in pick], sub(q), sub(mq.view(batch, Hq)), sub(mk.view(batch, Hkv, -1)), sub(ks), sub(vs), 9)
     empty = torch.tensor(lens) == 0
     assert (o.cpu()[empty] == 0).all() and (lse.cpu()[empty] == -math.inf).all() and o.isfinite().all()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("P,run,hole", [(16, 200, 0.0), (64, 37, 0.2), (128, 700, 0.22), (32, 5, 0.0)])
+def test_decode_runs_and_holes(D, P, run, hole):
+    """groups in runs of tokens: stretches that no head attends, tiles of 16 or 32 keys that are taken whole although some of their keys are
+    not attended (and hold infinities), and single keys between them"""
+    lens, Hq, Hkv, K = [20011, 3000], 2, 1, 8
+    g = gen(run + D)
+    n = max(lens)
+    shape = fb.make_shape(Hq, Hkv, n, D, K, 1, 33, batch=2)
+    table, num = table_of(lens, P, seed=run)
+    cache = pool(shape, P, table, num, lens)
+    k, v = (torch.randn((2, Hkv, n, D), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    group = (torch.arange(n, device="cuda") // run * 5) % K
+    mk = (1 << group).to(torch.int32).repeat(2 * Hkv, 1)
+    holes = torch.rand(mk.shape, generator=g, device="cuda") < hole
+    mk[holes] = 0
+    mq = torch.tensor([1, 4, 8, 8], dtype=torch.int32, device="cuda")
+    far = torch.stack([torch.arange(n, device="cuda") < m - 1 - 33 for m in lens])
+    bad = holes.view(2, Hkv, n) & far[:, None]                      # attended by nobody
+    k[bad], v[bad] = float("inf"), float("nan")
+    st = status()
+    fb.focus_kv4_append(shape, cache, k, v, mk, cache.tensors[2], st)
+    q = torch.randn((2, Hq, D), generator=g, device="cuda").to(torch.bfloat16)
+    o, lse = decode(cache, shape, q, mq, st=st)
+    assert st[0].item() == 0
+    ks, vs = stored(cache, Hkv, D, n)
+    compare(o, lse, lens, q, mq, mk, ks.nan_to_num(), vs.nan_to_num(), 33)
 
 
 def test_decode_long_cache_and_large_scores():

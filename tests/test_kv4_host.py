@@ -66,9 +66,12 @@ def test_cache_calls_refuse_what_does_not_fit():
                dict(c=cache(max_pages=1)), dict(o=fb.focus_tensor(4096, 0, 128, 128))):
         assert step(**kw) == -1, kw
     assert step(size=fb.focus_kv4_decode_workspace_bytes(S) - 1) == -3
+    # what the kernels do not take: nine heads a group, too many sequences, a pool of 32 GiB, too many keys in all
+    assert step(s=fb.make_shape(36, 4, 100, 128, 4, 2, 16, batch=2)) == -2 and step(s=fb.make_shape(8, 4, 100, 128, 4, 2, 16, batch=1025)) == -2
+    P256 = 4 * 256 * (128 + 16 + 4)
+    assert step(c=cache(page_tokens=256, num_pages=(1 << 35) // P256 + 1)) == -2
+    assert step(s=fb.make_shape(8, 8, 1 << 24, 128, 4, 2, 16, batch=1024), c=cache(max_pages=1 << 18)) == -2
     if not torch.cuda.is_available():
-        nine = fb.make_shape(36, 4, 100, 128, 4, 2, 16, batch=2)
-        assert step(s=nine) in (-2, -4, -5) and step(s=fb.make_shape(8, 4, 100, 128, 4, 2, 16, batch=1025)) in (-2, -4, -5)
         assert step() in (-4, -5) and L.focus_kv4_append(R(wide), R(c), t, t, 4096, None, None, None) in (-1, -2, -4, -5)
 
 

@@ -1,6 +1,7 @@
 // focus_kv4_append, focus_kv4_read, focus_kv4_copy_pages: what goes into the pages of the 4-bit cache, comes out of them, and moves
 // between them.  All three are HBM-bound.
 #include "kv4_common.cuh"
+#include "f32x2.cuh"
 
 namespace focus {
 
@@ -39,20 +40,10 @@ __device__ __forceinline__ float kv4_quotient(float a, float s, float r) {
     const float y = a * r;
     return fmaf(fmaf(-y, s, a), r, y);
 }
-__device__ __forceinline__ unsigned long long kv4_pair(float lo, float hi) {
-    unsigned long long r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
 // two of them at once; `ns` is -s twice
-__device__ __forceinline__ float2 kv4_quotient2(unsigned long long a, unsigned long long ns, unsigned long long r) {
-    unsigned long long y, e;
-    float2 q;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(r));
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(e) : "l"(y), "l"(ns), "l"(a));
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(e) : "l"(e), "l"(r), "l"(y));
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(q.x), "=f"(q.y) : "l"(e));
-    return q;
+__device__ __forceinline__ float2 kv4_quotient2(F2 a, F2 ns, F2 r) {
+    const F2 y = f2_mul(a, r);
+    return f2_get(f2_fma(f2_fma(y, ns, a), r, y));
 }
 
 // x (16 numbers of a block) -> codes and scale, with `gs` the power of two on top and `inv_gs` its inverse.  s = amax / 6 rounded to e4m3, code =
@@ -80,14 +71,14 @@ __device__ __forceinline__ uint2 kv4_quantise(const uint4 (&raw)[2], float gs, f
             w[i] = __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xffff0000u);
         }
     }
-    const unsigned long long ns2 = kv4_pair(-s, -s), r2 = kv4_pair(r, r);
+    const F2 ns2 = f2(-s, -s), r2 = f2(r, r);
     uint32_t c[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         float2 y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            y[i] = kv4_quotient2(kv4_pair(__uint_as_float(w[4 * h + i] << 16), __uint_as_float(w[4 * h + i] & 0xffff0000u)), ns2, r2);
+            y[i] = kv4_quotient2(f2(__uint_as_float(w[4 * h + i] << 16), __uint_as_float(w[4 * h + i] & 0xffff0000u)), ns2, r2);
         c[h] = kv4_code8(y);
     }
     return make_uint2(c[0], c[1]);
@@ -141,7 +132,7 @@ kv4_append_kernel(const Kv4View c, const __nv_bfloat16* k, int64_t k_sb, int64_t
 // a block's codes and scale as 16 bf16 numbers (exact)
 __device__ __forceinline__ void kv4_expand(uint2 code, uint32_t sc, float gs, uint4* dst) {
     const float s = __half2float(__ushort_as_half((unsigned short)(kv4_scales(sc) & 0xffffu))) * gs;
-    const unsigned long long s2 = kv4_pair(s, s);
+    const F2 s2 = f2(s, s);
     uint32_t out[8];
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
@@ -150,10 +141,7 @@ __device__ __forceinline__ void kv4_expand(uint2 code, uint32_t sc, float gs, ui
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&f[e]));
-            unsigned long long t;
-            float2 z;
-            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(kv4_pair(y.x, y.y)), "l"(s2));
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(z.x), "=f"(z.y) : "l"(t));
+            const float2 z = f2_get(f2_mul(f2(y.x, y.y), s2));
             const __nv_bfloat162 b2 = __floats2bfloat162_rn(z.x, z.y);
             out[4 * w + e] = *reinterpret_cast<const uint32_t*>(&b2);
         }

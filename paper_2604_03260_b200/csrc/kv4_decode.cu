@@ -19,6 +19,7 @@
 // Rows come through a ring in shared memory, private to a warp, by asynchronous copies: one address per 16 bytes, none for the operands.
 // Every warp keeps its own maximum, sum and O; a CTA joins its warps, a second kernel the CTAs.
 #include "kv4_common.cuh"
+#include "f32x2.cuh"
 
 #include <float.h>
 
@@ -114,6 +115,10 @@ __device__ __forceinline__ void kd_read(uint32_t (&r)[WORDS], const unsigned cha
 
 __host__ __device__ __forceinline__ int kd_cdiv(int a, int b) { return (a + b - 1) / b; }
 
+// Where the flags of key x of a tile are: those of the keys x % 8, + 8, ... that one lane has, side by side.
+template <int KEYS>
+__device__ __forceinline__ int kd_spot(int x) { return (x & ~(KEYS - 1)) + (x & 7) * (KEYS / 8) + ((x & (KEYS - 1)) >> 3); }
+
 // How the work is cut.  Every KV head of a sequence has ceil(len / 64) units of 64 keys; the units of all heads form one list, dealt out
 // in equal contiguous ranges of `per` units.  A CTA whose range enters another head writes one more partial result and starts over, which
 // takes as long as KD_TURN units: every head ends with that many empty ones, so that such a CTA gets the fewer keys.  Where whole ranges per
@@ -159,7 +164,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     __shared__ uint2 tile_s[KD_WARPS][KD_BATCH / 16];          // where the 16 keys start of tiles that are taken as they lie
     // which heads attend a key: of the listed keys, and of the last four batches that had whole tiles (the tiles under way, at most two, are
     // of two of them, and a third is being written)
-    __shared__ uint8_t bit_s[KD_WARPS][KD_LIST + 4 * KD_BATCH];
+    __shared__ __align__(4) uint8_t bit_s[KD_WARPS][KD_LIST + 4 * KD_BATCH];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, qd = lane & 3;
     const int Hkv = c.Hkv, lgP = c.lgP;
@@ -294,7 +299,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 pg[k] = pg_next[k];
                 mk[k] = 0u;
                 if (pg[k] < (uint32_t)c.num_pages)
-                    mk[k] = dep_load(reinterpret_cast<const uint32_t*>(masks + (size_t)pg[k] * c.page_bytes) + (j & pmask));
+                    mk[k] = dep_load(reinterpret_cast<const uint32_t*>(masks + (size_t)(pg[k] * page16) * 16) + (j & pmask));
                 else if (j < k_end)
                     kv4_report(status, KV4_BAD_PAGE, b, j >> lgP, (int)pg[k]);     // its keys are passed over
             }
@@ -308,6 +313,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         int tail = 0, taken = 0;                               // keys listed, and taken off the list
         uint32_t whole = 0, batches = 0;                       // whole tiles of the batch still to come; batches that had some
         uint32_t under_way = 0, depth = 0;                     // where the tiles under way have their flags, 10 bits each; how many they are
+        const int spot = kd_spot<KEYS>(lane);
         // look at the next batch: its whole tiles, and its other attended keys for the list
         auto look = [&] {
             uint32_t bits[2], any[2];
@@ -315,12 +321,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int j = next + 32 * k + lane;
-                bits[k] = 0;
+                bits[k] = 0;                                   // (a key without a page has no group either)
 #pragma unroll
                 for (int gg = 0; gg < GP; ++gg)
                     if (mq_all[gg] & mk[k]) bits[k] |= 1u << gg;
-                if (j >= near) bits[k] = (1u << G) - 1u;
-                if (pg[k] >= (uint32_t)c.num_pages) bits[k] = 0;
+                if (next + KD_BATCH > near && j >= near && pg[k] < (uint32_t)c.num_pages) bits[k] = (1u << G) - 1u;
                 any[k] = __ballot_sync(0xffffffffu, bits[k] != 0u);
                 if constexpr (SUB == 2) {
                     if (__popc(any[k]) >= C::WHOLE) { whole |= 1u << k; any[k] = 0; }
@@ -331,7 +336,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             }
             const uint32_t slot = next + lane;
             if (whole) {
-                uint8_t* flags = &bit_s[warp][KD_LIST + (batches & 3u) * KD_BATCH + lane];
+                uint8_t* flags = &bit_s[warp][KD_LIST + (batches & 3u) * KD_BATCH + spot];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     flags[32 * k] = (uint8_t)bits[k];
@@ -350,7 +355,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                         const int at = (tail + __popc(any[k] & lower)) & (KD_LIST - 1);
                         const uint32_t sl = (slot + 32 * k) & pmask;
                         key_s[warp][at] = make_uint2(pg[k] * page16 + sl * (D / 16), pg[k] * (2 * page16) + sl * (D / 64));
-                        bit_s[warp][at] = (uint8_t)bits[k];
+                        bit_s[warp][kd_spot<KEYS>(at)] = (uint8_t)bits[k];
                     }
                     tail += __popc(any[k]);
                 }
@@ -382,16 +387,15 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 whole &= whole - 1;
 #pragma unroll
                 for (int u = 0; u < SUB; ++u) {
-                    const uint2 at = tile_s[warp][t * SUB + u];
-                    const unsigned char* src = csrc + ctok * D + (size_t)at.x * 16;
+                    const unsigned char* src = csrc + ctok * D + (size_t)tile_s[warp][t * SUB + u].x * 16;
 #pragma unroll
                     for (int i = 0; i < COPIES; ++i) kd_copy16(into + cdst + (u * COPIES + i) * cstep, src + i * ROWSTEP * D);
-                    if (lane < 16 * SP) {
-                        const unsigned char* sc = scales + lane * (D == 64 ? 8 : 16) + (size_t)at.y * 8;
-                        const uint32_t to = into + C::S_AT + (u * 16 * SP + lane) * (D == 64 ? 8 : 16);
-                        if constexpr (D == 64) kd_copy8(to, sc);
-                        else kd_copy16(to, sc);
-                    }
+                }
+                // the scales: 32 rows of 8 or 16 bytes, or 16 of 32
+                {
+                    const unsigned char* sc = scales + (size_t)tile_s[warp][t * SUB + (SUB == 2 ? lane >> 4 : 0)].y * 8;
+                    if constexpr (D == 64) kd_copy8(into + C::S_AT + lane * 8, sc + (lane & 15) * 8);
+                    else kd_copy16(into + C::S_AT + lane * 16, sc + (D == 256 ? lane : lane & 15) * 16);
                 }
                 flags = KD_LIST + ((batches - 1) & 3u) * KD_BATCH + KEYS * t;
             } else if (tail > taken) {
@@ -399,7 +403,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                     const uint2 pad = key_s[warp][(tail - 1) & (KD_LIST - 1)];
                     if (lane < taken + KEYS - tail) {
                         key_s[warp][(tail + lane) & (KD_LIST - 1)] = pad;
-                        bit_s[warp][(tail + lane) & (KD_LIST - 1)] = 0;
+                        bit_s[warp][kd_spot<KEYS>((tail + lane) & (KD_LIST - 1))] = 0;
                     }
                     tail = taken + KEYS;
                     __syncwarp();
@@ -408,14 +412,10 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 const uint2* keys = &key_s[warp][flags];
 #pragma unroll
                 for (int i = 0; i < COPIES * SUB; ++i) kd_copy16(into + cdst + i * cstep, csrc + (size_t)keys[ctok + i * ROWSTEP].x * 16);
-#pragma unroll
-                for (int u = 0; u < SUB; ++u) {
-                    if (lane < 16 * SP) {
-                        const unsigned char* sc = scales + (lane % SP) * 16 + (size_t)keys[u * 16 + lane / SP].y * 8;
-                        const uint32_t to = into + C::S_AT + (u * 16 * SP + lane) * (D == 64 ? 8 : 16);
-                        if constexpr (D == 64) kd_copy8(to, sc);
-                        else kd_copy16(to, sc);
-                    }
+                {
+                    const unsigned char* sc = scales + (size_t)keys[lane / SP].y * 8;
+                    if constexpr (D == 64) kd_copy8(into + C::S_AT + lane * 8, sc);
+                    else kd_copy16(into + C::S_AT + lane * 16, sc + (lane % SP) * 16);
                 }
                 taken += KEYS;
             } else {
@@ -466,7 +466,8 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
 
         // of heads 2 qd, 2 qd + 1; l: this lane's keys alone.  A reference that no key has moved yet is FLT_MAX below everything, and its limit
         // for y is such that any score but minus infinity is beyond it
-        float m_ref[2] = {-FLT_MAX, -FLT_MAX}, limit[2] = {-FLT_MAX, -FLT_MAX}, l_run[2] = {0.f, 0.f};
+        float m_ref[2] = {-FLT_MAX, -FLT_MAX}, limit[2] = {-FLT_MAX, -FLT_MAX};
+        F2 l_run = f2(0.f, 0.f);
         float acc[MT][4];                                      // O: dimensions (D / 8) g + 2 i (elements 0, 1) and + 1 (2, 3), heads 2 qd, 2 qd + 1
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
@@ -477,7 +478,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             if (depth == 0) break;
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
             __syncwarp();
-            const uint8_t* flags = &bit_s[warp][(under_way & 1023u) + g];
+            uint32_t flags;                                    // of this lane's keys g, g + 8, ... a byte each; from the bit of head 2 qd on
+            {
+                const uint8_t* at = &bit_s[warp][(under_way & 1023u) + g * (2 * SUB)];
+                flags = (SUB == 2 ? *reinterpret_cast<const uint32_t*>(at) : (uint32_t) * reinterpret_cast<const uint16_t*>(at)) >> (2 * qd);
+            }
             under_way >>= 10;
             --depth;
             // ---- S = K Q^T: keys g (elements 0, 1) and g + 8 (2, 3) of 16 for heads 2 qd, 2 qd + 1; two sums in turn
@@ -516,7 +521,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                     }
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[u][e] = s0[e] + s1[e];
+                for (int e = 0; e < 4; e += 2) {
+                    const float2 t = f2_get(f2_add(f2(s0[e], s0[e + 1]), f2(s1[e], s1[e + 1])));
+                    y[u][e] = t.x;
+                    y[u][e + 1] = t.y;
+                }
             }
             if (softcap > 0.f) {
 #pragma unroll
@@ -527,9 +536,8 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-                const uint32_t bt[2] = {(uint32_t)flags[u * 16] >> (2 * qd), (uint32_t)flags[u * 16 + 8] >> (2 * qd)};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[u][e] = bt[e >> 1] & (1u << (e & 1)) ? y[u][e] : -INFINITY;
+                for (int e = 0; e < 4; ++e) y[u][e] = flags & (1u << (16 * u + 8 * (e >> 1) + (e & 1))) ? y[u][e] : -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) top[e] = fmaxf(top[e], fmaxf(y[u][e], y[u][e + 2]));
             }
@@ -543,8 +551,8 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                     fac[e] = kd_exp2(m_ref[e] - m_new);
                     m_ref[e] = m_new;
                     limit[e] = m_new == -FLT_MAX ? -FLT_MAX : (m_new + KD_SLACK) / mul[e];
-                    l_run[e] *= fac[e];
                 }
+                l_run = f2_mul(l_run, f2(fac[0], fac[1]));
 #pragma unroll
                 for (int i = 0; i < MT; ++i) { acc[i][0] *= fac[0]; acc[i][1] *= fac[1]; acc[i][2] *= fac[0]; acc[i][3] *= fac[1]; }
             }
@@ -552,9 +560,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             for (int u = 0; u < SUB; ++u) {
                 float p[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[e] = kd_exp2(fmaf(y[u][e], mul[e & 1], KD_PSHIFT - m_ref[e & 1]));
-                    l_run[e & 1] += p[e];
+                for (int e = 0; e < 4; e += 2) {
+                    const float2 t = f2_get(f2_fma(f2(y[u][e], y[u][e + 1]), f2(mul[0], mul[1]), f2(KD_PSHIFT - m_ref[0], KD_PSHIFT - m_ref[1])));
+                    p[e] = kd_exp2(t.x);
+                    p[e + 1] = kd_exp2(t.y);
+                    l_run = f2_add(l_run, f2(p[e], p[e + 1]));
                 }
                 // probabilities as the column operand (key, head): two transposed 8 x 8 blocks
                 const uint32_t pb0 = kd_transpose(kd_pack(p[0], p[1])), pb1 = kd_transpose(kd_pack(p[2], p[3]));
@@ -595,14 +605,14 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         // ---- join the warps
 #pragma unroll
         for (int off = 4; off <= 16; off <<= 1) {
-            l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], off);
-            l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], off);
+            const float2 l = f2_get(l_run);
+            l_run = f2_add(l_run, f2(__shfl_xor_sync(0xffffffffu, l.x, off), __shfl_xor_sync(0xffffffffu, l.y, off)));
         }
         __syncthreads();                                       // the rings are through
         auto xw = reinterpret_cast<float(*)[KD_GMAX][D + 2]>(smem);
         if (g == 0) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { xw[warp][2 * qd + e][0] = m_ref[e]; xw[warp][2 * qd + e][1] = l_run[e]; }
+            for (int e = 0; e < 2; ++e) { xw[warp][2 * qd + e][0] = m_ref[e]; xw[warp][2 * qd + e][1] = e ? f2_get(l_run).y : f2_get(l_run).x; }
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {

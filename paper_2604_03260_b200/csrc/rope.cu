@@ -6,6 +6,7 @@
 //   dx = r (u - xhat mean(u xhat)),   dw = sum over rows of g xhat.
 // HBM-bound: every vector read once and written once (backward: vectors and gradients read, gradients written).
 #include "common.cuh"
+#include "f32x2.cuh"
 
 #include <math.h>
 
@@ -32,31 +33,6 @@ struct RopeArgs {
     FixedDiv by_parts;
     int ctas[2];                                  // backward: CTAs of a side
 };
-
-// two fp32 operations at once
-struct F2 {
-    unsigned long long v;
-};
-__device__ __forceinline__ F2 f2(float lo, float hi) {
-    F2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ float2 f2_get(F2 a) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
-    return r;
-}
-__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
-    F2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
 
 // cos and sin (times the amplitude) of position * freq: the angle is reduced in 64 bits, since positions reach a million and fp32 would
 // leave an error of 0.06 there

@@ -27,9 +27,9 @@ namespace focus {
 
 constexpr int KD_GMAX = 8;
 constexpr int KD_WARPS = 4;
-constexpr int KD_UNIT = 64;              // keys: the grain of the split over CTAs, 16 per warp
 constexpr int KD_SMS = 148;
 constexpr int KD_MAX_BATCH = 1024;
+constexpr int KD_ALONE = 256;            // keys up to which a head is one CTA's: no merge (3 us; its warps' second tile takes less than one)
 constexpr int KD_LIST = 256;             // ring of listed keys: at most 31 left over, 64 new, and those of the tiles under way
 constexpr int KD_BATCH = 64;             // keys whose masks a warp looks at together (128: six registers more, 2 % slower)
 constexpr float KD_LOG2E = 1.4426950408889634f;
@@ -42,6 +42,8 @@ template <int D> struct KdCfg {
     static constexpr int CTAS = KD_SMS * PER_SM;
     static constexpr int SUB = D == 256 ? 1 : 2;              // a tile of the walk: 16 or 32 keys, whose copies, flags and vote are one
     static constexpr int KEYS = 16 * SUB;
+    static constexpr int UNIT = KEYS * KD_WARPS;              // keys: the grain of the split over CTAs, a tile per warp
+    static constexpr int TURN = (320 + UNIT - 1) / UNIT;      // units that a range loses when it enters another head, see below
     static constexpr int WHOLE = KEYS * 3 / 4;                // attended keys of an aligned tile from which on all are loaded
     static constexpr int STAGES = D == 128 ? 2 : 3;           // tiles in a warp's ring
     // a stage: rows of key codes, of value codes, of scales.  A lane reads 16 bytes of a key row (8 at D = 64), eight lanes two whole rows
@@ -119,15 +121,15 @@ __host__ __device__ __forceinline__ int kd_cdiv(int a, int b) { return (a + b - 
 template <int KEYS>
 __device__ __forceinline__ int kd_spot(int x) { return (x & ~(KEYS - 1)) + (x & 7) * (KEYS / 8) + ((x & (KEYS - 1)) >> 3); }
 
-// How the work is cut.  Every KV head of a sequence has ceil(len / 64) units of 64 keys; the units of all heads form one list, dealt out
-// in equal contiguous ranges of `per` units.  A CTA whose range enters another head writes one more partial result and starts over, which
-// takes as long as KD_TURN units: every head ends with that many empty ones, so that such a CTA gets the fewer keys.  Where whole ranges per
-// head make no longer ranges, the heads are padded to them instead (`aligned`).  The lengths are on the device, and so every CTA works
-// this out for itself (a microsecond; the sums are over the sequences of the batch).
+// How the work is cut.  Every KV head of a sequence has ceil(len / UNIT) units; the units of all heads form one list, dealt out in equal
+// contiguous ranges of `per` units.  A CTA whose range enters another head writes one more partial result and starts over, which takes as
+// long as TURN units: every head ends with that many empty ones, so that such a CTA gets the fewer keys (24 ragged sequences: 58 -> 52 us).
+// Where whole ranges per head make no longer ranges, the heads are padded to them instead; where no sequence can be longer than KD_ALONE,
+// they are padded to `span` units, its length, and a range is whole heads.  The lengths are on the device, and so every CTA works this out
+// for itself (every warp for itself, up to 32 sequences); the sums are over the sequences of the batch.
 struct KdPlan {
-    int per, aligned;
+    int per, pad;                        // units of a range; heads are padded to multiples of `pad`, or by TURN (0)
 };
-constexpr int KD_TURN = 5;
 
 __device__ __forceinline__ int kd_length(const Kv4View& c, int b, int n, int32_t* status) {
     const int len = dep_load(c.lens + b);
@@ -139,15 +141,16 @@ __device__ __forceinline__ int kd_length(const Kv4View& c, int b, int n, int32_t
 }
 
 // units of a head in the list
+template <int D>
 __device__ __forceinline__ int kd_padded(int len, const KdPlan& p) {
-    const int u = kd_cdiv(len, KD_UNIT);
-    return u == 0 ? 0 : p.aligned ? kd_cdiv(u, p.per) * p.per : u + KD_TURN;
+    const int u = kd_cdiv(len, KdCfg<D>::UNIT);
+    return u == 0 ? 0 : p.pad > 0 ? kd_cdiv(u, p.pad) * p.pad : u + KdCfg<D>::TURN;
 }
 
 // GP: query heads per KV head, G, rounded up to a power of two
 template <int D, int GP>
 __global__ void __launch_bounds__(KD_WARPS * 32, KdCfg<D>::PER_SM)
-kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t q_sh, const uint32_t* mq_new, int batch, int Hq, int G, int n, int w,
+kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t q_sh, const uint32_t* mq_new, int batch, int Hq, int G, int n, int span, int w,
                   float scale, float softcap, float* part, int2* ranges, __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, float* lse, int32_t* status) {
     using C = KdCfg<D>;
     constexpr int SUB = C::SUB, KEYS = C::KEYS, STAGES = C::STAGES;
@@ -179,14 +182,14 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     const int len0 = lane < batch ? kd_length(c, lane, n, blockIdx.x == 0 && warp == 0 ? status : nullptr) : 0;   // of the first 32 sequences
     {
         const int ctas = gridDim.x;
-        int sum = kd_cdiv(len0, KD_UNIT), turns = len0 > 0 ? KD_TURN : 0;
+        int sum = kd_cdiv(len0, C::UNIT), turns = len0 > 0 ? C::TURN : 0;
         // a wider batch: the warps share the rest out (every warp has the first 32)
         if (batch > 32) {
             int more = 0, more_turns = 0;
             for (int b = 32 + threadIdx.x; b < batch; b += KD_WARPS * 32) {
                 const int len = kd_length(c, b, n, blockIdx.x == 0 ? status : nullptr);
-                more += kd_cdiv(len, KD_UNIT);
-                more_turns += len > 0 ? KD_TURN : 0;
+                more += kd_cdiv(len, C::UNIT);
+                more_turns += len > 0 ? C::TURN : 0;
             }
             more = __reduce_add_sync(0xffffffffu, more);
             more_turns = __reduce_add_sync(0xffffffffu, more_turns);
@@ -201,11 +204,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         const int cand[3] = {per0, per0 + kd_cdiv(per0, 8), per0 + kd_cdiv(per0, 4)};
         int cnt[3];
 #pragma unroll
-        for (int i = 0; i < 3; ++i) cnt[i] = kd_cdiv(kd_cdiv(len0, KD_UNIT), cand[i]);
+        for (int i = 0; i < 3; ++i) cnt[i] = kd_cdiv(kd_cdiv(len0, C::UNIT), cand[i]);
         if (batch > 32) {
             int more[3] = {0, 0, 0};
             for (int b = 32 + threadIdx.x; b < batch; b += KD_WARPS * 32) {
-                const int u = kd_cdiv(kd_length(c, b, n, nullptr), KD_UNIT);
+                const int u = kd_cdiv(kd_length(c, b, n, nullptr), C::UNIT);
 #pragma unroll
                 for (int i = 0; i < 3; ++i) more[i] += kd_cdiv(u, cand[i]);
             }
@@ -220,17 +223,21 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 if (lane < KD_WARPS) cnt[i] += red_s[lane][1 + i];
         }
         plan.per = kd_cdiv(with_turns, ctas);
-        plan.aligned = 0;
+        plan.pad = 0;
 #pragma unroll
         for (int i = 2; i >= 0; --i)
-            if ((int)__reduce_add_sync(0xffffffffu, cnt[i]) * Hkv <= ctas && cand[i] <= plan.per) { plan.per = cand[i]; plan.aligned = 1; }
-        int u = kd_padded(len0, plan) * Hkv;
+            if ((int)__reduce_add_sync(0xffffffffu, cnt[i]) * Hkv <= ctas && cand[i] <= plan.per) plan.per = plan.pad = cand[i];
+        if (span > 0) {                                        // (with_turns - total: TURN for every head that has keys)
+            plan.pad = span;
+            plan.per = span * max(kd_cdiv((with_turns - total) / C::TURN, ctas), 1);
+        }
+        int u = kd_padded<D>(len0, plan) * Hkv;
         if (batch > 32) {
             // first unit of every 32 sequences, by the first warp
             if (warp == 0) {
                 int base = 0;
                 for (int b0 = 0; b0 < batch; b0 += 32) {
-                    if (b0 > 0) u = b0 + lane < batch ? kd_padded(kd_length(c, b0 + lane, n, nullptr), plan) * Hkv : 0;
+                    if (b0 > 0) u = b0 + lane < batch ? kd_padded<D>(kd_length(c, b0 + lane, n, nullptr), plan) * Hkv : 0;
                     if (lane == 0) chunk_s[b0 / 32] = base;
                     base += __reduce_add_sync(0xffffffffu, u);
                 }
@@ -250,11 +257,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         {
             int ch = 0, base = 0, l = len0;
             if (batch > 32) {
-                while (chunk_s[ch + 1] <= f) ++ch;
+                while (ch < kd_cdiv(batch, 32) - 1 && chunk_s[ch + 1] <= f) ++ch;      // (lengths that change under the kernel do not lead beyond it)
                 base = chunk_s[ch];
                 if (ch > 0) l = ch * 32 + lane < batch ? kd_length(c, ch * 32 + lane, n, nullptr) : 0;
             }
-            const int u = kd_padded(l, plan) * Hkv;
+            const int u = kd_padded<D>(l, plan) * Hkv;
             int incl = u;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
@@ -262,12 +269,14 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 if (lane >= off) incl += t;
             }
             incl += base;
-            const int at = __ffs(__ballot_sync(0xffffffffu, incl > f)) - 1;
+            const uint32_t beyond = __ballot_sync(0xffffffffu, incl > f);
+            if (beyond == 0) break;
+            const int at = __ffs(beyond) - 1;
             b = ch * 32 + at;
             len = __shfl_sync(0xffffffffu, l, at);
             start = __shfl_sync(0xffffffffu, incl - u, at);
         }
-        const int units = kd_cdiv(len, KD_UNIT), stride = kd_padded(len, plan);
+        const int units = kd_cdiv(len, C::UNIT), stride = kd_padded<D>(len, plan);
         const int hk = (f - start) / stride;
         const int f0 = start + hk * stride;                    // the head's first unit
         const int bh = b * Hkv + hk;
@@ -275,7 +284,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         f = min(f_end, f0 + stride);
         if (u0 == 0 && threadIdx.x == 0) ranges[bh] = make_int2(f0 / plan.per, (f0 + units - 1) / plan.per);
         if (u0 >= u1) continue;                                // (the padding of a head)
-        const int t0 = u0 * KD_UNIT, t1 = min(u1 * KD_UNIT, len), near = len - 1 - w;      // keys from `near` on are local
+        const int t0 = u0 * C::UNIT, t1 = min(u1 * C::UNIT, len), near = len - 1 - w;      // keys from `near` on are local
 
         // ---- this warp's keys: a quarter of the range, in whole tiles.  Pages are on their way two batches ahead, masks one
         const int32_t* table = c.table + (size_t)b * c.max_pages;
@@ -661,13 +670,19 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         }
         __syncthreads();                                       // the next head's rows and results
     }
+    // empty sequences: nothing to attend
+    for (int b = blockIdx.x; b < batch; b += gridDim.x) {
+        if (kd_length(c, b, n, nullptr) > 0) continue;
+        for (int i = threadIdx.x; i < Hq * D; i += KD_WARPS * 32) o[(size_t)b * o_sb + (size_t)(i / D) * o_sh + i % D] = __float2bfloat16(0.f);
+        for (int i = threadIdx.x; i < Hq; i += KD_WARPS * 32) lse[(size_t)b * Hq + i] = -INFINITY;
+    }
 }
 
 // Joins the partial results of a query head whose keys went to several CTAs by their maxima; a block per 2 LANES dimensions: 32 where that
 // leaves room for all blocks at once (ragged, 24 sequences of 32 heads: 63 us with it, 58 without), else all.  Partial result s of KV
 // head bh is in place bh + s of the list: each step along the list of ranges moves to another head or to another CTA.  Latency is all of it:
 // the threads form 256 / LANES rows, row r taking every so many partials, eight of a thread's loads are under way while the weights are worked out
-// (a block per head with 4 rows, 74 partials: 7.4 us behind the partial pass; so MERGE_FIGURE).
+// (74 partials of 32 heads: 3.6 us behind the partial pass; a block per head with 4 rows 7.4).
 template <int D, int LANES>
 __global__ void __launch_bounds__(256)
 kv4_merge_kernel(const Kv4View c, const float* part, const int2* ranges, int Hq, int G, int n, __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, float* lse) {
@@ -683,13 +698,8 @@ kv4_merge_kernel(const Kv4View c, const float* part, const int2* ranges, int Hq,
     __nv_bfloat16* dst = o + (size_t)b * o_sb + (size_t)hq * o_sh + slice * (2 * LANES) + 2 * col;
     const int len = dep_load(c.lens + b);
     const int2 rg = ranges[bh];                                // (of an empty sequence: not written, not used)
-    if (len <= 0 || len > n) {                                 // nothing to attend
-        if (row == 0) dst[0] = dst[1] = __float2bfloat16(0.f);
-        if (t == 0 && slice == 0) lse[head] = -INFINITY;
-        return;
-    }
     const int cnt = rg.y - rg.x + 1;
-    if (cnt == 1) return;                                      // written by its CTA
+    if (len <= 0 || len > n || cnt == 1) return;               // written by a CTA of the partial pass
     const float* p = part + ((size_t)(bh + rg.x) * G + (hq - hk * G)) * (D + 2);
     const float* pv = p + 2 + slice * (2 * LANES) + 2 * col;
     const size_t step = (size_t)G * (D + 2);
@@ -760,7 +770,8 @@ size_t kv4_decode_workspace_bytes(const focus_shape* s) {
 template <int D, int GP>
 static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
                     float scale, int32_t* status, cudaStream_t st) {
-    const long long most = (long long)s->batch * s->Hkv * cdiv(s->n, KD_UNIT);
+    const int span = s->n <= KD_ALONE ? cdiv(s->n, KdCfg<D>::UNIT) : 0;
+    const long long most = (long long)s->batch * s->Hkv * (span > 0 ? 1 : cdiv(s->n, KdCfg<D>::UNIT));
     const int grid = (int)(most < KdCfg<D>::CTAS ? most : KdCfg<D>::CTAS);
     const int G = s->Hq / s->Hkv;
     int2* ranges = reinterpret_cast<int2*>(ws);
@@ -768,9 +779,9 @@ static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor&
     int rc = check_cuda(allow_smem<kv4_decode_kernel<D, GP>>(KdCfg<D>::SMEM, true), "cudaFuncSetAttribute(kv4 decode)");
     if (rc) return rc;
     rc = check_cuda(launch_dependent(kv4_decode_kernel<D, GP>, dim3(grid), dim3(KD_WARPS * 32), KdCfg<D>::SMEM, st, c, reinterpret_cast<const __nv_bfloat16*>(q.ptr),
-                                         q.stride_b, q.stride_h, mq_new, s->batch, s->Hq, G, s->n, s->window, scale, s->softcap, part, ranges,
+                                         q.stride_b, q.stride_h, mq_new, s->batch, s->Hq, G, s->n, span, s->window, scale, s->softcap, part, ranges,
                                          reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse, status), "kv4 decode kernel launch");
-    if (rc) return rc;
+    if (rc || span > 0) return rc;                             // (every head is one CTA's)
     const bool narrow = (long long)s->batch * s->Hq * (D / 32) <= KD_SMS * 8;
     return check_cuda(launch_dependent(narrow ? kv4_merge_kernel<D, 16> : kv4_merge_kernel<D, D / 2>, dim3(s->batch * s->Hq * (narrow ? D / 32 : 1)), dim3(256), 0, st, c, part, ranges, s->Hq, G, s->n,
                                        reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse), "kv4 merge kernel launch");
@@ -789,7 +800,7 @@ static int decode_d(const focus_shape* s, const Kv4View& c, const focus_tensor& 
 int kv4_decode_check(const focus_shape* s, const Kv4View& c) {
     if (s->Hq / s->Hkv > KD_GMAX) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d query heads per KV head", KD_GMAX);
     if (s->batch > KD_MAX_BATCH) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d sequences in one call", KD_MAX_BATCH);
-    if ((long long)s->batch * s->Hkv * cdiv(s->n, KD_UNIT) >= (1ll << 29)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: batch * Hkv * n is too large");
+    if ((long long)s->batch * s->Hkv * cdiv(s->n, 64) >= (1ll << 28)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: batch * Hkv * n is too large");
     // listed keys say where their codes are in 16 bytes and their scales in 8
     if ((size_t)c.num_pages * c.page_bytes >= (1ull << 35)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: a pool of 32 GiB or more");
     return FOCUS_OK;

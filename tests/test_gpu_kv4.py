@@ -222,7 +222,9 @@ def test_decode_softcap_and_scale(D, cap, scale):
     compare(o, lse, lens, q, mq, mk, *stored(cache, 4, D, 700), 20, cap, scale)
 
 
-@pytest.mark.parametrize("batch,Hq,Hkv,most,D", [(150, 4, 4, 90, 128), (40, 8, 8, 700, 64), (600, 2, 1, 40, 128), (3, 8, 2, 30000, 128), (9, 16, 2, 9000, 256), (1024, 2, 2, 20, 64)])
+@pytest.mark.parametrize("batch,Hq,Hkv,most,D", [(150, 4, 4, 90, 128), (40, 8, 8, 700, 64), (600, 2, 1, 40, 128), (3, 8, 2, 30000, 128), (9, 16, 2, 9000, 256), (1024, 2, 2, 20, 64),
+                                                   (32, 4, 2, 257, 128), (33, 4, 2, 256, 64), (128, 8, 8, 300, 128), (129, 2, 2, 500, 256), (500, 1, 1, 255, 128),
+                                                   (128, 16, 2, 100, 128), (5, 8, 8, 256, 256), (97, 4, 1, 2000, 64)])
 def test_decode_ranges_across_heads(batch, Hq, Hkv, most, D):
     """ranges of the list of units that cover several heads and sequences, end inside one, or are whole ones"""
     g = torch.Generator().manual_seed(batch)

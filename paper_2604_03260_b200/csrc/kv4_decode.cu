@@ -125,7 +125,8 @@ __device__ __forceinline__ int kd_spot(int x) { return (x & ~(KEYS - 1)) + (x & 
 // contiguous ranges of `per` units.  A CTA whose range enters another head writes one more partial result and starts over, which takes as
 // long as TURN units: every head ends with that many empty ones, so that such a CTA gets the fewer keys (24 ragged sequences: 58 -> 52 us).
 // Where whole ranges per head make no longer ranges, the heads are padded to them instead; where no sequence can be longer than KD_ALONE,
-// they are padded to `span` units, its length, and a range is whole heads.  The lengths are on the device, and so every CTA works this out
+// they are padded to `span` units, its length, and a range is whole heads (one each, CTA by CTA and with nothing to work out, where there
+// are no more of them than CTAs: `direct`).  The lengths are on the device, and so every CTA works this out
 // for itself (every warp for itself, up to 32 sequences); the sums are over the sequences of the batch.
 struct KdPlan {
     int per, pad;                        // units of a range; heads are padded to multiples of `pad`, or by TURN (0)
@@ -179,8 +180,13 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     // ---- the plan (the host has seen to it that the list has fewer than 2^29 units)
     KdPlan plan;
     int total;
-    const int len0 = lane < batch ? kd_length(c, lane, n, blockIdx.x == 0 && warp == 0 ? status : nullptr) : 0;   // of the first 32 sequences
-    {
+    const bool direct = span > 0 && (int)gridDim.x == batch * Hkv;
+    int len0 = 0;                                              // lengths of the first 32 sequences
+    if (direct) {
+        plan.per = plan.pad = span;
+        total = batch * Hkv * span;
+    } else {
+        len0 = lane < batch ? kd_length(c, lane, n, blockIdx.x == 0 && warp == 0 ? status : nullptr) : 0;
         const int ctas = gridDim.x;
         int sum = kd_cdiv(len0, C::UNIT), turns = len0 > 0 ? C::TURN : 0;
         // a wider batch: the warps share the rest out (every warp has the first 32)
@@ -254,7 +260,12 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
     for (int f = (int)blockIdx.x * plan.per; f < f_end;) {
         // ---- the sequence and head of unit f (every warp for itself)
         int b, len, start;
-        {
+        if (direct) {
+            b = (int)blockIdx.x / Hkv;
+            len = kd_length(c, b, n, status);
+            start = b * Hkv * span;
+            if (len == 0) break;
+        } else {
             int ch = 0, base = 0, l = len0;
             if (batch > 32) {
                 while (ch < kd_cdiv(batch, 32) - 1 && chunk_s[ch + 1] <= f) ++ch;      // (lengths that change under the kernel do not lead beyond it)
@@ -276,7 +287,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             len = __shfl_sync(0xffffffffu, l, at);
             start = __shfl_sync(0xffffffffu, incl - u, at);
         }
-        const int units = kd_cdiv(len, C::UNIT), stride = kd_padded<D>(len, plan);
+        const int units = kd_cdiv(len, C::UNIT), stride = direct ? span : kd_padded<D>(len, plan);
         const int hk = (f - start) / stride;
         const int f0 = start + hk * stride;                    // the head's first unit
         const int bh = b * Hkv + hk;

@@ -7,7 +7,8 @@
 // HBM-bound: every vector read once and written once (backward: vectors and gradients read, gradients written).  One pass over them, rows
 // under way in shared memory; what is left to the bound is the start of a CTA, before which its angles and weights have to be there (8192
 // tokens, 32 + 8 heads of 128, bf16: forward 29.3 us, 5.7 TB/s, 87 % of what a copy reaches; backward with the weights' gradients 47.5 us,
-// 5.3 TB/s, 81 %).  Few rows are bound by latency: the forward pass over 16 sequences of one token takes 2.8 us.
+// 5.3 TB/s, 81 %).  Few rows are bound by latency: the forward pass over 16 sequences of one token takes 2.9 us, the backward pass over
+// 1024 tokens of 12 + 12 heads of 64 takes 9.9 with the sums of the weights' gradients.
 #include "common.cuh"
 #include "f32x2.cuh"
 
@@ -34,7 +35,9 @@ struct RopeArgs {
     FixedDiv by_seq[2];                           // division by per_seq
     uint32_t parts;                               // forward: parts that a tile's heads are cut into
     FixedDiv by_parts;
-    int ctas[2];                                  // backward: CTAs of a side
+    int ctas[2], passes[2];                       // backward: CTAs of a side, passes of a tile;
+    int whole[2], rest[2], over[2];               // whole tiles of each CTA, passes behind those, CTAs that share them
+    FixedDiv by_passes[2];
 };
 
 // cos and sin (times the amplitude) of position * freq: the angle is reduced in 64 bits, since positions reach a million and fp32 would
@@ -306,8 +309,11 @@ qk_norm_rope_kernel(const RopeArgs a) {
     }
 }
 
-// Backward: the CTAs of a side walk its tiles of tokens, all heads of a tile, the copies two rows ahead; the sums over rows of g xhat stay in
-// registers to the end, then go to `partial`.
+// Backward: the CTAs of a side walk its tiles of tokens, all heads of a tile, side by side; the tiles behind
+// the last round, too few for all CTAs, are dealt out pass by pass (12 heads of 64, 3 sequences of 1021 tokens: 14.3 -> 12.1 us).  Behind four
+// rounds and more it is a tile per CTA, as the memory is busy without the others (32 + 8 heads of 128, 8192 tokens: 47.5 us, and 48.6 pass by
+// pass; dealt out in one piece per CTA 49.5).  The copies go two rows ahead.  The sums over rows of g xhat stay in registers to the end, then go to
+// `partial`.
 constexpr int ROPE_BWD_STAGES = 3;
 template <int D>
 struct RopeBwd {
@@ -327,62 +333,73 @@ qk_norm_rope_bwd_kernel(const RopeArgs a) {
     const int unit = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
     const int side = (int)blockIdx.x >= a.ctas[0];
     const int id = blockIdx.x - (side ? a.ctas[0] : 0);
-    const int lgT = a.lgT[side], T = 1 << lgT, tiles = a.batch * a.per_seq[side];
+    const int lgT = a.lgT[side], T = 1 << lgT;
     const int tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT, H = a.heads[side];
     const RopePlace at = rope_place(a, unit);
     const int apart = at.d1 - at.d0;
     const bool norm = a.w[side] != nullptr;
-    const int64_t x_step = hstep * a.x_h[side], g_step = hstep * a.g_h[side], o_step = hstep * a.o_h[side];
+    const int64_t o_step = hstep * a.o_h[side];
     dep_wait();
     dep_trigger();
     rope_put_weights<D>(w_s, a, side);
     RopeUnit dw;
 #pragma unroll
     for (int e = 0; e < 4; ++e) dw.p[e] = dw.r[e] = f2(0.f, 0.f);
+    const int passes = a.passes[side];
+    const int whole = a.whole[side], over = a.over[side], rest_lo = (int)((long long)a.rest[side] * min(id, over) / over);
+    int left = whole * passes + (int)((long long)a.rest[side] * min(id + 1, over) / over) - rest_lo;
+    // the CTA's i-th tile, after `tile`, and its first pass there
+    auto enter = [&](int i, int& tile, int& k) {
+        tile = i < whole ? id + i * a.ctas[side] : i > whole ? tile + 1 : whole * a.ctas[side] + (int)a.by_passes[side](rest_lo);
+        k = i == whole ? rest_lo - (tile - whole * a.ctas[side]) * passes : 0;
+    };
     // the copies' own walk over the rows, ahead of the work's
     const uint32_t stages = (uint32_t)__cvta_generic_to_shared(smem);
-    int c_tile = id, c_h = 0, into = 0;
+    int c_left = left, c_i = 0, c_tile = 0, c_k = 0, c_h = 0, into = 0;
     const __nv_bfloat16 *xp = nullptr, *gp = nullptr;
     bool c_live = false;
-    auto aim = [&] {                                           // at the rows of the tile c_tile
+    auto aim = [&] {                                           // at the rows of the next tile
+        enter(c_i++, c_tile, c_k);
         const int b = a.by_seq[side](c_tile), t0 = (int)(c_tile - b * a.per_seq[side]) << lgT, t = min(t0 + tok, a.n - 1);
         c_live = t0 + tok < a.n;
         xp = a.x[side] + b * a.x_b[side] + t * a.x_n[side] + at.d0;
         gp = a.g[side] + b * a.g_b[side] + t * a.g_n[side] + at.d0;
-        c_h = hofs;
+        c_h = c_k * hstep + hofs;
     };
     auto issue = [&] {
-        if (c_tile < tiles) {
+        if (c_left > 0) {
             const bool on = c_live && c_h < H;
             const __nv_bfloat16* p = gp + (on ? c_h : 0) * a.g_h[side];
             rope_copy(stages + rope_place_of(into, 4, 0), p, on);
             rope_copy(stages + rope_place_of(into, 4, 1), p + apart, on);
             if (norm) {
-                const __nv_bfloat16* q = xp + (on ? c_h : 0) * a.x_h[side];
-                rope_copy(stages + rope_place_of(into, 4, 2), q, on);
-                rope_copy(stages + rope_place_of(into, 4, 3), q + apart, on);
+                p = xp + (on ? c_h : 0) * a.x_h[side];
+                rope_copy(stages + rope_place_of(into, 4, 2), p, on);
+                rope_copy(stages + rope_place_of(into, 4, 3), p + apart, on);
             }
             c_h += hstep;
-            if (c_h - hofs >= H) {
-                c_tile += a.ctas[side];
-                if (c_tile < tiles) aim();
-            }
+            --c_left;
+            if (++c_k == passes && c_left > 0) aim();
         }
         into = into == STAGES - 1 ? 0 : into + 1;
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if (c_tile < tiles) aim();
+    if (c_left > 0) aim();
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) issue();
     int buf = 0, from = 0;
-    for (int tile = id; tile < tiles; tile += a.ctas[side], buf ^= 1) {
+    for (int i = 0, tile = 0, k0; left > 0; ++i, buf ^= 1) {
+        enter(i, tile, k0);
         const int b = a.by_seq[side](tile), t0 = (int)(tile - b * a.per_seq[side]) << lgT, t = min(t0 + tok, a.n - 1);
         const bool live = t0 + tok < a.n;
-        __nv_bfloat16* z = a.out[side] + b * a.o_b[side] + t * a.o_n[side] + hofs * a.o_h[side] + at.d0;
+        const int count = min(passes - k0, left);
+        left -= count;
+        int h = k0 * hstep + hofs;
+        __nv_bfloat16* z = a.out[side] + b * a.o_b[side] + t * a.o_n[side] + h * a.o_h[side] + at.d0;
         rope_put_angles<D>(cs_s[buf], a, b, t0, T, -1.f);      // (worked out a tile ahead instead: 47.6 -> 49.0 us)
         __syncthreads();                                       // (the other table is free: its readers have passed this barrier)
         const RopeAngles ang = rope_get_angles(cs_s[buf][tok][unit]);
-        for (int h = hofs; h - hofs < H; h += hstep) {
+        for (int k = 0; k < count; ++k, h += hstep) {
             const bool on = live && h < H;
             issue();                                           // into the stage that the row before has left
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
@@ -574,6 +591,7 @@ static int rope_tile(int rows, int heads, int batch, int n) {
 }
 
 constexpr int ROPE_PASSES = 8;                    // of a CTA over a tile's heads
+constexpr int ROPE_EVEN = 4;                      // rounds of whole tiles up to which the tiles behind them are dealt out pass by pass, see above
 
 template <int D>
 static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq, float* dwk, cudaStream_t st) {
@@ -599,20 +617,33 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
         return check_cuda(launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)(tiles * parts)), dim3(ROPE_THREADS), smem, st, a),
                           "norm and rotation kernel launch");
     }
-    long long tiles[2];
+    long long work[2];                            // passes of a side (of the kernel for odd halves: eight rows)
     for (int i = 0; i < 2; ++i) {
-        a.lgT[i] = rope_tile(ROPE_PASSES * C::RPP, a.heads[i], s->batch, s->n);
-        a.per_seq[i] = cdiv(s->n, 1 << a.lgT[i]);
+        // tokens per tile: 16, as above, with passes enough for all CTAs
+        const int H = a.heads[i];
+        int lg = 0;
+        while ((2 << lg) <= ROPE_TOKENS && (long long)(2 << lg) * H <= ROPE_PASSES * C::RPP &&
+               (long long)s->batch * cdiv(s->n, 2 << lg) * cdiv(H, C::RPP >> (lg + 1)) >= 2 * ROPE_SMS) ++lg;
+        a.lgT[i] = lg;
+        a.per_seq[i] = cdiv(s->n, 1 << lg);
         a.by_seq[i] = fixed_div(a.per_seq[i]);
-        tiles[i] = (long long)s->batch * a.per_seq[i];
+        a.passes[i] = cdiv(H, C::RPP >> lg);
+        a.by_passes[i] = fixed_div(a.passes[i]);
+        work[i] = odd ? (tokens + 7) / 8 : (long long)s->batch * a.per_seq[i] * a.passes[i];
+        if (work[i] >= (1ll << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: batch * n * heads (%lld rows) is too large for one call", tokens * H);
     }
-    // CTAs of the two sides: in proportion to their heads, no more than they have tiles (or rows for the warps)
+    // CTAs of the two sides: in proportion to their heads, no more than they have work
     const int places = bwd && !odd ? 2 * ROPE_SMS : ROPE_GRID;
-    if (odd) tiles[0] = tiles[1] = (tokens + 7) / 8;
     int kc = (int)((long long)places * a.heads[1] / (a.heads[0] + a.heads[1]));
     if (kc < 1) kc = 1;
-    a.ctas[0] = (int)(tiles[0] < places - kc ? tiles[0] : places - kc);
-    a.ctas[1] = (int)(tiles[1] < kc ? tiles[1] : kc);
+    a.ctas[0] = (int)(work[0] < places - kc ? work[0] : places - kc);
+    a.ctas[1] = (int)(work[1] < kc ? work[1] : kc);
+    for (int i = 0; i < 2; ++i) {
+        a.whole[i] = s->batch * a.per_seq[i] / a.ctas[i];
+        const int tiles = s->batch * a.per_seq[i] - a.whole[i] * a.ctas[i];
+        a.rest[i] = tiles * a.passes[i];
+        a.over[i] = a.whole[i] < ROPE_EVEN || tiles == 0 ? a.ctas[i] : tiles;
+    }
     const dim3 g(a.ctas[0] + a.ctas[1]), t(ROPE_THREADS);
     int rc = odd ? FOCUS_OK : check_cuda(allow_smem<qk_norm_rope_bwd_kernel<D>>(RopeBwd<D>::SMEM), "cudaFuncSetAttribute(norm and rotation backward)");
     if (rc) return rc;

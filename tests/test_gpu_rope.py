@@ -60,6 +60,8 @@ CASES = [  # D, Hq, Hkv, B, n, rotary, interleaved, norm, layout
     (64, 3, 1, 2, 19, 2, False, True, "head"), (256, 2, 1, 1, 21, 250, False, True, "token"), (128, 5, 5, 1, 31, 70, True, True, "token"),
     (256, 2, 2, 1, 9, 6, False, False, "token"), (128, 1, 1, 1, 5000, 128, False, True, "head"), (64, 2, 1, 300, 1, 64, False, True, "token"),
     (128, 40, 1, 1, 2500, 96, False, True, "token"),
+    # one round of whole tiles and a few behind it, two, five
+    (64, 12, 12, 3, 1021, 32, True, True, "token"), (256, 16, 8, 1, 2600, 256, False, True, "head"), (64, 12, 4, 8, 1301, 64, False, True, "token"),
 ]
 
 

@@ -12,8 +12,9 @@ bookkeeping.  The entry points that it calls are those of the C ABI (through ``b
     free      a sequence is forgotten; pages that no other sequence shares are free again
     compact   pages in use move to the front of the pool (focus_kv4_copy_pages)
 
-A call whose pages do not fit raises ``FocusError`` (capacity) and changes nothing.  All calls enqueue on the current stream (or
-``stream``), as the entry points do; use one stream, or order them.  Sequences without tokens take part in ``decode`` with o = 0.
+A call whose pages do not fit raises ``FocusError`` (capacity), one whose tensors are refused what ``binding`` raises; neither changes
+what the sequences hold.  All calls enqueue on the current stream (or ``stream``), as the entry points do; use one stream, or order
+them.  Sequences without tokens take part in ``decode`` with o = 0.
 """
 from __future__ import annotations
 
@@ -108,10 +109,16 @@ class Kv4Cache:
         each = [n] * self.B if counts is None else list(counts)
         if len(each) != self.B or max(each) > n:
             raise fb.FocusError(-1, f"one count of at most {n} per sequence is wanted")
+        before = self.refs, self.held, self.tokens
         self.reserve(each, stream)
-        with torch.cuda.stream(stream):
-            dev = None if counts is None else torch.tensor(each, dtype=torch.int32).to(self.device)
-        fb.focus_kv4_append(self._shape(n), self.cache, k, v, mk, dev, self.status, stream)
+        try:
+            with torch.cuda.stream(stream):
+                dev = None if counts is None else torch.tensor(each, dtype=torch.int32).to(self.device)
+            fb.focus_kv4_append(self._shape(n), self.cache, k, v, mk, dev, self.status, stream)
+        except Exception:                                  # refused: nothing is written, and the tokens do not count
+            self.refs, self.held, self.tokens = before
+            self._push(stream)
+            raise
         if dev is not None and stream is not None:
             dev.record_stream(stream)
 

@@ -499,6 +499,22 @@ def test_refusals_on_the_gpu():
         decode(cache, fb.make_shape(4, 2, 10, 128, 4, 2, 0, batch=2), torch.cat([q, q]), torch.cat([mq, mq]))
 
 
+def test_a_refused_append_counts_no_tokens():
+    B, Hkv, D = 2, 2, 64
+    layer = Kv4Cache(B, 4, Hkv, D, 4, 2, 16, max_tokens=64, num_pages=6, page_tokens=16)
+    k = torch.randn((B, Hkv, 5, D), device="cuda").to(torch.bfloat16)
+    mk = torch.ones((B * Hkv, 5), dtype=torch.int32, device="cuda")
+    layer.append(k, k, mk, [5, 3])
+    before = layer.pages.clone(), list(layer.refs), [list(p) for p in layer.held], list(layer.tokens), layer.table.clone(), layer.lens.clone()
+    for bad in ((k.float(), k, mk), (k, k[:, :1], mk), (k, k, mk[:, :4])):
+        with pytest.raises((AssertionError, fb.FocusError)):
+            layer.append(*bad)
+    assert torch.equal(layer.pages, before[0]) and (layer.refs, layer.held, layer.tokens) == before[1:4]
+    assert torch.equal(layer.table, before[4]) and torch.equal(layer.lens, before[5])
+    layer.append(k, k, mk)
+    assert layer.tokens == [10, 8] and layer.lens.tolist() == [10, 8] and layer.status.tolist() == [0] * 4
+
+
 def test_a_serving_loop():
     """norm and rotation, groups, append, decode step by step, a fork, a sequence freed, the pool compacted: against attention in 64 bits
     over what was stored"""

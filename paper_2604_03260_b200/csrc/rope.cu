@@ -6,9 +6,9 @@
 //   dx = r (u - xhat mean(u xhat)),   dw = sum over rows of g xhat.
 // HBM-bound: every vector read once and written once (backward: vectors and gradients read, gradients written).  One pass over them, rows
 // under way in shared memory; what is left to the bound is the start of a CTA, before which its angles and weights have to be there (8192
-// tokens, 32 + 8 heads of 128, bf16: forward 29.3 us, 5.7 TB/s, 87 % of what a copy reaches; backward with the weights' gradients 47.5 us,
-// 5.3 TB/s, 81 %).  Few rows are bound by latency: the forward pass over 16 sequences of one token takes 2.9 us, the backward pass over
-// 1024 tokens of 12 + 12 heads of 64 takes 9.9 with the sums of the weights' gradients.
+// tokens, 32 + 8 heads of 128, bf16: forward 28.9 us, 5.8 TB/s, 88 % of what a copy reaches; backward with the weights' gradients 46.8 us,
+// 5.4 TB/s, 82 %).  Few rows are bound by latency: the forward pass over 16 sequences of one token takes 2.9 us, the backward pass over
+// 3 sequences of 1021 tokens of 12 + 12 heads of 64 takes 9.7 with the sums of the weights' gradients.
 #include "common.cuh"
 #include "f32x2.cuh"
 
@@ -29,7 +29,7 @@ struct RopeArgs {
     const double* freq;
     const int32_t* positions;
     float* partial;                               // backward with a norm: [CTAs of a side][D] sums of g xhat, queries' CTAs first
-    int heads[2], batch, n, rot, interleaved;
+    int heads[2], batch, n, rot;
     float eps, amplitude;
     int lgT[2], per_seq[2];                       // tokens per tile (log), tiles per sequence (forward: [0] for both sides)
     FixedDiv by_seq[2];                           // division by per_seq
@@ -51,9 +51,11 @@ __device__ __forceinline__ float2 rope_cos_sin(const RopeArgs& a, int pos, int f
 }
 
 // A row is cut into units of 16 dimensions, one per lane: two 16-byte pieces, whose eight pairs are turned.  Rotating halves, unit
-// u < rot / 16 has the pieces at 8 u and rot / 2 + 8 u; interleaved, and behind the rotated part, the two from 16 u on.  In registers a unit
-// is the pairs' first numbers and their second ones, which only the unpacking tells apart: in halves the first piece and the second,
-// interleaved the low and the high numbers of the words.
+// u < rot / 16 has the pieces at 8 u and rot / 2 + 8 u, and behind the rotated part the pieces likewise lie half of the rest apart; interleaved, every
+// piece is four whole pairs, and they lie D / 2 apart: so neighbouring lanes have neighbouring pieces (interleaved with both pieces of a lane side by
+// side, whose every 32 bytes are then asked for twice: 8192 tokens forward 40.8 us, not 28.3, backward 70.5, not 46.8).  In registers a unit is
+// the pairs' first numbers and their second ones, which only the unpacking tells apart (and tables; a template's flag, since a branch on it per row costs 5 %): in halves the first piece and the second, interleaved
+// the low and the high numbers of the words.
 template <int D> struct RopeCfg {
     static constexpr int LPR = D / 16;                        // lanes per row
     static constexpr int RPP = ROPE_THREADS / LPR;            // rows per pass of a CTA
@@ -64,10 +66,11 @@ struct RopeUnit {
 };
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ RopeUnit rope_unpack(const uint4 (&raw)[2], bool inter) {
+template <bool INTER>
+__device__ __forceinline__ RopeUnit rope_unpack(const uint4 (&raw)[2]) {
     const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
     RopeUnit u;
-    if (inter) {
+    if constexpr (INTER) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             u.p[i] = f2(bf_lo(w[2 * i]), bf_lo(w[2 * i + 1]));
@@ -86,9 +89,10 @@ __device__ __forceinline__ uint32_t bf_pack(float lo, float hi) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&t);
 }
-__device__ __forceinline__ void rope_pack(const RopeUnit& u, bool inter, uint4 (&raw)[2]) {
+template <bool INTER>
+__device__ __forceinline__ void rope_pack(const RopeUnit& u, uint4 (&raw)[2]) {
     uint32_t w[8];
-    if (inter) {
+    if constexpr (INTER) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 p = f2_get(u.p[i]), r = f2_get(u.r[i]);
@@ -135,36 +139,37 @@ __device__ __forceinline__ float rope_row_sum(float x) {
 // where a lane's unit lies in a row
 struct RopePlace {
     int d0, d1;
-    bool inter;
 };
+template <int D, bool INTER>
 __device__ __forceinline__ RopePlace rope_place(const RopeArgs& a, int u) {
     RopePlace x;
-    x.inter = a.interleaved || 16 * u >= a.rot;
-    x.d0 = x.inter ? 16 * u : 8 * u;
-    x.d1 = x.inter ? 16 * u + 8 : a.rot / 2 + 8 * u;
+    const bool rest = !INTER && 16 * u >= a.rot;
+    x.d0 = 8 * u + (rest ? a.rot / 2 : 0);         // (rot + 8 (u - rot / 16))
+    x.d1 = x.d0 + (INTER ? D : rest ? D - a.rot : a.rot) / 2;
     return x;
 }
 // Weights and angles wait in shared memory as the units want them, 16 numbers each (firsts then seconds; cosines then sines), 4 numbers
 // apart: eight lanes read eight units' 16 bytes without asking a bank twice.
 constexpr int ROPE_UROW = 20;
-template <int D>
+template <int D, bool INTER>
 __device__ __forceinline__ void rope_put_weights(float (*w)[ROPE_UROW], const RopeArgs& a, int side) {
     for (int i = threadIdx.x; i < D; i += ROPE_THREADS) {
         const int u = i / 16, e = i % 16;
-        const RopePlace x = rope_place(a, u);
+        const RopePlace x = rope_place<D, INTER>(a, u);
         // e-th number of the unit: pair e % 8, its first (e < 8) or second
-        const int pr = e % 8, d = x.inter ? x.d0 + 2 * pr + e / 8 : (e < 8 ? x.d0 : x.d1) + pr;
+        const int pr = e % 8, d = INTER ? (pr < 4 ? x.d0 : x.d1) + 2 * (pr % 4) + e / 8 : (e < 8 ? x.d0 : x.d1) + pr;
         w[u][e] = a.w[side] ? dep_load(a.w[side] + d) : 1.f;
     }
 }
-template <int D>
+template <int D, bool INTER>
 __device__ __forceinline__ void rope_put_angles(float (*t)[D / 16][ROPE_UROW], const RopeArgs& a, int b, int t0, int T, float sign) {
     for (int i = threadIdx.x; i < T * (D / 2); i += ROPE_THREADS) {
         const int k = i / (D / 2), f = i % (D / 2);
         float2 x = make_float2(1.f, 0.f);                     // (behind the rotated part, and where there is no token)
         if (2 * f < a.rot && t0 + k < a.n) x = rope_cos_sin(a, a.positions ? dep_load(a.positions + (size_t)b * a.n + t0 + k) : t0 + k, f);
-        t[k][f / 8][f % 8] = x.x;
-        t[k][f / 8][8 + f % 8] = sign * x.y;
+        const int u = INTER ? f % (D / 4) / 4 : f / 8, pr = INTER ? f / (D / 4) * 4 + f % 4 : f % 8;
+        t[k][u][pr] = x.x;
+        t[k][u][8 + pr] = sign * x.y;
     }
 }
 __device__ __forceinline__ RopeUnit rope_get(const float* row) {
@@ -198,9 +203,10 @@ __device__ __forceinline__ uint32_t rope_place_of(int stage, int pieces, int i) 
 __device__ __forceinline__ void rope_copy(uint32_t dst, const __nv_bfloat16* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void rope_store(__nv_bfloat16* p, int apart, const RopeUnit& u, bool inter) {
+template <bool INTER>
+__device__ __forceinline__ void rope_store(__nv_bfloat16* p, int apart, const RopeUnit& u) {
     uint4 out[2];
-    rope_pack(u, inter, out);
+    rope_pack<INTER>(u, out);
     *reinterpret_cast<uint4*>(p) = out[0];
     *reinterpret_cast<uint4*>(p + apart) = out[1];
 }
@@ -209,7 +215,7 @@ __device__ __forceinline__ void rope_store(__nv_bfloat16* p, int apart, const Ro
 // and place in the row are the same in every pass, and so what a pair is multiplied by, cosine and sine (worked out once per token) times
 // the side's weights, stays in registers; the row's own scale comes last.
 constexpr int ROPE_FWD_STAGES = 4;
-template <int D>
+template <int D, bool INTER>
 __global__ void __launch_bounds__(ROPE_THREADS, 3)
 qk_norm_rope_kernel(const RopeArgs a) {
     using C = RopeCfg<D>;
@@ -219,7 +225,7 @@ qk_norm_rope_kernel(const RopeArgs a) {
     __shared__ __align__(16) float w_s[2][D / 16][ROPE_UROW];
     const int unit = threadIdx.x % C::LPR, rs = threadIdx.x / C::LPR;
     const int lgT = a.lgT[0], T = 1 << lgT, tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT;
-    const RopePlace at = rope_place(a, unit);
+    const RopePlace at = rope_place<D, INTER>(a, unit);
     const int apart = at.d1 - at.d0;
     const uint32_t tile = a.by_parts(blockIdx.x), part = blockIdx.x - tile * a.parts;
     const int b = a.by_seq[0](tile), t0 = (int)(tile - b * a.per_seq[0]) << lgT, t = min(t0 + tok, a.n - 1);
@@ -265,9 +271,9 @@ qk_norm_rope_kernel(const RopeArgs a) {
     };
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) issue();
-    rope_put_weights<D>(w_s[0], a, 0);
-    rope_put_weights<D>(w_s[1], a, 1);
-    rope_put_angles<D>(cs_s, a, b, t0, T, 1.f);
+    rope_put_weights<D, INTER>(w_s[0], a, 0);
+    rope_put_weights<D, INTER>(w_s[1], a, 1);
+    rope_put_angles<D, INTER>(cs_s, a, b, t0, T, 1.f);
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -293,7 +299,7 @@ qk_norm_rope_kernel(const RopeArgs a) {
             uint4 raw[2];
             raw[0] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 2, 0));
             raw[1] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 2, 1));
-            RopeUnit x = rope_unpack(raw, at.inter);
+            RopeUnit x = rope_unpack<INTER>(raw);
             const float r = norm ? rsqrtf(rope_row_sum<C::LPR>(rope_dot(x, x)) * (1.f / D) + a.eps) : 1.f;
             const F2 r2 = f2(r, r);
 #pragma unroll
@@ -302,7 +308,7 @@ qk_norm_rope_kernel(const RopeArgs a) {
                 x.p[e] = f2_mul(f2_fma(q, B[e], f2_mul(p, A[e])), r2);
                 x.r[e] = f2_mul(f2_fma(q, F[e], f2_mul(p, E[e])), r2);
             }
-            if (live && h_lo[s] + k * hstep < h_hi[s]) rope_store(z, apart, x, at.inter);
+            if (live && h_lo[s] + k * hstep < h_hi[s]) rope_store<INTER>(z, apart, x);
             z += o_step;
             from = (from + 1) % STAGES;
         }
@@ -310,7 +316,7 @@ qk_norm_rope_kernel(const RopeArgs a) {
 }
 
 // Backward: the CTAs of a side walk its tiles of tokens, all heads of a tile, side by side; the tiles behind
-// the last round, too few for all CTAs, are dealt out pass by pass (12 heads of 64, 3 sequences of 1021 tokens: 14.3 -> 12.1 us).  Behind four
+// the last round, too few for all CTAs, are dealt out pass by pass (12 heads of 64, 3 sequences of 1021 tokens: 14.3 -> 12.1 us, when interleaved rows cost 2.4 more).  Behind four
 // rounds and more it is a tile per CTA, as the memory is busy without the others (32 + 8 heads of 128, 8192 tokens: 47.5 us, and 48.6 pass by
 // pass; dealt out in one piece per CTA 49.5).  The copies go two rows ahead.  The sums over rows of g xhat stay in registers to the end, then go to
 // `partial`.
@@ -321,7 +327,7 @@ struct RopeBwd {
     static constexpr size_t COPIES = (size_t)ROPE_BWD_STAGES * 4 * ROPE_THREADS * 16;
     static constexpr size_t SMEM = COPIES + (TABLES > SUMS ? TABLES : SUMS);
 };
-template <int D>
+template <int D, bool INTER>
 __global__ void __launch_bounds__(ROPE_THREADS, 2)
 qk_norm_rope_bwd_kernel(const RopeArgs a) {
     using C = RopeCfg<D>;
@@ -335,13 +341,13 @@ qk_norm_rope_bwd_kernel(const RopeArgs a) {
     const int id = blockIdx.x - (side ? a.ctas[0] : 0);
     const int lgT = a.lgT[side], T = 1 << lgT;
     const int tok = rs & (T - 1), hofs = rs >> lgT, hstep = C::RPP >> lgT, H = a.heads[side];
-    const RopePlace at = rope_place(a, unit);
+    const RopePlace at = rope_place<D, INTER>(a, unit);
     const int apart = at.d1 - at.d0;
     const bool norm = a.w[side] != nullptr;
     const int64_t o_step = hstep * a.o_h[side];
     dep_wait();
     dep_trigger();
-    rope_put_weights<D>(w_s, a, side);
+    rope_put_weights<D, INTER>(w_s, a, side);
     RopeUnit dw;
 #pragma unroll
     for (int e = 0; e < 4; ++e) dw.p[e] = dw.r[e] = f2(0.f, 0.f);
@@ -396,7 +402,7 @@ qk_norm_rope_bwd_kernel(const RopeArgs a) {
         left -= count;
         int h = k0 * hstep + hofs;
         __nv_bfloat16* z = a.out[side] + b * a.o_b[side] + t * a.o_n[side] + h * a.o_h[side] + at.d0;
-        rope_put_angles<D>(cs_s[buf], a, b, t0, T, -1.f);      // (worked out a tile ahead instead: 47.6 -> 49.0 us)
+        rope_put_angles<D, INTER>(cs_s[buf], a, b, t0, T, -1.f);      // (worked out a tile ahead instead: 47.6 -> 49.0 us)
         __syncthreads();                                       // (the other table is free: its readers have passed this barrier)
         const RopeAngles ang = rope_get_angles(cs_s[buf][tok][unit]);
         for (int k = 0; k < count; ++k, h += hstep) {
@@ -406,12 +412,12 @@ qk_norm_rope_bwd_kernel(const RopeArgs a) {
             uint4 raw[2];
             raw[0] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 4, 0));
             raw[1] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 4, 1));
-            RopeUnit g = rope_unpack(raw, at.inter);
+            RopeUnit g = rope_unpack<INTER>(raw);
             rope_turn(g, ang);
             if (norm) {
                 raw[0] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 4, 2));
                 raw[1] = *reinterpret_cast<const uint4*>(smem + rope_place_of(from, 4, 3));
-                const RopeUnit x = rope_unpack(raw, at.inter);
+                const RopeUnit x = rope_unpack<INTER>(raw);
                 RopeUnit u;
                 {
                     const RopeUnit w = rope_get(w_s[unit]);
@@ -436,7 +442,7 @@ qk_norm_rope_bwd_kernel(const RopeArgs a) {
                     g.r[e] = f2_fma(xq2, mr2, f2_mul(u.r[e], r2));
                 }
             }
-            if (on) rope_store(z, apart, g, at.inter);
+            if (on) rope_store<INTER>(z, apart, g);
             z += o_step;
             from = from == STAGES - 1 ? 0 : from + 1;
         }
@@ -448,8 +454,9 @@ qk_norm_rope_bwd_kernel(const RopeArgs a) {
     for (int e = 0; e < 4; ++e) {
         const float2 p = f2_get(dw.p[e]), r = f2_get(dw.r[e]);
         float* row = red_s[rs];
-        if (at.inter) {
-            row[at.d0 + 4 * e] = p.x; row[at.d0 + 4 * e + 1] = r.x; row[at.d0 + 4 * e + 2] = p.y; row[at.d0 + 4 * e + 3] = r.y;
+        if constexpr (INTER) {
+            float* z = row + (e < 2 ? at.d0 : at.d1) + 4 * (e % 2);
+            z[0] = p.x; z[1] = r.x; z[2] = p.y; z[3] = r.y;
         } else {
             row[at.d0 + 2 * e] = p.x; row[at.d0 + 2 * e + 1] = p.y; row[at.d1 + 2 * e] = r.x; row[at.d1 + 2 * e + 1] = r.y;
         }
@@ -593,10 +600,10 @@ static int rope_tile(int rows, int heads, int batch, int n) {
 constexpr int ROPE_PASSES = 8;                    // of a CTA over a tile's heads
 constexpr int ROPE_EVEN = 4;                      // rounds of whole tiles up to which the tiles behind them are dealt out pass by pass, see above
 
-template <int D>
+template <int D, bool INTER>
 static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq, float* dwk, cudaStream_t st) {
     using C = RopeCfg<D>;
-    const bool odd = !a.interleaved && a.rot % 16 != 0;
+    const bool odd = !INTER && a.rot % 16 != 0;
     const long long tokens = (long long)s->batch * s->n;
     if (tokens >= (1ll << 30)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: batch * n (%lld) is too large for one call", tokens);
     if (!bwd && !odd) {
@@ -612,9 +619,9 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
         a.parts = (uint32_t)parts;
         a.by_parts = fixed_div(a.parts);
         constexpr size_t smem = (size_t)ROPE_FWD_STAGES * 2 * ROPE_THREADS * 16;
-        const int rc = check_cuda(allow_smem<qk_norm_rope_kernel<D>>(smem), "cudaFuncSetAttribute(norm and rotation)");
+        const int rc = check_cuda(allow_smem<qk_norm_rope_kernel<D, INTER>>(smem), "cudaFuncSetAttribute(norm and rotation)");
         if (rc) return rc;
-        return check_cuda(launch_dependent(qk_norm_rope_kernel<D>, dim3((unsigned)(tiles * parts)), dim3(ROPE_THREADS), smem, st, a),
+        return check_cuda(launch_dependent(qk_norm_rope_kernel<D, INTER>, dim3((unsigned)(tiles * parts)), dim3(ROPE_THREADS), smem, st, a),
                           "norm and rotation kernel launch");
     }
     long long work[2];                            // passes of a side (of the kernel for odd halves: eight rows)
@@ -645,11 +652,11 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
         a.over[i] = a.whole[i] < ROPE_EVEN || tiles == 0 ? a.ctas[i] : tiles;
     }
     const dim3 g(a.ctas[0] + a.ctas[1]), t(ROPE_THREADS);
-    int rc = odd ? FOCUS_OK : check_cuda(allow_smem<qk_norm_rope_bwd_kernel<D>>(RopeBwd<D>::SMEM), "cudaFuncSetAttribute(norm and rotation backward)");
+    int rc = odd ? FOCUS_OK : check_cuda(allow_smem<qk_norm_rope_bwd_kernel<D, INTER>>(RopeBwd<D>::SMEM), "cudaFuncSetAttribute(norm and rotation backward)");
     if (rc) return rc;
     rc = odd ? check_cuda(bwd ? launch_dependent(qk_norm_rope_odd_kernel<D, true>, g, t, 0, st, a) : launch_dependent(qk_norm_rope_odd_kernel<D, false>, g, t, 0, st, a),
                               "norm and rotation kernel launch")
-                 : check_cuda(launch_dependent(qk_norm_rope_bwd_kernel<D>, g, t, RopeBwd<D>::SMEM, st, a), "norm and rotation backward kernel launch");
+                 : check_cuda(launch_dependent(qk_norm_rope_bwd_kernel<D, INTER>, g, t, RopeBwd<D>::SMEM, st, a), "norm and rotation backward kernel launch");
     if (rc || !bwd || !a.partial) return rc;
     return check_cuda(launch_dependent(norm_weight_grad_kernel, dim3(2 * D / 32), dim3(32, 32), 0, st, a.partial, a.ctas[0], a.ctas[1], D, dwq, dwk),
                       "norm weight gradient kernel launch");
@@ -679,16 +686,19 @@ int launch_qk_norm_rope(const focus_shape* s, const focus_rope* rope, const focu
     a.batch = s->batch;
     a.n = s->n;
     a.rot = rope->rotary;
-    a.interleaved = rope->interleaved;
     a.eps = rope->eps;
     a.amplitude = rope->amplitude == 0.f ? 1.f : rope->amplitude;
     a.freq = freq;
     a.positions = positions;
     a.partial = w[0] || w[1] ? partial : nullptr;
-    switch (s->D) {
-        case 64: return launch_rope_d<64>(s, a, grads != nullptr, dwq, dwk, st);
-        case 128: return launch_rope_d<128>(s, a, grads != nullptr, dwq, dwk, st);
-        default: return launch_rope_d<256>(s, a, grads != nullptr, dwq, dwk, st);
+    const bool bwd = grads != nullptr;
+    switch (s->D * 2 + (rope->interleaved ? 1 : 0)) {
+        case 128: return launch_rope_d<64, false>(s, a, bwd, dwq, dwk, st);
+        case 129: return launch_rope_d<64, true>(s, a, bwd, dwq, dwk, st);
+        case 256: return launch_rope_d<128, false>(s, a, bwd, dwq, dwk, st);
+        case 257: return launch_rope_d<128, true>(s, a, bwd, dwq, dwk, st);
+        case 512: return launch_rope_d<256, false>(s, a, bwd, dwq, dwk, st);
+        default: return launch_rope_d<256, true>(s, a, bwd, dwq, dwk, st);
     }
 }
 

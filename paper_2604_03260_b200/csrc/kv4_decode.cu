@@ -23,6 +23,8 @@
 
 #include <float.h>
 
+#include <type_traits>
+
 namespace focus {
 
 constexpr int KD_GMAX = 8;
@@ -148,8 +150,9 @@ __device__ __forceinline__ int kd_padded(int len, const KdPlan& p) {
     return u == 0 ? 0 : p.pad > 0 ? kd_cdiv(u, p.pad) * p.pad : u + KdCfg<D>::TURN;
 }
 
-// GP: query heads per KV head, G, rounded up to a power of two
-template <int D, int GP>
+// GP: query heads per KV head, G, rounded up to a power of two; CAP: with a cap on the scores (kernels of their own: 2049 keys
+// without one 9.0 -> 8.5 us, 131072 43.7 -> 42.8)
+template <int D, int GP, bool CAP>
 __global__ void __launch_bounds__(KD_WARPS * 32, KdCfg<D>::PER_SM)
 kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t q_sh, const uint32_t* mq_new, int batch, int Hq, int G, int n, int span, int w,
                   float scale, float softcap, float* part, int2* ranges, __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, float* lse, int32_t* status) {
@@ -479,8 +482,8 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float x = __shfl_sync(0xffffffffu, down, (2 * qd + i) * 4) * c.k_scale * scale;
-                mul[i] = softcap > 0.f ? softcap * KD_LOG2E : x * KD_LOG2E;
-                cap_in[i] = softcap > 0.f ? x / softcap : 0.f;
+                mul[i] = CAP ? softcap * KD_LOG2E : x * KD_LOG2E;
+                cap_in[i] = CAP ? x / softcap : 0.f;
             }
         }
 
@@ -547,7 +550,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                     y[u][e + 1] = t.y;
                 }
             }
-            if (softcap > 0.f) {
+            if constexpr (CAP) {
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -778,7 +781,7 @@ size_t kv4_decode_workspace_bytes(const focus_shape* s) {
     return align_up(heads * sizeof(int2), 16) + (heads + ctas) * (s->Hq / s->Hkv) * (s->D + 2) * sizeof(float);
 }
 
-template <int D, int GP>
+template <int D, int GP, bool CAP>
 static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
                     float scale, int32_t* status, cudaStream_t st) {
     const int span = s->n <= KD_ALONE ? cdiv(s->n, KdCfg<D>::UNIT) : 0;
@@ -787,9 +790,9 @@ static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor&
     const int G = s->Hq / s->Hkv;
     int2* ranges = reinterpret_cast<int2*>(ws);
     float* part = reinterpret_cast<float*>((char*)ws + align_up((size_t)s->batch * s->Hkv * sizeof(int2), 16));
-    int rc = check_cuda(allow_smem<kv4_decode_kernel<D, GP>>(KdCfg<D>::SMEM, true), "cudaFuncSetAttribute(kv4 decode)");
+    int rc = check_cuda(allow_smem<kv4_decode_kernel<D, GP, CAP>>(KdCfg<D>::SMEM, true), "cudaFuncSetAttribute(kv4 decode)");
     if (rc) return rc;
-    rc = check_cuda(launch_dependent(kv4_decode_kernel<D, GP>, dim3(grid), dim3(KD_WARPS * 32), KdCfg<D>::SMEM, st, c, reinterpret_cast<const __nv_bfloat16*>(q.ptr),
+    rc = check_cuda(launch_dependent(kv4_decode_kernel<D, GP, CAP>, dim3(grid), dim3(KD_WARPS * 32), KdCfg<D>::SMEM, st, c, reinterpret_cast<const __nv_bfloat16*>(q.ptr),
                                          q.stride_b, q.stride_h, mq_new, s->batch, s->Hq, G, s->n, span, s->window, scale, s->softcap, part, ranges,
                                          reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse, status), "kv4 decode kernel launch");
     if (rc || span > 0) return rc;                             // (every head is one CTA's)
@@ -802,10 +805,15 @@ template <int D>
 static int decode_d(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
                     float scale, int32_t* status, cudaStream_t st) {
     const int G = s->Hq / s->Hkv;
-    if (G == 1) return decode_dg<D, 1>(s, c, q, mq_new, o, lse, ws, scale, status, st);
-    if (G == 2) return decode_dg<D, 2>(s, c, q, mq_new, o, lse, ws, scale, status, st);
-    if (G <= 4) return decode_dg<D, 4>(s, c, q, mq_new, o, lse, ws, scale, status, st);
-    return decode_dg<D, 8>(s, c, q, mq_new, o, lse, ws, scale, status, st);
+    const bool cap = s->softcap > 0.f;
+    auto go = [&](auto gp) {
+        constexpr int GP = decltype(gp)::value;
+        return cap ? decode_dg<D, GP, true>(s, c, q, mq_new, o, lse, ws, scale, status, st) : decode_dg<D, GP, false>(s, c, q, mq_new, o, lse, ws, scale, status, st);
+    };
+    if (G == 1) return go(std::integral_constant<int, 1>());
+    if (G == 2) return go(std::integral_constant<int, 2>());
+    if (G <= 4) return go(std::integral_constant<int, 4>());
+    return go(std::integral_constant<int, 8>());
 }
 
 int kv4_decode_check(const focus_shape* s, const Kv4View& c) {

@@ -154,7 +154,7 @@ __device__ __forceinline__ int kd_padded(int len, const KdPlan& p) {
 // without one 9.0 -> 8.5 us, 131072 43.7 -> 42.8)
 template <int D, int GP, bool CAP>
 __global__ void __launch_bounds__(KD_WARPS * 32, KdCfg<D>::PER_SM)
-kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t q_sh, const uint32_t* mq_new, int batch, int Hq, int G, int n, int span, int w,
+kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t q_sh, const uint32_t* mq_new, int batch, int Hq, int G, int n, int span, FixedDiv by_ctas, int w,
                   float scale, float softcap, float* part, int2* ranges, __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, float* lse, int32_t* status) {
     using C = KdCfg<D>;
     constexpr int SUB = C::SUB, KEYS = C::KEYS, STAGES = C::STAGES;
@@ -208,7 +208,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         }
         total = (int)__reduce_add_sync(0xffffffffu, sum) * Hkv;
         const int with_turns = total + (int)__reduce_add_sync(0xffffffffu, turns) * Hkv;
-        const int per0 = total > ctas ? kd_cdiv(total, ctas) : 1;
+        const int per0 = total > ctas ? (int)by_ctas(total + ctas - 1) : 1;
         // three lengths of a range to try with whole ranges per head: the shortest, an eighth and a quarter longer
         const int cand[3] = {per0, per0 + kd_cdiv(per0, 8), per0 + kd_cdiv(per0, 4)};
         int cnt[3];
@@ -231,7 +231,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             for (int i = 0; i < 3; ++i)
                 if (lane < KD_WARPS) cnt[i] += red_s[lane][1 + i];
         }
-        plan.per = kd_cdiv(with_turns, ctas);
+        plan.per = (int)by_ctas(with_turns + ctas - 1);
         plan.pad = 0;
 #pragma unroll
         for (int i = 2; i >= 0; --i)
@@ -268,6 +268,10 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             len = kd_length(c, b, n, status);
             start = b * Hkv * span;
             if (len == 0) break;
+        } else if (batch == 1) {                               // (nothing to search: 2049 keys 8.4 -> 8.2 us)
+            b = 0;
+            len = __shfl_sync(0xffffffffu, len0, 0);
+            start = 0;
         } else {
             int ch = 0, base = 0, l = len0;
             if (batch > 32) {
@@ -793,7 +797,7 @@ static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor&
     int rc = check_cuda(allow_smem<kv4_decode_kernel<D, GP, CAP>>(KdCfg<D>::SMEM, true), "cudaFuncSetAttribute(kv4 decode)");
     if (rc) return rc;
     rc = check_cuda(launch_dependent(kv4_decode_kernel<D, GP, CAP>, dim3(grid), dim3(KD_WARPS * 32), KdCfg<D>::SMEM, st, c, reinterpret_cast<const __nv_bfloat16*>(q.ptr),
-                                         q.stride_b, q.stride_h, mq_new, s->batch, s->Hq, G, s->n, span, s->window, scale, s->softcap, part, ranges,
+                                         q.stride_b, q.stride_h, mq_new, s->batch, s->Hq, G, s->n, span, fixed_div(grid), s->window, scale, s->softcap, part, ranges,
                                          reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse, status), "kv4 decode kernel launch");
     if (rc || span > 0) return rc;                             // (every head is one CTA's)
     const bool narrow = (long long)s->batch * s->Hq * (D / 32) <= KD_SMS * 8;

@@ -14,10 +14,13 @@
 //     instructions for 8 numbers; after it, 8).
 //   - The maximum that probabilities are relative to follows the scores only when one of them is 2^5 beyond it: a vote per tile instead
 //     of six exchanges.
-//   - A warp walks the masks.  16 keys in a row of which most are attended are a tile as they lie (one address); of the others the attended
-//     ones are listed, and 16 off the list are a tile.
+//   - A warp walks the masks.  32 keys (16 at D = 256) that lie together, of which three quarters are attended, are a tile as they lie; of the
+//     others the attended ones are listed, and as many off the list are a tile.
 // Rows come through a ring in shared memory, private to a warp, by asynchronous copies: one address per 16 bytes, none for the operands.
 // Every warp keeps its own maximum, sum and O; a CTA joins its warps, a second kernel the CTAs.
+// Measured (32 + 8 heads of 128): 131072 keys 42.5 us, of which 11 are the plan, the first masks and copies, the joins (24 at the copy rate of all
+// bytes; issue slots 61 %); 24 sequences of 1 to 16385 keys 49.9 us (25.7); 2049 keys 8.1 us.  65536 keys, 16 + 8 heads of 256, 44 % of them
+// attended, with a cap: 38.8 us (11.2).
 #include "kv4_common.cuh"
 #include "f32x2.cuh"
 

@@ -804,8 +804,9 @@ static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor&
                                          reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse, status), "kv4 decode kernel launch");
     if (rc || span > 0) return rc;                             // (every head is one CTA's)
     const bool narrow = (long long)s->batch * s->Hq * (D / 32) <= KD_SMS * 8;
-    return check_cuda(launch_dependent(narrow ? kv4_merge_kernel<D, 16> : kv4_merge_kernel<D, D / 2>, dim3(s->batch * s->Hq * (narrow ? D / 32 : 1)), dim3(256), 0, st, c, part, ranges, s->Hq, G, s->n,
-                                       reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse), "kv4 merge kernel launch");
+    const dim3 blocks(s->batch * s->Hq * (narrow ? D / 32 : 1));
+    return check_cuda(launch_dependent(narrow ? kv4_merge_kernel<D, 16> : kv4_merge_kernel<D, D / 2>, blocks, dim3(256), 0, st, c, part, ranges, s->Hq, G,
+                                       s->n, reinterpret_cast<__nv_bfloat16*>(o.ptr), o.stride_b, o.stride_h, lse), "kv4 merge kernel launch");
 }
 
 template <int D>

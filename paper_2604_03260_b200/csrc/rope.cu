@@ -6,9 +6,9 @@
 //   dx = r (u - xhat mean(u xhat)),   dw = sum over rows of g xhat.
 // HBM-bound: every vector read once and written once (backward: vectors and gradients read, gradients written).  One pass over them, rows
 // under way in shared memory; what is left to the bound is the start of a CTA, before which its angles and weights have to be there (8192
-// tokens, 32 + 8 heads of 128, bf16: forward 28.9 us, 5.8 TB/s, 88 % of what a copy reaches; backward with the weights' gradients 46.8 us,
+// tokens, 32 + 8 heads of 128, bf16: forward 28.9 us, 5.8 TB/s, 88 % of what a copy reaches; backward with the weights' gradients 46.4 us,
 // 5.4 TB/s, 82 %).  Few rows are bound by latency: the forward pass over 16 sequences of one token takes 2.9 us, the backward pass over
-// 3 sequences of 1021 tokens of 12 + 12 heads of 64 takes 9.7 with the sums of the weights' gradients.
+// 3 sequences of 1021 tokens of 12 + 12 heads of 64 takes 9.3 with the sums of the weights' gradients.
 #include "common.cuh"
 #include "f32x2.cuh"
 
@@ -54,8 +54,8 @@ __device__ __forceinline__ float2 rope_cos_sin(const RopeArgs& a, int pos, int f
 // u < rot / 16 has the pieces at 8 u and rot / 2 + 8 u, and behind the rotated part the pieces likewise lie half of the rest apart; interleaved, every
 // piece is four whole pairs, and they lie D / 2 apart: so neighbouring lanes have neighbouring pieces (interleaved with both pieces of a lane side by
 // side, whose every 32 bytes are then asked for twice: 8192 tokens forward 40.8 us, not 28.3, backward 70.5, not 46.8).  In registers a unit is
-// the pairs' first numbers and their second ones, which only the unpacking tells apart (and tables; a template's flag, since a branch on it per row costs 5 %): in halves the first piece and the second, interleaved
-// the low and the high numbers of the words.
+// the pairs' first numbers and their second ones: in halves the first piece and the second, interleaved the low and the high numbers of the
+// words (INTER, a flag of the template: a branch on it in every row costs 5 %).
 template <int D> struct RopeCfg {
     static constexpr int LPR = D / 16;                        // lanes per row
     static constexpr int RPP = ROPE_THREADS / LPR;            // rows per pass of a CTA
@@ -565,26 +565,31 @@ qk_norm_rope_odd_kernel(const RopeArgs a) {
     }
 }
 
-// dw[d] of a side = sum over its CTAs of partial[cta][d]; a block per 32 dimensions, 32 rows of threads in a fixed order
+// dw[d] of a side = sum over its CTAs of partial[cta][d]; a block per 32 dimensions, 32 rows of threads, eight loads of each under way, all sums in
+// a fixed order
 __global__ void __launch_bounds__(1024)
 norm_weight_grad_kernel(const float* partial, int ctas_q, int ctas_k, int D, float* dwq, float* dwk) {
     __shared__ float red[32][33];
-    const int side = blockIdx.x * 32 >= D, col = blockIdx.x * 32 - (side ? D : 0) + threadIdx.x;
+    const int side = blockIdx.x * 32 >= D, col0 = blockIdx.x * 32 - (side ? D : 0), col = col0 + threadIdx.x;
     const int first = side ? ctas_q : 0, last = first + (side ? ctas_k : ctas_q);
     dep_wait();
     dep_trigger();
     float t = 0.f;
-#pragma unroll 4
-    for (int r = first + threadIdx.y; r < last; r += 32) t += dep_load(partial + (size_t)r * D + col);
+    for (int r = first + threadIdx.y; r < last; r += 32 * 8) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = r + 32 * i < last ? dep_load(partial + (size_t)(r + 32 * i) * D + col) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t += x[i];
+    }
     red[threadIdx.y][threadIdx.x] = t;
     __syncthreads();
-    if (threadIdx.y == 0) {
-        t = 0.f;
+    // a warp per column
+    t = red[threadIdx.x][threadIdx.y];
 #pragma unroll
-        for (int r = 0; r < 32; ++r) t += red[r][threadIdx.x];
-        float* dst = side ? dwk : dwq;
-        if (dst) dst[col] = t;
-    }
+    for (int off = 16; off >= 1; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
+    float* dst = side ? dwk : dwq;
+    if (threadIdx.x == 0 && dst) dst[col0 + threadIdx.y] = t;
 }
 
 size_t qk_norm_rope_bwd_workspace_bytes(const focus_shape* s) { return (size_t)ROPE_GRID * s->D * sizeof(float); }

@@ -8,7 +8,7 @@
 // under way in shared memory; what is left to the bound is the start of a CTA, before which its angles and weights have to be there (8192
 // tokens, 32 + 8 heads of 128, bf16: forward 28.9 us, 5.8 TB/s, 88 % of what a copy reaches; backward with the weights' gradients 46.4 us,
 // 5.4 TB/s, 82 %).  Few rows are bound by latency: the forward pass over 16 sequences of one token takes 2.9 us, the backward pass over
-// 3 sequences of 1021 tokens of 12 + 12 heads of 64 takes 9.3 with the sums of the weights' gradients.
+// 3 sequences of 1021 tokens of 12 + 12 heads of 64 takes 9.3 to 9.7 with the sums of the weights' gradients.
 #include "common.cuh"
 #include "f32x2.cuh"
 
@@ -629,28 +629,32 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
         return check_cuda(launch_dependent(qk_norm_rope_kernel<D, INTER>, dim3((unsigned)(tiles * parts)), dim3(ROPE_THREADS), smem, st, a),
                           "norm and rotation kernel launch");
     }
-    long long work[2];                            // passes of a side (of the kernel for odd halves: eight rows)
-    for (int i = 0; i < 2; ++i) {
-        // tokens per tile: 16, as above, with passes enough for all CTAs
-        const int H = a.heads[i];
-        int lg = 0;
-        while ((2 << lg) <= ROPE_TOKENS && (long long)(2 << lg) * H <= ROPE_PASSES * C::RPP &&
-               (long long)s->batch * cdiv(s->n, 2 << lg) * cdiv(H, C::RPP >> (lg + 1)) >= 2 * ROPE_SMS) ++lg;
-        a.lgT[i] = lg;
-        a.per_seq[i] = cdiv(s->n, 1 << lg);
-        a.by_seq[i] = fixed_div(a.per_seq[i]);
-        a.passes[i] = cdiv(H, C::RPP >> lg);
-        a.by_passes[i] = fixed_div(a.passes[i]);
-        work[i] = odd ? (tokens + 7) / 8 : (long long)s->batch * a.per_seq[i] * a.passes[i];
-        if (work[i] >= (1ll << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: batch * n * heads (%lld rows) is too large for one call", tokens * H);
-    }
     // CTAs of the two sides: in proportion to their heads, no more than they have work
     const int places = bwd && !odd ? 2 * ROPE_SMS : ROPE_GRID;
-    int kc = (int)((long long)places * a.heads[1] / (a.heads[0] + a.heads[1]));
-    if (kc < 1) kc = 1;
-    a.ctas[0] = (int)(work[0] < places - kc ? work[0] : places - kc);
-    a.ctas[1] = (int)(work[1] < kc ? work[1] : kc);
+    int share[2] = {0, (int)((long long)places * a.heads[1] / (a.heads[0] + a.heads[1]))};
+    if (share[1] < 1) share[1] = 1;
+    share[0] = places - share[1];
     for (int i = 0; i < 2; ++i) {
+        // tokens per tile: those with the fewest passes and tiles (a tile's angles and barrier take about as long as a pass) one after another
+        // (as many as leave every CTA a pass: 8 sequences of 68 tokens of 12 + 12 heads 9.6 us, not 5.6, 400 tokens of 32 + 8 heads 12.3, not 7.3)
+        const int H = a.heads[i];
+        long long best = 0, work = (tokens + 7) / 8;            // (of the kernel for odd halves: eight rows at a time)
+        for (int lg = 0; !odd && (1 << lg) <= ROPE_TOKENS && (lg == 0 || (long long)(1 << lg) * H <= ROPE_PASSES * C::RPP); ++lg) {
+            const int per_seq = cdiv(s->n, 1 << lg), passes = cdiv(H, C::RPP >> lg);
+            const long long tiles = (long long)s->batch * per_seq, all = tiles * passes;
+            const long long cost = (all + share[i] - 1) / share[i] + (tiles + share[i] - 1) / share[i];
+            if (lg > 0 && cost >= best) continue;
+            best = cost;
+            work = all;
+            a.lgT[i] = lg;
+            a.per_seq[i] = per_seq;
+            a.passes[i] = passes;
+        }
+        if (work >= (1ll << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: batch * n * heads (%lld rows) is too large for one call", tokens * H);
+        a.ctas[i] = (int)(work < share[i] ? work : share[i]);
+        if (odd) continue;
+        a.by_seq[i] = fixed_div(a.per_seq[i]);
+        a.by_passes[i] = fixed_div(a.passes[i]);
         a.whole[i] = s->batch * a.per_seq[i] / a.ctas[i];
         const int tiles = s->batch * a.per_seq[i] - a.whole[i] * a.ctas[i];
         a.rest[i] = tiles * a.passes[i];

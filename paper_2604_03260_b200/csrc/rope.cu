@@ -594,11 +594,12 @@ norm_weight_grad_kernel(const float* partial, int ctas_q, int ctas_k, int D, flo
 
 size_t qk_norm_rope_bwd_workspace_bytes(const focus_shape* s) { return (size_t)ROPE_GRID * s->D * sizeof(float); }
 
-// Tokens per tile: as many as `rows` rows of a CTA have room for all their heads (16 rows of a token block are 4 KB in one piece when the
-// layout is head by head), fewer where that leaves multiprocessors without a tile.
+// Tokens per tile of the forward pass: as many as `rows` rows of a CTA have room for all their heads (16 rows of a token block are 4 KB in one piece
+// when the layout is head by head), fewer where that leaves more than half of the multiprocessors without a tile; where it leaves some, the
+// heads are cut too (1024 tokens of 12 + 12 heads of 64: 3.7 us; fewer tokens from two tiles per multiprocessor on 5.6, from a quarter on 3.8).
 static int rope_tile(int rows, int heads, int batch, int n) {
     int lg = 0;
-    while ((2 << lg) <= ROPE_TOKENS && (long long)(2 << lg) * heads <= rows && (long long)batch * cdiv(n, 2 << lg) >= 2 * ROPE_SMS) ++lg;
+    while ((2 << lg) <= ROPE_TOKENS && (long long)(2 << lg) * heads <= rows && (long long)batch * cdiv(n, 2 << lg) >= ROPE_SMS / 2) ++lg;
     return lg;
 }
 

@@ -34,7 +34,7 @@ constexpr int KD_GMAX = 8;
 constexpr int KD_WARPS = 4;
 constexpr int KD_SMS = 148;
 constexpr int KD_MAX_BATCH = 1024;
-constexpr int KD_ALONE = 256;            // keys up to which a head is one CTA's: no merge (3 us; its warps' second tile takes less than one)
+constexpr int KD_ALONE = 256;            // keys up to which a head is one CTA's even when there are more heads than CTAs, see kd_alone
 constexpr int KD_LIST = 256;             // ring of listed keys: at most 31 left over, 64 new, and those of the tiles under way
 constexpr int KD_BATCH = 64;             // keys whose masks a warp looks at together (128: six registers more, 2 % slower)
 constexpr float KD_LOG2E = 1.4426950408889634f;
@@ -129,7 +129,7 @@ __device__ __forceinline__ int kd_spot(int x) { return (x & ~(KEYS - 1)) + (x & 
 // How the work is cut.  Every KV head of a sequence has ceil(len / UNIT) units; the units of all heads form one list, dealt out in equal
 // contiguous ranges of `per` units.  A CTA whose range enters another head writes one more partial result and starts over, which takes as
 // long as TURN units: every head ends with that many empty ones, so that such a CTA gets the fewer keys (24 ragged sequences: 58 -> 52 us).
-// Where whole ranges per head make no longer ranges, the heads are padded to them instead; where no sequence can be longer than KD_ALONE,
+// Where whole ranges per head make no longer ranges, the heads are padded to them instead; where no sequence can be longer than a CTA's share (kd_alone),
 // they are padded to `span` units, its length, and a range is whole heads (one each, CTA by CTA and with nothing to work out, where there
 // are no more of them than CTAs: `direct`).  The lengths are on the device, and so every CTA works this out
 // for itself (every warp for itself, up to 32 sequences); the sums are over the sequences of the batch.
@@ -788,10 +788,20 @@ size_t kv4_decode_workspace_bytes(const focus_shape* s) {
     return align_up(heads * sizeof(int2), 16) + (heads + ctas) * (s->Hq / s->Hkv) * (s->D + 2) * sizeof(float);
 }
 
+// Whether every head is one CTA's, so that nothing is merged (3 us and more), by the longest length alone.  Heads that have a CTA each: up to 8 units
+// of keys, where few heads leave the machine empty up to 4 (before -> now, us: 1 sequence of 300 keys, 8 KV heads 7.6 -> 6.8, of 600 stays 7.9, would
+// be 8.9; 8 sequences of 500 12.6 -> 8.4, of 900 13.3 -> 12.1; 64 of 1000 30.6 -> 25.3, of 1800 45.7 and would be 40.0, but 30.4 -> 31.9
+// when their lengths differ).  More heads than CTAs: up to KD_ALONE keys (150 sequences of 500: 45.8, would be 44.9, but 32.4 -> 37.5 when they differ).
+template <int D>
+static bool kd_alone(int heads, int n) {
+    const int units = cdiv(n, KdCfg<D>::UNIT);
+    return heads > KdCfg<D>::CTAS ? n <= KD_ALONE : units <= (heads >= 32 ? 8 : 4);
+}
+
 template <int D, int GP, bool CAP>
 static int decode_dg(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o, float* lse, void* ws,
                     float scale, int32_t* status, cudaStream_t st) {
-    const int span = s->n <= KD_ALONE ? cdiv(s->n, KdCfg<D>::UNIT) : 0;
+    const int span = kd_alone<D>(s->batch * s->Hkv, s->n) ? cdiv(s->n, KdCfg<D>::UNIT) : 0;
     const long long most = (long long)s->batch * s->Hkv * (span > 0 ? 1 : cdiv(s->n, KdCfg<D>::UNIT));
     const int grid = (int)(most < KdCfg<D>::CTAS ? most : KdCfg<D>::CTAS);
     const int G = s->Hq / s->Hkv;

@@ -239,6 +239,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
 #pragma unroll
         for (int i = 2; i >= 0; --i)
             if ((int)__reduce_add_sync(0xffffffffu, cnt[i]) * Hkv <= ctas && cand[i] <= plan.per) plan.per = plan.pad = cand[i];
+        // lengths that turn out so short are left whole too (8 sequences of 200 keys of 4296 possible ones 11.6 -> 9.0 us; of 500: ragged 10.7 -> 11.3)
+        if (span == 0 && batch <= 32) {
+            const int longest = (int)__reduce_max_sync(0xffffffffu, kd_cdiv(len0, C::UNIT));
+            if (longest <= 2 && (with_turns - total) / C::TURN <= ctas) plan.per = plan.pad = max(longest, 1);
+        }
         if (span > 0) {                                        // (with_turns - total: TURN for every head that has keys)
             plan.pad = span;
             plan.per = span * max(kd_cdiv((with_turns - total) / C::TURN, ctas), 1);

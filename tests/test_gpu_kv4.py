@@ -241,6 +241,19 @@ def test_decode_ranges_across_heads(batch, Hq, Hkv, most, D):
     assert (o.cpu()[empty] == 0).all() and (lse.cpu()[empty] == -math.inf).all() and o.isfinite().all()
 
 
+@pytest.mark.parametrize("bound", [0, 5000])
+@pytest.mark.parametrize("D,batch,Hkv,most", [(128, 1, 8, 512), (128, 1, 8, 513), (64, 4, 8, 1024), (64, 4, 8, 1025), (256, 3, 2, 256), (256, 3, 2, 257), (256, 4, 8, 512),
+                                              (256, 5, 8, 513), (128, 6, 2, 256), (128, 32, 2, 257), (64, 31, 1, 128), (256, 7, 2, 128), (256, 32, 4, 129), (128, 2, 1, 1)])
+def test_decode_heads_of_one_cta(D, batch, Hkv, most, bound):
+    """the longest lengths of which a head is left whole, and the first that is not, by the bound of the call or by the lengths"""
+    lens = [most if b % 3 == 0 else (37 * b) % (most + 1) for b in range(batch)]
+    Hq = 2 * Hkv
+    cache, q, mq, mk, k, v = filled(lens, 16, Hq, Hkv, D, 4, 2, most + batch, extra=bound // 16 + 1)
+    shape = fb.make_shape(Hq, Hkv, most + bound, D, 4, 2, 9, batch=batch)
+    o, lse = decode(cache, shape, q, mq)
+    compare(o, lse, lens, q, mq, mk, *stored(cache, Hkv, D, most), 9)
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("P,run,hole", [(16, 200, 0.0), (64, 37, 0.2), (128, 700, 0.22), (32, 5, 0.0)])
 def test_decode_runs_and_holes(D, P, run, hole):

@@ -40,7 +40,7 @@ constexpr int KD_BATCH = 64;             // keys whose masks a warp looks at tog
 constexpr float KD_LOG2E = 1.4426950408889634f;
 constexpr float KD_LN2 = 0.6931471805599453f;
 constexpr float KD_PSHIFT = 10.f;
-constexpr float KD_SLACK = 5.f;          // 2^15 < 65504, the largest fp16 number
+constexpr float KD_SLACK = 5.f;          // 2^15 < 65504, the largest fp16 number (`limit` is rounded down, and differences of scores taken before they are scaled)
 
 template <int D> struct KdCfg {
     static constexpr int PER_SM = D == 256 ? 3 : 4;           // CTAs that fit an SM
@@ -499,9 +499,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             }
         }
 
-        // of heads 2 qd, 2 qd + 1; l: this lane's keys alone.  A reference that no key has moved yet is FLT_MAX below everything, and its limit
-        // for y is such that any score but minus infinity is beyond it
-        float m_ref[2] = {-FLT_MAX, -FLT_MAX}, limit[2] = {-FLT_MAX, -FLT_MAX};
+        // of heads 2 qd, 2 qd + 1; l: this lane's keys alone.  The reference is a y: near it the difference of two is exact, where products with `mul`
+        // differ by their own rounding, at 2^26 by more than fp16 has room for.  One that no key has moved yet is FLT_MAX below
+        // everything, and its limit such that any score but minus infinity is beyond it
+        F2 n_ref = f2(FLT_MAX, FLT_MAX);                       // (minus the reference)
+        float limit[2] = {-FLT_MAX, -FLT_MAX};
         F2 l_run = f2(0.f, 0.f);
         float acc[MT][4];                                      // O: dimensions (D / 8) g + 2 i (elements 0, 1) and + 1 (2, 3), heads 2 qd, 2 qd + 1
 #pragma unroll
@@ -577,16 +579,18 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 for (int e = 0; e < 2; ++e) top[e] = fmaxf(top[e], fmaxf(y[u][e], y[u][e + 2]));
             }
             if (__any_sync(0xffffffffu, top[0] > limit[0] || top[1] > limit[1])) {
-                float fac[2];
+                float fac[2], y_ref[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
+                    y_ref[e] = e ? -f2_get(n_ref).y : -f2_get(n_ref).x;
 #pragma unroll
                     for (int off = 4; off <= 16; off <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], off));
-                    const float m_new = fmaxf(m_ref[e], top[e] * mul[e]);
-                    fac[e] = kd_exp2(m_ref[e] - m_new);
-                    m_ref[e] = m_new;
-                    limit[e] = m_new == -FLT_MAX ? -FLT_MAX : (m_new + KD_SLACK) / mul[e];
+                    const float y_new = fmaxf(y_ref[e], top[e]);
+                    fac[e] = kd_exp2((y_ref[e] - y_new) * mul[e]);
+                    y_ref[e] = y_new;
+                    limit[e] = y_new == -FLT_MAX ? -FLT_MAX : __fadd_rd(y_new, KD_SLACK / mul[e]);
                 }
+                n_ref = f2(-y_ref[0], -y_ref[1]);
                 l_run = f2_mul(l_run, f2(fac[0], fac[1]));
 #pragma unroll
                 for (int i = 0; i < MT; ++i) { acc[i][0] *= fac[0]; acc[i][1] *= fac[1]; acc[i][2] *= fac[0]; acc[i][3] *= fac[1]; }
@@ -596,7 +600,7 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
                 float p[4];
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
-                    const float2 t = f2_get(f2_fma(f2(y[u][e], y[u][e + 1]), f2(mul[0], mul[1]), f2(KD_PSHIFT - m_ref[0], KD_PSHIFT - m_ref[1])));
+                    const float2 t = f2_get(f2_fma(f2_add(f2(y[u][e], y[u][e + 1]), n_ref), f2(mul[0], mul[1]), f2(KD_PSHIFT, KD_PSHIFT)));
                     p[e] = kd_exp2(t.x);
                     p[e + 1] = kd_exp2(t.y);
                     l_run = f2_add(l_run, f2(p[e], p[e + 1]));
@@ -647,7 +651,11 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
         auto xw = reinterpret_cast<float(*)[KD_GMAX][D + 2]>(smem);
         if (g == 0) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { xw[warp][2 * qd + e][0] = m_ref[e]; xw[warp][2 * qd + e][1] = e ? f2_get(l_run).y : f2_get(l_run).x; }
+            for (int e = 0; e < 2; ++e) {
+                const float y_ref = e ? -f2_get(n_ref).y : -f2_get(n_ref).x;
+                xw[warp][2 * qd + e][0] = y_ref == -FLT_MAX ? -FLT_MAX : fmaxf(y_ref * mul[e], -FLT_MAX);      // in log2 units from here on
+                xw[warp][2 * qd + e][1] = e ? f2_get(l_run).y : f2_get(l_run).x;
+            }
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {

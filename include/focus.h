@@ -388,6 +388,7 @@ FOCUS_API int focus_kv4_copy_pages(const focus_shape* shape, const focus_kv4* ca
  * probabilities with 11 significant bits), fp32 accumulation.  An empty sequence has o = 0 and lse = -inf.
  *   shape       n = the longest length that `lens` may hold, at most max_pages * page_tokens; Hq / Hkv <= 8, batch <= 1024, the pool
  *               smaller than 32 GiB (FOCUS_ERR_UNSUPPORTED otherwise)
+ *               scale and softcap finite
  *   q, o        device bf16 [batch, Hq, D] (stride_n ignored; q 4-byte aligned with even strides)
  *   mq_new      device uint32 [batch*Hq]           lse   device fp32 [batch*Hq], natural log
  *   ws          device scratch of focus_kv4_decode_workspace_bytes(shape) bytes (the same for every n), 16-byte aligned; contents need

@@ -475,7 +475,9 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
 #pragma unroll
         for (int i = 0; i < STAGES - 1; ++i) issue();
         uint32_t qb[MT][2];
-        // a score is y = S (or, with a cap, tanh(S * cap_in)) times `mul`, in log2 units; per head of this lane's two
+        // a score is y = S (or, with a cap, tanh(S * cap_in)) times `mul`, in log2 units; per head of this lane's two.  `mul` is kept a positive
+        // number, so that a key that is not attended (y = -inf) is -inf after it and a score of 0 is 0: the sums S are below 2^35, and what is lost at
+        // the lower end is below 2^-91
         float mul[2], cap_in[2];
         {
             float top = 0.f;
@@ -493,9 +495,9 @@ kv4_decode_kernel(const Kv4View c, const __nv_bfloat16* q, int64_t q_sb, int64_t
             // scores come out as (key, head) with heads 2 qd and 2 qd + 1 in this lane
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float x = __shfl_sync(0xffffffffu, down, (2 * qd + i) * 4) * c.k_scale * scale;
-                mul[i] = CAP ? softcap * KD_LOG2E : x * KD_LOG2E;
-                cap_in[i] = CAP ? x / softcap : 0.f;
+                const float x = fminf(__shfl_sync(0xffffffffu, down, (2 * qd + i) * 4) * scale * c.k_scale, FLT_MAX);
+                mul[i] = fminf(fmaxf((CAP ? softcap : x) * KD_LOG2E, FLT_MIN), FLT_MAX);
+                cap_in[i] = CAP ? fminf(x / softcap, FLT_MAX) : 0.f;
             }
         }
 
@@ -848,6 +850,7 @@ static int decode_d(const focus_shape* s, const Kv4View& c, const focus_tensor& 
 }
 
 int kv4_decode_check(const focus_shape* s, const Kv4View& c) {
+    if (s->scale > FLT_MAX || s->softcap > FLT_MAX) return fail(FOCUS_ERR_INVALID_ARG, "kv4 decode: scale and softcap must be finite");
     if (s->Hq / s->Hkv > KD_GMAX) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d query heads per KV head", KD_GMAX);
     if (s->batch > KD_MAX_BATCH) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: more than %d sequences in one call", KD_MAX_BATCH);
     if ((long long)s->batch * s->Hkv * cdiv(s->n, 64) >= (1ll << 28)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4 decode: batch * Hkv * n is too large");

@@ -10,7 +10,7 @@ import pytest
 import torch
 
 from paper_2604_03260_b200 import binding as fb
-from tests.test_gpu_kv4 import decode, gen, pool, status, stored, table_of
+from tests.test_gpu_kv4 import compare, decode, filled, gen, pool, status, stored, table_of
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,37 @@ def test_large_cap(cap):
     o, lse, ro, pv, rl = two_numbers(D, steps, 2.0 ** -4, 2.0 ** -6, 1.0, torch.ones(n - 1, dtype=torch.bool, device="cuda"), cap)
     tol = 2.0 ** -8 * ro.abs() + (2.0 ** -11 + 2.0 ** -18) * pv + n * 2.0 ** -35 * 8
     assert (o - ro).abs().sub(tol).max() <= 0 and (lse - rl).abs() <= 2.0 ** -17
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("cap", [0.0, 1.0, 2.0 ** -140])
+@pytest.mark.parametrize("lg", [-120, -60, -24, 0])
+def test_queries_of_zeros_and_scales_near_nothing(D, cap, lg):
+    """All scores are 0 (or too small to tell from it): o is the mean of the attended values, and the others have no weight."""
+    lens, Hq, Hkv = [700, 33, 1], 4, 2
+    cache, q, mq, mk, k, v = filled(lens, 32, Hq, Hkv, D, 8, 1, D)
+    pages, table, dl = cache.tensors
+    cache = fb.make_kv4(pages, 32, table, dl, 2.0 ** -16, 2.0)       # (the codes as they are, for keys 2^15 times smaller)
+    q[:, ::2] = 0
+    q *= 2.0 ** -40
+    shape = fb.make_shape(Hq, Hkv, 700, D, 8, 1, 5, 2.0 ** lg, cap, batch=3)
+    o, lse = decode(cache, shape, q, mq)
+    ks, vs = stored(cache, Hkv, D, 700)
+    compare(o, lse, lens, q, mq, mk, ks, vs, 5, cap, 2.0 ** lg)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_the_largest_queries_and_scales_over_keys_of_zeros(D, cap):
+    """scores are 0 however large what they are multiplied by: the factor stays a number"""
+    lens, Hq, Hkv, n = [300], 4, 2, 300
+    cache, q, mq, mk, k, v = filled(lens, 32, Hq, Hkv, D, 4, 1, D)
+    pages, table, dl = cache.tensors
+    cache = fb.make_kv4(pages, 32, table, dl, 2.0 ** 16, 1.0)
+    fb.focus_kv4_append(fb.make_shape(Hq, Hkv, n, D, 4, 1, 0), cache, torch.zeros_like(k), v, mk)
+    q.fill_(torch.finfo(torch.bfloat16).max)
+    shape = fb.make_shape(Hq, Hkv, n, D, 4, 1, 3, 2.0 ** 20, cap)
+    o, lse = decode(cache, shape, q, mq)
+    ks, vs = stored(cache, Hkv, D, n)
+    assert (ks == 0).all()
+    compare(o, lse, lens, torch.zeros_like(q), mq, mk, ks, vs, 3)

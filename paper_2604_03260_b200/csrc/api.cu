@@ -380,7 +380,6 @@ int focus_qk_norm_rope(const focus_shape* shape, const focus_rope* rope, focus_t
     if ((rc = validate_tensor("q", q, true, nb)) || (rc = validate_tensor("k", k, true, nb)) || (rc = validate_tensor("q_out", q_out, true, nb)) ||
         (rc = validate_tensor("k_out", k_out, true, nb)))
         return rc;
-    if ((rc = require_sm100())) return rc;
     return launch_qk_norm_rope(shape, rope, {q, k}, {wq, wk}, freq, positions, nullptr, {q_out, k_out}, nullptr, nullptr, nullptr,
                                (cudaStream_t)stream);
 }
@@ -406,7 +405,6 @@ int focus_qk_norm_rope_bwd(const focus_shape* shape, const focus_rope* rope, foc
     if (!ws || (uintptr_t)ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is NULL or not 16-byte aligned");
     if (ws_bytes < qk_norm_rope_bwd_workspace_bytes(shape))
         return fail(FOCUS_ERR_CAPACITY, "workspace has %zu bytes, %zu needed", ws_bytes, qk_norm_rope_bwd_workspace_bytes(shape));
-    if ((rc = require_sm100())) return rc;
     const focus_tensor grads[2] = {dq_out, dk_out};
     return launch_qk_norm_rope(shape, rope, {q, k}, {wq, wk}, freq, positions, grads, {dq, dk}, dwq, dwk, (float*)ws, (cudaStream_t)stream);
 }
@@ -461,7 +459,7 @@ int focus_kv4_append(const focus_shape* shape, const focus_kv4* cache, focus_ten
     if (rc || (rc = kv4_view(shape, cache, true, &c))) return rc;
     if ((rc = validate_tensor("k", k, true, shape->batch)) || (rc = validate_tensor("v", v, true, shape->batch))) return rc;
     if (!mk) return fail(FOCUS_ERR_INVALID_ARG, "mk is NULL");
-    if ((rc = require_sm100())) return rc;
+    if ((rc = kv4_rows_check(shape)) || (rc = require_sm100())) return rc;
     return launch_kv4_append(shape, c, k, v, mk, counts, dev_status, (cudaStream_t)stream);
 }
 
@@ -471,7 +469,7 @@ int focus_kv4_read(const focus_shape* shape, const focus_kv4* cache, const int32
     int rc = validate_shape(shape);
     if (rc || (rc = kv4_view(shape, cache, true, &c))) return rc;
     if ((rc = validate_tensor("k", k, true, shape->batch)) || (rc = validate_tensor("v", v, true, shape->batch))) return rc;
-    if ((rc = require_sm100())) return rc;
+    if ((rc = kv4_rows_check(shape)) || (rc = require_sm100())) return rc;
     return launch_kv4_read(shape, c, first, k, v, mk, dev_status, (cudaStream_t)stream);
 }
 
@@ -483,7 +481,7 @@ int focus_kv4_copy_pages(const focus_shape* shape, const focus_kv4* cache, const
     if (count < 0) return fail(FOCUS_ERR_INVALID_ARG, "count must be >= 0");
     if (count == 0) return FOCUS_OK;
     if (!src || !dst) return fail(FOCUS_ERR_INVALID_ARG, "src or dst is NULL");
-    if ((rc = require_sm100())) return rc;
+    if ((rc = kv4_copy_check(c, count)) || (rc = require_sm100())) return rc;
     return launch_kv4_copy(c, src, dst, count, dev_status, (cudaStream_t)stream);
 }
 

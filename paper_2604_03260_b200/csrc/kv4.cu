@@ -211,23 +211,30 @@ kv4_copy_kernel(unsigned char* pages, size_t page_bytes, int num_pages, const in
         if (at + i * KV4_THREADS < count) z[at + i * KV4_THREADS] = x[i];
 }
 
-static int rows_of(const focus_shape* s, Kv4Rows& rows) {
+int kv4_rows_check(const focus_shape* s) {
     const long long r = (long long)s->batch * s->Hkv * s->n;
-    if (r >= (1ll << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4: batch * Hkv * n (%lld) is too large for one call", r);
-    rows.rows = (uint32_t)r;
+    return r >= (1ll << 31) ? fail(FOCUS_ERR_UNSUPPORTED, "kv4: batch * Hkv * n (%lld) is too large for one call", r) : FOCUS_OK;
+}
+
+static long long copy_chunks(const Kv4View& c) { return ((long long)(c.page_bytes / 16) + KV4_COPY_CHUNK - 1) / KV4_COPY_CHUNK; }
+int kv4_copy_check(const Kv4View& c, int count) {
+    return copy_chunks(c) * count >= (1ll << 31) ? fail(FOCUS_ERR_UNSUPPORTED, "kv4: %d pages of %zu bytes are too much for one call", count, c.page_bytes) : FOCUS_OK;
+}
+
+static Kv4Rows rows_of(const focus_shape* s) {
+    Kv4Rows rows;
+    rows.rows = (uint32_t)((long long)s->batch * s->Hkv * s->n);
     rows.n = s->n;
     rows.Hkv = s->Hkv;
     rows.by_n = fixed_div((uint32_t)s->n);
     rows.by_heads = fixed_div((uint32_t)s->Hkv);
-    return FOCUS_OK;
+    return rows;
 }
 
 template <int D>
 static int append_d(const focus_shape* s, const Kv4View& c, const focus_tensor& k, const focus_tensor& v, const uint32_t* mk, const int32_t* counts,
                     int32_t* status, cudaStream_t st) {
-    Kv4Rows rows;
-    int rc = rows_of(s, rows);
-    if (rc) return rc;
+    const Kv4Rows rows = rows_of(s);
     const uint32_t per = Kv4Row<D>::ROWS;
     return check_cuda(launch_dependent(kv4_append_kernel<D>, dim3((rows.rows + per - 1) / per), dim3(KV4_THREADS), 0, st, c,
                                        reinterpret_cast<const __nv_bfloat16*>(k.ptr), k.stride_b, k.stride_h, k.stride_n,
@@ -238,9 +245,7 @@ static int append_d(const focus_shape* s, const Kv4View& c, const focus_tensor& 
 template <int D>
 static int read_d(const focus_shape* s, const Kv4View& c, const int32_t* first, const focus_tensor& k, const focus_tensor& v, uint32_t* mk,
                   int32_t* status, cudaStream_t st) {
-    Kv4Rows rows;
-    int rc = rows_of(s, rows);
-    if (rc) return rc;
+    const Kv4Rows rows = rows_of(s);
     const uint32_t per = Kv4Row<D>::ROWS;
     return check_cuda(launch_dependent(kv4_read_kernel<D>, dim3((rows.rows + per - 1) / per), dim3(KV4_THREADS), 0, st, c, first,
                                        reinterpret_cast<__nv_bfloat16*>(k.ptr), k.stride_b, k.stride_h, k.stride_n,
@@ -267,8 +272,7 @@ int launch_kv4_read(const focus_shape* s, const Kv4View& c, const int32_t* first
 }
 
 int launch_kv4_copy(const Kv4View& c, const int32_t* src, const int32_t* dst, int count, int32_t* status, cudaStream_t st) {
-    const long long chunks = ((long long)(c.page_bytes / 16) + KV4_COPY_CHUNK - 1) / KV4_COPY_CHUNK;
-    if (chunks * count >= (1ll << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "kv4: %d pages of %zu bytes are too much for one call", count, c.page_bytes);
+    const long long chunks = copy_chunks(c);
     return check_cuda(launch_dependent(kv4_copy_kernel, dim3((unsigned)(chunks * count)), dim3(KV4_THREADS), 0, st, c.pages, c.page_bytes, c.num_pages,
                                        src, dst, (uint32_t)chunks, status), "kv4 copy kernel launch");
 }

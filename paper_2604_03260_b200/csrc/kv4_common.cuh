@@ -67,14 +67,16 @@ __device__ __forceinline__ uint32_t kv4_scale_code(float s) {
 }
 #endif
 
-// the launchers of kv4.cu and kv4_decode.cu
+// what the kernels of kv4.cu and kv4_decode.cu take, beyond the checks of a shape and a cache; their launchers
+int kv4_rows_check(const focus_shape* s);
+int kv4_copy_check(const Kv4View& c, int count);
+int kv4_decode_check(const focus_shape* s, const Kv4View& c);
 int launch_kv4_append(const focus_shape* s, const Kv4View& c, const focus_tensor& k, const focus_tensor& v, const uint32_t* mk,
                       const int32_t* counts, int32_t* status, cudaStream_t st);
 int launch_kv4_read(const focus_shape* s, const Kv4View& c, const int32_t* first, const focus_tensor& k, const focus_tensor& v,
                     uint32_t* mk, int32_t* status, cudaStream_t st);
 int launch_kv4_copy(const Kv4View& c, const int32_t* src, const int32_t* dst, int count, int32_t* status, cudaStream_t st);
 size_t kv4_decode_workspace_bytes(const focus_shape* s);
-int kv4_decode_check(const focus_shape* s, const Kv4View& c);           // what the kernels take, beyond the checks of a shape and a cache
 int launch_kv4_decode(const focus_shape* s, const Kv4View& c, const focus_tensor& q, const uint32_t* mq_new, const focus_tensor& o,
                       float* lse, void* ws, float scale, int32_t* status, cudaStream_t st);
 

@@ -613,6 +613,8 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
     const long long tokens = (long long)s->batch * s->n;
     if (tokens >= (1ll << 30)) return fail(FOCUS_ERR_UNSUPPORTED, "norm and rotation: batch * n (%lld) is too large for one call", tokens);
     if (!bwd && !odd) {
+        int rc = require_sm100();                              // (when the sizes have been looked at: they are refused without a device too)
+        if (rc) return rc;
         const int all = s->Hq + s->Hkv;
         a.lgT[0] = rope_tile(ROPE_PASSES * C::RPP, all, s->batch, s->n);
         a.per_seq[0] = cdiv(s->n, 1 << a.lgT[0]);
@@ -625,7 +627,7 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
         a.parts = (uint32_t)parts;
         a.by_parts = fixed_div(a.parts);
         constexpr size_t smem = (size_t)ROPE_FWD_STAGES * 2 * ROPE_THREADS * 16;
-        const int rc = check_cuda(allow_smem<qk_norm_rope_kernel<D, INTER>>(smem), "cudaFuncSetAttribute(norm and rotation)");
+        rc = check_cuda(allow_smem<qk_norm_rope_kernel<D, INTER>>(smem), "cudaFuncSetAttribute(norm and rotation)");
         if (rc) return rc;
         return check_cuda(launch_dependent(qk_norm_rope_kernel<D, INTER>, dim3((unsigned)(tiles * parts)), dim3(ROPE_THREADS), smem, st, a),
                           "norm and rotation kernel launch");
@@ -662,7 +664,9 @@ static int launch_rope_d(const focus_shape* s, RopeArgs& a, bool bwd, float* dwq
         a.over[i] = a.whole[i] < ROPE_EVEN || tiles == 0 ? a.ctas[i] : tiles;
     }
     const dim3 g(a.ctas[0] + a.ctas[1]), t(ROPE_THREADS);
-    int rc = odd ? FOCUS_OK : check_cuda(allow_smem<qk_norm_rope_bwd_kernel<D, INTER>>(RopeBwd<D>::SMEM), "cudaFuncSetAttribute(norm and rotation backward)");
+    int rc = require_sm100();
+    if (rc) return rc;
+    rc = odd ? FOCUS_OK : check_cuda(allow_smem<qk_norm_rope_bwd_kernel<D, INTER>>(RopeBwd<D>::SMEM), "cudaFuncSetAttribute(norm and rotation backward)");
     if (rc) return rc;
     rc = odd ? check_cuda(bwd ? launch_dependent(qk_norm_rope_odd_kernel<D, true>, g, t, 0, st, a) : launch_dependent(qk_norm_rope_odd_kernel<D, false>, g, t, 0, st, a),
                               "norm and rotation kernel launch")

@@ -23,3 +23,69 @@ def decode_shape(**kw):
 @pytest.mark.parametrize("kw", [dict(scale=float("inf")), dict(softcap=float("inf")), dict(scale=float("nan")), dict(softcap=float("nan"))])
 def test_scales_and_caps_that_are_no_numbers(kw):
     assert decode(decode_shape(**kw)) == -1
+
+
+BIG = 1 << 31
+
+
+def append(shape, c=None, k=None, v=None, mk=4096, counts=None, status=None):
+    t = heads(shape.Hkv, shape.n)
+    return fb.lib().focus_kv4_append(R(shape), R(c or cache()), k or t, v or t, mk, counts, status, None)
+
+
+def read(shape, c=None, first=None, mk=None, status=None):
+    t = heads(shape.Hkv, shape.n)
+    return fb.lib().focus_kv4_read(R(shape), R(c or cache()), first, t, t, mk, status, None)
+
+
+def copy(count, c=None, src=4096, dst=4096, status=None):
+    return fb.lib().focus_kv4_copy_pages(R(decode_shape()), R(c or cache()), src, dst, count, status, None)
+
+
+def asked(rc):
+    """all that the host can check has been passed: it is the device that is missing here (or one of another kind)"""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("would be launched")
+    return rc in (-4, -5)
+
+
+@pytest.mark.parametrize("batch,Hkv,n", [(1 << 10, 1, 1 << 21), (2, 1, 1 << 30), (1 << 15, 4, 1 << 14), (3, 7, 102261127)])
+def test_rows_of_an_append_or_a_read(batch, Hkv, n):
+    """batch * Hkv * n is below 2^31"""
+    assert batch * Hkv * n >= BIG and batch * Hkv * (n - 1) < BIG
+    at = decode_shape(Hq=Hkv, Hkv=Hkv, n=n, batch=batch)
+    assert append(at) == -2 and read(at) == -2
+    below = decode_shape(Hq=Hkv, Hkv=Hkv, n=n - 1, batch=batch)
+    assert asked(append(below)) and asked(read(below))
+
+
+def test_pages_of_a_copy():
+    """16 KB of a page are a CTA's, of which there are fewer than 2^31"""
+    chunks = -(-(4 * 256 * (128 + 16 + 4) // 16) // 1024)
+    most = (BIG - 1) // chunks
+    c = cache(page_tokens=256)
+    assert copy(most + 1, c) == -2 and asked(copy(most, c))
+
+
+def rope(shape, back=False, rotary=128):
+    L, q, k = fb.lib(), heads(shape.Hq, shape.n), heads(shape.Hkv, shape.n)
+    r = fb.make_rope(rotary)
+    if not back:
+        return L.focus_qk_norm_rope(R(shape), R(r), q, k, 4096, 4096, 4096, None, q, k, None)
+    return L.focus_qk_norm_rope_bwd(R(shape), R(r), q, k, 4096, 4096, 4096, None, q, k, q, k, 8192, 12288, 4096, BIG, None)
+
+
+@pytest.mark.parametrize("rotary", [128, 70])
+def test_tokens_of_norm_and_rotation(rotary):
+    """batch * n is below 2^30, and the passes over all heads below 2^31 (backward)"""
+    for batch, n in ((1, 1 << 30), (1 << 10, 1 << 20), (3, 357913942)):
+        at, below = (decode_shape(Hq=1, Hkv=1, n=m, batch=batch) for m in (n, n - 1))
+        for back in (False, True):
+            assert rope(at, back, rotary) == -2 and asked(rope(below, back, rotary))
+    many = decode_shape(Hq=1 << 10, Hkv=1, n=(1 << 30) - 1, batch=1)
+    assert asked(rope(many, False, rotary))
+    assert rope(many, True, rotary) == -2 if rotary == 128 else asked(rope(many, True, rotary))
+    if rotary == 128:                        # 1024 heads of a token are 32 passes
+        many = [decode_shape(Hq=1 << 10, Hkv=1, n=m, batch=1) for m in (1 << 26, (1 << 26) - 1)]
+        assert rope(many[0], True) == -2 and asked(rope(many[1], True))

@@ -350,6 +350,7 @@ FOCUS_API int focus_qk_norm_rope_bwd(const focus_shape* shape, const focus_rope*
  * `lens` counts the tokens of a sequence with the new ones of a call among them, as focus_decode_step's n does: the caller sets it (and
  * the pages in `table`) before it appends.  Entries of `table` behind a sequence's last page are not used.  Sequences may share pages
  * that none of them writes to.
+ * Arrays of int32, uint32 and fp32 are 4-byte aligned.
  *   dev_status  device int32[4], nullable, zeroed by the caller: [0] stays 0 on success.  1: an entry of `table` that is no page ([1]
  *               sequence, [2] place in its row, [3] the entry); 2: a length that cannot be ([1] sequence, [2] its entry of lens, [3] the
  *               count, the first token or the bound it does not agree with); 3: a pair of pages that are not both in the pool ([1] pair,

@@ -443,6 +443,12 @@ static int kv4_view(const focus_shape* shape, const focus_kv4* c, bool paged, Kv
     return FOCUS_OK;
 }
 
+// arrays of 4-byte words of the calls around a 4-bit cache (NULL is for the caller to judge)
+static int kv4_words(const char* names, const void* a, const void* b, const void* c) {
+    if (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c) % 4) return fail(FOCUS_ERR_INVALID_ARG, "%s must be 4-byte aligned", names);
+    return FOCUS_OK;
+}
+
 size_t focus_kv4_page_bytes(const focus_shape* shape, int32_t page_tokens) {
     if (validate_shape(shape)) return 0;
     if (page_tokens < 16 || page_tokens > 256 || (page_tokens & (page_tokens - 1))) {
@@ -459,6 +465,7 @@ int focus_kv4_append(const focus_shape* shape, const focus_kv4* cache, focus_ten
     if (rc || (rc = kv4_view(shape, cache, true, &c))) return rc;
     if ((rc = validate_tensor("k", k, true, shape->batch)) || (rc = validate_tensor("v", v, true, shape->batch))) return rc;
     if (!mk) return fail(FOCUS_ERR_INVALID_ARG, "mk is NULL");
+    if ((rc = kv4_words("mk, counts and dev_status", mk, counts, dev_status))) return rc;
     if ((rc = kv4_rows_check(shape)) || (rc = require_sm100())) return rc;
     return launch_kv4_append(shape, c, k, v, mk, counts, dev_status, (cudaStream_t)stream);
 }
@@ -469,6 +476,7 @@ int focus_kv4_read(const focus_shape* shape, const focus_kv4* cache, const int32
     int rc = validate_shape(shape);
     if (rc || (rc = kv4_view(shape, cache, true, &c))) return rc;
     if ((rc = validate_tensor("k", k, true, shape->batch)) || (rc = validate_tensor("v", v, true, shape->batch))) return rc;
+    if ((rc = kv4_words("first, mk and dev_status", first, mk, dev_status))) return rc;
     if ((rc = kv4_rows_check(shape)) || (rc = require_sm100())) return rc;
     return launch_kv4_read(shape, c, first, k, v, mk, dev_status, (cudaStream_t)stream);
 }
@@ -481,6 +489,7 @@ int focus_kv4_copy_pages(const focus_shape* shape, const focus_kv4* cache, const
     if (count < 0) return fail(FOCUS_ERR_INVALID_ARG, "count must be >= 0");
     if (count == 0) return FOCUS_OK;
     if (!src || !dst) return fail(FOCUS_ERR_INVALID_ARG, "src or dst is NULL");
+    if ((rc = kv4_words("src, dst and dev_status", src, dst, dev_status))) return rc;
     if ((rc = kv4_copy_check(c, count)) || (rc = require_sm100())) return rc;
     return launch_kv4_copy(c, src, dst, count, dev_status, (cudaStream_t)stream);
 }
@@ -503,8 +512,8 @@ int focus_kv4_decode_step(const focus_shape* shape, const focus_kv4* cache, focu
         return fail(FOCUS_ERR_INVALID_ARG, "q must be 4-byte aligned with even, positive head strides (o: positive strides)");
     if (shape->batch > 1 && (q.stride_b < 1 || o.stride_b < 1))
         return fail(FOCUS_ERR_INVALID_ARG, "q.stride_b and o.stride_b must be positive when batch > 1");
-    if ((uintptr_t)ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is not 16-byte aligned");
-    if ((rc = kv4_decode_check(shape, c))) return rc;
+    if ((uintptr_t)ws % 16 || (uintptr_t)o.ptr % 2) return fail(FOCUS_ERR_INVALID_ARG, "ws is not 16-byte aligned, or o not 2-byte aligned");
+    if ((rc = kv4_words("mq_new, lse and dev_status", mq_new, lse, dev_status)) || (rc = kv4_decode_check(shape, c))) return rc;
     if (ws_bytes < kv4_decode_workspace_bytes(shape))
         return fail(FOCUS_ERR_CAPACITY, "decode workspace has %zu bytes, %zu needed", ws_bytes, kv4_decode_workspace_bytes(shape));
     if ((rc = require_sm100())) return rc;

@@ -89,3 +89,20 @@ def test_tokens_of_norm_and_rotation(rotary):
     if rotary == 128:                        # 1024 heads of a token are 32 passes
         many = [decode_shape(Hq=1 << 10, Hkv=1, n=m, batch=1) for m in (1 << 26, (1 << 26) - 1)]
         assert rope(many[0], True) == -2 and asked(rope(many[1], True))
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_misaligned_words(off):
+    """masks, counts, lists, log-sum-exps and the status are read and written four bytes at a time"""
+    s, p = decode_shape(), 4096 + off
+    one = decode_shape(n=100)
+    for kw in (dict(mk=p), dict(counts=p), dict(status=p)):
+        assert append(one, **kw) == -1, kw
+    for kw in (dict(first=p), dict(mk=p), dict(status=p)):
+        assert read(one, **kw) == -1, kw
+    for kw in (dict(src=p), dict(dst=p), dict(status=p)):
+        assert copy(3, **kw) == -1, kw
+    for kw in (dict(mq=p), dict(lse=p), dict(status=p), *([dict(o=p)] if off % 2 else [])):
+        assert decode(s, **kw) == -1, kw
+    if off == 2:
+        assert asked(decode(s, o=p))         # (o is written number by number)

@@ -302,6 +302,12 @@ def _dev(t, dtype, *shape):
     return t.data_ptr()
 
 
+def _scratch(ws):
+    """address and bytes of a workspace, checked: on the GPU, in one piece"""
+    assert ws.is_cuda and ws.is_contiguous(), (ws.dtype, tuple(ws.shape), ws.stride())
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _opt(t, dtype, *shape):
     return None if t is None else _dev(t, dtype, *shape)
 
@@ -362,7 +368,7 @@ def focus_qk_norm_rope_bwd(shape, rope, q, k, wq, wk, freq, positions, dq_out, d
                                           _opt(wq, torch.float32, D), _opt(wk, torch.float32, D), _opt(freq, torch.float64, rope.rotary // 2),
                                           _opt(positions, torch.int32, B, n), _heads(dq_out, shape, shape.Hq), _heads(dk_out, shape, shape.Hkv),
                                           _heads(dq, shape, shape.Hq), _heads(dk, shape, shape.Hkv), _opt(dwq, torch.float32, D),
-                                          _opt(dwk, torch.float32, D), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+                                          _opt(dwk, torch.float32, D), *_scratch(ws), _stream(stream))
     _check(rc)
 
 
@@ -434,8 +440,8 @@ def focus_kv4_decode_step(shape, cache, q, mq_new, o, lse, ws, dev_status=None, 
     rc = _short().kv4_decode_step(shape, cache, q, mq_new, o, lse, ws, dev_status, stream)
     if rc is None:
         rc = lib().focus_kv4_decode_step(C.byref(shape), C.byref(cache), _vecs(q, shape, shape.Hq), _dev(mq_new, torch.int32, shape.batch, shape.Hq),
-                                         _vecs(o, shape, shape.Hq), _dev(lse, torch.float32, shape.batch, shape.Hq), _p(ws),
-                                         ws.numel() * ws.element_size(), _opt(dev_status, torch.int32, 4), _stream(stream))
+                                         _vecs(o, shape, shape.Hq), _dev(lse, torch.float32, shape.batch, shape.Hq),
+                                         *_scratch(ws), _opt(dev_status, torch.int32, 4), _stream(stream))
     _check(rc)
 
 

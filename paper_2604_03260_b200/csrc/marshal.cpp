@@ -104,6 +104,12 @@ struct Args {
         if (!t || !t->is_cuda() || t->scalar_type() != type || t->numel() != count || !t->is_contiguous()) { known = false; return nullptr; }
         return t->data_ptr();
     }
+    // address of a workspace on the GPU, in one piece
+    void* scratch(int i) {
+        const at::Tensor* t = tensor(i);
+        if (!t || !t->is_cuda() || !t->is_contiguous()) { known = false; return nullptr; }
+        return t->data_ptr();
+    }
     size_t bytes(int i) {
         const at::Tensor* t = tensor(i);
         return t ? (size_t)t->numel() * t->element_size() : 0;
@@ -265,7 +271,7 @@ PyObject* qk_norm_rope_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
         auto pos = static_cast<const int32_t*>(a.counted(7, at::kInt, s ? (int64_t)s->batch * s->n : 0, true));
         auto gq = a.sized(8, s, Hq, false), gk = a.sized(9, s, Hkv, false), dq = a.sized(10, s, Hq, false), dk = a.sized(11, s, Hkv, false);
         auto dwq = static_cast<float*>(a.counted(12, at::kFloat, D, true)), dwk = static_cast<float*>(a.counted(13, at::kFloat, D, true));
-        auto ws = a.ptr(14);
+        auto ws = a.scratch(14);
         auto bytes = a.bytes(14);
         auto st = a.stream(15);
         return [=] { return p_qk_norm_rope_bwd(s, r, q, k, wq, wk, freq, pos, gq, gk, dq, dk, dwq, dwk, ws, bytes, st); };
@@ -324,7 +330,7 @@ PyObject* kv4_decode_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
         auto mq = static_cast<const uint32_t*>(a.counted(3, at::kInt, vectors, false));
         auto o = a.sized(4, s, Hq, true);
         auto lse = static_cast<float*>(a.counted(5, at::kFloat, vectors, false));
-        auto ws = a.ptr(6);
+        auto ws = a.scratch(6);
         auto bytes = a.bytes(6);
         auto status = static_cast<int32_t*>(a.counted(7, at::kInt, 4, true));
         auto st = a.stream(8);

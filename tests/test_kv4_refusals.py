@@ -1,7 +1,10 @@
 """4-bit cache, norm and rotation: refusals that no device is asked for, with their exact status.  CPU."""
 import ctypes
+import math
+import types
 
 import pytest
+import torch
 
 from paper_2604_03260_b200 import binding as fb
 from tests.test_kv4_host import cache, heads
@@ -44,7 +47,6 @@ def copy(count, c=None, src=4096, dst=4096, status=None):
 
 def asked(rc):
     """all that the host can check has been passed: it is the device that is missing here (or one of another kind)"""
-    import torch
     if torch.cuda.is_available():
         pytest.skip("would be launched")
     return rc in (-4, -5)
@@ -106,3 +108,43 @@ def test_misaligned_words(off):
         assert decode(s, **kw) == -1, kw
     if off == 2:
         assert asked(decode(s, o=p))         # (o is written number by number)
+
+
+class OnGpu:
+    """a tensor as far as the binding looks at one, for calls whose pointers nobody follows"""
+    def __init__(self, dtype, *shape, cuda=True, contiguous=True):
+        self.dtype, self.shape, self.is_cuda, self.flat = dtype, shape, cuda, contiguous
+
+    def stride(self):
+        return tuple(math.prod(self.shape[i + 1:]) for i in range(len(self.shape)))
+
+    def is_contiguous(self):
+        return self.flat
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def data_ptr(self):
+        return 4096
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="would be launched")
+@pytest.mark.parametrize("kw,error", [(dict(), fb.FocusError), (dict(cuda=False), AssertionError), (dict(contiguous=False), AssertionError)])
+def test_scratch_that_is_not_on_the_gpu_or_not_in_one_piece(monkeypatch, kw, error):
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    stream = types.SimpleNamespace(cuda_stream=0)
+    s = decode_shape()
+    ws = OnGpu(torch.uint8, 1 << 30, **kw)
+    c = cache()
+    c.tensors = OnGpu(torch.uint8, 8, fb.focus_kv4_page_bytes(s, 64)), OnGpu(i32, 2, 4), OnGpu(i32, 2)
+    vec = OnGpu(bf, 2, 8, 128)
+    with pytest.raises(error):
+        fb.focus_kv4_decode_step(s, c, vec, OnGpu(i32, 16), vec, OnGpu(f32, 16), ws, None, stream)
+    q, k, w = OnGpu(bf, 2, 8, 100, 128), OnGpu(bf, 2, 4, 100, 128), OnGpu(f32, 128)
+    other = OnGpu(f32, 128)
+    monkeypatch.setattr(other, "data_ptr", lambda: 8192, raising=False)
+    with pytest.raises(error):
+        fb.focus_qk_norm_rope_bwd(s, fb.make_rope(128), q, k, w, w, OnGpu(torch.float64, 64), None, q, k, q, k, w, other, ws, stream)

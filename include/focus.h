@@ -365,8 +365,8 @@ FOCUS_API int focus_qk_norm_rope_bwd(const focus_shape* shape, const focus_rope*
  *   k, v        device bf16 [batch, Hkv, n, D], 16-byte aligned, strides multiples of 8       mk   device uint32 [batch*Hkv, n]
  *   counts      device int32 [batch], 0 to n; NULL: n for every sequence
  *
- * focus_kv4_read -- the way back: tokens first[b] .. first[b] + n - 1 of every sequence as bf16 (exact), for a pass of focus_attn_fwd over
- * a cached prefix.  Rows behind the last token of a sequence are left as they were.
+ * focus_kv4_read -- the way back: tokens first[b] .. first[b] + n - 1 of every sequence as bf16 (exact).  With the queries of the same n
+ * tokens (it has one length for both) focus_attn_fwd can go over them.  Rows behind the last token of a sequence are left as they were.
  *   shape       n = tokens per sequence; batch, Hkv, D are read
  *   first       device int32 [batch]; NULL: 0     k, v  device bf16 [batch, Hkv, n, D], written     mk  device uint32 [batch*Hkv, n] or NULL
  *

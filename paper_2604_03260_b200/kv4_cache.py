@@ -7,7 +7,7 @@ bookkeeping.  The entry points that it calls are those of the C ABI (through ``b
     append    focus_kv4_append, after the pages for the new tokens are found (and the page that a sequence is about to write to is
               copied, focus_kv4_copy_pages, if another sequence shares it)
     decode    focus_kv4_decode_step, one new query per sequence
-    read      focus_kv4_read, tokens back in bf16 (a pass of focus_attn_fwd over a cached prefix)
+    read      focus_kv4_read, tokens back in bf16 (focus_attn_fwd goes over a prefix with the queries of all its tokens)
     fork      another sequence with the same tokens: pages are shared, none is copied yet
     free      a sequence is forgotten; pages that no other sequence shares are free again
     compact   pages in use move to the front of the pool (focus_kv4_copy_pages)

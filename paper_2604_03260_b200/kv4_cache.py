@@ -12,9 +12,15 @@ bookkeeping.  The entry points that it calls are those of the C ABI (through ``b
     free      a sequence is forgotten; pages that no other sequence shares are free again
     compact   pages in use move to the front of the pool (focus_kv4_copy_pages)
 
-A call whose pages do not fit raises ``FocusError`` (capacity), one whose tensors are refused what ``binding`` raises.  No call that raises,
-wherever on its way, changes what the sequences hold.  All calls enqueue on the current stream (or ``stream``), as the entry points do; use one stream, or order
-them.  Sequences without tokens take part in ``decode`` with o = 0.
+A call whose pages do not fit raises ``FocusError`` (capacity), one whose tensors are refused what ``binding`` raises.  No call that
+raises, wherever on its way, changes what the sequences hold.  All calls enqueue on the current stream (or ``stream``); use one
+stream, or order them.  Sequences without tokens take part in ``decode`` with o = 0.
+
+``decode`` and ``read`` only enqueue, as the entry points do.  ``append``, ``reserve``, ``fork``, ``free`` and ``compact`` cannot be
+captured into a graph: they write the whole page table and all lengths anew on the host and copy them from pageable memory, and the host
+waits until the stream has come to that copy.  Besides the wait a call takes 0.2 ms for one sequence of 130000 tokens in pages of 64,
+0.4 ms for 32 of 5000 and 1.5 ms for 128 of 5000.  A loop for which that is too long keeps a table and lengths of its own and calls
+``focus_kv4_append``.
 """
 from __future__ import annotations
 

@@ -18,9 +18,9 @@
 //     others the attended ones are listed, and as many off the list are a tile.
 // Rows come through a ring in shared memory, private to a warp, by asynchronous copies: one address per 16 bytes, none for the operands.
 // Every warp keeps its own maximum, sum and O; a CTA joins its warps, a second kernel the CTAs.
-// Measured (32 + 8 heads of 128): 131072 keys 42.5 us, of which 11 are the plan, the first masks and copies, the joins (24 at the copy rate of all
-// bytes; issue slots 61 %); 24 sequences of 1 to 16385 keys 49.9 us (25.7); 2049 keys 8.1 us.  65536 keys, 16 + 8 heads of 256, 44 % of them
-// attended, with a cap: 38.8 us (11.2).
+// Measured (32 + 8 heads of 128): 131072 keys 42.8 us, of which 11 are the plan, the first masks and copies, the joins (24 at the copy rate of all
+// bytes; issue slots 61 %); 24 sequences of 1 to 16385 keys 50.5 us (25.7); 2049 keys 8.1 us.  65536 keys, 16 + 8 heads of 256, 44 % of them
+// attended, with a cap: 38.8 us (11.2); there half of the issue slots are free and latency is what is left.
 #include "kv4_common.cuh"
 #include "f32x2.cuh"
 
@@ -128,7 +128,8 @@ __device__ __forceinline__ int kd_spot(int x) { return (x & ~(KEYS - 1)) + (x & 
 
 // How the work is cut.  Every KV head of a sequence has ceil(len / UNIT) units; the units of all heads form one list, dealt out in equal
 // contiguous ranges of `per` units.  A CTA whose range enters another head writes one more partial result and starts over, which takes as
-// long as TURN units: every head ends with that many empty ones, so that such a CTA gets the fewer keys (24 ragged sequences: 58 -> 52 us).
+// long as TURN units: every head ends with that many empty ones, so that such a CTA gets the fewer keys (24 ragged sequences of D = 128: 58 -> 52 us;
+// 64 and 256 take the same 320 keys).
 // Where whole ranges per head make no longer ranges, the heads are padded to them instead; where no sequence can be longer than a CTA's share (kd_alone),
 // they are padded to `span` units, its length, and a range is whole heads (one each, CTA by CTA and with nothing to work out, where there
 // are no more of them than CTAs: `direct`).  The lengths are on the device, and so every CTA works this out
@@ -804,7 +805,7 @@ size_t kv4_decode_workspace_bytes(const focus_shape* s) {
 }
 
 // Whether every head is one CTA's, so that nothing is merged (3 us and more), by the longest length alone.  Heads that have a CTA each: up to 8 units
-// of keys, where few heads leave the machine empty up to 4 (before -> now, us: 1 sequence of 300 keys, 8 KV heads 7.6 -> 6.8, of 600 stays 7.9, would
+// of keys, where few heads leave the machine empty up to 4 (before -> now at D = 128, us: 1 sequence of 300 keys, 8 KV heads 7.6 -> 6.8, of 600 stays 7.9, would
 // be 8.9; 8 sequences of 500 12.6 -> 8.4, of 900 13.3 -> 12.1; 64 of 1000 30.6 -> 25.3, of 1800 45.7 and would be 40.0, but 30.4 -> 31.9
 // when their lengths differ).  More heads than CTAs: up to KD_ALONE keys (150 sequences of 500: 45.8, would be 44.9, but 32.4 -> 37.5 when they differ).
 template <int D>

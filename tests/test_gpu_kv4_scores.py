@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 
 def two_numbers(D, steps, big, small, scale, attended, cap=0.0, seed=1):
     """One head, keys (3, steps[j] / 2, 0, ...) and a query (big, small, 0, ...): scores 3 big + steps[j] / 2 small.  The newest key, which is always
-    attended, lies far below.  (o, lse, reference o, sum of p |v|, exponents below the largest, values)"""
+    attended, lies far below.  (o, lse, o in 64 bits, the sum of p |v| there, lse in 64 bits)"""
     n = len(steps) + 1
     g = gen(seed)
     shape = fb.make_shape(1, 1, n, D, 4, 1, 0, scale, cap)

@@ -493,11 +493,80 @@ FOCUS_API int focus_gate_attn_fwd(const focus_shape* shape, focus_tensor q, focu
  *   ws           device scratch, focus_sinkhorn_bwd_workspace_bytes(shape, iters) bytes, 16-byte aligned
  *   dg           device fp32 [batch, n, ld]; entries g >= K are ignored
  *   dscores_out  device fp32 [batch, n, ld]; entries g >= K are written as 0; may be the dg buffer, not the scores
- * The derivatives of the gated attention itself (Eq. 2) have an oracle and pins only; no kernel computes them.
  */
 FOCUS_API size_t focus_sinkhorn_bwd_workspace_bytes(const focus_shape* shape, int32_t iters);
 FOCUS_API int focus_sinkhorn_bwd(const focus_shape* shape, const float* scores, float tau, int32_t iters, void* ws,
                                  size_t ws_bytes, const float* dg, float* dscores_out, void* stream);
+
+/*
+ * focus_attn_bwd -- the derivative of focus_attn_fwd: from do = d loss / d o those of q, k and v.  With p = exp(s - lse) over the attended
+ * pairs and delta_i = do_i.o_i: ds = p (do.v - delta) (times 1 - tanh^2 with a softcap), dv_j = sum_i p do_i, dk_j = scale sum_i ds q_i over
+ * the rows of all query heads of the KV head, dq_i = scale sum_j ds k_j.  The probabilities are worked out again; nothing of size n x n is
+ * kept.  bf16 operands, fp32 accumulation; p and ds are rounded to bf16 before their products, the results once.  The order of the sums
+ * depends on the shape and the masks alone (the same bits in every call).
+ *   q, k, v, mq, mk, tiles_ws, layout   as for the forward pass, with any layout (tiles are walked in token order); NULL tiles_ws = every
+ *               causal pair
+ *   o, lse      what the forward pass wrote (finite; a row whose lse is -inf has no pairs and no gradient)
+ *   d_o, dq     device bf16 [batch, Hq, n, D]      dk, dv   device bf16 [batch, Hkv, n, D], like q and k; written; they overlap none of the
+ *               other tensors
+ *   ws          device scratch of focus_attn_bwd_workspace_bytes(shape) bytes, 16-byte aligned; contents need not be preserved between
+ *               calls, calls that may overlap need one each
+ *   dev_status  device int32[4], nullable, as for focus_attn_fwd
+ *
+ * focus_gate_attn_bwd -- the derivative of focus_gate_attn_fwd: those of q, k, v and of the soft assignments,
+ *     da_ij = ds_ij scale q_i.k_j lambda f (1 - f), f = sigmoid(lambda g_i.g_j), over the distant pairs of all heads;
+ *     dg_i += da_ij g_j,  dg_j += da_ij g_i
+ * with the sums of dg in fp32 throughout and f from exp (no tanh approximation).
+ *   g, lambda   as for the forward pass
+ *   dg          device fp32 [batch, n, ld], overwritten; entries g >= K are written as 0; 16-byte aligned
+ */
+FOCUS_API size_t focus_attn_bwd_workspace_bytes(const focus_shape* shape);
+FOCUS_API int focus_attn_bwd(const focus_shape* shape, focus_tensor q, focus_tensor k, focus_tensor v, const uint32_t* mq,
+                             const uint32_t* mk, const void* tiles_ws, int32_t layout, focus_tensor o, const float* lse,
+                             focus_tensor d_o, focus_tensor dq, focus_tensor dk, focus_tensor dv, void* ws, size_t ws_bytes,
+                             int32_t* dev_status, void* stream);
+FOCUS_API size_t focus_gate_attn_bwd_workspace_bytes(const focus_shape* shape);
+FOCUS_API int focus_gate_attn_bwd(const focus_shape* shape, focus_tensor q, focus_tensor k, focus_tensor v, const float* g,
+                                  float lambda, focus_tensor o, const float* lse, focus_tensor d_o, focus_tensor dq,
+                                  focus_tensor dk, focus_tensor dv, float* dg, void* ws, size_t ws_bytes, int32_t* dev_status,
+                                  void* stream);
+
+/*
+ * focus_router_scores_bwd -- the derivative of focus_router_scores: from dscores = d loss / d scores those of the hidden states, the
+ * projection and the centroids.  With T = dscores' h (summed over the tokens of all sequences): dC = T Wg, dWg = T' C, dh = dscores (C Wg').
+ *   shape, h, strides, d_model, d_g, Wg, C   as for focus_router_scores
+ *   dscores     device fp32 [batch, n, ld], ld = focus_soft_ld(K), 16-byte aligned; entries g >= K are ignored
+ *   dh          device bf16 [batch, n, d_model], strides as those of h; written; NULL: not wanted.  May be h itself, overlaps it not otherwise
+ *   dWg, dC     device fp32 [d_model, d_g], [K, d_g]; overwritten.  Sums in fp32 (over blocks of tokens in fp64), in an order that depends on
+ *               the shape alone
+ *   ws          device scratch of focus_router_scores_bwd_workspace_bytes(shape, d_model, d_g) bytes, 16-byte aligned
+ */
+FOCUS_API size_t focus_router_scores_bwd_workspace_bytes(const focus_shape* shape, int32_t d_model, int32_t d_g);
+FOCUS_API int focus_router_scores_bwd(const focus_shape* shape, const void* h, int64_t stride_b, int64_t stride_n, int32_t d_model,
+                                      int32_t d_g, const float* Wg, const float* C, const float* dscores, void* dh, int64_t dh_stride_b,
+                                      int64_t dh_stride_n, float* dWg, float* dC, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * focus_grad_clip -- norm = sqrt(sum of the squares of all numbers of all tensors); every tensor times max_norm / norm where the norm is
+ * above max_norm, as it is otherwise.  A norm that is not finite is reported and the tensors are left as they are.
+ *   grads       host array of `count` tensors (read during the call): src, dst device, `count` numbers each, contiguous, of type
+ *               FOCUS_GRAD_F32 or FOCUS_GRAD_BF16, aligned to a number; dst may be src and overlaps no tensor otherwise
+ *   max_norm    >= 0; infinity: nothing is scaled
+ *   norm_out    device fp32, or NULL
+ *   ws          device scratch of focus_grad_clip_workspace_bytes() bytes, 16-byte aligned
+ * Squares of numbers whose fp32 square overflows or is tiny are taken in fp64; sums in an order that depends on the sizes alone.
+ */
+#define FOCUS_GRAD_F32 0
+#define FOCUS_GRAD_BF16 1
+typedef struct {
+    const void* src;
+    void* dst;
+    int64_t count;
+    int32_t dtype;
+} focus_grad;
+FOCUS_API size_t focus_grad_clip_workspace_bytes(void);
+FOCUS_API int focus_grad_clip(const focus_grad* grads, int32_t count, float max_norm, float* norm_out, void* ws, size_t ws_bytes,
+                              void* stream);
 
 /*
  * focus_selftest_umma -- diagnostic, not on the hot path (the paper has no counterpart): one

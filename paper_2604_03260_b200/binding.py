@@ -62,6 +62,10 @@ class focus_kv4(C.Structure):
                 ("max_pages", C.c_int32), ("k_scale", C.c_float), ("v_scale", C.c_float)]
 
 
+class focus_grad(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32)]
+
+
 class FocusError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"focus status {status}: {message}")
@@ -138,6 +142,22 @@ def lib():
         L.focus_kv4_decode_workspace_bytes.argtypes = [SP]
         L.focus_kv4_decode_step.restype = C.c_int
         L.focus_kv4_decode_step.argtypes = [SP, KP, ft, vp, ft, vp, vp, sz, vp, vp]
+        L.focus_attn_bwd_workspace_bytes.restype = sz
+        L.focus_attn_bwd_workspace_bytes.argtypes = [SP]
+        L.focus_attn_bwd.restype = C.c_int
+        L.focus_attn_bwd.argtypes = [SP, ft, ft, ft, vp, vp, vp, i32, ft, vp, ft, ft, ft, ft, vp, sz, vp, vp]
+        L.focus_gate_attn_bwd_workspace_bytes.restype = sz
+        L.focus_gate_attn_bwd_workspace_bytes.argtypes = [SP]
+        L.focus_gate_attn_bwd.restype = C.c_int
+        L.focus_gate_attn_bwd.argtypes = [SP, ft, ft, ft, vp, f32, ft, vp, ft, ft, ft, ft, vp, vp, sz, vp, vp]
+        L.focus_router_scores_bwd_workspace_bytes.restype = sz
+        L.focus_router_scores_bwd_workspace_bytes.argtypes = [SP, i32, i32]
+        L.focus_router_scores_bwd.restype = C.c_int
+        L.focus_router_scores_bwd.argtypes = [SP, vp, C.c_int64, C.c_int64, i32, i32, vp, vp, vp, vp, C.c_int64, C.c_int64, vp, vp, vp, sz, vp]
+        L.focus_grad_clip_workspace_bytes.restype = sz
+        L.focus_grad_clip_workspace_bytes.argtypes = []
+        L.focus_grad_clip.restype = C.c_int
+        L.focus_grad_clip.argtypes = [C.POINTER(focus_grad), i32, f32, vp, vp, sz, vp]
         L.focus_count_kept.restype = C.c_int
         L.focus_count_kept.argtypes = [SP, vp, vp, vp, vp]
         L.focus_count_kept_noalloc.restype = C.c_int
@@ -481,6 +501,79 @@ def focus_gate_attn_fwd(shape, q, k, v, g, lam, o, lse, dev_status=None, stream=
     """training-time gated forward; g fp32 [batch, n, focus_soft_ld(K)]"""
     _check(lib().focus_gate_attn_fwd(C.byref(shape), tensor_arg(q), tensor_arg(k), tensor_arg(v), _p(g), lam, tensor_arg(o),
                                      _p(lse), _p(dev_status), _stream(stream)))
+
+
+def focus_attn_bwd_workspace_bytes(shape) -> int:
+    return int(lib().focus_attn_bwd_workspace_bytes(C.byref(shape)))
+
+
+def focus_attn_bwd(shape, q, k, v, mq, mk, tiles_ws, layout, o, lse, d_o, dq, dk, dv, ws, dev_status=None, stream=None):
+    """dq (like q), dk, dv (like k) bf16 from d_o (like o) and what the forward pass left: o, lse fp32 [batch, Hq, n]; ws uint8 scratch"""
+    B, Hq, Hkv, n = shape.batch, shape.Hq, shape.Hkv, shape.n
+    _check(lib().focus_attn_bwd(C.byref(shape), _heads(q, shape, Hq), _heads(k, shape, Hkv), _heads(v, shape, Hkv), _opt(mq, torch.int32, B, Hq, n),
+                                _opt(mk, torch.int32, B, Hkv, n), _p(tiles_ws), layout, _heads(o, shape, Hq), _dev(lse, torch.float32, B, Hq, n),
+                                _heads(d_o, shape, Hq), _heads(dq, shape, Hq), _heads(dk, shape, Hkv), _heads(dv, shape, Hkv), *_scratch(ws),
+                                _opt(dev_status, torch.int32, 4), _stream(stream)))
+
+
+def focus_gate_attn_bwd_workspace_bytes(shape) -> int:
+    return int(lib().focus_gate_attn_bwd_workspace_bytes(C.byref(shape)))
+
+
+def focus_gate_attn_bwd(shape, q, k, v, g, lam, o, lse, d_o, dq, dk, dv, dg, ws, dev_status=None, stream=None):
+    """the same for the training-time gate; g, dg fp32 [batch, n, focus_soft_ld(K)]"""
+    B, Hq, Hkv, n, ld = shape.batch, shape.Hq, shape.Hkv, shape.n, focus_soft_ld(shape.K)
+    _check(lib().focus_gate_attn_bwd(C.byref(shape), _heads(q, shape, Hq), _heads(k, shape, Hkv), _heads(v, shape, Hkv), _dev(g, torch.float32, B, n, ld), lam,
+                                     _heads(o, shape, Hq), _dev(lse, torch.float32, B, Hq, n), _heads(d_o, shape, Hq), _heads(dq, shape, Hq),
+                                     _heads(dk, shape, Hkv), _heads(dv, shape, Hkv), _dev(dg, torch.float32, B, n, ld), *_scratch(ws),
+                                     _opt(dev_status, torch.int32, 4), _stream(stream)))
+
+
+def _hidden(t, shape):
+    """address and strides of hidden states bf16 [batch, n, d_model] (or [n, d_model] for one sequence)"""
+    assert t.is_cuda and t.dtype is torch.bfloat16 and t.stride(-1) == 1, (t.dtype, t.stride())
+    d = t.shape[-1]
+    assert tuple(t.shape) == (shape.batch, shape.n, d) or (shape.batch == 1 and tuple(t.shape) == (shape.n, d)), (tuple(t.shape), (shape.batch, shape.n, d))
+    return t.data_ptr(), t.stride(0) if shape.batch > 1 else 0, t.stride(-2) if shape.n > 1 else d
+
+
+def focus_router_scores_bwd_workspace_bytes(shape, d_model, d_g) -> int:
+    return int(lib().focus_router_scores_bwd_workspace_bytes(C.byref(shape), d_model, d_g))
+
+
+def focus_router_scores_bwd(shape, h, Wg, Cg, dscores, dh, dWg, dC, ws, stream=None):
+    """dh (like h; None: not wanted), dWg fp32 [d_model, d_g], dC fp32 [K, d_g] from dscores fp32 [batch, n, focus_soft_ld(K)]; ws uint8 scratch"""
+    d, dg, K = h.shape[-1], Wg.shape[-1], shape.K
+    assert dh is None or dh.shape == h.shape, (tuple(dh.shape), tuple(h.shape))
+    ph, pd = _hidden(h, shape), _hidden(dh, shape) if dh is not None else (None, 0, d)
+    _check(lib().focus_router_scores_bwd(C.byref(shape), *ph, d, dg, _dev(Wg, torch.float32, d, dg), _dev(Cg, torch.float32, K, dg),
+                                         _dev(dscores, torch.float32, shape.batch, shape.n, focus_soft_ld(K)), *pd, _dev(dWg, torch.float32, d, dg),
+                                         _dev(dC, torch.float32, K, dg), *_scratch(ws), _stream(stream)))
+
+
+def focus_grad_clip_workspace_bytes() -> int:
+    return int(lib().focus_grad_clip_workspace_bytes())
+
+
+def make_grad_list(grads, out=None):
+    """the argument of focus_grad_clip: fp32 and bf16 tensors, each contiguous, and where their scaled forms go (None: in place).  The list
+    holds the tensors."""
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    assert len(out) == len(grads)
+    kinds = {torch.float32: 0, torch.bfloat16: 1}
+    c = (focus_grad * max(1, len(grads)))()
+    for e, s, d in zip(c, grads, out):
+        assert s.is_cuda and s.dtype in kinds and s.is_contiguous(), (s.dtype, tuple(s.shape), s.stride())
+        assert d.dtype is s.dtype and d.device == s.device and d.is_contiguous() and d.numel() == s.numel(), (d.dtype, tuple(d.shape), d.stride())
+        e.src, e.dst, e.count, e.dtype = s.data_ptr(), d.data_ptr(), s.numel(), kinds[s.dtype]
+    c.tensors = (grads, out)
+    return c
+
+
+def focus_grad_clip(grads, max_norm, norm_out, ws, stream=None):
+    """grads from make_grad_list; norm_out fp32 [1] or None; ws uint8 scratch"""
+    _check(lib().focus_grad_clip(grads, len(grads.tensors[0]), max_norm, _opt(norm_out, torch.float32, 1), *_scratch(ws), _stream(stream)))
 
 
 def focus_count_kept(shape, mq, tiles_ws, counts_out, stream=None):

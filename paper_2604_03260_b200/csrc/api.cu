@@ -1,5 +1,6 @@
 // C-ABI entry points: argument validation, workspace layout, dispatch.  No kernels here.
 #include "common.cuh"
+#include "attn_bwd.cuh"
 #include "kv4_common.cuh"
 
 #include <math.h>
@@ -614,6 +615,126 @@ int focus_gate_attn_fwd(const focus_shape* shape, focus_tensor q, focus_tensor k
     a.gate_ld = focus_soft_ld(shape->K);
     a.gate_lambda = lambda;
     return launch_attn_sm100(a, (cudaStream_t)stream);
+}
+
+size_t focus_attn_bwd_workspace_bytes(const focus_shape* shape) { return validate_shape(shape) ? 0 : attn_bwd_workspace_bytes(shape, false); }
+
+size_t focus_gate_attn_bwd_workspace_bytes(const focus_shape* shape) { return validate_shape(shape) ? 0 : attn_bwd_workspace_bytes(shape, true); }
+
+// what the two backward passes check alike
+static int attn_bwd_args(AttnBwdArgs& a, size_t ws_bytes) {
+    const focus_shape* shape = &a.s;
+    const int nb = shape->batch;
+    int rc;
+    if ((rc = validate_tensor("q", a.q, true, nb)) || (rc = validate_tensor("k", a.k, true, nb)) || (rc = validate_tensor("v", a.v, true, nb)) ||
+        (rc = validate_tensor("o", a.o, true, nb)) || (rc = validate_tensor("d_o", a.dO, true, nb)) || (rc = validate_tensor("dq", a.dq, true, nb)) ||
+        (rc = validate_tensor("dk", a.dk, true, nb)) || (rc = validate_tensor("dv", a.dv, true, nb)))
+        return rc;
+    if (!a.lse || (uintptr_t)a.lse % 4) return fail(FOCUS_ERR_INVALID_ARG, "lse is NULL or misaligned");
+    const void* in[5] = {a.q.ptr, a.k.ptr, a.v.ptr, a.o.ptr, a.dO.ptr};
+    const void* out[3] = {a.dq.ptr, a.dk.ptr, a.dv.ptr};
+    for (int i = 0; i < 3; ++i) {
+        for (const void* x : in)
+            if (out[i] == x) return fail(FOCUS_ERR_INVALID_ARG, "dq, dk and dv must not be one of the inputs");
+        if (out[i] == out[(i + 1) % 3]) return fail(FOCUS_ERR_INVALID_ARG, "dq, dk and dv must be three buffers");
+    }
+    if (!isfinite(shape->scale) || !isfinite(shape->softcap)) return fail(FOCUS_ERR_INVALID_ARG, "scale and softcap must be finite");
+    if ((long long)shape->batch * shape->Hq > 65535) return fail(FOCUS_ERR_UNSUPPORTED, "batch*Hq (%lld) must not exceed 65535", (long long)shape->batch * shape->Hq);
+    const size_t need = attn_bwd_workspace_bytes(shape, a.g != nullptr);
+    if (!a.ws || (uintptr_t)a.ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is NULL or not 16-byte aligned");
+    if (ws_bytes < need) return fail(FOCUS_ERR_CAPACITY, "attention backward workspace has %zu bytes, %zu needed", ws_bytes, need);
+    if ((uintptr_t)a.dev_status % 4) return fail(FOCUS_ERR_INVALID_ARG, "dev_status must be 4-byte aligned");
+    a.scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)shape->D);
+    return FOCUS_OK;
+}
+
+int focus_attn_bwd(const focus_shape* shape, focus_tensor q, focus_tensor k, focus_tensor v, const uint32_t* mq, const uint32_t* mk,
+                   const void* tiles_ws, int32_t layout, focus_tensor o, const float* lse, focus_tensor d_o, focus_tensor dq, focus_tensor dk,
+                   focus_tensor dv, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) {
+    int rc = validate_shape(shape);
+    if (rc) return rc;
+    if (tiles_ws && (!mq || !mk)) return fail(FOCUS_ERR_INVALID_ARG, "mq/mk are required with a tiles workspace");
+    if (((uintptr_t)mq | (uintptr_t)mk) % 4 || (uintptr_t)tiles_ws % 256) return fail(FOCUS_ERR_INVALID_ARG, "mq, mk or tiles_ws is misaligned");
+    AttnBwdArgs a = {*shape, q, k, v, o, d_o, dq, dk, dv, mq, mk, (const char*)tiles_ws, {}, lse, 0.f, nullptr, 0.f, nullptr, (char*)ws, dev_status};
+    if ((rc = attn_bwd_args(a, ws_bytes))) return rc;
+    if (tiles_ws && (rc = layout_of(shape, layout, &a.L))) return rc;
+    if ((rc = require_sm100())) return rc;
+    return launch_attn_bwd(a, (cudaStream_t)stream);
+}
+
+int focus_gate_attn_bwd(const focus_shape* shape, focus_tensor q, focus_tensor k, focus_tensor v, const float* g, float lambda, focus_tensor o,
+                        const float* lse, focus_tensor d_o, focus_tensor dq, focus_tensor dk, focus_tensor dv, float* dg, void* ws, size_t ws_bytes,
+                        int32_t* dev_status, void* stream) {
+    int rc = validate_shape(shape);
+    if (rc) return rc;
+    if (!g || !dg || ((uintptr_t)g | (uintptr_t)dg) % 16) return fail(FOCUS_ERR_INVALID_ARG, "g or dg is NULL or not 16-byte aligned");
+    if (g == dg) return fail(FOCUS_ERR_INVALID_ARG, "dg must not be g");
+    if (!isfinite(lambda)) return fail(FOCUS_ERR_INVALID_ARG, "lambda must be finite");
+    if (shape->softcap > 0.f) return fail(FOCUS_ERR_UNSUPPORTED, "the gated attention takes no softcap");
+    if (shape->D == 256 && shape->K > 16)
+        return fail(FOCUS_ERR_UNSUPPORTED, "the gated attention supports K <= 32 (K <= 16 at D = 256); K = %d", shape->K);
+    AttnBwdArgs a = {*shape, q, k, v, o, d_o, dq, dk, dv, nullptr, nullptr, nullptr, {}, lse, 0.f, g, lambda, dg, (char*)ws, dev_status};
+    if ((rc = attn_bwd_args(a, ws_bytes))) return rc;
+    if ((rc = require_sm100())) return rc;
+    return launch_attn_bwd(a, (cudaStream_t)stream);
+}
+
+// sizes that the router's backward pass takes
+static int router_bwd_sizes(const focus_shape* shape, int32_t d_model, int32_t d_g) {
+    int rc = validate_shape(shape);
+    if (rc) return rc;
+    if (d_model < 8 || d_model % 8 || d_g < 1) return fail(FOCUS_ERR_INVALID_ARG, "d_model must be a positive multiple of 8 and d_g >= 1");
+    if (d_model > 1 << 20 || d_g > 1 << 16) return fail(FOCUS_ERR_UNSUPPORTED, "d_model (%d) above 2^20 or d_g (%d) above 2^16", d_model, d_g);
+    if ((long long)shape->batch * shape->n > (1ll << 31)) return fail(FOCUS_ERR_UNSUPPORTED, "more than 2^31 tokens");
+    return FOCUS_OK;
+}
+
+size_t focus_router_scores_bwd_workspace_bytes(const focus_shape* shape, int32_t d_model, int32_t d_g) {
+    return router_bwd_sizes(shape, d_model, d_g) ? 0 : router_bwd_workspace_bytes(shape, d_model);
+}
+
+int focus_router_scores_bwd(const focus_shape* shape, const void* h, int64_t stride_b, int64_t stride_n, int32_t d_model, int32_t d_g, const float* Wg,
+                            const float* C, const float* dscores, void* dh, int64_t dh_stride_b, int64_t dh_stride_n, float* dWg, float* dC, void* ws,
+                            size_t ws_bytes, void* stream) {
+    int rc = router_bwd_sizes(shape, d_model, d_g);
+    if (rc) return rc;
+    if (!h || !Wg || !C || !dscores || !dWg || !dC) return fail(FOCUS_ERR_INVALID_ARG, "h, Wg, C, dscores, dWg or dC is NULL");
+    if (((uintptr_t)h | (uintptr_t)dh | (uintptr_t)dscores) % 16 || ((uintptr_t)Wg | (uintptr_t)C | (uintptr_t)dWg | (uintptr_t)dC) % 4)
+        return fail(FOCUS_ERR_INVALID_ARG, "h, dh and dscores must be 16-byte aligned, weights 4-byte aligned");
+    if (stride_n % 8 || stride_b % 8 || stride_n < d_model || (shape->batch > 1 && stride_b < 1))
+        return fail(FOCUS_ERR_INVALID_ARG, "strides of h must be multiples of 8 elements, stride_n >= d_model");
+    if (dh && (dh_stride_n % 8 || dh_stride_b % 8 || dh_stride_n < d_model || (shape->batch > 1 && dh_stride_b < 1)))
+        return fail(FOCUS_ERR_INVALID_ARG, "strides of dh must be multiples of 8 elements, stride_n >= d_model");
+    if (dh == h && (dh_stride_n != stride_n || (shape->batch > 1 && dh_stride_b != stride_b)))
+        return fail(FOCUS_ERR_INVALID_ARG, "dh in the place of h has its strides");
+    if (dWg == Wg || dC == C || dWg == dC) return fail(FOCUS_ERR_INVALID_ARG, "dWg and dC are buffers of their own");
+    const size_t need = router_bwd_workspace_bytes(shape, d_model);
+    if (!ws || (uintptr_t)ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is NULL or not 16-byte aligned");
+    if (ws_bytes < need) return fail(FOCUS_ERR_CAPACITY, "router backward workspace has %zu bytes, %zu needed", ws_bytes, need);
+    if ((rc = require_sm100())) return rc;
+    const RouterBwdArgs a = {(const __nv_bfloat16*)h, stride_b, stride_n, d_model, d_g, Wg, C, dscores, (__nv_bfloat16*)dh, dh_stride_b, dh_stride_n, dWg, dC, (char*)ws};
+    return launch_router_bwd(shape, a, (cudaStream_t)stream);
+}
+
+size_t focus_grad_clip_workspace_bytes(void) { return grad_clip_workspace_bytes(); }
+
+int focus_grad_clip(const focus_grad* grads, int32_t count, float max_norm, float* norm_out, void* ws, size_t ws_bytes, void* stream) {
+    int rc;
+    if (count < 0 || (count > 0 && !grads)) return fail(FOCUS_ERR_INVALID_ARG, "grads is NULL or count (%d) negative", count);
+    if (!(max_norm >= 0.f)) return fail(FOCUS_ERR_INVALID_ARG, "max_norm must be >= 0");
+    if ((uintptr_t)norm_out % 4) return fail(FOCUS_ERR_INVALID_ARG, "norm_out must be 4-byte aligned");
+    for (int i = 0; i < count; ++i) {
+        const focus_grad& g = grads[i];
+        if (g.dtype != FOCUS_GRAD_F32 && g.dtype != FOCUS_GRAD_BF16) return fail(FOCUS_ERR_INVALID_ARG, "grads[%d]: unknown dtype (%d)", i, g.dtype);
+        const uintptr_t size = g.dtype == FOCUS_GRAD_F32 ? 4 : 2;
+        if (g.count < 0 || (g.count > 0 && (!g.src || !g.dst))) return fail(FOCUS_ERR_INVALID_ARG, "grads[%d]: a null pointer or a negative count", i);
+        if (g.count > 1ll << 40) return fail(FOCUS_ERR_UNSUPPORTED, "grads[%d]: more than 2^40 numbers", i);
+        if (((uintptr_t)g.src | (uintptr_t)g.dst) % size) return fail(FOCUS_ERR_INVALID_ARG, "grads[%d] is not aligned to its numbers", i);
+    }
+    if (!ws || (uintptr_t)ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is NULL or not 16-byte aligned");
+    if (ws_bytes < grad_clip_workspace_bytes()) return fail(FOCUS_ERR_CAPACITY, "workspace has %zu bytes, %zu needed", ws_bytes, grad_clip_workspace_bytes());
+    if ((rc = require_sm100())) return rc;
+    return launch_grad_clip(grads, count, (double)max_norm, norm_out, (double*)ws, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -139,6 +139,20 @@ int launch_sinkhorn_stalled(const focus_shape* s, const float* S, float tau, int
 size_t sinkhorn_bwd_workspace_bytes(const focus_shape* s, int iters);
 int launch_sinkhorn_bwd(const focus_shape* s, const float* S, float tau, int iters, void* ws, const float* dG, float* dS,
                         cudaStream_t st);
+struct RouterBwdArgs {
+    const __nv_bfloat16* h;
+    int64_t h_sb, h_sn;
+    int d_model, d_g;
+    const float *Wg, *C, *ds;
+    __nv_bfloat16* dh;        // nullptr: not wanted
+    int64_t dh_sb, dh_sn;
+    float *dWg, *dC;
+    char* ws;
+};
+size_t router_bwd_workspace_bytes(const focus_shape* s, int d_model);
+int launch_router_bwd(const focus_shape* s, const RouterBwdArgs& a, cudaStream_t st);
+size_t grad_clip_workspace_bytes();
+int launch_grad_clip(const focus_grad* grads, int count, double bound, float* norm_out, double* sums, cudaStream_t st);
 size_t decode_workspace_bytes(const focus_shape* s);
 int launch_decode(const focus_shape* s, const focus_tensor& q, const focus_tensor& k, const focus_tensor& v,
                   const uint32_t* mq_new, const uint32_t* mk, const focus_tensor& o, float* lse, float* part, float scale,

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfocus_b200.so")
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))     # (other interpreters do not look for that name)
-SOURCES = ["api.cu", "assign.cu", "assign_hidden.cu", "sinkhorn.cu", "decode.cu", "rope.cu", "kv4.cu", "kv4_decode.cu", "tiles.cu", "tiles_sorted.cu", "attn_sm100.cu", "attn_bwd.cu", "router_bwd.cu", "grad_clip.cu", "selftest.cu",
+SOURCES = ["api.cu", "assign.cu", "assign_hidden.cu", "sinkhorn.cu", "decode.cu", "rope.cu", "kv4.cu", "kv4_decode.cu", "tiles.cu", "tiles_sorted.cu", "attn_sm100.cu", "attn_bwd.cu", "attn_bwd_d64.cu", "attn_bwd_d128.cu", "attn_bwd_d256.cu", "router_bwd.cu", "grad_clip.cu", "selftest.cu",
            "tma_host.cu", "noalloc.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]

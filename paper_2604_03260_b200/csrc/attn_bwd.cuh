@@ -1,7 +1,8 @@
-// What the entry points hand to the attention's backward pass.
+// What the entry points hand to the attention's backward pass, and what its kernels share.
 #pragma once
 
 #include "attn_common.cuh"
+#include "tma_host.cuh"
 
 namespace focus {
 
@@ -23,5 +24,32 @@ struct AttnBwdArgs {
 
 size_t attn_bwd_workspace_bytes(const focus_shape* s, bool gate);
 int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st);
+
+// A pass: rows R1, R2 stay in shared memory, columns C1, C2 stream by.  X = R1 C1^T, Y = R2 C2^T, P and dS of the tile; then
+// BWD_KV   rows are keys: dV += P^T C2 and dK += dS^T C1 (R1 = K, R2 = V, C1 = Q, C2 = dO)
+// BWD_V    rows are keys: dV alone (where the two sums do not fit tensor memory)
+// BWD_K    rows are keys: dK alone
+// BWD_Q    rows are queries: dQ += dS C1 (R1 = Q, R2 = dO, C1 = K, C2 = V)
+enum : int { BWD_KV = 0, BWD_V = 1, BWD_K = 2, BWD_Q = 3 };
+
+struct BwdParams {
+    int Hq, Hkv, G, n, nt, K, w;
+    int heads;                // batch * heads of the rows
+    Divisor by_heads, by_rows_H;          // by that; by heads per sequence of the rows
+    float scale, softcap, lambda;
+    const float* stat;        // [batch Hq][nt][2][128]: lse log2(e), delta
+    const uint32_t* row_mask; // masks of the rows' tokens
+    const uint32_t* bits;     // columns' bitmaps per group [heads of the columns][nt][K][4]; nullptr = every causal pair
+    const uint32_t* live;     // live far tiles [batch Hq][nt][nkw]
+    int nkw;
+    const float* g;
+    float* dg_part;           // [batch heads of the rows][n][ld]
+    __nv_bfloat16 *out1, *out2;           // dV (BWD_KV, BWD_V); dK / dQ
+    int64_t s1b, s1h, s1n, s2b, s2h, s2n;
+    bool wide1, wide2;        // 32-byte stores
+    int32_t* status;
+};
+
+template <int D> int launch_bwd_d(const AttnBwdArgs& a, const BwdParams& kv, const BwdParams& q, cudaStream_t st);
 
 }  // namespace focus

@@ -101,19 +101,26 @@ size_t router_bwd_workspace_bytes(const focus_shape* s, int d) {
     return align_up((size_t)s->K * d * 4, 256) * 2 + align_up((size_t)router_tiles(s) * s->K * d * 4, 256);
 }
 
+template <int LD>
+static int launch_tokens(const focus_shape* s, const RouterBwdArgs& a, const float* F, float* part, cudaStream_t st) {
+    auto kern = router_bwd_kernel<LD>;
+    return check_cuda(launch_dependent(kern, dim3((unsigned)cdiv(a.d_model, RB_COLS), (unsigned)router_tiles(s)), dim3(256), 0, st, a.h, a.h_sb, a.h_sn, a.ds, F, s->n,
+                                       cdiv(s->n, RB_TOKENS), a.d_model, s->K, a.dh, a.dh_sb, a.dh_sn, part), "router backward launch");
+}
+
 int launch_router_bwd(const focus_shape* s, const RouterBwdArgs& a, cudaStream_t st) {
-    const int d = a.d_model, nt = cdiv(s->n, RB_TOKENS), tiles = router_tiles(s), K = s->K;
+    const int d = a.d_model, tiles = router_tiles(s), K = s->K;
     float* F = reinterpret_cast<float*>(a.ws);
     float* T = F + align_up((size_t)K * d * 4, 256) / 4;
     float* part = T + align_up((size_t)K * d * 4, 256) / 4;
     int rc = check_cuda(launch_dependent(router_fold_kernel, dim3((unsigned)cdiv(d, 256), (unsigned)K), dim3(256), 0, st, a.Wg, a.C, d, a.d_g, F), "router fold launch");
     if (rc) return rc;
-    const dim3 grid((unsigned)cdiv(d, RB_COLS), (unsigned)tiles);
-    auto go = [&](auto kern) {
-        return check_cuda(launch_dependent(kern, grid, dim3(256), 0, st, a.h, a.h_sb, a.h_sn, a.ds, F, s->n, nt, d, K, a.dh, a.dh_sb, a.dh_sn, part), "router backward launch");
-    };
-    const int ld = focus_soft_ld(K);
-    rc = ld == 4 ? go(router_bwd_kernel<4>) : ld == 8 ? go(router_bwd_kernel<8>) : ld == 16 ? go(router_bwd_kernel<16>) : go(router_bwd_kernel<32>);
+    switch (focus_soft_ld(K)) {
+        case 4: rc = launch_tokens<4>(s, a, F, part, st); break;
+        case 8: rc = launch_tokens<8>(s, a, F, part, st); break;
+        case 16: rc = launch_tokens<16>(s, a, F, part, st); break;
+        default: rc = launch_tokens<32>(s, a, F, part, st);
+    }
     if (rc) return rc;
     if ((rc = check_cuda(launch_dependent(router_bwd_weights_kernel, dim3((unsigned)cdiv(d, 8)), dim3(256), 0, st, part, a.C, tiles, d, a.d_g, K, T, a.dWg), "router weights launch"))) return rc;
     return check_cuda(launch_dependent(router_bwd_centroids_kernel, dim3((unsigned)a.d_g, (unsigned)K), dim3(256), 0, st, T, a.Wg, d, a.d_g, a.dC), "router centroids launch");

@@ -66,6 +66,11 @@ class focus_grad(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32)]
 
 
+class focus_grads(C.Structure):
+    """a list of gradients (make_grad_list), which holds their tensors"""
+    _fields_ = [("grads", C.c_void_p), ("count", C.c_int32)]
+
+
 class FocusError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"focus status {status}: {message}")
@@ -157,7 +162,7 @@ def lib():
         L.focus_grad_clip_workspace_bytes.restype = sz
         L.focus_grad_clip_workspace_bytes.argtypes = []
         L.focus_grad_clip.restype = C.c_int
-        L.focus_grad_clip.argtypes = [C.POINTER(focus_grad), i32, f32, vp, vp, sz, vp]
+        L.focus_grad_clip.argtypes = [vp, i32, f32, vp, vp, sz, vp]
         L.focus_count_kept.restype = C.c_int
         L.focus_count_kept.argtypes = [SP, vp, vp, vp, vp]
         L.focus_count_kept_noalloc.restype = C.c_int
@@ -182,6 +187,7 @@ class _Ctypes:
     def assign(*args):
         return None
     assign_hidden = build_tiles = attn_fwd = decode_step = assign
+    attn_bwd = gate_attn_bwd = router_scores_bwd = grad_clip = assign
     qk_norm_rope = qk_norm_rope_bwd = kv4_append = kv4_read = kv4_copy_pages = kv4_decode_step = assign
 
 
@@ -198,6 +204,7 @@ def _load_marshal(L):
     m.init(focus_shape, *at(L.focus_assign, L.focus_assign_hidden, L.focus_build_tiles, L.focus_attn_fwd, L.focus_decode_step))
     m.init_kv4(focus_rope, focus_kv4, *at(L.focus_qk_norm_rope, L.focus_qk_norm_rope_bwd, L.focus_kv4_append, L.focus_kv4_read, L.focus_kv4_copy_pages,
                                           L.focus_kv4_decode_step))
+    m.init_bwd(focus_grads, *at(L.focus_attn_bwd, L.focus_gate_attn_bwd, L.focus_router_scores_bwd, L.focus_grad_clip))
     return m
 
 
@@ -509,11 +516,14 @@ def focus_attn_bwd_workspace_bytes(shape) -> int:
 
 def focus_attn_bwd(shape, q, k, v, mq, mk, tiles_ws, layout, o, lse, d_o, dq, dk, dv, ws, dev_status=None, stream=None):
     """dq (like q), dk, dv (like k) bf16 from d_o (like o) and what the forward pass left: o, lse fp32 [batch, Hq, n]; ws uint8 scratch"""
-    B, Hq, Hkv, n = shape.batch, shape.Hq, shape.Hkv, shape.n
-    _check(lib().focus_attn_bwd(C.byref(shape), _heads(q, shape, Hq), _heads(k, shape, Hkv), _heads(v, shape, Hkv), _opt(mq, torch.int32, B, Hq, n),
-                                _opt(mk, torch.int32, B, Hkv, n), _p(tiles_ws), layout, _heads(o, shape, Hq), _dev(lse, torch.float32, B, Hq, n),
-                                _heads(d_o, shape, Hq), _heads(dq, shape, Hq), _heads(dk, shape, Hkv), _heads(dv, shape, Hkv), *_scratch(ws),
-                                _opt(dev_status, torch.int32, 4), _stream(stream)))
+    rc = _short().attn_bwd(shape, q, k, v, mq, mk, tiles_ws, layout, o, lse, d_o, dq, dk, dv, ws, dev_status, stream)
+    if rc is None:
+        B, Hq, Hkv, n = shape.batch, shape.Hq, shape.Hkv, shape.n
+        rc = lib().focus_attn_bwd(C.byref(shape), _heads(q, shape, Hq), _heads(k, shape, Hkv), _heads(v, shape, Hkv), _opt(mq, torch.int32, B, Hq, n),
+                                  _opt(mk, torch.int32, B, Hkv, n), _p(tiles_ws), layout, _heads(o, shape, Hq), _dev(lse, torch.float32, B, Hq, n),
+                                  _heads(d_o, shape, Hq), _heads(dq, shape, Hq), _heads(dk, shape, Hkv), _heads(dv, shape, Hkv), *_scratch(ws),
+                                  _opt(dev_status, torch.int32, 4), _stream(stream))
+    _check(rc)
 
 
 def focus_gate_attn_bwd_workspace_bytes(shape) -> int:
@@ -522,11 +532,14 @@ def focus_gate_attn_bwd_workspace_bytes(shape) -> int:
 
 def focus_gate_attn_bwd(shape, q, k, v, g, lam, o, lse, d_o, dq, dk, dv, dg, ws, dev_status=None, stream=None):
     """the same for the training-time gate; g, dg fp32 [batch, n, focus_soft_ld(K)]"""
-    B, Hq, Hkv, n, ld = shape.batch, shape.Hq, shape.Hkv, shape.n, focus_soft_ld(shape.K)
-    _check(lib().focus_gate_attn_bwd(C.byref(shape), _heads(q, shape, Hq), _heads(k, shape, Hkv), _heads(v, shape, Hkv), _dev(g, torch.float32, B, n, ld), lam,
-                                     _heads(o, shape, Hq), _dev(lse, torch.float32, B, Hq, n), _heads(d_o, shape, Hq), _heads(dq, shape, Hq),
-                                     _heads(dk, shape, Hkv), _heads(dv, shape, Hkv), _dev(dg, torch.float32, B, n, ld), *_scratch(ws),
-                                     _opt(dev_status, torch.int32, 4), _stream(stream)))
+    rc = _short().gate_attn_bwd(shape, q, k, v, g, lam, o, lse, d_o, dq, dk, dv, dg, ws, dev_status, stream)
+    if rc is None:
+        B, Hq, Hkv, n, ld = shape.batch, shape.Hq, shape.Hkv, shape.n, focus_soft_ld(shape.K)
+        rc = lib().focus_gate_attn_bwd(C.byref(shape), _heads(q, shape, Hq), _heads(k, shape, Hkv), _heads(v, shape, Hkv), _dev(g, torch.float32, B, n, ld), lam,
+                                       _heads(o, shape, Hq), _dev(lse, torch.float32, B, Hq, n), _heads(d_o, shape, Hq), _heads(dq, shape, Hq),
+                                       _heads(dk, shape, Hkv), _heads(dv, shape, Hkv), _dev(dg, torch.float32, B, n, ld), *_scratch(ws),
+                                       _opt(dev_status, torch.int32, 4), _stream(stream))
+    _check(rc)
 
 
 def _hidden(t, shape):
@@ -543,12 +556,15 @@ def focus_router_scores_bwd_workspace_bytes(shape, d_model, d_g) -> int:
 
 def focus_router_scores_bwd(shape, h, Wg, Cg, dscores, dh, dWg, dC, ws, stream=None):
     """dh (like h; None: not wanted), dWg fp32 [d_model, d_g], dC fp32 [K, d_g] from dscores fp32 [batch, n, focus_soft_ld(K)]; ws uint8 scratch"""
-    d, dg, K = h.shape[-1], Wg.shape[-1], shape.K
-    assert dh is None or dh.shape == h.shape, (tuple(dh.shape), tuple(h.shape))
-    ph, pd = _hidden(h, shape), _hidden(dh, shape) if dh is not None else (None, 0, d)
-    _check(lib().focus_router_scores_bwd(C.byref(shape), *ph, d, dg, _dev(Wg, torch.float32, d, dg), _dev(Cg, torch.float32, K, dg),
-                                         _dev(dscores, torch.float32, shape.batch, shape.n, focus_soft_ld(K)), *pd, _dev(dWg, torch.float32, d, dg),
-                                         _dev(dC, torch.float32, K, dg), *_scratch(ws), _stream(stream)))
+    rc = _short().router_scores_bwd(shape, h, Wg, Cg, dscores, dh, dWg, dC, ws, stream)
+    if rc is None:
+        d, dg, K = h.shape[-1], Wg.shape[-1], shape.K
+        assert dh is None or dh.shape == h.shape, (tuple(dh.shape), tuple(h.shape))
+        ph, pd = _hidden(h, shape), _hidden(dh, shape) if dh is not None else (None, 0, d)
+        rc = lib().focus_router_scores_bwd(C.byref(shape), *ph, d, dg, _dev(Wg, torch.float32, d, dg), _dev(Cg, torch.float32, K, dg),
+                                           _dev(dscores, torch.float32, shape.batch, shape.n, focus_soft_ld(K)), *pd, _dev(dWg, torch.float32, d, dg),
+                                           _dev(dC, torch.float32, K, dg), *_scratch(ws), _stream(stream))
+    _check(rc)
 
 
 def focus_grad_clip_workspace_bytes() -> int:
@@ -562,18 +578,22 @@ def make_grad_list(grads, out=None):
     out = grads if out is None else list(out)
     assert len(out) == len(grads)
     kinds = {torch.float32: 0, torch.bfloat16: 1}
-    c = (focus_grad * max(1, len(grads)))()
-    for e, s, d in zip(c, grads, out):
+    entries = (focus_grad * max(1, len(grads)))()
+    for e, s, d in zip(entries, grads, out):
         assert s.is_cuda and s.dtype in kinds and s.is_contiguous(), (s.dtype, tuple(s.shape), s.stride())
         assert d.dtype is s.dtype and d.device == s.device and d.is_contiguous() and d.numel() == s.numel(), (d.dtype, tuple(d.shape), d.stride())
         e.src, e.dst, e.count, e.dtype = s.data_ptr(), d.data_ptr(), s.numel(), kinds[s.dtype]
-    c.tensors = (grads, out)
+    c = focus_grads(C.addressof(entries), len(grads))
+    c.tensors = (entries, grads, out)
     return c
 
 
 def focus_grad_clip(grads, max_norm, norm_out, ws, stream=None):
     """grads from make_grad_list; norm_out fp32 [1] or None; ws uint8 scratch"""
-    _check(lib().focus_grad_clip(grads, len(grads.tensors[0]), max_norm, _opt(norm_out, torch.float32, 1), *_scratch(ws), _stream(stream)))
+    rc = _short().grad_clip(grads, max_norm, norm_out, ws, stream)
+    if rc is None:
+        rc = lib().focus_grad_clip(grads.grads, grads.count, max_norm, _opt(norm_out, torch.float32, 1), *_scratch(ws), _stream(stream))
+    _check(rc)
 
 
 def focus_count_kept(shape, mq, tiles_ws, counts_out, stream=None):

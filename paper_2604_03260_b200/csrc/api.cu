@@ -690,7 +690,7 @@ static int router_bwd_sizes(const focus_shape* shape, int32_t d_model, int32_t d
 }
 
 size_t focus_router_scores_bwd_workspace_bytes(const focus_shape* shape, int32_t d_model, int32_t d_g) {
-    return router_bwd_sizes(shape, d_model, d_g) ? 0 : router_bwd_workspace_bytes(shape, d_model);
+    return router_bwd_sizes(shape, d_model, d_g) ? 0 : router_bwd_workspace_bytes(shape, d_model, d_g);
 }
 
 int focus_router_scores_bwd(const focus_shape* shape, const void* h, int64_t stride_b, int64_t stride_n, int32_t d_model, int32_t d_g, const float* Wg,
@@ -708,7 +708,7 @@ int focus_router_scores_bwd(const focus_shape* shape, const void* h, int64_t str
     if (dh == h && (dh_stride_n != stride_n || (shape->batch > 1 && dh_stride_b != stride_b)))
         return fail(FOCUS_ERR_INVALID_ARG, "dh in the place of h has its strides");
     if (dWg == Wg || dC == C || dWg == dC) return fail(FOCUS_ERR_INVALID_ARG, "dWg and dC are buffers of their own");
-    const size_t need = router_bwd_workspace_bytes(shape, d_model);
+    const size_t need = router_bwd_workspace_bytes(shape, d_model, d_g);
     if (!ws || (uintptr_t)ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is NULL or not 16-byte aligned");
     if (ws_bytes < need) return fail(FOCUS_ERR_CAPACITY, "router backward workspace has %zu bytes, %zu needed", ws_bytes, need);
     if ((rc = require_sm100())) return rc;

@@ -149,7 +149,7 @@ struct RouterBwdArgs {
     float *dWg, *dC;
     char* ws;
 };
-size_t router_bwd_workspace_bytes(const focus_shape* s, int d_model);
+size_t router_bwd_workspace_bytes(const focus_shape* s, int d_model, int d_g);
 int launch_router_bwd(const focus_shape* s, const RouterBwdArgs& a, cudaStream_t st);
 size_t grad_clip_workspace_bytes();
 int launch_grad_clip(const focus_grad* grads, int count, double bound, float* norm_out, double* sums, cudaStream_t st);

@@ -23,6 +23,11 @@ namespace {
 
 PyObject* shape_type;                // binding.focus_shape
 PyObject *rope_type, *kv4_type;      // binding.focus_rope, binding.focus_kv4
+PyObject* grads_type;                // binding.focus_grads
+struct Grads {                       // its layout
+    const focus_grad* grads;
+    int32_t count;
+};
 
 // The entry points, from the library that binding.py has loaded: linked against, the loader might find another copy of it.
 decltype(&focus_assign) p_assign;
@@ -36,6 +41,10 @@ decltype(&focus_kv4_append) p_kv4_append;
 decltype(&focus_kv4_read) p_kv4_read;
 decltype(&focus_kv4_copy_pages) p_kv4_copy_pages;
 decltype(&focus_kv4_decode_step) p_kv4_decode_step;
+decltype(&focus_attn_bwd) p_attn_bwd;
+decltype(&focus_gate_attn_bwd) p_gate_attn_bwd;
+decltype(&focus_router_scores_bwd) p_router_scores_bwd;
+decltype(&focus_grad_clip) p_grad_clip;
 
 struct Args {
     PyObject* const* a;
@@ -103,6 +112,23 @@ struct Args {
         const at::Tensor* t = tensor(i);
         if (!t || !t->is_cuda() || t->scalar_type() != type || t->numel() != count || !t->is_contiguous()) { known = false; return nullptr; }
         return t->data_ptr();
+    }
+    // hidden states bf16 [batch, n, d] (or [n, d] for one sequence); their `d`
+    focus_tensor hidden(int i, const focus_shape* s, int64_t& d) {
+        focus_tensor out = {};
+        const at::Tensor* t = tensor(i);
+        if (!t || !s) { known = false; return out; }
+        const int dims = (int)t->dim();
+        if (!t->is_cuda() || t->scalar_type() != at::kBFloat16 || (dims != 3 && !(dims == 2 && s->batch == 1)) || t->stride(dims - 1) != 1 ||
+            (dims == 3 && t->size(0) != s->batch) || t->size(dims - 2) != s->n || t->size(dims - 1) > INT32_MAX) {
+            known = false;
+            return out;
+        }
+        d = t->size(dims - 1);
+        out.ptr = t->data_ptr();
+        out.stride_b = s->batch > 1 ? t->stride(0) : 0;
+        out.stride_n = s->n > 1 ? t->stride(dims - 2) : d;
+        return out;
     }
     // address of a workspace on the GPU, in one piece
     void* scratch(int i) {
@@ -338,6 +364,86 @@ PyObject* kv4_decode_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+int soft_ld(int K) { return K <= 4 ? 4 : K <= 8 ? 8 : K <= 16 ? 16 : 32; }
+
+PyObject* attn_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return enter(args, n, 17, [](Args& a) {
+        auto s = a.shape(0);
+        const int Hq = s ? s->Hq : 0, Hkv = s ? s->Hkv : 0;
+        const int64_t rows = s ? (int64_t)s->batch * s->n : 0;
+        auto q = a.sized(1, s, Hq, false), k = a.sized(2, s, Hkv, false), v = a.sized(3, s, Hkv, false);
+        auto mq = static_cast<const uint32_t*>(a.counted(4, at::kInt, rows * Hq, true)), mk = static_cast<const uint32_t*>(a.counted(5, at::kInt, rows * Hkv, true));
+        auto tiles = a.ptr(6);
+        auto layout = a.integer(7);
+        auto o = a.sized(8, s, Hq, false);
+        auto lse = static_cast<const float*>(a.counted(9, at::kFloat, rows * Hq, false));
+        auto d_o = a.sized(10, s, Hq, false), dq = a.sized(11, s, Hq, false), dk = a.sized(12, s, Hkv, false), dv = a.sized(13, s, Hkv, false);
+        auto ws = a.scratch(14);
+        auto bytes = a.bytes(14);
+        auto status = static_cast<int32_t*>(a.counted(15, at::kInt, 4, true));
+        auto st = a.stream(16);
+        return [=] { return p_attn_bwd(s, q, k, v, mq, mk, tiles, layout, o, lse, d_o, dq, dk, dv, ws, bytes, status, st); };
+    });
+}
+
+PyObject* gate_attn_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return enter(args, n, 16, [](Args& a) {
+        auto s = a.shape(0);
+        const int Hq = s ? s->Hq : 0, Hkv = s ? s->Hkv : 0;
+        const int64_t rows = s ? (int64_t)s->batch * s->n : 0, ld = s ? soft_ld(s->K) : 0;
+        auto q = a.sized(1, s, Hq, false), k = a.sized(2, s, Hkv, false), v = a.sized(3, s, Hkv, false);
+        auto g = static_cast<const float*>(a.counted(4, at::kFloat, rows * ld, false));
+        auto lam = a.number(5);
+        auto o = a.sized(6, s, Hq, false);
+        auto lse = static_cast<const float*>(a.counted(7, at::kFloat, rows * Hq, false));
+        auto d_o = a.sized(8, s, Hq, false), dq = a.sized(9, s, Hq, false), dk = a.sized(10, s, Hkv, false), dv = a.sized(11, s, Hkv, false);
+        auto dg = static_cast<float*>(a.counted(12, at::kFloat, rows * ld, false));
+        auto ws = a.scratch(13);
+        auto bytes = a.bytes(13);
+        auto status = static_cast<int32_t*>(a.counted(14, at::kInt, 4, true));
+        auto st = a.stream(15);
+        return [=] { return p_gate_attn_bwd(s, q, k, v, g, lam, o, lse, d_o, dq, dk, dv, dg, ws, bytes, status, st); };
+    });
+}
+
+PyObject* router_scores_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return enter(args, n, 10, [](Args& a) {
+        auto s = a.shape(0);
+        int64_t d = 0, dd = 0, dg = 0;
+        const int K = s ? s->K : 0;
+        auto h = a.hidden(1, s, d);
+        if (const at::Tensor* t = a.tensor(2)) {
+            if (t->dim() == 2 && t->size(1) <= INT32_MAX) dg = t->size(1);
+            else a.known = false;
+        }
+        auto Wg = static_cast<const float*>(a.counted(2, at::kFloat, d * dg, false)), Cg = static_cast<const float*>(a.counted(3, at::kFloat, K * dg, false));
+        auto ds = static_cast<const float*>(a.counted(4, at::kFloat, s ? (int64_t)s->batch * s->n * soft_ld(K) : 0, false));
+        focus_tensor dh = {};
+        if (a.known && !a.failed && a.a[5] != Py_None) {
+            dh = a.hidden(5, s, dd);
+            if (dd != d) a.known = false;
+        }
+        auto dWg = static_cast<float*>(a.counted(6, at::kFloat, d * dg, false)), dC = static_cast<float*>(a.counted(7, at::kFloat, K * dg, false));
+        auto ws = a.scratch(8);
+        auto bytes = a.bytes(8);
+        auto st = a.stream(9);
+        return [=] { return p_router_scores_bwd(s, h.ptr, h.stride_b, h.stride_n, (int32_t)d, (int32_t)dg, Wg, Cg, ds, dh.ptr, dh.stride_b, dh.stride_n, dWg, dC, ws, bytes, st); };
+    });
+}
+
+PyObject* grad_clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return enter(args, n, 5, [](Args& a) {
+        auto g = a.object<Grads>(0, grads_type);
+        auto bound = a.number(1);
+        auto norm = static_cast<float*>(a.counted(2, at::kFloat, 1, true));
+        auto ws = a.scratch(3);
+        auto bytes = a.bytes(3);
+        auto st = a.stream(4);
+        const Grads list = g ? *g : Grads{};
+        return [=] { return p_grad_clip(list.grads, list.count, bound, norm, ws, bytes, st); };
+    });
+}
+
 // init(type of a shape, addresses of the entry points in the order above)
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 6) return PyErr_Format(PyExc_TypeError, "%zd arguments, not 6", n);
@@ -377,6 +483,23 @@ PyObject* init_kv4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// init_bwd(type of a list of gradients, addresses of the entry points from attn_bwd on)
+PyObject* init_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "%zd arguments, not 5", n);
+    void* at[4];
+    for (int i = 0; i < 4; ++i) {
+        at[i] = PyLong_AsVoidPtr(args[1 + i]);
+        if (!at[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "no address");
+    }
+    p_attn_bwd = reinterpret_cast<decltype(p_attn_bwd)>(at[0]);
+    p_gate_attn_bwd = reinterpret_cast<decltype(p_gate_attn_bwd)>(at[1]);
+    p_router_scores_bwd = reinterpret_cast<decltype(p_router_scores_bwd)>(at[2]);
+    p_grad_clip = reinterpret_cast<decltype(p_grad_clip)>(at[3]);
+    Py_INCREF(args[0]);
+    Py_XSETREF(grads_type, args[0]);
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     {"init", (PyCFunction)(void*)init, METH_FASTCALL, nullptr},
     {"assign", (PyCFunction)(void*)assign, METH_FASTCALL, nullptr},
@@ -391,6 +514,11 @@ PyMethodDef methods[] = {
     {"kv4_read", (PyCFunction)(void*)kv4_read, METH_FASTCALL, nullptr},
     {"kv4_copy_pages", (PyCFunction)(void*)kv4_copy_pages, METH_FASTCALL, nullptr},
     {"kv4_decode_step", (PyCFunction)(void*)kv4_decode_step, METH_FASTCALL, nullptr},
+    {"init_bwd", (PyCFunction)(void*)init_bwd, METH_FASTCALL, nullptr},
+    {"attn_bwd", (PyCFunction)(void*)attn_bwd, METH_FASTCALL, nullptr},
+    {"gate_attn_bwd", (PyCFunction)(void*)gate_attn_bwd, METH_FASTCALL, nullptr},
+    {"router_scores_bwd", (PyCFunction)(void*)router_scores_bwd, METH_FASTCALL, nullptr},
+    {"grad_clip", (PyCFunction)(void*)grad_clip, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "short calls of binding.py", -1, methods};

@@ -10,43 +10,85 @@
 
 namespace focus {
 
-// delta and lse log2(e), 128 of each per tile: rows past the end, and rows without any pair (lse = -inf), get lse = +inf, so that every
-// probability is 0.  With masks, which queries of the tile are members of each group.  A block per (head, tile), a warp per row.
+// -lse log2(e) and -delta, 128 of each per tile: rows past the end, and rows without any pair (lse = -inf), get -inf in the place of the
+// first, so that every probability is 0.  The same as six bf16 numbers a row (the first divided by scale log2(e), in place of -inf a number
+// beyond every score): what the passes over keys add to their products.  With masks, which queries of the tile are members of each group.
+// A block per (head, tile):
+// D / 8 threads a row, every 16-byte piece of the tile asked for at once.
+template <int D>
 __global__ void __launch_bounds__(256)
 bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn, const __nv_bfloat16* dO, int64_t d_sb, int64_t d_sh, int64_t d_sn,
-                const float* lse, int Hq, int n, int nt, int D, const uint32_t* mq, int K, float* stat, uint32_t* qbits) {
+                const float* lse, int Hq, int n, int nt, const uint32_t* mq, int K, float sl2, float* stat, __nv_bfloat16* aug, uint32_t* qbits) {
+    __shared__ float sl[128], sd[128];
+    constexpr int TPR = D / 8, RPP = 256 / TPR, U = D == 256 ? 8 : 128 / RPP;       // threads a row, rows a turn, turns at once
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int hq = blockIdx.x / nt, tile = blockIdx.x % nt, b = hq / Hq, h = hq % Hq;
+    const int hq = blockIdx.x / nt, tile = blockIdx.x % nt, b = hq / Hq, h = hq % Hq, i0 = tile * 128;
     dep_wait();
     dep_trigger();
     float* const t = stat + (size_t)blockIdx.x * 256;
-    for (int r = warp; r < 128; r += 8) {
-        const int i = tile * 128 + r;
-        float s = 0.f, l = INFINITY;
-        if (i < n) {
-            const __nv_bfloat162* orow = reinterpret_cast<const __nv_bfloat162*>(o + b * o_sb + h * o_sh + (int64_t)i * o_sn);
-            const __nv_bfloat162* drow = reinterpret_cast<const __nv_bfloat162*>(dO + b * d_sb + h * d_sh + (int64_t)i * d_sn);
-            for (int d = lane; d < D / 2; d += 32) {
-                const float2 x = __bfloat1622float2(orow[d]), y = __bfloat1622float2(drow[d]);
-                s = fmaf(x.x, y.x, fmaf(x.y, y.y, s));
+    const int r0 = threadIdx.x / TPR, c = threadIdx.x % TPR * 8;
+    const __nv_bfloat16* const ob = o + b * o_sb + h * o_sh + (int64_t)i0 * o_sn + c;
+    const __nv_bfloat16* const db = dO + b * d_sb + h * d_sh + (int64_t)i0 * d_sn + c;
+    if (threadIdx.x < 128) {
+        const int i = i0 + threadIdx.x;
+        const float l = i < n ? lse[(size_t)hq * n + i] : -INFINITY;
+        t[threadIdx.x] = sl[threadIdx.x] = l == -INFINITY ? -INFINITY : -l * LOG2E;
+    }
+#pragma unroll 1
+    for (int v = 0; v < 128 / RPP; v += U) {
+        uint4 x[U], y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int r = r0 + (v + u) * RPP;
+            x[u] = y[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (i0 + r < n) {
+                x[u] = *reinterpret_cast<const uint4*>(ob + r * o_sn);
+                y[u] = *reinterpret_cast<const uint4*>(db + r * d_sn);
             }
-            for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-            l = lse[(size_t)hq * n + i];
-            l = l == -INFINITY ? INFINITY : l * LOG2E;
         }
-        if (lane == 0) {
-            t[r] = l;
-            t[128 + r] = s;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, ys[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
+            float s = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), s);
+                s = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), s);
+            }
+#pragma unroll
+            for (int off = TPR / 2; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+            if (threadIdx.x % TPR == 0) t[128 + r0 + (v + u) * RPP] = sd[r0 + (v + u) * RPP] = -s;
         }
     }
+    __syncthreads();
+    if (threadIdx.x < 128) {
+        const float x = sl[threadIdx.x] / sl2;
+        float v[2] = {isnan(x) ? x : fminf(fmaxf(x, -3e38f), 3e38f), sd[threadIdx.x]};
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 6; ++e) {
+            const __nv_bfloat16 y = __float2bfloat16_rn(v[e / 3]);
+            v[e / 3] -= __bfloat162float(y);
+            w[e / 2] |= (uint32_t)__bfloat16_as_ushort(y) << (16 * (e & 1));
+        }
+        reinterpret_cast<uint4*>(aug)[(size_t)blockIdx.x * 128 + threadIdx.x] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
     if (mq && warp < 4) {
-        const int i = tile * 128 + warp * 32 + lane;
+        const int i = i0 + warp * 32 + lane;
         const uint32_t m = i < n ? mq[(size_t)hq * n + i] : 0u;
         for (int g = 0; g < K; ++g) {
             const uint32_t w = __ballot_sync(0xffffffffu, (m >> g) & 1u);
             if (lane == 0) qbits[((size_t)blockIdx.x * K + g) * 4 + warp] = w;
         }
     }
+}
+
+template <int D>
+static int launch_bwd_rows(const AttnBwdArgs& a, int nt, float* stat, __nv_bfloat16* aug, uint32_t* qbits, cudaStream_t st) {
+    auto kern = bwd_rows_kernel<D>;
+    return check_cuda(launch_dependent(kern, dim3((unsigned)(a.s.batch * a.s.Hq * nt)), dim3(256), 0, st, (const __nv_bfloat16*)a.o.ptr, a.o.stride_b, a.o.stride_h,
+                                       a.o.stride_n, (const __nv_bfloat16*)a.dO.ptr, a.dO.stride_b, a.dO.stride_h, a.dO.stride_n, a.lse, a.s.Hq, a.s.n, nt,
+                                       a.tiles ? a.mq : nullptr, a.s.K, a.scale * LOG2E, stat, aug, qbits), "attention backward rows launch");
 }
 
 // dg[b][i][:] = sum over the heads of both sides' partial sums, in their order; columns from K on are written as 0
@@ -64,7 +106,7 @@ bwd_gate_sum_kernel(const float* gq, const float* gk, int Hq, int Hkv, long long
 }
 
 struct BwdWorkspace {
-    size_t stat, qbits, gq, gk, bytes;
+    size_t stat, aug, qbits, gq, gk, bytes;
 };
 static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
     const size_t HQ = (size_t)s->batch * s->Hq, HK = (size_t)s->batch * s->Hkv, nt = cdiv(s->n, 128), row = (size_t)s->n * focus_soft_ld(s->K) * 4;
@@ -72,6 +114,7 @@ static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
     w.stat = take(HQ * nt * 256 * 4);
+    w.aug = take(HQ * nt * 128 * 16);
     w.qbits = gate ? 0 : take(HQ * nt * s->K * 16);
     w.gq = gate ? take(HQ * row) : 0;
     w.gk = gate ? take(HK * row) : 0;
@@ -87,15 +130,15 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st) {
     const int nt = cdiv(s.n, 128), HQ = s.batch * s.Hq, HK = s.batch * s.Hkv;
     if ((long long)HQ * nt > 0x7fffffffll) return fail(FOCUS_ERR_UNSUPPORTED, "attention backward: %lld tiles exceed 2^31 - 1", (long long)HQ * nt);
     float* const stat = reinterpret_cast<float*>(a.ws + w.stat);
+    __nv_bfloat16* const aug = reinterpret_cast<__nv_bfloat16*>(a.ws + w.aug);
     uint32_t* const qbits = reinterpret_cast<uint32_t*>(a.ws + w.qbits);
-    int rc = check_cuda(launch_dependent(bwd_rows_kernel, dim3((unsigned)(HQ * nt)), dim3(256), 0, st, (const __nv_bfloat16*)a.o.ptr, a.o.stride_b, a.o.stride_h,
-                                         a.o.stride_n, (const __nv_bfloat16*)a.dO.ptr, a.dO.stride_b, a.dO.stride_h, a.dO.stride_n, a.lse, s.Hq, s.n, nt, s.D,
-                                         a.tiles ? a.mq : nullptr, s.K, stat, qbits), "attention backward rows launch");
+    int rc = s.D == 64 ? launch_bwd_rows<64>(a, nt, stat, aug, qbits, st) : s.D == 128 ? launch_bwd_rows<128>(a, nt, stat, aug, qbits, st) : launch_bwd_rows<256>(a, nt, stat, aug, qbits, st);
     if (rc) return rc;
     BwdParams p = {};
     p.Hq = s.Hq; p.Hkv = s.Hkv; p.G = s.Hq / s.Hkv; p.n = s.n; p.nt = nt; p.K = s.K; p.w = s.window < s.n ? s.window : s.n;
     p.scale = a.scale; p.softcap = s.softcap; p.lambda = a.lambda;
     p.stat = stat;
+    p.aug = aug;
     p.g = a.g;
     p.nkw = cdiv(nt, 32);
     p.live = a.tiles ? reinterpret_cast<const uint32_t*>(a.tiles + a.L.live) : nullptr;

@@ -37,7 +37,8 @@ struct BwdParams {
     int heads;                // batch * heads of the rows
     Divisor by_heads, by_rows_H;          // by that; by heads per sequence of the rows
     float scale, softcap, lambda;
-    const float* stat;        // [batch Hq][nt][2][128]: lse log2(e), delta
+    const float* stat;        // [batch Hq][nt][2][128]: -lse log2(e), -delta
+    const __nv_bfloat16* aug; // [batch Hq][nt][128][8]: -lse / scale, -delta in three terms each
     const uint32_t* row_mask; // masks of the rows' tokens
     const uint32_t* bits;     // columns' bitmaps per group [heads of the columns][nt][K][4]; nullptr = every causal pair
     const uint32_t* live;     // live far tiles [batch Hq][nt][nkw]

@@ -1,10 +1,17 @@
 // The passes of the attention's backward: one CTA per (head, 128 rows), its tiles of columns one after another.
 //   warp 0        TMA: the two row tiles once, then both column tiles of every visited tile into a ring of slots (128-byte swizzle)
-//   warp 2        number, head, lse, delta and assignments of the visited tiles, through a ring of their own
 //   warp 1        MMA issuer: X = R1 C1^T, Y = R2 C2^T (operands in shared memory), then the sums with P or dS (bf16, tensor memory) as the
 //                 first operand and C2 or C1 read along its other dimension as the second
-//   warps 4-11    P = exp2(X - lse), dS = P (Y - delta): two threads a row, each half of the tile's columns
-// The tensor pipe works in order, so a product may be issued into the place of an operand that an earlier one reads.
+//   warp 2        what the others need to know of the visited tiles: number and head; lse, delta and assignments of the columns
+//   warps 4-7     P = exp2(X - lse), dS = P (Y - delta) of the even tiles, a thread a row
+//   warps 8-11    of the odd ones
+// The tensor pipe works in order, so a product may be issued into the place of an operand that an earlier one reads.  Two tiles are at work
+// at a time: while one group of warps takes exponentials the other waits for, or works on, the other tile's products.  With both groups on
+// the halves of one tile a tile took the sum of what both phases wait for (D = 128: 3300 and 2650 cycles for the two passes).
+//
+// Tensor memory: the sums, and three places X0, X1, Y in turn -- P goes to the first half of its X, dS to the second (with one sum: the
+// first), so that Y is free for the next tile as soon as it has been read.  Where two sums of 128 columns leave room for two places
+// only (BWD_KV at D = 128) a tile has one: X, P, then Y when the sum with P has been issued, then dS.
 #pragma once
 
 #include "attn_bwd.cuh"
@@ -19,44 +26,76 @@ __device__ __forceinline__ float rcp_approx(float x) {
     return y;
 }
 
-template <int D, int MODE, int LD>
+// The bits of 32 columns in the order in which they become masks of packed pairs: columns 0, 2, ... 14 in byte 0, 1, 3, ... 15 in byte 1,
+// 16, 18, ... in byte 2, 17, 19, ... in byte 3; a shift brings a pair's two bits to the tops of two bytes, whose signs are then spread.
+__device__ __forceinline__ uint32_t pair_bits(uint32_t x) {
+    auto even = [](uint32_t v) {
+        v &= 0x55555555u;
+        v = (v | v >> 1) & 0x33333333u;
+        v = (v | v >> 2) & 0x0f0f0f0fu;
+        return (v | v >> 4) & 0x00ff00ffu;
+    };
+    return even(x) | even(x >> 1) << 8;
+}
+
+// bytes of a word, each the sign of one of its bytes eight times over (selectors 8 to 11: byte 0 to 3)
+template <uint32_t SEL> __device__ __forceinline__ uint32_t byte_signs(uint32_t x) {
+    uint32_t y;
+    asm("prmt.b32 %0, %1, %1, %2;" : "=r"(y) : "r"(x), "n"(SEL));
+    return y;
+}
+
+template <int D, int MODE, bool CAP, int LD>
 struct BwdCfg {
     static constexpr bool KEYS = MODE != BWD_Q;
     static constexpr bool HAS_V = MODE == BWD_KV || MODE == BWD_V, HAS_DS = MODE != BWD_V;
-    static constexpr int NCOL = D == 256 ? 64 : 128;             // columns of a tile
-    static constexpr int NC = NCOL / 2;                          // of a thread
+    // Columns of a tile, all of them one thread's: 128 probabilities in registers; with the gate two numbers a pair are held, so 64, and at
+    // D = 256 the row tiles leave no room for wider ones
+    static constexpr int NCOL = D == 256 || LD > 0 ? 64 : 128;
+    static constexpr bool ONE_PLACE = MODE == BWD_KV && D == 128 && NCOL == 128;        // X and Y of a tile in the same place
     static constexpr int SUBT = D / 64;
     static constexpr uint32_t SUBR = 128 * 128, SUBC = NCOL * 128;
     static constexpr uint32_t R_BYTES = SUBR * SUBT, C_BYTES = SUBC * SUBT;
     static constexpr int NR = MODE == BWD_V ? 1 : 2;             // row tiles
-    static constexpr int NX = MODE == BWD_KV ? 1 : 2;            // places of X
-    static constexpr int NINFO = 2;                              // tiles handed on ahead
-    static constexpr uint32_t STAT_BYTES = KEYS ? 2 * NCOL * 4 : 0;
+    // Rows are keys: lse and delta go by the column.  They come as six more numbers a column (-lse / scale and -delta in three bf16 terms
+    // each, 24 bits), which one more 16-deep step of X and of Y, against rows of ones, adds to the products; a thread then needs nothing that
+    // goes by the column.  Not where a cap or a gate comes between the product and lse, nor where shared memory has no room for it (D = 128,
+    // dK at D = 256); there they are copied to shared memory and read.
+    static constexpr bool AUG = KEYS && !CAP && LD == 0 && !ONE_PLACE && !(D == 256 && MODE == BWD_K);
+    static constexpr uint32_t AUG_BYTES = AUG ? NCOL * 16 : 0, CONST_BYTES = AUG ? 4 * 2048 : 0;        // (ones for X, zeros, ones for Y, zeros)
+    static constexpr uint32_t C1_BYTES = C_BYTES + AUG_BYTES;
+    static constexpr uint32_t STAT_BYTES = KEYS && !AUG ? 2 * NCOL * 4 : 0;
     // The columns' assignments, copied beside the tile; at D = 256 there is no room, they are read from L1 (one address a warp)
     static constexpr bool GATE_SMEM = LD > 0 && D != 256;
     static constexpr uint32_t GATE_BYTES = GATE_SMEM ? NCOL * LD * 4 : 0;
-    static constexpr uint32_t INFO_BYTES = STAT_BYTES + GATE_BYTES;
-    static constexpr uint32_t CTL_BYTES = 512;
-    static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - NINFO * INFO_BYTES;
-    static constexpr int NSLOT = ROOM / C_BYTES > 8 ? 8 : ROOM / C_BYTES;
-    static_assert(NSLOT >= 3, "two tiles of columns and one ahead");
-    static constexpr uint32_t OFF_C = NR * R_BYTES, OFF_INFO = OFF_C + NSLOT * C_BYTES, OFF_CTL = OFF_INFO + NINFO * INFO_BYTES;
-    static constexpr uint32_t SMEM = OFF_CTL + CTL_BYTES;
-    static constexpr uint32_t COL_X = 0, COL_Y = NX * NCOL, COL_A = NCOL == 64 ? 256 : NX * NCOL + (MODE == BWD_V ? 0 : NCOL);
-    static constexpr uint32_t COL_V = COL_A, COL_S = MODE == BWD_KV ? COL_A + D : COL_A;       // sums with P, with dS
+    static constexpr uint32_t INFO_BYTES = STAT_BYTES + GATE_BYTES;               // one tile; two of them
+    static constexpr uint32_t CTL_BYTES = 1024;
+    static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - 2 * INFO_BYTES - CONST_BYTES;
+    // C1 of a tile is held from its X to its sum with dS, two tiles later, C2 for a product or two rings of their own, the larger for C1
+    static constexpr int NFIT = ROOM / C1_BYTES > 8 ? 8 : ROOM / C1_BYTES;
+    static constexpr int NS2 = NFIT / 2, NS1 = NFIT - NS2, NSLOT = NS1 + NS2;
+    static_assert(NS2 >= 1 && NS1 >= 2 && (!HAS_DS || NS1 >= 3 || (NS2 == 1 && !ONE_PLACE)), "two tiles at work");
+    static constexpr int P_PARTS = LD == 0 && KEYS ? 2 : 1;      // parts in which P and dS are handed over: most of a sum runs while the last are worked out
+    static constexpr int PART0 = P_PARTS == 1 ? NCOL : NCOL == 128 ? 96 : 32;     // columns of the first
+    static constexpr uint32_t OFF_C = NR * R_BYTES, OFF_CONST = OFF_C + NS1 * C1_BYTES + NS2 * C_BYTES, OFF_INFO = OFF_CONST + CONST_BYTES;
+    static constexpr uint32_t OFF_CTL = OFF_INFO + 2 * INFO_BYTES, SMEM = OFF_CTL + CTL_BYTES;
+    static __device__ __forceinline__ uint32_t slot_at(uint32_t s) { return s < NS1 ? s * C1_BYTES : NS1 * C1_BYTES + (s - NS1) * C_BYTES; }
+    static constexpr uint32_t COL_X = 0, COL_Y = 2 * NCOL, COL_V = NCOL == 64 || ONE_PLACE || MODE == BWD_V ? 256 : 384, COL_S = MODE == BWD_KV ? COL_V + D : COL_V;
     static_assert(COL_S + D <= 512, "tensor memory");
+    static constexpr uint32_t DS_AT = HAS_V && !ONE_PLACE ? NCOL / 2 : 0;         // of dS in the place of X
 };
 
 struct BwdCtl {
-    uint64_t r_full, full[8], empty[8];
-    uint64_t info_full[2], info_empty[2];
-    uint64_t x_full[2], p_full[2], y_full, ds_full, acc_full, dg_full;
+    uint64_t r_full, acc_full, dg_full, full[8], empty[8];      // slots of C1, then of C2
+    uint64_t id_full[4], id_empty[4];             // numbers of the tiles
+    uint64_t info_full[2], info_empty[2];         // what else there is of a tile
+    uint64_t x_full[2], p_full[2][2], y_full[2], y_taken[2], ds_full[2][2];       // by the tile's parity (and part)
     uint32_t limit, tmem_base;
     int abort_flag;
     int more[8];                  // of a slot with C1: whether there is a tile at all
-    int tile[2], head[2];         // column tile and its head; tile -1: no more
+    int tile[4], head[4];         // column tile and its head; tile -1: no more
 };
-static_assert(sizeof(BwdCtl) <= 512, "CTL_BYTES");
+static_assert(sizeof(BwdCtl) <= 1024, "CTL_BYTES");
 
 // The visited tiles of an item, in order; run by the whole TMA warp
 template <bool KEYS, int NCOL>
@@ -108,9 +147,9 @@ template <int D, int MODE, bool CAP, int LD>
 __global__ void __launch_bounds__(BWD_THREADS, 1)
 attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant__ CUtensorMap tm_r2, const __grid_constant__ CUtensorMap tm_c1,
                 const __grid_constant__ CUtensorMap tm_c2, const __grid_constant__ BwdParams p) {
-    using C = BwdCfg<D, MODE, LD>;
-    constexpr bool KEYS = C::KEYS;
-    constexpr int NCOL = C::NCOL, NC = C::NC, NX = C::NX;
+    using C = BwdCfg<D, MODE, CAP, LD>;
+    constexpr bool KEYS = C::KEYS, ONE = C::ONE_PLACE;
+    constexpr int NCOL = C::NCOL;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     BwdCtl& ctl = *reinterpret_cast<BwdCtl*>(smem_raw + C::OFF_CTL);
     const uint32_t base = smem_u32(smem_raw);
@@ -146,23 +185,30 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
     }
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&ctl.r_full), 1);
-        for (int s = 0; s < C::NSLOT; ++s) { mbar_init(smem_u32(&ctl.full[s]), 1); mbar_init(smem_u32(&ctl.empty[s]), 1); }
-        for (int x = 0; x < 2; ++x) {
-            mbar_init(smem_u32(&ctl.info_full[x]), 1);
-            mbar_init(smem_u32(&ctl.info_empty[x]), 8);             // (warps 4 to 11)
-            mbar_init(smem_u32(&ctl.x_full[x]), 1);
-            mbar_init(smem_u32(&ctl.p_full[x]), 256);
-        }
-        mbar_init(smem_u32(&ctl.y_full), 1);
-        mbar_init(smem_u32(&ctl.ds_full), 256);
         mbar_init(smem_u32(&ctl.acc_full), 1);
         mbar_init(smem_u32(&ctl.dg_full), 128);
+        for (int s = 0; s < C::NSLOT; ++s) { mbar_init(smem_u32(&ctl.full[s]), 1); mbar_init(smem_u32(&ctl.empty[s]), 1); }
+        for (int x = 0; x < 4; ++x) { mbar_init(smem_u32(&ctl.id_full[x]), 1); mbar_init(smem_u32(&ctl.id_empty[x]), 4); }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(smem_u32(&ctl.info_full[x]), 1);
+            mbar_init(smem_u32(&ctl.info_empty[x]), 4);             // (the four warps of a tile)
+            mbar_init(smem_u32(&ctl.x_full[x]), 1);
+            for (int q = 0; q < 2; ++q) { mbar_init(smem_u32(&ctl.p_full[x][q]), 128); mbar_init(smem_u32(&ctl.ds_full[x][q]), 128); }
+            mbar_init(smem_u32(&ctl.y_full[x]), 1);
+            mbar_init(smem_u32(&ctl.y_taken[x]), 128);
+        }
         ctl.abort_flag = 0;
         ctl.limit = wait_limit(4000000000ull);
         fence_mbar_init();
     }
+    if constexpr (C::AUG) {                 // rows of ones against the terms of lse, and of delta
+        for (int e = threadIdx.x; e < 512; e += BWD_THREADS)
+            *reinterpret_cast<uint4*>(smem_raw + C::OFF_CONST + e * 16) = e < 128 ? make_uint4(0x3f803f80u, 0x3f80u, 0u, 0u)
+                                                                          : e >= 256 && e < 384 ? make_uint4(0u, 0x3f800000u, 0x3f803f80u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+        fence_proxy_async_smem();
+    }
     if constexpr (C::GATE_SMEM) {           // (rows of assignments past the end of a sequence are not copied)
-        for (int e = threadIdx.x; e < C::NINFO * (int)C::INFO_BYTES / 4; e += BWD_THREADS) reinterpret_cast<float*>(smem_raw + C::OFF_INFO)[e] = 0.f;
+        for (int e = threadIdx.x; e < 2 * (int)C::INFO_BYTES / 4; e += BWD_THREADS) reinterpret_cast<float*>(smem_raw + C::OFF_INFO)[e] = 0.f;
         fence_proxy_async_smem();
     }
     if (warp == 1) {
@@ -189,29 +235,34 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
             }
         }
         BwdWalk<KEYS, NCOL> walk(p, lane, row_tile, b, h);
-        RingAt<C::NSLOT> slot;
+        RingAt<C::NS1> ring1;
+        RingAt<C::NS2> ring2;
         for (;;) {
             const int t = walk.next();
             const int hc = KEYS ? h * p.G + walk.hi : hk;           // head of the columns
-#pragma unroll
-            for (int x = 0; x < 2; ++x, slot.next()) {
-                if (!wait(ctl.empty[slot.slot], slot.phase ^ 1, 11)) break;
+            auto load = [&](uint32_t slot, uint32_t phase, const CUtensorMap* map, bool first) -> bool {
+                if (!wait(ctl.empty[slot], phase ^ 1, 11)) return false;
                 if (lane == 0) {
-                    const uint32_t bar = smem_u32(&ctl.full[slot.slot]);
-                    if (x == 0) ctl.more[slot.slot] = t >= 0;
+                    const uint32_t bar = smem_u32(&ctl.full[slot]);
+                    if (first) ctl.more[slot] = t >= 0;
                     if (t < 0) {
                         mbar_arrive(bar);
                     } else {
-                        mbar_arrive_expect_tx(bar, C::C_BYTES);
+                        const uint32_t at = base + C::OFF_C + C::slot_at(slot);
+                        mbar_arrive_expect_tx(bar, first ? C::C1_BYTES : C::C_BYTES);
 #pragma unroll
-                        for (int c = 0; c < C::SUBT; ++c)
-                            tma_load_4d(base + C::OFF_C + slot.slot * C::C_BYTES + c * C::SUBC, x ? &tm_c2 : &tm_c1, bar, c * 64, t * NCOL, hc, b);
+                        for (int c = 0; c < C::SUBT; ++c) tma_load_4d(at + c * C::SUBC, map, bar, c * 64, t * NCOL, hc, b);
+                        if (C::AUG && first)
+                            bulk_load(at + C::C_BYTES, p.aug + (((size_t)(b * p.Hq + hc) * p.nt + t * NCOL / 128) * 128 + t * NCOL % 128) * 8, C::AUG_BYTES, bar);
                     }
                 }
                 __syncwarp();
-                if (t < 0) break;
-            }
-            if (bad || t < 0) break;
+                return true;
+            };
+            if (!load(ring1.slot, ring1.phase, &tm_c1, true) || t < 0) break;
+            ring1.next();
+            if (!load(C::NS1 + ring2.slot, ring2.phase, &tm_c2, false)) break;
+            ring2.next();
         }
         if (bad && lane == 0) give_up(bad);
         __syncwarp();
@@ -219,32 +270,49 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
         // ------------------------------------------------------------------ what the other warps need to know of a tile
         const int hk = KEYS ? h : h / p.G;
         BwdWalk<KEYS, NCOL> walk(p, lane, row_tile, b, h);
-        RingAt<C::NINFO> handed;
+        RingAt<4> id;
+        RingAt<2> info;
+        // A tile's number is handed on up to four tiles ahead, the rest when its place is free, which is two tiles behind: so the tiles
+        // are walked one ahead of what is copied
+        int t = walk.next(), ends = 0;
+        int held = -1, held_head = 0;            // tile whose number has been handed on, the rest not yet
         for (;;) {
-            const int t = walk.next();
             const int hc = KEYS ? h * p.G + walk.hi : hk;
-            if (!wait(ctl.info_empty[handed.slot], handed.phase ^ 1, 12)) break;
-            if (lane == 0) {
-                const uint32_t bar = smem_u32(&ctl.info_full[handed.slot]), at = base + C::OFF_INFO + handed.slot * C::INFO_BYTES;
-                ctl.tile[handed.slot] = t;
-                ctl.head[handed.slot] = hc;
-                const int rows = min(NCOL, p.n - t * NCOL);           // (a half tile may lie past the end)
-                const uint32_t gbytes = C::GATE_SMEM && t >= 0 && rows > 0 ? (uint32_t)rows * LD * 4 : 0u;
-                if (t < 0 || C::STAT_BYTES + gbytes == 0) {
-                    mbar_arrive(bar);
-                } else {
-                    mbar_arrive_expect_tx(bar, C::STAT_BYTES + gbytes);
+            if (ends < 2) {
+                if (!wait(ctl.id_empty[id.slot], id.phase ^ 1, 13)) break;
+                if (lane == 0) {
+                    ctl.tile[id.slot] = t;
+                    ctl.head[id.slot] = hc;
+                    mbar_arrive(smem_u32(&ctl.id_full[id.slot]));
+                }
+                __syncwarp();
+                id.next();
+                if (t < 0) ++ends;               // (a last one for each group of warps)
+            }
+            if (C::INFO_BYTES > 0 && held >= 0) {
+                if (!wait(ctl.info_empty[info.slot], info.phase ^ 1, 12)) break;
+                if (lane == 0) {
+                    const uint32_t bar = smem_u32(&ctl.info_full[info.slot]), at = base + C::OFF_INFO + info.slot * C::INFO_BYTES;
+                    const int rows = min(NCOL, p.n - held * NCOL);    // (a half tile may lie past the end)
+                    const uint32_t gbytes = C::GATE_SMEM && rows > 0 ? (uint32_t)rows * LD * 4 : 0u;
+                    if (C::STAT_BYTES + gbytes == 0) mbar_arrive(bar); else mbar_arrive_expect_tx(bar, C::STAT_BYTES + gbytes);
                     if constexpr (KEYS) {
-                        const float* st = p.stat + ((size_t)(b * p.Hq + hc) * p.nt + t * NCOL / 128) * 256 + t * NCOL % 128;
+                        const float* st = p.stat + ((size_t)(b * p.Hq + held_head) * p.nt + held * NCOL / 128) * 256 + held * NCOL % 128;
                         bulk_load(at, st, NCOL * 4, bar);
                         bulk_load(at + NCOL * 4, st + 128, NCOL * 4, bar);
                     }
-                    if (gbytes) bulk_load(at + C::STAT_BYTES, p.g + ((size_t)b * p.n + (size_t)t * NCOL) * (LD > 0 ? LD : 1), gbytes, bar);
+                    if (gbytes) bulk_load(at + C::STAT_BYTES, p.g + ((size_t)b * p.n + (size_t)held * NCOL) * (LD > 0 ? LD : 1), gbytes, bar);
                 }
+                __syncwarp();
+                info.next();
             }
-            __syncwarp();
-            handed.next();
-            if (t < 0) break;
+            held = t;
+            held_head = hc;
+            if (t < 0) {
+                if (ends >= 2) break;
+            } else {
+                t = walk.next();
+            }
         }
         if (bad && lane == 0) give_up(bad);
         __syncwarp();
@@ -254,110 +322,177 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
         const uint32_t r1 = (uint32_t)smem_desc_sw128(base, 16, 1024), r2 = r1 + (C::R_BYTES >> 4);
         const uint32_t ck = (uint32_t)smem_desc_sw128(base + C::OFF_C, 16, 1024);                  // columns along D
         const uint32_t cm = (uint32_t)smem_desc_sw128(base + C::OFF_C, C::SUBC, 1024);             // along the tokens
-        RingAt<C::NSLOT> slot;              // next slot to be taken, in the ring's order: C1 of a tile with its X, C2 with its Y (without Y, behind X)
-        auto take = [&](uint32_t& at, int where) -> bool {
-            at = slot.slot;
-            if (!wait(ctl.full[at], slot.phase, where)) return false;
-            slot.next();
-            tc_fence_after();
-            return true;
-        };
-        auto product = [&](uint32_t d, uint32_t r, uint32_t at) {
-            const uint32_t c = ck + at * (C::C_BYTES >> 4);
+        RingAt<C::NS1> at1;                                // slots that the next X, the next Y reads
+        RingAt<C::NS2> at2;
+        // d = rows (X: R1, Y: R2) times the columns in slot `at`; `aug`: slot of the tile's C1, behind which its lse and delta are
+        auto product = [&](uint32_t d, bool y, uint32_t at, uint32_t aug) {
+            const uint32_t r = y ? r2 : r1, c = ck + (C::slot_at(at) >> 4);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) umma_ss_lo(d, r + (ks >> 2) * (C::SUBR >> 4) + (ks & 3) * 2, c + (ks >> 2) * (C::SUBC >> 4) + (ks & 3) * 2, IDESC_X, ks > 0);
+            if constexpr (C::AUG) {
+                const uint32_t ones = base + C::OFF_CONST + (y ? 4096 : 0), x = base + C::OFF_C + C::slot_at(aug) + C::C_BYTES;
+                umma_ss(d, smem_desc_plain(ones, 2048, 128), smem_desc_plain(x, base + C::OFF_CONST + 2048 - x, 128), IDESC_X, 1);
+            }
         };
-        // the two halves of the columns lie NC columns of tensor memory apart
-        auto sum = [&](uint32_t d, uint32_t a, uint32_t at, bool more) {
-            const uint32_t c = cm + at * (C::C_BYTES >> 4);
-#pragma unroll
-            for (int ks = 0; ks < NCOL / 16; ++ks) umma_ts_lo(d, a + (ks / (NC / 16)) * NC + (ks % (NC / 16)) * 8, c + ks * 128, IDESC_A, more || ks > 0);
-        };
-        // X of the next tile into place u; false: there is none (or `bad`)
-        auto issue_x = [&](uint32_t u, uint32_t& c1) -> bool {
-            if (!take(c1, 21)) return false;
+        // the slot with C1 of the next tile; false: there is none (or `bad`)
+        auto take1 = [&](uint32_t& c1) -> bool {
+            c1 = at1.slot;
+            if (!wait(ctl.full[c1], at1.phase, 21)) return false;
             if (!*(volatile int*)&ctl.more[c1]) return false;
-            if (elect_one()) {
-                product(tmem + C::COL_X + u * NCOL, r1, c1);
-                umma_commit(smem_u32(&ctl.x_full[u]));
-                if (!C::HAS_DS) umma_commit(smem_u32(&ctl.empty[c1]));
-            }
-            __syncwarp();
+            at1.next();
             return true;
         };
-        auto issue_y = [&](uint32_t& c2) -> bool {
-            if (!take(c2, 22)) return false;
-            if (elect_one()) {
-                product(tmem + C::COL_Y, r2, c2);
-                umma_commit(smem_u32(&ctl.y_full));
-                if (!C::HAS_V) umma_commit(smem_u32(&ctl.empty[c2]));
-            }
-            __syncwarp();
+        auto take2 = [&](uint32_t& c2) -> bool {
+            c2 = C::NS1 + at2.slot;
+            if (!wait(ctl.full[c2], at2.phase, 22)) return false;
+            at2.next();
             return true;
         };
+        // (by the elected lane)
+        auto put_x = [&](uint32_t i, uint32_t c1) {
+            product(tmem + C::COL_X + i * NCOL, false, c1, c1);
+            umma_commit(smem_u32(&ctl.x_full[i]));
+            if (!C::HAS_DS) umma_commit(smem_u32(&ctl.empty[c1]));
+        };
+        auto put_y = [&](uint32_t i, uint32_t c2, uint32_t c1) {
+            product(tmem + (ONE ? C::COL_X + i * NCOL : C::COL_Y), true, c2, c1);
+            umma_commit(smem_u32(&ctl.y_full[i]));
+            if (!C::HAS_V || ONE) umma_commit(smem_u32(&ctl.empty[c2]));
+        };
+        // a sum's steps, part by part as the first operand (at `a`) comes; then what `last` issues
+        auto sum = [&](uint64_t (&bars)[2], uint32_t parity, int where, uint32_t d, uint32_t a, uint32_t at, bool more, auto last) -> bool {
+            const uint32_t c = cm + (C::slot_at(at) >> 4);
+#pragma unroll
+            for (int q = 0; q < C::P_PARTS; ++q) {
+                if (!wait(bars[q], parity, where + q)) return false;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = q ? C::PART0 / 16 : 0; ks < (q == C::P_PARTS - 1 ? NCOL : C::PART0) / 16; ++ks)
+                        umma_ts_lo(d, a + ks * 8, c + ks * 128, IDESC_A, more || ks > 0);
+                    if (q == C::P_PARTS - 1) last();
+                }
+            }
+            return true;
+        };
+        // by the parity of a tile: the slots of its C1 and C2.  The slots that a step will read are waited for ahead of it, while the
+        // products before it run: a wait takes some 120 cycles even where it need not wait, and what has been issued lasts little longer.
+        uint32_t s1[2] = {0, 0}, s2[2] = {0, 0};
         do {
             if (!wait(ctl.r_full, 0, 20)) break;
+            if (!take1(s1[0])) break;                      // (every item has its diagonal tile)
             tc_fence_after();
-            uint32_t a1 = 0, a2 = 0, b1 = 0, b2 = 0;       // slots of tile t and of the next
-            if (!issue_x(0, a1)) break;                    // (every item has its diagonal tile)
-            if (C::HAS_DS ? !issue_y(a2) : !take(a2, 22)) break;
-            bool next = false;                             // X of tile t + 1 has been issued
-            if (NX == 2) {
-                next = issue_x(1, b1);
-                if (bad || (next && !C::HAS_DS && !take(b2, 22))) break;
-            }
-            for (uint32_t t = 0;; ++t) {
-                const uint32_t i = NX == 2 ? t & 1 : 0;
-                if (C::HAS_V) {
-                    if (!wait(ctl.p_full[i], (NX == 2 ? t >> 1 : t) & 1, 24)) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        sum(tmem + C::COL_V, tmem + C::COL_X + i * NCOL, a2, t > 0);
-                        umma_commit(smem_u32(&ctl.empty[a2]));
+            if (elect_one()) put_x(0, s1[0]);
+            if (!take2(s2[0])) break;
+            if (C::HAS_DS && !ONE && elect_one()) put_y(0, s2[0], s1[0]);
+            bool more = take1(s1[1]);                      // X of the last tile asked for has been issued
+            if (bad) break;
+            if (more && elect_one()) put_x(1, s1[1]);
+            if constexpr (ONE) {
+                // first step of a tile: sum with P, then Y into the same place; second: sum with dS, then X of the tile after next.  The
+                // order lets the other group's step run while a group is at work: even first, odd second, even second, odd first
+                auto first = [&](int i, uint32_t u) -> bool {          // u: tiles of this parity before
+                    return sum(ctl.p_full[i], u & 1, 24, tmem + C::COL_V, tmem + C::COL_X + i * NCOL, s2[i], i > 0 || u > 0, [&] { put_y(i, s2[i], s1[i]); });
+                };
+                auto second = [&](int i, uint32_t u) -> bool {
+                    const uint32_t old = s1[i];
+                    if (more) more = take1(s1[i]);
+                    if (bad) return false;
+                    return sum(ctl.ds_full[i], u & 1, 26, tmem + C::COL_S, tmem + C::COL_X + i * NCOL, old, i > 0 || u > 0, [&] {
+                        umma_commit(smem_u32(&ctl.empty[old]));
+                        if (more) put_x(i, s1[i]);
+                    });
+                };
+                bool odd = more;                           // tiles 2 u and 2 u + 1 exist
+                for (uint32_t u = 0;; ++u) {
+                    if (!first(0, u)) break;
+                    if (u > 0) {
+                        if (!second(1, u - 1)) break;
+                        odd = more;
                     }
-                    __syncwarp();
-                    if (NX == 1) {
-                        next = issue_x(0, b1);
+                    if (odd && !take2(s2[1])) break;       // C2 of tile 2 u + 1
+                    if (!second(0, u)) break;
+                    const bool even = more;                // tile 2 u + 2
+                    if (!odd) break;
+                    if (!first(1, u)) break;
+                    if (!even) {
+                        second(1, u);
+                        break;
+                    }
+                    if (!take2(s2[0])) break;
+                }
+            } else {
+                bool next = more, ahead = false;           // tile t + 1; C2 of it is there
+                for (uint32_t t = 0;; ++t) {
+                    const uint32_t i = t & 1, par = (t >> 1) & 1;
+                    uint32_t c1 = 0, c2 = i ? s2[1] : s2[0];
+                    const uint32_t old = i ? s1[1] : s1[0];
+                    bool after = false;                    // tile t + 2
+                    if (C::HAS_V) {
+                        if (!sum(ctl.p_full[i], par, 24, tmem + C::COL_V, tmem + C::COL_X + i * NCOL, c2, t > 0, [&] { umma_commit(smem_u32(&ctl.empty[c2])); })) break;
+                    }
+                    if (C::HAS_DS) {
+                        // Y of the next tile, when this one's has been read; where C2 has one slot, or C1 but two, behind the sum instead
+                        constexpr bool EARLY = C::NS2 > 1;
+                        if (EARLY && next) {
+                            if ((!ahead && !take2(c2)) || !wait(ctl.y_taken[i], par, 23)) break;
+                            if (ahead) c2 = i ? s2[0] : s2[1];
+                            tc_fence_after();
+                            if (elect_one()) put_y(i ^ 1, c2, i ? s1[0] : s1[1]);
+                            after = take1(c1);
+                            if (bad) break;
+                        }
+                        if (!sum(ctl.ds_full[i], par, 26, tmem + C::COL_S, tmem + C::COL_X + i * NCOL + C::DS_AT, old, t > 0, [&] {
+                                umma_commit(smem_u32(&ctl.empty[old]));
+                                if (EARLY && after) put_x(i, c1);
+                            })) break;
+                        if (!EARLY && next) {
+                            if (!take2(c2)) break;
+                            tc_fence_after();
+                            if (elect_one()) put_y(i ^ 1, c2, i ? s1[0] : s1[1]);
+                            after = take1(c1);
+                            if (bad) break;
+                            tc_fence_after();
+                            if (after && elect_one()) put_x(i, c1);
+                        }
+                        if (i) s2[0] = c2; else s2[1] = c2;
+                        ahead = false;
+                        if (EARLY && after) {              // C2 of the tile after next
+                            uint32_t x;
+                            if (!take2(x)) break;
+                            if (i) s2[1] = x; else s2[0] = x;
+                            ahead = true;
+                        }
+                    } else if (next) {
+                        uint32_t x;
+                        if (!take2(x)) break;              // C2 of tile t + 1
+                        if (i) s2[0] = x; else s2[1] = x;
+                        after = take1(c1);
                         if (bad) break;
+                        tc_fence_after();
+                        if (after && elect_one()) put_x(i, c1);
                     }
-                }
-                if (C::HAS_DS) {
-                    if (!wait(ctl.ds_full, t & 1, 25)) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        sum(tmem + C::COL_S, tmem + C::COL_Y, a1, t > 0);
-                        umma_commit(smem_u32(&ctl.empty[a1]));
-                    }
-                    __syncwarp();
-                    if (next && !issue_y(b2)) break;
-                }
-                if (!next) {
-                    if (elect_one()) umma_commit(smem_u32(&ctl.acc_full));
-                    __syncwarp();
-                    break;
-                }
-                a1 = b1;
-                a2 = b2;
-                if (NX == 2) {
-                    next = issue_x(i, b1);
-                    if (bad || (next && !C::HAS_DS && !take(b2, 22))) break;
+                    if (!next) break;
+                    if (i) s1[1] = c1; else s1[0] = c1;
+                    next = after;
                 }
             }
+            if (!bad && elect_one()) umma_commit(smem_u32(&ctl.acc_full));
         } while (false);
         if (bad && lane == 0) give_up(bad);
         __syncwarp();
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ P, dS, results
         reg_inc<REGS_SOFTMAX_2WG>();
-        const int half = (warp - 4) >> 2;                  // of the tile's columns
+        const int wg = (warp - 4) >> 2;                    // tiles of this parity
         const int row_in_tile = ((warp & 3) << 5) | lane;
         const int row = row_tile * 128 + row_in_tile;      // position of this thread's token
         const bool valid = row < p.n;
-        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tm = tmem + lane_base;
+        const uint32_t tm = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t t_x = tm + C::COL_X + wg * NCOL, t_y = ONE ? t_x : tm + C::COL_Y;
         const float sl2 = CAP ? p.softcap * LOG2E : p.scale * LOG2E;
         const float cap_in = CAP ? p.scale / p.softcap : 0.f;
-        float lrow = 0.f, drow = 0.f;                      // rows are queries: lse and delta of the row
+        float lrow = 0.f, drow = 0.f;                      // rows are queries: -lse log2(e) and -delta of the row
         if constexpr (!KEYS) {
             const float* st = p.stat + ((size_t)head * p.nt + row_tile) * 256 + row_in_tile;
             lrow = dep_load(st);
@@ -365,7 +500,7 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
         }
         uint32_t mask = 0;
         if (p.bits) mask = valid ? dep_load(p.row_mask + (size_t)head * p.n + row) & (0xffffffffu >> (32 - p.K)) : 0u;
-        constexpr int LDR = LD > 0 ? LD : 1;
+        constexpr int LDR = LD > 0 ? LD : 1, NW = NCOL / 32;
         float gr[LDR], dg[LDR];                            // assignment of the row times -lambda log2(e), its gradient
         if constexpr (LD > 0) {
 #pragma unroll
@@ -374,161 +509,254 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
                 dg[e] = 0.f;
             }
         }
-        RingAt<C::NINFO> taken;
-        uint32_t t = 0;
-        for (;; ++t) {
-            if (!wait(ctl.info_full[taken.slot], taken.phase, 39)) break;
-            const int ct = *(volatile int*)&ctl.tile[taken.slot];
-            if (ct < 0) break;
-            const float* const info = reinterpret_cast<const float*>(smem_raw + C::OFF_INFO + taken.slot * C::INFO_BYTES) + half * NC;
-            const float* const gcol = reinterpret_cast<const float*>(smem_raw + C::OFF_INFO + taken.slot * C::INFO_BYTES + C::STAT_BYTES) + half * NC * LDR;
-            // ---- which columns count: bit c of word c / 32
-            const int col0 = ct * NCOL + half * NC;
-            auto gate_row = [&](int c) -> const float4* {
-                return reinterpret_cast<const float4*>(C::GATE_SMEM ? gcol + c * LDR : p.g + ((size_t)b * p.n + min(col0 + c, p.n - 1)) * LDR);
+        const float* const info = reinterpret_cast<const float*>(smem_raw + C::OFF_INFO + wg * C::INFO_BYTES);
+        const float* const gcol = reinterpret_cast<const float*>(smem_raw + C::OFF_INFO + wg * C::INFO_BYTES + C::STAT_BYTES);
+        // This group's next tile, and its columns' bitmaps of the row's groups, asked for while the tile before is at work.  (The words
+        // of the first two groups are joined only when they are used.)
+        int ct = -1;
+        uint32_t w0[NW], w1[NW];
+        auto peek = [&](uint32_t k) -> bool {              // k: the how manieth tile of this group
+            const uint32_t slot = wg + 2 * (k & 1);
+            if (!wait(ctl.id_full[slot], (k >> 1) & 1, 39)) return false;
+            ct = *(volatile int*)&ctl.tile[slot];
+            const int hc = *(volatile int*)&ctl.head[slot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl.id_empty[slot]));
+#pragma unroll
+            for (int q = 0; q < NW; ++q) w0[q] = w1[q] = 0u;
+            const int lo_k = KEYS ? row_tile * 128 : ct * NCOL, hi_q = KEYS ? ct * NCOL + NCOL - 1 : row_tile * 128 + 127;
+            if (!p.bits || ct < 0 || hi_q - lo_k <= p.w) return true;
+            const uint32_t* gb = p.bits + ((size_t)(b * (KEYS ? p.Hq : p.Hkv) + hc) * p.nt + ct * NCOL / 128) * p.K * 4 + ct * NCOL % 128 / 32;
+            uint32_t rem = mask;
+            auto word = [&](uint32_t (&w)[NW], bool join) {
+                const uint32_t* x = gb + (__ffs(rem) - 1) * 4;
+                rem &= rem - 1;
+                uint32_t v[NW];
+                if constexpr (NW == 4) {
+                    const uint4 y = dep_load(reinterpret_cast<const uint4*>(x));
+                    v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w;
+                } else {
+                    const uint2 y = dep_load(reinterpret_cast<const uint2*>(x));
+                    v[0] = y.x; v[1] = y.y;
+                }
+#pragma unroll
+                for (int q = 0; q < NW; ++q) w[q] = join ? w[q] | v[q] : v[q];
             };
-            uint32_t kw[NC / 32];
-            bool masked;
-            {
-                const int lo_q = KEYS ? ct * NCOL : row_tile * 128, hi_q = KEYS ? ct * NCOL + NCOL - 1 : row_tile * 128 + 127;
-                const int lo_k = KEYS ? row_tile * 128 : ct * NCOL, hi_k = KEYS ? row_tile * 128 + 127 : ct * NCOL + NCOL - 1;
-                const bool causal = lo_q < hi_k, outside = hi_q - lo_k > p.w, far = lo_q - hi_k > p.w;
-                masked = causal || (p.bits && outside);
-                if (masked) {
-#pragma unroll
-                    for (int q = 0; q < NC / 32; ++q) kw[q] = 0xffffffffu;
-                    if (p.bits && outside) {
-#pragma unroll
-                        for (int q = 0; q < NC / 32; ++q) kw[q] = 0u;
-                        const uint32_t* gb = p.bits + ((size_t)(b * (KEYS ? p.Hq : p.Hkv) + ctl.head[taken.slot]) * p.nt + ct * NCOL / 128) * p.K * 4 + (col0 % 128) / 32;
+            if (rem) word(w0, false);
+            if (rem) word(w1, false);
 #pragma unroll 1
-                        for (uint32_t rem = mask; rem; rem &= rem - 1) {
-                            const uint32_t* x = gb + (__ffs(rem) - 1) * 4;
+            while (rem) word(w1, true);
+            return true;
+        };
+        uint32_t k = 0;
+        if (peek(0)) {
+#pragma unroll 1
+            for (; ct >= 0; ++k) {
+                const uint32_t par = k & 1;
+                const int now = ct;
+                // ---- which columns count: bit c of word c / 32
+                const int col0 = now * NCOL;
+                auto gate_row = [&](int c) -> const float4* {
+                    return reinterpret_cast<const float4*>(C::GATE_SMEM ? gcol + c * LDR : p.g + ((size_t)b * p.n + min(col0 + c, p.n - 1)) * LDR);
+                };
+                uint32_t kw[NW];
+                bool masked;
+                {
+                    const int lo_q = KEYS ? col0 : row_tile * 128, hi_q = KEYS ? col0 + NCOL - 1 : row_tile * 128 + 127;
+                    const int lo_k = KEYS ? row_tile * 128 : col0, hi_k = KEYS ? row_tile * 128 + 127 : col0 + NCOL - 1;
+                    const bool causal = lo_q < hi_k, outside = p.bits && hi_q - lo_k > p.w;
+                    masked = causal || outside;
 #pragma unroll
-                            for (int q = 0; q < NC / 32; ++q) kw[q] |= dep_load(x + q);
-                        }
-                        if (!far) {
+                    for (int q = 0; q < NW; ++q) kw[q] = outside ? w0[q] | w1[q] : 0xffffffffu;
+                    if (outside && lo_q - hi_k <= p.w) {
 #pragma unroll
-                            for (int q = 0; q < NC / 32; ++q)        // inside the window: queries up to j + w, keys from i - w on
-                                kw[q] |= KEYS ? low_bits(row - col0 - 32 * q + p.w + 1) : ~low_bits(row - p.w - col0 - 32 * q);
-                        }
+                        for (int q = 0; q < NW; ++q)             // inside the window: queries up to j + w, keys from i - w on
+                            kw[q] |= KEYS ? low_bits(row - col0 - 32 * q + p.w + 1) : ~low_bits(row - p.w - col0 - 32 * q);
                     }
                     if (causal) {
 #pragma unroll
-                        for (int q = 0; q < NC / 32; ++q) kw[q] &= KEYS ? ~low_bits(row - col0 - 32 * q) : low_bits(row + 1 - col0 - 32 * q);
+                        for (int q = 0; q < NW; ++q) kw[q] &= KEYS ? ~low_bits(row - col0 - 32 * q) : low_bits(row + 1 - col0 - 32 * q);
                     }
                 }
-            }
-            // ---- P
-            const uint32_t xb = NX == 2 ? t & 1 : 0;
-            if (!wait(ctl.x_full[xb], NX == 2 ? (t >> 1) & 1 : t & 1, 30)) break;
-            tc_fence_after();
-            const uint32_t t_x = tm + C::COL_X + xb * NCOL + half * NC, t_y = tm + C::COL_Y + half * NC;
-            float pr[NC];                                  // P times the slope of the logit
-            float da[LD > 0 ? NC : 1];                     // gate: what turns ds into the gradient of g_i . g_j
+                if (LD == 0 && masked) {
 #pragma unroll
-            for (int c = 0; c < NC; c += 32) {
-                uint32_t sr[32];
-                tmem_ld32(t_x + c, sr);
+                    for (int q = 0; q < NW; ++q) kw[q] = pair_bits(kw[q]);
+                }
+                // words of packed pairs, those that do not count set to zero
+                auto strike = [&](uint32_t (&w)[16], uint32_t bits) {
+                    if (LD == 0 && masked) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t y = bits << (7 - e);
+                            w[e] &= byte_signs<0x9988>(y);
+                            w[e + 8] &= byte_signs<0xbbaa>(y);
+                        }
+                    }
+                };
+                // ---- what comes after this tile
+                if (!peek(k + 1)) break;
+                // ---- P
+                if (C::INFO_BYTES > 0 && !wait(ctl.info_full[wg], par, 38)) break;
+                if (!wait(ctl.x_full[wg], par, 30)) break;
+                tc_fence_after();
+                uint32_t pr[NCOL];                             // X, then P times the slope of the logit
+                float da[LD > 0 ? NCOL : 1];                   // gate: what turns ds into the gradient of g_i . g_j
+#pragma unroll
+                for (int c = 0; c < NCOL; c += 32) tmem_ld32(t_x + c, *reinterpret_cast<uint32_t(*)[32]>(&pr[c]));
                 tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    float l[4];
-                    if constexpr (KEYS) *reinterpret_cast<float4*>(l) = *reinterpret_cast<const float4*>(info + c + e);
-                    else l[0] = l[1] = l[2] = l[3] = lrow;
-                    float pv[4];
+                for (int c = 0; c < NCOL; c += 32) {
+                    uint32_t pk[16];
+                    float4 lc[C::STAT_BYTES ? 8 : 1];          // (asked for together)
+                    if constexpr (C::STAT_BYTES > 0) {
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        const float x = __uint_as_float(sr[e + f]);
-                        if constexpr (LD > 0) {
-                            // sigmoid of a distant pair: 1 / (1 + z), z = exp(-lambda g_i . g_j); 1 - f = z f
-                            const int col = col0 + c + e + f;
-                            const bool distant = (KEYS ? col - row : row - col) > p.w;
-                            const float4* gc = gate_row(c + e + f);
-                            float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+                        for (int e = 0; e < 8; ++e) lc[e] = reinterpret_cast<const float4*>(info + c)[e];
+                    }
 #pragma unroll
-                            for (int k = 0; k < LD / 4; ++k) {
-                                const float4 v = gc[k];
-                                s0 = __ffma2_rn(make_float2(gr[4 * k], gr[4 * k + 1]), make_float2(v.x, v.y), s0);
-                                s1 = __ffma2_rn(make_float2(gr[4 * k + 2], gr[4 * k + 3]), make_float2(v.z, v.w), s1);
+                    for (int e = c; e < c + 32; e += 4) {
+                        float2 l[2];
+                        if constexpr (C::STAT_BYTES > 0) *reinterpret_cast<float4*>(l) = lc[(e - c) / 4];
+                        else l[0] = l[1] = make_float2(lrow, lrow);
+#pragma unroll
+                        for (int f = 0; f < 2; ++f) {
+                            uint32_t &u0 = pr[e + 2 * f], &u1 = pr[e + 2 * f + 1];
+                            float2 x = make_float2(__uint_as_float(u0), __uint_as_float(u1)), y;
+                            if constexpr (LD > 0) {
+                                float2 fac;
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    // sigmoid of a distant pair: 1 / (1 + z), z = exp(-lambda g_i . g_j); 1 - f = z f
+                                    const int at = e + 2 * f + i, col = col0 + at;
+                                    const bool distant = (KEYS ? col - row : row - col) > p.w;
+                                    const float4* gc = gate_row(at);
+                                    float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+                                    for (int q = 0; q < LD / 4; ++q) {
+                                        const float4 v = gc[q];
+                                        s0 = __ffma2_rn(make_float2(gr[4 * q], gr[4 * q + 1]), make_float2(v.x, v.y), s0);
+                                        s1 = __ffma2_rn(make_float2(gr[4 * q + 2], gr[4 * q + 3]), make_float2(v.z, v.w), s1);
+                                    }
+                                    s0 = __fadd2_rn(s0, s1);
+                                    const float z = distant ? ex2_approx(fminf(s0.x + s0.y, 126.f)) : 0.f, r = rcp_approx(1.f + z);
+                                    (i ? fac.y : fac.x) = r;
+                                    da[at] = (i ? x.y : x.x) * p.scale * p.lambda * z * r;
+                                }
+                                y = __ffma2_rn(__fmul2_rn(x, fac), make_float2(sl2, sl2), l[f]);
+                                y.x = ex2_approx(y.x);
+                                y.y = ex2_approx(y.y);
+                                if (masked) {
+                                    y.x = kw[(e + 2 * f) >> 5] >> ((e + 2 * f) & 31) & 1u ? y.x : 0.f;
+                                    y.y = kw[(e + 2 * f) >> 5] >> ((e + 2 * f + 1) & 31) & 1u ? y.y : 0.f;
+                                }
+                                x = __fmul2_rn(y, fac);
+                            } else if constexpr (CAP) {
+                                x = __fmul2_rn(x, make_float2(cap_in, cap_in));
+                                x.x = tanh_approx(x.x);
+                                x.y = tanh_approx(x.y);
+                                y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
+                                y.x = ex2_approx(y.x);
+                                y.y = ex2_approx(y.y);
+                                x = __fmul2_rn(y, __ffma2_rn(make_float2(-x.x, -x.y), x, make_float2(1.f, 1.f)));
+                            } else {
+                                if constexpr (C::AUG) y = __fmul2_rn(x, make_float2(sl2, sl2));
+                                else y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
+                                y.x = ex2_approx(y.x);
+                                y.y = ex2_approx(y.y);
+                                x = y;
                             }
-                            const float z = distant ? ex2_approx(fminf((s0.x + s0.y) + (s1.x + s1.y), 126.f)) : 0.f;
-                            const float fac = rcp_approx(1.f + z);
-                            const float y = ex2_approx(fmaf(x * fac, sl2, -l[f]));
-                            pv[f] = !masked || (kw[(c + e + f) >> 5] >> ((c + e + f) & 31) & 1u) ? y : 0.f;
-                            pr[c + e + f] = pv[f] * fac;
-                            da[c + e + f] = x * p.scale * p.lambda * z * fac;
-                        } else if constexpr (CAP) {
-                            const float th = tanh_approx(x * cap_in);
-                            const float y = ex2_approx(fmaf(th, sl2, -l[f]));
-                            pv[f] = !masked || (kw[(c + e + f) >> 5] >> ((c + e + f) & 31) & 1u) ? y : 0.f;
-                            pr[c + e + f] = pv[f] * fmaf(-th, th, 1.f);
-                        } else {
-                            const float y = ex2_approx(fmaf(x, sl2, -l[f]));
-                            pv[f] = !masked || (kw[(c + e + f) >> 5] >> ((c + e + f) & 31) & 1u) ? y : 0.f;
-                            pr[c + e + f] = pv[f];
+                            u0 = __float_as_uint(x.x);
+                            u1 = __float_as_uint(x.y);
+                            if constexpr (C::HAS_V) pk[(e - c) / 2 + f] = pack_bf16x2(y.x, y.y);
                         }
                     }
                     if constexpr (C::HAS_V) {
-                        sr[e / 2] = pack_bf16x2(pv[0], pv[1]);          // (words of this loop's earlier turns)
-                        sr[e / 2 + 1] = pack_bf16x2(pv[2], pv[3]);
+                        strike(pk, kw[c / 32]);
+                        tmem_st16(t_x + c / 2, pk);
+                        if (c + 32 == C::PART0 || c + 32 == NCOL) {
+                            tmem_wait_st();
+                            tc_fence_before();
+                            mbar_arrive(smem_u32(&ctl.p_full[wg][c + 32 == C::PART0 ? 0 : 1]));
+                        }
                     }
                 }
-                if constexpr (C::HAS_V) tmem_st16(t_x + c / 2, *reinterpret_cast<uint32_t(*)[16]>(&sr[0]));
-            }
-            if constexpr (C::HAS_V) tmem_wait_st();
-            tc_fence_before();
-            if constexpr (C::HAS_V) mbar_arrive(smem_u32(&ctl.p_full[xb]));
-            // ---- dS
-            if constexpr (C::HAS_DS) {
-                if (!wait(ctl.y_full, t & 1, 31)) break;
-                tc_fence_after();
+                // ---- dS
+                if constexpr (C::HAS_DS) {
+                    if (!wait(ctl.y_full[wg], par, 31)) break;
+                    tc_fence_after();
+                    uint32_t ya[16], yb[16];                   // two pieces of Y, the second on its way
+                    tmem_ld16(t_y, ya);
 #pragma unroll
-                for (int c = 0; c < NC; c += 32) {
-                    uint32_t sr[32];
-                    tmem_ld32(t_y + c, sr);
-                    tmem_wait_ld();
+                    for (int c = 0; c < NCOL; c += 32) {
+                        uint32_t pk[16];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        float d[4], ds[4];
-                        if constexpr (KEYS) *reinterpret_cast<float4*>(d) = *reinterpret_cast<const float4*>(info + NCOL + c + e);
-                        else d[0] = d[1] = d[2] = d[3] = drow;
+                        for (int hf = 0; hf < 2; ++hf) {
+                            tmem_wait_ld();
+                            if (hf == 0) {
+                                tmem_ld16(t_y + c + 16, yb);
+                            } else if (c + 32 < NCOL) {
+                                tmem_ld16(t_y + c + 32, ya);
+                            } else {
+                                tc_fence_before();
+                                if constexpr (!ONE) mbar_arrive(smem_u32(&ctl.y_taken[wg]));
+                            }
+                            const uint32_t (&yr)[16] = hf ? yb : ya;
+                            float4 dc[C::STAT_BYTES ? 4 : 1];
+                            if constexpr (C::STAT_BYTES > 0) {
 #pragma unroll
-                        for (int f = 0; f < 4; ++f) {
-                            ds[f] = pr[c + e + f] * (__uint_as_float(sr[e + f]) - d[f]);
-                            if constexpr (LD > 0) {
-                                const float a = ds[f] * da[c + e + f];
-                                const float4* gc = gate_row(c + e + f);
+                                for (int e = 0; e < 4; ++e) dc[e] = reinterpret_cast<const float4*>(info + NCOL + c + 16 * hf)[e];
+                            }
 #pragma unroll
-                                for (int k = 0; k < LD / 4; ++k) {
-                                    const float4 v = gc[k];
-                                    const float2 lo = __ffma2_rn(make_float2(a, a), make_float2(v.x, v.y), make_float2(dg[4 * k], dg[4 * k + 1]));
-                                    const float2 hi = __ffma2_rn(make_float2(a, a), make_float2(v.z, v.w), make_float2(dg[4 * k + 2], dg[4 * k + 3]));
-                                    dg[4 * k] = lo.x; dg[4 * k + 1] = lo.y; dg[4 * k + 2] = hi.x; dg[4 * k + 3] = hi.y;
+                            for (int e = 0; e < 16; e += 4) {
+                                const int at0 = c + 16 * hf + e;
+                                float2 d[2];
+                                if constexpr (C::STAT_BYTES > 0) *reinterpret_cast<float4*>(d) = dc[e / 4];
+                                else d[0] = d[1] = make_float2(drow, drow);
+#pragma unroll
+                                for (int f = 0; f < 2; ++f) {
+                                    const int at = at0 + 2 * f;
+                                    const float2 u = make_float2(__uint_as_float(pr[at]), __uint_as_float(pr[at + 1]));
+                                    float2 ds = make_float2(__uint_as_float(yr[e + 2 * f]), __uint_as_float(yr[e + 2 * f + 1]));
+                                    ds = __fmul2_rn(u, C::AUG ? ds : __fadd2_rn(ds, d[f]));
+                                    if constexpr (LD > 0) {
+#pragma unroll
+                                        for (int i = 0; i < 2; ++i) {
+                                            const float a = (i ? ds.y : ds.x) * da[at + i];
+                                            const float4* gc = gate_row(at + i);
+#pragma unroll
+                                            for (int q = 0; q < LD / 4; ++q) {
+                                                const float4 v = gc[q];
+                                                const float2 lo = __ffma2_rn(make_float2(a, a), make_float2(v.x, v.y), make_float2(dg[4 * q], dg[4 * q + 1]));
+                                                const float2 hi = __ffma2_rn(make_float2(a, a), make_float2(v.z, v.w), make_float2(dg[4 * q + 2], dg[4 * q + 3]));
+                                                dg[4 * q] = lo.x; dg[4 * q + 1] = lo.y; dg[4 * q + 2] = hi.x; dg[4 * q + 3] = hi.y;
+                                            }
+                                        }
+                                    }
+                                    pk[8 * hf + e / 2 + f] = pack_bf16x2(ds.x, ds.y);
                                 }
                             }
                         }
-                        sr[e / 2] = pack_bf16x2(ds[0], ds[1]);
-                        sr[e / 2 + 1] = pack_bf16x2(ds[2], ds[3]);
+                        strike(pk, kw[c / 32]);
+                        // (in the place of Y itself only behind what has been read of it)
+                        tmem_st16(t_x + C::DS_AT + c / 2, pk);
+                        if (c + 32 == C::PART0 || c + 32 == NCOL) {
+                            tmem_wait_st();
+                            tc_fence_before();
+                            mbar_arrive(smem_u32(&ctl.ds_full[wg][c + 32 == C::PART0 ? 0 : 1]));
+                        }
                     }
-                    tmem_st16(t_y + c / 2, *reinterpret_cast<uint32_t(*)[16]>(&sr[0]));
                 }
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(smem_u32(&ctl.ds_full));
+                __syncwarp();
+                if (C::INFO_BYTES > 0 && lane == 0) mbar_arrive(smem_u32(&ctl.info_empty[wg]));
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl.info_empty[taken.slot]));
-            taken.next();
         }
-        if (!bad && t > 0) wait(ctl.acc_full, 0, 40);
+        if (!bad) wait(ctl.acc_full, 0, 40);
         if (!bad) {
             tc_fence_after();
             // ---- results: BWD_KV: dV by the first four warps, dK by the others; one sum: half of its columns each
             constexpr int NOUT = MODE == BWD_KV ? D : D / 2;
-            const bool v = MODE == BWD_V || (MODE == BWD_KV && half == 0);
+            const bool v = MODE == BWD_V || (MODE == BWD_KV && wg == 0);
             const float by = v ? 1.f : p.scale;
-            const int col0 = MODE == BWD_KV ? 0 : half * NOUT;
+            const int col0 = MODE == BWD_KV ? 0 : wg * NOUT;
             const uint32_t t_a = tm + (v ? C::COL_V : C::COL_S) + col0;
             __nv_bfloat16* out = v ? p.out1 + b * p.s1b + h * p.s1h + (int64_t)(valid ? row : 0) * p.s1n : p.out2 + b * p.s2b + h * p.s2h + (int64_t)(valid ? row : 0) * p.s2n;
             const bool wide = v ? p.wide1 : p.wide2;
@@ -551,14 +779,13 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
             }
             tc_fence_before();
             if constexpr (LD > 0 && MODE != BWD_V) {
-                // the two halves of a row's columns: the second hands its sums to the first (the slots are through)
+                // the even and the odd tiles' sums: the second group hands its own to the first (the slots are through)
                 float* const x = reinterpret_cast<float*>(smem_raw + C::OFF_C) + row_in_tile;
-                if (half == 1) {
+                if (wg == 1) {
 #pragma unroll
                     for (int e = 0; e < LD; ++e) x[e * 128] = dg[e];
-                }
-                if (half == 1) mbar_arrive(smem_u32(&ctl.dg_full));
-                if (half == 0 && wait(ctl.dg_full, 0, 41) && valid) {
+                    mbar_arrive(smem_u32(&ctl.dg_full));
+                } else if (wait(ctl.dg_full, 0, 41) && valid) {
 #pragma unroll
                     for (int e = 0; e < LD; e += 4)
                         *reinterpret_cast<float4*>(p.dg_part + ((size_t)head * p.n + row) * LD + e) =
@@ -582,7 +809,7 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
 
 template <int D, int MODE, bool CAP, int LD>
 static int launch_bwd_pass(const AttnBwdArgs& a, const BwdParams& p, cudaStream_t st) {
-    using C = BwdCfg<D, MODE, LD>;
+    using C = BwdCfg<D, MODE, CAP, LD>;
     const int B = a.s.batch, n = a.s.n;
     const focus_tensor &r1 = C::KEYS ? a.k : a.q, &r2 = C::KEYS ? a.v : a.dO, &c1 = C::KEYS ? a.q : a.k, &c2 = C::KEYS ? a.dO : a.v;
     const int HR = C::KEYS ? a.s.Hkv : a.s.Hq, HC = C::KEYS ? a.s.Hq : a.s.Hkv;

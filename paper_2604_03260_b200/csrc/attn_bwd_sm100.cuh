@@ -1,17 +1,18 @@
 // The passes of the attention's backward: one CTA per (head, 128 rows), its tiles of columns one after another.
-//   warp 0        TMA: the two row tiles once, then both column tiles of every visited tile into a ring of slots (128-byte swizzle)
-//   warp 1        MMA issuer: X = R1 C1^T, Y = R2 C2^T (operands in shared memory), then the sums with P or dS (bf16, tensor memory) as the
-//                 first operand and C2 or C1 read along its other dimension as the second
-//   warp 2        what the others need to know of the visited tiles: number and head; lse, delta and assignments of the columns
+//   warp 0        TMA: the two row tiles once, then C1 of every visited tile into a ring of slots (128-byte swizzle); the tiles' numbers
+//   warp 3        C2 of every tile into another ring; lse, delta and assignments of the columns
+//   warps 1, 2    MMA issuers: X = R1 C1^T, Y = R2 C2^T (operands in shared memory), and the sums with P or dS (bf16, tensor memory) as the
+//                 first operand and C2 or C1 read along its other dimension as the second.  Warp 1 what C2 is for, warp 2 what C1 is for.
+//                 (One warp for both: 2360 cycles a tile of dQ at D = 128 with nothing else to wait for, where the products take 1630: a wait and
+//                 what comes with it is some 150 cycles even where it need not wait, and what has been issued before lasts little longer.)
 //   warps 4-7     P = exp2(X - lse), dS = P (Y - delta) of the even tiles, a thread a row
 //   warps 8-11    of the odd ones
 // The tensor pipe works in order, so a product may be issued into the place of an operand that an earlier one reads.  Two tiles are at work
 // at a time: while one group of warps takes exponentials the other waits for, or works on, the other tile's products.  With both groups on
 // the halves of one tile a tile took the sum of what both phases wait for (D = 128: 3300 and 2650 cycles for the two passes).
 //
-// Tensor memory: the sums, and three places X0, X1, Y in turn -- P goes to the first half of its X, dS to the second (with one sum: the
-// first), so that Y is free for the next tile as soon as it has been read.  Where two sums of 128 columns leave room for two places
-// only (BWD_KV at D = 128) a tile has one: X, P, then Y when the sum with P has been issued, then dS.
+// Tensor memory: the sums, and two or three places for the tiles at work.  A tile has one place: X, P over it, Y when X (and the sum with P)
+// is through, dS over that.  With three places the X of a group's next tile is there before it is done with the one before.
 #pragma once
 
 #include "attn_bwd.cuh"
@@ -52,7 +53,7 @@ struct BwdCfg {
     // Columns of a tile, all of them one thread's: 128 probabilities in registers; with the gate two numbers a pair are held, so 64, and at
     // D = 256 the row tiles leave no room for wider ones
     static constexpr int NCOL = D == 256 || LD > 0 ? 64 : 128;
-    static constexpr bool ONE_PLACE = MODE == BWD_KV && D == 128 && NCOL == 128;        // X and Y of a tile in the same place
+    static constexpr int NPL = (MODE == BWD_KV && D == 128 && NCOL == 128) || (D == 256 && HAS_DS) ? 2 : 3;       // places (as many as fit; at D = 256 as many slots fit)
     static constexpr int SUBT = D / 64;
     static constexpr uint32_t SUBR = 128 * 128, SUBC = NCOL * 128;
     static constexpr uint32_t R_BYTES = SUBR * SUBT, C_BYTES = SUBC * SUBT;
@@ -61,7 +62,7 @@ struct BwdCfg {
     // each, 24 bits), which one more 16-deep step of X and of Y, against rows of ones, adds to the products; a thread then needs nothing that
     // goes by the column.  Not where a cap or a gate comes between the product and lse, nor where shared memory has no room for it (D = 128,
     // dK at D = 256); there they are copied to shared memory and read.
-    static constexpr bool AUG = KEYS && !CAP && LD == 0 && !ONE_PLACE && !(D == 256 && MODE == BWD_K);
+    static constexpr bool AUG = KEYS && !CAP && LD == 0 && !(D == 128 && MODE == BWD_KV) && !(D == 256 && MODE == BWD_K);
     static constexpr uint32_t AUG_BYTES = AUG ? NCOL * 16 : 0, CONST_BYTES = AUG ? 4 * 2048 : 0;        // (ones for X, zeros, ones for Y, zeros)
     static constexpr uint32_t C1_BYTES = C_BYTES + AUG_BYTES;
     static constexpr uint32_t STAT_BYTES = KEYS && !AUG ? 2 * NCOL * 4 : 0;
@@ -71,28 +72,29 @@ struct BwdCfg {
     static constexpr uint32_t INFO_BYTES = STAT_BYTES + GATE_BYTES;               // one tile; two of them
     static constexpr uint32_t CTL_BYTES = 1024;
     static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - 2 * INFO_BYTES - CONST_BYTES;
-    // C1 of a tile is held from its X to its sum with dS, two tiles later, C2 for a product or two rings of their own, the larger for C1
+    // C1 of a tile is held from its X to its sum with dS, NPL tiles later, C2 for a product or two: rings of their own
     static constexpr int NFIT = ROOM / C1_BYTES > 8 ? 8 : ROOM / C1_BYTES;
-    static constexpr int NS2 = NFIT / 2, NS1 = NFIT - NS2, NSLOT = NS1 + NS2;
-    static_assert(NS2 >= 1 && NS1 >= 2 && (!HAS_DS || NS1 >= 3 || (NS2 == 1 && !ONE_PLACE)), "two tiles at work");
+    static constexpr int NS1 = MODE == BWD_V ? NFIT - NFIT / 2 : NFIT > NPL + 1 ? (NFIT + 1 > 2 * (NPL + 1) ? (NFIT + 1) / 2 : NPL + 1) : NFIT - 1;
+    static constexpr int NS2 = NFIT - NS1, NSLOT = NFIT;
+    static constexpr bool EARLY = MODE == BWD_V || NS1 > NPL;    // C1 of the tile after next can be there before the sum with dS frees a slot
+    static_assert(NS2 >= 1 && NS1 >= 2 && (EARLY || NS1 == NPL), "two tiles at work");
     static constexpr int P_PARTS = LD == 0 && KEYS ? 2 : 1;      // parts in which P and dS are handed over: most of a sum runs while the last are worked out
     static constexpr int PART0 = P_PARTS == 1 ? NCOL : NCOL == 128 ? 96 : 32;     // columns of the first
     static constexpr uint32_t OFF_C = NR * R_BYTES, OFF_CONST = OFF_C + NS1 * C1_BYTES + NS2 * C_BYTES, OFF_INFO = OFF_CONST + CONST_BYTES;
     static constexpr uint32_t OFF_CTL = OFF_INFO + 2 * INFO_BYTES, SMEM = OFF_CTL + CTL_BYTES;
     static __device__ __forceinline__ uint32_t slot_at(uint32_t s) { return s < NS1 ? s * C1_BYTES : NS1 * C1_BYTES + (s - NS1) * C_BYTES; }
-    static constexpr uint32_t COL_X = 0, COL_Y = 2 * NCOL, COL_V = NCOL == 64 || ONE_PLACE || MODE == BWD_V ? 256 : 384, COL_S = MODE == BWD_KV ? COL_V + D : COL_V;
-    static_assert(COL_S + D <= 512, "tensor memory");
-    static constexpr uint32_t DS_AT = HAS_V && !ONE_PLACE ? NCOL / 2 : 0;         // of dS in the place of X
+    static constexpr uint32_t COL_V = NPL * NCOL > 256 ? 384 : 256, COL_S = MODE == BWD_KV ? COL_V + D : COL_V;
+    static_assert(NPL * NCOL <= COL_V && COL_S + D <= 512, "tensor memory");
 };
 
 struct BwdCtl {
     uint64_t r_full, acc_full, dg_full, full[8], empty[8];      // slots of C1, then of C2
     uint64_t id_full[4], id_empty[4];             // numbers of the tiles
     uint64_t info_full[2], info_empty[2];         // what else there is of a tile
-    uint64_t x_full[2], p_full[2][2], y_full[2], y_taken[2], ds_full[2][2];       // by the tile's parity (and part)
+    uint64_t x_full[3], x_taken[3], p_full[3][2], y_full[3], ds_full[3][2];       // by the tile's place (and part)
     uint32_t limit, tmem_base;
     int abort_flag;
-    int more[8];                  // of a slot with C1: whether there is a tile at all
+    int more[8];                  // of a slot: whether there is a tile at all
     int tile[4], head[4];         // column tile and its head; tile -1: no more
 };
 static_assert(sizeof(BwdCtl) <= 1024, "CTL_BYTES");
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1)
 attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant__ CUtensorMap tm_r2, const __grid_constant__ CUtensorMap tm_c1,
                 const __grid_constant__ CUtensorMap tm_c2, const __grid_constant__ BwdParams p) {
     using C = BwdCfg<D, MODE, CAP, LD>;
-    constexpr bool KEYS = C::KEYS, ONE = C::ONE_PLACE;
+    constexpr bool KEYS = C::KEYS;
     constexpr int NCOL = C::NCOL;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     BwdCtl& ctl = *reinterpret_cast<BwdCtl*>(smem_raw + C::OFF_CTL);
@@ -185,17 +187,19 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
     }
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&ctl.r_full), 1);
-        mbar_init(smem_u32(&ctl.acc_full), 1);
+        mbar_init(smem_u32(&ctl.acc_full), (C::HAS_V ? 1 : 0) + (C::HAS_DS ? 1 : 0));
         mbar_init(smem_u32(&ctl.dg_full), 128);
         for (int s = 0; s < C::NSLOT; ++s) { mbar_init(smem_u32(&ctl.full[s]), 1); mbar_init(smem_u32(&ctl.empty[s]), 1); }
         for (int x = 0; x < 4; ++x) { mbar_init(smem_u32(&ctl.id_full[x]), 1); mbar_init(smem_u32(&ctl.id_empty[x]), 4); }
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&ctl.info_full[x]), 1);
             mbar_init(smem_u32(&ctl.info_empty[x]), 4);             // (the four warps of a tile)
+        }
+        for (int x = 0; x < C::NPL; ++x) {
             mbar_init(smem_u32(&ctl.x_full[x]), 1);
-            for (int q = 0; q < 2; ++q) { mbar_init(smem_u32(&ctl.p_full[x][q]), 128); mbar_init(smem_u32(&ctl.ds_full[x][q]), 128); }
+            mbar_init(smem_u32(&ctl.x_taken[x]), 128);
             mbar_init(smem_u32(&ctl.y_full[x]), 1);
-            mbar_init(smem_u32(&ctl.y_taken[x]), 128);
+            for (int q = 0; q < 2; ++q) { mbar_init(smem_u32(&ctl.p_full[x][q]), 128); mbar_init(smem_u32(&ctl.ds_full[x][q]), 128); }
         }
         ctl.abort_flag = 0;
         ctl.limit = wait_limit(4000000000ull);
@@ -223,10 +227,11 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
     dep_trigger();
 
     if (warp < 4) reg_dec<REGS_CONTROL>();
-    if (warp == 0) {
-        // ------------------------------------------------------------------ TMA: row tiles, column tiles
+    if (warp == 0 || warp == 3) {
+        // ------------------------------------------------------------------ TMA: row tiles, C1 and the tiles' numbers; C2 and what goes by the column
+        const bool one = warp == 0;
         const int hk = KEYS ? h : h / p.G;
-        if (lane == 0) {
+        if (one && lane == 0) {
             mbar_arrive_expect_tx(smem_u32(&ctl.r_full), C::NR * C::R_BYTES);
 #pragma unroll 1
             for (int c = 0; c < C::SUBT; ++c) {
@@ -235,95 +240,75 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
             }
         }
         BwdWalk<KEYS, NCOL> walk(p, lane, row_tile, b, h);
-        RingAt<C::NS1> ring1;
-        RingAt<C::NS2> ring2;
+        const CUtensorMap* const map = one ? &tm_c1 : &tm_c2;
+        const uint32_t slot0 = one ? 0 : C::NS1, slots = one ? C::NS1 : C::NS2;
+        uint32_t slot = 0, phase = 0;
+        RingAt<4> id;
+        RingAt<2> info;
+        // The numbers go ahead of the tiles: a group asks for its next one when it begins with a tile, and C1 of that may have to wait for it
+        BwdWalk<KEYS, NCOL> ahead(p, lane, row_tile, b, h);
+        int ends = one ? 0 : 2;
+        auto hand_id = [&]() -> bool {
+            if (ends == 2) return true;
+            const int t = ends ? -1 : ahead.next();
+            if (t < 0) ++ends;                                      // (a last one for each group of warps)
+            if (!wait(ctl.id_empty[id.slot], id.phase ^ 1, 13)) return false;
+            if (lane == 0) {
+                ctl.tile[id.slot] = t;
+                ctl.head[id.slot] = KEYS ? h * p.G + ahead.hi : hk;
+                mbar_arrive(smem_u32(&ctl.id_full[id.slot]));
+            }
+            __syncwarp();
+            id.next();
+            return true;
+        };
+        for (int x = 0; x < 3; ++x) hand_id();
         for (;;) {
             const int t = walk.next();
             const int hc = KEYS ? h * p.G + walk.hi : hk;           // head of the columns
-            auto load = [&](uint32_t slot, uint32_t phase, const CUtensorMap* map, bool first) -> bool {
-                if (!wait(ctl.empty[slot], phase ^ 1, 11)) return false;
-                if (lane == 0) {
-                    const uint32_t bar = smem_u32(&ctl.full[slot]);
-                    if (first) ctl.more[slot] = t >= 0;
-                    if (t < 0) {
-                        mbar_arrive(bar);
-                    } else {
-                        const uint32_t at = base + C::OFF_C + C::slot_at(slot);
-                        mbar_arrive_expect_tx(bar, first ? C::C1_BYTES : C::C_BYTES);
+            if (!hand_id() || !wait(ctl.empty[slot0 + slot], phase ^ 1, 11)) break;
+            if (lane == 0) {
+                const uint32_t bar = smem_u32(&ctl.full[slot0 + slot]), at = base + C::OFF_C + C::slot_at(slot0 + slot);
+                ctl.more[slot0 + slot] = t >= 0;
+                if (t < 0) {
+                    mbar_arrive(bar);
+                } else {
+                    mbar_arrive_expect_tx(bar, one ? C::C1_BYTES : C::C_BYTES);
 #pragma unroll
-                        for (int c = 0; c < C::SUBT; ++c) tma_load_4d(at + c * C::SUBC, map, bar, c * 64, t * NCOL, hc, b);
-                        if (C::AUG && first)
-                            bulk_load(at + C::C_BYTES, p.aug + (((size_t)(b * p.Hq + hc) * p.nt + t * NCOL / 128) * 128 + t * NCOL % 128) * 8, C::AUG_BYTES, bar);
-                    }
+                    for (int c = 0; c < C::SUBT; ++c) tma_load_4d(at + c * C::SUBC, map, bar, c * 64, t * NCOL, hc, b);
+                    if (C::AUG && one)
+                        bulk_load(at + C::C_BYTES, p.aug + (((size_t)(b * p.Hq + hc) * p.nt + t * NCOL / 128) * 128 + t * NCOL % 128) * 8, C::AUG_BYTES, bar);
                 }
-                __syncwarp();
-                return true;
-            };
-            if (!load(ring1.slot, ring1.phase, &tm_c1, true) || t < 0) break;
-            ring1.next();
-            if (!load(C::NS1 + ring2.slot, ring2.phase, &tm_c2, false)) break;
-            ring2.next();
-        }
-        if (bad && lane == 0) give_up(bad);
-        __syncwarp();
-    } else if (warp == 2) {
-        // ------------------------------------------------------------------ what the other warps need to know of a tile
-        const int hk = KEYS ? h : h / p.G;
-        BwdWalk<KEYS, NCOL> walk(p, lane, row_tile, b, h);
-        RingAt<4> id;
-        RingAt<2> info;
-        // A tile's number is handed on up to four tiles ahead, the rest when its place is free, which is two tiles behind: so the tiles
-        // are walked one ahead of what is copied
-        int t = walk.next(), ends = 0;
-        int held = -1, held_head = 0;            // tile whose number has been handed on, the rest not yet
-        for (;;) {
-            const int hc = KEYS ? h * p.G + walk.hi : hk;
-            if (ends < 2) {
-                if (!wait(ctl.id_empty[id.slot], id.phase ^ 1, 13)) break;
-                if (lane == 0) {
-                    ctl.tile[id.slot] = t;
-                    ctl.head[id.slot] = hc;
-                    mbar_arrive(smem_u32(&ctl.id_full[id.slot]));
-                }
-                __syncwarp();
-                id.next();
-                if (t < 0) ++ends;               // (a last one for each group of warps)
             }
-            if (C::INFO_BYTES > 0 && held >= 0) {
+            __syncwarp();
+            if (!one && C::INFO_BYTES > 0 && t >= 0) {
                 if (!wait(ctl.info_empty[info.slot], info.phase ^ 1, 12)) break;
                 if (lane == 0) {
                     const uint32_t bar = smem_u32(&ctl.info_full[info.slot]), at = base + C::OFF_INFO + info.slot * C::INFO_BYTES;
-                    const int rows = min(NCOL, p.n - held * NCOL);    // (a half tile may lie past the end)
+                    const int rows = min(NCOL, p.n - t * NCOL);       // (a half tile may lie past the end)
                     const uint32_t gbytes = C::GATE_SMEM && rows > 0 ? (uint32_t)rows * LD * 4 : 0u;
                     if (C::STAT_BYTES + gbytes == 0) mbar_arrive(bar); else mbar_arrive_expect_tx(bar, C::STAT_BYTES + gbytes);
-                    if constexpr (KEYS) {
-                        const float* st = p.stat + ((size_t)(b * p.Hq + held_head) * p.nt + held * NCOL / 128) * 256 + held * NCOL % 128;
+                    if constexpr (C::STAT_BYTES > 0) {
+                        const float* st = p.stat + ((size_t)(b * p.Hq + hc) * p.nt + t * NCOL / 128) * 256 + t * NCOL % 128;
                         bulk_load(at, st, NCOL * 4, bar);
                         bulk_load(at + NCOL * 4, st + 128, NCOL * 4, bar);
                     }
-                    if (gbytes) bulk_load(at + C::STAT_BYTES, p.g + ((size_t)b * p.n + (size_t)held * NCOL) * (LD > 0 ? LD : 1), gbytes, bar);
+                    if (gbytes) bulk_load(at + C::STAT_BYTES, p.g + ((size_t)b * p.n + (size_t)t * NCOL) * (LD > 0 ? LD : 1), gbytes, bar);
                 }
                 __syncwarp();
                 info.next();
             }
-            held = t;
-            held_head = hc;
-            if (t < 0) {
-                if (ends >= 2) break;
-            } else {
-                t = walk.next();
-            }
+            if (t < 0) break;
+            if (++slot == slots) { slot = 0; phase ^= 1; }
         }
         if (bad && lane == 0) give_up(bad);
         __syncwarp();
-    } else if (warp == 1) {
-        // ------------------------------------------------------------------ MMA issuer
+    } else if (warp < 4) {
+        // ------------------------------------------------------------------ MMA issuers
         constexpr uint32_t IDESC_X = idesc_bf16(128, NCOL, 0, 0), IDESC_A = idesc_bf16(128, D, 0, 1);
         const uint32_t r1 = (uint32_t)smem_desc_sw128(base, 16, 1024), r2 = r1 + (C::R_BYTES >> 4);
         const uint32_t ck = (uint32_t)smem_desc_sw128(base + C::OFF_C, 16, 1024);                  // columns along D
         const uint32_t cm = (uint32_t)smem_desc_sw128(base + C::OFF_C, C::SUBC, 1024);             // along the tokens
-        RingAt<C::NS1> at1;                                // slots that the next X, the next Y reads
-        RingAt<C::NS2> at2;
         // d = rows (X: R1, Y: R2) times the columns in slot `at`; `aug`: slot of the tile's C1, behind which its lse and delta are
         auto product = [&](uint32_t d, bool y, uint32_t at, uint32_t aug) {
             const uint32_t r = y ? r2 : r1, c = ck + (C::slot_at(at) >> 4);
@@ -334,30 +319,13 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
                 umma_ss(d, smem_desc_plain(ones, 2048, 128), smem_desc_plain(x, base + C::OFF_CONST + 2048 - x, 128), IDESC_X, 1);
             }
         };
-        // the slot with C1 of the next tile; false: there is none (or `bad`)
-        auto take1 = [&](uint32_t& c1) -> bool {
-            c1 = at1.slot;
-            if (!wait(ctl.full[c1], at1.phase, 21)) return false;
-            if (!*(volatile int*)&ctl.more[c1]) return false;
-            at1.next();
-            return true;
-        };
-        auto take2 = [&](uint32_t& c2) -> bool {
-            c2 = C::NS1 + at2.slot;
-            if (!wait(ctl.full[c2], at2.phase, 22)) return false;
-            at2.next();
-            return true;
-        };
+        // a slot of either ring is waited for; false: there is no such tile (or `bad`)
+        auto take = [&](uint32_t slot, uint32_t phase) -> bool { return wait(ctl.full[slot], phase, 21) && *(volatile int*)&ctl.more[slot]; };
         // (by the elected lane)
-        auto put_x = [&](uint32_t i, uint32_t c1) {
-            product(tmem + C::COL_X + i * NCOL, false, c1, c1);
-            umma_commit(smem_u32(&ctl.x_full[i]));
+        auto put_x = [&](uint32_t place, uint32_t c1) {
+            product(tmem + place * NCOL, false, c1, c1);
+            umma_commit(smem_u32(&ctl.x_full[place]));
             if (!C::HAS_DS) umma_commit(smem_u32(&ctl.empty[c1]));
-        };
-        auto put_y = [&](uint32_t i, uint32_t c2, uint32_t c1) {
-            product(tmem + (ONE ? C::COL_X + i * NCOL : C::COL_Y), true, c2, c1);
-            umma_commit(smem_u32(&ctl.y_full[i]));
-            if (!C::HAS_V || ONE) umma_commit(smem_u32(&ctl.empty[c2]));
         };
         // a sum's steps, part by part as the first operand (at `a`) comes; then what `last` issues
         auto sum = [&](uint64_t (&bars)[2], uint32_t parity, int where, uint32_t d, uint32_t a, uint32_t at, bool more, auto last) -> bool {
@@ -375,109 +343,81 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
             }
             return true;
         };
-        // by the parity of a tile: the slots of its C1 and C2.  The slots that a step will read are waited for ahead of it, while the
-        // products before it run: a wait takes some 120 cycles even where it need not wait, and what has been issued lasts little longer.
-        uint32_t s1[2] = {0, 0}, s2[2] = {0, 0};
+        // The steps of a tile.  Warp 2: X; when dS is there, the sum with it, then X of the tile that has the place next.  Warp 1: when P is
+        // there (with dS alone: when X has been read), the sum with it, then Y into the same place.  dV alone (no Y) is all warp 1's, since an
+        // X has to come behind the sum whose place it takes.  Each sum is one warp's, and so in order.
+        RingAt<C::NS1> at1, done1;                         // slots of C1: of the next X; of the next sum with dS, or the next Y (its lse and delta)
+        RingAt<C::NS2> at2;                                // slots of C2
+        RingAt<C::NPL> pl;                                 // place of the tile at work, parity of its use
+        bool more = true;                                  // the last tile that X was asked for was there
+        int left = 0;                                      // X's issued whose sum has not been
+        auto first_x = [&]() -> bool {
+#pragma unroll 1
+            for (int x = 0; x < C::NPL; ++x) {             // (every item has its diagonal tile)
+                more = take(at1.slot, at1.phase);
+                if (!more) break;
+                tc_fence_after();
+                if (elect_one()) put_x(x, at1.slot);
+                at1.next();
+                ++left;
+            }
+            return !bad;
+        };
         do {
             if (!wait(ctl.r_full, 0, 20)) break;
-            if (!take1(s1[0])) break;                      // (every item has its diagonal tile)
             tc_fence_after();
-            if (elect_one()) put_x(0, s1[0]);
-            if (!take2(s2[0])) break;
-            if (C::HAS_DS && !ONE && elect_one()) put_y(0, s2[0], s1[0]);
-            bool more = take1(s1[1]);                      // X of the last tile asked for has been issued
-            if (bad) break;
-            if (more && elect_one()) put_x(1, s1[1]);
-            if constexpr (ONE) {
-                // first step of a tile: sum with P, then Y into the same place; second: sum with dS, then X of the tile after next.  The
-                // order lets the other group's step run while a group is at work: even first, odd second, even second, odd first
-                auto first = [&](int i, uint32_t u) -> bool {          // u: tiles of this parity before
-                    return sum(ctl.p_full[i], u & 1, 24, tmem + C::COL_V, tmem + C::COL_X + i * NCOL, s2[i], i > 0 || u > 0, [&] { put_y(i, s2[i], s1[i]); });
-                };
-                auto second = [&](int i, uint32_t u) -> bool {
-                    const uint32_t old = s1[i];
-                    if (more) more = take1(s1[i]);
-                    if (bad) return false;
-                    return sum(ctl.ds_full[i], u & 1, 26, tmem + C::COL_S, tmem + C::COL_X + i * NCOL, old, i > 0 || u > 0, [&] {
-                        umma_commit(smem_u32(&ctl.empty[old]));
-                        if (more) put_x(i, s1[i]);
-                    });
-                };
-                bool odd = more;                           // tiles 2 u and 2 u + 1 exist
-                for (uint32_t u = 0;; ++u) {
-                    if (!first(0, u)) break;
-                    if (u > 0) {
-                        if (!second(1, u - 1)) break;
-                        odd = more;
-                    }
-                    if (odd && !take2(s2[1])) break;       // C2 of tile 2 u + 1
-                    if (!second(0, u)) break;
-                    const bool even = more;                // tile 2 u + 2
-                    if (!odd) break;
-                    if (!first(1, u)) break;
-                    if (!even) {
-                        second(1, u);
-                        break;
-                    }
-                    if (!take2(s2[0])) break;
-                }
-            } else {
-                bool next = more, ahead = false;           // tile t + 1; C2 of it is there
-                for (uint32_t t = 0;; ++t) {
-                    const uint32_t i = t & 1, par = (t >> 1) & 1;
-                    uint32_t c1 = 0, c2 = i ? s2[1] : s2[0];
-                    const uint32_t old = i ? s1[1] : s1[0];
-                    bool after = false;                    // tile t + 2
-                    if (C::HAS_V) {
-                        if (!sum(ctl.p_full[i], par, 24, tmem + C::COL_V, tmem + C::COL_X + i * NCOL, c2, t > 0, [&] { umma_commit(smem_u32(&ctl.empty[c2])); })) break;
-                    }
-                    if (C::HAS_DS) {
-                        // Y of the next tile, when this one's has been read; where C2 has one slot, or C1 but two, behind the sum instead
-                        constexpr bool EARLY = C::NS2 > 1;
-                        if (EARLY && next) {
-                            if ((!ahead && !take2(c2)) || !wait(ctl.y_taken[i], par, 23)) break;
-                            if (ahead) c2 = i ? s2[0] : s2[1];
-                            tc_fence_after();
-                            if (elect_one()) put_y(i ^ 1, c2, i ? s1[0] : s1[1]);
-                            after = take1(c1);
-                            if (bad) break;
-                        }
-                        if (!sum(ctl.ds_full[i], par, 26, tmem + C::COL_S, tmem + C::COL_X + i * NCOL + C::DS_AT, old, t > 0, [&] {
-                                umma_commit(smem_u32(&ctl.empty[old]));
-                                if (EARLY && after) put_x(i, c1);
-                            })) break;
-                        if (!EARLY && next) {
-                            if (!take2(c2)) break;
-                            tc_fence_after();
-                            if (elect_one()) put_y(i ^ 1, c2, i ? s1[0] : s1[1]);
-                            after = take1(c1);
-                            if (bad) break;
-                            tc_fence_after();
-                            if (after && elect_one()) put_x(i, c1);
-                        }
-                        if (i) s2[0] = c2; else s2[1] = c2;
-                        ahead = false;
-                        if (EARLY && after) {              // C2 of the tile after next
-                            uint32_t x;
-                            if (!take2(x)) break;
-                            if (i) s2[1] = x; else s2[0] = x;
-                            ahead = true;
-                        }
-                    } else if (next) {
-                        uint32_t x;
-                        if (!take2(x)) break;              // C2 of tile t + 1
-                        if (i) s2[0] = x; else s2[1] = x;
-                        after = take1(c1);
+            if (warp == 2) {
+                if (!C::HAS_DS || !first_x()) break;
+                for (bool begun = false; left > 0; begun = true) {
+                    if (C::EARLY && more) more = take(at1.slot, at1.phase);
+                    if (bad) break;
+                    if (!sum(ctl.ds_full[pl.slot], pl.phase, 26, tmem + C::COL_S, tmem + pl.slot * NCOL, done1.slot, begun, [&] {
+                            umma_commit(smem_u32(&ctl.empty[done1.slot]));
+                            if (C::EARLY && more) put_x(pl.slot, at1.slot);
+                        })) break;
+                    if (!C::EARLY && more) {
+                        more = take(at1.slot, at1.phase);
                         if (bad) break;
                         tc_fence_after();
-                        if (after && elect_one()) put_x(i, c1);
+                        if (more && elect_one()) put_x(pl.slot, at1.slot);
                     }
-                    if (!next) break;
-                    if (i) s1[1] = c1; else s1[0] = c1;
-                    next = after;
+                    if (more) at1.next(); else --left;
+                    pl.next();
+                    done1.next();
                 }
+                if (!bad && elect_one()) umma_commit(smem_u32(&ctl.acc_full));
+            } else {
+                if (!C::HAS_DS && !first_x()) break;
+                for (bool begun = false;; begun = true) {
+                    const uint32_t c2 = C::NS1 + at2.slot;
+                    if (!take(c2, at2.phase)) break;
+                    if (!C::HAS_DS && more) more = take(at1.slot, at1.phase);
+                    if (bad) break;
+                    auto put_y = [&] {
+                        product(tmem + pl.slot * NCOL, true, c2, done1.slot);
+                        umma_commit(smem_u32(&ctl.y_full[pl.slot]));
+                    };
+                    if constexpr (C::HAS_V) {
+                        if (!sum(ctl.p_full[pl.slot], pl.phase, 24, tmem + C::COL_V, tmem + pl.slot * NCOL, c2, begun, [&] {
+                                if (C::HAS_DS) put_y();
+                                umma_commit(smem_u32(&ctl.empty[c2]));
+                                if (!C::HAS_DS && more) put_x(pl.slot, at1.slot);
+                            })) break;
+                        if (!C::HAS_DS && more) at1.next();
+                    } else {
+                        if (!wait(ctl.x_taken[pl.slot], pl.phase, 23)) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            put_y();
+                            umma_commit(smem_u32(&ctl.empty[c2]));
+                        }
+                    }
+                    at2.next();
+                    pl.next();
+                    done1.next();
+                }
+                if (C::HAS_V && !bad && elect_one()) umma_commit(smem_u32(&ctl.acc_full));
             }
-            if (!bad && elect_one()) umma_commit(smem_u32(&ctl.acc_full));
         } while (false);
         if (bad && lane == 0) give_up(bad);
         __syncwarp();
@@ -489,7 +429,6 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
         const int row = row_tile * 128 + row_in_tile;      // position of this thread's token
         const bool valid = row < p.n;
         const uint32_t tm = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t t_x = tm + C::COL_X + wg * NCOL, t_y = ONE ? t_x : tm + C::COL_Y;
         const float sl2 = CAP ? p.softcap * LOG2E : p.scale * LOG2E;
         const float cap_in = CAP ? p.scale / p.softcap : 0.f;
         float lrow = 0.f, drow = 0.f;                      // rows are queries: -lse log2(e) and -delta of the row
@@ -548,11 +487,11 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
             while (rem) word(w1, true);
             return true;
         };
-        uint32_t k = 0;
+        uint32_t k = 0, place = wg, par = 0;               // the tile's place, the parity of its use
         if (peek(0)) {
 #pragma unroll 1
             for (; ct >= 0; ++k) {
-                const uint32_t par = k & 1;
+                const uint32_t t_x = tm + place * NCOL;
                 const int now = ct;
                 // ---- which columns count: bit c of word c / 32
                 const int col0 = now * NCOL;
@@ -596,14 +535,18 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
                 // ---- what comes after this tile
                 if (!peek(k + 1)) break;
                 // ---- P
-                if (C::INFO_BYTES > 0 && !wait(ctl.info_full[wg], par, 38)) break;
-                if (!wait(ctl.x_full[wg], par, 30)) break;
+                if (C::INFO_BYTES > 0 && !wait(ctl.info_full[wg], k & 1, 38)) break;
+                if (!wait(ctl.x_full[place], par, 30)) break;
                 tc_fence_after();
                 uint32_t pr[NCOL];                             // X, then P times the slope of the logit
                 float da[LD > 0 ? NCOL : 1];                   // gate: what turns ds into the gradient of g_i . g_j
 #pragma unroll
                 for (int c = 0; c < NCOL; c += 32) tmem_ld32(t_x + c, *reinterpret_cast<uint32_t(*)[32]>(&pr[c]));
                 tmem_wait_ld();
+                if constexpr (!C::HAS_V) {
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&ctl.x_taken[place]));
+                }
 #pragma unroll
                 for (int c = 0; c < NCOL; c += 32) {
                     uint32_t pk[16];
@@ -675,16 +618,16 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
                         if (c + 32 == C::PART0 || c + 32 == NCOL) {
                             tmem_wait_st();
                             tc_fence_before();
-                            mbar_arrive(smem_u32(&ctl.p_full[wg][c + 32 == C::PART0 ? 0 : 1]));
+                            mbar_arrive(smem_u32(&ctl.p_full[place][c + 32 == C::PART0 ? 0 : 1]));
                         }
                     }
                 }
                 // ---- dS
                 if constexpr (C::HAS_DS) {
-                    if (!wait(ctl.y_full[wg], par, 31)) break;
+                    if (!wait(ctl.y_full[place], par, 31)) break;
                     tc_fence_after();
                     uint32_t ya[16], yb[16];                   // two pieces of Y, the second on its way
-                    tmem_ld16(t_y, ya);
+                    tmem_ld16(t_x, ya);
 #pragma unroll
                     for (int c = 0; c < NCOL; c += 32) {
                         uint32_t pk[16];
@@ -692,12 +635,9 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
                         for (int hf = 0; hf < 2; ++hf) {
                             tmem_wait_ld();
                             if (hf == 0) {
-                                tmem_ld16(t_y + c + 16, yb);
+                                tmem_ld16(t_x + c + 16, yb);
                             } else if (c + 32 < NCOL) {
-                                tmem_ld16(t_y + c + 32, ya);
-                            } else {
-                                tc_fence_before();
-                                if constexpr (!ONE) mbar_arrive(smem_u32(&ctl.y_taken[wg]));
+                                tmem_ld16(t_x + c + 32, ya);
                             }
                             const uint32_t (&yr)[16] = hf ? yb : ya;
                             float4 dc[C::STAT_BYTES ? 4 : 1];
@@ -737,16 +677,18 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
                         }
                         strike(pk, kw[c / 32]);
                         // (in the place of Y itself only behind what has been read of it)
-                        tmem_st16(t_x + C::DS_AT + c / 2, pk);
+                        tmem_st16(t_x + c / 2, pk);
                         if (c + 32 == C::PART0 || c + 32 == NCOL) {
                             tmem_wait_st();
                             tc_fence_before();
-                            mbar_arrive(smem_u32(&ctl.ds_full[wg][c + 32 == C::PART0 ? 0 : 1]));
+                            mbar_arrive(smem_u32(&ctl.ds_full[place][c + 32 == C::PART0 ? 0 : 1]));
                         }
                     }
                 }
                 __syncwarp();
                 if (C::INFO_BYTES > 0 && lane == 0) mbar_arrive(smem_u32(&ctl.info_empty[wg]));
+                place += 2;
+                if (place >= C::NPL) { place -= C::NPL; par ^= 1; }
             }
         }
         if (!bad) wait(ctl.acc_full, 0, 40);

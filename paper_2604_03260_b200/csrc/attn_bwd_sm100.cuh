@@ -46,6 +46,30 @@ template <uint32_t SEL> __device__ __forceinline__ uint32_t byte_signs(uint32_t 
     return y;
 }
 
+// 16 lanes x 32 columns: thread t has of lane t/4 (words 4 j, 4 j + 1) and of lane t/4 + 8 (4 j + 2, 4 j + 3) columns 8 j + 2 (t % 4) and the next
+__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_frag(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// the same 32 columns as packed pairs, 16 columns: words 2 j of lane t/4, 2 j + 1 of lane t/4 + 8, column 4 j + t % 4
+__device__ __forceinline__ void tmem_st_pairs(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
 template <int D, int MODE, bool CAP, int LD>
 struct BwdCfg {
     static constexpr bool KEYS = MODE != BWD_Q;
@@ -53,16 +77,17 @@ struct BwdCfg {
     // Columns of a tile, all of them one thread's: 128 probabilities in registers; with the gate two numbers a pair are held, so 64, and at
     // D = 256 the row tiles leave no room for wider ones
     static constexpr int NCOL = D == 256 || LD > 0 ? 64 : 128;
-    static constexpr int NPL = (MODE == BWD_KV && D == 128 && NCOL == 128) || (D == 256 && HAS_DS) ? 2 : 3;       // places (as many as fit; at D = 256 as many slots fit)
+    static constexpr int NPL = LD > 0 || (MODE == BWD_KV && D == 128) || (D == 256 && HAS_DS) ? 2 : 3;       // places (as many as fit; at D = 256 as many slots fit)
+    static constexpr uint32_t COL_U = NPL * NCOL;                // gate: a place for each group's P times the factor
     static constexpr int SUBT = D / 64;
     static constexpr uint32_t SUBR = 128 * 128, SUBC = NCOL * 128;
     static constexpr uint32_t R_BYTES = SUBR * SUBT, C_BYTES = SUBC * SUBT;
     static constexpr int NR = MODE == BWD_V ? 1 : 2;             // row tiles
     // Rows are keys: lse and delta go by the column.  They come as six more numbers a column (-lse / scale and -delta in three bf16 terms
     // each, 24 bits), which one more 16-deep step of X and of Y, against rows of ones, adds to the products; a thread then needs nothing that
-    // goes by the column.  Not where a cap or a gate comes between the product and lse, nor where shared memory has no room for it (D = 128,
-    // dK at D = 256); there they are copied to shared memory and read.
-    static constexpr bool AUG = KEYS && !CAP && LD == 0 && !(D == 128 && MODE == BWD_KV) && !(D == 256 && MODE == BWD_K);
+    // goes by the column.  Not where a cap or a gate comes between the product and lse, nor where shared memory has no room for it (dK at
+    // D = 256); there they are copied to shared memory and read.
+    static constexpr bool AUG = KEYS && !CAP && LD == 0 && !(D == 256 && MODE == BWD_K);
     static constexpr uint32_t AUG_BYTES = AUG ? NCOL * 16 : 0, CONST_BYTES = AUG ? 4 * 2048 : 0;        // (ones for X, zeros, ones for Y, zeros)
     static constexpr uint32_t C1_BYTES = C_BYTES + AUG_BYTES;
     static constexpr uint32_t STAT_BYTES = KEYS && !AUG ? 2 * NCOL * 4 : 0;
@@ -84,7 +109,7 @@ struct BwdCfg {
     static constexpr uint32_t OFF_CTL = OFF_INFO + 2 * INFO_BYTES, SMEM = OFF_CTL + CTL_BYTES;
     static __device__ __forceinline__ uint32_t slot_at(uint32_t s) { return s < NS1 ? s * C1_BYTES : NS1 * C1_BYTES + (s - NS1) * C_BYTES; }
     static constexpr uint32_t COL_V = NPL * NCOL > 256 ? 384 : 256, COL_S = MODE == BWD_KV ? COL_V + D : COL_V;
-    static_assert(NPL * NCOL <= COL_V && COL_S + D <= 512, "tensor memory");
+    static_assert(NPL * NCOL + (LD > 0 ? 2 * NCOL : 0) <= COL_V && COL_S + D <= 512, "tensor memory");
 };
 
 struct BwdCtl {
@@ -431,21 +456,33 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
         const uint32_t tm = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const float sl2 = CAP ? p.softcap * LOG2E : p.scale * LOG2E;
         const float cap_in = CAP ? p.scale / p.softcap : 0.f;
-        float lrow = 0.f, drow = 0.f;                      // rows are queries: -lse log2(e) and -delta of the row
+        // A thread has a row.  With the gate, which needs a column's assignment for every pair, it has four rows, 8 apart, and of every 8 columns
+        // two, so that what goes by the column is read once for four rows (tensor memory gives a row a thread faster, which counts otherwise:
+        // 3390 cycles a tile of dK and dV at D = 128 with four rows, 3130 so).
+        const int l4 = lane >> 2, c2 = 2 * (lane & 3);     // row (of each 8) and first column (of each 8)
+        const int rowq = row_tile * 128 + (warp & 3) * 32 + l4;        // its rows: rowq + 8 q
+        constexpr int ROWS = LD > 0 ? 4 : 1;
+        float lrow[ROWS] = {}, drow[ROWS] = {};            // rows are queries: -lse log2(e) and -delta
         if constexpr (!KEYS) {
-            const float* st = p.stat + ((size_t)head * p.nt + row_tile) * 256 + row_in_tile;
-            lrow = dep_load(st);
-            drow = dep_load(st + 128);
+            const float* st = p.stat + ((size_t)head * p.nt + row_tile) * 256 + (LD > 0 ? (warp & 3) * 32 + l4 : row_in_tile);
+#pragma unroll
+            for (int q = 0; q < ROWS; ++q) {
+                lrow[q] = dep_load(st + 8 * q);
+                drow[q] = dep_load(st + 128 + 8 * q);
+            }
         }
         uint32_t mask = 0;
         if (p.bits) mask = valid ? dep_load(p.row_mask + (size_t)head * p.n + row) & (0xffffffffu >> (32 - p.K)) : 0u;
-        constexpr int LDR = LD > 0 ? LD : 1, NW = NCOL / 32;
-        float gr[LDR], dg[LDR];                            // assignment of the row times -lambda log2(e), its gradient
+        constexpr int LDR = LD > 0 ? LD : 1, LQ = LD > 0 ? 4 : 1, NW = NCOL / 32;
+        float gr[LQ][LDR], dg[LQ][LDR];                    // assignments of the rows times -lambda log2(e), their gradients
         if constexpr (LD > 0) {
 #pragma unroll
-            for (int e = 0; e < LD; ++e) {
-                gr[e] = valid ? dep_load(p.g + ((size_t)b * p.n + row) * LD + e) * (-p.lambda * LOG2E) : 0.f;
-                dg[e] = 0.f;
+            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                for (int e = 0; e < LD; ++e) {
+                    gr[q][e] = rowq + 8 * q < p.n ? dep_load(p.g + ((size_t)b * p.n + rowq + 8 * q) * LD + e) * (-p.lambda * LOG2E) : 0.f;
+                    dg[q][e] = 0.f;
+                }
             }
         }
         const float* const info = reinterpret_cast<const float*>(smem_raw + C::OFF_INFO + wg * C::INFO_BYTES);
@@ -538,150 +575,248 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
                 if (C::INFO_BYTES > 0 && !wait(ctl.info_full[wg], k & 1, 38)) break;
                 if (!wait(ctl.x_full[place], par, 30)) break;
                 tc_fence_after();
-                uint32_t pr[NCOL];                             // X, then P times the slope of the logit
-                float da[LD > 0 ? NCOL : 1];                   // gate: what turns ds into the gradient of g_i . g_j
+                if constexpr (LD == 0) {
+                    uint32_t pr[NCOL];                             // X, then P times the slope of the logit
 #pragma unroll
-                for (int c = 0; c < NCOL; c += 32) tmem_ld32(t_x + c, *reinterpret_cast<uint32_t(*)[32]>(&pr[c]));
-                tmem_wait_ld();
-                if constexpr (!C::HAS_V) {
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&ctl.x_taken[place]));
-                }
-#pragma unroll
-                for (int c = 0; c < NCOL; c += 32) {
-                    uint32_t pk[16];
-                    float4 lc[C::STAT_BYTES ? 8 : 1];          // (asked for together)
-                    if constexpr (C::STAT_BYTES > 0) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) lc[e] = reinterpret_cast<const float4*>(info + c)[e];
+                    for (int c = 0; c < NCOL; c += 32) tmem_ld32(t_x + c, *reinterpret_cast<uint32_t(*)[32]>(&pr[c]));
+                    tmem_wait_ld();
+                    if constexpr (!C::HAS_V) {
+                        tc_fence_before();
+                        mbar_arrive(smem_u32(&ctl.x_taken[place]));
                     }
-#pragma unroll
-                    for (int e = c; e < c + 32; e += 4) {
-                        float2 l[2];
-                        if constexpr (C::STAT_BYTES > 0) *reinterpret_cast<float4*>(l) = lc[(e - c) / 4];
-                        else l[0] = l[1] = make_float2(lrow, lrow);
-#pragma unroll
-                        for (int f = 0; f < 2; ++f) {
-                            uint32_t &u0 = pr[e + 2 * f], &u1 = pr[e + 2 * f + 1];
-                            float2 x = make_float2(__uint_as_float(u0), __uint_as_float(u1)), y;
-                            if constexpr (LD > 0) {
-                                float2 fac;
-#pragma unroll
-                                for (int i = 0; i < 2; ++i) {
-                                    // sigmoid of a distant pair: 1 / (1 + z), z = exp(-lambda g_i . g_j); 1 - f = z f
-                                    const int at = e + 2 * f + i, col = col0 + at;
-                                    const bool distant = (KEYS ? col - row : row - col) > p.w;
-                                    const float4* gc = gate_row(at);
-                                    float2 s0 = make_float2(0.f, 0.f), s1 = s0;
-#pragma unroll
-                                    for (int q = 0; q < LD / 4; ++q) {
-                                        const float4 v = gc[q];
-                                        s0 = __ffma2_rn(make_float2(gr[4 * q], gr[4 * q + 1]), make_float2(v.x, v.y), s0);
-                                        s1 = __ffma2_rn(make_float2(gr[4 * q + 2], gr[4 * q + 3]), make_float2(v.z, v.w), s1);
-                                    }
-                                    s0 = __fadd2_rn(s0, s1);
-                                    const float z = distant ? ex2_approx(fminf(s0.x + s0.y, 126.f)) : 0.f, r = rcp_approx(1.f + z);
-                                    (i ? fac.y : fac.x) = r;
-                                    da[at] = (i ? x.y : x.x) * p.scale * p.lambda * z * r;
-                                }
-                                y = __ffma2_rn(__fmul2_rn(x, fac), make_float2(sl2, sl2), l[f]);
-                                y.x = ex2_approx(y.x);
-                                y.y = ex2_approx(y.y);
-                                if (masked) {
-                                    y.x = kw[(e + 2 * f) >> 5] >> ((e + 2 * f) & 31) & 1u ? y.x : 0.f;
-                                    y.y = kw[(e + 2 * f) >> 5] >> ((e + 2 * f + 1) & 31) & 1u ? y.y : 0.f;
-                                }
-                                x = __fmul2_rn(y, fac);
-                            } else if constexpr (CAP) {
-                                x = __fmul2_rn(x, make_float2(cap_in, cap_in));
-                                x.x = tanh_approx(x.x);
-                                x.y = tanh_approx(x.y);
-                                y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
-                                y.x = ex2_approx(y.x);
-                                y.y = ex2_approx(y.y);
-                                x = __fmul2_rn(y, __ffma2_rn(make_float2(-x.x, -x.y), x, make_float2(1.f, 1.f)));
-                            } else {
-                                if constexpr (C::AUG) y = __fmul2_rn(x, make_float2(sl2, sl2));
-                                else y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
-                                y.x = ex2_approx(y.x);
-                                y.y = ex2_approx(y.y);
-                                x = y;
-                            }
-                            u0 = __float_as_uint(x.x);
-                            u1 = __float_as_uint(x.y);
-                            if constexpr (C::HAS_V) pk[(e - c) / 2 + f] = pack_bf16x2(y.x, y.y);
-                        }
-                    }
-                    if constexpr (C::HAS_V) {
-                        strike(pk, kw[c / 32]);
-                        tmem_st16(t_x + c / 2, pk);
-                        if (c + 32 == C::PART0 || c + 32 == NCOL) {
-                            tmem_wait_st();
-                            tc_fence_before();
-                            mbar_arrive(smem_u32(&ctl.p_full[place][c + 32 == C::PART0 ? 0 : 1]));
-                        }
-                    }
-                }
-                // ---- dS
-                if constexpr (C::HAS_DS) {
-                    if (!wait(ctl.y_full[place], par, 31)) break;
-                    tc_fence_after();
-                    uint32_t ya[16], yb[16];                   // two pieces of Y, the second on its way
-                    tmem_ld16(t_x, ya);
 #pragma unroll
                     for (int c = 0; c < NCOL; c += 32) {
                         uint32_t pk[16];
+                        float4 lc[C::STAT_BYTES ? 8 : 1];          // (asked for together)
+                        if constexpr (C::STAT_BYTES > 0) {
 #pragma unroll
-                        for (int hf = 0; hf < 2; ++hf) {
-                            tmem_wait_ld();
-                            if (hf == 0) {
-                                tmem_ld16(t_x + c + 16, yb);
-                            } else if (c + 32 < NCOL) {
-                                tmem_ld16(t_x + c + 32, ya);
-                            }
-                            const uint32_t (&yr)[16] = hf ? yb : ya;
-                            float4 dc[C::STAT_BYTES ? 4 : 1];
-                            if constexpr (C::STAT_BYTES > 0) {
+                            for (int e = 0; e < 8; ++e) lc[e] = reinterpret_cast<const float4*>(info + c)[e];
+                        }
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) dc[e] = reinterpret_cast<const float4*>(info + NCOL + c + 16 * hf)[e];
-                            }
+                        for (int e = c; e < c + 32; e += 4) {
+                            float2 l[2];
+                            if constexpr (C::STAT_BYTES > 0) *reinterpret_cast<float4*>(l) = lc[(e - c) / 4];
+                            else l[0] = l[1] = make_float2(lrow[0], lrow[0]);
 #pragma unroll
-                            for (int e = 0; e < 16; e += 4) {
-                                const int at0 = c + 16 * hf + e;
-                                float2 d[2];
-                                if constexpr (C::STAT_BYTES > 0) *reinterpret_cast<float4*>(d) = dc[e / 4];
-                                else d[0] = d[1] = make_float2(drow, drow);
-#pragma unroll
-                                for (int f = 0; f < 2; ++f) {
-                                    const int at = at0 + 2 * f;
-                                    const float2 u = make_float2(__uint_as_float(pr[at]), __uint_as_float(pr[at + 1]));
-                                    float2 ds = make_float2(__uint_as_float(yr[e + 2 * f]), __uint_as_float(yr[e + 2 * f + 1]));
-                                    ds = __fmul2_rn(u, C::AUG ? ds : __fadd2_rn(ds, d[f]));
-                                    if constexpr (LD > 0) {
-#pragma unroll
-                                        for (int i = 0; i < 2; ++i) {
-                                            const float a = (i ? ds.y : ds.x) * da[at + i];
-                                            const float4* gc = gate_row(at + i);
-#pragma unroll
-                                            for (int q = 0; q < LD / 4; ++q) {
-                                                const float4 v = gc[q];
-                                                const float2 lo = __ffma2_rn(make_float2(a, a), make_float2(v.x, v.y), make_float2(dg[4 * q], dg[4 * q + 1]));
-                                                const float2 hi = __ffma2_rn(make_float2(a, a), make_float2(v.z, v.w), make_float2(dg[4 * q + 2], dg[4 * q + 3]));
-                                                dg[4 * q] = lo.x; dg[4 * q + 1] = lo.y; dg[4 * q + 2] = hi.x; dg[4 * q + 3] = hi.y;
-                                            }
-                                        }
-                                    }
-                                    pk[8 * hf + e / 2 + f] = pack_bf16x2(ds.x, ds.y);
+                            for (int f = 0; f < 2; ++f) {
+                                uint32_t &u0 = pr[e + 2 * f], &u1 = pr[e + 2 * f + 1];
+                                float2 x = make_float2(__uint_as_float(u0), __uint_as_float(u1)), y;
+                                if constexpr (CAP) {
+                                    x = __fmul2_rn(x, make_float2(cap_in, cap_in));
+                                    x.x = tanh_approx(x.x);
+                                    x.y = tanh_approx(x.y);
+                                    y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
+                                    y.x = ex2_approx(y.x);
+                                    y.y = ex2_approx(y.y);
+                                    x = __fmul2_rn(y, __ffma2_rn(make_float2(-x.x, -x.y), x, make_float2(1.f, 1.f)));
+                                } else {
+                                    if constexpr (C::AUG) y = __fmul2_rn(x, make_float2(sl2, sl2));
+                                    else y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
+                                    y.x = ex2_approx(y.x);
+                                    y.y = ex2_approx(y.y);
+                                    x = y;
                                 }
+                                u0 = __float_as_uint(x.x);
+                                u1 = __float_as_uint(x.y);
+                                if constexpr (C::HAS_V) pk[(e - c) / 2 + f] = pack_bf16x2(y.x, y.y);
                             }
                         }
-                        strike(pk, kw[c / 32]);
-                        // (in the place of Y itself only behind what has been read of it)
-                        tmem_st16(t_x + c / 2, pk);
-                        if (c + 32 == C::PART0 || c + 32 == NCOL) {
-                            tmem_wait_st();
+                        if constexpr (C::HAS_V) {
+                            strike(pk, kw[c / 32]);
+                            tmem_st16(t_x + c / 2, pk);
+                            if (c + 32 == C::PART0 || c + 32 == NCOL) {
+                                tmem_wait_st();
+                                tc_fence_before();
+                                mbar_arrive(smem_u32(&ctl.p_full[place][c + 32 == C::PART0 ? 0 : 1]));
+                            }
+                        }
+                    }
+                    // ---- dS
+                    if constexpr (C::HAS_DS) {
+                        if (!wait(ctl.y_full[place], par, 31)) break;
+                        tc_fence_after();
+                        uint32_t ya[16], yb[16];                   // two pieces of Y, the second on its way
+                        tmem_ld16(t_x, ya);
+#pragma unroll
+                        for (int c = 0; c < NCOL; c += 32) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int hf = 0; hf < 2; ++hf) {
+                                tmem_wait_ld();
+                                if (hf == 0) {
+                                    tmem_ld16(t_x + c + 16, yb);
+                                } else if (c + 32 < NCOL) {
+                                    tmem_ld16(t_x + c + 32, ya);
+                                }
+                                const uint32_t (&yr)[16] = hf ? yb : ya;
+                                float4 dc[C::STAT_BYTES ? 4 : 1];
+                                if constexpr (C::STAT_BYTES > 0) {
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) dc[e] = reinterpret_cast<const float4*>(info + NCOL + c + 16 * hf)[e];
+                                }
+#pragma unroll
+                                for (int e = 0; e < 16; e += 4) {
+                                    const int at0 = c + 16 * hf + e;
+                                    float2 d[2];
+                                    if constexpr (C::STAT_BYTES > 0) *reinterpret_cast<float4*>(d) = dc[e / 4];
+                                    else d[0] = d[1] = make_float2(drow[0], drow[0]);
+#pragma unroll
+                                    for (int f = 0; f < 2; ++f) {
+                                        const int at = at0 + 2 * f;
+                                        const float2 u = make_float2(__uint_as_float(pr[at]), __uint_as_float(pr[at + 1]));
+                                        float2 ds = make_float2(__uint_as_float(yr[e + 2 * f]), __uint_as_float(yr[e + 2 * f + 1]));
+                                        ds = __fmul2_rn(u, C::AUG ? ds : __fadd2_rn(ds, d[f]));
+                                        pk[8 * hf + e / 2 + f] = pack_bf16x2(ds.x, ds.y);
+                                    }
+                                }
+                            }
+                            strike(pk, kw[c / 32]);
+                            // (in the place of Y itself only behind what has been read of it)
+                            tmem_st16(t_x + c / 2, pk);
+                            if (c + 32 == C::PART0 || c + 32 == NCOL) {
+                                tmem_wait_st();
+                                tc_fence_before();
+                                mbar_arrive(smem_u32(&ctl.ds_full[place][c + 32 == C::PART0 ? 0 : 1]));
+                            }
+                        }
+                    }
+                } else {
+                    // The gate.  P times the factor waits for Y in tensor memory, what turns dS into the gradient of g_i . g_j in registers.
+                    constexpr uint32_t HALF = 16u << 16;       // 16 lanes on
+                    const uint32_t t_u = tm + C::COL_U + wg * NCOL;
+                    float da[4][NCOL / 4];                     // [row][two columns of every 8]
+                    int bound[4], last[4];                     // columns beyond which a pair is distant; the diagonal
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        last[q] = rowq + 8 * q - col0 - c2;
+                        bound[q] = KEYS ? last[q] + p.w : last[q] - p.w;
+                    }
+                    const float xs = p.scale * p.lambda;
+#pragma unroll
+                    for (int c = 0; c < NCOL; c += 32) {
+                        uint32_t xr[2][16];
+                        tmem_ld_frag(t_x + c, xr[0]);
+                        tmem_ld_frag(t_x + HALF + c, xr[1]);
+                        tmem_wait_ld();
+                        if (!C::HAS_V && c + 32 == NCOL) {
                             tc_fence_before();
-                            mbar_arrive(smem_u32(&ctl.ds_full[place][c + 32 == C::PART0 ? 0 : 1]));
+                            mbar_arrive(smem_u32(&ctl.x_taken[place]));
+                        }
+                        uint32_t pk[2][8];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int cj = c + 8 * j;
+                            float2 lc = make_float2(0.f, 0.f);
+                            if constexpr (KEYS) lc = *reinterpret_cast<const float2*>(info + cj + c2);
+                            float2 s[2][4];                    // [column][row]: partial sums of g_i . g_j
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const float4* gc = gate_row(cj + c2 + i);
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) s[i][q] = make_float2(0.f, 0.f);
+#pragma unroll
+                                for (int e = 0; e < LD / 4; ++e) {
+                                    const float4 v = gc[e];
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q) {
+                                        s[i][q] = __ffma2_rn(make_float2(gr[q][4 * e], gr[q][4 * e + 1]), make_float2(v.x, v.y), s[i][q]);
+                                        s[i][q] = __ffma2_rn(make_float2(gr[q][4 * e + 2], gr[q][4 * e + 3]), make_float2(v.z, v.w), s[i][q]);
+                                    }
+                                }
+                            }
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const int hf = q / 2, r = q % 2;
+                                uint32_t &u0 = xr[hf][4 * j + 2 * r], &u1 = xr[hf][4 * j + 2 * r + 1];
+                                const float2 x = make_float2(__uint_as_float(u0), __uint_as_float(u1));
+                                const float2 l = KEYS ? lc : make_float2(lrow[q], lrow[q]);
+                                // sigmoid of a distant pair: 1 / (1 + z), z = exp(-lambda g_i . g_j); 1 - f = z f
+                                float2 z, f;
+                                z.x = (KEYS ? cj > bound[q] : cj < bound[q]) ? ex2_approx(fminf(s[0][q].x + s[0][q].y, 126.f)) : 0.f;
+                                z.y = (KEYS ? cj + 1 > bound[q] : cj + 1 < bound[q]) ? ex2_approx(fminf(s[1][q].x + s[1][q].y, 126.f)) : 0.f;
+                                f.x = rcp_approx(1.f + z.x);
+                                f.y = rcp_approx(1.f + z.y);
+                                const float2 d = __fmul2_rn(__fmul2_rn(x, make_float2(xs, xs)), __fmul2_rn(z, f));
+                                da[q][cj / 4] = d.x;
+                                da[q][cj / 4 + 1] = d.y;
+                                float2 y = __ffma2_rn(__fmul2_rn(x, f), make_float2(sl2, sl2), l);
+                                y.x = ex2_approx(y.x);
+                                y.y = ex2_approx(y.y);
+                                if (masked) {                  // (causality alone)
+                                    y.x = (KEYS ? cj >= last[q] : cj <= last[q]) ? y.x : 0.f;
+                                    y.y = (KEYS ? cj + 1 >= last[q] : cj + 1 <= last[q]) ? y.y : 0.f;
+                                }
+                                if constexpr (C::HAS_V) pk[hf][2 * j + r] = pack_bf16x2(y.x, y.y);
+                                y = __fmul2_rn(y, f);
+                                u0 = __float_as_uint(y.x);
+                                u1 = __float_as_uint(y.y);
+                            }
+                        }
+                        if constexpr (C::HAS_DS) {
+                            tmem_st_frag(t_u + c, xr[0]);
+                            tmem_st_frag(t_u + HALF + c, xr[1]);
+                        }
+                        if constexpr (C::HAS_V) {
+                            tmem_st_pairs(t_x + c / 2, pk[0]);
+                            tmem_st_pairs(t_x + HALF + c / 2, pk[1]);
+                        }
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    if constexpr (C::HAS_V) mbar_arrive(smem_u32(&ctl.p_full[place][0]));
+                    // ---- dS
+                    if constexpr (C::HAS_DS) {
+                        if (!wait(ctl.y_full[place], par, 31)) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int c = 0; c < NCOL; c += 32) {
+                            uint32_t pk[2][8];
+#pragma unroll
+                            for (int hf = 0; hf < 2; ++hf) {
+                                uint32_t yr[16], ur[16];
+                                tmem_ld_frag(t_x + hf * HALF + c, yr);
+                                tmem_ld_frag(t_u + hf * HALF + c, ur);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const int cj = c + 8 * j;
+                                    float2 dc = make_float2(0.f, 0.f);
+                                    if constexpr (KEYS) dc = *reinterpret_cast<const float2*>(info + NCOL + cj + c2);
+#pragma unroll
+                                    for (int r = 0; r < 2; ++r) {
+                                        const int q = 2 * hf + r;
+                                        const float2 d = KEYS ? dc : make_float2(drow[q], drow[q]);
+                                        const float2 y = __fadd2_rn(make_float2(__uint_as_float(yr[4 * j + 2 * r]), __uint_as_float(yr[4 * j + 2 * r + 1])), d);
+                                        const float2 ds = __fmul2_rn(make_float2(__uint_as_float(ur[4 * j + 2 * r]), __uint_as_float(ur[4 * j + 2 * r + 1])), y);
+                                        da[q][cj / 4] *= ds.x;
+                                        da[q][cj / 4 + 1] *= ds.y;
+                                        pk[hf][2 * j + r] = pack_bf16x2(ds.x, ds.y);
+                                    }
+                                }
+                            }
+                            tmem_st_pairs(t_x + c / 2, pk[0]);
+                            tmem_st_pairs(t_x + HALF + c / 2, pk[1]);
+                        }
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(smem_u32(&ctl.ds_full[place][0]));
+#pragma unroll
+                        for (int cj = 0; cj < NCOL; cj += 8) {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const float4* gc = gate_row(cj + c2 + i);
+#pragma unroll
+                                for (int e = 0; e < LD / 4; ++e) {
+                                    const float4 v = gc[e];
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q) {
+                                        const float a = da[q][cj / 4 + i];
+                                        const float2 lo = __ffma2_rn(make_float2(a, a), make_float2(v.x, v.y), make_float2(dg[q][4 * e], dg[q][4 * e + 1]));
+                                        const float2 hi = __ffma2_rn(make_float2(a, a), make_float2(v.z, v.w), make_float2(dg[q][4 * e + 2], dg[q][4 * e + 3]));
+                                        dg[q][4 * e] = lo.x; dg[q][4 * e + 1] = lo.y; dg[q][4 * e + 2] = hi.x; dg[q][4 * e + 3] = hi.y;
+                                    }
+                                }
+                            }
                         }
                     }
                 }
@@ -721,18 +856,32 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
             }
             tc_fence_before();
             if constexpr (LD > 0 && MODE != BWD_V) {
-                // the even and the odd tiles' sums: the second group hands its own to the first (the slots are through)
-                float* const x = reinterpret_cast<float*>(smem_raw + C::OFF_C) + row_in_tile;
-                if (wg == 1) {
+                // a row's sums are those of four lanes, and of the even and the odd tiles: the second group hands its own to the first (the
+                // slots are through)
 #pragma unroll
-                    for (int e = 0; e < LD; ++e) x[e * 128] = dg[e];
-                    mbar_arrive(smem_u32(&ctl.dg_full));
-                } else if (wait(ctl.dg_full, 0, 41) && valid) {
+                for (int q = 0; q < 4; ++q) {
 #pragma unroll
-                    for (int e = 0; e < LD; e += 4)
-                        *reinterpret_cast<float4*>(p.dg_part + ((size_t)head * p.n + row) * LD + e) =
-                            make_float4(dg[e] + x[e * 128], dg[e + 1] + x[(e + 1) * 128], dg[e + 2] + x[(e + 2) * 128], dg[e + 3] + x[(e + 3) * 128]);
+                    for (int e = 0; e < LD; ++e) {
+                        dg[q][e] += __shfl_xor_sync(0xffffffffu, dg[q][e], 1);
+                        dg[q][e] += __shfl_xor_sync(0xffffffffu, dg[q][e], 2);
+                    }
                 }
+                float* const x = reinterpret_cast<float*>(smem_raw + C::OFF_C) + (threadIdx.x & 127);       // [e][thread]: lane t has row t / 4 + 8 (t % 4)
+                const bool other = wg == 0 && wait(ctl.dg_full, 0, 41);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if ((lane & 3) != q) continue;
+                    if (wg == 1) {
+#pragma unroll
+                        for (int e = 0; e < LD; ++e) x[e * 128] = dg[q][e];
+                    } else if (other && rowq + 8 * q < p.n) {
+#pragma unroll
+                        for (int e = 0; e < LD; e += 4)
+                            *reinterpret_cast<float4*>(p.dg_part + ((size_t)head * p.n + rowq + 8 * q) * LD + e) =
+                                make_float4(dg[q][e] + x[e * 128], dg[q][e + 1] + x[(e + 1) * 128], dg[q][e + 2] + x[(e + 2) * 128], dg[q][e + 3] + x[(e + 3) * 128]);
+                    }
+                }
+                if (wg == 1) mbar_arrive(smem_u32(&ctl.dg_full));
             }
         }
         if (bad && lane == 0) give_up(bad);

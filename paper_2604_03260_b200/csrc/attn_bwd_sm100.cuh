@@ -170,10 +170,10 @@ struct BwdWalk {
     }
 };
 
+// One pass's item number `block`
 template <int D, int MODE, bool CAP, int LD>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
-attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant__ CUtensorMap tm_r2, const __grid_constant__ CUtensorMap tm_c1,
-                const __grid_constant__ CUtensorMap tm_c2, const __grid_constant__ BwdParams p) {
+__device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtensorMap& tm_r2, const CUtensorMap& tm_c1, const CUtensorMap& tm_c2, const BwdParams& p,
+                                         const int block) {
     using C = BwdCfg<D, MODE, CAP, LD>;
     constexpr bool KEYS = C::KEYS;
     constexpr int NCOL = C::NCOL;
@@ -182,7 +182,7 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
     const uint32_t base = smem_u32(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // the longest items first: key tile 0, or the last query tile
-    const int q0 = p.by_heads.div((int)blockIdx.x), head = (int)blockIdx.x - q0 * p.heads;
+    const int q0 = p.by_heads.div(block), head = block - q0 * p.heads;
     const int row_tile = KEYS ? q0 : p.nt - 1 - q0;
     const int b = p.by_rows_H.div(head), h = head - b * (KEYS ? p.Hkv : p.Hq);
     auto give_up = [&](int where) {
@@ -898,31 +898,43 @@ attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_r1, const __grid_constant
     if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
-template <int D, int MODE, bool CAP, int LD>
-static int launch_bwd_pass(const AttnBwdArgs& a, const BwdParams& p, cudaStream_t st) {
-    using C = BwdCfg<D, MODE, CAP, LD>;
-    const int B = a.s.batch, n = a.s.n;
-    const focus_tensor &r1 = C::KEYS ? a.k : a.q, &r2 = C::KEYS ? a.v : a.dO, &c1 = C::KEYS ? a.q : a.k, &c2 = C::KEYS ? a.dO : a.v;
-    const int HR = C::KEYS ? a.s.Hkv : a.s.Hq, HC = C::KEYS ? a.s.Hq : a.s.Hkv;
-    CUtensorMap m1, m2, m3, m4;
-    int rc;
-    if ((rc = make_tmap_qkv(&m1, r1, B, HR, n, D)) || (rc = make_tmap_qkv(&m2, r2, B, HR, n, D)) || (rc = make_tmap_qkv(&m3, c1, B, HC, n, D, C::NCOL)) ||
-        (rc = make_tmap_qkv(&m4, c2, B, HC, n, D, C::NCOL)))
-        return rc;
-    if ((rc = check_cuda(allow_smem<attn_bwd_kernel<D, MODE, CAP, LD>>(C::SMEM), "cudaFuncSetAttribute(attn_bwd)"))) return rc;
-    auto kern = attn_bwd_kernel<D, MODE, CAP, LD>;
-    return check_cuda(launch_dependent(kern, dim3((unsigned)(p.heads * p.nt)), dim3(BWD_THREADS), C::SMEM, st, m1, m2, m3, m4, p), "attention backward launch");
+// All passes in one launch: they need nothing of one another, and the blocks of one fill the places that the other's last ones leave
+// (32 query on 8 KV heads x 8192 tokens: TODO).  Tensor maps of q, k, v and do, first for row tiles, then for column tiles.
+struct BwdMaps {
+    CUtensorMap r[4], c[4];
+};
+
+template <int D, bool CAP, int LD>
+__global__ void __launch_bounds__(BWD_THREADS, 1)
+attn_bwd_kernel(const __grid_constant__ BwdMaps m, const __grid_constant__ BwdParams kv, const __grid_constant__ BwdParams q) {
+    const int nkv = kv.heads * kv.nt, block = (int)blockIdx.x;
+    if constexpr (D == 256) {
+        if (block < nkv) bwd_item<D, BWD_K, CAP, LD>(m.r[1], m.r[2], m.c[0], m.c[3], kv, block);
+        else if (block < 2 * nkv) bwd_item<D, BWD_V, CAP, LD>(m.r[1], m.r[2], m.c[0], m.c[3], kv, block - nkv);
+        else bwd_item<D, BWD_Q, CAP, LD>(m.r[0], m.r[3], m.c[1], m.c[2], q, block - 2 * nkv);
+    } else {
+        if (block < nkv) bwd_item<D, BWD_KV, CAP, LD>(m.r[1], m.r[2], m.c[0], m.c[3], kv, block);
+        else bwd_item<D, BWD_Q, CAP, LD>(m.r[0], m.r[3], m.c[1], m.c[2], q, block - nkv);
+    }
 }
 
 template <int D, bool CAP, int LD>
 static int launch_bwd_passes(const AttnBwdArgs& a, const BwdParams& kv, const BwdParams& q, cudaStream_t st) {
+    using KV = BwdCfg<D, D == 256 ? BWD_K : BWD_KV, CAP, LD>;
+    using V = BwdCfg<D, D == 256 ? BWD_V : BWD_KV, CAP, LD>;
+    using Q = BwdCfg<D, BWD_Q, CAP, LD>;
+    constexpr uint32_t smem = KV::SMEM > Q::SMEM ? (KV::SMEM > V::SMEM ? KV::SMEM : V::SMEM) : (Q::SMEM > V::SMEM ? Q::SMEM : V::SMEM);
+    const focus_tensor* const t[4] = {&a.q, &a.k, &a.v, &a.dO};
+    const int heads[4] = {a.s.Hq, a.s.Hkv, a.s.Hkv, a.s.Hq};
+    BwdMaps m;
     int rc;
-    if constexpr (D == 256) {
-        if ((rc = launch_bwd_pass<D, BWD_V, CAP, LD>(a, kv, st)) || (rc = launch_bwd_pass<D, BWD_K, CAP, LD>(a, kv, st))) return rc;
-    } else {
-        if ((rc = launch_bwd_pass<D, BWD_KV, CAP, LD>(a, kv, st))) return rc;
-    }
-    return launch_bwd_pass<D, BWD_Q, CAP, LD>(a, q, st);
+    for (int i = 0; i < 4; ++i)
+        if ((rc = make_tmap_qkv(&m.r[i], *t[i], a.s.batch, heads[i], a.s.n, D)) || (rc = make_tmap_qkv(&m.c[i], *t[i], a.s.batch, heads[i], a.s.n, D, Q::NCOL))) return rc;
+    const long long blocks = (long long)kv.heads * kv.nt * (D == 256 ? 2 : 1) + (long long)q.heads * q.nt;
+    if (blocks > 0x7fffffffll) return fail(FOCUS_ERR_UNSUPPORTED, "attention backward: %lld tiles exceed 2^31 - 1", blocks);
+    if ((rc = check_cuda(allow_smem<attn_bwd_kernel<D, CAP, LD>>(smem), "cudaFuncSetAttribute(attn_bwd)"))) return rc;
+    auto kern = attn_bwd_kernel<D, CAP, LD>;
+    return check_cuda(launch_dependent(kern, dim3((unsigned)blocks), dim3(BWD_THREADS), smem, st, m, kv, q), "attention backward launch");
 }
 
 template <int D>

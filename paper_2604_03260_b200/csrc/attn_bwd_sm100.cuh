@@ -77,12 +77,16 @@ struct BwdCfg {
     // Columns of a tile, all of them one thread's: 128 probabilities in registers; with the gate two numbers a pair are held, so 64, and at
     // D = 256 the row tiles leave no room for wider ones
     static constexpr int NCOL = D == 256 || LD > 0 ? 64 : 128;
-    static constexpr int NPL = LD > 0 || (MODE == BWD_KV && D == 128) || (D == 256 && HAS_DS) ? 2 : 3;       // places (as many as fit; at D = 256 as many slots fit)
+    static constexpr int NPL = LD > 0 || (MODE != BWD_V && D >= 128) ? 2 : 3;       // places (as many as fit)
     static constexpr uint32_t COL_U = NPL * NCOL;                // gate: a place for each group's P times the factor
     static constexpr int SUBT = D / 64;
     static constexpr uint32_t SUBR = 128 * 128, SUBC = NCOL * 128;
     static constexpr uint32_t R_BYTES = SUBR * SUBT, C_BYTES = SUBC * SUBT;
-    static constexpr int NR = MODE == BWD_V ? 1 : 2;             // row tiles
+    // Row tiles that go to tensor memory, where there is room for them, and are the first operand from there: more slots for columns, and
+    // half the shared memory's traffic of a product
+    static constexpr bool R1T = LD == 0 && MODE == BWD_Q && D <= 128, R2T = LD == 0 && (MODE == BWD_Q || (MODE == BWD_K && D == 256));
+    static constexpr int NR = (R1T ? 0 : 1) + (R2T || MODE == BWD_V ? 0 : 1);     // those that stay in shared memory
+    static constexpr int RU = ((R1T ? 1 : 0) + (R2T ? 1 : 0)) * SUBT;             // 64-column pieces of the others; they come through the last slots of both rings
     // Rows are keys: lse and delta go by the column.  They come as six more numbers a column (-lse / scale and -delta in three bf16 terms
     // each, 24 bits), which one more 16-deep step of X and of Y, against rows of ones, adds to the products; a thread then needs nothing that
     // goes by the column.  Not where a cap or a gate comes between the product and lse, nor where shared memory has no room for it (dK at
@@ -103,17 +107,18 @@ struct BwdCfg {
     static constexpr int NS2 = NFIT - NS1, NSLOT = NFIT;
     static constexpr bool EARLY = MODE == BWD_V || NS1 > NPL;    // C1 of the tile after next can be there before the sum with dS frees a slot
     static_assert(NS2 >= 1 && NS1 >= 2 && (EARLY || NS1 == NPL), "two tiles at work");
-    static constexpr int P_PARTS = LD == 0 && KEYS ? 2 : 1;      // parts in which P and dS are handed over: most of a sum runs while the last are worked out
+    static constexpr int P_PARTS = LD == 0 ? 2 : 1;      // parts in which P and dS are handed over: most of a sum runs while the last are worked out
     static constexpr int PART0 = P_PARTS == 1 ? NCOL : NCOL == 128 ? 96 : 32;     // columns of the first
     static constexpr uint32_t OFF_C = NR * R_BYTES, OFF_CONST = OFF_C + NS1 * C1_BYTES + NS2 * C_BYTES, OFF_INFO = OFF_CONST + CONST_BYTES;
     static constexpr uint32_t OFF_CTL = OFF_INFO + 2 * INFO_BYTES, SMEM = OFF_CTL + CTL_BYTES;
     static __device__ __forceinline__ uint32_t slot_at(uint32_t s) { return s < NS1 ? s * C1_BYTES : NS1 * C1_BYTES + (s - NS1) * C_BYTES; }
-    static constexpr uint32_t COL_V = NPL * NCOL > 256 ? 384 : 256, COL_S = MODE == BWD_KV ? COL_V + D : COL_V;
+    static constexpr uint32_t COL_R = NPL * NCOL;                // row tiles
+    static constexpr uint32_t COL_V = RU > 0 ? COL_R + RU * 32 : NPL * NCOL > 256 ? 384 : 256, COL_S = MODE == BWD_KV ? COL_V + D : COL_V;
     static_assert(NPL * NCOL + (LD > 0 ? 2 * NCOL : 0) <= COL_V && COL_S + D <= 512, "tensor memory");
 };
 
 struct BwdCtl {
-    uint64_t r_full, acc_full, dg_full, full[8], empty[8];      // slots of C1, then of C2
+    uint64_t r_full, r_taken, acc_full, dg_full, full[8], empty[8];      // slots of C1, then of C2
     uint64_t id_full[4], id_empty[4];             // numbers of the tiles
     uint64_t info_full[2], info_empty[2];         // what else there is of a tile
     uint64_t x_full[3], x_taken[3], p_full[3][2], y_full[3], ds_full[3][2];       // by the tile's place (and part)
@@ -212,6 +217,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
     }
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&ctl.r_full), 1);
+        mbar_init(smem_u32(&ctl.r_taken), 256);
         mbar_init(smem_u32(&ctl.acc_full), (C::HAS_V ? 1 : 0) + (C::HAS_DS ? 1 : 0));
         mbar_init(smem_u32(&ctl.dg_full), 128);
         for (int s = 0; s < C::NSLOT; ++s) { mbar_init(smem_u32(&ctl.full[s]), 1); mbar_init(smem_u32(&ctl.empty[s]), 1); }
@@ -226,6 +232,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
             mbar_init(smem_u32(&ctl.y_full[x]), 1);
             for (int q = 0; q < 2; ++q) { mbar_init(smem_u32(&ctl.p_full[x][q]), 128); mbar_init(smem_u32(&ctl.ds_full[x][q]), 128); }
         }
+        for (int x = 0; x < 8; ++x) ctl.more[x] = 1;
         ctl.abort_flag = 0;
         ctl.limit = wait_limit(4000000000ull);
         fence_mbar_init();
@@ -251,17 +258,23 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
     dep_wait();
     dep_trigger();
 
+    // 64-column piece u of the row tiles on their way to tensor memory
+    auto unit_at = [&](int u) -> uint32_t {
+        constexpr int H = C::RU > 0 ? C::RU / 2 : 1;
+        return base + C::OFF_C + C::slot_at(u < H ? C::NS1 - 1 : C::NSLOT - 1) + (uint32_t)(u % H) * C::SUBR;
+    };
     if (warp < 4) reg_dec<REGS_CONTROL>();
     if (warp == 0 || warp == 3) {
         // ------------------------------------------------------------------ TMA: row tiles, C1 and the tiles' numbers; C2 and what goes by the column
         const bool one = warp == 0;
         const int hk = KEYS ? h : h / p.G;
         if (one && lane == 0) {
-            mbar_arrive_expect_tx(smem_u32(&ctl.r_full), C::NR * C::R_BYTES);
+            mbar_arrive_expect_tx(smem_u32(&ctl.r_full), C::NR * C::R_BYTES + C::RU * C::SUBR);
 #pragma unroll 1
             for (int c = 0; c < C::SUBT; ++c) {
-                tma_load_4d(base + c * C::SUBR, &tm_r1, smem_u32(&ctl.r_full), c * 64, row_tile * 128, h, b);
-                if (C::NR == 2) tma_load_4d(base + C::R_BYTES + c * C::SUBR, &tm_r2, smem_u32(&ctl.r_full), c * 64, row_tile * 128, h, b);
+                tma_load_4d(C::R1T ? unit_at(c) : base + c * C::SUBR, &tm_r1, smem_u32(&ctl.r_full), c * 64, row_tile * 128, h, b);
+                if (MODE != BWD_V)
+                    tma_load_4d(C::R2T ? unit_at((C::R1T ? C::SUBT : 0) + c) : base + C::R_BYTES + c * C::SUBR, &tm_r2, smem_u32(&ctl.r_full), c * 64, row_tile * 128, h, b);
             }
         }
         BwdWalk<KEYS, NCOL> walk(p, lane, row_tile, b, h);
@@ -291,18 +304,23 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         for (;;) {
             const int t = walk.next();
             const int hc = KEYS ? h * p.G + walk.hi : hk;           // head of the columns
-            if (!hand_id() || !wait(ctl.empty[slot0 + slot], phase ^ 1, 11)) break;
+            if (!hand_id()) break;
+            // (what can be is done before the slot is free: what comes after is in the way of the tile.  The bytes are announced behind the
+            // wait: before it the slot's last copy may be under way, and its phase with it.)
+            const uint32_t bar = smem_u32(&ctl.full[slot0 + slot]), at = base + C::OFF_C + C::slot_at(slot0 + slot);
+            const int row0 = t * NCOL;
+            const __nv_bfloat16* const aug = p.aug + (((size_t)(b * p.Hq + hc) * p.nt + row0 / 128) * 128 + row0 % 128) * 8;
+            if (!wait(ctl.empty[slot0 + slot], phase ^ 1, 11)) break;
+            if (C::RU > 0 && phase == 0 && slot == slots - 1 && !wait(ctl.r_taken, 0, 14)) break;
             if (lane == 0) {
-                const uint32_t bar = smem_u32(&ctl.full[slot0 + slot]), at = base + C::OFF_C + C::slot_at(slot0 + slot);
-                ctl.more[slot0 + slot] = t >= 0;
-                if (t < 0) {
-                    mbar_arrive(bar);
-                } else {
+                if (t >= 0) {
                     mbar_arrive_expect_tx(bar, one ? C::C1_BYTES : C::C_BYTES);
 #pragma unroll
-                    for (int c = 0; c < C::SUBT; ++c) tma_load_4d(at + c * C::SUBC, map, bar, c * 64, t * NCOL, hc, b);
-                    if (C::AUG && one)
-                        bulk_load(at + C::C_BYTES, p.aug + (((size_t)(b * p.Hq + hc) * p.nt + t * NCOL / 128) * 128 + t * NCOL % 128) * 8, C::AUG_BYTES, bar);
+                    for (int c = 0; c < C::SUBT; ++c) tma_load_4d(at + c * C::SUBC, map, bar, c * 64, row0, hc, b);
+                    if (C::AUG && one) bulk_load(at + C::C_BYTES, aug, C::AUG_BYTES, bar);
+                } else {
+                    ctl.more[slot0 + slot] = 0;
+                    mbar_arrive(bar);
                 }
             }
             __syncwarp();
@@ -336,9 +354,17 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         const uint32_t cm = (uint32_t)smem_desc_sw128(base + C::OFF_C, C::SUBC, 1024);             // along the tokens
         // d = rows (X: R1, Y: R2) times the columns in slot `at`; `aug`: slot of the tile's C1, behind which its lse and delta are
         auto product = [&](uint32_t d, bool y, uint32_t at, uint32_t aug) {
-            const uint32_t r = y ? r2 : r1, c = ck + (C::slot_at(at) >> 4);
+            const uint32_t c = ck + (C::slot_at(at) >> 4);
+            auto step = [&](int ks) { return c + (ks >> 2) * (C::SUBC >> 4) + (ks & 3) * 2; };
+            if (y ? C::R2T : C::R1T) {
+                const uint32_t r = tmem + C::COL_R + (y && C::R1T ? D / 2 : 0);
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) umma_ss_lo(d, r + (ks >> 2) * (C::SUBR >> 4) + (ks & 3) * 2, c + (ks >> 2) * (C::SUBC >> 4) + (ks & 3) * 2, IDESC_X, ks > 0);
+                for (int ks = 0; ks < D / 16; ++ks) umma_ts_lo(d, r + ks * 8, step(ks), IDESC_X, ks > 0);
+            } else {
+                const uint32_t r = y ? r2 : r1;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) umma_ss_lo(d, r + (ks >> 2) * (C::SUBR >> 4) + (ks & 3) * 2, step(ks), IDESC_X, ks > 0);
+            }
             if constexpr (C::AUG) {
                 const uint32_t ones = base + C::OFF_CONST + (y ? 4096 : 0), x = base + C::OFF_C + C::slot_at(aug) + C::C_BYTES;
                 umma_ss(d, smem_desc_plain(ones, 2048, 128), smem_desc_plain(x, base + C::OFF_CONST + 2048 - x, 128), IDESC_X, 1);
@@ -389,7 +415,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
             return !bad;
         };
         do {
-            if (!wait(ctl.r_full, 0, 20)) break;
+            if (!wait(ctl.r_full, 0, 20) || (C::RU > 0 && !wait(ctl.r_taken, 0, 28))) break;
             tc_fence_after();
             if (warp == 2) {
                 if (!C::HAS_DS || !first_x()) break;
@@ -524,8 +550,24 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
             while (rem) word(w1, true);
             return true;
         };
+        if constexpr (C::RU > 0) {
+            // the row tiles to tensor memory: a thread its row, each group half of the pieces
+            if (wait(ctl.r_full, 0, 29)) {
+#pragma unroll 1
+                for (int u = wg * (C::RU / 2); u < (wg + 1) * (C::RU / 2); ++u) {
+                    const unsigned char* const at = smem_raw + (unit_at(u) - base) + row_in_tile * 128;
+                    uint32_t w[32];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(&w[4 * e]) = *reinterpret_cast<const uint4*>(at + ((e ^ (row_in_tile & 7)) << 4));
+                    tmem_st32(tm + C::COL_R + u * 32, w);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&ctl.r_taken));
+            }
+        }
         uint32_t k = 0, place = wg, par = 0;               // the tile's place, the parity of its use
-        if (peek(0)) {
+        if (!bad && peek(0)) {
 #pragma unroll 1
             for (; ct >= 0; ++k) {
                 const uint32_t t_x = tm + place * NCOL;

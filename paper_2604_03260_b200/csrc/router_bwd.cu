@@ -7,7 +7,7 @@
 //
 // A block has a strip of columns and a run of tokens, a warp 64 columns of it (32 and 16 at K > 8 and > 16), and goes down its rows 32 at a time; the
 // rows come by asynchronous copies through a ring of three to four such pieces in shared memory.  Measured with dh (device time, graph replay): 32768 x 4096,
-// K = 8, d_g = 32: 104 us, of which 94 for the pass over the tokens (5.7 TB/s) and the rest for adding the parts up; 1024 x 768, K = 4: 10.9 us, two
+// K = 8, d_g = 32: 108 us, of which some 96 for the pass over the tokens (5.6 TB/s) and the rest for adding the parts up; 1024 x 768, K = 4: 11.1 us, two
 // launches and the chain of loads of each.  The same on the fp32 pipe, rows through a private ring: 175 and 16.4 us.
 #include "common.cuh"
 
@@ -172,6 +172,13 @@ router_bwd_kernel(const __nv_bfloat16* h, int64_t h_sb, int64_t h_sn, const floa
         copy(x + R::STAGES - 1);
         load((x + 1) * RB_ROWS);
         const uint32_t st = base + (x % R::STAGES) * R::STAGE_BYTES;
+        // (sums of the tensor cores are cut off, not rounded: one of 32 rows at a time, and those are added here)
+        float P[CW / 16][G8][4];
+#pragma unroll
+        for (int m = 0; m < CW / 16; ++m) {
+#pragma unroll
+            for (int v = 0; v < G8; ++v) P[m][v][0] = P[m][v][1] = P[m][v][2] = P[m][v][3] = 0.f;
+        }
 #pragma unroll
         for (int k16 = 0; k16 < RB_ROWS / 16; ++k16) {
             const int r0 = 16 * k16;
@@ -190,7 +197,7 @@ router_bwd_kernel(const __nv_bfloat16* h, int64_t h_sb, int64_t h_sn, const floa
                 aa[v][2] = *reinterpret_cast<const uint32_t*>(y + 8);
                 aa[v][3] = *reinterpret_cast<const uint32_t*>(y + 8 * R::APITCH + 8);
             }
-            // T += h^T dS: rows of the product are columns of h
+            // P += h^T dS: rows of the product are columns of h
 #pragma unroll
             for (int m = 0; m < CW / 16; ++m) {
                 const int r = r0 + (lane & 7) + (lane >= 16 ? 8 : 0), c = warp * (CW / 8) + 2 * m + ((lane >> 3) & 1);
@@ -200,7 +207,7 @@ router_bwd_kernel(const __nv_bfloat16* h, int64_t h_sb, int64_t h_sn, const floa
 #pragma unroll
                 for (int v = 0; v < G8; ++v) {
 #pragma unroll
-                    for (int z = 2; z >= 0; --z) rb_mma(T[m][v], a, bt[z][v][0], bt[z][v][1]);
+                    for (int z = 2; z >= 0; --z) rb_mma(P[m][v], a, bt[z][v][0], bt[z][v][1]);
                 }
             }
             // dh = dS F
@@ -229,6 +236,14 @@ router_bwd_kernel(const __nv_bfloat16* h, int64_t h_sb, int64_t h_sn, const floa
                         else *reinterpret_cast<uint2*>(to) = make_uint2(o[u][0], o[u][1]);
                     }
                 }
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < CW / 16; ++m) {
+#pragma unroll
+            for (int v = 0; v < G8; ++v) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) T[m][v][i] += P[m][v][i];
             }
         }
     }

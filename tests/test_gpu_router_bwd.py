@@ -1,4 +1,4 @@
-"""focus_router_scores_bwd against the formula in 64 bits, and the chain from a loss to the router's weights by the library's kernels."""
+"""focus_router_scores_bwd against the formula in 64 bits (the chain from a loss to the router's weights: test_gpu_gate_layer.py)."""
 import math
 
 import pytest
@@ -10,7 +10,8 @@ from paper_2604_03260_b200 import binding as fb
 pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -8
-# sums over N tokens in fp32: pieces of a few hundred products each (N_piece 2^-24 of the absolute terms), added up in 64 bits
+# sums over N tokens in fp32, 2^-24 of the absolute terms for each of some hundred steps in a row at most (pieces of 32 tokens, runs, blocks of runs),
+# twice over for the two products, and the lost ends of bf16 terms
 E = 2.0 ** -14
 
 
@@ -90,3 +91,18 @@ def test_captured_on_a_stream():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((dh, dWg, dC), want))
+
+
+def test_long_sums_stay_in_32_bits():
+    """32768 tokens whose terms all have one sign.  A sum of 32 tokens on the tensor cores is six steps, each cut off by less than 2^-23 of what it has
+    by then (a half and the whole of the piece: 4.5 2^-23 at most, taken as six); pieces, parts and columns are added with roundings of half a step,
+    2^-24 of the running sum at most and of both signs, some 40 + 4 + 8 of them on average halfway up: below 2^-22 together.  In all below 2^-20."""
+    n, d, dg, K = 32768, 4096, 16, 8
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(8)
+    rnd = lambda *s: 1 + 0.25 * torch.rand(s, generator=gen, device="cuda")
+    h, Wg, C, ds = rnd(1, n, d).to(torch.bfloat16), rnd(d, dg), rnd(K, dg), rnd(1, n, K)
+    _, dWg, dC = call(fb.make_shape(2, 1, n, 64, K, 1, 0), h, Wg, C, ds, None)
+    T = sum(ds[0, i:i + 4096].double().T @ h[0, i:i + 4096].double() for i in range(0, n, 4096))
+    for got, want in ((dWg, T.T @ C.double()), (dC, T @ Wg.double())):
+        assert (got.double() - want).norm() <= 2.0 ** -20 * want.norm(), ((got.double() - want).norm() / want.norm()).item()

@@ -14,17 +14,44 @@ namespace focus {
 // first, so that every probability is 0.  The same as six bf16 numbers a row (the first divided by scale log2(e), in place of -inf a number
 // beyond every score): what the passes over keys add to their products.  With masks, which queries of the tile are members of each group.
 // A block per (head, tile):
-// D / 8 threads a row, every 16-byte piece of the tile asked for at once.
+// D / 8 threads a row, every 16-byte piece of the tile asked for at once.  Behind those, with the gate, a block per tile of a sequence: terms of
+// its assignments (`depth` > 0), of the rows times `by` and of the columns: in the order of the products lo hi, hi lo, mid mid, mid hi, hi mid,
+// hi hi (the smallest first).
 template <int D>
 __global__ void __launch_bounds__(256)
 bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn, const __nv_bfloat16* dO, int64_t d_sb, int64_t d_sh, int64_t d_sn,
-                const float* lse, int Hq, int n, int nt, const uint32_t* mq, int K, float sl2, float* stat, __nv_bfloat16* aug, uint32_t* qbits) {
+                const float* lse, int Hq, int n, int nt, const uint32_t* mq, int K, float sl2, float* stat, __nv_bfloat16* aug, uint32_t* qbits, int own, const float* g, float by,
+                int ld, int depth, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols) {
     __shared__ float sl[128], sd[128];
     constexpr int TPR = D / 8, RPP = 256 / TPR, U = D == 256 ? 8 : 128 / RPP;       // threads a row, rows a turn, turns at once
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int hq = blockIdx.x / nt, tile = blockIdx.x % nt, b = hq / Hq, h = hq % Hq, i0 = tile * 128;
     dep_wait();
     dep_trigger();
+    if ((int)blockIdx.x >= own) {
+        const int bt = blockIdx.x - own, r = threadIdx.x & 127, i = bt % nt * 128 + r;
+        const bool col = threadIdx.x >= 128;
+        const float* const gp = g + ((size_t)(bt / nt) * n + i) * ld;
+        for (int ch = 0; ch < depth / 8; ++ch) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int at = ch * 8 + e, product = at / ld;
+                float v = i < n && product < 6 ? gp[at % ld] * (col ? 1.f : by) : 0.f;
+                const int term = (col ? 0x010120 : 0x001102) >> (4 * product) & 3;
+                __nv_bfloat16 y = __float2bfloat16_rn(v);
+                for (int x = 0; x < term; ++x) {
+                    v -= __bfloat162float(y);
+                    y = __float2bfloat16_rn(v);
+                }
+                w[e / 2] = e & 1 ? w[e / 2] | (uint32_t)__bfloat16_as_ushort(y) << 16 : (uint32_t)__bfloat16_as_ushort(y);
+            }
+            uint4* const to = col ? reinterpret_cast<uint4*>(g_cols) + ((size_t)(2 * bt + (r >> 6)) * (depth / 8) + ch) * 64 + (r & 63)
+                                  : reinterpret_cast<uint4*>(g_rows) + ((size_t)bt * (depth / 8) + ch) * 128 + r;
+            *to = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        return;
+    }
     float* const t = stat + (size_t)blockIdx.x * 256;
     const int r0 = threadIdx.x / TPR, c = threadIdx.x % TPR * 8;
     const __nv_bfloat16* const ob = o + b * o_sb + h * o_sh + (int64_t)i0 * o_sn + c;
@@ -84,11 +111,13 @@ bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn
 }
 
 template <int D>
-static int launch_bwd_rows(const AttnBwdArgs& a, int nt, float* stat, __nv_bfloat16* aug, uint32_t* qbits, cudaStream_t st) {
+static int launch_bwd_rows(const AttnBwdArgs& a, int nt, float* stat, __nv_bfloat16* aug, uint32_t* qbits, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols, cudaStream_t st) {
     auto kern = bwd_rows_kernel<D>;
-    return check_cuda(launch_dependent(kern, dim3((unsigned)(a.s.batch * a.s.Hq * nt)), dim3(256), 0, st, (const __nv_bfloat16*)a.o.ptr, a.o.stride_b, a.o.stride_h,
+    const int own = a.s.batch * a.s.Hq * nt, ld = focus_soft_ld(a.s.K);
+    return check_cuda(launch_dependent(kern, dim3((unsigned)(own + (g_rows ? a.s.batch * nt : 0))), dim3(256), 0, st, (const __nv_bfloat16*)a.o.ptr, a.o.stride_b, a.o.stride_h,
                                        a.o.stride_n, (const __nv_bfloat16*)a.dO.ptr, a.dO.stride_b, a.dO.stride_h, a.dO.stride_n, a.lse, a.s.Hq, a.s.n, nt,
-                                       a.tiles ? a.mq : nullptr, a.s.K, a.scale * LOG2E, stat, aug, qbits), "attention backward rows launch");
+                                       a.tiles ? a.mq : nullptr, a.s.K, a.scale * LOG2E, stat, aug, qbits, own, a.g, -a.lambda * LOG2E, ld, g_rows ? gate_depth(ld) : 0, g_rows, g_cols),
+                      "attention backward rows launch");
 }
 
 // dg[b][i][:] = sum over the heads of both sides' partial sums, in their order; columns from K on are written as 0
@@ -106,7 +135,7 @@ bwd_gate_sum_kernel(const float* gq, const float* gk, int Hq, int Hkv, long long
 }
 
 struct BwdWorkspace {
-    size_t stat, aug, qbits, gq, gk, bytes;
+    size_t stat, aug, qbits, gq, gk, g_rows, g_cols, bytes;
 };
 static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
     const size_t HQ = (size_t)s->batch * s->Hq, HK = (size_t)s->batch * s->Hkv, nt = cdiv(s->n, 128), row = (size_t)s->n * focus_soft_ld(s->K) * 4;
@@ -118,6 +147,9 @@ static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
     w.qbits = gate ? 0 : take(HQ * nt * s->K * 16);
     w.gq = gate ? take(HQ * row) : 0;
     w.gk = gate ? take(HK * row) : 0;
+    const size_t terms = gate && s->D != 256 ? (size_t)s->batch * nt * 128 * gate_depth(focus_soft_ld(s->K)) * 2 : 0;
+    w.g_rows = take(terms);
+    w.g_cols = take(terms);
     w.bytes = off;
     return w;
 }
@@ -128,11 +160,16 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st) {
     const focus_shape& s = a.s;
     const BwdWorkspace w = bwd_workspace(&s, a.g != nullptr);
     const int nt = cdiv(s.n, 128), HQ = s.batch * s.Hq, HK = s.batch * s.Hkv;
-    if ((long long)HQ * nt > 0x7fffffffll) return fail(FOCUS_ERR_UNSUPPORTED, "attention backward: %lld tiles exceed 2^31 - 1", (long long)HQ * nt);
+    if ((long long)(HQ + s.batch) * nt > 0x7fffffffll) return fail(FOCUS_ERR_UNSUPPORTED, "attention backward: %lld tiles exceed 2^31 - 1", (long long)HQ * nt);
     float* const stat = reinterpret_cast<float*>(a.ws + w.stat);
     __nv_bfloat16* const aug = reinterpret_cast<__nv_bfloat16*>(a.ws + w.aug);
     uint32_t* const qbits = reinterpret_cast<uint32_t*>(a.ws + w.qbits);
-    int rc = s.D == 64 ? launch_bwd_rows<64>(a, nt, stat, aug, qbits, st) : s.D == 128 ? launch_bwd_rows<128>(a, nt, stat, aug, qbits, st) : launch_bwd_rows<256>(a, nt, stat, aug, qbits, st);
+    const bool terms = a.g && s.D != 256;
+    __nv_bfloat16* const g_rows = terms ? reinterpret_cast<__nv_bfloat16*>(a.ws + w.g_rows) : nullptr;
+    __nv_bfloat16* const g_cols = terms ? reinterpret_cast<__nv_bfloat16*>(a.ws + w.g_cols) : nullptr;
+    int rc = s.D == 64    ? launch_bwd_rows<64>(a, nt, stat, aug, qbits, g_rows, g_cols, st)
+             : s.D == 128 ? launch_bwd_rows<128>(a, nt, stat, aug, qbits, g_rows, g_cols, st)
+                          : launch_bwd_rows<256>(a, nt, stat, aug, qbits, g_rows, g_cols, st);
     if (rc) return rc;
     BwdParams p = {};
     p.Hq = s.Hq; p.Hkv = s.Hkv; p.G = s.Hq / s.Hkv; p.n = s.n; p.nt = nt; p.K = s.K; p.w = s.window < s.n ? s.window : s.n;
@@ -140,6 +177,8 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st) {
     p.stat = stat;
     p.aug = aug;
     p.g = a.g;
+    p.g_rows = g_rows;
+    p.g_cols = g_cols;
     p.nkw = cdiv(nt, 32);
     p.live = a.tiles ? reinterpret_cast<const uint32_t*>(a.tiles + a.L.live) : nullptr;
     p.status = a.dev_status;

@@ -32,6 +32,9 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st);
 // BWD_Q    rows are queries: dQ += dS C1 (R1 = Q, R2 = dO, C1 = K, C2 = V)
 enum : int { BWD_KV = 0, BWD_V = 1, BWD_K = 2, BWD_Q = 3 };
 
+// Depth of the product that gives the gate's g_i . g_j: six products of bf16 terms, in steps of 16
+constexpr int gate_depth(int ld) { return (6 * ld + 15) / 16 * 16; }
+
 struct BwdParams {
     int Hq, Hkv, G, n, nt, K, w;
     int heads;                // batch * heads of the rows
@@ -44,6 +47,7 @@ struct BwdParams {
     const uint32_t* live;     // live far tiles [batch Hq][nt][nkw]
     int nkw;
     const float* g;
+    const __nv_bfloat16 *g_rows, *g_cols; // its terms: of the rows [batch][nt][depth / 8][128][8], of the columns [batch][2 nt][depth / 8][64][8]
     float* dg_part;           // [batch heads of the rows][n][ld]
     __nv_bfloat16 *out1, *out2;           // dV (BWD_KV, BWD_V); dK / dQ
     int64_t s1b, s1h, s1n, s2b, s2h, s2n;

@@ -78,7 +78,7 @@ struct BwdCfg {
     // D = 256 the row tiles leave no room for wider ones
     static constexpr int NCOL = D == 256 || LD > 0 ? 64 : 128;
     static constexpr int NPL = LD > 0 || (MODE != BWD_V && D >= 128) ? 2 : 3;       // places (as many as fit)
-    static constexpr uint32_t COL_U = NPL * NCOL;                // gate: a place for each group's P times the factor
+    static constexpr uint32_t COL_U = NPL * NCOL;                // gate: a place for each group's g_i . g_j, then P times the factor
     static constexpr int SUBT = D / 64;
     static constexpr uint32_t SUBR = 128 * 128, SUBC = NCOL * 128;
     static constexpr uint32_t R_BYTES = SUBR * SUBT, C_BYTES = SUBC * SUBT;
@@ -93,24 +93,31 @@ struct BwdCfg {
     // D = 256); there they are copied to shared memory and read.
     static constexpr bool AUG = KEYS && !CAP && LD == 0 && !(D == 256 && MODE == BWD_K);
     static constexpr uint32_t AUG_BYTES = AUG ? NCOL * 16 : 0, CONST_BYTES = AUG ? 4 * 2048 : 0;        // (ones for X, zeros, ones for Y, zeros)
-    static constexpr uint32_t C1_BYTES = C_BYTES + AUG_BYTES;
+    // The gate's g_i . g_j times -lambda log2(e), from the tensor cores too: both sides in three bf16 terms, the six products of terms above 2^-24 side
+    // by side in GK steps' depth.  The columns' come with C1, behind it.  (At D = 256 there is no room: by instructions.)
+    static constexpr bool GM = LD > 0 && D != 256;
+    static constexpr int GK = GM ? gate_depth(LD) : 0;
+    static constexpr uint32_t GC_BYTES = GK * NCOL * 2, GR_BYTES = GK * 256;
+    static constexpr uint32_t C1_BYTES = C_BYTES + AUG_BYTES + GC_BYTES;
     static constexpr uint32_t STAT_BYTES = KEYS && !AUG ? 2 * NCOL * 4 : 0;
     // The columns' assignments, copied beside the tile; at D = 256 there is no room, they are read from L1 (one address a warp)
     static constexpr bool GATE_SMEM = LD > 0 && D != 256;
     static constexpr uint32_t GATE_BYTES = GATE_SMEM ? NCOL * LD * 4 : 0;
     static constexpr uint32_t INFO_BYTES = STAT_BYTES + GATE_BYTES;               // one tile; two of them
     static constexpr uint32_t CTL_BYTES = 1024;
-    static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - 2 * INFO_BYTES - CONST_BYTES;
+    static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - 2 * INFO_BYTES - CONST_BYTES - GR_BYTES;
     // C1 of a tile is held from its X to its sum with dS, NPL tiles later, C2 for a product or two: rings of their own
     static constexpr int NFIT = ROOM / C1_BYTES > 8 ? 8 : ROOM / C1_BYTES;
-    static constexpr int NS1 = MODE == BWD_V ? NFIT - NFIT / 2 : NFIT > NPL + 1 ? (NFIT + 1 > 2 * (NPL + 1) ? (NFIT + 1) / 2 : NPL + 1) : NFIT - 1;
-    static constexpr int NS2 = NFIT - NS1, NSLOT = NFIT;
+    static constexpr int NG1 = 4 * C1_BYTES + 2 * C_BYTES <= ROOM ? 4 : 3 * C1_BYTES + C_BYTES <= ROOM ? 3 : 2, NG2 = (ROOM - NG1 * C1_BYTES) / C_BYTES;
+    static constexpr int NS1 = GM ? NG1 : MODE == BWD_V ? NFIT - NFIT / 2 : NFIT > NPL + 1 ? (NFIT + 1 > 2 * (NPL + 1) ? (NFIT + 1) / 2 : NPL + 1) : NFIT - 1;
+    static constexpr int NS2 = GM ? (NG2 > 8 - NG1 ? 8 - NG1 : NG2) : NFIT - NS1, NSLOT = NS1 + NS2;
     static constexpr bool EARLY = MODE == BWD_V || NS1 > NPL;    // C1 of the tile after next can be there before the sum with dS frees a slot
     static_assert(NS2 >= 1 && NS1 >= 2 && (EARLY || NS1 == NPL), "two tiles at work");
     static constexpr int P_PARTS = LD == 0 ? 2 : 1;      // parts in which P and dS are handed over: most of a sum runs while the last are worked out
     static constexpr int PART0 = P_PARTS == 1 ? NCOL : NCOL == 128 ? 96 : 32;     // columns of the first
-    static constexpr uint32_t OFF_C = NR * R_BYTES, OFF_CONST = OFF_C + NS1 * C1_BYTES + NS2 * C_BYTES, OFF_INFO = OFF_CONST + CONST_BYTES;
+    static constexpr uint32_t OFF_C = NR * R_BYTES, OFF_CONST = OFF_C + NS1 * C1_BYTES + NS2 * C_BYTES, OFF_GR = OFF_CONST + CONST_BYTES, OFF_INFO = OFF_GR + GR_BYTES;
     static constexpr uint32_t OFF_CTL = OFF_INFO + 2 * INFO_BYTES, SMEM = OFF_CTL + CTL_BYTES;
+    static_assert(SMEM <= 227 * 1024 && C1_BYTES % 1024 == 0, "shared memory");
     static __device__ __forceinline__ uint32_t slot_at(uint32_t s) { return s < NS1 ? s * C1_BYTES : NS1 * C1_BYTES + (s - NS1) * C_BYTES; }
     static constexpr uint32_t COL_R = NPL * NCOL;                // row tiles
     static constexpr uint32_t COL_V = RU > 0 ? COL_R + RU * 32 : NPL * NCOL > 256 ? 384 : 256, COL_S = MODE == BWD_KV ? COL_V + D : COL_V;
@@ -269,7 +276,8 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         const bool one = warp == 0;
         const int hk = KEYS ? h : h / p.G;
         if (one && lane == 0) {
-            mbar_arrive_expect_tx(smem_u32(&ctl.r_full), C::NR * C::R_BYTES + C::RU * C::SUBR);
+            mbar_arrive_expect_tx(smem_u32(&ctl.r_full), C::NR * C::R_BYTES + C::RU * C::SUBR + C::GR_BYTES);
+            if constexpr (C::GM) bulk_load(base + C::OFF_GR, p.g_rows + ((size_t)b * p.nt + row_tile) * 128 * C::GK, C::GR_BYTES, smem_u32(&ctl.r_full));
 #pragma unroll 1
             for (int c = 0; c < C::SUBT; ++c) {
                 tma_load_4d(C::R1T ? unit_at(c) : base + c * C::SUBR, &tm_r1, smem_u32(&ctl.r_full), c * 64, row_tile * 128, h, b);
@@ -318,6 +326,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
 #pragma unroll
                     for (int c = 0; c < C::SUBT; ++c) tma_load_4d(at + c * C::SUBC, map, bar, c * 64, row0, hc, b);
                     if (C::AUG && one) bulk_load(at + C::C_BYTES, aug, C::AUG_BYTES, bar);
+                    if (C::GM && one) bulk_load(at + C::C_BYTES, p.g_cols + ((size_t)b * p.nt * 2 + t) * 64 * C::GK, C::GC_BYTES, bar);
                 } else {
                     ctl.more[slot0 + slot] = 0;
                     mbar_arrive(bar);
@@ -375,6 +384,11 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         // (by the elected lane)
         auto put_x = [&](uint32_t place, uint32_t c1) {
             product(tmem + place * NCOL, false, c1, c1);
+            if constexpr (C::GM) {
+                const uint64_t r = smem_desc_plain(base + C::OFF_GR, 2048, 128), c = smem_desc_plain(base + C::OFF_C + C::slot_at(c1) + C::C_BYTES, NCOL * 16, 128);
+#pragma unroll
+                for (int ks = 0; ks < C::GK / 16; ++ks) umma_ss(tmem + C::COL_U + place * NCOL, r + ks * (4096 >> 4), c + ks * (NCOL * 32 >> 4), IDESC_X, ks > 0);
+            }
             umma_commit(smem_u32(&ctl.x_full[place]));
             if (!C::HAS_DS) umma_commit(smem_u32(&ctl.empty[c1]));
         };
@@ -500,13 +514,13 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         uint32_t mask = 0;
         if (p.bits) mask = valid ? dep_load(p.row_mask + (size_t)head * p.n + row) & (0xffffffffu >> (32 - p.K)) : 0u;
         constexpr int LDR = LD > 0 ? LD : 1, LQ = LD > 0 ? 4 : 1, NW = NCOL / 32;
-        float gr[LQ][LDR], dg[LQ][LDR];                    // assignments of the rows times -lambda log2(e), their gradients
+        float gr[C::GM ? 1 : LQ][C::GM ? 1 : LDR], dg[LQ][LDR];        // assignments of the rows times -lambda log2(e), their gradients over scale lambda
         if constexpr (LD > 0) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
 #pragma unroll
                 for (int e = 0; e < LD; ++e) {
-                    gr[q][e] = rowq + 8 * q < p.n ? dep_load(p.g + ((size_t)b * p.n + rowq + 8 * q) * LD + e) * (-p.lambda * LOG2E) : 0.f;
+                    if constexpr (!C::GM) gr[q][e] = rowq + 8 * q < p.n ? dep_load(p.g + ((size_t)b * p.n + rowq + 8 * q) * LD + e) * (-p.lambda * LOG2E) : 0.f;
                     dg[q][e] = 0.f;
                 }
             }
@@ -726,19 +740,23 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                     // The gate.  P times the factor waits for Y in tensor memory, what turns dS into the gradient of g_i . g_j in registers.
                     constexpr uint32_t HALF = 16u << 16;       // 16 lanes on
                     const uint32_t t_u = tm + C::COL_U + wg * NCOL;
-                    float da[4][NCOL / 4];                     // [row][two columns of every 8]
+                    float2 da[4][NCOL / 8];                    // [row][two columns of every 8]
                     int bound[4], last[4];                     // columns beyond which a pair is distant; the diagonal
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         last[q] = rowq + 8 * q - col0 - c2;
                         bound[q] = KEYS ? last[q] + p.w : last[q] - p.w;
                     }
-                    const float xs = p.scale * p.lambda;
 #pragma unroll
                     for (int c = 0; c < NCOL; c += 32) {
                         uint32_t xr[2][16];
                         tmem_ld_frag(t_x + c, xr[0]);
                         tmem_ld_frag(t_x + HALF + c, xr[1]);
+                        uint32_t gx[2][C::GM ? 16 : 1];
+                        if constexpr (C::GM) {
+                            tmem_ld_frag(t_u + c, gx[0]);
+                            tmem_ld_frag(t_u + HALF + c, gx[1]);
+                        }
                         tmem_wait_ld();
                         if (!C::HAS_V && c + 32 == NCOL) {
                             tc_fence_before();
@@ -750,21 +768,30 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                             const int cj = c + 8 * j;
                             float2 lc = make_float2(0.f, 0.f);
                             if constexpr (KEYS) lc = *reinterpret_cast<const float2*>(info + cj + c2);
-                            float2 s[2][4];                    // [column][row]: partial sums of g_i . g_j
+                            float2 s[4];                       // [row]: both columns' g_i . g_j times -lambda log2(e)
+                            if constexpr (C::GM) {
 #pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const float4* gc = gate_row(cj + c2 + i);
+                                for (int q = 0; q < 4; ++q)
+                                    s[q] = make_float2(__uint_as_float(gx[q / 2][4 * j + 2 * (q % 2)]), __uint_as_float(gx[q / 2][4 * j + 2 * (q % 2) + 1]));
+                            } else {
+                                float2 part[2][4];
 #pragma unroll
-                                for (int q = 0; q < 4; ++q) s[i][q] = make_float2(0.f, 0.f);
+                                for (int i = 0; i < 2; ++i) {
+                                    const float4* gc = gate_row(cj + c2 + i);
 #pragma unroll
-                                for (int e = 0; e < LD / 4; ++e) {
-                                    const float4 v = gc[e];
+                                    for (int q = 0; q < 4; ++q) part[i][q] = make_float2(0.f, 0.f);
 #pragma unroll
-                                    for (int q = 0; q < 4; ++q) {
-                                        s[i][q] = __ffma2_rn(make_float2(gr[q][4 * e], gr[q][4 * e + 1]), make_float2(v.x, v.y), s[i][q]);
-                                        s[i][q] = __ffma2_rn(make_float2(gr[q][4 * e + 2], gr[q][4 * e + 3]), make_float2(v.z, v.w), s[i][q]);
+                                    for (int e = 0; e < LD / 4; ++e) {
+                                        const float4 v = gc[e];
+#pragma unroll
+                                        for (int q = 0; q < 4; ++q) {
+                                            part[i][q] = __ffma2_rn(make_float2(gr[q][4 * e], gr[q][4 * e + 1]), make_float2(v.x, v.y), part[i][q]);
+                                            part[i][q] = __ffma2_rn(make_float2(gr[q][4 * e + 2], gr[q][4 * e + 3]), make_float2(v.z, v.w), part[i][q]);
+                                        }
                                     }
                                 }
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) s[q] = make_float2(part[0][q].x + part[0][q].y, part[1][q].x + part[1][q].y);
                             }
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
@@ -774,14 +801,14 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                                 const float2 l = KEYS ? lc : make_float2(lrow[q], lrow[q]);
                                 // sigmoid of a distant pair: 1 / (1 + z), z = exp(-lambda g_i . g_j); 1 - f = z f
                                 float2 z, f;
-                                z.x = (KEYS ? cj > bound[q] : cj < bound[q]) ? ex2_approx(fminf(s[0][q].x + s[0][q].y, 126.f)) : 0.f;
-                                z.y = (KEYS ? cj + 1 > bound[q] : cj + 1 < bound[q]) ? ex2_approx(fminf(s[1][q].x + s[1][q].y, 126.f)) : 0.f;
-                                f.x = rcp_approx(1.f + z.x);
-                                f.y = rcp_approx(1.f + z.y);
-                                const float2 d = __fmul2_rn(__fmul2_rn(x, make_float2(xs, xs)), __fmul2_rn(z, f));
-                                da[q][cj / 4] = d.x;
-                                da[q][cj / 4 + 1] = d.y;
-                                float2 y = __ffma2_rn(__fmul2_rn(x, f), make_float2(sl2, sl2), l);
+                                z.x = (KEYS ? cj > bound[q] : cj < bound[q]) ? ex2_approx(fminf(s[q].x, 126.f)) : 0.f;
+                                z.y = (KEYS ? cj + 1 > bound[q] : cj + 1 < bound[q]) ? ex2_approx(fminf(s[q].y, 126.f)) : 0.f;
+                                f = __fadd2_rn(z, make_float2(1.f, 1.f));
+                                f.x = rcp_approx(f.x);
+                                f.y = rcp_approx(f.y);
+                                const float2 xf = __fmul2_rn(x, f);
+                                da[q][cj / 8] = __fmul2_rn(z, xf);             // (dS, by which it is multiplied, has the other f)
+                                float2 y = __ffma2_rn(xf, make_float2(sl2, sl2), l);
                                 y.x = ex2_approx(y.x);
                                 y.y = ex2_approx(y.y);
                                 if (masked) {                  // (causality alone)
@@ -830,8 +857,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                                         const float2 d = KEYS ? dc : make_float2(drow[q], drow[q]);
                                         const float2 y = __fadd2_rn(make_float2(__uint_as_float(yr[4 * j + 2 * r]), __uint_as_float(yr[4 * j + 2 * r + 1])), d);
                                         const float2 ds = __fmul2_rn(make_float2(__uint_as_float(ur[4 * j + 2 * r]), __uint_as_float(ur[4 * j + 2 * r + 1])), y);
-                                        da[q][cj / 4] *= ds.x;
-                                        da[q][cj / 4 + 1] *= ds.y;
+                                        da[q][cj / 8] = __fmul2_rn(da[q][cj / 8], ds);
                                         pk[hf][2 * j + r] = pack_bf16x2(ds.x, ds.y);
                                     }
                                 }
@@ -852,7 +878,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                                     const float4 v = gc[e];
 #pragma unroll
                                     for (int q = 0; q < 4; ++q) {
-                                        const float a = da[q][cj / 4 + i];
+                                        const float a = i ? da[q][cj / 8].y : da[q][cj / 8].x;
                                         const float2 lo = __ffma2_rn(make_float2(a, a), make_float2(v.x, v.y), make_float2(dg[q][4 * e], dg[q][4 * e + 1]));
                                         const float2 hi = __ffma2_rn(make_float2(a, a), make_float2(v.z, v.w), make_float2(dg[q][4 * e + 2], dg[q][4 * e + 3]));
                                         dg[q][4 * e] = lo.x; dg[q][4 * e + 1] = lo.y; dg[q][4 * e + 2] = hi.x; dg[q][4 * e + 3] = hi.y;
@@ -906,6 +932,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                     for (int e = 0; e < LD; ++e) {
                         dg[q][e] += __shfl_xor_sync(0xffffffffu, dg[q][e], 1);
                         dg[q][e] += __shfl_xor_sync(0xffffffffu, dg[q][e], 2);
+                        dg[q][e] *= p.scale * p.lambda;
                     }
                 }
                 float* const x = reinterpret_cast<float*>(smem_raw + C::OFF_C) + (threadIdx.x & 127);       // [e][thread]: lane t has row t / 4 + 8 (t % 4)

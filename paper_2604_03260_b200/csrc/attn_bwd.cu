@@ -15,13 +15,13 @@ namespace focus {
 // beyond every score): what the passes over keys add to their products.  With masks, which queries of the tile are members of each group.
 // A block per (head, tile):
 // D / 8 threads a row, every 16-byte piece of the tile asked for at once.  Behind those, with the gate, a block per tile of a sequence: terms of
-// its assignments (`depth` > 0), of the rows times `by` and of the columns: in the order of the products lo hi, hi lo, mid mid, mid hi, hi mid,
-// hi hi (the smallest first).
+// its assignments, of the rows times `by` and of the columns: in the order of the products lo hi, hi lo, mid mid, mid hi, hi mid,
+// hi hi (the smallest first); and the columns' assignments as they are, in the order in which they are read.
 template <int D>
 __global__ void __launch_bounds__(256)
 bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn, const __nv_bfloat16* dO, int64_t d_sb, int64_t d_sh, int64_t d_sn,
                 const float* lse, int Hq, int n, int nt, const uint32_t* mq, int K, float sl2, float* stat, __nv_bfloat16* aug, uint32_t* qbits, int own, const float* g, float by,
-                int ld, int depth, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols) {
+                int ld, int depth, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols, float* g_flat) {
     __shared__ float sl[128], sd[128];
     constexpr int TPR = D / 8, RPP = 256 / TPR, U = D == 256 ? 8 : 128 / RPP;       // threads a row, rows a turn, turns at once
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -50,6 +50,10 @@ bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn
                                   : reinterpret_cast<uint4*>(g_rows) + ((size_t)bt * (depth / 8) + ch) * 128 + r;
             *to = make_uint4(w[0], w[1], w[2], w[3]);
         }
+        if (col)
+            for (int e = 0; e < ld / 4; ++e)
+                reinterpret_cast<float4*>(g_flat)[(((size_t)bt * 16 + r / 8) * 2 + r % 2) * ld + e * 4 + r % 8 / 2] =
+                    i < n ? reinterpret_cast<const float4*>(gp)[e] : make_float4(0.f, 0.f, 0.f, 0.f);
         return;
     }
     float* const t = stat + (size_t)blockIdx.x * 256;
@@ -111,12 +115,13 @@ bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn
 }
 
 template <int D>
-static int launch_bwd_rows(const AttnBwdArgs& a, int nt, float* stat, __nv_bfloat16* aug, uint32_t* qbits, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols, cudaStream_t st) {
+static int launch_bwd_rows(const AttnBwdArgs& a, int nt, float* stat, __nv_bfloat16* aug, uint32_t* qbits, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols, float* g_flat,
+                           cudaStream_t st) {
     auto kern = bwd_rows_kernel<D>;
     const int own = a.s.batch * a.s.Hq * nt, ld = focus_soft_ld(a.s.K);
     return check_cuda(launch_dependent(kern, dim3((unsigned)(own + (g_rows ? a.s.batch * nt : 0))), dim3(256), 0, st, (const __nv_bfloat16*)a.o.ptr, a.o.stride_b, a.o.stride_h,
                                        a.o.stride_n, (const __nv_bfloat16*)a.dO.ptr, a.dO.stride_b, a.dO.stride_h, a.dO.stride_n, a.lse, a.s.Hq, a.s.n, nt,
-                                       a.tiles ? a.mq : nullptr, a.s.K, a.scale * LOG2E, stat, aug, qbits, own, a.g, -a.lambda * LOG2E, ld, g_rows ? gate_depth(ld) : 0, g_rows, g_cols),
+                                       a.tiles ? a.mq : nullptr, a.s.K, a.scale * LOG2E, stat, aug, qbits, own, a.g, -a.lambda * LOG2E, ld, g_rows ? gate_depth(ld) : 0, g_rows, g_cols, g_flat),
                       "attention backward rows launch");
 }
 
@@ -135,7 +140,7 @@ bwd_gate_sum_kernel(const float* gq, const float* gk, int Hq, int Hkv, long long
 }
 
 struct BwdWorkspace {
-    size_t stat, aug, qbits, gq, gk, g_rows, g_cols, bytes;
+    size_t stat, aug, qbits, gq, gk, g_rows, g_cols, g_flat, bytes;
 };
 static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
     const size_t HQ = (size_t)s->batch * s->Hq, HK = (size_t)s->batch * s->Hkv, nt = cdiv(s->n, 128), row = (size_t)s->n * focus_soft_ld(s->K) * 4;
@@ -150,6 +155,7 @@ static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
     const size_t terms = gate && s->D != 256 ? (size_t)s->batch * nt * 128 * gate_depth(focus_soft_ld(s->K)) * 2 : 0;
     w.g_rows = take(terms);
     w.g_cols = take(terms);
+    w.g_flat = take(terms ? (size_t)s->batch * nt * 128 * focus_soft_ld(s->K) * 4 : 0);
     w.bytes = off;
     return w;
 }
@@ -167,9 +173,10 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st) {
     const bool terms = a.g && s.D != 256;
     __nv_bfloat16* const g_rows = terms ? reinterpret_cast<__nv_bfloat16*>(a.ws + w.g_rows) : nullptr;
     __nv_bfloat16* const g_cols = terms ? reinterpret_cast<__nv_bfloat16*>(a.ws + w.g_cols) : nullptr;
-    int rc = s.D == 64    ? launch_bwd_rows<64>(a, nt, stat, aug, qbits, g_rows, g_cols, st)
-             : s.D == 128 ? launch_bwd_rows<128>(a, nt, stat, aug, qbits, g_rows, g_cols, st)
-                          : launch_bwd_rows<256>(a, nt, stat, aug, qbits, g_rows, g_cols, st);
+    float* const g_flat = reinterpret_cast<float*>(a.ws + w.g_flat);
+    int rc = s.D == 64    ? launch_bwd_rows<64>(a, nt, stat, aug, qbits, g_rows, g_cols, g_flat, st)
+             : s.D == 128 ? launch_bwd_rows<128>(a, nt, stat, aug, qbits, g_rows, g_cols, g_flat, st)
+                          : launch_bwd_rows<256>(a, nt, stat, aug, qbits, g_rows, g_cols, g_flat, st);
     if (rc) return rc;
     BwdParams p = {};
     p.Hq = s.Hq; p.Hkv = s.Hkv; p.G = s.Hq / s.Hkv; p.n = s.n; p.nt = nt; p.K = s.K; p.w = s.window < s.n ? s.window : s.n;
@@ -179,6 +186,7 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st) {
     p.g = a.g;
     p.g_rows = g_rows;
     p.g_cols = g_cols;
+    p.g_flat = g_flat;
     p.nkw = cdiv(nt, 32);
     p.live = a.tiles ? reinterpret_cast<const uint32_t*>(a.tiles + a.L.live) : nullptr;
     p.status = a.dev_status;

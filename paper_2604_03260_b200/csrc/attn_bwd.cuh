@@ -48,6 +48,7 @@ struct BwdParams {
     int nkw;
     const float* g;
     const __nv_bfloat16 *g_rows, *g_cols; // its terms: of the rows [batch][nt][depth / 8][128][8], of the columns [batch][2 nt][depth / 8][64][8]
+    const float* g_flat;      // and as it is [batch][2 nt][8 columns at a time][even, odd][ld / 4][4 of them][4]
     float* dg_part;           // [batch heads of the rows][n][ld]
     __nv_bfloat16 *out1, *out2;           // dV (BWD_KV, BWD_V); dK / dQ
     int64_t s1b, s1h, s1n, s2b, s2h, s2n;

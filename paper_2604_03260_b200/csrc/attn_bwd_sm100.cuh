@@ -46,28 +46,20 @@ template <uint32_t SEL> __device__ __forceinline__ uint32_t byte_signs(uint32_t 
     return y;
 }
 
-// 16 lanes x 32 columns: thread t has of lane t/4 (words 4 j, 4 j + 1) and of lane t/4 + 8 (4 j + 2, 4 j + 3) columns 8 j + 2 (t % 4) and the next
-__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
-        : "memory");
+// 16 lanes x 16 columns: thread t has of lane t/4 (words 4 j, 4 j + 1) and of lane t/4 + 8 (4 j + 2, 4 j + 3) columns 8 j + 2 (t % 4) and the next
+__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
 }
-__device__ __forceinline__ void tmem_st_frag(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
+__device__ __forceinline__ void tmem_st_frag(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-// the same 32 columns as packed pairs, 16 columns: words 2 j of lane t/4, 2 j + 1 of lane t/4 + 8, column 4 j + t % 4
-__device__ __forceinline__ void tmem_st_pairs(uint32_t taddr, const uint32_t (&r)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
-                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+// the same 16 columns as packed pairs, 8 columns: words 2 j of lane t/4, 2 j + 1 of lane t/4 + 8, column 4 j + t % 4
+__device__ __forceinline__ void tmem_st_pairs(uint32_t taddr, const uint32_t (&r)[4]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 
 template <int D, int MODE, bool CAP, int LD>
@@ -103,9 +95,12 @@ struct BwdCfg {
     // The columns' assignments, copied beside the tile; at D = 256 there is no room, they are read from L1 (one address a warp)
     static constexpr bool GATE_SMEM = LD > 0 && D != 256;
     static constexpr uint32_t GATE_BYTES = GATE_SMEM ? NCOL * LD * 4 : 0;
-    static constexpr uint32_t INFO_BYTES = STAT_BYTES + GATE_BYTES;               // one tile; two of them
+    // One tile's, and how many there are: a group's next one is on its way while it works (with two in all, for which alone 32 assignments leave
+    // room, a group waits for it some 1000 cycles a tile)
+    static constexpr uint32_t INFO_BYTES = STAT_BYTES + GATE_BYTES;
+    static constexpr int NI = D * LD >= 64 * 64 ? 2 : 4;
     static constexpr uint32_t CTL_BYTES = 1024;
-    static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - 2 * INFO_BYTES - CONST_BYTES - GR_BYTES;
+    static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - NI * INFO_BYTES - CONST_BYTES - GR_BYTES;
     // C1 of a tile is held from its X to its sum with dS, NPL tiles later, C2 for a product or two: rings of their own
     static constexpr int NFIT = ROOM / C1_BYTES > 8 ? 8 : ROOM / C1_BYTES;
     static constexpr int NG1 = 4 * C1_BYTES + 2 * C_BYTES <= ROOM ? 4 : 3 * C1_BYTES + C_BYTES <= ROOM ? 3 : 2, NG2 = (ROOM - NG1 * C1_BYTES) / C_BYTES;
@@ -116,7 +111,7 @@ struct BwdCfg {
     static constexpr int P_PARTS = LD == 0 ? 2 : 1;      // parts in which P and dS are handed over: most of a sum runs while the last are worked out
     static constexpr int PART0 = P_PARTS == 1 ? NCOL : NCOL == 128 ? 96 : 32;     // columns of the first
     static constexpr uint32_t OFF_C = NR * R_BYTES, OFF_CONST = OFF_C + NS1 * C1_BYTES + NS2 * C_BYTES, OFF_GR = OFF_CONST + CONST_BYTES, OFF_INFO = OFF_GR + GR_BYTES;
-    static constexpr uint32_t OFF_CTL = OFF_INFO + 2 * INFO_BYTES, SMEM = OFF_CTL + CTL_BYTES;
+    static constexpr uint32_t OFF_CTL = OFF_INFO + NI * INFO_BYTES, SMEM = OFF_CTL + CTL_BYTES;
     static_assert(SMEM <= 227 * 1024 && C1_BYTES % 1024 == 0, "shared memory");
     static __device__ __forceinline__ uint32_t slot_at(uint32_t s) { return s < NS1 ? s * C1_BYTES : NS1 * C1_BYTES + (s - NS1) * C_BYTES; }
     static constexpr uint32_t COL_R = NPL * NCOL;                // row tiles
@@ -127,7 +122,7 @@ struct BwdCfg {
 struct BwdCtl {
     uint64_t r_full, r_taken, acc_full, dg_full, full[8], empty[8];      // slots of C1, then of C2
     uint64_t id_full[4], id_empty[4];             // numbers of the tiles
-    uint64_t info_full[2], info_empty[2];         // what else there is of a tile
+    uint64_t info_full[4], info_empty[4];         // what else there is of a tile
     uint64_t x_full[3], x_taken[3], p_full[3][2], y_full[3], ds_full[3][2];       // by the tile's place (and part)
     uint32_t limit, tmem_base;
     int abort_flag;
@@ -229,7 +224,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         mbar_init(smem_u32(&ctl.dg_full), 128);
         for (int s = 0; s < C::NSLOT; ++s) { mbar_init(smem_u32(&ctl.full[s]), 1); mbar_init(smem_u32(&ctl.empty[s]), 1); }
         for (int x = 0; x < 4; ++x) { mbar_init(smem_u32(&ctl.id_full[x]), 1); mbar_init(smem_u32(&ctl.id_empty[x]), 4); }
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < C::NI; ++x) {
             mbar_init(smem_u32(&ctl.info_full[x]), 1);
             mbar_init(smem_u32(&ctl.info_empty[x]), 4);             // (the four warps of a tile)
         }
@@ -248,10 +243,6 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         for (int e = threadIdx.x; e < 512; e += BWD_THREADS)
             *reinterpret_cast<uint4*>(smem_raw + C::OFF_CONST + e * 16) = e < 128 ? make_uint4(0x3f803f80u, 0x3f80u, 0u, 0u)
                                                                           : e >= 256 && e < 384 ? make_uint4(0u, 0x3f800000u, 0x3f803f80u, 0u) : make_uint4(0u, 0u, 0u, 0u);
-        fence_proxy_async_smem();
-    }
-    if constexpr (C::GATE_SMEM) {           // (rows of assignments past the end of a sequence are not copied)
-        for (int e = threadIdx.x; e < 2 * (int)C::INFO_BYTES / 4; e += BWD_THREADS) reinterpret_cast<float*>(smem_raw + C::OFF_INFO)[e] = 0.f;
         fence_proxy_async_smem();
     }
     if (warp == 1) {
@@ -290,7 +281,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         const uint32_t slot0 = one ? 0 : C::NS1, slots = one ? C::NS1 : C::NS2;
         uint32_t slot = 0, phase = 0;
         RingAt<4> id;
-        RingAt<2> info;
+        RingAt<C::NI> info;
         // The numbers go ahead of the tiles: a group asks for its next one when it begins with a tile, and C1 of that may have to wait for it
         BwdWalk<KEYS, NCOL> ahead(p, lane, row_tile, b, h);
         int ends = one ? 0 : 2;
@@ -337,15 +328,13 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                 if (!wait(ctl.info_empty[info.slot], info.phase ^ 1, 12)) break;
                 if (lane == 0) {
                     const uint32_t bar = smem_u32(&ctl.info_full[info.slot]), at = base + C::OFF_INFO + info.slot * C::INFO_BYTES;
-                    const int rows = min(NCOL, p.n - t * NCOL);       // (a half tile may lie past the end)
-                    const uint32_t gbytes = C::GATE_SMEM && rows > 0 ? (uint32_t)rows * LD * 4 : 0u;
-                    if (C::STAT_BYTES + gbytes == 0) mbar_arrive(bar); else mbar_arrive_expect_tx(bar, C::STAT_BYTES + gbytes);
+                    mbar_arrive_expect_tx(bar, C::INFO_BYTES);
                     if constexpr (C::STAT_BYTES > 0) {
                         const float* st = p.stat + ((size_t)(b * p.Hq + hc) * p.nt + t * NCOL / 128) * 256 + t * NCOL % 128;
                         bulk_load(at, st, NCOL * 4, bar);
                         bulk_load(at + NCOL * 4, st + 128, NCOL * 4, bar);
                     }
-                    if (gbytes) bulk_load(at + C::STAT_BYTES, p.g + ((size_t)b * p.n + (size_t)t * NCOL) * (LD > 0 ? LD : 1), gbytes, bar);
+                    if constexpr (C::GATE_SMEM) bulk_load(at + C::STAT_BYTES, p.g_flat + ((size_t)b * p.nt * 2 + t) * 64 * LD, C::GATE_BYTES, bar);
                 }
                 __syncwarp();
                 info.next();
@@ -525,8 +514,6 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                 }
             }
         }
-        const float* const info = reinterpret_cast<const float*>(smem_raw + C::OFF_INFO + wg * C::INFO_BYTES);
-        const float* const gcol = reinterpret_cast<const float*>(smem_raw + C::OFF_INFO + wg * C::INFO_BYTES + C::STAT_BYTES);
         // This group's next tile, and its columns' bitmaps of the row's groups, asked for while the tile before is at work.  (The words
         // of the first two groups are joined only when they are used.)
         int ct = -1;
@@ -585,19 +572,25 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
 #pragma unroll 1
             for (; ct >= 0; ++k) {
                 const uint32_t t_x = tm + place * NCOL;
+                const uint32_t at_info = C::NI == 2 ? wg : wg + 2 * (k & 1);
+                const float* const info = reinterpret_cast<const float*>(smem_raw + C::OFF_INFO + at_info * C::INFO_BYTES);
+                const float* const gcol = info + C::STAT_BYTES / 4;
                 const int now = ct;
                 // ---- which columns count: bit c of word c / 32
                 const int col0 = now * NCOL;
-                auto gate_row = [&](int c) -> const float4* {
-                    return reinterpret_cast<const float4*>(C::GATE_SMEM ? gcol + c * LDR : p.g + ((size_t)b * p.n + min(col0 + c, p.n - 1)) * LDR);
+                // a quarter of column c + c2's assignments (in shared memory side by side for the four lanes that read at once)
+                auto gate_at = [&](int c, int e) -> float4 {
+                    if constexpr (C::GATE_SMEM) return reinterpret_cast<const float4*>(gcol)[((c / 8 * 2 + c % 2) * (LDR / 4) + e) * 4 + (lane & 3)];
+                    else return reinterpret_cast<const float4*>(p.g + ((size_t)b * p.n + min(col0 + c + c2, p.n - 1)) * LDR)[e];
                 };
                 uint32_t kw[NW];
-                bool masked;
+                bool masked, near;                             // near: some pairs of the tile are not distant
                 {
                     const int lo_q = KEYS ? col0 : row_tile * 128, hi_q = KEYS ? col0 + NCOL - 1 : row_tile * 128 + 127;
                     const int lo_k = KEYS ? row_tile * 128 : col0, hi_k = KEYS ? row_tile * 128 + 127 : col0 + NCOL - 1;
                     const bool causal = lo_q < hi_k, outside = p.bits && hi_q - lo_k > p.w;
                     masked = causal || outside;
+                    near = lo_q - hi_k <= p.w;
 #pragma unroll
                     for (int q = 0; q < NW; ++q) kw[q] = outside ? w0[q] | w1[q] : 0xffffffffu;
                     if (outside && lo_q - hi_k <= p.w) {
@@ -628,7 +621,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                 // ---- what comes after this tile
                 if (!peek(k + 1)) break;
                 // ---- P
-                if (C::INFO_BYTES > 0 && !wait(ctl.info_full[wg], k & 1, 38)) break;
+                if (C::INFO_BYTES > 0 && !wait(ctl.info_full[at_info], (C::NI == 2 ? k : k >> 1) & 1, 38)) break;
                 if (!wait(ctl.x_full[place], par, 30)) break;
                 tc_fence_after();
                 if constexpr (LD == 0) {
@@ -748,41 +741,51 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                         bound[q] = KEYS ? last[q] + p.w : last[q] - p.w;
                     }
 #pragma unroll
-                    for (int c = 0; c < NCOL; c += 32) {
-                        uint32_t xr[2][16];
+                    for (int c = 0; c < NCOL; c += 16) {
+                        uint32_t xr[2][8];
                         tmem_ld_frag(t_x + c, xr[0]);
                         tmem_ld_frag(t_x + HALF + c, xr[1]);
-                        uint32_t gx[2][C::GM ? 16 : 1];
+                        uint32_t gx[2][C::GM ? 8 : 1];
                         if constexpr (C::GM) {
                             tmem_ld_frag(t_u + c, gx[0]);
                             tmem_ld_frag(t_u + HALF + c, gx[1]);
                         }
                         tmem_wait_ld();
-                        if (!C::HAS_V && c + 32 == NCOL) {
+                        if (C::GM && near) {                   // pairs that are not distant: f = 1, z = 0
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const int cj = c + 8 * (e / 2) + e % 2;
+                                    uint32_t& u = gx[q / 2][C::GM ? 4 * (e / 2) + 2 * (q % 2) + e % 2 : 0];
+                                    u = (KEYS ? cj > bound[q] : cj < bound[q]) ? u : 0xff800000u;
+                                }
+                            }
+                        }
+                        if (!C::HAS_V && c + 16 == NCOL) {
                             tc_fence_before();
                             mbar_arrive(smem_u32(&ctl.x_taken[place]));
                         }
-                        uint32_t pk[2][8];
+                        uint32_t pk[2][4];
+                        // (step by step for all 16 columns)
+                        float2 s[8], f[8], lc[2] = {};             // [j][row]; s: both columns' g_i . g_j times -lambda log2(e), then z
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
+                        for (int j = 0; j < 2; ++j) {
                             const int cj = c + 8 * j;
-                            float2 lc = make_float2(0.f, 0.f);
-                            if constexpr (KEYS) lc = *reinterpret_cast<const float2*>(info + cj + c2);
-                            float2 s[4];                       // [row]: both columns' g_i . g_j times -lambda log2(e)
+                            if constexpr (KEYS) lc[j] = *reinterpret_cast<const float2*>(info + cj + c2);
                             if constexpr (C::GM) {
 #pragma unroll
                                 for (int q = 0; q < 4; ++q)
-                                    s[q] = make_float2(__uint_as_float(gx[q / 2][4 * j + 2 * (q % 2)]), __uint_as_float(gx[q / 2][4 * j + 2 * (q % 2) + 1]));
+                                    s[4 * j + q] = make_float2(__uint_as_float(gx[q / 2][4 * j + 2 * (q % 2)]), __uint_as_float(gx[q / 2][4 * j + 2 * (q % 2) + 1]));
                             } else {
                                 float2 part[2][4];
 #pragma unroll
                                 for (int i = 0; i < 2; ++i) {
-                                    const float4* gc = gate_row(cj + c2 + i);
 #pragma unroll
                                     for (int q = 0; q < 4; ++q) part[i][q] = make_float2(0.f, 0.f);
 #pragma unroll
                                     for (int e = 0; e < LD / 4; ++e) {
-                                        const float4 v = gc[e];
+                                        const float4 v = gate_at(cj + i, e);
 #pragma unroll
                                         for (int q = 0; q < 4; ++q) {
                                             part[i][q] = __ffma2_rn(make_float2(gr[q][4 * e], gr[q][4 * e + 1]), make_float2(v.x, v.y), part[i][q]);
@@ -791,34 +794,58 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                                     }
                                 }
 #pragma unroll
-                                for (int q = 0; q < 4; ++q) s[q] = make_float2(part[0][q].x + part[0][q].y, part[1][q].x + part[1][q].y);
+                                for (int q = 0; q < 4; ++q) {
+                                    s[4 * j + q] = make_float2(part[0][q].x + part[0][q].y, part[1][q].x + part[1][q].y);
+                                    if (!(KEYS ? cj > bound[q] : cj < bound[q])) s[4 * j + q].x = -INFINITY;
+                                    if (!(KEYS ? cj + 1 > bound[q] : cj + 1 < bound[q])) s[4 * j + q].y = -INFINITY;
+                                }
                             }
+                        }
+                        // sigmoid of a distant pair: 1 / (1 + z), z = exp(-lambda g_i . g_j); 1 - f = z f
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            s[e].x = ex2_approx(fminf(s[e].x, 126.f));
+                            s[e].y = ex2_approx(fminf(s[e].y, 126.f));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            f[e] = __fadd2_rn(s[e], make_float2(1.f, 1.f));
+                            f[e].x = rcp_approx(f[e].x);
+                            f[e].y = rcp_approx(f[e].y);
+                        }
+                        float2 y[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int j = e / 4, q = e % 4;
+                            const uint32_t* const u = &xr[q / 2][4 * j + 2 * (q % 2)];
+                            const float2 xf = __fmul2_rn(make_float2(__uint_as_float(u[0]), __uint_as_float(u[1])), f[e]);
+                            da[q][c / 8 + j] = __fmul2_rn(s[e], xf);            // (dS, by which it is multiplied, has the other f)
+                            y[e] = __ffma2_rn(xf, make_float2(sl2, sl2), KEYS ? lc[j] : make_float2(lrow[q], lrow[q]));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            y[e].x = ex2_approx(y[e].x);
+                            y[e].y = ex2_approx(y[e].y);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int j = e / 4, q = e % 4, hf = q / 2, r = q % 2;
+                            if constexpr (C::HAS_V) pk[hf][2 * j + r] = pack_bf16x2(y[e].x, y[e].y);
+                            const float2 u = __fmul2_rn(y[e], f[e]);
+                            xr[hf][4 * j + 2 * r] = __float_as_uint(u.x);
+                            xr[hf][4 * j + 2 * r + 1] = __float_as_uint(u.y);
+                        }
+                        if (masked) {                          // (causality alone)
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
-                                const int hf = q / 2, r = q % 2;
-                                uint32_t &u0 = xr[hf][4 * j + 2 * r], &u1 = xr[hf][4 * j + 2 * r + 1];
-                                const float2 x = make_float2(__uint_as_float(u0), __uint_as_float(u1));
-                                const float2 l = KEYS ? lc : make_float2(lrow[q], lrow[q]);
-                                // sigmoid of a distant pair: 1 / (1 + z), z = exp(-lambda g_i . g_j); 1 - f = z f
-                                float2 z, f;
-                                z.x = (KEYS ? cj > bound[q] : cj < bound[q]) ? ex2_approx(fminf(s[q].x, 126.f)) : 0.f;
-                                z.y = (KEYS ? cj + 1 > bound[q] : cj + 1 < bound[q]) ? ex2_approx(fminf(s[q].y, 126.f)) : 0.f;
-                                f = __fadd2_rn(z, make_float2(1.f, 1.f));
-                                f.x = rcp_approx(f.x);
-                                f.y = rcp_approx(f.y);
-                                const float2 xf = __fmul2_rn(x, f);
-                                da[q][cj / 8] = __fmul2_rn(z, xf);             // (dS, by which it is multiplied, has the other f)
-                                float2 y = __ffma2_rn(xf, make_float2(sl2, sl2), l);
-                                y.x = ex2_approx(y.x);
-                                y.y = ex2_approx(y.y);
-                                if (masked) {                  // (causality alone)
-                                    y.x = (KEYS ? cj >= last[q] : cj <= last[q]) ? y.x : 0.f;
-                                    y.y = (KEYS ? cj + 1 >= last[q] : cj + 1 <= last[q]) ? y.y : 0.f;
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    const int cj = c + 8 * j, hf = q / 2, w = 2 * j + q % 2;
+                                    const bool k0 = KEYS ? cj >= last[q] : cj <= last[q], k1 = KEYS ? cj + 1 >= last[q] : cj + 1 <= last[q];
+                                    xr[hf][2 * w] = k0 ? xr[hf][2 * w] : 0u;
+                                    xr[hf][2 * w + 1] = k1 ? xr[hf][2 * w + 1] : 0u;
+                                    if constexpr (C::HAS_V) pk[hf][w] &= (k0 ? 0xffffu : 0u) | (k1 ? 0xffff0000u : 0u);
                                 }
-                                if constexpr (C::HAS_V) pk[hf][2 * j + r] = pack_bf16x2(y.x, y.y);
-                                y = __fmul2_rn(y, f);
-                                u0 = __float_as_uint(y.x);
-                                u1 = __float_as_uint(y.y);
                             }
                         }
                         if constexpr (C::HAS_DS) {
@@ -838,16 +865,16 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                         if (!wait(ctl.y_full[place], par, 31)) break;
                         tc_fence_after();
 #pragma unroll
-                        for (int c = 0; c < NCOL; c += 32) {
-                            uint32_t pk[2][8];
+                        for (int c = 0; c < NCOL; c += 16) {
+                            uint32_t pk[2][4];
 #pragma unroll
                             for (int hf = 0; hf < 2; ++hf) {
-                                uint32_t yr[16], ur[16];
+                                uint32_t yr[8], ur[8];
                                 tmem_ld_frag(t_x + hf * HALF + c, yr);
                                 tmem_ld_frag(t_u + hf * HALF + c, ur);
                                 tmem_wait_ld();
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) {
+                                for (int j = 0; j < 2; ++j) {
                                     const int cj = c + 8 * j;
                                     float2 dc = make_float2(0.f, 0.f);
                                     if constexpr (KEYS) dc = *reinterpret_cast<const float2*>(info + NCOL + cj + c2);
@@ -872,10 +899,9 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                         for (int cj = 0; cj < NCOL; cj += 8) {
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                const float4* gc = gate_row(cj + c2 + i);
 #pragma unroll
                                 for (int e = 0; e < LD / 4; ++e) {
-                                    const float4 v = gc[e];
+                                    const float4 v = gate_at(cj + i, e);
 #pragma unroll
                                     for (int q = 0; q < 4; ++q) {
                                         const float a = i ? da[q][cj / 8].y : da[q][cj / 8].x;
@@ -889,7 +915,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                     }
                 }
                 __syncwarp();
-                if (C::INFO_BYTES > 0 && lane == 0) mbar_arrive(smem_u32(&ctl.info_empty[wg]));
+                if (C::INFO_BYTES > 0 && lane == 0) mbar_arrive(smem_u32(&ctl.info_empty[at_info]));
                 place += 2;
                 if (place >= C::NPL) { place -= C::NPL; par ^= 1; }
             }

@@ -619,7 +619,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                     }
                 };
                 // ---- what comes after this tile
-                if (!peek(k + 1)) break;
+                if (LD == 0 && !peek(k + 1)) break;
                 // ---- P
                 if (C::INFO_BYTES > 0 && !wait(ctl.info_full[at_info], (C::NI == 2 ? k : k >> 1) & 1, 38)) break;
                 if (!wait(ctl.x_full[place], par, 30)) break;
@@ -860,6 +860,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                     tmem_wait_st();
                     tc_fence_before();
                     if constexpr (C::HAS_V) mbar_arrive(smem_u32(&ctl.p_full[place][0]));
+                    if (!peek(k + 1)) break;                   // (a number alone: while Y is on its way)
                     // ---- dS
                     if constexpr (C::HAS_DS) {
                         if (!wait(ctl.y_full[place], par, 31)) break;

@@ -512,12 +512,14 @@ FOCUS_API int focus_sinkhorn_bwd(const focus_shape* shape, const float* scores, 
  *   ws          device scratch of focus_attn_bwd_workspace_bytes(shape) bytes, 16-byte aligned; contents need not be preserved between
  *               calls, calls that may overlap need one each
  *   dev_status  device int32[4], nullable, as for focus_attn_fwd
+ * FOCUS_ERR_UNSUPPORTED: batch*Hq above 65535, a scale above 0 but below 2^-100.
  *
  * focus_gate_attn_bwd -- the derivative of focus_gate_attn_fwd: those of q, k, v and of the soft assignments,
  *     da_ij = ds_ij scale q_i.k_j lambda f (1 - f), f = sigmoid(lambda g_i.g_j), over the distant pairs of all heads;
  *     dg_i += da_ij g_j,  dg_j += da_ij g_i
  * with the sums of dg in fp32 throughout and f from exp (no tanh approximation).
- *   g, lambda   as for the forward pass
+ *   shape       as for the forward pass: softcap 0, K <= 32 (K <= 16 at D = 256)
+ *   g, lambda   as for the forward pass; lambda finite
  *   dg          device fp32 [batch, n, ld], overwritten; entries g >= K are written as 0; 16-byte aligned
  */
 FOCUS_API size_t focus_attn_bwd_workspace_bytes(const focus_shape* shape);
@@ -537,9 +539,9 @@ FOCUS_API int focus_gate_attn_bwd(const focus_shape* shape, focus_tensor q, focu
  *   shape, h, strides, d_model, d_g, Wg, C   as for focus_router_scores
  *   dscores     device fp32 [batch, n, ld], ld = focus_soft_ld(K), 16-byte aligned; entries g >= K are ignored
  *   dh          device bf16 [batch, n, d_model], strides as those of h; written; NULL: not wanted.  May be h itself, overlaps it not otherwise
- *   dWg, dC     device fp32 [d_model, d_g], [K, d_g]; overwritten.  Sums in fp32 (over blocks of tokens in fp64), in an order that depends on
- *               the shape alone
- *   ws          device scratch of focus_router_scores_bwd_workspace_bytes(shape, d_model, d_g) bytes, 16-byte aligned
+ *   dWg, dC     device fp32 [d_model, d_g], [K, d_g]; overwritten.  Sums in fp32, in an order that depends on the shape alone
+ *   ws          device scratch of focus_router_scores_bwd_workspace_bytes(shape, d_model, d_g) bytes, 16-byte aligned; as for focus_attn_bwd
+ * FOCUS_ERR_UNSUPPORTED: d_model above 2^20, d_g above 2^16, more than 2^31 tokens, more than 65535 sequences.
  */
 FOCUS_API size_t focus_router_scores_bwd_workspace_bytes(const focus_shape* shape, int32_t d_model, int32_t d_g);
 FOCUS_API int focus_router_scores_bwd(const focus_shape* shape, const void* h, int64_t stride_b, int64_t stride_n, int32_t d_model,
@@ -548,12 +550,14 @@ FOCUS_API int focus_router_scores_bwd(const focus_shape* shape, const void* h, i
 
 /*
  * focus_grad_clip -- norm = sqrt(sum of the squares of all numbers of all tensors); every tensor times max_norm / norm where the norm is
- * above max_norm, as it is otherwise.  A norm that is not finite is reported and the tensors are left as they are.
+ * above max_norm, as it is otherwise.  A norm that is not finite in fp32 is reported so, and the
+ * tensors are left as they are.
  *   grads       host array of `count` tensors (read during the call): src, dst device, `count` numbers each, contiguous, of type
- *               FOCUS_GRAD_F32 or FOCUS_GRAD_BF16, aligned to a number; dst may be src and overlaps no tensor otherwise
+ *               FOCUS_GRAD_F32 or FOCUS_GRAD_BF16, aligned to a number; dst may be src and overlaps no tensor otherwise (so no
+ *               tensor is listed twice with itself as dst)
  *   max_norm    >= 0; infinity: nothing is scaled
  *   norm_out    device fp32, or NULL
- *   ws          device scratch of focus_grad_clip_workspace_bytes() bytes, 16-byte aligned
+ *   ws          device scratch of focus_grad_clip_workspace_bytes() bytes, 16-byte aligned; calls that may overlap need one each
  * Squares of numbers whose fp32 square overflows or is tiny are taken in fp64; sums in an order that depends on the sizes alone.
  */
 #define FOCUS_GRAD_F32 0

@@ -583,6 +583,8 @@ def make_grad_list(grads, out=None):
         assert s.is_cuda and s.dtype in kinds and s.is_contiguous(), (s.dtype, tuple(s.shape), s.stride())
         assert d.dtype is s.dtype and d.device == s.device and d.is_contiguous() and d.numel() == s.numel(), (d.dtype, tuple(d.shape), d.stride())
         e.src, e.dst, e.count, e.dtype = s.data_ptr(), d.data_ptr(), s.numel(), kinds[s.dtype]
+    written = [d.data_ptr() for d in out if d.numel()]
+    assert len(set(written)) == len(written), "a tensor is listed twice"
     c = focus_grads(C.addressof(entries), len(grads))
     c.tensors = (entries, grads, out)
     return c

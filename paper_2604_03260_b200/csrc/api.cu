@@ -645,6 +645,7 @@ static int attn_bwd_args(AttnBwdArgs& a, size_t ws_bytes) {
     if (ws_bytes < need) return fail(FOCUS_ERR_CAPACITY, "attention backward workspace has %zu bytes, %zu needed", ws_bytes, need);
     if ((uintptr_t)a.dev_status % 4) return fail(FOCUS_ERR_INVALID_ARG, "dev_status must be 4-byte aligned");
     a.scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)shape->D);
+    if (a.scale < 0x1p-100f) return fail(FOCUS_ERR_UNSUPPORTED, "scale (%g) below 2^-100", (double)a.scale);      // (lse / scale has to be a number)
     return FOCUS_OK;
 }
 

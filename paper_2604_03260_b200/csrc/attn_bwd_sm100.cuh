@@ -3,13 +3,18 @@
 //   warp 3        C2 of every tile into another ring; lse, delta and assignments of the columns
 //   warps 1, 2    MMA issuers: X = R1 C1^T, Y = R2 C2^T (operands in shared memory), and the sums with P or dS (bf16, tensor memory) as the
 //                 first operand and C2 or C1 read along its other dimension as the second.  Warp 1 what C2 is for, warp 2 what C1 is for.
-//                 (One warp for both: 2360 cycles a tile of dQ at D = 128 with nothing else to wait for, where the products take 1630: a wait and
-//                 what comes with it is some 150 cycles even where it need not wait, and what has been issued before lasts little longer.)
+//                 (One warp for both, when it was so: 2360 cycles a tile of dQ at D = 128 with nothing else to wait for, where the products take
+//                 1540: a wait and what comes with it is some 150 cycles even where it need not wait.)
 //   warps 4-7     P = exp2(X - lse), dS = P (Y - delta) of the even tiles, a thread a row
 //   warps 8-11    of the odd ones
 // The tensor pipe works in order, so a product may be issued into the place of an operand that an earlier one reads.  Two tiles are at work
-// at a time: while one group of warps takes exponentials the other waits for, or works on, the other tile's products.  With both groups on
-// the halves of one tile a tile took the sum of what both phases wait for (D = 128: 3300 and 2650 cycles for the two passes).
+// at a time: while one group of warps takes exponentials the other waits for, or works on, the other tile's products.  (Both groups on the halves
+// of one tile, when it was so: a tile took the sum of what both phases wait for, 8/2 heads x 16384 tokens 1751 us.)
+//
+// What bounds it: at D = 64 and 128 the chain of a tile, X - exponentials - Y - dS - sum, of which two are under way: 128 x 128 pairs of dK and dV take
+// 3100 cycles at D = 128 (products alone 2048), of dQ 2200 (1536).  8/2 heads x 16384 tokens, D = 128, every causal pair: 1605 us, 856 TFLOP/s on the five
+// products that the formulas need (seven are done); 32/8 x 8192, K = 4, top-2: 1731; D = 256 with a cap, 16/8 x 4096: 555.  With the gate, the special
+// functions: three a pair and pass, 16 a clock, and what each group's 64 columns wait for before and after; 32/8 x 4096, K = 8: 891 us.
 //
 // Tensor memory: the sums, and two or three places for the tiles at work.  A tile has one place: X, P over it, Y when X (and the sum with P)
 // is through, dS over that.  With three places the X of a group's next tile is there before it is done with the one before.
@@ -86,7 +91,8 @@ struct BwdCfg {
     static constexpr bool AUG = KEYS && !CAP && LD == 0 && !(D == 256 && MODE == BWD_K);
     static constexpr uint32_t AUG_BYTES = AUG ? NCOL * 16 : 0, CONST_BYTES = AUG ? 4 * 2048 : 0;        // (ones for X, zeros, ones for Y, zeros)
     // The gate's g_i . g_j times -lambda log2(e), from the tensor cores too: both sides in three bf16 terms, the six products of terms above 2^-24 side
-    // by side in GK steps' depth.  The columns' come with C1, behind it.  (At D = 256 there is no room: by instructions.)
+    // by side in GK numbers' depth.  The columns' come with C1, behind it.  (32/8 heads x 4096 tokens, K = 8, D = 128: 1241 us by instructions, 1037 so.
+    // At D = 256 there is no room for them.)
     static constexpr bool GM = LD > 0 && D != 256;
     static constexpr int GK = GM ? gate_depth(LD) : 0;
     static constexpr uint32_t GC_BYTES = GK * NCOL * 2, GR_BYTES = GK * 256;
@@ -486,8 +492,8 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         const float sl2 = CAP ? p.softcap * LOG2E : p.scale * LOG2E;
         const float cap_in = CAP ? p.scale / p.softcap : 0.f;
         // A thread has a row.  With the gate, which needs a column's assignment for every pair, it has four rows, 8 apart, and of every 8 columns
-        // two, so that what goes by the column is read once for four rows (tensor memory gives a row a thread faster, which counts otherwise:
-        // 3390 cycles a tile of dK and dV at D = 128 with four rows, 3130 so).
+        // two, so that what goes by the column is read once for four rows.  (Without the gate: tensor memory gives a row a thread faster, 3130 cycles a
+        // tile of dK and dV at D = 128 where four rows a thread took 3390.)
         const int l4 = lane >> 2, c2 = 2 * (lane & 3);     // row (of each 8) and first column (of each 8)
         const int rowq = row_tile * 128 + (warp & 3) * 32 + l4;        // its rows: rowq + 8 q
         constexpr int ROWS = LD > 0 ? 4 : 1;
@@ -524,7 +530,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
             ct = *(volatile int*)&ctl.tile[slot];
             const int hc = *(volatile int*)&ctl.head[slot];
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl.id_empty[slot]));
+            if (lane == 0 && (ct | hc) >= -1) mbar_arrive(smem_u32(&ctl.id_empty[slot]));      // (always so: but not known before the two are there)
 #pragma unroll
             for (int q = 0; q < NW; ++q) w0[q] = w1[q] = 0u;
             const int lo_k = KEYS ? row_tile * 128 : ct * NCOL, hi_q = KEYS ? ct * NCOL + NCOL - 1 : row_tile * 128 + 127;
@@ -915,6 +921,10 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                         }
                     }
                 }
+                // Every read of the assignments has to be through before the next copy over them is asked for.  The arrival alone, one lane's behind
+                // __syncwarp() or, tried too, every thread's own, does not wait for the last read's answer (D = 64, K = 4: dg of some rows with the numbers of the
+                // tile after next); what else is read here goes into dS, which has been handed over.
+                if constexpr (C::GATE_SMEM) __threadfence_block();
                 __syncwarp();
                 if (C::INFO_BYTES > 0 && lane == 0) mbar_arrive(smem_u32(&ctl.info_empty[at_info]));
                 place += 2;
@@ -995,7 +1005,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
 }
 
 // All passes in one launch: they need nothing of one another, and the blocks of one fill the places that the other's last ones leave
-// (32 query on 8 KV heads x 8192 tokens: TODO).  Tensor maps of q, k, v and do, first for row tiles, then for column tiles.
+// (32 query on 8 KV heads x 8192 tokens 1801 -> 1753 us, 12 heads x 1024 34 -> 21).  Tensor maps of q, k, v and do, first for row tiles, then for column tiles.
 struct BwdMaps {
     CUtensorMap r[4], c[4];
 };

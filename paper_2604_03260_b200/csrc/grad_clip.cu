@@ -137,14 +137,17 @@ __global__ void __launch_bounds__(256, 4) clip_scale_kernel(const __grid_constan
     for (int e = threadIdx.x; e < blocks; e += 256) x += sums[e];
     const double norm = sqrt(block_sum(x, s));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-    const float f = norm > bound && isfinite(norm) ? (float)(bound / norm) : 1.f;       // (what is not finite is left to the caller)
+    const double by = norm > bound && isfinite((float)norm) ? bound / norm : 1.0;       // (what is reported as not finite is left to the caller)
+    // a factor below fp32's normal numbers would have lost bits: in two steps, the second one exact
+    const bool tiny = by < 0x1p-126;
+    const float f = (float)(tiny ? by * 0x1p64 : by), f2 = tiny ? 0x1p-64f : 1.f;
     const int total = t.first[t.tensors];
     for (int chunk = total - 1 - (int)blockIdx.x; chunk >= 0; chunk -= gridDim.x) {
         const ClipChunk c = clip_chunk(t, chunk);
-        if (f == 1.f && c.src == c.dst) continue;
+        if (by == 1.0 && c.src == c.dst) continue;
         const int size = c.half ? 2 : 4;
         auto one = [&](long long e) {
-            const float v = clip_number(c.src, e, c.half) * f;
+            const float v = clip_number(c.src, e, c.half) * f * f2;
             if (c.half) reinterpret_cast<__nv_bfloat16*>(c.dst)[e] = __float2bfloat16_rn(v);
             else reinterpret_cast<float*>(c.dst)[e] = v;
         };
@@ -168,10 +171,10 @@ __global__ void __launch_bounds__(256, 4) clip_scale_kernel(const __grid_constan
                 for (int e = 0; e < 4; ++e) {
                     if (c.half) {
                         const float2 y = clip_pair(v[e]);
-                        const __nv_bfloat162 z = __floats2bfloat162_rn(y.x * f, y.y * f);
+                        const __nv_bfloat162 z = __floats2bfloat162_rn(y.x * f * f2, y.y * f * f2);
                         v[e] = *reinterpret_cast<const uint32_t*>(&z);
                     } else {
-                        v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
+                        v[e] = __float_as_uint(__uint_as_float(v[e]) * f * f2);
                     }
                 }
                 if (i + 256 * u < pieces) q[i + 256 * u] = w[u];

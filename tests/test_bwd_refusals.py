@@ -90,3 +90,8 @@ def test_clip_entries(entry, status):
 def test_clip():
     assert clip([], count=-1) == -1 and fb.lib().focus_grad_clip(None, 3, 1.0, None, A, 1 << 20, None) == -1
     assert clip([], bound=-1.0) == -1 and clip([], bound=float("nan")) == -1 and clip([], norm=A + 2) == -1 and clip([], ws=None) == -1 and clip([], ws=A + 8) == -1 and clip([], size=8) == -3
+
+
+def test_scales_that_lse_cannot_be_divided_by():
+    assert attn_args(shape(scale=2.0 ** -101), False) == -2 and attn_args(shape(scale=2.0 ** -101), True) == -2
+    assert attn_args(shape(scale=2.0 ** -100), False, size=1000) == -3

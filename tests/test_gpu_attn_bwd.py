@@ -248,3 +248,16 @@ def test_behind_the_forward_kernels():
     fb.focus_attn_fwd(shape, t["q"], t["k"], t["v"], mq, mk, tiles, 0, t["o"], t["lse"], status)
     got = run_bwd(shape, t, mq, mk, tiles, status=status)
     plain.check(got, plain.backward(*(t[x] for x in ("q", "k", "v", "o", "lse", "do")), D ** -0.5, window, keep=plain.shared(mq, mk, 2)))
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n,D,K", [(1, 2, 1, 9000, 64, 4), (1, 2, 1, 5000, 64, 8), (1, 2, 1, 5000, 128, 4), (1, 2, 1, 3000, 128, 32), (1, 2, 1, 3000, 256, 8), (4, 12, 12, 1000, 64, 4)])
+def test_gate_same_bits_every_time(B, Hq, Hkv, n, D, K):
+    t, gen = make(B, Hq, Hkv, n, D, 3)
+    shape = fb.make_shape(Hq, Hkv, n, D, K, 1, 64, batch=B)
+    g = torch.softmax(torch.randn((B, n, K), generator=gen, device="cuda"), -1)
+    t["o"], t["lse"] = torch.empty_like(t["q"]), torch.empty((B, Hq, n), device="cuda")
+    fb.focus_gate_attn_fwd(shape, t["q"], t["k"], t["v"], g, 5.0, t["o"], t["lse"])
+    first = run_bwd(shape, t, g=g, lam=5.0)
+    for _ in range(8):
+        again = run_bwd(shape, t, g=g, lam=5.0)
+        assert all(torch.equal(first[x], again[x]) for x in first)

@@ -110,3 +110,20 @@ def test_same_bits_captured_and_on_two_streams():
     graph.replay()
     torch.cuda.synchronize()
     assert norms[0].item() == want and all(torch.equal(x, y) for x, y in zip(oa, wa))
+
+
+def test_a_factor_below_normal_numbers_loses_nothing():
+    check(tensors([60, 41], scale=3e37), 1e-3)
+
+
+def test_a_norm_beyond_fp32_is_reported_so_and_left():
+    g = [torch.full((1000,), 1e38, device="cuda")]
+    assert clip(g, 1.0) == math.inf and (g[0] == 1e38).all()
+
+
+def test_a_tensor_listed_twice_is_refused():
+    x = torch.ones(8, device="cuda")
+    with pytest.raises(AssertionError, match="twice"):
+        fb.make_grad_list([x, x])
+    fb.make_grad_list([x, x], [torch.empty_like(x) for _ in range(2)])
+    fb.make_grad_list([torch.empty(0, device="cuda")] * 2)

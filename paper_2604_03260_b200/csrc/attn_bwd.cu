@@ -14,30 +14,31 @@ namespace focus {
 // first, so that every probability is 0.  The same as six bf16 numbers a row (the first divided by scale log2(e), in place of -inf a number
 // beyond every score): what the passes over keys add to their products.  With masks, which queries of the tile are members of each group.
 // A block per (head, tile):
-// D / 8 threads a row, every 16-byte piece of the tile asked for at once.  Behind those, with the gate, a block per tile of a sequence: terms of
+// D / 8 threads a row, every 16-byte piece of the tile asked for at once.  Before those, with the gate, a block per tile of a sequence: terms of
 // its assignments, of the rows times `by` and of the columns: in the order of the products lo hi, hi lo, mid mid, mid hi, hi mid,
 // hi hi (the smallest first); and the columns' assignments as they are, in the order in which they are read.
 template <int D>
 __global__ void __launch_bounds__(256)
 bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn, const __nv_bfloat16* dO, int64_t d_sb, int64_t d_sh, int64_t d_sn,
-                const float* lse, int Hq, int n, int nt, const uint32_t* mq, int K, float sl2, float* stat, __nv_bfloat16* aug, uint32_t* qbits, int own, const float* g, float by,
-                int ld, int depth, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols, float* g_flat) {
+                const float* lse, int Hq, int n, int nt, const uint32_t* mq, int K, float sl2, float* stat, __nv_bfloat16* aug, uint32_t* qbits, int lead, const float* g, float by,
+                int log_ld, int depth, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols, float* g_flat) {
     __shared__ float sl[128], sd[128];
     constexpr int TPR = D / 8, RPP = 256 / TPR, U = D == 256 ? 8 : 128 / RPP;       // threads a row, rows a turn, turns at once
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int hq = blockIdx.x / nt, tile = blockIdx.x % nt, b = hq / Hq, h = hq % Hq, i0 = tile * 128;
+    const int block = (int)blockIdx.x - lead, hq = block / nt, tile = block % nt, b = hq / Hq, h = hq % Hq, i0 = tile * 128;
     dep_wait();
     dep_trigger();
-    if ((int)blockIdx.x >= own) {
-        const int bt = blockIdx.x - own, r = threadIdx.x & 127, i = bt % nt * 128 + r;
+    if (block < 0) {
+        const int bt = blockIdx.x, r = threadIdx.x & 127, i = bt % nt * 128 + r;
         const bool col = threadIdx.x >= 128;
+        const int ld = 1 << log_ld;
         const float* const gp = g + ((size_t)(bt / nt) * n + i) * ld;
         for (int ch = 0; ch < depth / 8; ++ch) {
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int at = ch * 8 + e, product = at / ld;
-                float v = i < n && product < 6 ? gp[at % ld] * (col ? 1.f : by) : 0.f;
+                const int at = ch * 8 + e, product = at >> log_ld;
+                float v = i < n && product < 6 ? gp[at & (ld - 1)] * (col ? 1.f : by) : 0.f;
                 const int term = (col ? 0x010120 : 0x001102) >> (4 * product) & 3;
                 __nv_bfloat16 y = __float2bfloat16_rn(v);
                 for (int x = 0; x < term; ++x) {
@@ -56,7 +57,7 @@ bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn
                     i < n ? reinterpret_cast<const float4*>(gp)[e] : make_float4(0.f, 0.f, 0.f, 0.f);
         return;
     }
-    float* const t = stat + (size_t)blockIdx.x * 256;
+    float* const t = stat + (size_t)block * 256;
     const int r0 = threadIdx.x / TPR, c = threadIdx.x % TPR * 8;
     const __nv_bfloat16* const ob = o + b * o_sb + h * o_sh + (int64_t)i0 * o_sn + c;
     const __nv_bfloat16* const db = dO + b * d_sb + h * d_sh + (int64_t)i0 * d_sn + c;
@@ -102,14 +103,14 @@ bwd_rows_kernel(const __nv_bfloat16* o, int64_t o_sb, int64_t o_sh, int64_t o_sn
             v[e / 3] -= __bfloat162float(y);
             w[e / 2] |= (uint32_t)__bfloat16_as_ushort(y) << (16 * (e & 1));
         }
-        reinterpret_cast<uint4*>(aug)[(size_t)blockIdx.x * 128 + threadIdx.x] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(aug)[(size_t)block * 128 + threadIdx.x] = make_uint4(w[0], w[1], w[2], w[3]);
     }
     if (mq && warp < 4) {
         const int i = i0 + warp * 32 + lane;
         const uint32_t m = i < n ? mq[(size_t)hq * n + i] : 0u;
         for (int g = 0; g < K; ++g) {
             const uint32_t w = __ballot_sync(0xffffffffu, (m >> g) & 1u);
-            if (lane == 0) qbits[((size_t)blockIdx.x * K + g) * 4 + warp] = w;
+            if (lane == 0) qbits[((size_t)block * K + g) * 4 + warp] = w;
         }
     }
 }
@@ -118,10 +119,11 @@ template <int D>
 static int launch_bwd_rows(const AttnBwdArgs& a, int nt, float* stat, __nv_bfloat16* aug, uint32_t* qbits, __nv_bfloat16* g_rows, __nv_bfloat16* g_cols, float* g_flat,
                            cudaStream_t st) {
     auto kern = bwd_rows_kernel<D>;
-    const int own = a.s.batch * a.s.Hq * nt, ld = focus_soft_ld(a.s.K);
-    return check_cuda(launch_dependent(kern, dim3((unsigned)(own + (g_rows ? a.s.batch * nt : 0))), dim3(256), 0, st, (const __nv_bfloat16*)a.o.ptr, a.o.stride_b, a.o.stride_h,
+    const int lead = g_rows ? a.s.batch * nt : 0, ld = focus_soft_ld(a.s.K);
+    return check_cuda(launch_dependent(kern, dim3((unsigned)(lead + a.s.batch * a.s.Hq * nt)), dim3(256), 0, st, (const __nv_bfloat16*)a.o.ptr, a.o.stride_b, a.o.stride_h,
                                        a.o.stride_n, (const __nv_bfloat16*)a.dO.ptr, a.dO.stride_b, a.dO.stride_h, a.dO.stride_n, a.lse, a.s.Hq, a.s.n, nt,
-                                       a.tiles ? a.mq : nullptr, a.s.K, a.scale * LOG2E, stat, aug, qbits, own, a.g, -a.lambda * LOG2E, ld, g_rows ? gate_depth(ld) : 0, g_rows, g_cols, g_flat),
+                                       a.tiles ? a.mq : nullptr, a.s.K, a.scale * LOG2E, stat, aug, qbits, lead, a.g, -a.lambda * LOG2E, ld == 4 ? 2 : ld == 8 ? 3 : ld == 16 ? 4 : 5,
+                      g_rows ? gate_depth(ld) : 0, g_rows, g_cols, g_flat),
                       "attention backward rows launch");
 }
 
@@ -134,7 +136,9 @@ bwd_gate_sum_kernel(const float* gq, const float* gk, int Hq, int Hkv, long long
     if (e >= count) return;
     const long long b = e / row, at = e % row;
     float s = 0.f;
+#pragma unroll 16
     for (int h = 0; h < Hq; ++h) s += gq[(b * Hq + h) * row + at];
+#pragma unroll 16
     for (int h = 0; h < Hkv; ++h) s += gk[(b * Hkv + h) * row + at];
     dg[e] = (int)(at % ld) < K ? s : 0.f;
 }

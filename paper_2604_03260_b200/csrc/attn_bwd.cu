@@ -143,7 +143,61 @@ bwd_gate_sum_kernel(const float* gq, const float* gk, int Hq, int Hkv, long long
     dg[e] = (int)(at % ld) < K ? s : 0.f;
 }
 
+// dk, dv: the parts' sums of a row, in their order.  Eight columns a thread.
+__global__ void __launch_bounds__(256)
+bwd_join_kernel(const float* part1, const float* part2, int split, int Hkv, int n, int D, long long count, float scale, focus_tensor dv, focus_tensor dk) {
+    const long long e = (long long)blockIdx.x * 256 + threadIdx.x;
+    dep_wait();
+    dep_trigger();
+    if (e >= count) return;
+    const int each = D / 8, c = (int)(e % each) * 8;
+    const long long at = e / each, owner = at / n, row = at % n;
+    const long long b = owner / Hkv, h = owner % Hkv;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const float* p = (x ? part2 : part1) + ((size_t)owner * split * n + row) * D + c;
+        float s[8] = {};
+#pragma unroll 4
+        for (int i = 0; i < split; ++i, p += (size_t)n * D) {
+            const float4 u = reinterpret_cast<const float4*>(p)[0], w = reinterpret_cast<const float4*>(p)[1];
+            s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w; s[4] += w.x; s[5] += w.y; s[6] += w.z; s[7] += w.w;
+        }
+        const float by = x ? scale : 1.f;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 y = __floats2bfloat162_rn(s[2 * i] * by, s[2 * i + 1] * by);
+            w[i] = *reinterpret_cast<const uint32_t*>(&y);
+        }
+        const focus_tensor& t = x ? dk : dv;
+        *reinterpret_cast<uint4*>((__nv_bfloat16*)t.ptr + b * t.stride_b + h * t.stride_h + row * t.stride_n + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// Parts into which a KV head's query heads are cut, so that the first key tile, which has every query tile of all G heads one after another, is not
+// what the launch takes: 8/2 heads x 4000 tokens, D = 128, 258 us with one part and 136 with four, with the gate (K = 16, 4096) 634 and 347; 32/8 x 1024
+// 74 and, with two, 58.  More
+// items cost what is around an item's tiles, and a launch that joins the parts' sums (16/8 heads x 1000, D = 256: 60 with one, 81 with two).  So the
+// longest item is weighed against an SM's share, in thousands of cycles: a tile of dK and dV 3 (D = 256: 4 and 3 in two items), of dQ 2 (4), with the gate
+// 6 more, 12 (24) around an item, 6 (12) for the join.  (With every causal pair: what the masks leave out is not known here.)
+static int bwd_split(const focus_shape* s, bool gate) {
+    const double nt = cdiv(s->n, 128), tiles = nt * (nt + 1) / 2 * s->batch * s->Hq, more = gate ? 6 : 0;
+    const bool two = s->D == 256;
+    const double kv = (two ? 4 : 3) + more, q = (two ? 4 : 2) + more, second = two ? 3 + more : 0, around = two ? 24 : 12, join = two ? 12 : 6;
+    const int G = s->Hq / s->Hkv;
+    int best = 1;
+    double least = 0;
+    for (int S = 1; S <= G; ++S) {
+        if (G % S) continue;
+        const double items = nt * s->batch * ((double)s->Hkv * S * (two ? 2 : 1) + s->Hq), longest = G / S * nt * kv + around;
+        const double share = (tiles * (kv + second + q) + items * around) / 148, t = (1.15 * longest > share ? 1.15 * longest : share) + (S > 1 ? join : 0);
+        if (S == 1 || t < least) { best = S; least = t; }
+    }
+    return best;
+}
+
 struct BwdWorkspace {
+    size_t part1, part2;
     size_t stat, aug, qbits, gq, gk, g_rows, g_cols, g_flat, bytes;
 };
 static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
@@ -155,7 +209,10 @@ static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
     w.aug = take(HQ * nt * 128 * 16);
     w.qbits = gate ? 0 : take(HQ * nt * s->K * 16);
     w.gq = gate ? take(HQ * row) : 0;
-    w.gk = gate ? take(HK * row) : 0;
+    const size_t split = bwd_split(s, gate), sums = split > 1 ? HK * split * s->n * s->D * 4 : 0;
+    w.gk = gate ? take(HK * split * row) : 0;
+    w.part1 = take(sums);
+    w.part2 = take(sums);
     const size_t terms = gate && s->D != 256 ? (size_t)s->batch * nt * 128 * gate_depth(focus_soft_ld(s->K)) * 2 : 0;
     w.g_rows = take(terms);
     w.g_cols = take(terms);
@@ -196,7 +253,9 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st) {
     p.status = a.dev_status;
     auto wide = [](const focus_tensor& t) { return (uintptr_t)t.ptr % 32 == 0 && (t.stride_b | t.stride_h | t.stride_n) % 16 == 0; };
     BwdParams kv = p, q = p;
-    kv.heads = HK; kv.by_heads = Divisor(HK); kv.by_rows_H = Divisor(s.Hkv);
+    kv.split = bwd_split(&s, a.g != nullptr); kv.heads_each = p.G / kv.split; kv.by_split = Divisor(kv.split);
+    kv.heads = HK * kv.split; kv.by_heads = Divisor(kv.heads); kv.by_rows_H = Divisor(s.Hkv);
+    kv.part1 = reinterpret_cast<float*>(a.ws + w.part1); kv.part2 = reinterpret_cast<float*>(a.ws + w.part2);
     kv.row_mask = a.mk; kv.bits = a.tiles ? qbits : nullptr;
     kv.dg_part = reinterpret_cast<float*>(a.ws + w.gk);
     kv.out1 = (__nv_bfloat16*)a.dv.ptr; kv.s1b = a.dv.stride_b; kv.s1h = a.dv.stride_h; kv.s1n = a.dv.stride_n; kv.wide1 = wide(a.dv);
@@ -206,11 +265,18 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st) {
     q.dg_part = reinterpret_cast<float*>(a.ws + w.gq);
     q.out2 = (__nv_bfloat16*)a.dq.ptr; q.s2b = a.dq.stride_b; q.s2h = a.dq.stride_h; q.s2n = a.dq.stride_n; q.wide2 = wide(a.dq);
     rc = s.D == 64 ? launch_bwd_d<64>(a, kv, q, st) : s.D == 128 ? launch_bwd_d<128>(a, kv, q, st) : launch_bwd_d<256>(a, kv, q, st);
+    if (rc) return rc;
+    if (kv.split > 1) {
+        const long long count = (long long)HK * s.n * (s.D / 8);
+        if (count > 0x7fffffffll * 256) return fail(FOCUS_ERR_UNSUPPORTED, "attention backward: too many keys");
+        rc = check_cuda(launch_dependent(bwd_join_kernel, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, (const float*)kv.part1, (const float*)kv.part2, kv.split, s.Hkv, s.n,
+                                         s.D, count, a.scale, a.dv, a.dk), "attention backward join launch");
+    }
     if (rc || !a.g) return rc;
     const int ld = focus_soft_ld(s.K);
     const long long row = (long long)s.n * ld, count = row * s.batch;
     if (count > 0x7fffffffll * 256) return fail(FOCUS_ERR_UNSUPPORTED, "attention backward: too many assignments");
-    return check_cuda(launch_dependent(bwd_gate_sum_kernel, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, (const float*)q.dg_part, (const float*)kv.dg_part, s.Hq, s.Hkv,
+    return check_cuda(launch_dependent(bwd_gate_sum_kernel, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, (const float*)q.dg_part, (const float*)kv.dg_part, s.Hq, s.Hkv * kv.split,
                                        row, ld, s.K, count, a.dg), "attention backward sum launch");
 }
 

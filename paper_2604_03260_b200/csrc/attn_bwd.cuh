@@ -37,8 +37,10 @@ constexpr int gate_depth(int ld) { return (6 * ld + 15) / 16 * 16; }
 
 struct BwdParams {
     int Hq, Hkv, G, n, nt, K, w;
-    int heads;                // batch * heads of the rows
-    Divisor by_heads, by_rows_H;          // by that; by heads per sequence of the rows
+    int heads;                // batch * heads of the rows (keys: times split)
+    Divisor by_heads, by_rows_H, by_split;          // by that; by heads per sequence of the rows; by split
+    int split, heads_each;    // keys: parts of a KV head's query heads, each an item with sums of its own; query heads of a part
+    float *part1, *part2;     // those sums [batch Hkv split][n][D]: dV, dK over scale
     float scale, softcap, lambda;
     const float* stat;        // [batch Hq][nt][2][128]: -lse log2(e), -delta
     const __nv_bfloat16* aug; // [batch Hq][nt][128][8]: -lse / scale, -delta in three terms each
@@ -49,7 +51,7 @@ struct BwdParams {
     const float* g;
     const __nv_bfloat16 *g_rows, *g_cols; // its terms: of the rows [batch][nt][depth / 8][128][8], of the columns [batch][2 nt][depth / 8][64][8]
     const float* g_flat;      // and as it is [batch][2 nt][8 columns at a time][even, odd][ld / 4][4 of them][4]
-    float* dg_part;           // [batch heads of the rows][n][ld]
+    float* dg_part;           // [heads][n][ld]
     __nv_bfloat16 *out1, *out2;           // dV (BWD_KV, BWD_V); dK / dQ
     int64_t s1b, s1h, s1n, s2b, s2h, s2n;
     bool wide1, wide2;        // 32-byte stores

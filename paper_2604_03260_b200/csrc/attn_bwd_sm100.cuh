@@ -109,6 +109,10 @@ struct BwdCfg {
     static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - NI * INFO_BYTES - CONST_BYTES - GR_BYTES;
     // C1 of a tile is held from its X to its sum with dS, NPL tiles later, C2 for a product or two: rings of their own
     static constexpr int NFIT = ROOM / C1_BYTES > 8 ? 8 : ROOM / C1_BYTES;
+    // Registers of the warps that issue and of those that compute (12 heads x 4000 tokens, D = 64: K = 32 829 us with the usual ones, 709 so;
+    // 8/2 heads x 4096, K = 16, where the others have what they need, 640 and 650)
+    static constexpr int REGS_FEW = LD > 16 ? 40 : REGS_CONTROL, REGS_MANY = LD > 16 ? 232 : REGS_SOFTMAX_2WG;
+    static_assert(REGS_FEW + 2 * REGS_MANY == 3 * 168, "the launch's registers");
     static constexpr int NG1 = 4 * C1_BYTES + 2 * C_BYTES <= ROOM ? 4 : 3 * C1_BYTES + C_BYTES <= ROOM ? 3 : 2, NG2 = (ROOM - NG1 * C1_BYTES) / C_BYTES;
     static constexpr int NS1 = GM ? NG1 : MODE == BWD_V ? NFIT - NFIT / 2 : NFIT > NPL + 1 ? (NFIT + 1 > 2 * (NPL + 1) ? (NFIT + 1) / 2 : NPL + 1) : NFIT - 1;
     static constexpr int NS2 = GM ? (NG2 > 8 - NG1 ? 8 - NG1 : NG2) : NFIT - NS1, NSLOT = NS1 + NS2;
@@ -142,13 +146,14 @@ template <bool KEYS, int NCOL>
 struct BwdWalk {
     const BwdParams& p;
     const int lane;
-    int row_tile, b, h, hi, c, word;      // hi: query head of the group; c: next 128-tile; word: of 32 tiles, which are visited
+    int row_tile, b, h, hi, hi_end, c, word;      // hi: query head of the group; c: next 128-tile; word: of 32 tiles, which are visited
     uint32_t bits;
     int part = NCOL == 64 ? 1 : 0;        // halves of a 128-tile
     int at = -1;
     __device__ __forceinline__ int first_col() const { return KEYS ? row_tile : 0; }
     __device__ __forceinline__ int end_col() const { return KEYS ? p.nt : row_tile + 1; }
-    __device__ __forceinline__ BwdWalk(const BwdParams& p_, int lane_, int rt, int b_, int h_) : p(p_), lane(lane_), row_tile(rt), b(b_), h(h_), hi(0), bits(0) {
+    __device__ __forceinline__ BwdWalk(const BwdParams& p_, int lane_, int rt, int b_, int h_, int part)
+        : p(p_), lane(lane_), row_tile(rt), b(b_), h(h_), hi(part * p_.heads_each), hi_end(hi + p_.heads_each), bits(0) {
         c = first_col();
         word = c - 32;
     }
@@ -168,7 +173,7 @@ struct BwdWalk {
             }
             word += 32;
             if (word >= end_col()) {
-                if (!KEYS || ++hi >= p.G) return -1;
+                if (!KEYS || ++hi >= hi_end) return -1;
                 word = first_col();
             }
             const int t = word + lane;
@@ -197,7 +202,8 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
     // the longest items first: key tile 0, or the last query tile
     const int q0 = p.by_heads.div(block), head = block - q0 * p.heads;
     const int row_tile = KEYS ? q0 : p.nt - 1 - q0;
-    const int b = p.by_rows_H.div(head), h = head - b * (KEYS ? p.Hkv : p.Hq);
+    const int owner = KEYS ? p.by_split.div(head) : head, part = head - owner * (KEYS ? p.split : 1);       // part: of the query heads
+    const int b = p.by_rows_H.div(owner), h = owner - b * (KEYS ? p.Hkv : p.Hq);
     auto give_up = [&](int where) {
         *(volatile int*)&ctl.abort_flag = 1;
         if (p.status && atomicCAS(p.status, 0, 1) == 0) {
@@ -267,7 +273,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         constexpr int H = C::RU > 0 ? C::RU / 2 : 1;
         return base + C::OFF_C + C::slot_at(u < H ? C::NS1 - 1 : C::NSLOT - 1) + (uint32_t)(u % H) * C::SUBR;
     };
-    if (warp < 4) reg_dec<REGS_CONTROL>();
+    if (warp < 4) reg_dec<C::REGS_FEW>();
     if (warp == 0 || warp == 3) {
         // ------------------------------------------------------------------ TMA: row tiles, C1 and the tiles' numbers; C2 and what goes by the column
         const bool one = warp == 0;
@@ -282,14 +288,14 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                     tma_load_4d(C::R2T ? unit_at((C::R1T ? C::SUBT : 0) + c) : base + C::R_BYTES + c * C::SUBR, &tm_r2, smem_u32(&ctl.r_full), c * 64, row_tile * 128, h, b);
             }
         }
-        BwdWalk<KEYS, NCOL> walk(p, lane, row_tile, b, h);
+        BwdWalk<KEYS, NCOL> walk(p, lane, row_tile, b, h, part);
         const CUtensorMap* const map = one ? &tm_c1 : &tm_c2;
         const uint32_t slot0 = one ? 0 : C::NS1, slots = one ? C::NS1 : C::NS2;
         uint32_t slot = 0, phase = 0;
         RingAt<4> id;
         RingAt<C::NI> info;
         // The numbers go ahead of the tiles: a group asks for its next one when it begins with a tile, and C1 of that may have to wait for it
-        BwdWalk<KEYS, NCOL> ahead(p, lane, row_tile, b, h);
+        BwdWalk<KEYS, NCOL> ahead(p, lane, row_tile, b, h, part);
         int ends = one ? 0 : 2;
         auto hand_id = [&]() -> bool {
             if (ends == 2) return true;
@@ -483,7 +489,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         __syncwarp();
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ P, dS, results
-        reg_inc<REGS_SOFTMAX_2WG>();
+        reg_inc<C::REGS_MANY>();
         const int wg = (warp - 4) >> 2;                    // tiles of this parity
         const int row_in_tile = ((warp & 3) << 5) | lane;
         const int row = row_tile * 128 + row_in_tile;      // position of this thread's token
@@ -507,7 +513,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
             }
         }
         uint32_t mask = 0;
-        if (p.bits) mask = valid ? dep_load(p.row_mask + (size_t)head * p.n + row) & (0xffffffffu >> (32 - p.K)) : 0u;
+        if (p.bits) mask = valid ? dep_load(p.row_mask + (size_t)owner * p.n + row) & (0xffffffffu >> (32 - p.K)) : 0u;
         constexpr int LDR = LD > 0 ? LD : 1, LQ = LD > 0 ? 4 : 1, NW = NCOL / 32;
         float gr[C::GM ? 1 : LQ][C::GM ? 1 : LDR], dg[LQ][LDR];        // assignments of the rows times -lambda log2(e), their gradients over scale lambda
         if constexpr (LD > 0) {
@@ -943,11 +949,19 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
             __nv_bfloat16* out = v ? p.out1 + b * p.s1b + h * p.s1h + (int64_t)(valid ? row : 0) * p.s1n : p.out2 + b * p.s2b + h * p.s2h + (int64_t)(valid ? row : 0) * p.s2n;
             const bool wide = v ? p.wide1 : p.wide2;
             out += col0;
+            float* const sums = KEYS && p.split > 1 ? (v ? p.part1 : p.part2) + ((size_t)head * p.n + (valid ? row : 0)) * D + col0 : nullptr;
 #pragma unroll 1
             for (int c = 0; c < NOUT; c += 16) {
                 uint32_t ov[16];
                 tmem_ld16(t_a + c, ov);
                 tmem_wait_ld();
+                if (KEYS && sums) {
+                    if (valid) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(sums + c + e) = make_uint4(ov[e], ov[e + 1], ov[e + 2], ov[e + 3]);
+                    }
+                    continue;
+                }
                 uint32_t w[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(__uint_as_float(ov[2 * e]) * by, __uint_as_float(ov[2 * e + 1]) * by);

@@ -261,3 +261,18 @@ def test_gate_same_bits_every_time(B, Hq, Hkv, n, D, K):
     for _ in range(8):
         again = run_bwd(shape, t, g=g, lam=5.0)
         assert all(torch.equal(first[x], again[x]) for x in first)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n,D,window", [(1, 8, 1, 700, 128, 30), (2, 6, 1, 600, 64, 9), (1, 12, 2, 515, 128, 1000), (1, 16, 2, 300, 256, 20)])
+def test_query_heads_in_parts(B, Hq, Hkv, n, D, window):
+    """so few KV heads that their query heads go to several blocks, six of them in parts of two or three too; outputs with strides of their own"""
+    K, lam = 4, 7.0
+    t, gen = make(B, Hq, Hkv, n, D, n)
+    mq, mk = groups(gen, B, Hq, n, K, 1), groups(gen, B, Hkv, n, K, 1)
+    shape = fb.make_shape(Hq, Hkv, n, D, K, 1, window, batch=B)
+    g = torch.softmax(torch.randn((B, n, K), generator=gen, device="cuda"), -1)
+    for how in (dict(keep=plain.shared(mq, mk, Hq // Hkv)), dict(g=g.double(), lam=lam)):
+        o, lse = plain.forward(t["q"], t["k"], t["v"], D ** -0.5, window, **how)
+        t["o"], t["lse"] = o.to(torch.bfloat16), lse.float()
+        got = run_bwd(shape, t, mq, mk, tiles_of(shape, mq, mk)) if "keep" in how else run_bwd(shape, t, g=g, lam=lam)
+        plain.check(got, plain.backward(*(t[x] for x in ("q", "k", "v", "o", "lse", "do")), D ** -0.5, window, **how))

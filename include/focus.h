@@ -558,7 +558,8 @@ FOCUS_API int focus_router_scores_bwd(const focus_shape* shape, const void* h, i
  *   max_norm    >= 0; infinity: nothing is scaled
  *   norm_out    device fp32, or NULL
  *   ws          device scratch of focus_grad_clip_workspace_bytes() bytes, 16-byte aligned; calls that may overlap need one each
- * Squares of numbers whose fp32 square overflows or is tiny are taken in fp64; sums in an order that depends on the sizes alone.
+ * Squares of numbers whose fp32 square overflows or is tiny are taken in fp64; sums in an order that depends on the sizes and
+ * on where the tensors begin (modulo 16 bytes) alone.
  */
 #define FOCUS_GRAD_F32 0
 #define FOCUS_GRAD_BF16 1

@@ -4,7 +4,7 @@
 //     dv_j = sum_i p do_i      dq_i = scale sum_j ds f k_j      dk_j = scale sum_i ds f q_i
 //     distant pairs, gate: da = ds scale (q.k) lambda f (1 - f);   dg_i += da g_j,  dg_j += da g_i   (sigmoid' = f (1 - f))
 // The probabilities are worked out again from lse; nothing of size n x n is kept.  A pass over key rows gives dk and dv, all query heads of
-// a KV head in one block, one over query rows dq: seven products of tiles where five would do, but every sum has one owner and one order.
+// a KV head in one block (or in a few, whose sums are joined), one over query rows dq: seven products of tiles where five would do, but every sum has one owner and one order.
 // Here: what comes before and after those passes.
 #include "attn_bwd.cuh"
 

@@ -95,3 +95,10 @@ def test_clip():
 def test_scales_that_lse_cannot_be_divided_by():
     assert attn_args(shape(scale=2.0 ** -101), False) == -2 and attn_args(shape(scale=2.0 ** -101), True) == -2
     assert attn_args(shape(scale=2.0 ** -100), False, size=1000) == -3
+
+
+def test_layer_of_a_shape_that_is_refused():
+    from paper_2604_03260_b200.gate_layer import GateLayer
+    for bad in (dict(Hq=3), dict(D=96), dict(d_model=60), dict(K=40)):
+        with pytest.raises(fb.FocusError):
+            GateLayer(**{**dict(batch=1, Hq=4, Hkv=2, n=10, D=64, K=4, d_model=64, d_g=16, window=0, lam=1.0), **bad})

@@ -17,17 +17,53 @@ constexpr int RB_THREADS = 128;
 constexpr int RB_ROWS = 32;                 // tokens at a time
 constexpr int RB_TOTAL_COLS = 32;           // columns of a block that adds the parts up
 constexpr int RB_TOTAL_DG = 64;             // up to this d_g, and K d_g of RB_FOLD, it has the weights in shared memory before it begins
+constexpr int RB_LAST = 256;                // up to K d_g of this, the last block of the totals adds dC's parts up
 constexpr int RB_FOLD = 512;                // up to K d_g of this, a block works out its columns of F itself
 
-// F[g][e] = sum_j W_g[e][j] C[g][j]
-__global__ void __launch_bounds__(256) router_fold_kernel(const float* Wg, const float* C, int d, int dg, float* F) {
-    const int e = blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
+// F[g][e] = sum_j W_g[e][j] C[g][j]: a block 32 rows of W_g, 64 of their numbers at a time, a thread a row and every eighth group
+// (a thread a row and group, rows read from global memory: 8000 x 4096 with K = 32, d_g = 128 took 426 us in all)
+__global__ void __launch_bounds__(256) router_fold_kernel(const float* Wg, const float* C, int d, int dg, int K, float* F) {
+    __shared__ float ws[32][65], cs[32][64];
+    const int t = threadIdx.x, e0 = blockIdx.x * 32, e = t % 32, q = t / 32;
     dep_wait();
     dep_trigger();
-    if (e >= d) return;
+    float s[4] = {};
+    for (int j0 = 0; j0 < dg; j0 += 64) {
+        const int w = min(64, dg - j0);
+        for (int i = t; i < 32 * 64; i += 256) {
+            const int r = i / 64, j = i % 64;
+            ws[r][j] = e0 + r < d && j < w ? Wg[(size_t)(e0 + r) * dg + j0 + j] : 0.f;
+            cs[r][j] = r < K && j < w ? C[(size_t)r * dg + j0 + j] : 0.f;
+        }
+        __syncthreads();
+#pragma unroll 16
+        for (int j = 0; j < 64; ++j) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) s[v] = fmaf(ws[e][j], cs[q + 8 * v][j], s[v]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (q + 8 * v < K && e0 + e < d) F[(size_t)(q + 8 * v) * d + e0 + e] = s[v];
+}
+
+// dC = sum of the blocks' parts, where they are too many numbers for the last block to add up: a block 32 of them, a thread every eighth part
+__global__ void __launch_bounds__(256) router_dc_kernel(const float* dC_part, int parts, int count, float* dC) {
+    __shared__ float eighth[8][32];
+    const int c = threadIdx.x % 32, q = threadIdx.x / 32, i = blockIdx.x * 32 + c;
+    dep_wait();
+    dep_trigger();
     float s = 0.f;
-    for (int j = 0; j < dg; ++j) s = fmaf(Wg[(size_t)e * dg + j], C[(size_t)g * dg + j], s);
-    F[(size_t)g * d + e] = s;
+    if (i < count) {
+#pragma unroll 16
+        for (int z = q; z < parts; z += 8) s += dC_part[(size_t)z * count + i];
+    }
+    eighth[q][c] = s;
+    __syncthreads();
+    if (q || i >= count) return;
+    for (int x = 1; x < 8; ++x) s += eighth[x][c];
+    dC[i] = s;
 }
 
 template <int LD> struct RouterCfg {
@@ -318,6 +354,7 @@ router_total_kernel(const float* part, const float* C, const float* Wg, int part
         for (int k = 0; k < cols; ++k) y = fmaf(T[g][k], Wx[(size_t)k * dg + j], y);
         dC_part[(size_t)blockIdx.x * K * dg + i] = y;
     }
+    if (K * dg > RB_LAST) return;
     __threadfence();
     __syncthreads();
     if (t == 0) last = atomicAdd(done, 1u) == gridDim.x - 1;
@@ -377,8 +414,12 @@ static int launch_router(const focus_shape* s, const RouterBwdArgs& a, const Rou
     rc = check_cuda(launch_dependent(kern, dim3((unsigned)router_strips(s, a.d_model), (unsigned)(s->batch * c.runs)), dim3(RB_THREADS), RouterCfg<LD>::SMEM, st, a.h, a.h_sb, a.h_sn, a.ds,
                                          F, a.Wg, a.C, a.d_g, s->n, c.runs, c.run, a.d_model, s->K, a.dh, a.dh_sb, a.dh_sn, part, done), "router backward launch");
     if (rc) return rc;
-    return check_cuda(launch_dependent(router_total_kernel<LD>, dim3((unsigned)cdiv(a.d_model, RB_TOTAL_COLS)), dim3(256), 0, st, (const float*)part, a.C, a.Wg,
-                                       s->batch * c.runs, a.d_model, a.d_g, s->K, a.dWg, dC_part, a.dC, done), "router totals launch");
+    rc = check_cuda(launch_dependent(router_total_kernel<LD>, dim3((unsigned)cdiv(a.d_model, RB_TOTAL_COLS)), dim3(256), 0, st, (const float*)part, a.C, a.Wg,
+                                     s->batch * c.runs, a.d_model, a.d_g, s->K, a.dWg, dC_part, a.dC, done), "router totals launch");
+    const long long count = (long long)s->K * a.d_g;
+    if (rc || count <= RB_LAST) return rc;
+    return check_cuda(launch_dependent(router_dc_kernel, dim3((unsigned)((count + 31) / 32)), dim3(256), 0, st, (const float*)dC_part, cdiv(a.d_model, RB_TOTAL_COLS), (int)count, a.dC),
+                      "router centroids launch");
 }
 
 int launch_router_bwd(const focus_shape* s, const RouterBwdArgs& a, cudaStream_t st) {
@@ -390,7 +431,7 @@ int launch_router_bwd(const focus_shape* s, const RouterBwdArgs& a, cudaStream_t
     unsigned* done = reinterpret_cast<unsigned*>(a.ws + w.done);
     const bool fold = a.dh && (long long)K * a.d_g > RB_FOLD;
     int rc = FOCUS_OK;
-    if (fold) rc = check_cuda(launch_dependent(router_fold_kernel, dim3((unsigned)cdiv(d, 256), (unsigned)K), dim3(256), 0, st, a.Wg, a.C, d, a.d_g, F), "router fold launch");
+    if (fold) rc = check_cuda(launch_dependent(router_fold_kernel, dim3((unsigned)cdiv(d, 32)), dim3(256), 0, st, a.Wg, a.C, d, a.d_g, K, F), "router fold launch");
     if (rc) return rc;
     if (!fold) F = nullptr;
     switch (focus_soft_ld(K)) {

@@ -7,7 +7,7 @@
 //
 // A block has a strip of columns and a run of tokens, a warp 64 columns of it (32 and 16 at K > 8 and > 16), and goes down its rows 32 at a time; the
 // rows come by asynchronous copies through a ring of three to four such pieces in shared memory.  Measured with dh (device time, graph replay): 32768 x 4096,
-// K = 8, d_g = 32: 108 us, of which some 96 for the pass over the tokens (5.6 TB/s) and the rest for adding the parts up; 1024 x 768, K = 4: 11.1 us, two
+// K = 8, d_g = 32: 108 us, of which some 96 for the pass over the tokens (5.6 TB/s) and the rest for adding the parts up; 1024 x 768, K = 4: 10.9 us, two
 // launches and the chain of loads of each.  The same on the fp32 pipe, rows through a private ring: 175 and 16.4 us.
 #include "common.cuh"
 
@@ -16,7 +16,7 @@ namespace focus {
 constexpr int RB_THREADS = 128;
 constexpr int RB_ROWS = 32;                 // tokens at a time
 constexpr int RB_TOTAL_COLS = 32;           // columns of a block that adds the parts up
-constexpr int RB_TOTAL_DG = 64;             // up to this d_g, and K d_g of RB_FOLD, it has the weights in shared memory before it begins
+constexpr int RB_TOTAL_DG = 32;             // and of those of W_g and C
 constexpr int RB_LAST = 256;                // up to K d_g of this, the last block of the totals adds dC's parts up
 constexpr int RB_FOLD = 512;                // up to K d_g of this, a block works out its columns of F itself
 
@@ -296,7 +296,8 @@ router_bwd_kernel(const __nv_bfloat16* h, int64_t h_sb, int64_t h_sn, const floa
     }
 }
 
-// T = sum of the parts, dW_g = T^T C and this block's part of dC = T W_g; the last block to be through adds those up, in their order.
+// T = sum of the parts, and for 32 of the d_g numbers dW_g = T^T C and this block's part of dC = T W_g; up to K d_g = RB_LAST the last block to be
+// through adds those up, in their order.  (All of d_g in a block: 1000 x 1024, K = 32, d_g = 128 48 us, so 29.)
 // A thread adds up an eighth of the parts of a column.
 template <int LD>
 __global__ void __launch_bounds__(256)
@@ -304,16 +305,12 @@ router_total_kernel(const float* part, const float* C, const float* Wg, int part
     __shared__ float eighth[8][LD][RB_TOTAL_COLS + 1];
     __shared__ float T[LD][RB_TOTAL_COLS + 1];
     __shared__ bool last;
-    __shared__ float cs[RB_FOLD], ws[RB_TOTAL_COLS * RB_TOTAL_DG];
+    __shared__ float cs[LD * RB_TOTAL_DG], ws[RB_TOTAL_COLS * RB_TOTAL_DG];
     const int t = threadIdx.x, e0 = blockIdx.x * RB_TOTAL_COLS, c = t % RB_TOTAL_COLS, q = t / RB_TOTAL_COLS, cols = min(RB_TOTAL_COLS, d - e0);
     // The weights while the kernel before runs (what wrote them is older than that one, and complete)
-    const bool small = dg <= RB_TOTAL_DG && K * dg <= RB_FOLD;
-    if (small) {
-        for (int i = t; i < K * dg; i += 256) cs[i] = C[i];
-        for (int i = t; i < cols * dg; i += 256) ws[i] = Wg[(size_t)e0 * dg + i];
-    }
-    const float* const Cx = small ? cs : C;
-    const float* const Wx = small ? ws : Wg + (size_t)e0 * dg;
+    const int j0 = blockIdx.y * RB_TOTAL_DG, w = min(RB_TOTAL_DG, dg - j0);
+    for (int i = t; i < K * RB_TOTAL_DG; i += 256) cs[i] = i % RB_TOTAL_DG < w ? C[(size_t)(i / RB_TOTAL_DG) * dg + j0 + i % RB_TOTAL_DG] : 0.f;
+    for (int i = t; i < cols * RB_TOTAL_DG; i += 256) ws[i] = i % RB_TOTAL_DG < w ? Wg[(size_t)(e0 + i / RB_TOTAL_DG) * dg + j0 + i % RB_TOTAL_DG] : 0.f;
     dep_wait();
     dep_trigger();
     float x[LD];
@@ -339,25 +336,25 @@ router_total_kernel(const float* part, const float* C, const float* Wg, int part
         T[g][k] = y;
     }
     __syncthreads();
-    for (int i = t; i < cols * dg; i += 256) {
-        const int k = i / dg, j = i % dg;
+    for (int i = t; i < cols * RB_TOTAL_DG; i += 256) {
+        const int k = i / RB_TOTAL_DG, j = i % RB_TOTAL_DG;
         float y = 0.f;
 #pragma unroll
         for (int g = 0; g < LD; ++g)
-            if (g < K) y = fmaf(T[g][k], Cx[(size_t)g * dg + j], y);
-        dWg[(size_t)(e0 + k) * dg + j] = y;
+            if (g < K) y = fmaf(T[g][k], cs[g * RB_TOTAL_DG + j], y);
+        if (j < w) dWg[(size_t)(e0 + k) * dg + j0 + j] = y;
     }
-    for (int i = t; i < K * dg; i += 256) {
-        const int g = i / dg, j = i % dg;
+    for (int i = t; i < K * RB_TOTAL_DG; i += 256) {
+        const int g = i / RB_TOTAL_DG, j = i % RB_TOTAL_DG;
         float y = 0.f;
 #pragma unroll 8
-        for (int k = 0; k < cols; ++k) y = fmaf(T[g][k], Wx[(size_t)k * dg + j], y);
-        dC_part[(size_t)blockIdx.x * K * dg + i] = y;
+        for (int k = 0; k < cols; ++k) y = fmaf(T[g][k], ws[k * RB_TOTAL_DG + j], y);
+        if (j < w) dC_part[(size_t)blockIdx.x * K * dg + (size_t)g * dg + j0 + j] = y;
     }
     if (K * dg > RB_LAST) return;
     __threadfence();
     __syncthreads();
-    if (t == 0) last = atomicAdd(done, 1u) == gridDim.x - 1;
+    if (t == 0) last = atomicAdd(done, 1u) == gridDim.x * gridDim.y - 1;
     __syncthreads();
     if (!last) return;
     __threadfence();
@@ -414,7 +411,7 @@ static int launch_router(const focus_shape* s, const RouterBwdArgs& a, const Rou
     rc = check_cuda(launch_dependent(kern, dim3((unsigned)router_strips(s, a.d_model), (unsigned)(s->batch * c.runs)), dim3(RB_THREADS), RouterCfg<LD>::SMEM, st, a.h, a.h_sb, a.h_sn, a.ds,
                                          F, a.Wg, a.C, a.d_g, s->n, c.runs, c.run, a.d_model, s->K, a.dh, a.dh_sb, a.dh_sn, part, done), "router backward launch");
     if (rc) return rc;
-    rc = check_cuda(launch_dependent(router_total_kernel<LD>, dim3((unsigned)cdiv(a.d_model, RB_TOTAL_COLS)), dim3(256), 0, st, (const float*)part, a.C, a.Wg,
+    rc = check_cuda(launch_dependent(router_total_kernel<LD>, dim3((unsigned)cdiv(a.d_model, RB_TOTAL_COLS), (unsigned)cdiv(a.d_g, RB_TOTAL_DG)), dim3(256), 0, st, (const float*)part, a.C, a.Wg,
                                      s->batch * c.runs, a.d_model, a.d_g, s->K, a.dWg, dC_part, a.dC, done), "router totals launch");
     const long long count = (long long)s->K * a.d_g;
     if (rc || count <= RB_LAST) return rc;

@@ -22,6 +22,8 @@
 
 #include "attn_bwd.cuh"
 
+#include <type_traits>
+
 namespace focus {
 
 constexpr int BWD_THREADS = 384;
@@ -653,35 +655,59 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
 #pragma unroll
                             for (int e = 0; e < 8; ++e) lc[e] = reinterpret_cast<const float4*>(info + c)[e];
                         }
+                        auto piece = [&](auto far) {
 #pragma unroll
-                        for (int e = c; e < c + 32; e += 4) {
-                            float2 l[2];
-                            if constexpr (C::STAT_BYTES > 0) *reinterpret_cast<float4*>(l) = lc[(e - c) / 4];
-                            else l[0] = l[1] = make_float2(lrow[0], lrow[0]);
+                            for (int e = c; e < c + 32; e += 4) {
+                                float2 l[2];
+                                if constexpr (C::STAT_BYTES > 0) *reinterpret_cast<float4*>(l) = lc[(e - c) / 4];
+                                else l[0] = l[1] = make_float2(lrow[0], lrow[0]);
 #pragma unroll
-                            for (int f = 0; f < 2; ++f) {
-                                uint32_t &u0 = pr[e + 2 * f], &u1 = pr[e + 2 * f + 1];
-                                float2 x = make_float2(__uint_as_float(u0), __uint_as_float(u1)), y;
-                                if constexpr (CAP) {
-                                    x = __fmul2_rn(x, make_float2(cap_in, cap_in));
-                                    x.x = tanh_approx(x.x);
-                                    x.y = tanh_approx(x.y);
-                                    y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
-                                    y.x = ex2_approx(y.x);
-                                    y.y = ex2_approx(y.y);
-                                    x = __fmul2_rn(y, __ffma2_rn(make_float2(-x.x, -x.y), x, make_float2(1.f, 1.f)));
-                                } else {
-                                    if constexpr (C::AUG) y = __fmul2_rn(x, make_float2(sl2, sl2));
-                                    else y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
-                                    y.x = ex2_approx(y.x);
-                                    y.y = ex2_approx(y.y);
-                                    x = y;
+                                for (int f = 0; f < 2; ++f) {
+                                    uint32_t &u0 = pr[e + 2 * f], &u1 = pr[e + 2 * f + 1];
+                                    float2 x = make_float2(__uint_as_float(u0), __uint_as_float(u1)), y;
+                                    if constexpr (CAP) {
+                                        x = __fmul2_rn(x, make_float2(cap_in, cap_in));
+                                        const float2 z = x;
+                                        x.x = tanh_approx(x.x);
+                                        x.y = tanh_approx(x.y);
+                                        y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
+                                        y.x = ex2_approx(y.x);
+                                        y.y = ex2_approx(y.y);
+                                        if constexpr (decltype(far)::value) {
+                                            const float2 w = make_float2(ex2_approx(fabsf(z.x) * (-2.f * LOG2E)), ex2_approx(fabsf(z.y) * (-2.f * LOG2E)));
+                                            x = make_float2(1.f + fabsf(x.x), 1.f + fabsf(x.y));
+                                            x = __fmul2_rn(__fmul2_rn(y, w), __fmul2_rn(x, x));
+                                        } else {
+                                            x = __fmul2_rn(y, __ffma2_rn(make_float2(-x.x, -x.y), x, make_float2(1.f, 1.f)));
+                                        }
+                                    } else {
+                                        if constexpr (C::AUG) y = __fmul2_rn(x, make_float2(sl2, sl2));
+                                        else y = __ffma2_rn(x, make_float2(sl2, sl2), l[f]);
+                                        y.x = ex2_approx(y.x);
+                                        y.y = ex2_approx(y.y);
+                                        x = y;
+                                    }
+                                    u0 = __float_as_uint(x.x);
+                                    u1 = __float_as_uint(x.y);
+                                    if constexpr (C::HAS_V) pk[(e - c) / 2 + f] = pack_bf16x2(y.x, y.y);
                                 }
-                                u0 = __float_as_uint(x.x);
-                                u1 = __float_as_uint(x.y);
-                                if constexpr (C::HAS_V) pk[(e - c) / 2 + f] = pack_bf16x2(y.x, y.y);
                             }
+                        };
+                        // The cap's slope 1 - t^2: where t is next to 1 the difference has nothing left (with the hardware's t: right to 2^-12
+                        // up to 3.5 caps, 1 % off from 4 on, a quarter at 7, all of it from 8).  Beyond 3.5 it is e (1 + |t|)^2, e = exp(-2 |x|):
+                        // t = (1 - e) / (1 + e), so that 1 + t = 2 / (1 + e).  That is an exponential more a pair, which a warp takes where one of its
+                        // 32 x 32 scores needs it (32/8 heads x 4096, D = 128: 669 us with the difference alone, 847 with the other alone, 691 so, and
+                        // 920 for scores most of which are beyond).  At D = 256, whose passes wait for copies, to look at the scores costs more
+                        // than the exponential (16/8 x 4096: 518, 550 and 561 us): always.
+                        bool far = D == 256;
+                        if constexpr (CAP && C::HAS_DS && D != 256) {
+                            float m = 0.f;
+#pragma unroll
+                            for (int e = c; e < c + 32; ++e) m = fmaxf(m, fabsf(__uint_as_float(pr[e])));
+                            far = __any_sync(0xffffffffu, m * cap_in > 3.5f);
                         }
+                        if (CAP && C::HAS_DS && far) piece(std::true_type());
+                        else piece(std::false_type());
                         if constexpr (C::HAS_V) {
                             strike(pk, kw[c / 32]);
                             tmem_st16(t_x + c / 2, pk);

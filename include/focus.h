@@ -503,8 +503,9 @@ FOCUS_API int focus_sinkhorn_bwd(const focus_shape* shape, const float* scores, 
  * pairs and delta_i = do_i.o_i: ds = p (do.v - delta) (times 1 - tanh^2 with a softcap), dv_j = sum_i p do_i, dk_j = scale sum_i ds q_i over
  * the rows of all query heads of the KV head, dq_i = scale sum_j ds k_j.  The probabilities are worked out again; nothing of size n x n is
  * kept.  With a softcap tanh is the hardware's, as in the forward pass (2^-11 of the capped score); the slope 1 - tanh^2 is right to 2^-11
- * of itself however far beyond the cap a score is.  bf16 operands, fp32 accumulation; p and ds are rounded to bf16 before their products, the results once.  The order of the sums
- * depends on the shape and the masks alone (the same bits in every call).
+ * of itself however far beyond the cap a score is.  bf16 operands, fp32 accumulation; p and ds are rounded to bf16 before their products, the results once.  A result's sum is
+ * the tensor cores' over at most 32768 rows or columns (they cut off: a sum of one sign loses up to 2^-12 of itself), and of such sums one in fp32.  The order of
+ * the sums depends on the shape and the masks alone (the same bits in every call).
  *   q, k, v, mq, mk, tiles_ws, layout   as for the forward pass, with any layout (tiles are walked in token order); NULL tiles_ws = every
  *               causal pair
  *   o, lse      what the forward pass wrote (finite; a row whose lse is -inf has no pairs and no gradient)

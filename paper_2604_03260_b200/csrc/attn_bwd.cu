@@ -197,7 +197,7 @@ static int bwd_split(const focus_shape* s, bool gate) {
 }
 
 struct BwdWorkspace {
-    size_t part1, part2;
+    size_t part1, part2, part_q;
     size_t stat, aug, qbits, gq, gk, g_rows, g_cols, g_flat, bytes;
 };
 static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
@@ -209,10 +209,13 @@ static BwdWorkspace bwd_workspace(const focus_shape* s, bool gate) {
     w.aug = take(HQ * nt * 128 * 16);
     w.qbits = gate ? 0 : take(HQ * nt * s->K * 16);
     w.gq = gate ? take(HQ * row) : 0;
-    const size_t split = bwd_split(s, gate), sums = split > 1 ? HK * split * s->n * s->D * 4 : 0;
+    const size_t split = bwd_split(s, gate), each = s->Hq / s->Hkv / split;
+    const bool parts = split > 1 || (int)nt > BWD_LAUNCH_TILES || bwd_heads_together((int)nt, (int)each) < (int)each;       // of a row's sums
+    const size_t sums = parts ? HK * split * s->n * s->D * 4 : 0;
     w.gk = gate ? take(HK * split * row) : 0;
     w.part1 = take(sums);
     w.part2 = take(sums);
+    w.part_q = take((int)nt > BWD_LAUNCH_TILES ? HQ * s->n * s->D * 4 : 0);
     const size_t terms = gate && s->D != 256 ? (size_t)s->batch * nt * 128 * gate_depth(focus_soft_ld(s->K)) * 2 : 0;
     w.g_rows = take(terms);
     w.g_cols = take(terms);
@@ -261,6 +264,7 @@ int launch_attn_bwd(const AttnBwdArgs& a, cudaStream_t st) {
     kv.out1 = (__nv_bfloat16*)a.dv.ptr; kv.s1b = a.dv.stride_b; kv.s1h = a.dv.stride_h; kv.s1n = a.dv.stride_n; kv.wide1 = wide(a.dv);
     kv.out2 = (__nv_bfloat16*)a.dk.ptr; kv.s2b = a.dk.stride_b; kv.s2h = a.dk.stride_h; kv.s2n = a.dk.stride_n; kv.wide2 = wide(a.dk);
     q.heads = HQ; q.by_heads = Divisor(HQ); q.by_rows_H = Divisor(s.Hq);
+    q.part2 = reinterpret_cast<float*>(a.ws + w.part_q);
     q.row_mask = a.mq; q.bits = a.tiles ? reinterpret_cast<const uint32_t*>(a.tiles + a.L.gbits) : nullptr;
     q.dg_part = reinterpret_cast<float*>(a.ws + w.gq);
     q.out2 = (__nv_bfloat16*)a.dq.ptr; q.s2b = a.dq.stride_b; q.s2h = a.dq.stride_h; q.s2n = a.dq.stride_n; q.wide2 = wide(a.dq);

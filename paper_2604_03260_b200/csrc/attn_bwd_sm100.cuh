@@ -140,6 +140,7 @@ struct BwdCtl {
     int abort_flag;
     int more[8];                  // of a slot: whether there is a tile at all
     int tile[4], head[4];         // column tile and its head; tile -1: no more
+    int none;                     // there is no tile at all
 };
 static_assert(sizeof(BwdCtl) <= 1024, "CTL_BYTES");
 
@@ -152,10 +153,10 @@ struct BwdWalk {
     uint32_t bits;
     int part = NCOL == 64 ? 1 : 0;        // halves of a 128-tile
     int at = -1;
-    __device__ __forceinline__ int first_col() const { return KEYS ? row_tile : 0; }
-    __device__ __forceinline__ int end_col() const { return KEYS ? p.nt : row_tile + 1; }
+    __device__ __forceinline__ int first_col() const { return KEYS ? max(row_tile, p.col_lo) : p.col_lo; }
+    __device__ __forceinline__ int end_col() const { return KEYS ? p.col_hi : min(row_tile + 1, p.col_hi); }
     __device__ __forceinline__ BwdWalk(const BwdParams& p_, int lane_, int rt, int b_, int h_, int part)
-        : p(p_), lane(lane_), row_tile(rt), b(b_), h(h_), hi(part * p_.heads_each), hi_end(hi + p_.heads_each), bits(0) {
+        : p(p_), lane(lane_), row_tile(rt), b(b_), h(h_), hi(part * p_.heads_each + p_.head_lo), hi_end(part * p_.heads_each + p_.head_hi), bits(0) {
         c = first_col();
         word = c - 32;
     }
@@ -250,6 +251,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         }
         for (int x = 0; x < 8; ++x) ctl.more[x] = 1;
         ctl.abort_flag = 0;
+        ctl.none = 0;
         ctl.limit = wait_limit(4000000000ull);
         fence_mbar_init();
     }
@@ -305,6 +307,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
             if (t < 0) ++ends;                                      // (a last one for each group of warps)
             if (!wait(ctl.id_empty[id.slot], id.phase ^ 1, 13)) return false;
             if (lane == 0) {
+                if (t < 0 && ahead.at < 0) ctl.none = 1;
                 ctl.tile[id.slot] = t;
                 ctl.head[id.slot] = KEYS ? h * p.G + ahead.hi : hk;
                 mbar_arrive(smem_u32(&ctl.id_full[id.slot]));
@@ -421,7 +424,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
         int left = 0;                                      // X's issued whose sum has not been
         auto first_x = [&]() -> bool {
 #pragma unroll 1
-            for (int x = 0; x < C::NPL; ++x) {             // (every item has its diagonal tile)
+            for (int x = 0; x < C::NPL; ++x) {
                 more = take(at1.slot, at1.phase);
                 if (!more) break;
                 tc_fence_after();
@@ -975,13 +978,30 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
             __nv_bfloat16* out = v ? p.out1 + b * p.s1b + h * p.s1h + (int64_t)(valid ? row : 0) * p.s1n : p.out2 + b * p.s2b + h * p.s2h + (int64_t)(valid ? row : 0) * p.s2n;
             const bool wide = v ? p.wide1 : p.wide2;
             out += col0;
-            float* const sums = KEYS && p.split > 1 ? (v ? p.part1 : p.part2) + ((size_t)head * p.n + (valid ? row : 0)) * D + col0 : nullptr;
+            // sums of the launches before, and whether this is the last for these rows
+            const bool add = KEYS ? p.later || row_tile < p.col_lo : p.col_lo > 0, done = KEYS ? p.last && p.split == 1 : row_tile < p.col_hi;
+            float* const sums = (v ? p.part1 : p.part2) + ((size_t)head * p.n + (valid ? row : 0)) * D + col0;
+            const bool none = *(volatile int*)&ctl.none;
 #pragma unroll 1
             for (int c = 0; c < NOUT; c += 16) {
                 uint32_t ov[16];
                 tmem_ld16(t_a + c, ov);
                 tmem_wait_ld();
-                if (KEYS && sums) {
+                if (none) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) ov[e] = 0u;
+                }
+                if (add && valid) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 x = *reinterpret_cast<const float4*>(sums + c + e);
+                        ov[e] = __float_as_uint(x.x + __uint_as_float(ov[e]));
+                        ov[e + 1] = __float_as_uint(x.y + __uint_as_float(ov[e + 1]));
+                        ov[e + 2] = __float_as_uint(x.z + __uint_as_float(ov[e + 2]));
+                        ov[e + 3] = __float_as_uint(x.w + __uint_as_float(ov[e + 3]));
+                    }
+                }
+                if (!done) {
                     if (valid) {
 #pragma unroll
                         for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(sums + c + e) = make_uint4(ov[e], ov[e + 1], ov[e + 2], ov[e + 3]);
@@ -1021,10 +1041,13 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
 #pragma unroll
                         for (int e = 0; e < LD; ++e) x[e * 128] = dg[q][e];
                     } else if (other && rowq + 8 * q < p.n) {
+                        float4* const to = reinterpret_cast<float4*>(p.dg_part + ((size_t)head * p.n + rowq + 8 * q) * LD);
 #pragma unroll
-                        for (int e = 0; e < LD; e += 4)
-                            *reinterpret_cast<float4*>(p.dg_part + ((size_t)head * p.n + rowq + 8 * q) * LD + e) =
-                                make_float4(dg[q][e] + x[e * 128], dg[q][e + 1] + x[(e + 1) * 128], dg[q][e + 2] + x[(e + 2) * 128], dg[q][e + 3] + x[(e + 3) * 128]);
+                        for (int e = 0; e < LD; e += 4) {
+                            const float4 old = add ? to[e / 4] : make_float4(0.f, 0.f, 0.f, 0.f);
+                            to[e / 4] = make_float4(old.x + (dg[q][e] + x[e * 128]), old.y + (dg[q][e + 1] + x[(e + 1) * 128]), old.z + (dg[q][e + 2] + x[(e + 2) * 128]),
+                                                    old.w + (dg[q][e + 3] + x[(e + 3) * 128]));
+                        }
                     }
                 }
                 if (wg == 1) mbar_arrive(smem_u32(&ctl.dg_full));
@@ -1053,7 +1076,7 @@ struct BwdMaps {
 template <int D, bool CAP, int LD>
 __global__ void __launch_bounds__(BWD_THREADS, 1)
 attn_bwd_kernel(const __grid_constant__ BwdMaps m, const __grid_constant__ BwdParams kv, const __grid_constant__ BwdParams q) {
-    const int nkv = kv.heads * kv.nt, block = (int)blockIdx.x;
+    const int nkv = kv.heads * kv.row_tiles, block = (int)blockIdx.x;
     if constexpr (D == 256) {
         if (block < nkv) bwd_item<D, BWD_K, CAP, LD>(m.r[1], m.r[2], m.c[0], m.c[3], kv, block);
         else if (block < 2 * nkv) bwd_item<D, BWD_V, CAP, LD>(m.r[1], m.r[2], m.c[0], m.c[3], kv, block - nkv);
@@ -1076,11 +1099,30 @@ static int launch_bwd_passes(const AttnBwdArgs& a, const BwdParams& kv, const Bw
     int rc;
     for (int i = 0; i < 4; ++i)
         if ((rc = make_tmap_qkv(&m.r[i], *t[i], a.s.batch, heads[i], a.s.n, D)) || (rc = make_tmap_qkv(&m.c[i], *t[i], a.s.batch, heads[i], a.s.n, D, Q::NCOL))) return rc;
-    const long long blocks = (long long)kv.heads * kv.nt * (D == 256 ? 2 : 1) + (long long)q.heads * q.nt;
-    if (blocks > 0x7fffffffll) return fail(FOCUS_ERR_UNSUPPORTED, "attention backward: %lld tiles exceed 2^31 - 1", blocks);
+    const long long most = (long long)kv.heads * kv.nt * (D == 256 ? 2 : 1) + (long long)q.heads * q.nt;
+    if (most > 0x7fffffffll) return fail(FOCUS_ERR_UNSUPPORTED, "attention backward: %lld tiles exceed 2^31 - 1", most);
     if ((rc = check_cuda(allow_smem<attn_bwd_kernel<D, CAP, LD>>(smem), "cudaFuncSetAttribute(attn_bwd)"))) return rc;
+    // The longest way first: a pass over keys takes its heads together as far as they go, or each in pieces; one over queries its keys in pieces
     auto kern = attn_bwd_kernel<D, CAP, LD>;
-    return check_cuda(launch_dependent(kern, dim3((unsigned)blocks), dim3(BWD_THREADS), smem, st, m, kv, q), "attention backward launch");
+    const int step = kv.nt < BWD_LAUNCH_TILES ? kv.nt : BWD_LAUNCH_TILES, pieces = cdiv(kv.nt, step), together = bwd_heads_together(kv.nt, kv.heads_each);
+    const int runs = cdiv(kv.heads_each, together) * pieces;
+    for (int x = 0; x < runs; ++x) {
+        BwdParams k = kv, r = q;
+        k.head_lo = x / pieces * together;
+        k.head_hi = k.head_lo + together < kv.heads_each ? k.head_lo + together : kv.heads_each;
+        k.col_lo = x % pieces * step;
+        k.col_hi = k.col_lo + step < kv.nt ? k.col_lo + step : kv.nt;
+        k.later = k.head_lo > 0;
+        k.last = x == runs - 1;
+        k.row_tiles = k.col_hi;
+        r.col_lo = x < pieces ? k.col_lo : kv.nt;
+        r.col_hi = x < pieces ? k.col_hi : kv.nt;
+        r.head_hi = 1;
+        r.row_tiles = kv.nt - r.col_lo;
+        const long long blocks = (long long)k.heads * k.row_tiles * (D == 256 ? 2 : 1) + (long long)r.heads * r.row_tiles;
+        if ((rc = check_cuda(launch_dependent(kern, dim3((unsigned)blocks), dim3(BWD_THREADS), smem, st, m, k, r), "attention backward launch"))) return rc;
+    }
+    return FOCUS_OK;
 }
 
 template <int D>

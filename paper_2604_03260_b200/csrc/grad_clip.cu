@@ -5,7 +5,7 @@
 //
 // Squares: 8 numbers' squares are added in fp32 and those sums in fp64 (a conversion per number would be as slow as the memory:
 // 16 a clock and SM).  Where such a sum is beyond the range in which fp32 loses nothing (overflow, or so small that squares may have
-// vanished) the 8 are taken again in fp64.
+// vanished) the 8 are taken again in fp64; 8 zeros too, so that 1 GB of fp32 zeros takes 1 % longer than of other numbers, 0.5 GB of bf16 zeros 10 % (304 us for 276).
 #include "common.cuh"
 
 #include <string.h>
@@ -138,20 +138,21 @@ __global__ void __launch_bounds__(256, 4) clip_scale_kernel(const __grid_constan
     const double norm = sqrt(block_sum(x, s));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const double by = norm > bound && isfinite((float)norm) ? bound / norm : 1.0;       // (what is reported as not finite is left to the caller)
-    // a factor below fp32's normal numbers would have lost bits: in two steps, the second one exact
+    // A factor below fp32's normal numbers would have lost bits (below 2^-149: all of them, though what a large number becomes may be a normal one):
+    // then every product is taken in fp64, one number at a time
     const bool tiny = by < 0x1p-126;
-    const float f = (float)(tiny ? by * 0x1p64 : by), f2 = tiny ? 0x1p-64f : 1.f;
+    const float f = (float)by;
     const int total = t.first[t.tensors];
     for (int chunk = total - 1 - (int)blockIdx.x; chunk >= 0; chunk -= gridDim.x) {
         const ClipChunk c = clip_chunk(t, chunk);
         if (by == 1.0 && c.src == c.dst) continue;
         const int size = c.half ? 2 : 4;
         auto one = [&](long long e) {
-            const float v = clip_number(c.src, e, c.half) * f * f2;
+            const float x = clip_number(c.src, e, c.half), v = tiny ? (float)((double)x * by) : x * f;
             if (c.half) reinterpret_cast<__nv_bfloat16*>(c.dst)[e] = __float2bfloat16_rn(v);
             else reinterpret_cast<float*>(c.dst)[e] = v;
         };
-        if (((uintptr_t)c.src ^ (uintptr_t)c.dst) & 15) {              // no boundary in common
+        if (tiny || ((uintptr_t)c.src ^ (uintptr_t)c.dst) & 15) {      // (or no boundary in common)
             for (long long e = threadIdx.x; e < c.count; e += 256) one(e);
             continue;
         }
@@ -171,10 +172,10 @@ __global__ void __launch_bounds__(256, 4) clip_scale_kernel(const __grid_constan
                 for (int e = 0; e < 4; ++e) {
                     if (c.half) {
                         const float2 y = clip_pair(v[e]);
-                        const __nv_bfloat162 z = __floats2bfloat162_rn(y.x * f * f2, y.y * f * f2);
+                        const __nv_bfloat162 z = __floats2bfloat162_rn(y.x * f, y.y * f);
                         v[e] = *reinterpret_cast<const uint32_t*>(&z);
                     } else {
-                        v[e] = __float_as_uint(__uint_as_float(v[e]) * f * f2);
+                        v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
                     }
                 }
                 if (i + 256 * u < pieces) q[i + 256 * u] = w[u];

@@ -514,7 +514,7 @@ FOCUS_API int focus_sinkhorn_bwd(const focus_shape* shape, const float* scores, 
  *   ws          device scratch of focus_attn_bwd_workspace_bytes(shape) bytes, 16-byte aligned; contents need not be preserved between
  *               calls, calls that may overlap need one each
  *   dev_status  device int32[4], nullable, as for focus_attn_fwd
- * FOCUS_ERR_UNSUPPORTED: batch*Hq above 65535, a scale above 0 but below 2^-100.
+ * FOCUS_ERR_UNSUPPORTED: batch*Hq above 65535, a scale above 0 but below 2^-100.  The workspace query is 0 for a shape that the call refuses.
  *
  * focus_gate_attn_bwd -- the derivative of focus_gate_attn_fwd: those of q, k, v and of the soft assignments,
  *     da_ij = ds_ij scale q_i.k_j lambda f (1 - f), f = sigmoid(lambda g_i.g_j), over the distant pairs of all heads;

@@ -617,9 +617,26 @@ int focus_gate_attn_fwd(const focus_shape* shape, focus_tensor q, focus_tensor k
     return launch_attn_sm100(a, (cudaStream_t)stream);
 }
 
-size_t focus_attn_bwd_workspace_bytes(const focus_shape* shape) { return validate_shape(shape) ? 0 : attn_bwd_workspace_bytes(shape, false); }
+// shapes that the attention's backward passes take
+static int attn_bwd_shape(const focus_shape* shape, bool gate) {
+    int rc = validate_shape(shape);
+    if (rc) return rc;
+    if (gate && shape->softcap > 0.f) return fail(FOCUS_ERR_UNSUPPORTED, "the gated attention takes no softcap");
+    if (gate && shape->D == 256 && shape->K > 16)
+        return fail(FOCUS_ERR_UNSUPPORTED, "the gated attention supports K <= 32 (K <= 16 at D = 256); K = %d", shape->K);
+    if (!isfinite(shape->scale) || !isfinite(shape->softcap)) return fail(FOCUS_ERR_INVALID_ARG, "scale and softcap must be finite");
+    if (shape->scale > 0.f && shape->scale < 0x1p-100f)
+        return fail(FOCUS_ERR_UNSUPPORTED, "scale (%g) below 2^-100", (double)shape->scale);      // (lse / scale has to be a number)
+    if ((long long)shape->batch * shape->Hq > 65535) return fail(FOCUS_ERR_UNSUPPORTED, "batch*Hq (%lld) must not exceed 65535", (long long)shape->batch * shape->Hq);
+    // blocks of a launch: an item for every tile and head of the queries, one or two for every tile and part of the keys' heads
+    if ((long long)shape->batch * (3ll * shape->Hq + 1) * cdiv(shape->n, 128) > 0x7fffffffll)
+        return fail(FOCUS_ERR_UNSUPPORTED, "batch*Hq (%lld) heads of %d tokens are too many tiles", (long long)shape->batch * shape->Hq, shape->n);
+    return FOCUS_OK;
+}
 
-size_t focus_gate_attn_bwd_workspace_bytes(const focus_shape* shape) { return validate_shape(shape) ? 0 : attn_bwd_workspace_bytes(shape, true); }
+size_t focus_attn_bwd_workspace_bytes(const focus_shape* shape) { return attn_bwd_shape(shape, false) ? 0 : attn_bwd_workspace_bytes(shape, false); }
+
+size_t focus_gate_attn_bwd_workspace_bytes(const focus_shape* shape) { return attn_bwd_shape(shape, true) ? 0 : attn_bwd_workspace_bytes(shape, true); }
 
 // what the two backward passes check alike
 static int attn_bwd_args(AttnBwdArgs& a, size_t ws_bytes) {
@@ -638,21 +655,18 @@ static int attn_bwd_args(AttnBwdArgs& a, size_t ws_bytes) {
             if (out[i] == x) return fail(FOCUS_ERR_INVALID_ARG, "dq, dk and dv must not be one of the inputs");
         if (out[i] == out[(i + 1) % 3]) return fail(FOCUS_ERR_INVALID_ARG, "dq, dk and dv must be three buffers");
     }
-    if (!isfinite(shape->scale) || !isfinite(shape->softcap)) return fail(FOCUS_ERR_INVALID_ARG, "scale and softcap must be finite");
-    if ((long long)shape->batch * shape->Hq > 65535) return fail(FOCUS_ERR_UNSUPPORTED, "batch*Hq (%lld) must not exceed 65535", (long long)shape->batch * shape->Hq);
     const size_t need = attn_bwd_workspace_bytes(shape, a.g != nullptr);
     if (!a.ws || (uintptr_t)a.ws % 16) return fail(FOCUS_ERR_INVALID_ARG, "ws is NULL or not 16-byte aligned");
     if (ws_bytes < need) return fail(FOCUS_ERR_CAPACITY, "attention backward workspace has %zu bytes, %zu needed", ws_bytes, need);
     if ((uintptr_t)a.dev_status % 4) return fail(FOCUS_ERR_INVALID_ARG, "dev_status must be 4-byte aligned");
     a.scale = shape->scale > 0.f ? shape->scale : 1.0f / sqrtf((float)shape->D);
-    if (a.scale < 0x1p-100f) return fail(FOCUS_ERR_UNSUPPORTED, "scale (%g) below 2^-100", (double)a.scale);      // (lse / scale has to be a number)
     return FOCUS_OK;
 }
 
 int focus_attn_bwd(const focus_shape* shape, focus_tensor q, focus_tensor k, focus_tensor v, const uint32_t* mq, const uint32_t* mk,
                    const void* tiles_ws, int32_t layout, focus_tensor o, const float* lse, focus_tensor d_o, focus_tensor dq, focus_tensor dk,
                    focus_tensor dv, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) {
-    int rc = validate_shape(shape);
+    int rc = attn_bwd_shape(shape, false);
     if (rc) return rc;
     if (tiles_ws && (!mq || !mk)) return fail(FOCUS_ERR_INVALID_ARG, "mq/mk are required with a tiles workspace");
     if (((uintptr_t)mq | (uintptr_t)mk) % 4 || (uintptr_t)tiles_ws % 256) return fail(FOCUS_ERR_INVALID_ARG, "mq, mk or tiles_ws is misaligned");
@@ -666,14 +680,11 @@ int focus_attn_bwd(const focus_shape* shape, focus_tensor q, focus_tensor k, foc
 int focus_gate_attn_bwd(const focus_shape* shape, focus_tensor q, focus_tensor k, focus_tensor v, const float* g, float lambda, focus_tensor o,
                         const float* lse, focus_tensor d_o, focus_tensor dq, focus_tensor dk, focus_tensor dv, float* dg, void* ws, size_t ws_bytes,
                         int32_t* dev_status, void* stream) {
-    int rc = validate_shape(shape);
+    int rc = attn_bwd_shape(shape, true);
     if (rc) return rc;
     if (!g || !dg || ((uintptr_t)g | (uintptr_t)dg) % 16) return fail(FOCUS_ERR_INVALID_ARG, "g or dg is NULL or not 16-byte aligned");
     if (g == dg) return fail(FOCUS_ERR_INVALID_ARG, "dg must not be g");
     if (!isfinite(lambda)) return fail(FOCUS_ERR_INVALID_ARG, "lambda must be finite");
-    if (shape->softcap > 0.f) return fail(FOCUS_ERR_UNSUPPORTED, "the gated attention takes no softcap");
-    if (shape->D == 256 && shape->K > 16)
-        return fail(FOCUS_ERR_UNSUPPORTED, "the gated attention supports K <= 32 (K <= 16 at D = 256); K = %d", shape->K);
     AttnBwdArgs a = {*shape, q, k, v, o, d_o, dq, dk, dv, nullptr, nullptr, nullptr, {}, lse, 0.f, g, lambda, dg, (char*)ws, dev_status};
     if ((rc = attn_bwd_args(a, ws_bytes))) return rc;
     if ((rc = require_sm100())) return rc;

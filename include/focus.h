@@ -519,7 +519,8 @@ FOCUS_API int focus_sinkhorn_bwd(const focus_shape* shape, const float* scores, 
  * focus_gate_attn_bwd -- the derivative of focus_gate_attn_fwd: those of q, k, v and of the soft assignments,
  *     da_ij = ds_ij scale q_i.k_j lambda f (1 - f), f = sigmoid(lambda g_i.g_j), over the distant pairs of all heads;
  *     dg_i += da_ij g_j,  dg_j += da_ij g_i
- * with the sums of dg in fp32 throughout and f from exp (no tanh approximation).
+ * with the sums of dg in fp32 throughout and f from exp (no tanh approximation).  The forward pass takes f from the hardware's tanh, so that o and lse
+ * belong to probabilities that differ from those worked out here by up to 2^-12 of a distant pair's |scale q_i.k_j| (measured: 2^-18 of it).
  *   shape       as for the forward pass: softcap 0, K <= 32 (K <= 16 at D = 256)
  *   g, lambda   as for the forward pass; lambda finite
  *   dg          device fp32 [batch, n, ld], overwritten; entries g >= K are written as 0; 16-byte aligned

@@ -522,7 +522,7 @@ FOCUS_API int focus_sinkhorn_bwd(const focus_shape* shape, const float* scores, 
  * with the sums of dg in fp32 throughout and f from exp (no tanh approximation).  The forward pass takes f from the hardware's tanh, so that o and lse
  * belong to probabilities that differ from those worked out here by up to 2^-12 of a distant pair's |scale q_i.k_j| (measured: 2^-18 of it).
  *   shape       as for the forward pass: softcap 0, K <= 32 (K <= 16 at D = 256)
- *   g, lambda   as for the forward pass; lambda finite
+ *   g, lambda   as for the forward pass; lambda finite and at most 2^100 either way (FOCUS_ERR_UNSUPPORTED beyond)
  *   dg          device fp32 [batch, n, ld], overwritten; entries g >= K are written as 0; 16-byte aligned
  */
 FOCUS_API size_t focus_attn_bwd_workspace_bytes(const focus_shape* shape);

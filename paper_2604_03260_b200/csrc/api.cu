@@ -685,6 +685,7 @@ int focus_gate_attn_bwd(const focus_shape* shape, focus_tensor q, focus_tensor k
     if (!g || !dg || ((uintptr_t)g | (uintptr_t)dg) % 16) return fail(FOCUS_ERR_INVALID_ARG, "g or dg is NULL or not 16-byte aligned");
     if (g == dg) return fail(FOCUS_ERR_INVALID_ARG, "dg must not be g");
     if (!isfinite(lambda)) return fail(FOCUS_ERR_INVALID_ARG, "lambda must be finite");
+    if (fabsf(lambda) > 0x1p100f) return fail(FOCUS_ERR_UNSUPPORTED, "lambda (%g) beyond 2^100", (double)lambda);      // (lambda log2(e) g has to be a number)
     AttnBwdArgs a = {*shape, q, k, v, o, d_o, dq, dk, dv, nullptr, nullptr, nullptr, {}, lse, 0.f, g, lambda, dg, (char*)ws, dev_status};
     if ((rc = attn_bwd_args(a, ws_bytes))) return rc;
     if ((rc = require_sm100())) return rc;

@@ -32,3 +32,10 @@ def test_sizes_of_what_is_taken():
 def test_no_layer_of_a_shape_that_only_the_backward_pass_refuses(bad):
     with pytest.raises(fb.FocusError, match="K = 17|65535|2\\^-100"):
         GateLayer(**{**dict(batch=1, Hq=4, Hkv=2, n=10, D=64, K=4, d_model=64, d_g=16, window=0, lam=1.0), **bad})
+
+
+@pytest.mark.parametrize("lam", [3e38, -3e38, 2.0 ** 101])
+def test_slopes_whose_products_are_no_numbers(lam):
+    """lambda log2(e) is infinite from 2.4e38 on, and times an assignment of 0 nothing at all"""
+    assert attn_args(shape(), True, lam=lam) == -2 and "lambda" in fb.lib().focus_last_error().decode()
+    assert attn_args(shape(), True, lam=2.0 ** 100, size=1000) == -3

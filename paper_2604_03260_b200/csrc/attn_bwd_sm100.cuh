@@ -580,6 +580,7 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                     tmem_st32(tm + C::COL_R + u * 32, w);
                 }
                 tmem_wait_st();
+                fence_proxy_async_smem();          // (read here, copied over by the tiles)
                 tc_fence_before();
                 mbar_arrive(smem_u32(&ctl.r_taken));
             }
@@ -956,10 +957,11 @@ __device__ __forceinline__ void bwd_item(const CUtensorMap& tm_r1, const CUtenso
                         }
                     }
                 }
-                // Every read of the assignments has to be through before the next copy over them is asked for.  The arrival alone, one lane's behind
-                // __syncwarp() or, tried too, every thread's own, does not wait for the last read's answer (D = 64, K = 4: dg of some rows with the numbers of the
-                // tile after next); what else is read here goes into dS, which has been handed over.
-                if constexpr (C::GATE_SMEM) __threadfence_block();
+                // Every read of what goes by the column has to be through before the next copy over it.  Reads go by the generic proxy, the copy writes by the
+                // async one, and a barrier's arrival orders the first with what comes after it only within its own proxy: so the fence between the two, by every
+                // thread that read.  (Without it, D = 64 and K = 4: dg of some rows with the numbers of the tile after next.  lse and delta had gone into what
+                // was handed over before, and were right all the same.)
+                if constexpr (C::INFO_BYTES > 0) fence_proxy_async_smem();
                 __syncwarp();
                 if (C::INFO_BYTES > 0 && lane == 0) mbar_arrive(smem_u32(&ctl.info_empty[at_info]));
                 place += 2;

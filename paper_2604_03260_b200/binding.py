@@ -585,6 +585,15 @@ def make_grad_list(grads, out=None):
         e.src, e.dst, e.count, e.dtype = s.data_ptr(), d.data_ptr(), s.numel(), kinds[s.dtype]
     written = [d.data_ptr() for d in out if d.numel()]
     assert len(set(written)) == len(written), "a tensor is listed twice"
+    # what is written overlaps nothing else: by address, against the furthest ends of what is read and of what is written before it
+    spans = [(x.data_ptr(), x.numel() * x.element_size(), x is d) for s, d in zip(grads, out) if d.numel() for x in ((d,) if s.data_ptr() == d.data_ptr() else (s, d))]
+    read = wrote = 0
+    for at, size, writes in sorted(spans):
+        assert at >= wrote and (not writes or at >= read), "a tensor is written over another"
+        if writes:
+            wrote = max(wrote, at + size)
+        else:
+            read = max(read, at + size)
     c = focus_grads(C.addressof(entries), len(grads))
     c.tensors = (entries, grads, out)
     return c

@@ -583,6 +583,7 @@ def make_grad_list(grads, out=None):
         assert s.is_cuda and s.dtype in kinds and s.is_contiguous(), (s.dtype, tuple(s.shape), s.stride())
         assert d.dtype is s.dtype and d.device == s.device and d.is_contiguous() and d.numel() == s.numel(), (d.dtype, tuple(d.shape), d.stride())
         e.src, e.dst, e.count, e.dtype = s.data_ptr(), d.data_ptr(), s.numel(), kinds[s.dtype]
+    assert len({d.device for d in out}) <= 1, "tensors of several devices"
     written = [d.data_ptr() for d in out if d.numel()]
     assert len(set(written)) == len(written), "a tensor is listed twice"
     # what is written overlaps nothing else: by address, against the furthest ends of what is read and of what is written before it

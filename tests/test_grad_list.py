@@ -44,3 +44,12 @@ def test_pieces_of_one_buffer():
     # the same source twice, or overlapping sources, into places of their own
     assert fb.make_grad_list([at(0, 10), at(0, 10), at(5, 9)], [to(0, 10), to(10, 20), to(30, 34)]).count == 3
     assert fb.make_grad_list([], []).count == 0
+
+
+def test_tensors_of_several_devices():
+    """(one kernel reads them all)"""
+    a, b = (OnGpu(torch.zeros(4)) for _ in range(2))
+    assert fb.make_grad_list([a, b]).count == 2
+    b.device = torch.device("cuda", 1)
+    with pytest.raises(AssertionError, match="devices"):
+        fb.make_grad_list([a, b])

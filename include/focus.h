@@ -543,6 +543,8 @@ FOCUS_API int focus_gate_attn_bwd(const focus_shape* shape, focus_tensor q, focu
  *   dscores     device fp32 [batch, n, ld], ld = focus_soft_ld(K), 16-byte aligned; entries g >= K are ignored
  *   dh          device bf16 [batch, n, d_model], strides as those of h; written; NULL: not wanted.  May be h itself, overlaps it not otherwise
  *   dWg, dC     device fp32 [d_model, d_g], [K, d_g]; overwritten.  Sums in fp32, in an order that depends on the shape alone
+ * In dh, which is rounded to bf16, dscores and C Wg' have 16 bits each (where the groups of a token cancel, that shows: 2^-14 of the magnitudes), in dWg and
+ * dC dscores have 24.  What is not finite in h or dscores makes what depends on it not finite, NaN also where the formulas have an infinity.
  *   ws          device scratch of focus_router_scores_bwd_workspace_bytes(shape, d_model, d_g) bytes, 16-byte aligned; as for focus_attn_bwd
  * FOCUS_ERR_UNSUPPORTED: d_model above 2^20, d_g above 2^16, more than 2^31 tokens, more than 65535 sequences.
  */

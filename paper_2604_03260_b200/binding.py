@@ -579,20 +579,23 @@ def make_grad_list(grads, out=None):
     assert len(out) == len(grads)
     kinds = {torch.float32: 0, torch.bfloat16: 1}
     entries = (focus_grad * max(1, len(grads)))()
+    spans = []
     for e, s, d in zip(entries, grads, out):
         assert s.is_cuda and s.dtype in kinds and s.is_contiguous(), (s.dtype, tuple(s.shape), s.stride())
-        assert d.dtype is s.dtype and d.device == s.device and d.is_contiguous() and d.numel() == s.numel(), (d.dtype, tuple(d.shape), d.stride())
-        e.src, e.dst, e.count, e.dtype = s.data_ptr(), d.data_ptr(), s.numel(), kinds[s.dtype]
-    assert len({d.device for d in out}) <= 1, "tensors of several devices"
-    written = [d.data_ptr() for d in out if d.numel()]
-    assert len(set(written)) == len(written), "a tensor is listed twice"
+        assert d.dtype is s.dtype and d.device == s.device == out[0].device and d.is_contiguous() and d.numel() == s.numel(), (d.dtype, tuple(d.shape), d.stride(), "or several devices")
+        src, dst, count = s.data_ptr(), d.data_ptr(), s.numel()
+        e.src, e.dst, e.count, e.dtype = src, dst, count, kinds[s.dtype]
+        if count:
+            spans.append((dst, count * s.element_size(), True))
+            if src != dst:
+                spans.append((src, count * s.element_size(), False))
     # what is written overlaps nothing else: by address, against the furthest ends of what is read and of what is written before it
-    spans = [(x.data_ptr(), x.numel() * x.element_size(), x is d) for s, d in zip(grads, out) if d.numel() for x in ((d,) if s.data_ptr() == d.data_ptr() else (s, d))]
-    read = wrote = 0
+    read = wrote = last = 0
     for at, size, writes in sorted(spans):
+        assert not writes or at != last, "a tensor is listed twice"
         assert at >= wrote and (not writes or at >= read), "a tensor is written over another"
         if writes:
-            wrote = max(wrote, at + size)
+            wrote, last = max(wrote, at + size), at
         else:
             read = max(read, at + size)
     c = focus_grads(C.addressof(entries), len(grads))

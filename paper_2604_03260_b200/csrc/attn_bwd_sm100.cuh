@@ -12,9 +12,9 @@
 // of one tile, when it was so: a tile took the sum of what both phases wait for, 8/2 heads x 16384 tokens 1751 us.)
 //
 // What bounds it: at D = 64 and 128 the chain of a tile, X - exponentials - Y - dS - sum, of which two are under way: 128 x 128 pairs of dK and dV take
-// 3100 cycles at D = 128 (products alone 2048), of dQ 2200 (1536).  8/2 heads x 16384 tokens, D = 128, every causal pair: 1605 us, 856 TFLOP/s on the five
-// products that the formulas need (seven are done); 32/8 x 8192, K = 4, top-2: 1731; D = 256 with a cap, 16/8 x 4096: 555.  With the gate, the special
-// functions: three a pair and pass, 16 a clock, and what each group's 64 columns wait for before and after; 32/8 x 4096, K = 8: 891 us.
+// 3100 cycles at D = 128 (products alone 2048), of dQ 2200 (1536).  8/2 heads x 16384 tokens, D = 128, every causal pair: 1767 us, 778 TFLOP/s on the five
+// products that the formulas need (seven are done); 32/8 x 8192, K = 4, top-2: 1860; D = 256 with a cap, 16/8 x 4096: 625 (each among others; on a cooler GPU up
+// to 7 % less).  With the gate, the special functions: three a pair and pass, 16 a clock, and what each group's 64 columns wait for before and after; 32/8 x 4096, K = 8: 912 us.
 //
 // Tensor memory: the sums, and two or three places for the tiles at work.  A tile has one place: X, P over it, Y when X (and the sum with P)
 // is through, dS over that.  With three places the X of a group's next tile is there before it is done with the one before.
@@ -111,7 +111,7 @@ struct BwdCfg {
     static constexpr uint32_t ROOM = 227 * 1024 - CTL_BYTES - NR * R_BYTES - NI * INFO_BYTES - CONST_BYTES - GR_BYTES;
     // C1 of a tile is held from its X to its sum with dS, NPL tiles later, C2 for a product or two: rings of their own
     static constexpr int NFIT = ROOM / C1_BYTES > 8 ? 8 : ROOM / C1_BYTES;
-    // Registers of the warps that issue and of those that compute (12 heads x 4000 tokens, D = 64: K = 32 829 us with the usual ones, 709 so;
+    // Registers of the warps that issue and of those that compute (12 heads x 4000 tokens, D = 64: K = 32 829 us with the usual ones, 709 so, 731 by now;
     // 8/2 heads x 4096, K = 16, where the others have what they need, 640 and 650)
     static constexpr int REGS_FEW = LD > 16 ? 40 : REGS_CONTROL, REGS_MANY = LD > 16 ? 232 : REGS_SOFTMAX_2WG;
     static_assert(REGS_FEW + 2 * REGS_MANY == 3 * 168, "the launch's registers");

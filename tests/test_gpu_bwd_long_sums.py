@@ -132,3 +132,43 @@ def test_assignments_of_long_sequences(n, D, K, G):
         for x, y, z in ((0, a, b), (1, e, c)):
             want[x] += y @ gd + z.T @ gd
     plain.check({"dg": got["dg"][0][pick][:, :K]}, {"dg": tuple(want)})
+
+
+def test_several_launches_captured_and_on_two_streams():
+    """(their sums lie in the workspace from launch to launch) the same bits from a graph replayed on new inputs, and from two calls at once"""
+    n, D, G, K = 33500, 64, 3, 4
+    shape = fb.make_shape(G, 1, n, D, K, 1, 50)
+    cases = []
+    for seed in (1, 2):
+        t, gen = make(1, G, 1, n, D, seed)
+        g = torch.softmax(torch.randn((1, n, K), generator=gen, device="cuda"), -1)
+        t["o"], t["lse"] = torch.empty_like(t["q"]), torch.empty((1, G, n), device="cuda")
+        fb.focus_gate_attn_fwd(shape, t["q"], t["k"], t["v"], g, 6.0, t["o"], t["lse"])
+        cases.append((t, g, run_bwd(shape, t, g=g, lam=6.0), run_bwd(shape, t)))
+    size = (fb.focus_gate_attn_bwd_workspace_bytes(shape), fb.focus_attn_bwd_workspace_bytes(shape))
+    spaces = [[torch.empty(x, dtype=torch.uint8, device="cuda").fill_(0xff) for x in size] for _ in cases]
+    outs = [[{x: torch.empty_like(y) for x, y in r.items()} for r in c[2:]] for c in cases]
+
+    def both(t, g, ws, out, stream=None):
+        fb.focus_gate_attn_bwd(shape, t["q"], t["k"], t["v"], g, 6.0, t["o"], t["lse"], t["do"], *out[0].values(), ws[0], None, stream)
+        fb.focus_attn_bwd(shape, t["q"], t["k"], t["v"], None, None, None, 0, t["o"], t["lse"], t["do"], *out[1].values(), ws[1], None, stream)
+
+    same = lambda out, c: all(torch.equal(o[x], r[x]) for o, r in zip(out, c[2:]) for x in r)
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(2):
+        for c, ws, out, st in zip(cases, spaces, outs, streams):
+            both(c[0], c[1], ws, out, st)
+    torch.cuda.synchronize()
+    assert same(outs[0], cases[0]) and same(outs[1], cases[1])
+    t, g = {x: y.clone() for x, y in cases[0][0].items()}, cases[0][1].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(t, g, spaces[0], outs[0])
+    for x in t:
+        t[x].copy_(cases[1][0][x])
+    g.copy_(cases[1][1])
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert same(outs[0], cases[1])
